@@ -408,6 +408,107 @@ tt_status tt_index_graph_edges(const int64_t *indices, const int64_t *offsets, i
                                int32_t *edge_v, int32_t *edge_w, int32_t *counts, void *stream);
 
 /*
+ * Dense side.  What a model does with pooled rows right behind the bags, and how cores and dense weights
+ * are updated by their orthogonalised gradients.  These calls take fp32, bf16 or fp16 data; sums are fp32
+ * on the matrix cores and reproducible (no atomics); they allocate nothing and follow the conventions above.
+ */
+typedef enum { TT_F32 = 0, TT_BF16 = 1, TT_F16 = 2 } tt_dtype;
+typedef enum {
+  TT_ACT_NONE = 0,
+  TT_ACT_RELU = 1,   /* z <= 0 ? 0 : z, slope 0 at 0                                            */
+  TT_ACT_GELU = 2,   /* z Phi(z), with the normal distribution's Phi                            */
+  TT_ACT_SILU = 3,   /* z / (1 + exp(-z))                                                       */
+  TT_ACT_SIGMOID = 4 /* 1 / (1 + exp(-z))                                                       */
+} tt_activation;
+
+/*
+ * The product of rows with a weight, its epilogue and its gradients:
+ *   z = x W^T + bias,  out = act(z) + residual       x [rows][in_dim], W [out_dim][in_dim]
+ *   groups == 0: one W and one bias [out_dim] for all rows.
+ *   groups >= 1: W [groups][out_dim][in_dim], bias [groups][out_dim]; group g's are used for the rows
+ *     [offsets[g], offsets[g+1]) -- the tables of a fused table (their bags follow each other in `out` of
+ *     the bag calls), or the experts of a router.  Groups may be empty.  Offsets are read on the device
+ *     only and need no order: each is clamped to [0, rows] and counts at least as much as those
+ *     before it.  Rows before offsets[0] and behind offsets[groups] belong to no group: in `out`, `pre` and
+ *     `dx` they are left as they were (zero_rest: cleared in `out` and `dx`), and no gradient gets anything from them.
+ * HOST struct, read during the call only.
+ */
+#define TT_DENSE_MAX_DIM (1 << 20)
+#define TT_DENSE_MAX_GROUPS 65536
+typedef struct {
+  int32_t dtype;       /* tt_dtype of every tensor of the call                                   */
+  int32_t activation;  /* tt_activation                                                          */
+  int64_t rows;        /* rows of x, fewer than 2^31 - 2^17 - 1                                  */
+  int32_t in_dim, out_dim; /* 1 .. TT_DENSE_MAX_DIM                                              */
+  int32_t groups;      /* 0, or 1 .. TT_DENSE_MAX_GROUPS                                         */
+  int32_t zero_rest;   /* rows of no group: 0 left as they were, 1 cleared                       */
+  const int64_t *offsets; /* DEVICE int64[groups + 1]; NULL if groups == 0                       */
+  int64_t ld_x;        /* elements between rows of x; 0: in_dim                                  */
+  int64_t ld_out;      /* ... of out; 0: out_dim                                                 */
+  int64_t ld_residual; /* ... of residual; 0: out_dim                                            */
+  int64_t ld_grad;     /* ... of grad_out; 0: out_dim                                            */
+  int64_t ld_dx;       /* ... of dx; 0: in_dim                                                   */
+} tt_dense;
+
+/*
+ * Forward.  bias and residual may be NULL.  pre (nullable) receives z, [rows][out_dim] packed, rounded to
+ * the dtype (in fp16 a z that would round to zero keeps its sign as the smallest number): what
+ * tt_dense_backward needs if there is an activation.  out may be the residual's own memory with the same
+ * row step; otherwise outputs overlap nothing.  Tensors need the alignment of an element only.
+ *   workspace  DEVICE, 256-byte aligned, tt_dense_workspace_bytes(op, 0) bytes (NULL if that is 0), borrowed
+ *              until the work has finished: calls that may overlap need one each.
+ * Backward, from grad_out = dL/d out:
+ *   dz = grad_out act'(z), dx = dz W, dW = dz^T x (per group, zeros for an empty one), dbias = sums of dz;
+ *   any of dx, dw, dbias may be NULL.  dL/d residual is grad_out itself.  dz is rounded to the dtype
+ *   before the products.  x is needed for dw, w for dx, pre if there is an activation.
+ *   workspace  tt_dense_workspace_bytes(op, 1) bytes, as above.
+ * tt_dense_workspace_bytes returns 0 on invalid arguments too.
+ */
+size_t tt_dense_workspace_bytes(const tt_dense *op, int backward);
+tt_status tt_dense_forward(const tt_dense *op, const void *x, const void *w, const void *bias, const void *residual,
+                           void *out, void *pre, void *workspace, size_t workspace_bytes, void *stream);
+tt_status tt_dense_backward(const tt_dense *op, const void *x, const void *w, const void *pre, const void *grad_out,
+                            void *dx, void *dw, void *dbias, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Orthogonalised updates (Newton-Schulz products, as the Muon optimiser takes them): for each matrix G of
+ * a batch
+ *   X = G / (|G| + eps) with the Frobenius norm;  for each step, with its coefficients (a, b, c):
+ *   X <- a X + (b A + c A^2) X,  A = X X^T           (a tall X from the other side: the same polynomial)
+ * which takes every singular value s to a s + b s^3 + c s^5, step after step.  fp32 arithmetic whatever the
+ * dtype (norms in 64 bits), the result rounded once.  A zero matrix gives zeros; one with an infinity or
+ * a NaN gives NaN in all its entries and does not touch the others of the batch.
+ *   coefficients HOST float[steps][3], finite; steps 1 .. TT_ORTHO_MAX_STEPS; eps >= 0
+ *   g, out       DEVICE; out may be g itself (with the same steps).
+ *   workspace    DEVICE, 256-byte aligned, tt_orthogonalize_workspace_bytes(m) (0 on invalid arguments)
+ */
+#define TT_ORTHO_MAX_STEPS 32
+#define TT_ORTHO_MAX_SIDE (1 << 20)
+typedef struct {
+  int32_t dtype;              /* tt_dtype of g and out                                           */
+  int64_t batch, rows, cols;  /* sides 1 .. TT_ORTHO_MAX_SIDE, batch * rows * cols < 2^36        */
+  int64_t batch_step, row_step;         /* elements between matrices / rows of g; 0: packed       */
+  int64_t out_batch_step, out_row_step; /* ... of out                                            */
+} tt_matrices;
+size_t tt_orthogonalize_workspace_bytes(const tt_matrices *m);
+tt_status tt_orthogonalize(const tt_matrices *m, const void *g, void *out, int steps, const float *coefficients,
+                           float eps, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * The core update that goes with it, beside tt_core_sgd_update: with momentum, slice by slice,
+ *   m <- mu m + dG,  u = nesterov ? dG + mu m : m,
+ *   G <- G - lr sqrt(max(1, rows / cols)) ortho(u)   for each slice G of each core,
+ * the slices being the matrices that multiply in a row of the table: G1[i1] d1 x R1, G2[i2] R1 x (d2 R2),
+ * G3[i3] R2 x d3.  A slice whose u is zero stays as it is.  table->core[] and momentum[] are updated in place.
+ *   dcore, momentum  HOST arrays of 3 DEVICE pointers, core-shaped
+ *   workspace        DEVICE, 256-byte aligned, tt_core_ortho_workspace_bytes(table) (0 on invalid arguments)
+ */
+size_t tt_core_ortho_workspace_bytes(const tt_table *table);
+tt_status tt_core_ortho_update(const tt_table *table, const float *const dcore[3], float *const momentum[3], float lr,
+                               float mu, int nesterov, int steps, const float *coefficients, float eps,
+                               void *workspace, size_t workspace_bytes, void *stream);
+
+/*
  * Waits for `stream`, copies the plan's device-side counters to the host and
  * reports deferred errors.  counts_out (HOST, nullable) receives
  * {U_r, U_p, valid lookups, status bits}.  Returns TT_ERR_INDEX_RANGE if any

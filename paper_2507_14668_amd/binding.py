@@ -29,7 +29,9 @@ EXPORTS = ("tt_workspace_bytes", "tt_index_reorder", "tt_emb_bag_forward", "tt_e
            "tt_forward_bf16_direct_pays", "tt_emb_bag_forward_bf16_direct",
            "tt_index_graph_workspace_bytes", "tt_index_graph_edges", "tt_fuse_shape", "tt_fuse_lookups", "tt_fuse_lookups_starts", "tt_plan_status", "tt_strerror", "tt_prof_create", "tt_prof_destroy",
            "tt_prof_collect", "tt_kernel_name", "tt_batch_desc_bytes", "tt_index_reorder_batched",
-           "tt_emb_bag_forward_batched", "tt_emb_bag_backward_batched", "tt_core_sgd_update_batched")
+           "tt_emb_bag_forward_batched", "tt_emb_bag_backward_batched", "tt_core_sgd_update_batched",
+           "tt_dense_workspace_bytes", "tt_dense_forward", "tt_dense_backward", "tt_orthogonalize_workspace_bytes", "tt_orthogonalize",
+           "tt_core_ortho_workspace_bytes", "tt_core_ortho_update")
 KERNELS = {"fwd_contract": 0, "bag_sum": 1, "grad_merge": 2, "bwd_contract": 3, "sort_scatter": 4, "sgd": 5,
            "p12_fill": 6, "bag_chains": 7}
 
@@ -76,6 +78,19 @@ TT_FUSE_MAX_TABLES = 32
 class CFuseMembers(ctypes.Structure):
     _fields_ = [("num_tables", ctypes.c_int32), ("n", (ctypes.c_int32 * 3) * TT_FUSE_MAX_TABLES),
                 ("num_rows", ctypes.c_int64 * TT_FUSE_MAX_TABLES)]
+
+
+class CDense(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("activation", ctypes.c_int32), ("rows", ctypes.c_int64), ("in_dim", ctypes.c_int32),
+                ("out_dim", ctypes.c_int32), ("groups", ctypes.c_int32), ("zero_rest", ctypes.c_int32), ("offsets", ctypes.c_void_p),
+                ("ld_x", ctypes.c_int64), ("ld_out", ctypes.c_int64), ("ld_residual", ctypes.c_int64), ("ld_grad", ctypes.c_int64),
+                ("ld_dx", ctypes.c_int64)]
+
+
+class CMatrices(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("batch", ctypes.c_int64), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64),
+                ("batch_step", ctypes.c_int64), ("row_step", ctypes.c_int64), ("out_batch_step", ctypes.c_int64),
+                ("out_row_step", ctypes.c_int64)]
 
 
 _lib = None
@@ -149,6 +164,21 @@ def load_library():
             f.argtypes = [ctypes.c_int, vp, vp, ctypes.c_size_t, vp]
         lib.tt_core_sgd_update_batched.restype = ctypes.c_int
         lib.tt_core_sgd_update_batched.argtypes = [ctypes.c_int, vp, f32, vp, ctypes.c_size_t, vp]
+        sz = ctypes.c_size_t
+        lib.tt_dense_workspace_bytes.restype = sz
+        lib.tt_dense_workspace_bytes.argtypes = [vp, ctypes.c_int]
+        lib.tt_dense_forward.restype = ctypes.c_int
+        lib.tt_dense_forward.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        lib.tt_dense_backward.restype = ctypes.c_int
+        lib.tt_dense_backward.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        lib.tt_orthogonalize_workspace_bytes.restype = sz
+        lib.tt_orthogonalize_workspace_bytes.argtypes = [vp]
+        lib.tt_orthogonalize.restype = ctypes.c_int
+        lib.tt_orthogonalize.argtypes = [vp, vp, vp, ctypes.c_int, vp, f32, vp, sz, vp]
+        lib.tt_core_ortho_workspace_bytes.restype = sz
+        lib.tt_core_ortho_workspace_bytes.argtypes = [vp]
+        lib.tt_core_ortho_update.restype = ctypes.c_int
+        lib.tt_core_ortho_update.argtypes = [vp, vp, vp, f32, f32, ctypes.c_int, ctypes.c_int, vp, f32, vp, sz, vp]
         _lib = lib
     return _lib
 
@@ -563,6 +593,227 @@ def fusion_groups(members, groups=None, max_factor_sum=1023):
                 raise ValueError("no fusion of these tables fits the limits")
             return [p for p in parts if p]  # largest member first: its long-running workgroups start early
         g += 1
+
+
+# ------------------------------------------------------------------ dense side
+DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3, "sigmoid": 4}
+# the Muon optimiser's coefficients (K. Jordan and others, 2024): steep at zero, so that five steps do
+ORTHO_COEFFICIENTS = (3.4445, -4.7750, 2.0315)
+
+
+class _On:
+    """The tensors' device as the current one, and the work's stream on it."""
+
+    def __init__(self, tensors, stream):
+        self.device = tensors[0].device
+        for t in tensors:
+            if t.device != self.device:
+                raise ValueError("tensors on %s and %s in one call" % (self.device, t.device))
+        if stream is not None and stream.device != self.device:
+            raise ValueError("the stream is on %s, the tensors are on %s" % (stream.device, self.device))
+        self.stream = stream
+
+    def __enter__(self):
+        self.before = torch._C._cuda_getDevice()
+        if self.device.index != self.before:
+            torch.cuda.set_device(self.device.index)
+        return _stream(self.stream)
+
+    def __exit__(self, *exc):
+        if self.device.index != self.before:
+            torch.cuda.set_device(self.before)
+        return False
+
+    def empty(self, shape, dtype):
+        """Memory for this call: freed early or late, it is not handed out again before the call's stream is done with it."""
+        t = torch.empty(shape, dtype=dtype, device=self.device)
+        if self.stream is not None:
+            t.record_stream(self.stream)
+        return t
+
+
+def _rows_of(t, name, dtype, rows, cols):
+    """The row step of a [rows, cols] device tensor whose columns are neighbours."""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == dtype):
+        raise TypeError("%s must be a CUDA tensor of %s" % (name, dtype))
+    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
+        raise ValueError("%s must be [%d, %d], got %s" % (name, rows, cols, tuple(t.shape)))
+    if rows == 0:
+        return cols
+    if cols > 1 and t.stride(1) != 1:
+        raise ValueError("the columns of %s must be contiguous" % name)
+    if rows > 1 and t.stride(0) < cols:
+        raise ValueError("the rows of %s must not overlap" % name)
+    return max(cols, t.stride(0))
+
+
+def _packed(t, name, dtype, shape):
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == dtype and t.is_contiguous()):
+        raise TypeError("%s must be a contiguous CUDA tensor of %s" % (name, dtype))
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError("%s must be %s, got %s" % (name, list(shape), list(t.shape)))
+    return t
+
+
+def _dense_op(x, w, activation, offsets):
+    if not (isinstance(x, torch.Tensor) and x.is_cuda and x.dtype in DTYPES):
+        raise TypeError("x must be a CUDA tensor of float32, bfloat16 or float16")
+    if activation not in ACTIVATIONS:
+        raise ValueError("activation is one of %s" % ", ".join(ACTIVATIONS))
+    grouped = offsets is not None
+    if w.dim() != (3 if grouped else 2):
+        raise ValueError("w must be [groups, out, in] with offsets, [out, in] without")
+    if x.dim() != 2 or x.shape[1] != w.shape[-1]:
+        raise ValueError("x must be [rows, %d], got %s" % (w.shape[-1], tuple(x.shape)))
+    op = CDense()
+    op.dtype, op.activation = DTYPES[x.dtype], ACTIVATIONS[activation]
+    op.rows, op.in_dim, op.out_dim = x.shape[0], w.shape[-1], w.shape[-2]
+    _packed(w, "w", x.dtype, w.shape)
+    if grouped:
+        _dev_i64(offsets, "offsets")
+        if offsets.dim() != 1 or offsets.numel() != w.shape[0] + 1:
+            raise ValueError("offsets must hold groups + 1 = %d row numbers" % (w.shape[0] + 1))
+        op.groups, op.offsets = w.shape[0], offsets.data_ptr()
+    op.ld_x = _rows_of(x, "x", x.dtype, x.shape[0], x.shape[1])
+    return op
+
+
+def _dense_workspace(op, backward, on, workspace):
+    need = int(load_library().tt_dense_workspace_bytes(ctypes.byref(op), int(backward)))
+    if workspace is None:
+        workspace = on.empty(need, torch.uint8) if need else None
+    elif not (workspace.is_cuda and workspace.dtype == torch.uint8 and workspace.is_contiguous()):
+        raise TypeError("workspace must be a contiguous CUDA uint8 tensor")
+    return workspace, 0 if workspace is None else workspace.numel()
+
+
+def tt_dense_workspace_bytes(x, w, activation="none", offsets=None, backward=False) -> int:
+    """Bytes of workspace the calls below take for these operands (they allocate it if none is given)."""
+    return int(load_library().tt_dense_workspace_bytes(ctypes.byref(_dense_op(x, w, activation, offsets)), int(backward)))
+
+
+def tt_dense_forward(x, w, bias=None, residual=None, activation="none", offsets=None, out=None, pre=None, workspace=None, stream=None):
+    """`act(x w^T + bias) + residual`, of x [rows, in] and w [out, in]; with `offsets` (int64 [groups + 1], on the device) of w
+    [groups, out, in] and bias [groups, out], group g's for the rows offsets[g] .. offsets[g + 1].  One dtype throughout (float32,
+    bfloat16 or float16); x, residual and out may be views into wider rows.  `pre` (packed, [rows, out]) receives the
+    pre-activation that `tt_dense_backward` takes.  Rows of no group are left as they were in a given `out`, zeros in a new one."""
+    op = _dense_op(x, w, activation, offsets)
+    rows, n = op.rows, op.out_dim
+    given = [t for t in (x, w, bias, residual, offsets, out, pre, workspace) if t is not None]
+    on = _On(given, stream)
+    if bias is not None:
+        _packed(bias, "bias", x.dtype, w.shape[:-1])
+    if residual is not None:
+        op.ld_residual = _rows_of(residual, "residual", x.dtype, rows, n)
+    if pre is not None:
+        _packed(pre, "pre", x.dtype, (rows, n))
+    if out is None:
+        out = on.empty((rows, n), x.dtype)
+        op.zero_rest = 1
+    op.ld_out = _rows_of(out, "out", x.dtype, rows, n)
+    workspace, size = _dense_workspace(op, False, on, workspace)
+    with on as s:
+        st = load_library().tt_dense_forward(ctypes.byref(op), _ptr(x), _ptr(w), _ptr(bias), _ptr(residual), _ptr(out), _ptr(pre), _ptr(workspace), size, s)
+    _check(st, "tt_dense_forward")
+    return out
+
+
+def tt_dense_backward(x, w, grad_out, pre=None, activation="none", offsets=None, needs=(True, True, True), workspace=None, stream=None):
+    """Gradients `(dx, dw, dbias)` of `tt_dense_forward` from grad_out [rows, out] (None where `needs` says so); the residual's
+    is grad_out itself.  With an activation `pre` is what the forward stored.  Rows of no group get zeros in dx."""
+    op = _dense_op(x, w, activation, offsets)
+    rows, n, k = op.rows, op.out_dim, op.in_dim
+    given = [t for t in (x, w, grad_out, pre, offsets, workspace) if t is not None]
+    on = _On(given, stream)
+    op.ld_grad = _rows_of(grad_out, "grad_out", x.dtype, rows, n)
+    if activation != "none":
+        if pre is None:
+            raise ValueError("the gradient of an activation needs the pre-activation")
+        _packed(pre, "pre", x.dtype, (rows, n))
+    dx = on.empty((rows, k), x.dtype) if needs[0] else None
+    dw = on.empty(tuple(w.shape), x.dtype) if needs[1] else None
+    db = on.empty(tuple(w.shape[:-1]), x.dtype) if needs[2] else None
+    op.zero_rest = 1
+    workspace, size = _dense_workspace(op, True, on, workspace)
+    with on as s:
+        st = load_library().tt_dense_backward(ctypes.byref(op), _ptr(x), _ptr(w), _ptr(pre), _ptr(grad_out), _ptr(dx), _ptr(dw), _ptr(db), _ptr(workspace), size, s)
+    _check(st, "tt_dense_backward")
+    return dx, dw, db
+
+
+def _coefficients(steps, coefficients):
+    steps = int(steps)
+    c = [float(v) for v in torch.as_tensor(coefficients, dtype=torch.float64).reshape(-1).tolist()]
+    if len(c) == 3:
+        c = c * steps
+    if steps < 1 or len(c) != 3 * steps:
+        raise ValueError("coefficients: one (a, b, c) for all steps, or one for each")
+    return (ctypes.c_float * len(c))(*c)
+
+
+def tt_orthogonalize(g, steps=5, coefficients=ORTHO_COEFFICIENTS, eps=1e-7, out=None, workspace=None, stream=None):
+    """The matrices of g [rows, cols] or [batch, rows, cols] with their singular values taken towards one by Newton-Schulz steps
+    (include/tt_emb.h has the formulas).  `coefficients`: one (a, b, c) for all steps or one for each.  Matrices may be views
+    whose columns are neighbours; `out` may be g."""
+    if not (isinstance(g, torch.Tensor) and g.is_cuda and g.dtype in DTYPES):
+        raise TypeError("g must be a CUDA tensor of float32, bfloat16 or float16")
+    if g.dim() not in (2, 3) or g.shape[-1] < 1 or g.shape[-2] < 1:
+        raise ValueError("g must be [rows, cols] or [batch, rows, cols]")
+    coef = _coefficients(steps, coefficients)
+    on = _On([t for t in (g, out, workspace) if t is not None], stream)
+    if out is None:
+        out = on.empty(tuple(g.shape), g.dtype)
+    if out.shape != g.shape or out.dtype != g.dtype:
+        raise ValueError("out must have the shape and dtype of g")
+    m = CMatrices()
+    m.dtype, m.batch, m.rows, m.cols = DTYPES[g.dtype], g.shape[0] if g.dim() == 3 else 1, g.shape[-2], g.shape[-1]
+    for name, t in (("g", g), ("out", out)):
+        if (m.cols > 1 and t.stride(-1) != 1) or (m.rows > 1 and t.stride(-2) < m.cols):
+            raise ValueError("the rows of %s must be contiguous and must not overlap" % name)
+        row = t.stride(-2) if m.rows > 1 else m.cols
+        size = row * (m.rows - 1) + m.cols
+        step = t.stride(0) if t.dim() == 3 and m.batch > 1 else size
+        if step < size:
+            raise ValueError("the matrices of %s must not overlap" % name)
+        if name == "g":
+            m.row_step, m.batch_step = row, step
+        else:
+            m.out_row_step, m.out_batch_step = row, step
+    lib = load_library()
+    need = int(lib.tt_orthogonalize_workspace_bytes(ctypes.byref(m)))
+    if need == 0:
+        raise TTError(TT_ERR_SHAPE, "tt_orthogonalize_workspace_bytes")
+    if workspace is None:
+        workspace = on.empty(need, torch.uint8)
+    with on as s:
+        st = lib.tt_orthogonalize(ctypes.byref(m), _ptr(g), _ptr(out), int(steps), coef, ctypes.c_float(eps), _ptr(workspace), workspace.numel(), s)
+    _check(st, "tt_orthogonalize")
+    return out
+
+
+def tt_core_ortho_update(table: Table, dcores, momenta, lr: float, momentum=0.95, nesterov=True, steps=5, coefficients=ORTHO_COEFFICIENTS,
+                         eps=1e-7, workspace=None, stream=None):
+    """Momentum, then every slice of every core by its orthogonalised momentum: cores and momenta are updated in place."""
+    coef = _coefficients(steps, coefficients)
+    for ts, name in ((dcores, "dcore"), (momenta, "momentum")):
+        if len(ts) != 3:
+            raise ValueError("three tensors of %s, one a core" % name)
+        for t, c in zip(ts, table.cores):
+            if _dev_f32(t, name).numel() != c.numel():
+                raise ValueError("%s must have the core's size" % name)
+    on = _On(list(table.cores) + list(dcores) + list(momenta) + ([workspace] if workspace is not None else []), stream)
+    lib = load_library()
+    if workspace is None:
+        need = int(lib.tt_core_ortho_workspace_bytes(ctypes.byref(table.c)))
+        if need == 0:
+            raise TTError(TT_ERR_SHAPE, "tt_core_ortho_workspace_bytes")
+        workspace = on.empty(need, torch.uint8)
+    ptrs = lambda ts: (ctypes.c_void_p * 3)(*[t.data_ptr() for t in ts])
+    with on as s:
+        st = lib.tt_core_ortho_update(ctypes.byref(table.c), ptrs(dcores), ptrs(momenta), ctypes.c_float(lr), ctypes.c_float(momentum), int(bool(nesterov)),
+                                      int(steps), coef, ctypes.c_float(eps), _ptr(workspace), workspace.numel(), s)
+    _check(st, "tt_core_ortho_update")
 
 
 # ------------------------------------------------------------------ batched calls

@@ -1,0 +1,37 @@
+// Matrix products with an epilogue, shared by the dense operators (tt_dense.hip) and the orthogonalised update
+// (tt_ortho.hip).  Internal; the C ABI is include/tt_emb.h.
+//
+//   out[m][n] = act(alpha * sum_k A(m, k) B(n, k) + bias[n]) + beta * res[m][n]
+//
+// An operand is stored either K-contiguous, [row][k], or row-contiguous, [k][row]; `lda` / `ldb` are the elements between
+// two stored rows.  One description covers one product, a batch at a fixed step, and groups of rows given by offsets.
+#pragma once
+
+#include "tt_internal.h"
+
+#define TT_GEMM_BATCH 0     // member z at z * step of every operand
+#define TT_GEMM_RAGGED_M 1  // rows [start(z), end(z)) of A, res and out belong to group z, whose B and bias are at z * step
+#define TT_GEMM_RAGGED_K 2  // group z sums over the stored rows [start(z), end(z)) of A and B; its out is at z * step
+
+struct TTGemm {
+  int dtype, out_dtype;        // of the operands, bias, res; of out
+  int a_kc, b_kc;              // 1: K-contiguous
+  int mode;
+  const void *a, *b;
+  void *out;
+  long long lda, ldb, ldo, a_step, b_step, o_step;
+  int M, N, K;                 // RAGGED_M: M rows in all; RAGGED_K: K stored rows in all
+  int batch;                   // members or groups
+  const int64_t *offsets;      // DEVICE [batch + 1], ragged modes
+  int zero_rest;               // RAGGED_M: rows of out outside every group are cleared (else left as they were)
+  const void *bias;            // [N], nullable
+  const void *res;             // nullable
+  void *pre;                   // nullable: alpha * sum + bias, rounded, [M][N]
+  void *rowsum;                // nullable, RAGGED_K and BATCH: sum_k A(m, k), [M] per member
+  long long bias_step, ldr, r_step, ldp, p_step, rs_step;
+  int act;
+  float alpha, beta;
+};
+
+// Enqueues the product.
+tt_status ttk_gemm(const TTGemm &g, hipStream_t s);

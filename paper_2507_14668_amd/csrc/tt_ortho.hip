@@ -1,0 +1,276 @@
+// Orthogonalised updates: X = G / (|G| + eps), then X <- a X + (b A + c A^2) X with A = X X^T, some steps of it
+// (Newton-Schulz: an odd polynomial of X that takes its singular values towards one), for a batch of matrices; and the
+// update of the TT cores by it, slice by slice, with momentum.
+#include <math.h>
+#include <string.h>
+
+#include "tt_gemm_device.h"
+
+namespace {
+using namespace ttg;
+
+size_t pad256(size_t n) { return (n + 255) & ~(size_t)255; }
+
+struct Steps {
+  int n;
+  const float *c;  // HOST [n][3]
+};
+struct Mats {
+  long long batch;
+  int rows, cols;
+  long long b_step, r_step;
+};
+
+// ---- norm and scaling ------------------------------------------------------------------------------
+// Sums of squares in 64 bits: neither 1e-25 nor 1e25 leaves the range, and the scale is not what limits the result.
+constexpr int kMaxParts = 64;
+int parts_of(long long elems) {
+  long long p = (elems + 8191) / 8192;
+  return (int)(p < 1 ? 1 : p > kMaxParts ? kMaxParts : p);
+}
+
+template <class T>
+__global__ void __launch_bounds__(TT_BLOCK) k_sum_squares(const T *__restrict__ g, Mats m, int parts, double *__restrict__ partial) {
+  const long long z = blockIdx.x / (unsigned)parts;
+  const int p = (int)(blockIdx.x % (unsigned)parts);
+  const long long elems = (long long)m.rows * m.cols;
+  double s = 0;
+  for (long long e = (long long)p * TT_BLOCK + threadIdx.x; e < elems; e += (long long)parts * TT_BLOCK) {
+    const long long r = e / m.cols;
+    const double v = (double)to_f32(g[z * m.b_step + r * m.r_step + (e - r * m.cols)]);
+    s += v * v;
+  }
+  __shared__ double red[TT_BLOCK];
+  red[threadIdx.x] = s;
+  __syncthreads();
+  for (int o = TT_BLOCK / 2; o > 0; o >>= 1) {
+    if (threadIdx.x < o) red[threadIdx.x] += red[threadIdx.x + o];
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) partial[z * parts + p] = red[0];
+}
+
+// x = g * s in fp32, packed.  A matrix whose squares do not sum to a number is NaN as a whole.
+template <class T>
+__global__ void __launch_bounds__(TT_BLOCK) k_scale_in(const T *__restrict__ g, Mats m, int parts, const double *__restrict__ partial, float eps,
+                                                       float *__restrict__ x) {
+  const long long z = blockIdx.x / (unsigned)parts;
+  const int p = (int)(blockIdx.x % (unsigned)parts);
+  const long long elems = (long long)m.rows * m.cols;
+  double sum = 0;
+  for (int i = 0; i < parts; ++i) sum += partial[z * parts + i];
+  double scale = 1.0 / (sqrt(sum) + (double)eps);
+  if (!(sum <= 1.7976931348623157e308)) scale = (double)NAN;
+  for (long long e = (long long)p * TT_BLOCK + threadIdx.x; e < elems; e += (long long)parts * TT_BLOCK) {
+    const long long r = e / m.cols;
+    x[z * elems + e] = (float)((double)to_f32(g[z * m.b_step + r * m.r_step + (e - r * m.cols)]) * scale);
+  }
+}
+
+struct Scratch {
+  size_t partial, x0, x1, a, b, total;
+};
+Scratch scratch(long long batch, long long rows, long long cols) {
+  Scratch w;
+  const long long elems = rows * cols, m = rows < cols ? rows : cols;
+  w.partial = 0;
+  w.x0 = pad256((size_t)batch * parts_of(elems) * 8);
+  w.x1 = w.x0 + pad256((size_t)batch * elems * 4);
+  w.a = w.x1 + pad256((size_t)batch * elems * 4);
+  w.b = w.a + pad256((size_t)batch * m * m * 4);
+  w.total = w.b + pad256((size_t)batch * m * m * 4);
+  return w;
+}
+
+template <class T>
+tt_status scale_in(const void *g, const Mats &m, float eps, char *ws, const Scratch &w, hipStream_t s) {
+  const int parts = parts_of((long long)m.rows * m.cols);
+  const unsigned blocks = (unsigned)(m.batch * parts);
+  hipLaunchKernelGGL(k_sum_squares<T>, dim3(blocks), dim3(TT_BLOCK), 0, s, (const T *)g, m, parts, (double *)(ws + w.partial));
+  hipLaunchKernelGGL(k_scale_in<T>, dim3(blocks), dim3(TT_BLOCK), 0, s, (const T *)g, m, parts, (const double *)(ws + w.partial), eps,
+                     (float *)(ws + w.x0));
+  return tt_launch_status();
+}
+
+// The iteration, all in fp32 (the polynomial takes small singular values up 485 times in five steps, and with them the rounding
+// errors that they carry).
+tt_status iterate(const Mats &m, const Steps &steps, int out_dtype, void *out, long long o_step, long long ldo, char *ws, const Scratch &w,
+                  hipStream_t s) {
+  const bool tall = m.rows > m.cols;
+  const int side = tall ? m.cols : m.rows;
+  const long long elems = (long long)m.rows * m.cols, sq = (long long)side * side;
+  float *x = (float *)(ws + w.x0), *y = (float *)(ws + w.x1), *A = (float *)(ws + w.a), *B = (float *)(ws + w.b);
+  for (int i = 0; i < steps.n; ++i) {
+    const float ca = steps.c[3 * i], cb = steps.c[3 * i + 1], cc = steps.c[3 * i + 2];
+    TTGemm g;
+    memset(&g, 0, sizeof(g));
+    g.dtype = g.out_dtype = TT_F32;
+    g.mode = TT_GEMM_BATCH;
+    g.batch = (int)m.batch;
+    g.alpha = 1.f;
+    // A = X X^T, or X^T X
+    g.a_kc = g.b_kc = tall ? 0 : 1;
+    g.M = g.N = side; g.K = tall ? m.rows : m.cols;
+    g.a = g.b = x; g.lda = g.ldb = m.cols; g.a_step = g.b_step = elems;
+    g.out = A; g.ldo = side; g.o_step = sq;
+    tt_status st = ttk_gemm(g, s);
+    if (st != TT_OK) return st;
+    // B = b A + c A A (A is symmetric)
+    g.a_kc = g.b_kc = 1;
+    g.K = side;
+    g.a = g.b = A; g.lda = g.ldb = side; g.a_step = g.b_step = sq;
+    g.out = B;
+    g.res = A; g.ldr = side; g.r_step = sq;
+    g.alpha = cc; g.beta = cb;
+    st = ttk_gemm(g, s);
+    if (st != TT_OK) return st;
+    // X <- a X + B X, or a X + X B (B is symmetric)
+    const bool last = i + 1 == steps.n;
+    g.M = m.rows; g.N = m.cols;
+    g.a = tall ? x : B; g.lda = side; g.a_step = tall ? elems : sq;
+    g.b = tall ? B : x; g.ldb = m.cols; g.b_step = tall ? sq : elems;
+    g.b_kc = tall ? 1 : 0;
+    g.res = x; g.ldr = m.cols; g.r_step = elems;
+    g.alpha = 1.f; g.beta = ca;
+    g.out = last ? out : (void *)y; g.ldo = last ? ldo : m.cols; g.o_step = last ? o_step : elems;
+    g.out_dtype = last ? out_dtype : TT_F32;
+    st = ttk_gemm(g, s);
+    if (st != TT_OK) return st;
+    float *t = x; x = y; y = t;
+  }
+  return TT_OK;
+}
+
+bool steps_ok(int steps, const float *coefficients, float eps) {
+  if (steps < 1 || steps > TT_ORTHO_MAX_STEPS || !coefficients || !(eps >= 0.f)) return false;
+  for (int i = 0; i < 3 * steps; ++i)
+    if (!isfinite(coefficients[i])) return false;
+  return true;
+}
+bool size_ok(int64_t batch, int64_t rows, int64_t cols) {
+  if (rows < 1 || cols < 1 || rows > TT_ORTHO_MAX_SIDE || cols > TT_ORTHO_MAX_SIDE) return false;
+  const int64_t side = rows < cols ? rows : cols;
+  // the largest launch is that of 64 x 64 tiles of the matrices
+  return batch >= 0 && batch * (rows * cols) < ((int64_t)1 << 36) && batch * (side * side) < ((int64_t)1 << 36) &&
+         batch * tt_ceil_div(rows, 64) * tt_ceil_div(cols, 64) <= TT_MAX_WORKGROUPS && batch * kMaxParts <= TT_MAX_WORKGROUPS;
+}
+
+// ---- TT cores --------------------------------------------------------------------------------------
+// Core k is [r][n][d r'] in memory; its slices i are r x (d r') matrices (core 0: d x r').  Packed: [i][r][d r'].
+struct CoreDims {
+  int r, n, c;  // stored order [r][n][c]
+};
+__device__ __forceinline__ long long packed_of(const CoreDims &d, long long e) {
+  const long long row = e / d.c;  // r index * n + i
+  const int a = (int)(row / d.n);
+  return ((row - (long long)a * d.n) * d.r + a) * d.c + (e - row * d.c);
+}
+__global__ void __launch_bounds__(TT_BLOCK) k_core_momentum(CoreDims d, const float *__restrict__ grad, float *__restrict__ mom, float mu, int nesterov,
+                                                            float *__restrict__ packed) {
+  const long long total = (long long)d.r * d.n * d.c, stride = (long long)gridDim.x * blockDim.x;
+  for (long long e = (long long)blockIdx.x * blockDim.x + threadIdx.x; e < total; e += stride) {
+    const float g = grad[e], m = mu * mom[e] + g;
+    mom[e] = m;
+    packed[packed_of(d, e)] = nesterov ? g + mu * m : m;
+  }
+}
+__global__ void __launch_bounds__(TT_BLOCK) k_core_apply(CoreDims d, float *__restrict__ core, const float *__restrict__ packed, float lr) {
+  const long long total = (long long)d.r * d.n * d.c, stride = (long long)gridDim.x * blockDim.x;
+  for (long long e = (long long)blockIdx.x * blockDim.x + threadIdx.x; e < total; e += stride) core[e] -= lr * packed[packed_of(d, e)];
+}
+
+bool table_ok(const tt_table *t) {
+  if (t->r[0] != 1 || t->r[3] != 1) return false;
+  for (int k = 0; k < 3; ++k)
+    if (t->n[k] < 1 || t->d[k] < 1 || t->r[k + 1] < 1 || t->r[k + 1] > 128 || t->d[k] > 4096) return false;
+  return (int64_t)t->d[0] * t->r[1] <= 4096 && (int64_t)t->d[1] * t->r[2] <= 4096 && (int64_t)t->d[2] * t->r[2] <= 4096;
+}
+// slices of core k
+Mats slices(const tt_table *t, int k) {
+  Mats m;
+  m.batch = t->n[k];
+  m.rows = k == 0 ? t->d[0] : t->r[k];
+  m.cols = k == 0 ? t->r[1] : t->d[k] * t->r[k + 1];
+  m.r_step = m.cols;
+  m.b_step = (long long)m.rows * m.cols;
+  return m;
+}
+size_t core_elems(const Mats &m) { return (size_t)m.batch * m.b_step; }
+
+}  // namespace
+
+extern "C" size_t tt_orthogonalize_workspace_bytes(const tt_matrices *m) {
+  if (!m || m->dtype < TT_F32 || m->dtype > TT_F16 || !size_ok(m->batch, m->rows, m->cols)) return 0;
+  return m->batch == 0 ? 256 : scratch(m->batch, m->rows, m->cols).total;
+}
+
+extern "C" tt_status tt_orthogonalize(const tt_matrices *m, const void *g, void *out, int steps, const float *coefficients, float eps, void *workspace,
+                                      size_t workspace_bytes, void *stream) {
+  if (!m || m->dtype < TT_F32 || m->dtype > TT_F16 || !steps_ok(steps, coefficients, eps)) return TT_ERR_INVALID_ARG;
+  if (!size_ok(m->batch, m->rows, m->cols)) return TT_ERR_SHAPE;
+  if (m->batch == 0) return TT_OK;
+  if (!g || !out) return TT_ERR_INVALID_ARG;
+  const uintptr_t low = m->dtype == TT_F32 ? 3 : 1;
+  if (((uintptr_t)g | (uintptr_t)out) & low) return TT_ERR_INVALID_ARG;
+  Mats in;
+  in.batch = m->batch; in.rows = (int)m->rows; in.cols = (int)m->cols;
+  in.r_step = m->row_step ? m->row_step : m->cols;
+  in.b_step = m->batch_step ? m->batch_step : in.r_step * m->rows;
+  const long long ldo = m->out_row_step ? m->out_row_step : m->cols, o_step = m->out_batch_step ? m->out_batch_step : ldo * m->rows;
+  if (in.r_step < m->cols || ldo < m->cols || in.b_step < 0 || o_step < ldo * (m->rows - 1) + m->cols) return TT_ERR_SHAPE;
+  const Scratch w = scratch(m->batch, m->rows, m->cols);
+  if (!workspace || ((uintptr_t)workspace & 255) != 0 || workspace_bytes < w.total) return TT_ERR_WORKSPACE;
+  hipStream_t s = (hipStream_t)stream;
+  char *ws = (char *)workspace;
+  tt_status st = m->dtype == TT_F32    ? scale_in<float>(g, in, eps, ws, w, s)
+                 : m->dtype == TT_BF16 ? scale_in<ttg::bf16>(g, in, eps, ws, w, s)
+                                       : scale_in<ttg::f16>(g, in, eps, ws, w, s);
+  if (st != TT_OK) return st;
+  return iterate(in, Steps{steps, coefficients}, m->dtype, out, o_step, ldo, ws, w, s);
+}
+
+extern "C" size_t tt_core_ortho_workspace_bytes(const tt_table *table) {
+  if (!table || !table_ok(table)) return 0;
+  size_t most = 0;
+  for (int k = 0; k < 3; ++k) {
+    const Mats m = slices(table, k);
+    if (!size_ok(m.batch, m.rows, m.cols)) return 0;
+    const size_t n = scratch(m.batch, m.rows, m.cols).total + 2 * pad256(core_elems(m) * 4);
+    if (n > most) most = n;
+  }
+  return most;
+}
+
+extern "C" tt_status tt_core_ortho_update(const tt_table *table, const float *const dcore[3], float *const momentum[3], float lr, float mu, int nesterov,
+                                          int steps, const float *coefficients, float eps, void *workspace, size_t workspace_bytes, void *stream) {
+  if (!table || !dcore || !momentum || !steps_ok(steps, coefficients, eps)) return TT_ERR_INVALID_ARG;
+  if (!table_ok(table)) return TT_ERR_SHAPE;
+  for (int k = 0; k < 3; ++k)
+    if (!table->core[k] || !dcore[k] || !momentum[k] || (((uintptr_t)table->core[k] | (uintptr_t)dcore[k] | (uintptr_t)momentum[k]) & 3))
+      return TT_ERR_INVALID_ARG;
+  const size_t need = tt_core_ortho_workspace_bytes(table);
+  if (need == 0) return TT_ERR_SHAPE;
+  if (!workspace || ((uintptr_t)workspace & 255) != 0 || workspace_bytes < need) return TT_ERR_WORKSPACE;
+  hipStream_t s = (hipStream_t)stream;
+  for (int k = 0; k < 3; ++k) {
+    const Mats m = slices(table, k);
+    const Scratch w = scratch(m.batch, m.rows, m.cols);
+    char *ws = (char *)workspace;
+    float *u = (float *)(ws + w.total), *o = (float *)(ws + w.total + pad256(core_elems(m) * 4));
+    CoreDims d;
+    d.r = k == 0 ? 1 : m.rows; d.n = (int)m.batch; d.c = k == 0 ? m.rows * m.cols : m.cols;
+    long long blocks = ((long long)core_elems(m) + TT_BLOCK - 1) / TT_BLOCK;
+    if (blocks > 8192) blocks = 8192;
+    const float *grad = dcore[k];
+    float *mom = momentum[k], *core = table->core[k];
+    hipLaunchKernelGGL(k_core_momentum, dim3((unsigned)blocks), dim3(TT_BLOCK), 0, s, d, grad, mom, mu, nesterov, u);
+    tt_status st = scale_in<float>(u, m, eps, ws, w, s);
+    if (st == TT_OK) st = iterate(m, Steps{steps, coefficients}, TT_F32, o, m.b_step, m.r_step, ws, w, s);
+    if (st != TT_OK) return st;
+    const float rate = (float)((double)lr * sqrt(m.rows > m.cols ? (double)m.rows / m.cols : 1.0));
+    hipLaunchKernelGGL(k_core_apply, dim3((unsigned)blocks), dim3(TT_BLOCK), 0, s, d, core, (const float *)o, rate);
+    st = tt_launch_status();
+    if (st != TT_OK) return st;
+  }
+  return TT_OK;
+}

@@ -19,11 +19,17 @@ Two more forward routes of the library are selectable:
   * `bf16_inference()` / `forward_bf16(...)`: forward on bf16 copies of the cores with fp32
     accumulation, for inference (no gradient); the copies are refreshed on request.
 
+`projection=width` puts a dense layer of the table's own behind the pooled rows (mixed-dimension tables): `TTDense`, the
+product with bias, activation and residual in one kernel, and in a fused module the product grouped by table.  `tt_dense` is
+the differentiable call, `TTOrthoSGD` the optimizer whose updates of cores and dense weights are orthogonalised.
+
 `TTFusedEmbeddingBags` holds SEVERAL tables of equal column factors and ranks as one fused TT table
 (cores side by side along the row-factor axis) and serves all of them with one reorder, one forward
 and one backward: what a model with many small tables needs to fill the GPU.
 """
 from __future__ import annotations
+
+import math
 
 import torch
 
@@ -73,6 +79,93 @@ def _csr_offsets(input, offsets, include_last_offset):
     return input.contiguous(), offsets.contiguous()
 
 
+class _DenseFunction(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, w, bias, residual, activation, offsets):
+        need = any(ctx.needs_input_grad[:3])
+        pre = torch.empty((x.shape[0], w.shape[-2]), dtype=x.dtype, device=x.device) if need and activation != "none" else None
+        out = binding.tt_dense_forward(x, w, bias, residual, activation, offsets=offsets, pre=pre)
+        ctx.activation, ctx.has_bias, ctx.has_residual = activation, bias is not None, residual is not None
+        ctx.save_for_backward(x, w, pre, offsets)
+        return out
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, grad_out):
+        x, w, pre, offsets = ctx.saved_tensors
+        need = ctx.needs_input_grad
+        dx = dw = db = None
+        if any(need[:3]):
+            g = grad_out
+            if g.dim() != 2 or g.stride(1) != 1 or (g.shape[0] > 1 and g.stride(0) < g.shape[1]):
+                g = g.contiguous()  # an expanded gradient (of a sum) has steps of zero
+            dx, dw, db = binding.tt_dense_backward(x, w, g, pre, ctx.activation, offsets=offsets,
+                                                   needs=(need[0], need[1], need[2] and ctx.has_bias))
+        dres = grad_out if ctx.has_residual and need[3] else None
+        return dx, dw, db, dres, None, None
+
+
+def _row_major(t):
+    """t as the library takes it: columns next to each other, rows that do not overlap (a copy where they are not)."""
+    if t is None or t.dim() != 2 or ((t.shape[1] <= 1 or t.stride(1) == 1) and (t.shape[0] <= 1 or t.stride(0) >= t.shape[1])):
+        return t
+    return t.contiguous()
+
+
+def tt_dense(x, w, bias=None, residual=None, activation="none", offsets=None):
+    """`act(x w^T + bias) + residual`, differentiable in its four tensors; grouped by `offsets` as in
+    `binding.tt_dense_forward`.  Rows of no group give zeros and get none: their residual is not added, and its gradient there
+    is left out too."""
+    if residual is not None and offsets is not None and residual.requires_grad and torch.is_grad_enabled():
+        residual = _GroupRows.apply(residual, offsets)
+    return _DenseFunction.apply(_row_major(x), w.contiguous(), None if bias is None else bias.contiguous(), _row_major(residual), activation, offsets)
+
+
+class _GroupRows(torch.autograd.Function):
+    """The identity, whose gradient is zero in rows of no group."""
+
+    @staticmethod
+    def forward(ctx, t, offsets):
+        ctx.save_for_backward(offsets)
+        return t.view_as(t)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, grad):
+        (offsets,) = ctx.saved_tensors
+        row = torch.arange(grad.shape[0], device=grad.device)
+        return torch.where(((row >= offsets[0]) & (row < offsets.max()))[:, None], grad, torch.zeros((), dtype=grad.dtype, device=grad.device)), None
+
+
+class TTDense(torch.nn.Module):
+    """Dense layer `act(x weight^T + bias) + residual` in one kernel: weight [out, in], or with `groups` [groups, out, in] where
+    group g's serves the rows offsets[g] .. offsets[g + 1] of x (offsets int64 [groups + 1] on the device).
+    activation: "none", "relu", "gelu", "silu" or "sigmoid"; dtype float32, bfloat16 or float16."""
+
+    def __init__(self, in_features: int, out_features: int, bias: bool = True, activation: str = "none", groups=None, device="cuda",
+                 dtype=torch.float32, generator=None):
+        super().__init__()
+        if activation not in binding.ACTIVATIONS:
+            raise ValueError("activation is one of %s" % ", ".join(binding.ACTIVATIONS))
+        if dtype not in binding.DTYPES:
+            raise ValueError("dtype is float32, bfloat16 or float16")
+        self.in_features, self.out_features, self.activation = int(in_features), int(out_features), activation
+        self.groups = None if groups is None else int(groups)
+        lead = () if groups is None else (self.groups,)
+        w = torch.empty(lead + (self.out_features, self.in_features), dtype=torch.float32, device=device)
+        w.normal_(0.0, self.in_features ** -0.5, generator=generator)
+        self.weight = torch.nn.Parameter(w.to(dtype))
+        self.bias = torch.nn.Parameter(torch.zeros(lead + (self.out_features,), dtype=dtype, device=device)) if bias else None
+
+    def forward(self, x, offsets=None, residual=None):
+        if (offsets is None) != (self.groups is None):
+            raise ValueError("offsets go with groups")
+        return tt_dense(x, self.weight, self.bias, residual, self.activation, offsets)
+
+    def extra_repr(self) -> str:
+        return "%d -> %d%s, %s" % (self.in_features, self.out_features, "" if self.groups is None else ", %d groups" % self.groups, self.activation)
+
+
 class TTEmbeddingBag(torch.nn.Module):
     """Sum-pooling embedding bag whose table of `num_embeddings x embedding_dim` is held as three
     TT cores `G_k[r_k][n_k][d_k][r_{k+1}]` (flat float32 parameters `core0..core2`).
@@ -83,11 +176,14 @@ class TTEmbeddingBag(torch.nn.Module):
     (bag starts; with include_last_offset the last entry is len(input)), or 2-D `input` whose rows
     are bags of equal length.  Not supported (raise): per_sample_weights, padding_idx, max_norm,
     modes other than "sum".
+    projection  width of a dense layer of the table's own behind the pooled rows (None: there is none), with
+    projection_activation (`TTDense`); the outputs are then [bags x projection]
     """
 
     def __init__(self, num_embeddings: int, embedding_dim: int, n, d, ranks, mode: str = "sum",
                  include_last_offset: bool = False, init_row_std: float = 0.1, fused_sgd_lr=None,
-                 forward_route: str = "batch", device="cuda", generator=None):
+                 forward_route: str = "batch", device="cuda", generator=None, projection=None,
+                 projection_activation: str = "none"):
         super().__init__()
         if mode != "sum":
             raise NotImplementedError("only sum pooling is defined for the TT embedding bag")
@@ -114,6 +210,8 @@ class TTEmbeddingBag(torch.nn.Module):
             w = torch.empty(numel, dtype=torch.float32, device=device)
             w.normal_(0.0, s, generator=generator)
             self.register_parameter("core%d" % k, torch.nn.Parameter(w))
+        self.projection = None if projection is None else TTDense(embedding_dim, projection, activation=projection_activation, device=device,
+                                                                  generator=generator)
 
     def cores(self):
         return [self.core0, self.core1, self.core2]
@@ -132,7 +230,8 @@ class TTEmbeddingBag(torch.nn.Module):
         if input.dtype != torch.int64:
             input = input.to(torch.int64)
         indices, offsets = self._bag_offsets(input, offsets)
-        return _TTBagFunction.apply(self.core0, self.core1, self.core2, indices, offsets, self)
+        out = _TTBagFunction.apply(self.core0, self.core1, self.core2, indices, offsets, self)
+        return out if self.projection is None else self.projection(out)
 
     def bf16_inference(self):
         """(Re)build the bf16 copies of the cores that `forward_bf16` reads; call again after the cores
@@ -152,9 +251,11 @@ class TTEmbeddingBag(torch.nn.Module):
         table = self._table(self.cores())
         # the plan would serve this call only: short batches are faster without one
         if binding.tt_forward_bf16_direct_pays(table, indices.numel(), offsets.numel() - 1):
-            return binding.tt_emb_bag_forward_bf16_direct(table, self._bf16_cores, indices, offsets)
-        plan = binding.tt_index_reorder(table, indices, offsets)
-        return binding.tt_emb_bag_forward_bf16(table, self._bf16_cores, plan, offsets)
+            out = binding.tt_emb_bag_forward_bf16_direct(table, self._bf16_cores, indices, offsets)
+        else:
+            plan = binding.tt_index_reorder(table, indices, offsets)
+            out = binding.tt_emb_bag_forward_bf16(table, self._bf16_cores, plan, offsets)
+        return out if self.projection is None else self.projection(out)
 
     def extra_repr(self) -> str:
         return "%d x %d, n=%s, d=%s, ranks=%s, %.1fx smaller than dense%s" % (
@@ -189,10 +290,13 @@ class TTFusedEmbeddingBags(torch.nn.Module):
     forward(inputs) takes one `(input, offsets)` pair (or a 2-D `input`) per table, as
     `TTEmbeddingBag.forward` does, and returns the list of pooled outputs in table order (views of
     one `[all bags x embedding_dim]` tensor).  `fused_sgd_lr` as for `TTEmbeddingBag`.
+    projection  width of a dense layer behind the pooled rows, a weight for every table (`TTDense` grouped by
+    table: one product for all), with projection_activation; outputs are then [bags x projection]
     """
 
     def __init__(self, tables, embedding_dim: int, d, ranks, include_last_offset: bool = False,
-                 init_row_std: float = 0.1, fused_sgd_lr=None, device="cuda", generator=None):
+                 init_row_std: float = 0.1, fused_sgd_lr=None, device="cuda", generator=None, projection=None,
+                 projection_activation: str = "none"):
         super().__init__()
         d, ranks = tuple(int(x) for x in d), tuple(int(x) for x in ranks)
         if len(d) != 3 or len(ranks) != 2 or d[0] * d[1] * d[2] != embedding_dim:
@@ -216,9 +320,20 @@ class TTFusedEmbeddingBags(torch.nn.Module):
             w = torch.empty(self.r[k] * self.n[k] * d[k] * self.r[k + 1], dtype=torch.float32, device=device)
             w.normal_(0.0, s, generator=generator)
             self.register_parameter("core%d" % k, torch.nn.Parameter(w))
+        self.projection = None if projection is None else TTDense(embedding_dim, projection, activation=projection_activation,
+                                                                  groups=len(tables), device=device, generator=generator)
+        self._table_rows = (None, None)  # bags of every table, and the device tensor of their running sums: kept while the counts stay
 
     def cores(self):
         return [self.core0, self.core1, self.core2]
+
+    def _row_offsets(self, bags, device):
+        if self._table_rows[0] != (bags, device):
+            ends = [0]
+            for b in bags:
+                ends.append(ends[-1] + b)
+            self._table_rows = ((bags, device), torch.tensor(ends, dtype=torch.int64, device=device))
+        return self._table_rows[1]
 
     def member_core(self, t: int, k: int, core=None):
         """Table t's part of fused core k (or of a tensor of its size, e.g. `.grad`): a strided view
@@ -248,7 +363,10 @@ class TTFusedEmbeddingBags(torch.nn.Module):
             self._fused = binding.FusedLayout(self.tables)
         f_idx, f_off = self._fused.fuse_lookups(idx, off, starts=not self.include_last_offset)
         out = _TTBagFunction.apply(self.core0, self.core1, self.core2, f_idx, f_off, self)
-        return list(torch.split(out, [o.numel() - (1 if self.include_last_offset else 0) for o in off]))
+        bags = tuple(o.numel() - (1 if self.include_last_offset else 0) for o in off)
+        if self.projection is not None:
+            out = self.projection(out, self._row_offsets(bags, out.device))
+        return list(torch.split(out, bags))
 
     def _bag_offsets(self, input, offsets):
         """Flat indices and CSR offsets, or (without include_last_offset) bag starts as they are given: the
@@ -299,19 +417,24 @@ class TTEmbeddingBagCollection(torch.nn.Module):
         self.tables = None
         families = {}
         for t, bag in enumerate(tables):
-            key = (bag.d, bag.r, bag.include_last_offset, bag.fused_sgd_lr, bag.core0.device)
+            p = bag.projection
+            key = (bag.d, bag.r, bag.include_last_offset, bag.fused_sgd_lr, bag.core0.device, p and (p.out_features, p.activation))
             families.setdefault(key, []).append(t)
         fused, where = [], [None] * len(tables)
-        for (d, r, last, lr, dev), idxs in families.items():
+        for (d, r, last, lr, dev, proj), idxs in families.items():
             members = [(tables[t].num_embeddings, tables[t].n) for t in idxs]
             for part in binding.fusion_groups(members, groups=fuse_groups):
                 m = TTFusedEmbeddingBags([members[p] for p in part], d[0] * d[1] * d[2], d, r[1:3],
-                                         include_last_offset=last, fused_sgd_lr=lr, device=dev)
+                                         include_last_offset=last, fused_sgd_lr=lr, device=dev,
+                                         projection=proj and proj[0], projection_activation=proj[1] if proj else "none")
                 with torch.no_grad():
                     for pos, p in enumerate(part):
                         src = tables[idxs[p]]
                         for k in range(3):
                             m.member_core(pos, k).copy_(src.cores()[k].view(r[k], src.n[k], d[k], r[k + 1]))
+                        if proj:
+                            m.projection.weight[pos].copy_(src.projection.weight)
+                            m.projection.bias[pos].copy_(src.projection.bias)
                         where[idxs[p]] = (len(fused), pos)
                 fused.append(m)
         self.fused = torch.nn.ModuleList(fused)
@@ -352,3 +475,62 @@ class TTEmbeddingBagCollection(torch.nn.Module):
         if self.fused is None:
             return results
         return [results[gi][pos] for gi, pos in self._where]
+
+
+class TTOrthoSGD(torch.optim.Optimizer):
+    """Gradient descent whose updates are orthogonalised (`binding.tt_orthogonalize`): momentum, then
+    `W <- W - lr sqrt(max(1, rows / cols)) ortho(u)` for every dense weight of the model's `TTDense` layers (every group's own)
+    and for every slice of the cores of its TT bags (`binding.tt_core_ortho_update`).  Whatever else the model has (biases,
+    other layers) takes plain steps of `other_lr` with the same momentum.  Momenta are float32.
+
+    model   a module; its parameters are sorted by the layers that own them
+    Tables without gradients (unused in this step, or with `fused_sgd_lr`) stay as they are.
+    """
+
+    def __init__(self, model, lr: float, momentum: float = 0.95, nesterov: bool = True, steps: int = 5,
+                 coefficients=binding.ORTHO_COEFFICIENTS, eps: float = 1e-7, other_lr=None):
+        if lr < 0 or not 0 <= momentum < 1:
+            raise ValueError("lr must not be negative, momentum is in [0, 1)")
+        self._tables = [m for m in model.modules() if isinstance(m, (TTEmbeddingBag, TTFusedEmbeddingBags))]
+        matrices = [m.weight for m in model.modules() if isinstance(m, TTDense)]
+        cores = [c for t in self._tables for c in t.cores()]
+        taken = {id(p) for p in matrices + cores}
+        rest = [p for p in model.parameters() if id(p) not in taken]
+        groups = [dict(params=ps, kind=kind, lr=rate) for ps, kind, rate in
+                  ((cores, "cores", lr), (matrices, "matrices", lr), (rest, "rest", lr if other_lr is None else other_lr)) if ps]
+        super().__init__(groups, dict(momentum=momentum, nesterov=nesterov, steps=steps, coefficients=coefficients, eps=eps))
+
+    def _momentum(self, p):
+        state = self.state[p]
+        if "momentum" not in state:
+            state["momentum"] = torch.zeros_like(p, dtype=torch.float32, memory_format=torch.contiguous_format)
+        return state["momentum"]
+
+    @torch.no_grad()
+    def step(self, closure=None):
+        loss = None
+        if closure is not None:
+            with torch.enable_grad():
+                loss = closure()
+        for group in self.param_groups:
+            lr, mu, how = group["lr"], group["momentum"], dict(steps=group["steps"], coefficients=group["coefficients"], eps=group["eps"])
+            if group["kind"] == "cores":
+                for t in self._tables:
+                    cores = t.cores()
+                    if any(c.grad is None for c in cores):
+                        continue
+                    binding.tt_core_ortho_update(t._table(cores), [c.grad.contiguous() for c in cores], [self._momentum(c) for c in cores], lr,
+                                                 momentum=mu, nesterov=group["nesterov"], **how)
+                continue
+            for p in group["params"]:
+                if p.grad is None:
+                    continue
+                g, buf = p.grad.float(), self._momentum(p)
+                buf.mul_(mu).add_(g)
+                u = torch.add(g, buf, alpha=mu) if group["nesterov"] else buf
+                if group["kind"] == "matrices":
+                    rows, cols = p.shape[-2:]
+                    p.add_(binding.tt_orthogonalize(u.to(p.dtype), **how), alpha=-lr * math.sqrt(max(1.0, rows / cols)))
+                else:
+                    p.add_(u.to(p.dtype), alpha=-lr)
+        return loss

@@ -166,3 +166,26 @@ static inline emu_f32x4 emu_mfma_4x4_bf16(emu_bf16x4 a, emu_bf16x4 b, emu_f32x4 
   return (emu_f32x4){t[0], t[1], t[2], t[3]};
 }
 #define __builtin_amdgcn_mfma_f32_4x4x4bf16_1k emu_mfma_4x4_bf16
+// 16x16x32 fp16: as for bf16
+template <class V>
+static inline emu_f32x4 emu_mfma_f16_k32(V a, V b, emu_f32x4 c, int, int, int) {
+  float t[4] = {c[0], c[1], c[2], c[3]};
+  for (int i = 0; i < 8; ++i) emu::wave_mfma_16x16x4((float)a[i], (float)b[i], t);
+  return (emu_f32x4){t[0], t[1], t[2], t[3]};
+}
+#define __builtin_amdgcn_mfma_f32_16x16x32_f16 emu_mfma_f16_k32
+// transposing LDS read: in every 16 lanes, lane j's address is that of elements 4 (j % 4) .. + 3 of row j / 4, and lane c
+// receives column c of the four rows
+template <class V>
+static inline auto emu_ds_read_tr16(const V *p) {
+  typedef short s4 __attribute__((ext_vector_type(4)));
+  const int lane = __lane(), c = lane & 15;
+  s4 r;
+  for (int row = 0; row < 4; ++row) {
+    const short *src = (const short *)(uintptr_t)emu::wave_exchange((uint64_t)(uintptr_t)p, (lane & ~15) + 4 * row + c / 4);
+    r[row] = src[c & 3];
+  }
+  emu::wave_exchange(0, -1);  // nobody writes before all have read
+  return r;
+}
+#define __builtin_amdgcn_ds_read_tr16_b64_v4i16(p) emu_ds_read_tr16((const __typeof__(*(p)) *)(uintptr_t)(p))

@@ -63,17 +63,69 @@ void describe(const tt_dense *op, TTGemm *g) {
   g->offsets = op->offsets;
   g->zero_rest = op->zero_rest;
   g->alpha = g->beta = 1.f;
+  g->parts = 3;
+}
+
+// The products of a call, without their operands' addresses.
+TTGemm of_out(const tt_dense *op) {  // x W^T
+  TTGemm g;
+  describe(op, &g);
+  g.a_kc = g.b_kc = 1;
+  g.mode = op->groups > 0 ? TT_GEMM_RAGGED_M : TT_GEMM_BATCH;
+  g.M = (int)op->rows; g.N = op->out_dim; g.K = op->in_dim;
+  g.lda = step(op->ld_x, op->in_dim);
+  g.ldb = op->in_dim; g.b_step = (long long)op->out_dim * op->in_dim;
+  g.ldo = step(op->ld_out, op->out_dim);
+  g.bias_step = op->out_dim;
+  g.ldr = step(op->ld_residual, op->out_dim);
+  g.ldp = op->out_dim;
+  g.act = op->activation;
+  return g;
+}
+TTGemm of_dx(const tt_dense *op, long long ldz) {  // dz W
+  TTGemm g;
+  describe(op, &g);
+  g.a_kc = 1; g.b_kc = 0;
+  g.mode = op->groups > 0 ? TT_GEMM_RAGGED_M : TT_GEMM_BATCH;
+  g.M = (int)op->rows; g.N = op->in_dim; g.K = op->out_dim;
+  g.lda = ldz;
+  g.ldb = op->in_dim; g.b_step = (long long)op->out_dim * op->in_dim;
+  g.ldo = step(op->ld_dx, op->in_dim);
+  return g;
+}
+TTGemm of_dw(const tt_dense *op, long long ldz, bool column) {  // dz^T x, or one column of dz^T dz
+  TTGemm g;
+  describe(op, &g);
+  g.a_kc = g.b_kc = 0;
+  g.mode = op->groups > 0 ? TT_GEMM_RAGGED_K : TT_GEMM_BATCH;
+  g.M = op->out_dim; g.N = column ? 1 : op->in_dim; g.K = (int)op->rows;
+  g.like_N = op->in_dim;
+  g.lda = ldz;
+  g.ldb = column ? ldz : step(op->ld_x, op->in_dim);
+  g.ldo = g.N; g.o_step = (long long)op->out_dim * g.N;
+  g.rs_step = op->out_dim;
+  return g;
 }
 
 struct Scratch {
-  size_t dz, column, total;  // byte offsets
+  size_t dz, column, pieces, total;  // byte offsets
 };
 Scratch scratch(const tt_dense *op, bool backward) {
-  Scratch w = {0, 0, 0};
-  if (!backward) return w;
-  if (op->activation != TT_ACT_NONE) w.total += pad256((size_t)op->rows * op->out_dim * elem(op->dtype));
-  w.column = w.total;
-  w.total += pad256((size_t)(op->groups > 0 ? op->groups : 1) * op->out_dim * elem(op->dtype));
+  Scratch w = {0, 0, 0, 0};
+  size_t most = ttk_gemm_partial_bytes(of_out(op));
+  if (backward) {
+    if (op->activation != TT_ACT_NONE) w.total += pad256((size_t)op->rows * op->out_dim * elem(op->dtype));
+    w.column = w.total;
+    w.total += pad256((size_t)(op->groups > 0 ? op->groups : 1) * op->out_dim * elem(op->dtype));
+    const TTGemm products[3] = {of_dx(op, op->out_dim), of_dw(op, op->out_dim, false), of_dw(op, op->out_dim, true)};
+    most = 0;
+    for (int i = 0; i < 3; ++i) {
+      const size_t n = ttk_gemm_partial_bytes(products[i]);
+      if (n > most) most = n;
+    }
+  }
+  w.pieces = w.total;
+  w.total += most;
   return w;
 }
 
@@ -95,19 +147,10 @@ extern "C" tt_status tt_dense_forward(const tt_dense *op, const void *x, const v
     return TT_ERR_INVALID_ARG;
   const Scratch need = scratch(op, false);
   if (need.total && (!workspace || ((uintptr_t)workspace & 255) != 0 || workspace_bytes < need.total)) return TT_ERR_WORKSPACE;
-  TTGemm g;
-  describe(op, &g);
-  g.a_kc = g.b_kc = 1;
-  g.mode = op->groups > 0 ? TT_GEMM_RAGGED_M : TT_GEMM_BATCH;
-  g.M = (int)op->rows; g.N = op->out_dim; g.K = op->in_dim;
-  g.a = x; g.lda = step(op->ld_x, op->in_dim);
-  g.b = w; g.ldb = op->in_dim; g.b_step = (long long)op->out_dim * op->in_dim;
-  g.out = out; g.ldo = step(op->ld_out, op->out_dim);
-  g.bias = bias; g.bias_step = op->out_dim;
-  g.res = residual; g.ldr = step(op->ld_residual, op->out_dim);
-  g.pre = pre; g.ldp = op->out_dim;
-  g.act = op->activation;
-  return ttk_gemm(g, (hipStream_t)stream);
+  TTGemm g = of_out(op);
+  g.a = x; g.b = w; g.out = out;
+  g.bias = bias; g.res = residual; g.pre = pre;
+  return ttk_gemm(g, workspace ? (char *)workspace + need.pieces : nullptr, (hipStream_t)stream);
 }
 
 extern "C" tt_status tt_dense_backward(const tt_dense *op, const void *x, const void *w, const void *pre, const void *grad_out, void *dx, void *dw,
@@ -135,35 +178,17 @@ extern "C" tt_status tt_dense_backward(const tt_dense *op, const void *x, const 
     ldz = op->out_dim;
   }
   if (dx && some) {
-    TTGemm g;
-    describe(op, &g);
-    g.a_kc = 1; g.b_kc = 0;
-    g.mode = op->groups > 0 ? TT_GEMM_RAGGED_M : TT_GEMM_BATCH;
-    g.M = (int)op->rows; g.N = op->in_dim; g.K = op->out_dim;
-    g.a = dz; g.lda = ldz;
-    g.b = w; g.ldb = op->in_dim; g.b_step = (long long)op->out_dim * op->in_dim;
-    g.out = dx; g.ldo = step(op->ld_dx, op->in_dim);
-    st = ttk_gemm(g, s);
+    TTGemm g = of_dx(op, ldz);
+    g.a = dz; g.b = w; g.out = dx;
+    st = ttk_gemm(g, ws + need.pieces, s);
     if (st != TT_OK) return st;
   }
-  if (dw || dbias) {
-    TTGemm g;
-    describe(op, &g);
-    g.a_kc = g.b_kc = 0;
-    g.mode = op->groups > 0 ? TT_GEMM_RAGGED_K : TT_GEMM_BATCH;
-    g.M = op->out_dim; g.K = (int)op->rows;
-    g.a = dz; g.lda = ldz;
-    if (dw) {
-      g.N = op->in_dim;
-      g.b = x; g.ldb = step(op->ld_x, op->in_dim);
-      g.out = dw; g.ldo = op->in_dim; g.o_step = (long long)op->out_dim * op->in_dim;
-    } else {  // the sums of dz's columns come beside a product: take one of a single column, into scratch
-      g.N = 1;
-      g.b = dz; g.ldb = ldz;
-      g.out = ws + need.column; g.ldo = 1; g.o_step = op->out_dim;
-    }
-    g.rowsum = dbias; g.rs_step = op->out_dim;
-    st = ttk_gemm(g, s);
+  if (dw || dbias) {  // the sums of dz's columns come beside a product: where that is not asked for, of a single column, into scratch
+    TTGemm g = of_dw(op, ldz, !dw);
+    g.a = dz; g.b = dw ? x : dz;
+    g.out = dw ? dw : ws + need.column;
+    g.rowsum = dbias;
+    st = ttk_gemm(g, ws + need.pieces, s);
   }
   return st;
 }

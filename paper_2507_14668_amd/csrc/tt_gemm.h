@@ -20,6 +20,7 @@ struct TTGemm {
   const void *a, *b;
   void *out;
   long long lda, ldb, ldo, a_step, b_step, o_step;
+  int like_N;                  // not 0: tiles and pieces are chosen as for this N
   int M, N, K;                 // RAGGED_M: M rows in all; RAGGED_K: K stored rows in all
   int batch;                   // members or groups
   const int64_t *offsets;      // DEVICE [batch + 1], ragged modes
@@ -31,7 +32,11 @@ struct TTGemm {
   long long bias_step, ldr, r_step, ldp, p_step, rs_step;
   int act;
   float alpha, beta;
+  int parts;                   // fp32 operands: bf16 parts of each that are multiplied (3: fp32's precision, 2: 16 bits)
 };
 
-// Enqueues the product.
-tt_status ttk_gemm(const TTGemm &g, hipStream_t s);
+// Long sums over few tiles of out are cut into pieces of K that run side by side; the pieces' sums go to `partial` and a
+// second launch adds them in order.  How many follows from types and sizes alone, so that a caller's workspace query knows.
+size_t ttk_gemm_partial_bytes(const TTGemm &g);  // 0: not split
+// Enqueues the product.  partial: ttk_gemm_partial_bytes(g) bytes of DEVICE memory, 256-byte aligned.
+tt_status ttk_gemm(const TTGemm &g, void *partial, hipStream_t s);

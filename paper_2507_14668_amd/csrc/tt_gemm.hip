@@ -4,69 +4,164 @@
 namespace {
 using namespace ttg;
 
-// ---- the general kernel ----------------------------------------------------------------------------
-// 64 x 64 of out per workgroup, four wavefronts of 32 x 32, operands through registers into LDS: any size, any row step, any
-// alignment down to the element's.  16 bytes of an operand per thread and step; elements outside are zeros.
-// The product is formed as out^T (B's rows are the instruction's M side), so that a lane's four results are neighbours in a row of out.
-constexpr int GT = 64;                                                // tile edge
-template <class T> struct Geo { static constexpr int E = 16 / sizeof(T), TK = 4 * E; };  // elements in 16 bytes; K of a step
-template <class T, bool KC> struct Lds {
-  // [64 rows][TK + pad] or [TK][64 + pad]; pads keep rows 8- / 16-byte aligned and spread them over the banks
-  static constexpr int LD = KC ? Geo<T>::TK + Geo<T>::E : GT + 8;
-  static constexpr int SIZE = KC ? GT * LD : Geo<T>::TK * LD;
+
+// ---- operands into LDS -----------------------------------------------------------------------------
+// A step of the product takes BK values of K.  An operand's tile of E = 128 or 64 rows is held in LDS as 16-bit parts, one plane of
+// E x BK after the other: K-contiguous operands [row][k], row-contiguous ones [k][row] (read with the transposing read, so that neither
+// is transposed on its way).  16-bit operands are one plane of themselves with BK = 64; fp32 operands are split into
+// bf16 parts on their way from registers to LDS (tt_split_bf16), BK = 32.
+template <class T> struct Step { static constexpr int BK = sizeof(T) == 2 ? 64 : 32; };
+
+// 16-byte pieces of a plane are spread over the banks: in an LDS row of 64 or 128 bytes (K-contiguous) by the tile's row, so that
+// eight neighbouring rows at one k meet every bank once; in a row of 2 E bytes (row-contiguous) pairs of pieces by k, so that the four
+// rows of a transposing read do.
+template <bool KC, int BK> __device__ __forceinline__ int piece_at(int row, int k8) {  // element offset of elements [row][8 k8 ..]
+  if constexpr (BK == 64) return row * 64 + ((k8 ^ (row & 7)) << 3);
+  else return row * 32 + ((k8 ^ ((row >> 1) & 3)) << 3);
+}
+template <int E> __device__ __forceinline__ int cross_at(int k, int row) {  // [k][row]
+  return k * E + ((((row >> 4) ^ (k & (E / 16 - 1))) << 4) | (row & 15));
+}
+
+// Eight elements of an operand that are neighbours in memory, as a thread carries them from memory to LDS.
+template <class T> struct Unit;
+template <> struct Unit<float> { f32x4 a, b; };
+template <> struct Unit<bf16> { u16x8 v; };
+template <> struct Unit<f16> { u16x8 v; };
+template <class T> __device__ __forceinline__ Unit<T> load_unit(const T *p, int valid) {
+  Unit<T> u;
+  if constexpr (sizeof(T) == 4) {
+    u.a = u.b = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (valid >= 8) {
+      u.a = *reinterpret_cast<const typename Vec<float>::v4 *>(p);
+      u.b = *reinterpret_cast<const typename Vec<float>::v4 *>(p + 4);
+    } else if (valid > 0) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (i < valid) u.a[i] = p[i];
+        if (i + 4 < valid) u.b[i] = p[i + 4];
+      }
+    }
+  } else {
+    u.v = u16x8{0, 0, 0, 0, 0, 0, 0, 0};
+    if (valid >= 8) u.v = *reinterpret_cast<const typename Vec<T>::v16b *>(p);
+    else if (valid > 0) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (i < valid) u.v[i] = __builtin_bit_cast(unsigned short, p[i]);
+    }
+  }
+  return u;
+}
+
+// The units of one operand that a thread carries, step after step.
+template <class T, bool KC, int E> struct Carrier {
+  static constexpr int BK = Step<T>::BK, N = E * BK / 8 / TT_BLOCK;
+  const T *p[N];
+  int valid[N];
+  long long step;
+  __device__ __forceinline__ void start(const T *base, long long ld, int row0, int rows, int k_first) {
+    step = KC ? BK : (long long)BK * ld;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int u = threadIdx.x + i * TT_BLOCK;
+      if constexpr (KC) {
+        const int r = row0 + u / (BK / 8);
+        valid[i] = r < rows ? 8 : 0;
+        p[i] = base + (long long)(r < rows ? r : 0) * ld + k_first + (u % (BK / 8)) * 8;
+      } else {
+        const int c = row0 + (u % (E / 8)) * 8, left = rows - c;
+        valid[i] = left >= 8 ? 8 : (left > 0 ? left : 0);
+        p[i] = base + (long long)(k_first + u / (E / 8)) * ld + (left > 0 ? c : 0);
+      }
+    }
+  }
+  // the units of the step at k0 (K: the end), and on to the next step
+  __device__ __forceinline__ void load(Unit<T> u[N], int k0, int K) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int n = threadIdx.x + i * TT_BLOCK;
+      const int left = K - k0 - (KC ? (n % (BK / 8)) * 8 : n / (E / 8));
+      u[i] = load_unit(p[i], KC ? (left < valid[i] ? left : valid[i]) : (left > 0 ? valid[i] : 0));
+      p[i] += step;
+    }
+  }
+  template <int P> __device__ __forceinline__ void store(const Unit<T> u[N], unsigned short *lds) const {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int n = threadIdx.x + i * TT_BLOCK;
+      const int o = KC ? piece_at<KC, BK>(n / (BK / 8), n % (BK / 8)) : cross_at<E>(n / (E / 8), (n % (E / 8)) * 8);
+      if constexpr (sizeof(T) == 2) {
+        *reinterpret_cast<u16x8 *>(lds + o) = u[i].v;
+      } else {
+        typedef unsigned u4 __attribute__((ext_vector_type(4)));
+        unsigned h[4], m[4], l[4];
+        tt_split_bf16(u[i].a[0], u[i].a[1], h[0], m[0], l[0]);
+        tt_split_bf16(u[i].a[2], u[i].a[3], h[1], m[1], l[1]);
+        tt_split_bf16(u[i].b[0], u[i].b[1], h[2], m[2], l[2]);
+        tt_split_bf16(u[i].b[2], u[i].b[3], h[3], m[3], l[3]);
+        *reinterpret_cast<u4 *>(lds + o) = u4{h[0], h[1], h[2], h[3]};
+        *reinterpret_cast<u4 *>(lds + E * BK + o) = u4{m[0], m[1], m[2], m[3]};
+        if constexpr (P == 3) *reinterpret_cast<u4 *>(lds + 2 * E * BK + o) = u4{l[0], l[1], l[2], l[3]};
+      }
+    }
+  }
+  // unsplit, for the fp32 instructions: [row][32 + 4] or [k][128 + 4] floats
+  static constexpr int LD32 = KC ? 36 : E + 4, SIZE32 = (KC ? E : 32) * LD32;
+  __device__ __forceinline__ void store32(const Unit<T> u[N], float *lds) const {
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int n = threadIdx.x + i * TT_BLOCK;
+        float *d = lds + (KC ? (n / (BK / 8)) * LD32 + (n % (BK / 8)) * 8 : (n / (E / 8)) * LD32 + (n % (E / 8)) * 8);
+        *reinterpret_cast<f32x4 *>(d) = u[i].a;
+        *reinterpret_cast<f32x4 *>(d + 4) = u[i].b;
+      }
+    }
+  }
 };
 
-// 16 bytes of an operand: chunk `c` (0..255) of the step at k0.  row0, rows: first row of the tile and the rows there are.
-template <class T, bool KC>
-__device__ __forceinline__ typename Vec<T>::v16b load_chunk(const T *base, long long ld, int row0, int rows, int k0, int K, int c) {
-  constexpr int E = Geo<T>::E;
-  const int major = KC ? row0 + c / 4 : k0 + c / (GT / E), minor = KC ? k0 + (c % 4) * E : row0 + (c % (GT / E)) * E;
-  const int nmajor = KC ? rows : K, nminor = KC ? K : rows;
-  typename Vec<T>::v16b v;
-#pragma unroll
-  for (int i = 0; i < E; ++i) v[i] = 0;
-  if (major >= nmajor || minor >= nminor) return v;
-  const T *p = base + (long long)major * ld + minor;
-  if (nminor - minor >= E) return *reinterpret_cast<const typename Vec<T>::v16b *>(p);
-#pragma unroll
-  for (int i = 0; i < E; ++i)
-    if (i < nminor - minor) {
-      if constexpr (sizeof(T) == 4) v[i] = p[i];
-      else v[i] = __builtin_bit_cast(unsigned short, p[i]);
-    }
-  return v;
-}
-template <class T, bool KC>
-__device__ __forceinline__ void store_chunk(T *lds, typename Vec<T>::v16b v, int c) {
-  constexpr int E = Geo<T>::E, LD = Lds<T, KC>::LD;
-  const int o = KC ? (c / 4) * LD + (c % 4) * E : (c / (GT / E)) * LD + (c % (GT / E)) * E;
-  typedef unsigned u4 __attribute__((ext_vector_type(4)));
-  *reinterpret_cast<u4 *>(lds + o) = __builtin_bit_cast(u4, v);
-}
-// The lane's elements of the 16 rows at r0: k = 8 (lane / 16) + i (16-bit), or k = 4 (lane / 16) + j for four steps j (fp32)
-template <class T, bool KC>
-__device__ __forceinline__ u16x8 frag16(const T *lds, int r0) {
-  constexpr int LD = Lds<T, KC>::LD;
+// The lane's eight elements of rows r0 .. r0 + 15 at k = 32 s + 8 (lane / 16) + i
+template <bool KC, int BK, int E> __device__ __forceinline__ u16x8 frag(const unsigned short *lds, int r0, int s) {
   const int lane = threadIdx.x & 63, q = lane >> 4, j = lane & 15;
-  if constexpr (KC) return *reinterpret_cast<const u16x8 *>(lds + (r0 + j) * LD + 8 * q);
-  const unsigned short *p = reinterpret_cast<const unsigned short *>(lds) + (8 * q + (j >> 2)) * LD + r0 + 4 * (j & 3);
-  const u16x4 x = lds_read_tr(p), y = lds_read_tr(p + 4 * LD);
+  if constexpr (KC) return *reinterpret_cast<const u16x8 *>(lds + piece_at<KC, BK>(r0 + j, 4 * s + q));
+  const int k = 32 * s + 8 * q + (j >> 2), c = r0 + 4 * (j & 3);
+  const u16x4 x = lds_read_tr(lds + cross_at<E>(k, c)), y = lds_read_tr(lds + cross_at<E>(k + 4, c));
   return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
 }
-template <bool KC>
-__device__ __forceinline__ f32x4 frag32(const float *lds, int r0) {
-  constexpr int LD = Lds<float, KC>::LD;
+template <bool KC, int LD32> __device__ __forceinline__ f32x4 frag32(const float *lds, int r0, int h) {  // k = 16 h + 4 (lane / 16) + i
   const int lane = threadIdx.x & 63, q = lane >> 4, j = lane & 15;
-  if constexpr (KC) return *reinterpret_cast<const f32x4 *>(lds + (r0 + j) * LD + 4 * q);
+  if constexpr (KC) return *reinterpret_cast<const f32x4 *>(lds + (r0 + j) * LD32 + 16 * h + 4 * q);
   f32x4 v;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) v[i] = lds[(4 * q + i) * LD + r0 + j];
+  for (int i = 0; i < 4; ++i) v[i] = lds[(16 * h + 4 * q + i) * LD32 + r0 + j];
   return v;
 }
 
-struct Tile {
-  int z, lo, hi, n0, k_lo, k_hi;  // member / group; rows [lo, hi) of out; first column; stored rows of K (RAGGED_K), else [0, K)
+// ---- which tile ------------------------------------------------------------------------------------
+struct Place {
+  int z, lo, hi, n0;  // member / group; rows [lo, hi) of out; first column
+  int k_lo, k_hi;     // values of K of this workgroup (stored rows in RAGGED_K)
 };
+// Workgroups go round the eight dies by their number; each die gets neighbouring tiles, and within them eight row tiles
+// take a column tile together, so that what they read of both operands is in the die's L2.
+__device__ __forceinline__ void tile_order(unsigned t, unsigned m_tiles, unsigned n_tiles, unsigned &mt, unsigned &nt) {
+  const unsigned total = m_tiles * n_tiles, per = total / 8, left = total % 8, die = t % 8;
+  t = die * per + (die < left ? die : left) + t / 8;
+  const unsigned band = t / (8 * n_tiles), rows = m_tiles - 8 * band < 8 ? m_tiles - 8 * band : 8, in = t - band * 8 * n_tiles;
+  mt = 8 * band + in % rows;
+  nt = in / rows;
+}
+
+// RAGGED_M: clears the rows that no group covers; `idx` of `n` workgroups that found no tile, for columns n0 .. n0 + width
+template <class O> __device__ __forceinline__ void clear_rest(const TTGemm &g, int above, int covered, int idx, int n, int n0, int width) {
+  const float zero[4] = {0.f, 0.f, 0.f, 0.f};
+  const long long rest = (long long)above + g.M - covered;
+  const int end = g.N < n0 + width ? g.N : n0 + width;
+  for (long long r = (long long)idx * 4 + (threadIdx.x >> 6); r < rest; r += (long long)n * 4)
+    for (int c = n0 + 4 * (threadIdx.x & 63); c < end; c += 256)
+      store4((O *)g.out + (r < above ? r : r - above + covered) * g.ldo + c, end - c < 4 ? end - c : 4, zero);
+}
 
 // out[m][n .. n + 3] from four sums
 template <class T, class O>
@@ -97,128 +192,362 @@ __device__ __forceinline__ void epilogue4(const TTGemm &g, int z, int m, int n, 
   store4((O *)g.out + z * g.o_step + (long long)m * g.ldo + n, valid, v);
 }
 
-template <class T, class O, bool AKC, bool BKC>
-__global__ void __launch_bounds__(TT_BLOCK) k_gemm(TTGemm g, int m_tiles, int n_tiles) {
-  constexpr int TK = Geo<T>::TK;
-  __shared__ __align__(16) T la[Lds<T, AKC>::SIZE];
-  __shared__ __align__(16) T lb[Lds<T, BKC>::SIZE];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  // column tiles fastest: workgroups in flight share rows of A
-  const int n0 = (int)(blockIdx.x % (unsigned)n_tiles) * GT;
-  const unsigned rest = blockIdx.x / (unsigned)n_tiles;
-  int z, lo, hi, K = g.K, k_lo = 0;
+// ---- the tile kernel -------------------------------------------------------------------------------
+// E x E of out per workgroup (E = 128, or 64 where there are few tiles), four wavefronts of a quarter each, any size, row step and alignment down to the element's; elements
+// outside are zeros.  The product is formed as out^T (B's rows are the instruction's M side), so that a lane's four results are
+// neighbours in a row of out.
+// P planes: 1 (16-bit operands), 2 or 3 (fp32 operands in bf16 parts).  Three parts hold all 24 bits; of the nine products
+// the six with hi * hi, hi * mid, hi * lo and mid * mid count, the rest is below 2^-24 of the product.  What parts cannot do:
+// infinities, NaN and numbers that round to a bf16 infinity give NaN sums, and products below 2^-92 lose parts to underflow.  A tile with
+// a sum that is not finite, or with a sum below 2^-80 beside operands whose smallest product is that small, is done
+// again with the fp32 instruction.  (P = 2 is for operands that are scaled to at most one, with no such products that count.)
+template <class T, class O, int P, bool AKC, bool BKC, int E>
+__global__ void __launch_bounds__(TT_BLOCK, 2) k_gemm(TTGemm g, int m_tiles, int n_tiles, int split, float *partial) {
+  typedef Carrier<T, AKC, E> CA;
+  typedef Carrier<T, BKC, E> CB;
+  constexpr int BK = Step<T>::BK, PLANE = E * BK, F = E / 32, BUF = P == 1 ? 2 : 1;  // fp32's planes fill the LDS of two workgroups with one buffer
+  constexpr int HALVES = 2 * BUF * P * PLANE, REDO = P == 3 ? 2 * (CA::SIZE32 + CB::SIZE32) : 0;
+  __shared__ __align__(16) unsigned short lds[HALVES > REDO ? HALVES : REDO];
+  __shared__ int flags[4];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  unsigned mt, nt;
+  tile_order(blockIdx.x, (unsigned)m_tiles, (unsigned)n_tiles, mt, nt);
+  Place w;
+  w.n0 = (int)nt * E;
+  w.k_lo = 0;
+  w.k_hi = g.K;
   if (g.mode == TT_GEMM_RAGGED_M) {
-    const int t = (int)rest, there = find_tile<GT>(g.offsets, g.batch, g.M, t, z, lo, hi);
-    if (z < 0) {  // a tile behind the last one: the rows that no group covers are dealt to these
-      if (!g.zero_rest) return;
-      const int above = lo, below = g.M - hi, idx = t - there, n = m_tiles - there;
-      const float zero[4] = {0.f, 0.f, 0.f, 0.f};
-      const int nn = n0 + 4 * (tid & 15), valid = g.N - nn < 4 ? g.N - nn : 4;
-      for (long long r = (long long)idx * 16 + (tid >> 4); r < (long long)above + below; r += (long long)n * 16)
-        if (valid > 0) store4((O *)g.out + (r < above ? r : r - above + hi) * g.ldo + nn, valid, zero);
+    const int there = find_tile<E>(g.offsets, g.batch, g.M, (int)mt, w.z, w.lo, w.hi);
+    if (w.z < 0) {
+      if (g.zero_rest) clear_rest<O>(g, w.lo, w.hi, (int)mt - there, m_tiles - there, w.n0, E);
       return;
     }
   } else {
-    z = (int)(rest / (unsigned)m_tiles);
-    lo = (int)(rest % (unsigned)m_tiles) * GT;
-    hi = g.M < lo + GT ? g.M : lo + GT;
-    if (g.mode == TT_GEMM_RAGGED_K) {
-      int k_hi;
-      group_rows(g.offsets, z, g.K, k_lo, k_hi);
-      K = k_hi - k_lo;
-    }
+    w.z = (int)blockIdx.y;
+    w.lo = (int)mt * E;
+    w.hi = g.M < w.lo + E ? g.M : w.lo + E;
+    if (g.mode == TT_GEMM_RAGGED_K) group_rows(g.offsets, w.z, g.K, w.k_lo, w.k_hi);
   }
-  const bool ragged_k = g.mode == TT_GEMM_RAGGED_K;
-  const T *a = (const T *)g.a + (g.mode == TT_GEMM_BATCH ? z * g.a_step : ragged_k ? (long long)k_lo * g.lda : 0);
-  const T *b = (const T *)g.b + (ragged_k ? (long long)k_lo * g.ldb : z * g.b_step);
-
-  const int wm = (wave >> 1) * 32, wn = (wave & 1) * 32, q = lane >> 4, j = lane & 15;
-  f32x4 acc[2][2] = {}, rs[2] = {};  // [m][n]; sums of A's rows
-  const bool sums = g.rowsum && n0 == 0;
-  typename Vec<T>::v16b va = load_chunk<T, AKC>(a, g.lda, lo, hi, 0, K, tid), vb = load_chunk<T, BKC>(b, g.ldb, n0, g.N, 0, K, tid);
-  for (int k0 = 0; k0 < K; k0 += TK) {
-    __syncthreads();
-    store_chunk<T, AKC>(la, va, tid);
-    store_chunk<T, BKC>(lb, vb, tid);
-    __syncthreads();
-    if (k0 + TK < K) {
-      va = load_chunk<T, AKC>(a, g.lda, lo, hi, k0 + TK, K, tid);
-      vb = load_chunk<T, BKC>(b, g.ldb, n0, g.N, k0 + TK, K, tid);
-    }
-    if constexpr (sizeof(T) == 2) {
-      u16x8 fa[2], fb[2];
+  if (split > 1) {  // whole steps to each piece
+    const int steps = (w.k_hi - w.k_lo + BK - 1) / BK, per = (steps + split - 1) / split;
+    const long long a = (long long)w.k_lo + (long long)blockIdx.z * per * BK, b = a + (long long)per * BK;
+    if (a < w.k_hi) w.k_lo = (int)a;
+    else w.k_lo = w.k_hi;
+    if (b < w.k_hi) w.k_hi = (int)b;
+  }
+  const bool by_member = g.mode == TT_GEMM_BATCH;
+  const T *a = (const T *)g.a + (by_member ? w.z * g.a_step : 0), *b = (const T *)g.b + (g.mode != TT_GEMM_RAGGED_K ? w.z * g.b_step : 0);
+  const int K = w.k_hi;
+  CA ca;
+  CB cb;
+  ca.start(a, g.lda, w.lo, w.hi, w.k_lo);
+  cb.start(b, g.ldb, w.n0, g.N, w.k_lo);
+  Unit<T> ua[CA::N], ub[CB::N];
+  const int wm = (wave >> 1) * (E / 2), wn = (wave & 1) * (E / 2);
+  f32x4 acc[F][F] = {}, rs[F] = {};  // [m][n]; sums of A's rows
+  const bool sums = g.rowsum && w.n0 == 0;
+  unsigned small_a = ~0u, small_b = ~0u;  // twice the bits of the smallest number that is not zero, less one
+  auto note = [&]() {
+    if constexpr (P == 3) {
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        fa[i] = frag16<T, AKC>(la, wm + 16 * i);
-        fb[i] = frag16<T, BKC>(lb, wn + 16 * i);
-      }
+      for (int i = 0; i < CA::N; ++i)
 #pragma unroll
-      for (int x = 0; x < 2; ++x)
+        for (int e = 0; e < 4; ++e) {
+          const unsigned x = 2 * __float_as_uint(ua[i].a[e]) - 1, y = 2 * __float_as_uint(ua[i].b[e]) - 1;
+          small_a = x < small_a ? x : small_a;
+          small_a = y < small_a ? y : small_a;
+        }
 #pragma unroll
-        for (int y = 0; y < 2; ++y) acc[x][y] = mma(T(), fb[y], fa[x], acc[x][y]);
-      if (sums) {
-        u16x8 ones;
+      for (int i = 0; i < CB::N; ++i)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) ones[i] = __builtin_bit_cast(unsigned short, (T)1.f);
-#pragma unroll
-        for (int x = 0; x < 2; ++x) rs[x] = mma(T(), ones, fa[x], rs[x]);
-      }
-    } else {
-      f32x4 fa[2], fb[2];
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        fa[i] = frag32<AKC>(la, wm + 16 * i);
-        fb[i] = frag32<BKC>(lb, wn + 16 * i);
-      }
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int x = 0; x < 2; ++x) {
-#pragma unroll
-          for (int y = 0; y < 2; ++y) acc[x][y] = __builtin_amdgcn_mfma_f32_16x16x4f32(fb[y][i], fa[x][i], acc[x][y], 0, 0, 0);
-          if (sums) rs[x] = __builtin_amdgcn_mfma_f32_16x16x4f32(1.f, fa[x][i], rs[x], 0, 0, 0);
+        for (int e = 0; e < 4; ++e) {
+          const unsigned x = 2 * __float_as_uint(ub[i].a[e]) - 1, y = 2 * __float_as_uint(ub[i].b[e]) - 1;
+          small_b = x < small_b ? x : small_b;
+          small_b = y < small_b ? y : small_b;
         }
     }
-  }
+  };
+  auto plane_a = [&](int buf, int p) { return lds + (buf * 2 * P + p) * PLANE; };
+  auto plane_b = [&](int buf, int p) { return lds + (buf * 2 * P + P + p) * PLANE; };
+  auto multiply = [&](int buf) {
 #pragma unroll
-  for (int x = 0; x < 2; ++x) {
-    const int m = lo + wm + 16 * x + j;
-    if (m >= hi) continue;
+    for (int s = 0; s < BK / 32; ++s) {
+      u16x8 fa[F][P];
 #pragma unroll
-    for (int y = 0; y < 2; ++y) {
-      const int n = n0 + wn + 16 * y + 4 * q;
-      if (n < g.N) epilogue4<T, O>(g, z, m, n, acc[x][y]);
+      for (int x = 0; x < F; ++x)
+#pragma unroll
+        for (int p = 0; p < P; ++p) fa[x][p] = frag<AKC, BK, E>(plane_a(buf, p), wm + 16 * x, s);
+#pragma unroll
+      for (int y = 0; y < F; ++y) {
+        u16x8 fb[P];
+#pragma unroll
+        for (int p = 0; p < P; ++p) fb[p] = frag<BKC, BK, E>(plane_b(buf, p), wn + 16 * y, s);
+        if constexpr (P == 1) {
+#pragma unroll
+          for (int x = 0; x < F; ++x) acc[x][y] = mma(T(), fb[0], fa[x][0], acc[x][y]);
+        } else {  // the smallest terms first
+#pragma unroll
+          for (int d = P - 1; d >= 0; --d)
+#pragma unroll
+            for (int p = 0; p <= d; ++p)
+#pragma unroll
+              for (int x = 0; x < F; ++x) acc[x][y] = mma(bf16(), fb[d - p], fa[x][p], acc[x][y]);
+        }
+      }
+      if (sums) {
+        unsigned short one = 0x3f80;  // of bf16
+        if constexpr (std::is_same<T, f16>::value) one = 0x3c00;
+        const u16x8 ones = {one, one, one, one, one, one, one, one};
+#pragma unroll
+        for (int x = 0; x < F; ++x)
+#pragma unroll
+          for (int p = P - 1; p >= 0; --p) {
+            if constexpr (P == 1) rs[x] = mma(T(), ones, fa[x][0], rs[x]);
+            else rs[x] = mma(bf16(), ones, fa[x][p], rs[x]);
+          }
+      }
     }
-    if (sums && wn == 0 && q == 0) ((O *)g.rowsum)[z * g.rs_step + m] = from_f32<O>(rs[x][0]);
+  };
+  if (w.k_lo < K) {
+    ca.load(ua, w.k_lo, K);
+    cb.load(ub, w.k_lo, K);
+    if constexpr (BUF == 2) {
+      ca.template store<P>(ua, plane_a(0, 0));
+      cb.template store<P>(ub, plane_b(0, 0));
+    }
+    int buf = 0;
+    for (int k0 = w.k_lo; k0 < K; k0 += BK) {
+      const bool more = k0 + BK < K;
+      if constexpr (BUF == 2) {
+        __syncthreads();  // this step's tiles are whole, and nobody reads the other buffer any more
+        if (more) {
+          ca.load(ua, k0 + BK, K);
+          cb.load(ub, k0 + BK, K);
+        }
+        multiply(buf);
+        if (more) {
+          ca.template store<P>(ua, plane_a(buf ^ 1, 0));
+          cb.template store<P>(ub, plane_b(buf ^ 1, 0));
+        }
+        buf ^= 1;
+      } else {
+        __syncthreads();
+        note();
+        ca.template store<P>(ua, plane_a(0, 0));
+        cb.template store<P>(ub, plane_b(0, 0));
+        __syncthreads();
+        if (more) {
+          ca.load(ua, k0 + BK, K);
+          cb.load(ub, k0 + BK, K);
+        }
+        multiply(0);
+      }
+    }
+  }
+  if constexpr (P == 3) {
+    bool odd = false, tiny = false;
+#pragma unroll
+    for (int x = 0; x < F; ++x) {
+#pragma unroll
+      for (int y = 0; y < F; ++y)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          odd |= !(fabsf(acc[x][y][i]) < INFINITY);
+          tiny |= fabsf(acc[x][y][i]) < 0x1p-80f;
+        }
+      if (sums) {
+        odd |= !(fabsf(rs[x][0]) < INFINITY);
+        tiny |= fabsf(rs[x][0]) < 0x1p-80f;
+      }
+    }
+    // exponents of the smallest numbers of the workgroup; the two floats' product is below 2^-92 if the exponents' sum (each 127 too many) is
+    unsigned ea = small_a == ~0u ? 255 : small_a >> 24, eb = small_b == ~0u ? 255 : small_b >> 24;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const unsigned x = (unsigned)__shfl((int)ea, lane ^ o, 64), y = (unsigned)__shfl((int)eb, lane ^ o, 64);
+      ea = x < ea ? x : ea;
+      eb = y < eb ? y : eb;
+    }
+    const int mine = (__ballot(odd) ? 1 << 16 : 0) | (__ballot(tiny) ? 1 << 17 : 0) | (int)ea << 8 | (int)eb;
+    if (lane == 0) flags[wave] = mine;
+    __syncthreads();
+    int all = 0;
+    ea = eb = 255;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int f = flags[i];
+      all |= f & (3 << 16);
+      ea = (unsigned)(f >> 8 & 255) < ea ? (unsigned)(f >> 8 & 255) : ea;
+      eb = (unsigned)(f & 255) < eb ? (unsigned)(f & 255) : eb;
+    }
+    // parts themselves are whole down to 2^-100
+    const bool under = (int)(ea + eb) - 254 < -92 || ea < 27 || eb < 27;
+    if ((all & (1 << 16)) || ((all & (1 << 17)) && under)) {
+      float *l32a = reinterpret_cast<float *>(lds), *l32b = l32a + CA::SIZE32;
+#pragma unroll
+      for (int x = 0; x < F; ++x) {
+        rs[x] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int y = 0; y < F; ++y) acc[x][y] = f32x4{0.f, 0.f, 0.f, 0.f};
+      }
+      ca.start(a, g.lda, w.lo, w.hi, w.k_lo);
+      cb.start(b, g.ldb, w.n0, g.N, w.k_lo);
+      for (int k0 = w.k_lo; k0 < K; k0 += BK) {
+        ca.load(ua, k0, K);
+        cb.load(ub, k0, K);
+        __syncthreads();
+        ca.store32(ua, l32a);
+        cb.store32(ub, l32b);
+        __syncthreads();
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          f32x4 fa[F];
+#pragma unroll
+          for (int x = 0; x < F; ++x) fa[x] = frag32<AKC, CA::LD32>(l32a, wm + 16 * x, h);
+#pragma unroll
+          for (int y = 0; y < F; ++y) {
+            const f32x4 fb = frag32<BKC, CB::LD32>(l32b, wn + 16 * y, h);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+              for (int x = 0; x < F; ++x) acc[x][y] = __builtin_amdgcn_mfma_f32_16x16x4f32(fb[i], fa[x][i], acc[x][y], 0, 0, 0);
+          }
+          if (sums)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+              for (int x = 0; x < F; ++x) rs[x] = __builtin_amdgcn_mfma_f32_16x16x4f32(1.f, fa[x][i], rs[x], 0, 0, 0);
+        }
+      }
+    }
+  }
+  const int q = lane >> 4, j = lane & 15;
+#pragma unroll
+  for (int x = 0; x < F; ++x) {
+    const int m = w.lo + wm + 16 * x + j;
+    if (m >= w.hi) continue;
+    if (split > 1) {
+      float *piece = partial + ((long long)blockIdx.z * g.batch + w.z) * g.M * (g.N + 1LL);  // [M][N] sums, then [M] sums of A's rows
+#pragma unroll
+      for (int y = 0; y < F; ++y) {
+        const int n = w.n0 + wn + 16 * y + 4 * q, valid = g.N - n < 4 ? g.N - n : 4;
+        const float v[4] = {acc[x][y][0], acc[x][y][1], acc[x][y][2], acc[x][y][3]};
+        if (valid > 0) store4(piece + (long long)m * g.N + n, valid, v);
+      }
+      if (sums && wn == 0 && q == 0) piece[(long long)g.M * g.N + m] = rs[x][0];
+      continue;
+    }
+#pragma unroll
+    for (int y = 0; y < F; ++y) {
+      const int n = w.n0 + wn + 16 * y + 4 * q;
+      if (n < g.N) epilogue4<T, O>(g, w.z, m, n, acc[x][y]);
+    }
+    if (sums && wn == 0 && q == 0) ((O *)g.rowsum)[w.z * g.rs_step + m] = from_f32<O>(rs[x][0]);
   }
 }
 
-template <class T, class O>
-void launch_general(const TTGemm &g, unsigned blocks, int m_tiles, int n_tiles, hipStream_t s) {
-  if (g.a_kc && g.b_kc)
-    hipLaunchKernelGGL((k_gemm<T, O, true, true>), dim3(blocks), dim3(TT_BLOCK), 0, s, g, m_tiles, n_tiles);
-  else if (g.a_kc)
-    hipLaunchKernelGGL((k_gemm<T, O, true, false>), dim3(blocks), dim3(TT_BLOCK), 0, s, g, m_tiles, n_tiles);
-  else
-    hipLaunchKernelGGL((k_gemm<T, O, false, false>), dim3(blocks), dim3(TT_BLOCK), 0, s, g, m_tiles, n_tiles);
+// The pieces of a split product, added in order; four columns of a row per thread.
+template <class T, class O> __global__ void __launch_bounds__(TT_BLOCK) k_join(TTGemm g, int split, const float *__restrict__ partial) {
+  const int per = (g.N + 3) / 4, z = (int)blockIdx.y;
+  const long long total = (long long)g.M * per, piece = (long long)g.M * (g.N + 1LL);
+  const float *p = partial + z * piece;
+  for (long long e = (long long)blockIdx.x * TT_BLOCK + threadIdx.x; e < total + g.M; e += (long long)gridDim.x * TT_BLOCK) {
+    if (e >= total) {
+      if (!g.rowsum) continue;
+      const long long m = e - total;
+      float s = 0.f;
+      for (int i = 0; i < split; ++i) s += p[i * g.batch * piece + (long long)g.M * g.N + m];
+      ((O *)g.rowsum)[z * g.rs_step + m] = from_f32<O>(s);
+      continue;
+    }
+    const int m = (int)(e / per), n = (int)(e - (long long)m * per) * 4, valid = g.N - n < 4 ? g.N - n : 4;
+    f32x4 s = {0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < split; ++i) {
+      float t[4];
+      load4(p + i * g.batch * piece + (long long)m * g.N + n, valid, t);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) s[c] += t[c];
+    }
+    epilogue4<T, O>(g, z, m, n, s);
+  }
+}
+
+// ---- host ------------------------------------------------------------------------------------------
+#ifndef TT_GEMM_LARGE_TILES
+#define TT_GEMM_LARGE_TILES 256  // tiles of 128 from which they are taken
+#endif
+struct Shape {
+  int e, split;
+  long long m_tiles, n_tiles, members;
+};
+Shape shape_of(const TTGemm &g) {
+  Shape h;
+  const int bk = g.dtype == TT_F32 ? 32 : 64;
+  // (as for N = like_N: sums of A's rows beside one column have the bits of those beside all)
+  auto tiles = [&](int e) {
+    // every group ends in at most one part tile; one more for the rows outside the groups
+    h.m_tiles = g.mode == TT_GEMM_RAGGED_M ? (long long)tt_ceil_div(g.M, e) + g.batch + 1 : tt_ceil_div(g.M, e);
+    h.n_tiles = tt_ceil_div(g.N, e);
+    h.members = g.mode == TT_GEMM_RAGGED_M ? 1 : g.batch;
+    h.e = e;
+    return (long long)tt_ceil_div(g.M, e) * tt_ceil_div(g.like_N ? g.like_N : g.N, e) * h.members;
+  };
+  long long n = tiles(128);
+  if (n < TT_GEMM_LARGE_TILES) n = tiles(64);
+  // two workgroups and more run on a compute unit: long sums in pieces up to 512 workgroups in all, of eight steps at least
+  h.split = 1;
+  if (g.mode != TT_GEMM_RAGGED_M) {
+    long long steps = tt_ceil_div(g.K, bk);
+    if (g.mode == TT_GEMM_RAGGED_K) steps = tt_ceil_div(steps, g.batch);  // of a group of the average size
+    long long split = 512 / n;
+    if (split > steps / 8) split = steps / 8;
+    if (split > 64) split = 64;
+    if (split > 1) h.split = (int)split;
+  }
+  return h;
+}
+
+template <class T, class O, int P, int E> void launch_e(const TTGemm &g, const Shape &h, float *part, hipStream_t s) {
+  const dim3 grid((unsigned)(h.m_tiles * h.n_tiles), (unsigned)h.members, (unsigned)h.split);
+  const int mti = (int)h.m_tiles, nti = (int)h.n_tiles, split = h.split;
+  if (g.a_kc && g.b_kc) hipLaunchKernelGGL((k_gemm<T, O, P, true, true, E>), grid, dim3(TT_BLOCK), 0, s, g, mti, nti, split, part);
+  else if (g.a_kc) hipLaunchKernelGGL((k_gemm<T, O, P, true, false, E>), grid, dim3(TT_BLOCK), 0, s, g, mti, nti, split, part);
+  else hipLaunchKernelGGL((k_gemm<T, O, P, false, false, E>), grid, dim3(TT_BLOCK), 0, s, g, mti, nti, split, part);
+}
+template <class T, class O, int P> tt_status launch(const TTGemm &g, void *partial, hipStream_t s) {
+  const Shape h = shape_of(g);
+  if (h.m_tiles * h.n_tiles > TT_MAX_WORKGROUPS || h.m_tiles * h.n_tiles * h.members * h.split > TT_MAX_WORKGROUPS || h.members > 65535)
+    return TT_ERR_SHAPE;
+  if (h.split > 1 && !partial) return TT_ERR_WORKSPACE;
+  float *part = (float *)partial;
+  if (h.e == 128) launch_e<T, O, P, 128>(g, h, part, s);
+  else launch_e<T, O, P, 64>(g, h, part, s);
+  if (h.split > 1) {
+    long long blocks = ((long long)g.M * ((g.N + 3) / 4) + g.M + TT_BLOCK - 1) / TT_BLOCK;
+    if (blocks > 4096) blocks = 4096;
+    const int split = h.split;
+    hipLaunchKernelGGL((k_join<T, O>), dim3((unsigned)blocks, (unsigned)h.members), dim3(TT_BLOCK), 0, s, g, split, (const float *)part);
+  }
+  return tt_launch_status();
 }
 
 }  // namespace
 
-tt_status ttk_gemm(const TTGemm &g, hipStream_t s) {
+size_t ttk_gemm_partial_bytes(const TTGemm &g) {
+  if (g.M < 1 || g.N < 1 || g.batch < 1) return 0;
+  const Shape h = shape_of(g);
+  return h.split < 2 ? 0 : (((size_t)h.split * g.batch * g.M * (g.N + 1LL) * 4) + 255) & ~(size_t)255;
+}
+
+tt_status ttk_gemm(const TTGemm &g, void *partial, hipStream_t s) {
   if (g.M < 1 || g.N < 1 || g.batch < 1) return TT_OK;
-  const long long n_tiles = tt_ceil_div(g.N, GT);
-  // every group ends in at most one part tile; one more for the rows outside the groups
-  const long long m_tiles = g.mode == TT_GEMM_RAGGED_M ? (long long)tt_ceil_div(g.M, GT) + g.batch + 1 : tt_ceil_div(g.M, GT);
-  const long long members = g.mode == TT_GEMM_RAGGED_M ? 1 : g.batch;
-  if (m_tiles * members > TT_MAX_WORKGROUPS || m_tiles * members * n_tiles > TT_MAX_WORKGROUPS) return TT_ERR_SHAPE;
-  const unsigned blocks = (unsigned)(m_tiles * members * n_tiles);
   if (!g.a_kc && g.b_kc) return TT_ERR_INVALID_ARG;  // no caller needs it
-  if (g.dtype == TT_F32 && g.out_dtype == TT_F32) launch_general<float, float>(g, blocks, (int)m_tiles, (int)n_tiles, s);
-  else if (g.dtype == TT_F32 && g.out_dtype == TT_BF16) launch_general<float, ttg::bf16>(g, blocks, (int)m_tiles, (int)n_tiles, s);
-  else if (g.dtype == TT_F32 && g.out_dtype == TT_F16) launch_general<float, ttg::f16>(g, blocks, (int)m_tiles, (int)n_tiles, s);
-  else if (g.dtype == TT_BF16 && g.out_dtype == TT_BF16) launch_general<ttg::bf16, ttg::bf16>(g, blocks, (int)m_tiles, (int)n_tiles, s);
-  else if (g.dtype == TT_F16 && g.out_dtype == TT_F16) launch_general<ttg::f16, ttg::f16>(g, blocks, (int)m_tiles, (int)n_tiles, s);
-  else return TT_ERR_INVALID_ARG;
-  return tt_launch_status();
+  if (g.dtype == TT_BF16 && g.out_dtype == TT_BF16) return launch<ttg::bf16, ttg::bf16, 1>(g, partial, s);
+  if (g.dtype == TT_F16 && g.out_dtype == TT_F16) return launch<ttg::f16, ttg::f16, 1>(g, partial, s);
+  if (g.dtype != TT_F32) return TT_ERR_INVALID_ARG;
+  if (g.parts == 3 && g.out_dtype == TT_F32) return launch<float, float, 3>(g, partial, s);
+  if (g.parts == 2 && g.out_dtype == TT_F32) return launch<float, float, 2>(g, partial, s);
+  if (g.parts == 2 && g.out_dtype == TT_BF16) return launch<float, ttg::bf16, 2>(g, partial, s);
+  if (g.parts == 2 && g.out_dtype == TT_F16) return launch<float, ttg::f16, 2>(g, partial, s);
+  return TT_ERR_INVALID_ARG;
 }

@@ -67,18 +67,61 @@ __global__ void __launch_bounds__(TT_BLOCK) k_scale_in(const T *__restrict__ g, 
   }
 }
 
-struct Scratch {
-  size_t partial, x0, x1, a, b, total;
+// The three products of a step, without their operands' addresses.  For results in 16 bits two bf16 parts of each operand are
+// multiplied (16 bits of significand: five steps take errors up 485 times at most, in a few directions), for fp32 three.
+struct Products {
+  TTGemm gram, square, move;
 };
-Scratch scratch(long long batch, long long rows, long long cols) {
+Products products(const Mats &m, int dtype) {
+  const bool tall = m.rows > m.cols;
+  const int side = tall ? m.cols : m.rows;
+  const long long elems = (long long)m.rows * m.cols, sq = (long long)side * side;
+  Products p;
+  TTGemm g;
+  memset(&g, 0, sizeof(g));
+  g.dtype = g.out_dtype = TT_F32;
+  g.mode = TT_GEMM_BATCH;
+  g.batch = (int)m.batch;
+  g.alpha = 1.f;
+  g.parts = dtype == TT_F32 ? 3 : 2;
+  // A = X X^T, or X^T X
+  p.gram = g;
+  p.gram.a_kc = p.gram.b_kc = tall ? 0 : 1;
+  p.gram.M = p.gram.N = side; p.gram.K = tall ? m.rows : m.cols;
+  p.gram.lda = p.gram.ldb = m.cols; p.gram.a_step = p.gram.b_step = elems;
+  p.gram.ldo = side; p.gram.o_step = sq;
+  // B = b A + c A A (A is symmetric)
+  p.square = g;
+  p.square.a_kc = p.square.b_kc = 1;
+  p.square.M = p.square.N = p.square.K = side;
+  p.square.lda = p.square.ldb = p.square.ldo = p.square.ldr = side;
+  p.square.a_step = p.square.b_step = p.square.o_step = p.square.r_step = sq;
+  // X <- a X + B X, or a X + X B (B is symmetric)
+  p.move = g;
+  p.move.a_kc = 1; p.move.b_kc = tall ? 1 : 0;
+  p.move.M = m.rows; p.move.N = m.cols; p.move.K = side;
+  p.move.lda = side; p.move.a_step = tall ? elems : sq;
+  p.move.ldb = m.cols; p.move.b_step = tall ? sq : elems;
+  p.move.ldr = p.move.ldo = m.cols; p.move.r_step = p.move.o_step = elems;
+  return p;
+}
+
+struct Scratch {
+  size_t partial, x0, x1, a, b, pieces, total;
+};
+Scratch scratch(long long batch, long long rows, long long cols, int dtype) {
   Scratch w;
-  const long long elems = rows * cols, m = rows < cols ? rows : cols;
+  const long long elems = rows * cols, side = rows < cols ? rows : cols;
   w.partial = 0;
   w.x0 = pad256((size_t)batch * parts_of(elems) * 8);
   w.x1 = w.x0 + pad256((size_t)batch * elems * 4);
   w.a = w.x1 + pad256((size_t)batch * elems * 4);
-  w.b = w.a + pad256((size_t)batch * m * m * 4);
-  w.total = w.b + pad256((size_t)batch * m * m * 4);
+  w.b = w.a + pad256((size_t)batch * side * side * 4);
+  w.pieces = w.b + pad256((size_t)batch * side * side * 4);
+  Mats m = {batch, (int)rows, (int)cols, 0, 0};
+  const Products p = products(m, dtype);
+  const size_t n[3] = {ttk_gemm_partial_bytes(p.gram), ttk_gemm_partial_bytes(p.square), ttk_gemm_partial_bytes(p.move)};
+  w.total = w.pieces + (n[0] > n[1] ? (n[0] > n[2] ? n[0] : n[2]) : (n[1] > n[2] ? n[1] : n[2]));
   return w;
 }
 
@@ -92,49 +135,34 @@ tt_status scale_in(const void *g, const Mats &m, float eps, char *ws, const Scra
   return tt_launch_status();
 }
 
-// The iteration, all in fp32 (the polynomial takes small singular values up 485 times in five steps, and with them the rounding
-// errors that they carry).
+// The iteration.  X, A and B stay in fp32 (the polynomial takes small singular values up 485 times in five steps, and with them
+// the rounding errors that they carry).
 tt_status iterate(const Mats &m, const Steps &steps, int out_dtype, void *out, long long o_step, long long ldo, char *ws, const Scratch &w,
                   hipStream_t s) {
   const bool tall = m.rows > m.cols;
-  const int side = tall ? m.cols : m.rows;
-  const long long elems = (long long)m.rows * m.cols, sq = (long long)side * side;
   float *x = (float *)(ws + w.x0), *y = (float *)(ws + w.x1), *A = (float *)(ws + w.a), *B = (float *)(ws + w.b);
+  Products p = products(m, out_dtype);
   for (int i = 0; i < steps.n; ++i) {
     const float ca = steps.c[3 * i], cb = steps.c[3 * i + 1], cc = steps.c[3 * i + 2];
-    TTGemm g;
-    memset(&g, 0, sizeof(g));
-    g.dtype = g.out_dtype = TT_F32;
-    g.mode = TT_GEMM_BATCH;
-    g.batch = (int)m.batch;
-    g.alpha = 1.f;
-    // A = X X^T, or X^T X
-    g.a_kc = g.b_kc = tall ? 0 : 1;
-    g.M = g.N = side; g.K = tall ? m.rows : m.cols;
-    g.a = g.b = x; g.lda = g.ldb = m.cols; g.a_step = g.b_step = elems;
-    g.out = A; g.ldo = side; g.o_step = sq;
-    tt_status st = ttk_gemm(g, s);
+    p.gram.a = p.gram.b = x;
+    p.gram.out = A;
+    tt_status st = ttk_gemm(p.gram, ws + w.pieces, s);
     if (st != TT_OK) return st;
-    // B = b A + c A A (A is symmetric)
-    g.a_kc = g.b_kc = 1;
-    g.K = side;
-    g.a = g.b = A; g.lda = g.ldb = side; g.a_step = g.b_step = sq;
-    g.out = B;
-    g.res = A; g.ldr = side; g.r_step = sq;
-    g.alpha = cc; g.beta = cb;
-    st = ttk_gemm(g, s);
+    p.square.a = p.square.b = p.square.res = A;
+    p.square.out = B;
+    p.square.alpha = cc; p.square.beta = cb;
+    st = ttk_gemm(p.square, ws + w.pieces, s);
     if (st != TT_OK) return st;
-    // X <- a X + B X, or a X + X B (B is symmetric)
-    const bool last = i + 1 == steps.n;
-    g.M = m.rows; g.N = m.cols;
-    g.a = tall ? x : B; g.lda = side; g.a_step = tall ? elems : sq;
-    g.b = tall ? B : x; g.ldb = m.cols; g.b_step = tall ? sq : elems;
-    g.b_kc = tall ? 1 : 0;
-    g.res = x; g.ldr = m.cols; g.r_step = elems;
-    g.alpha = 1.f; g.beta = ca;
-    g.out = last ? out : (void *)y; g.ldo = last ? ldo : m.cols; g.o_step = last ? o_step : elems;
-    g.out_dtype = last ? out_dtype : TT_F32;
-    st = ttk_gemm(g, s);
+    p.move.a = tall ? x : B;
+    p.move.b = tall ? B : x;
+    p.move.res = x;
+    p.move.beta = ca;
+    p.move.out = y;
+    if (i + 1 == steps.n) {
+      p.move.out = out; p.move.ldo = ldo; p.move.o_step = o_step;
+      p.move.out_dtype = out_dtype;
+    }
+    st = ttk_gemm(p.move, ws + w.pieces, s);
     if (st != TT_OK) return st;
     float *t = x; x = y; y = t;
   }
@@ -201,7 +229,7 @@ size_t core_elems(const Mats &m) { return (size_t)m.batch * m.b_step; }
 
 extern "C" size_t tt_orthogonalize_workspace_bytes(const tt_matrices *m) {
   if (!m || m->dtype < TT_F32 || m->dtype > TT_F16 || !size_ok(m->batch, m->rows, m->cols)) return 0;
-  return m->batch == 0 ? 256 : scratch(m->batch, m->rows, m->cols).total;
+  return m->batch == 0 ? 256 : scratch(m->batch, m->rows, m->cols, m->dtype).total;
 }
 
 extern "C" tt_status tt_orthogonalize(const tt_matrices *m, const void *g, void *out, int steps, const float *coefficients, float eps, void *workspace,
@@ -218,7 +246,7 @@ extern "C" tt_status tt_orthogonalize(const tt_matrices *m, const void *g, void 
   in.b_step = m->batch_step ? m->batch_step : in.r_step * m->rows;
   const long long ldo = m->out_row_step ? m->out_row_step : m->cols, o_step = m->out_batch_step ? m->out_batch_step : ldo * m->rows;
   if (in.r_step < m->cols || ldo < m->cols || in.b_step < 0 || o_step < ldo * (m->rows - 1) + m->cols) return TT_ERR_SHAPE;
-  const Scratch w = scratch(m->batch, m->rows, m->cols);
+  const Scratch w = scratch(m->batch, m->rows, m->cols, m->dtype);
   if (!workspace || ((uintptr_t)workspace & 255) != 0 || workspace_bytes < w.total) return TT_ERR_WORKSPACE;
   hipStream_t s = (hipStream_t)stream;
   char *ws = (char *)workspace;
@@ -235,7 +263,7 @@ extern "C" size_t tt_core_ortho_workspace_bytes(const tt_table *table) {
   for (int k = 0; k < 3; ++k) {
     const Mats m = slices(table, k);
     if (!size_ok(m.batch, m.rows, m.cols)) return 0;
-    const size_t n = scratch(m.batch, m.rows, m.cols).total + 2 * pad256(core_elems(m) * 4);
+    const size_t n = scratch(m.batch, m.rows, m.cols, TT_F32).total + 2 * pad256(core_elems(m) * 4);
     if (n > most) most = n;
   }
   return most;
@@ -254,7 +282,7 @@ extern "C" tt_status tt_core_ortho_update(const tt_table *table, const float *co
   hipStream_t s = (hipStream_t)stream;
   for (int k = 0; k < 3; ++k) {
     const Mats m = slices(table, k);
-    const Scratch w = scratch(m.batch, m.rows, m.cols);
+    const Scratch w = scratch(m.batch, m.rows, m.cols, TT_F32);
     char *ws = (char *)workspace;
     float *u = (float *)(ws + w.total), *o = (float *)(ws + w.total + pad256(core_elems(m) * 4));
     CoreDims d;

@@ -18,9 +18,11 @@ DT = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 GUARD = 512
 
 
-@pytest.fixture(scope="module")
-def lib():
-    lib = ctypes.CDLL(emu_build.build_shared(BUILD_DIR, "dense"))
+@pytest.fixture(scope="module", params=["small tiles", "large tiles"])
+def lib(request):
+    """The library as it is (these sizes take the small tiles), and with large tiles from the first one on."""
+    large = request.param == "large tiles"
+    lib = ctypes.CDLL(emu_build.build_shared(BUILD_DIR, "dense_large" if large else "dense", ["-DTT_GEMM_LARGE_TILES=1"] if large else []))
     vp, sz, f32 = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_float
     lib.tt_dense_workspace_bytes.restype = lib.tt_orthogonalize_workspace_bytes.restype = lib.tt_core_ortho_workspace_bytes.restype = sz
     lib.tt_dense_workspace_bytes.argtypes = [vp, ctypes.c_int]

@@ -62,6 +62,11 @@ SIZES = [
     (2048, 1024, 256, None, 0, 0),
     (4097, 136, 384, None, 0, 0),
     (5000, 16, 24, None, 0, 0),
+    (2050, 200, 2100, None, 0, 0),
+    (2100, 131, 2049, None, 3, 1),
+    (8200, 2056, 520, None, 8, 0),
+    (6000, 96, 700, (2500, 0, 1, 3499), 0, 0),
+    (5000, 328, 1030, (130, 2700, 5, 2100), 6, 0),
     (30, 128, 512, (3, 0, 1, 26), 0, 0),
     (100, 64, 72, (1,) * 100, 0, 0),
     (515, 128, 128, (0, 256, 0, 1, 258, 0), 0, 0),

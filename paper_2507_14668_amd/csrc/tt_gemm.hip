@@ -210,6 +210,7 @@ __global__ void __launch_bounds__(TT_BLOCK, 2) k_gemm(TTGemm g, int m_tiles, int
   __shared__ __align__(16) unsigned short lds[HALVES > REDO ? HALVES : REDO];
   __shared__ int flags[4];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int members = (int)gridDim.y / split, cut = (int)blockIdx.y / members;  // which piece of K
   unsigned mt, nt;
   tile_order(blockIdx.x, (unsigned)m_tiles, (unsigned)n_tiles, mt, nt);
   Place w;
@@ -223,14 +224,14 @@ __global__ void __launch_bounds__(TT_BLOCK, 2) k_gemm(TTGemm g, int m_tiles, int
       return;
     }
   } else {
-    w.z = (int)blockIdx.y;
+    w.z = (int)blockIdx.y - cut * members;
     w.lo = (int)mt * E;
     w.hi = g.M < w.lo + E ? g.M : w.lo + E;
     if (g.mode == TT_GEMM_RAGGED_K) group_rows(g.offsets, w.z, g.K, w.k_lo, w.k_hi);
   }
   if (split > 1) {  // whole steps to each piece
     const int steps = (w.k_hi - w.k_lo + BK - 1) / BK, per = (steps + split - 1) / split;
-    const long long a = (long long)w.k_lo + (long long)blockIdx.z * per * BK, b = a + (long long)per * BK;
+    const long long a = (long long)w.k_lo + (long long)cut * per * BK, b = a + (long long)per * BK;
     if (a < w.k_hi) w.k_lo = (int)a;
     else w.k_lo = w.k_hi;
     if (b < w.k_hi) w.k_hi = (int)b;
@@ -427,7 +428,7 @@ __global__ void __launch_bounds__(TT_BLOCK, 2) k_gemm(TTGemm g, int m_tiles, int
     const int m = w.lo + wm + 16 * x + j;
     if (m >= w.hi) continue;
     if (split > 1) {
-      float *piece = partial + ((long long)blockIdx.z * g.batch + w.z) * g.M * (g.N + 1LL);  // [M][N] sums, then [M] sums of A's rows
+      float *piece = partial + ((long long)cut * g.batch + w.z) * g.M * (g.N + 1LL);  // [M][N] sums, then [M] sums of A's rows
 #pragma unroll
       for (int y = 0; y < F; ++y) {
         const int n = w.n0 + wn + 16 * y + 4 * q, valid = g.N - n < 4 ? g.N - n : 4;
@@ -508,7 +509,7 @@ Shape shape_of(const TTGemm &g) {
 }
 
 template <class T, class O, int P, int E> void launch_e(const TTGemm &g, const Shape &h, float *part, hipStream_t s) {
-  const dim3 grid((unsigned)(h.m_tiles * h.n_tiles), (unsigned)h.members, (unsigned)h.split);
+  const dim3 grid((unsigned)(h.m_tiles * h.n_tiles), (unsigned)(h.members * h.split));
   const int mti = (int)h.m_tiles, nti = (int)h.n_tiles, split = h.split;
   if (g.a_kc && g.b_kc) hipLaunchKernelGGL((k_gemm<T, O, P, true, true, E>), grid, dim3(TT_BLOCK), 0, s, g, mti, nti, split, part);
   else if (g.a_kc) hipLaunchKernelGGL((k_gemm<T, O, P, true, false, E>), grid, dim3(TT_BLOCK), 0, s, g, mti, nti, split, part);
@@ -516,7 +517,7 @@ template <class T, class O, int P, int E> void launch_e(const TTGemm &g, const S
 }
 template <class T, class O, int P> tt_status launch(const TTGemm &g, void *partial, hipStream_t s) {
   const Shape h = shape_of(g);
-  if (h.m_tiles * h.n_tiles > TT_MAX_WORKGROUPS || h.m_tiles * h.n_tiles * h.members * h.split > TT_MAX_WORKGROUPS || h.members > 65535)
+  if (h.m_tiles * h.n_tiles > TT_MAX_WORKGROUPS || h.m_tiles * h.n_tiles * h.members * h.split > TT_MAX_WORKGROUPS || h.members * h.split > 65535)
     return TT_ERR_SHAPE;
   if (h.split > 1 && !partial) return TT_ERR_WORKSPACE;
   float *part = (float *)partial;

@@ -5,6 +5,7 @@
 #include <string.h>
 
 #include "tt_gemm_device.h"
+#include "tt_ortho_slice.h"
 
 namespace {
 using namespace ttg;
@@ -112,6 +113,11 @@ struct Scratch {
 Scratch scratch(long long batch, long long rows, long long cols, int dtype) {
   Scratch w;
   const long long elems = rows * cols, side = rows < cols ? rows : cols;
+  memset(&w, 0, sizeof(w));
+  if (ttk_slices_serves(side, rows < cols ? cols : rows)) {  // these need none
+    w.total = 256;
+    return w;
+  }
   w.partial = 0;
   w.x0 = pad256((size_t)batch * parts_of(elems) * 8);
   w.x1 = w.x0 + pad256((size_t)batch * elems * 4);
@@ -180,7 +186,8 @@ bool size_ok(int64_t batch, int64_t rows, int64_t cols) {
   const int64_t side = rows < cols ? rows : cols;
   // the largest launch is that of 64 x 64 tiles of the matrices
   return batch >= 0 && batch * (rows * cols) < ((int64_t)1 << 36) && batch * (side * side) < ((int64_t)1 << 36) &&
-         batch * tt_ceil_div(rows, 64) * tt_ceil_div(cols, 64) <= TT_MAX_WORKGROUPS && batch * kMaxParts <= TT_MAX_WORKGROUPS;
+         batch * tt_ceil_div(rows, 64) * tt_ceil_div(cols, 64) <= TT_MAX_WORKGROUPS && batch * kMaxParts <= TT_MAX_WORKGROUPS &&
+         (batch <= 65535 || (side <= 64 && (rows > cols ? rows : cols) <= 512));  // (larger matrices: one of a grid's second side each)
 }
 
 // ---- TT cores --------------------------------------------------------------------------------------
@@ -205,6 +212,21 @@ __global__ void __launch_bounds__(TT_BLOCK) k_core_momentum(CoreDims d, const fl
 __global__ void __launch_bounds__(TT_BLOCK) k_core_apply(CoreDims d, float *__restrict__ core, const float *__restrict__ packed, float lr) {
   const long long total = (long long)d.r * d.n * d.c, stride = (long long)gridDim.x * blockDim.x;
   for (long long e = (long long)blockIdx.x * blockDim.x + threadIdx.x; e < total; e += stride) core[e] -= lr * packed[packed_of(d, e)];
+}
+
+// A batch of matrices that the kernels of one launch serve.
+TTSlices slices_of(const Mats &m, int dtype, const Steps &steps, float eps) {
+  const bool tall = m.rows > m.cols;
+  TTSlices p;
+  memset(&p, 0, sizeof(p));
+  p.dtype = dtype;
+  p.shorter = tall ? m.cols : m.rows;
+  p.longer = tall ? m.rows : m.cols;
+  p.batch = m.batch;
+  p.eps = eps;
+  p.steps = steps.n;
+  memcpy(p.c, steps.c, sizeof(float) * 3 * steps.n);
+  return p;
 }
 
 bool table_ok(const tt_table *t) {
@@ -250,6 +272,13 @@ extern "C" tt_status tt_orthogonalize(const tt_matrices *m, const void *g, void 
   if (!workspace || ((uintptr_t)workspace & 255) != 0 || workspace_bytes < w.total) return TT_ERR_WORKSPACE;
   hipStream_t s = (hipStream_t)stream;
   char *ws = (char *)workspace;
+  if (ttk_slices_serves(m->rows < m->cols ? m->rows : m->cols, m->rows < m->cols ? m->cols : m->rows)) {
+    const bool tall = m->rows > m->cols;
+    TTSlices p = slices_of(in, m->dtype, Steps{steps, coefficients}, eps);
+    p.in = g; p.in_b = in.b_step; p.in_s = tall ? 1 : in.r_step; p.in_l = tall ? in.r_step : 1;
+    p.out = out; p.out_b = o_step; p.out_s = tall ? 1 : ldo; p.out_l = tall ? ldo : 1;
+    return ttk_slices(p, s);
+  }
   tt_status st = m->dtype == TT_F32    ? scale_in<float>(g, in, eps, ws, w, s)
                  : m->dtype == TT_BF16 ? scale_in<ttg::bf16>(g, in, eps, ws, w, s)
                                        : scale_in<ttg::f16>(g, in, eps, ws, w, s);
@@ -263,7 +292,8 @@ extern "C" size_t tt_core_ortho_workspace_bytes(const tt_table *table) {
   for (int k = 0; k < 3; ++k) {
     const Mats m = slices(table, k);
     if (!size_ok(m.batch, m.rows, m.cols)) return 0;
-    const size_t n = scratch(m.batch, m.rows, m.cols, TT_F32).total + 2 * pad256(core_elems(m) * 4);
+    const bool served = ttk_slices_serves(m.rows < m.cols ? m.rows : m.cols, m.rows < m.cols ? m.cols : m.rows);
+    const size_t n = scratch(m.batch, m.rows, m.cols, TT_F32).total + (served ? 0 : 2 * pad256(core_elems(m) * 4));
     if (n > most) most = n;
   }
   return most;
@@ -291,11 +321,24 @@ extern "C" tt_status tt_core_ortho_update(const tt_table *table, const float *co
     if (blocks > 8192) blocks = 8192;
     const float *grad = dcore[k];
     float *mom = momentum[k], *core = table->core[k];
+    const float rate = (float)((double)lr * sqrt(m.rows > m.cols ? (double)m.rows / m.cols : 1.0));
+    const bool tall = m.rows > m.cols;
+    if (ttk_slices_serves(tall ? m.cols : m.rows, tall ? m.rows : m.cols)) {
+      TTSlices p = slices_of(m, TT_F32, Steps{steps, coefficients}, eps);
+      const long long row = k == 0 ? m.cols : (long long)m.batch * m.cols;  // between a slice's rows; slices are a row apart, in core 0 whole
+      p.in = grad; p.out = core; p.mom = mom;
+      p.in_b = p.out_b = k == 0 ? m.b_step : m.cols;
+      p.in_s = p.out_s = tall ? 1 : row;
+      p.in_l = p.out_l = tall ? row : 1;
+      p.mu = mu; p.rate = rate; p.nesterov = nesterov;
+      const tt_status st = ttk_slices(p, s);
+      if (st != TT_OK) return st;
+      continue;
+    }
     hipLaunchKernelGGL(k_core_momentum, dim3((unsigned)blocks), dim3(TT_BLOCK), 0, s, d, grad, mom, mu, nesterov, u);
     tt_status st = scale_in<float>(u, m, eps, ws, w, s);
     if (st == TT_OK) st = iterate(m, Steps{steps, coefficients}, TT_F32, o, m.b_step, m.r_step, ws, w, s);
     if (st != TT_OK) return st;
-    const float rate = (float)((double)lr * sqrt(m.rows > m.cols ? (double)m.rows / m.cols : 1.0));
     hipLaunchKernelGGL(k_core_apply, dim3((unsigned)blocks), dim3(TT_BLOCK), 0, s, d, core, (const float *)o, rate);
     st = tt_launch_status();
     if (st != TT_OK) return st;

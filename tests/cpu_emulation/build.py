@@ -25,7 +25,7 @@ ROOT = os.path.dirname(os.path.dirname(HERE))
 CSRC = os.path.join(ROOT, "paper_2507_14668_amd", "csrc")
 CLANG = os.environ.get("TT_EMU_CXX", "/opt/rocm/llvm/bin/clang++")
 UNITS = ("tt_api", "tt_reorder", "tt_forward", "tt_forward_mfma", "tt_forward_sample", "tt_bf16", "tt_index_graph", "tt_fuse", "tt_backward",
-         "tt_backward_mfma", "tt_gemm", "tt_dense", "tt_ortho")
+         "tt_backward_mfma", "tt_gemm", "tt_dense", "tt_ortho", "tt_ortho_slice")
 
 
 def available() -> bool:
@@ -47,7 +47,7 @@ def _generate(gen: str) -> list:
         path = os.path.join(gen, u + ".cpp")
         open(path, "w").write(text)
         out.append(path)
-    for header in ("tt_internal.h", "tt_gemm.h", "tt_gemm_device.h"):
+    for header in ("tt_internal.h", "tt_gemm.h", "tt_gemm_device.h", "tt_ortho_slice.h"):
         shutil.copy(os.path.join(CSRC, header), gen)
     return out
 

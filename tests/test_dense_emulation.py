@@ -239,7 +239,11 @@ def coefs(*c):
 
 @pytest.mark.parametrize("batch,rows,cols,dtype,pad", [(1, 1, 1, torch.float32, 0), (3, 4, 16, torch.float32, 0), (2, 16, 4, torch.bfloat16, 0),
                                                         (2, 33, 70, torch.float32, 3), (1, 70, 33, torch.float16, 1), (5, 1, 9, torch.float32, 0),
-                                                        (2, 9, 1, torch.float32, 0), (1, 64, 64, torch.bfloat16, 8)])
+                                                        (2, 9, 1, torch.float32, 0), (1, 64, 64, torch.bfloat16, 8),
+                                                        (6, 4, 64, torch.float32, 0), (5, 130, 3, torch.float32, 2), (2, 7, 140, torch.bfloat16, 0),
+                                                        (1, 300, 8, torch.float16, 0), (1, 3, 512, torch.float32, 0), (2, 9, 260, torch.float32, 1),
+                                                        (1, 512, 20, torch.float32, 0), (1, 50, 300, torch.float32, 5), (1, 65, 70, torch.float32, 0),
+                                                        (1, 8, 513, torch.float32, 0)])
 def test_orthogonalize_values(lib, batch, rows, cols, dtype, pad):
     gen = torch.Generator().manual_seed(rows + cols)
     g = (torch.randn(batch, rows, cols, generator=gen) * 1e-3).to(dtype)

@@ -351,7 +351,7 @@ def test_refusals(tt):
             (ValueError, lambda: tt.tt_orthogonalize(w, coefficients=((1, 2, 3), (1, 2, 3)))),
             (ValueError, lambda: tt.tt_orthogonalize(w, out=w[:4])),
             (tt.TTError, lambda: tt.tt_orthogonalize(w, eps=-1.0)),
-            (tt.TTError, lambda: tt.tt_orthogonalize(w, workspace=torch.empty(256, dtype=torch.uint8, device="cuda"))),
+            (tt.TTError, lambda: tt.tt_orthogonalize(w, workspace=torch.empty(128, dtype=torch.uint8, device="cuda"))),
             (tt.TTError, lambda: tt.tt_dense_backward(x, w, grad, x[:, :8].contiguous(), "silu", workspace=torch.empty(0, dtype=torch.uint8, device="cuda")))):
         with pytest.raises(error):
             call()

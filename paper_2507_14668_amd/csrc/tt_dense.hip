@@ -31,23 +31,23 @@ long long step(int64_t ld, int dim) { return ld ? ld : dim; }
 template <class T>
 __global__ void __launch_bounds__(TT_BLOCK) k_act_grad(const T *__restrict__ grad, long long ldg, const T *__restrict__ pre, T *__restrict__ dz,
                                                        long long rows, int n, int act) {
-  const int per = (n + 3) / 4;
+  const int per = (n + 7) / 8;
   const long long total = rows * per, stride = (long long)gridDim.x * blockDim.x;
   for (long long e = (long long)blockIdx.x * blockDim.x + threadIdx.x; e < total; e += stride) {
-    const long long r = e / per;
-    const int c = (int)(e - r * per) * 4, valid = n - c < 4 ? n - c : 4;
-    float v[4], z[4];
-    load4(grad + r * ldg + c, valid, v);
-    load4(pre + r * n + c, valid, z);
+    const long long r = total < 2147483648LL ? (long long)((unsigned)e / (unsigned)per) : e / per;  // (a 64-bit division costs as much as the rest)
+    const int c = (int)(e - r * per) * 8, valid = n - c;
+    float v[8], z[8];
+    load_n<T, 8>(grad + r * ldg + c, valid, v);
+    load_n<T, 8>(pre + r * n + c, valid, z);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] *= act_slope(z[i], act);
-    store4(dz + r * n + c, valid, v);
+    for (int i = 0; i < 8; ++i) v[i] *= slope_of<T>(z[i], act);
+    store_n<T, 8>(dz + r * n + c, valid, v);
   }
 }
 
 template <class T>
 tt_status act_grad(const tt_dense *op, const void *grad, const void *pre, void *dz, hipStream_t s) {
-  const long long total = op->rows * ((op->out_dim + 3) / 4);
+  const long long total = op->rows * ((op->out_dim + 7) / 8);
   long long blocks = (total + TT_BLOCK - 1) / TT_BLOCK;
   if (blocks > 16384) blocks = 16384;
   const long long ldg = step(op->ld_grad, op->out_dim);

@@ -40,3 +40,7 @@ struct TTGemm {
 size_t ttk_gemm_partial_bytes(const TTGemm &g);  // 0: not split
 // Enqueues the product.  partial: ttk_gemm_partial_bytes(g) bytes of DEVICE memory, 256-byte aligned.
 tt_status ttk_gemm(const TTGemm &g, void *partial, hipStream_t s);
+
+// Large 16-bit products on aligned operands (tt_gemm_direct.hip); ttk_gemm passes them on.
+bool ttk_gemm_direct_serves(const TTGemm &g);
+tt_status ttk_gemm_direct(const TTGemm &g, hipStream_t s);

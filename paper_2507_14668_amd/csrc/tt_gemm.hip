@@ -138,60 +138,6 @@ template <bool KC, int LD32> __device__ __forceinline__ f32x4 frag32(const float
   return v;
 }
 
-// ---- which tile ------------------------------------------------------------------------------------
-struct Place {
-  int z, lo, hi, n0;  // member / group; rows [lo, hi) of out; first column
-  int k_lo, k_hi;     // values of K of this workgroup (stored rows in RAGGED_K)
-};
-// Workgroups go round the eight dies by their number; each die gets neighbouring tiles, and within them eight row tiles
-// take a column tile together, so that what they read of both operands is in the die's L2.
-__device__ __forceinline__ void tile_order(unsigned t, unsigned m_tiles, unsigned n_tiles, unsigned &mt, unsigned &nt) {
-  const unsigned total = m_tiles * n_tiles, per = total / 8, left = total % 8, die = t % 8;
-  t = die * per + (die < left ? die : left) + t / 8;
-  const unsigned band = t / (8 * n_tiles), rows = m_tiles - 8 * band < 8 ? m_tiles - 8 * band : 8, in = t - band * 8 * n_tiles;
-  mt = 8 * band + in % rows;
-  nt = in / rows;
-}
-
-// RAGGED_M: clears the rows that no group covers; `idx` of `n` workgroups that found no tile, for columns n0 .. n0 + width
-template <class O> __device__ __forceinline__ void clear_rest(const TTGemm &g, int above, int covered, int idx, int n, int n0, int width) {
-  const float zero[4] = {0.f, 0.f, 0.f, 0.f};
-  const long long rest = (long long)above + g.M - covered;
-  const int end = g.N < n0 + width ? g.N : n0 + width;
-  for (long long r = (long long)idx * 4 + (threadIdx.x >> 6); r < rest; r += (long long)n * 4)
-    for (int c = n0 + 4 * (threadIdx.x & 63); c < end; c += 256)
-      store4((O *)g.out + (r < above ? r : r - above + covered) * g.ldo + c, end - c < 4 ? end - c : 4, zero);
-}
-
-// out[m][n .. n + 3] from four sums
-template <class T, class O>
-__device__ __forceinline__ void epilogue4(const TTGemm &g, int z, int m, int n, const f32x4 &acc) {
-  const int valid = g.N - n < 4 ? g.N - n : 4;
-  float v[4], t[4];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) v[i] = g.alpha * acc[i];
-  if (g.bias) {
-    load4((const T *)g.bias + z * g.bias_step + n, valid, t);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] += t[i];
-  }
-  if (g.pre) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) t[i] = keep_sign<O>(v[i]);
-    store4((O *)g.pre + z * g.p_step + (long long)m * g.ldp + n, valid, t);
-  }
-  if (g.act != TT_ACT_NONE) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = act_value(v[i], g.act);
-  }
-  if (g.res) {
-    load4((const T *)g.res + z * g.r_step + (long long)m * g.ldr + n, valid, t);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] += g.beta * t[i];
-  }
-  store4((O *)g.out + z * g.o_step + (long long)m * g.ldo + n, valid, v);
-}
-
 // ---- the tile kernel -------------------------------------------------------------------------------
 // E x E of out per workgroup (E = 128, or 64 where there are few tiles), four wavefronts of a quarter each, any size, row step and alignment down to the element's; elements
 // outside are zeros.  The product is formed as out^T (B's rows are the instruction's M side), so that a lane's four results are
@@ -423,12 +369,12 @@ __global__ void __launch_bounds__(TT_BLOCK, 2) k_gemm(TTGemm g, int m_tiles, int
     }
   }
   const int q = lane >> 4, j = lane & 15;
+  if (split > 1) {
+    float *piece = partial + ((long long)cut * g.batch + w.z) * g.M * (g.N + 1LL);  // [M][N] sums, then [M] sums of A's rows
 #pragma unroll
-  for (int x = 0; x < F; ++x) {
-    const int m = w.lo + wm + 16 * x + j;
-    if (m >= w.hi) continue;
-    if (split > 1) {
-      float *piece = partial + ((long long)cut * g.batch + w.z) * g.M * (g.N + 1LL);  // [M][N] sums, then [M] sums of A's rows
+    for (int x = 0; x < F; ++x) {
+      const int m = w.lo + wm + 16 * x + j;
+      if (m >= w.hi) continue;
 #pragma unroll
       for (int y = 0; y < F; ++y) {
         const int n = w.n0 + wn + 16 * y + 4 * q, valid = g.N - n < 4 ? g.N - n : 4;
@@ -436,15 +382,18 @@ __global__ void __launch_bounds__(TT_BLOCK, 2) k_gemm(TTGemm g, int m_tiles, int
         if (valid > 0) store4(piece + (long long)m * g.N + n, valid, v);
       }
       if (sums && wn == 0 && q == 0) piece[(long long)g.M * g.N + m] = rs[x][0];
-      continue;
     }
-#pragma unroll
-    for (int y = 0; y < F; ++y) {
-      const int n = w.n0 + wn + 16 * y + 4 * q;
-      if (n < g.N) epilogue4<T, O>(g, w.z, m, n, acc[x][y]);
-    }
-    if (sums && wn == 0 && q == 0) ((O *)g.rowsum)[w.z * g.rs_step + m] = from_f32<O>(rs[x][0]);
+    return;
   }
+  if (sums && wn == 0 && q == 0) {
+#pragma unroll
+    for (int x = 0; x < F; ++x) {
+      const int m = w.lo + wm + 16 * x + j;
+      if (m < w.hi) ((O *)g.rowsum)[w.z * g.rs_step + m] = from_f32<O>(rs[x][0]);
+    }
+  }
+  __syncthreads();  // nobody reads the operands any more
+  finish_tile<T, O, F, F>(g, w.z, w.lo + wm, w.hi, w.n0 + wn, acc, reinterpret_cast<float *>(lds) + wave * 16 * (16 * F + 4));
 }
 
 // The pieces of a split product, added in order; four columns of a row per thread.
@@ -469,7 +418,8 @@ template <class T, class O> __global__ void __launch_bounds__(TT_BLOCK) k_join(T
 #pragma unroll
       for (int c = 0; c < 4; ++c) s[c] += t[c];
     }
-    epilogue4<T, O>(g, z, m, n, s);
+    float v[4] = {s[0], s[1], s[2], s[3]};
+    finish<T, O, 4>(g, z, m, n, valid, v);
   }
 }
 
@@ -543,6 +493,7 @@ size_t ttk_gemm_partial_bytes(const TTGemm &g) {
 tt_status ttk_gemm(const TTGemm &g, void *partial, hipStream_t s) {
   if (g.M < 1 || g.N < 1 || g.batch < 1) return TT_OK;
   if (!g.a_kc && g.b_kc) return TT_ERR_INVALID_ARG;  // no caller needs it
+  if (ttk_gemm_direct_serves(g)) return ttk_gemm_direct(g, s);
   if (g.dtype == TT_BF16 && g.out_dtype == TT_BF16) return launch<ttg::bf16, ttg::bf16, 1>(g, partial, s);
   if (g.dtype == TT_F16 && g.out_dtype == TT_F16) return launch<ttg::f16, ttg::f16, 1>(g, partial, s);
   if (g.dtype != TT_F32) return TT_ERR_INVALID_ARG;

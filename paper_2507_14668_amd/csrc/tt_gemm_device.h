@@ -56,6 +56,32 @@ template <class T> __device__ __forceinline__ void store4(T *p, int valid, const
   }
 }
 
+template <class T, int C> __device__ __forceinline__ void load_n(const T *p, int valid, float v[C]) {
+  if constexpr (C == 8 && sizeof(T) == 2) {
+    if (valid >= 8) {
+      const typename Vec<T>::v16b r = *reinterpret_cast<const typename Vec<T>::v16b *>(p);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = to_f32(__builtin_bit_cast(T, (unsigned short)r[i]));
+      return;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < C; i += 4) load4(p + i, valid - i, v + i);
+}
+template <class T, int C> __device__ __forceinline__ void store_n(T *p, int valid, const float v[C]) {
+  if constexpr (C == 8 && sizeof(T) == 2) {
+    if (valid >= 8) {
+      typename Vec<T>::v16b r;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) r[i] = __builtin_bit_cast(unsigned short, from_f32<T>(v[i]));
+      *reinterpret_cast<typename Vec<T>::v16b *>(p) = r;
+      return;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < C; i += 4) store4(p + i, valid - i, v + i);
+}
+
 // ---- activations ---------------------------------------------------------------------------------
 // With the slope taken from the stored pre-activation: NaN passes through both, relu has slope 0 at 0.
 __device__ __forceinline__ float act_value(float z, int act) {
@@ -84,6 +110,40 @@ __device__ __forceinline__ float act_slope(float z, int act) {
       return s * t;
     }
     default: return 1.f;
+  }
+}
+// The same for results of 16 bits.  exp and the reciprocal are the hardware's (good to a few units of 2^-24); Phi is by the
+// rational approximation 7.1.26 of Abramowitz and Stegun, off by at most 7.5e-8, which is below half a step of either type wherever z Phi(z) is
+// not itself below 1e-4 of |z|.  erfc as the library has it costs 100 us of vector instructions over 16384 x 4096 results, this 35.
+__device__ __forceinline__ float fast_sigmoid(float z) { return __builtin_amdgcn_rcpf(1.f + __expf(-z)); }
+__device__ __forceinline__ float fast_phi(float z, float e) {  // e = exp(-z^2 / 2)
+  const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(z), 0.3275911f * 0.70710678118654752f, 1.f));
+  const float p = 0.5f * e * t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
+  return z < 0.f ? p : 1.f - p;
+}
+template <class O> __device__ __forceinline__ float act_of(float z, int act) {
+  if constexpr (sizeof(O) == 4) return act_value(z, act);
+  switch (act) {
+    case TT_ACT_RELU: return z <= 0.f ? 0.f : z;
+    case TT_ACT_GELU: return z * fast_phi(z, __expf(-0.5f * z * z));
+    case TT_ACT_SILU: return z * fast_sigmoid(z);
+    case TT_ACT_SIGMOID: return fast_sigmoid(z);
+    default: return z;
+  }
+}
+template <class O> __device__ __forceinline__ float slope_of(float z, int act) {
+  if constexpr (sizeof(O) == 4) return act_slope(z, act);
+  switch (act) {
+    case TT_ACT_GELU: {
+      const float e = __expf(-0.5f * z * z);  // 0 for large z: the product below must not be inf * 0
+      return fast_phi(z, e) + (e == 0.f ? 0.f : z * e * 0.39894228040143268f);
+    }
+    case TT_ACT_SILU: {
+      const float s = fast_sigmoid(z), t = fast_sigmoid(-z);
+      return s + (s == 0.f || t == 0.f ? 0.f : z * s * t);
+    }
+    case TT_ACT_SIGMOID: return fast_sigmoid(z) * fast_sigmoid(-z);
+    default: return act_slope(z, act);
   }
 }
 // A stored pre-activation keeps its sign: one that would round to zero in half precision becomes the smallest number, so
@@ -169,6 +229,84 @@ __device__ __forceinline__ f32x4 mma(f16, u16x8 a, u16x8 b, f32x4 c) {
 __device__ __forceinline__ u16x4 lds_read_tr(const unsigned short *p) {
   typedef short s4 __attribute__((ext_vector_type(4)));
   return __builtin_bit_cast(u16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4 *)(p)));
+}
+
+// ---- which tile ------------------------------------------------------------------------------------
+struct Place {
+  int z, lo, hi, n0;  // member / group; rows [lo, hi) of out; first column
+  int k_lo, k_hi;     // values of K of this workgroup (stored rows in RAGGED_K)
+};
+// Workgroups go round the eight dies by their number; each die gets neighbouring tiles, and within them eight row tiles
+// take a column tile together, so that what they read of both operands is in the die's L2.
+__device__ __forceinline__ void tile_order(unsigned t, unsigned m_tiles, unsigned n_tiles, unsigned &mt, unsigned &nt) {
+  const unsigned total = m_tiles * n_tiles, per = total / 8, left = total % 8, die = t % 8;
+  t = die * per + (die < left ? die : left) + t / 8;
+  const unsigned band = t / (8 * n_tiles), rows = m_tiles - 8 * band < 8 ? m_tiles - 8 * band : 8, in = t - band * 8 * n_tiles;
+  mt = 8 * band + in % rows;
+  nt = in / rows;
+}
+
+// RAGGED_M: clears the rows that no group covers; `idx` of `n` workgroups that found no tile, for columns n0 .. n0 + width
+template <class O> __device__ __forceinline__ void clear_rest(const TTGemm &g, int above, int covered, int idx, int n, int n0, int width) {
+  const float zero[4] = {0.f, 0.f, 0.f, 0.f};
+  const long long rest = (long long)above + g.M - covered;
+  const int end = g.N < n0 + width ? g.N : n0 + width;
+  for (long long r = (long long)idx * 4 + (threadIdx.x >> 6); r < rest; r += (long long)n * 4)
+    for (int c = n0 + 4 * (threadIdx.x & 63); c < end; c += 256)
+      store4((O *)g.out + (r < above ? r : r - above + covered) * g.ldo + c, end - c < 4 ? end - c : 4, zero);
+}
+
+// out[m][n .. n + C - 1] from C = 4 or 8 sums, of which `valid` columns exist
+template <class T, class O, int C>
+__device__ __forceinline__ void finish(const TTGemm &g, int z, int m, int n, int valid, float v[C]) {
+  float t[C];
+#pragma unroll
+  for (int i = 0; i < C; ++i) v[i] *= g.alpha;
+  if (g.bias) {
+    load_n<T, C>((const T *)g.bias + z * g.bias_step + n, valid, t);
+#pragma unroll
+    for (int i = 0; i < C; ++i) v[i] += t[i];
+  }
+  if (g.pre) {
+#pragma unroll
+    for (int i = 0; i < C; ++i) t[i] = keep_sign<O>(v[i]);
+    store_n<O, C>((O *)g.pre + z * g.p_step + (long long)m * g.ldp + n, valid, t);
+  }
+  if (g.act != TT_ACT_NONE) {
+#pragma unroll
+    for (int i = 0; i < C; ++i) v[i] = act_of<O>(v[i], g.act);
+  }
+  if (g.res) {
+    load_n<T, C>((const T *)g.res + z * g.r_step + (long long)m * g.ldr + n, valid, t);
+#pragma unroll
+    for (int i = 0; i < C; ++i) v[i] = fmaf(g.beta, t[i], v[i]);
+  }
+  store_n<O, C>((O *)g.out + z * g.o_step + (long long)m * g.ldo + n, valid, v);
+}
+
+// The results of a wavefront, 16 FX x 16 FY of out from row m0 and column n0, rows below `end`.  The instruction leaves a lane
+// four columns of a row, 8 bytes of a 16-bit row at a time; through 16 rows of LDS (`lds`: 16 x (16 FY + 4) floats of the wavefront's
+// own) a lane gets eight, and what is read and written is whole lines of 128 bytes.  (Measured for 16384 x 4096 x 4096 in bf16 with
+// gelu and residual: 238 us of 700 were the end of the tiles before, 105 now.)
+template <class T, class O, int FX, int FY>
+__device__ __forceinline__ void finish_tile(const TTGemm &g, int z, int m0, int end, int n0, const f32x4 (&acc)[FX][FY], float *lds) {
+  constexpr int LD = 16 * FY + 4, PER = 2 * FY, ROWS = 64 / PER;  // lanes of a row, rows at a time
+  const int lane = threadIdx.x & 63, q = lane >> 4, j = lane & 15, c = 8 * (lane % PER), r = lane / PER;
+  const int valid = g.N - n0 - c;
+#pragma unroll
+  for (int x = 0; x < FX; ++x) {
+#pragma unroll
+    for (int y = 0; y < FY; ++y) *reinterpret_cast<f32x4 *>(lds + j * LD + 16 * y + 4 * q) = acc[x][y];
+    tt_wave_lds_order();
+#pragma unroll
+    for (int h = 0; h < 16 / ROWS; ++h) {
+      const int row = r + h * ROWS, m = m0 + 16 * x + row;
+      const f32x4 a = *reinterpret_cast<const f32x4 *>(lds + row * LD + c), b = *reinterpret_cast<const f32x4 *>(lds + row * LD + c + 4);
+      float v[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+      if (m < end && valid > 0) finish<T, O, 8>(g, z, m, n0 + c, valid, v);
+    }
+    tt_wave_lds_order();
+  }
 }
 
 }  // namespace ttg

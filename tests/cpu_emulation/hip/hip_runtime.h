@@ -189,3 +189,12 @@ static inline auto emu_ds_read_tr16(const V *p) {
   return r;
 }
 #define __builtin_amdgcn_ds_read_tr16_b64_v4i16(p) emu_ds_read_tr16((const __typeof__(*(p)) *)(uintptr_t)(p))
+// loads straight into LDS: 16 bytes a lane, lane after lane from the wavefront's address
+static inline void emu_global_load_lds(const void *src, void *lds, int size, int, int) { memcpy((char *)lds + size * __lane(), src, (size_t)size); }
+#define __builtin_amdgcn_global_load_lds(src, lds, size, offset, aux) \
+  emu_global_load_lds((const void *)(uintptr_t)(src), (void *)(uintptr_t)(lds), size, offset, aux)
+#define __builtin_amdgcn_rcpf(x) (1.f / (x))
+#define __expf(x) expf(x)
+static inline void emu_waitcnt(int) {}  // loads are done at once
+#define __builtin_amdgcn_s_waitcnt(n) emu_waitcnt(n)
+#define __builtin_amdgcn_s_barrier() emu::syncthreads()

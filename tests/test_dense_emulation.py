@@ -18,11 +18,13 @@ DT = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 GUARD = 512
 
 
-@pytest.fixture(scope="module", params=["small tiles", "large tiles"])
+VARIANTS = {"small tiles": ("dense", []), "large tiles": ("dense_large", ["-DTT_GEMM_LARGE_TILES=1"]), "direct tiles": ("dense_direct", ["-DTT_GEMM_DIRECT_TILES=1"])}
+
+
+@pytest.fixture(scope="module", params=VARIANTS)
 def lib(request):
-    """The library as it is (these sizes take the small tiles), and with large tiles from the first one on."""
-    large = request.param == "large tiles"
-    lib = ctypes.CDLL(emu_build.build_shared(BUILD_DIR, "dense_large" if large else "dense", ["-DTT_GEMM_LARGE_TILES=1"] if large else []))
+    """The library as it is (these sizes take the small tiles), and with the larger kinds from the first tile on."""
+    lib = ctypes.CDLL(emu_build.build_shared(BUILD_DIR, *VARIANTS[request.param]))
     vp, sz, f32 = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_float
     lib.tt_dense_workspace_bytes.restype = lib.tt_orthogonalize_workspace_bytes.restype = lib.tt_core_ortho_workspace_bytes.restype = sz
     lib.tt_dense_workspace_bytes.argtypes = [vp, ctypes.c_int]
@@ -101,6 +103,8 @@ CASES = [
     (90, 9, 33, torch.float16, "gelu", [5, 8, 80], 2, 1),
     (30, 16, 16, torch.float32, "none", [0, 20, 10, 25], 0, 0),      # not in order: the running maximum counts
     (30, 16, 16, torch.bfloat16, "none", [-4, 12, 99], 0, 0),        # outside: clamped
+    (300, 72, 264, torch.bfloat16, "silu", [0, 130, 130, 299], 8, 0),
+    (270, 136, 40, torch.float16, "relu", None, 0, 0),
     (20, 8, 8, torch.float32, "relu", [20, 20], 0, 0),               # one group, without rows
     (70, 8, 8, torch.float32, "none", [min(i, 70) for i in range(132)], 0, 0),  # 131 groups: more than a wavefront's lanes
 ]

@@ -603,94 +603,100 @@ ORTHO_COEFFICIENTS = (3.4445, -4.7750, 2.0315)
 
 
 class _On:
-    """The tensors' device as the current one, and the work's stream on it."""
+    """The tensors' device as the current one, and the work's stream on it (the calls below take a few microseconds on the
+    host, so what they need of a tensor is asked once)."""
+    __slots__ = ("index", "before", "stream")
 
-    def __init__(self, tensors, stream):
-        self.device = tensors[0].device
-        for t in tensors:
-            if t.device != self.device:
-                raise ValueError("tensors on %s and %s in one call" % (self.device, t.device))
-        if stream is not None and stream.device != self.device:
-            raise ValueError("the stream is on %s, the tensors are on %s" % (stream.device, self.device))
-        self.stream = stream
+    def __init__(self, index, stream):
+        if stream is not None and stream.device.index != index:
+            raise ValueError("the stream is on %s, the tensors are on cuda:%d" % (stream.device, index))
+        self.index, self.stream = index, stream
 
     def __enter__(self):
         self.before = torch._C._cuda_getDevice()
-        if self.device.index != self.before:
-            torch.cuda.set_device(self.device.index)
-        return _stream(self.stream)
+        if self.index != self.before:
+            torch.cuda.set_device(self.index)
+        return torch._C._cuda_getCurrentRawStream(self.index) if self.stream is None else self.stream.cuda_stream
 
     def __exit__(self, *exc):
-        if self.device.index != self.before:
+        if self.index != self.before:
             torch.cuda.set_device(self.before)
         return False
 
     def empty(self, shape, dtype):
         """Memory for this call: freed early or late, it is not handed out again before the call's stream is done with it."""
-        t = torch.empty(shape, dtype=dtype, device=self.device)
+        t = torch.empty(shape, dtype=dtype, device=self.index)
         if self.stream is not None:
             t.record_stream(self.stream)
         return t
 
 
-def _rows_of(t, name, dtype, rows, cols):
-    """The row step of a [rows, cols] device tensor whose columns are neighbours."""
-    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == dtype):
+def _index(t, name, dtype, at):
+    """The device index of a CUDA tensor of `dtype`, which has to be `at` (None: any)."""
+    index = t.get_device() if isinstance(t, torch.Tensor) else -1
+    if index < 0 or t.dtype != dtype:
         raise TypeError("%s must be a CUDA tensor of %s" % (name, dtype))
-    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
+    if at is not None and index != at:
+        raise ValueError("%s is on cuda:%d, other tensors of the call are on cuda:%d" % (name, index, at))
+    return index
+
+
+def _rows_of(t, name, dtype, at, rows, cols):
+    """The row step of a [rows, cols] device tensor whose columns are neighbours."""
+    _index(t, name, dtype, at)
+    if t.shape != (rows, cols):
         raise ValueError("%s must be [%d, %d], got %s" % (name, rows, cols, tuple(t.shape)))
+    step, one = t.stride()
     if rows == 0:
         return cols
-    if cols > 1 and t.stride(1) != 1:
+    if one != 1 and cols > 1:
         raise ValueError("the columns of %s must be contiguous" % name)
-    if rows > 1 and t.stride(0) < cols:
-        raise ValueError("the rows of %s must not overlap" % name)
-    return max(cols, t.stride(0))
+    if step < cols:
+        if rows > 1:
+            raise ValueError("the rows of %s must not overlap" % name)
+        return cols
+    return step
 
 
-def _packed(t, name, dtype, shape):
-    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == dtype and t.is_contiguous()):
+def _packed(t, name, dtype, at, shape):
+    _index(t, name, dtype, at)
+    if not t.is_contiguous():
         raise TypeError("%s must be a contiguous CUDA tensor of %s" % (name, dtype))
-    if tuple(t.shape) != tuple(shape):
+    if t.shape != shape:
         raise ValueError("%s must be %s, got %s" % (name, list(shape), list(t.shape)))
-    return t
+    return t.data_ptr()
 
 
 def _dense_op(x, w, activation, offsets):
-    if not (isinstance(x, torch.Tensor) and x.is_cuda and x.dtype in DTYPES):
+    """The call's description, without the row steps of tensors other than x, and the device."""
+    if not isinstance(x, torch.Tensor) or x.dtype not in DTYPES:
         raise TypeError("x must be a CUDA tensor of float32, bfloat16 or float16")
     if activation not in ACTIVATIONS:
         raise ValueError("activation is one of %s" % ", ".join(ACTIVATIONS))
-    grouped = offsets is not None
-    if w.dim() != (3 if grouped else 2):
+    dtype, shape = x.dtype, w.shape
+    at = _index(x, "x", dtype, None)
+    if len(shape) != (2 if offsets is None else 3):
         raise ValueError("w must be [groups, out, in] with offsets, [out, in] without")
-    if x.dim() != 2 or x.shape[1] != w.shape[-1]:
-        raise ValueError("x must be [rows, %d], got %s" % (w.shape[-1], tuple(x.shape)))
-    op = CDense()
-    op.dtype, op.activation = DTYPES[x.dtype], ACTIVATIONS[activation]
-    op.rows, op.in_dim, op.out_dim = x.shape[0], w.shape[-1], w.shape[-2]
-    _packed(w, "w", x.dtype, w.shape)
-    if grouped:
-        _dev_i64(offsets, "offsets")
-        if offsets.dim() != 1 or offsets.numel() != w.shape[0] + 1:
-            raise ValueError("offsets must hold groups + 1 = %d row numbers" % (w.shape[0] + 1))
-        op.groups, op.offsets = w.shape[0], offsets.data_ptr()
-    op.ld_x = _rows_of(x, "x", x.dtype, x.shape[0], x.shape[1])
-    return op
+    n, k = shape[-2:]
+    if x.dim() != 2 or x.shape[1] != k:
+        raise ValueError("x must be [rows, %d], got %s" % (k, tuple(x.shape)))
+    _packed(w, "w", dtype, at, shape)
+    rows, groups, starts = x.shape[0], 0, None
+    if offsets is not None:
+        groups = shape[0]
+        starts = _packed(offsets, "offsets", torch.int64, at, (groups + 1,))
+    return CDense(DTYPES[dtype], ACTIVATIONS[activation], rows, k, n, groups, 0, starts, _rows_of(x, "x", dtype, at, rows, k)), at
 
 
-def _dense_workspace(op, backward, on, workspace):
-    need = int(load_library().tt_dense_workspace_bytes(ctypes.byref(op), int(backward)))
-    if workspace is None:
-        workspace = on.empty(need, torch.uint8) if need else None
-    elif not (workspace.is_cuda and workspace.dtype == torch.uint8 and workspace.is_contiguous()):
+def _workspace(t, at):
+    if _index(t, "workspace", torch.uint8, at) != at or not t.is_contiguous():
         raise TypeError("workspace must be a contiguous CUDA uint8 tensor")
-    return workspace, 0 if workspace is None else workspace.numel()
+    return t.data_ptr(), t.numel()
 
 
 def tt_dense_workspace_bytes(x, w, activation="none", offsets=None, backward=False) -> int:
     """Bytes of workspace the calls below take for these operands (they allocate it if none is given)."""
-    return int(load_library().tt_dense_workspace_bytes(ctypes.byref(_dense_op(x, w, activation, offsets)), int(backward)))
+    return int(load_library().tt_dense_workspace_bytes(ctypes.byref(_dense_op(x, w, activation, offsets)[0]), int(backward)))
 
 
 def tt_dense_forward(x, w, bias=None, residual=None, activation="none", offsets=None, out=None, pre=None, workspace=None, stream=None):
@@ -698,53 +704,63 @@ def tt_dense_forward(x, w, bias=None, residual=None, activation="none", offsets=
     [groups, out, in] and bias [groups, out], group g's for the rows offsets[g] .. offsets[g + 1].  One dtype throughout (float32,
     bfloat16 or float16); x, residual and out may be views into wider rows.  `pre` (packed, [rows, out]) receives the
     pre-activation that `tt_dense_backward` takes.  Rows of no group are left as they were in a given `out`, zeros in a new one."""
-    op = _dense_op(x, w, activation, offsets)
-    rows, n = op.rows, op.out_dim
-    given = [t for t in (x, w, bias, residual, offsets, out, pre, workspace) if t is not None]
-    on = _On(given, stream)
-    if bias is not None:
-        _packed(bias, "bias", x.dtype, w.shape[:-1])
+    op, at = _dense_op(x, w, activation, offsets)
+    rows, n, dtype = op.rows, op.out_dim, x.dtype
+    on = _On(at, stream)
+    p_bias = None if bias is None else _packed(bias, "bias", dtype, at, w.shape[:-1])
+    p_pre = None if pre is None else _packed(pre, "pre", dtype, at, (rows, n))
+    p_res = None
     if residual is not None:
-        op.ld_residual = _rows_of(residual, "residual", x.dtype, rows, n)
-    if pre is not None:
-        _packed(pre, "pre", x.dtype, (rows, n))
+        op.ld_residual = _rows_of(residual, "residual", dtype, at, rows, n)
+        p_res = residual.data_ptr()
     if out is None:
-        out = on.empty((rows, n), x.dtype)
+        out = on.empty((rows, n), dtype)
         op.zero_rest = 1
-    op.ld_out = _rows_of(out, "out", x.dtype, rows, n)
-    workspace, size = _dense_workspace(op, False, on, workspace)
+    else:
+        op.ld_out = _rows_of(out, "out", dtype, at, rows, n)
+    p_work, size = (None, 0) if workspace is None else _workspace(workspace, at)
+    lib, ref = load_library(), ctypes.byref(op)
     with on as s:
-        st = load_library().tt_dense_forward(ctypes.byref(op), _ptr(x), _ptr(w), _ptr(bias), _ptr(residual), _ptr(out), _ptr(pre), _ptr(workspace), size, s)
-    _check(st, "tt_dense_forward")
+        st = lib.tt_dense_forward(ref, x.data_ptr(), w.data_ptr(), p_bias, p_res, out.data_ptr(), p_pre, p_work, size, s)
+        if st == TT_ERR_WORKSPACE and workspace is None:  # few sizes need any
+            workspace = on.empty(lib.tt_dense_workspace_bytes(ref, 0), torch.uint8)
+            st = lib.tt_dense_forward(ref, x.data_ptr(), w.data_ptr(), p_bias, p_res, out.data_ptr(), p_pre, workspace.data_ptr(), workspace.numel(), s)
+    if st != TT_OK:
+        raise TTError(st, "tt_dense_forward")
     return out
 
 
 def tt_dense_backward(x, w, grad_out, pre=None, activation="none", offsets=None, needs=(True, True, True), workspace=None, stream=None):
     """Gradients `(dx, dw, dbias)` of `tt_dense_forward` from grad_out [rows, out] (None where `needs` says so); the residual's
     is grad_out itself.  With an activation `pre` is what the forward stored.  Rows of no group get zeros in dx."""
-    op = _dense_op(x, w, activation, offsets)
-    rows, n, k = op.rows, op.out_dim, op.in_dim
-    given = [t for t in (x, w, grad_out, pre, offsets, workspace) if t is not None]
-    on = _On(given, stream)
-    op.ld_grad = _rows_of(grad_out, "grad_out", x.dtype, rows, n)
+    op, at = _dense_op(x, w, activation, offsets)
+    rows, n, k, dtype = op.rows, op.out_dim, op.in_dim, x.dtype
+    on = _On(at, stream)
+    op.ld_grad = _rows_of(grad_out, "grad_out", dtype, at, rows, n)
+    p_pre = None
     if activation != "none":
         if pre is None:
             raise ValueError("the gradient of an activation needs the pre-activation")
-        _packed(pre, "pre", x.dtype, (rows, n))
-    dx = on.empty((rows, k), x.dtype) if needs[0] else None
-    dw = on.empty(tuple(w.shape), x.dtype) if needs[1] else None
-    db = on.empty(tuple(w.shape[:-1]), x.dtype) if needs[2] else None
+        p_pre = _packed(pre, "pre", dtype, at, (rows, n))
+    dx = on.empty((rows, k), dtype) if needs[0] else None
+    dw = on.empty(w.shape, dtype) if needs[1] else None
+    db = on.empty(w.shape[:-1], dtype) if needs[2] else None
     op.zero_rest = 1
-    workspace, size = _dense_workspace(op, True, on, workspace)
+    lib, ref = load_library(), ctypes.byref(op)
+    if workspace is None:
+        workspace = on.empty(lib.tt_dense_workspace_bytes(ref, 1), torch.uint8)
+    p_work, size = _workspace(workspace, at)
     with on as s:
-        st = load_library().tt_dense_backward(ctypes.byref(op), _ptr(x), _ptr(w), _ptr(pre), _ptr(grad_out), _ptr(dx), _ptr(dw), _ptr(db), _ptr(workspace), size, s)
-    _check(st, "tt_dense_backward")
+        st = lib.tt_dense_backward(ref, x.data_ptr(), w.data_ptr(), p_pre, grad_out.data_ptr(), None if dx is None else dx.data_ptr(),
+                                   None if dw is None else dw.data_ptr(), None if db is None else db.data_ptr(), p_work, size, s)
+    if st != TT_OK:
+        raise TTError(st, "tt_dense_backward")
     return dx, dw, db
 
 
 def _coefficients(steps, coefficients):
     steps = int(steps)
-    c = [float(v) for v in torch.as_tensor(coefficients, dtype=torch.float64).reshape(-1).tolist()]
+    c = [float(v) for row in coefficients for v in (row if isinstance(row, (tuple, list)) else (row,))]
     if len(c) == 3:
         c = c * steps
     if steps < 1 or len(c) != 3 * steps:
@@ -761,11 +777,13 @@ def tt_orthogonalize(g, steps=5, coefficients=ORTHO_COEFFICIENTS, eps=1e-7, out=
     if g.dim() not in (2, 3) or g.shape[-1] < 1 or g.shape[-2] < 1:
         raise ValueError("g must be [rows, cols] or [batch, rows, cols]")
     coef = _coefficients(steps, coefficients)
-    on = _On([t for t in (g, out, workspace) if t is not None], stream)
+    at = g.get_device()
+    on = _On(at, stream)
     if out is None:
-        out = on.empty(tuple(g.shape), g.dtype)
-    if out.shape != g.shape or out.dtype != g.dtype:
-        raise ValueError("out must have the shape and dtype of g")
+        out = on.empty(g.shape, g.dtype)
+    _index(out, "out", g.dtype, at)
+    if out.shape != g.shape:
+        raise ValueError("out must have the shape of g")
     m = CMatrices()
     m.dtype, m.batch, m.rows, m.cols = DTYPES[g.dtype], g.shape[0] if g.dim() == 3 else 1, g.shape[-2], g.shape[-1]
     for name, t in (("g", g), ("out", out)):
@@ -786,8 +804,9 @@ def tt_orthogonalize(g, steps=5, coefficients=ORTHO_COEFFICIENTS, eps=1e-7, out=
         raise TTError(TT_ERR_SHAPE, "tt_orthogonalize_workspace_bytes")
     if workspace is None:
         workspace = on.empty(need, torch.uint8)
+    p_work, size = _workspace(workspace, at)
     with on as s:
-        st = lib.tt_orthogonalize(ctypes.byref(m), _ptr(g), _ptr(out), int(steps), coef, ctypes.c_float(eps), _ptr(workspace), workspace.numel(), s)
+        st = lib.tt_orthogonalize(ctypes.byref(m), g.data_ptr(), out.data_ptr(), int(steps), coef, eps, p_work, size, s)
     _check(st, "tt_orthogonalize")
     return out
 
@@ -800,19 +819,22 @@ def tt_core_ortho_update(table: Table, dcores, momenta, lr: float, momentum=0.95
         if len(ts) != 3:
             raise ValueError("three tensors of %s, one a core" % name)
         for t, c in zip(ts, table.cores):
+            _index(t, name, torch.float32, table.cores[0].get_device())
             if _dev_f32(t, name).numel() != c.numel():
                 raise ValueError("%s must have the core's size" % name)
-    on = _On(list(table.cores) + list(dcores) + list(momenta) + ([workspace] if workspace is not None else []), stream)
+    at = table.cores[0].get_device()
+    on = _On(at, stream)
     lib = load_library()
     if workspace is None:
         need = int(lib.tt_core_ortho_workspace_bytes(ctypes.byref(table.c)))
         if need == 0:
             raise TTError(TT_ERR_SHAPE, "tt_core_ortho_workspace_bytes")
         workspace = on.empty(need, torch.uint8)
+    p_work, size = _workspace(workspace, at)
     ptrs = lambda ts: (ctypes.c_void_p * 3)(*[t.data_ptr() for t in ts])
     with on as s:
         st = lib.tt_core_ortho_update(ctypes.byref(table.c), ptrs(dcores), ptrs(momenta), ctypes.c_float(lr), ctypes.c_float(momentum), int(bool(nesterov)),
-                                      int(steps), coef, ctypes.c_float(eps), _ptr(workspace), workspace.numel(), s)
+                                      int(steps), coef, eps, p_work, size, s)
     _check(st, "tt_core_ortho_update")
 
 

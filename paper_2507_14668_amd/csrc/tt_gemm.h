@@ -44,3 +44,6 @@ tt_status ttk_gemm(const TTGemm &g, void *partial, hipStream_t s);
 // Large 16-bit products on aligned operands (tt_gemm_direct.hip); ttk_gemm passes them on.
 bool ttk_gemm_direct_serves(const TTGemm &g);
 tt_status ttk_gemm_direct(const TTGemm &g, hipStream_t s);
+// Few rows with a K-contiguous weight (tt_gemm_rows.hip); likewise.
+bool ttk_gemm_rows_serves(const TTGemm &g);
+tt_status ttk_gemm_rows(const TTGemm &g, hipStream_t s);

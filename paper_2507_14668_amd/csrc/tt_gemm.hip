@@ -151,9 +151,11 @@ template <class T, class O, int P, bool AKC, bool BKC, int E>
 __global__ void __launch_bounds__(TT_BLOCK, 2) k_gemm(TTGemm g, int m_tiles, int n_tiles, int split, float *partial) {
   typedef Carrier<T, AKC, E> CA;
   typedef Carrier<T, BKC, E> CB;
+  constexpr int D = 1;
   constexpr int BK = Step<T>::BK, PLANE = E * BK, F = E / 32, BUF = P == 1 ? 2 : 1;  // fp32's planes fill the LDS of two workgroups with one buffer
-  constexpr int HALVES = 2 * BUF * P * PLANE, REDO = P == 3 ? 2 * (CA::SIZE32 + CB::SIZE32) : 0;
-  __shared__ __align__(16) unsigned short lds[HALVES > REDO ? HALVES : REDO];
+  constexpr int HALVES = 2 * BUF * P * PLANE, REDO = P == 3 ? 2 * (CA::SIZE32 + CB::SIZE32) : 0,
+                FINISH = 8 * finish_floats<F, 2>();
+  __shared__ __align__(16) unsigned short lds[HALVES > REDO ? (HALVES > FINISH ? HALVES : FINISH) : (REDO > FINISH ? REDO : FINISH)];
   __shared__ int flags[4];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int members = (int)gridDim.y / split, cut = (int)blockIdx.y / members;  // which piece of K
@@ -189,28 +191,20 @@ __global__ void __launch_bounds__(TT_BLOCK, 2) k_gemm(TTGemm g, int m_tiles, int
   CB cb;
   ca.start(a, g.lda, w.lo, w.hi, w.k_lo);
   cb.start(b, g.ldb, w.n0, g.N, w.k_lo);
-  Unit<T> ua[CA::N], ub[CB::N];
+  Unit<T> ua[D][CA::N], ub[D][CB::N];
   const int wm = (wave >> 1) * (E / 2), wn = (wave & 1) * (E / 2);
   f32x4 acc[F][F] = {}, rs[F] = {};  // [m][n]; sums of A's rows
   const bool sums = g.rowsum && w.n0 == 0;
   unsigned small_a = ~0u, small_b = ~0u;  // twice the bits of the smallest number that is not zero, less one
-  auto note = [&]() {
+  auto note = [&](const Unit<T> *u, int n, unsigned &small) {
     if constexpr (P == 3) {
 #pragma unroll
-      for (int i = 0; i < CA::N; ++i)
+      for (int i = 0; i < n; ++i)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const unsigned x = 2 * __float_as_uint(ua[i].a[e]) - 1, y = 2 * __float_as_uint(ua[i].b[e]) - 1;
-          small_a = x < small_a ? x : small_a;
-          small_a = y < small_a ? y : small_a;
-        }
-#pragma unroll
-      for (int i = 0; i < CB::N; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const unsigned x = 2 * __float_as_uint(ub[i].a[e]) - 1, y = 2 * __float_as_uint(ub[i].b[e]) - 1;
-          small_b = x < small_b ? x : small_b;
-          small_b = y < small_b ? y : small_b;
+          const unsigned x = 2 * __float_as_uint(u[i].a[e]) - 1, y = 2 * __float_as_uint(u[i].b[e]) - 1;
+          small = x < small ? x : small;
+          small = y < small ? y : small;
         }
     }
   };
@@ -256,38 +250,47 @@ __global__ void __launch_bounds__(TT_BLOCK, 2) k_gemm(TTGemm g, int m_tiles, int
     }
   };
   if (w.k_lo < K) {
-    ca.load(ua, w.k_lo, K);
-    cb.load(ub, w.k_lo, K);
+#pragma unroll
+    for (int d = 0; d < D; ++d)
+      if (w.k_lo + d * BK < K) {
+        ca.load(ua[d], w.k_lo + d * BK, K);
+        cb.load(ub[d], w.k_lo + d * BK, K);
+      }
     if constexpr (BUF == 2) {
-      ca.template store<P>(ua, plane_a(0, 0));
-      cb.template store<P>(ub, plane_b(0, 0));
+      ca.template store<P>(ua[0], plane_a(0, 0));
+      cb.template store<P>(ub[0], plane_b(0, 0));
     }
     int buf = 0;
-    for (int k0 = w.k_lo; k0 < K; k0 += BK) {
-      const bool more = k0 + BK < K;
-      if constexpr (BUF == 2) {
-        __syncthreads();  // this step's tiles are whole, and nobody reads the other buffer any more
-        if (more) {
-          ca.load(ua, k0 + BK, K);
-          cb.load(ub, k0 + BK, K);
+    for (int k1 = w.k_lo; k1 < K; k1 += D * BK) {
+#pragma unroll
+      for (int d = 0; d < D; ++d) {
+        const int k0 = k1 + d * BK;
+        if (k0 >= K) break;
+        if constexpr (BUF == 2) {
+          __syncthreads();  // this step's tiles are whole, and nobody reads the other buffer any more
+          if (k0 + D * BK < K) {
+            ca.load(ua[d], k0 + D * BK, K);
+            cb.load(ub[d], k0 + D * BK, K);
+          }
+          multiply(buf);
+          if (k0 + BK < K) {
+            ca.template store<P>(ua[(d + 1) % D], plane_a(buf ^ 1, 0));
+            cb.template store<P>(ub[(d + 1) % D], plane_b(buf ^ 1, 0));
+          }
+          buf ^= 1;
+        } else {
+          __syncthreads();
+          note(ua[d], CA::N, small_a);
+          note(ub[d], CB::N, small_b);
+          ca.template store<P>(ua[d], plane_a(0, 0));
+          cb.template store<P>(ub[d], plane_b(0, 0));
+          __syncthreads();
+          if (k0 + D * BK < K) {
+            ca.load(ua[d], k0 + D * BK, K);
+            cb.load(ub[d], k0 + D * BK, K);
+          }
+          multiply(0);
         }
-        multiply(buf);
-        if (more) {
-          ca.template store<P>(ua, plane_a(buf ^ 1, 0));
-          cb.template store<P>(ub, plane_b(buf ^ 1, 0));
-        }
-        buf ^= 1;
-      } else {
-        __syncthreads();
-        note();
-        ca.template store<P>(ua, plane_a(0, 0));
-        cb.template store<P>(ub, plane_b(0, 0));
-        __syncthreads();
-        if (more) {
-          ca.load(ua, k0 + BK, K);
-          cb.load(ub, k0 + BK, K);
-        }
-        multiply(0);
       }
     }
   }
@@ -340,11 +343,11 @@ __global__ void __launch_bounds__(TT_BLOCK, 2) k_gemm(TTGemm g, int m_tiles, int
       ca.start(a, g.lda, w.lo, w.hi, w.k_lo);
       cb.start(b, g.ldb, w.n0, g.N, w.k_lo);
       for (int k0 = w.k_lo; k0 < K; k0 += BK) {
-        ca.load(ua, k0, K);
-        cb.load(ub, k0, K);
+        ca.load(ua[0], k0, K);
+        cb.load(ub[0], k0, K);
         __syncthreads();
-        ca.store32(ua, l32a);
-        cb.store32(ub, l32b);
+        ca.store32(ua[0], l32a);
+        cb.store32(ub[0], l32b);
         __syncthreads();
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -393,7 +396,7 @@ __global__ void __launch_bounds__(TT_BLOCK, 2) k_gemm(TTGemm g, int m_tiles, int
     }
   }
   __syncthreads();  // nobody reads the operands any more
-  finish_tile<T, O, F, F>(g, w.z, w.lo + wm, w.hi, w.n0 + wn, acc, reinterpret_cast<float *>(lds) + wave * 16 * (16 * F + 4));
+  finish_tile<T, O, F, F, 2>(g, w.z, w.lo + wm, w.hi, w.n0 + wn, acc, reinterpret_cast<float *>(lds) + wave * finish_floats<F, 2>());
 }
 
 // The pieces of a split product, added in order; four columns of a row per thread.
@@ -485,7 +488,7 @@ template <class T, class O, int P> tt_status launch(const TTGemm &g, void *parti
 }  // namespace
 
 size_t ttk_gemm_partial_bytes(const TTGemm &g) {
-  if (g.M < 1 || g.N < 1 || g.batch < 1) return 0;
+  if (g.M < 1 || g.N < 1 || g.batch < 1 || ttk_gemm_rows_serves(g)) return 0;
   const Shape h = shape_of(g);
   return h.split < 2 ? 0 : (((size_t)h.split * g.batch * g.M * (g.N + 1LL) * 4) + 255) & ~(size_t)255;
 }
@@ -493,6 +496,7 @@ size_t ttk_gemm_partial_bytes(const TTGemm &g) {
 tt_status ttk_gemm(const TTGemm &g, void *partial, hipStream_t s) {
   if (g.M < 1 || g.N < 1 || g.batch < 1) return TT_OK;
   if (!g.a_kc && g.b_kc) return TT_ERR_INVALID_ARG;  // no caller needs it
+  if (ttk_gemm_rows_serves(g)) return ttk_gemm_rows(g, s);
   if (ttk_gemm_direct_serves(g)) return ttk_gemm_direct(g, s);
   if (g.dtype == TT_BF16 && g.out_dtype == TT_BF16) return launch<ttg::bf16, ttg::bf16, 1>(g, partial, s);
   if (g.dtype == TT_F16 && g.out_dtype == TT_F16) return launch<ttg::f16, ttg::f16, 1>(g, partial, s);

@@ -121,14 +121,26 @@ __device__ __forceinline__ float fast_phi(float z, float e) {  // e = exp(-z^2 /
   const float p = 0.5f * e * t * fmaf(t, fmaf(t, fmaf(t, fmaf(t, 1.061405429f, -1.453152027f), 1.421413741f), -0.284496736f), 0.254829592f);
   return z < 0.f ? p : 1.f - p;
 }
-template <class O> __device__ __forceinline__ float act_of(float z, int act) {
-  if constexpr (sizeof(O) == 4) return act_value(z, act);
+template <class O, int C> __device__ __forceinline__ void act_of(float v[C], int act) {
+  constexpr bool fast = sizeof(O) == 2;
   switch (act) {
-    case TT_ACT_RELU: return z <= 0.f ? 0.f : z;
-    case TT_ACT_GELU: return z * fast_phi(z, __expf(-0.5f * z * z));
-    case TT_ACT_SILU: return z * fast_sigmoid(z);
-    case TT_ACT_SIGMOID: return fast_sigmoid(z);
-    default: return z;
+    case TT_ACT_RELU:
+#pragma unroll
+      for (int i = 0; i < C; ++i) v[i] = act_value(v[i], TT_ACT_RELU);
+      break;
+    case TT_ACT_GELU:
+#pragma unroll
+      for (int i = 0; i < C; ++i) v[i] = fast ? v[i] * fast_phi(v[i], __expf(-0.5f * v[i] * v[i])) : act_value(v[i], TT_ACT_GELU);
+      break;
+    case TT_ACT_SILU:
+#pragma unroll
+      for (int i = 0; i < C; ++i) v[i] = fast ? v[i] * fast_sigmoid(v[i]) : act_value(v[i], TT_ACT_SILU);
+      break;
+    case TT_ACT_SIGMOID:
+#pragma unroll
+      for (int i = 0; i < C; ++i) v[i] = fast ? fast_sigmoid(v[i]) : act_value(v[i], TT_ACT_SIGMOID);
+      break;
+    default: break;
   }
 }
 template <class O> __device__ __forceinline__ float slope_of(float z, int act) {
@@ -272,10 +284,7 @@ __device__ __forceinline__ void finish(const TTGemm &g, int z, int m, int n, int
     for (int i = 0; i < C; ++i) t[i] = keep_sign<O>(v[i]);
     store_n<O, C>((O *)g.pre + z * g.p_step + (long long)m * g.ldp + n, valid, t);
   }
-  if (g.act != TT_ACT_NONE) {
-#pragma unroll
-    for (int i = 0; i < C; ++i) v[i] = act_of<O>(v[i], g.act);
-  }
+  act_of<O, C>(v, g.act);
   if (g.res) {
     load_n<T, C>((const T *)g.res + z * g.r_step + (long long)m * g.ldr + n, valid, t);
 #pragma unroll
@@ -285,22 +294,25 @@ __device__ __forceinline__ void finish(const TTGemm &g, int z, int m, int n, int
 }
 
 // The results of a wavefront, 16 FX x 16 FY of out from row m0 and column n0, rows below `end`.  The instruction leaves a lane
-// four columns of a row, 8 bytes of a 16-bit row at a time; through 16 rows of LDS (`lds`: 16 x (16 FY + 4) floats of the wavefront's
-// own) a lane gets eight, and what is read and written is whole lines of 128 bytes.  (Measured for 16384 x 4096 x 4096 in bf16 with
-// gelu and residual: 238 us of 700 were the end of the tiles before, 105 now.)
-template <class T, class O, int FX, int FY>
+// four columns of a row, 8 bytes of a 16-bit row at a time; through 16 XB rows of LDS (`lds`: finish_floats of the wavefront's own) a lane
+// gets eight, and what is read and written is whole lines of 128 bytes.  The loop over the rows is not unrolled: with all activations in it
+// 16 times, the code is longer than the instruction cache.
+template <int FY, int XB> constexpr int finish_floats() { return 16 * XB * (16 * FY + 4); }
+template <class T, class O, int FX, int FY, int XB>
 __device__ __forceinline__ void finish_tile(const TTGemm &g, int z, int m0, int end, int n0, const f32x4 (&acc)[FX][FY], float *lds) {
   constexpr int LD = 16 * FY + 4, PER = 2 * FY, ROWS = 64 / PER;  // lanes of a row, rows at a time
   const int lane = threadIdx.x & 63, q = lane >> 4, j = lane & 15, c = 8 * (lane % PER), r = lane / PER;
   const int valid = g.N - n0 - c;
 #pragma unroll
-  for (int x = 0; x < FX; ++x) {
+  for (int x0 = 0; x0 < FX; x0 += XB) {
 #pragma unroll
-    for (int y = 0; y < FY; ++y) *reinterpret_cast<f32x4 *>(lds + j * LD + 16 * y + 4 * q) = acc[x][y];
+    for (int x = 0; x < XB; ++x)
+#pragma unroll
+      for (int y = 0; y < FY; ++y) *reinterpret_cast<f32x4 *>(lds + (16 * x + j) * LD + 16 * y + 4 * q) = acc[x0 + x][y];
     tt_wave_lds_order();
-#pragma unroll
-    for (int h = 0; h < 16 / ROWS; ++h) {
-      const int row = r + h * ROWS, m = m0 + 16 * x + row;
+#pragma unroll 1
+    for (int row = r; row < 16 * XB; row += ROWS) {
+      const int m = m0 + 16 * x0 + row;
       const f32x4 a = *reinterpret_cast<const f32x4 *>(lds + row * LD + c), b = *reinterpret_cast<const f32x4 *>(lds + row * LD + c + 4);
       float v[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
       if (m < end && valid > 0) finish<T, O, 8>(g, z, m, n0 + c, valid, v);

@@ -115,7 +115,8 @@ __device__ __forceinline__ void step_of(unsigned short *__restrict__ now, const 
 }
 
 template <class T, bool AKC, bool BKC> __global__ void __launch_bounds__(THREADS, 2) k_gemm_direct(TTGemm g, int m_tiles, int n_tiles) {
-  __shared__ __align__(16) unsigned short lds[STAGES * 2 * OPERAND];
+  __shared__ __align__(16) unsigned short lds[16 * finish_floats<4, 4>()];  // (more than two buffers take)
+  static_assert(16 * finish_floats<4, 4>() >= STAGES * 2 * OPERAND, "LDS");
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   unsigned mt, nt;
   tile_order(blockIdx.x, (unsigned)m_tiles, (unsigned)n_tiles, mt, nt);
@@ -184,7 +185,7 @@ template <class T, bool AKC, bool BKC> __global__ void __launch_bounds__(THREADS
     }
   }
   __syncthreads();  // nobody reads the operands any more
-  finish_tile<T, T, 8, 4>(g, w.z, w.lo + wm, w.hi, w.n0 + wn, acc, reinterpret_cast<float *>(lds) + wave * 16 * 68);
+  finish_tile<T, T, 8, 4, 4>(g, w.z, w.lo + wm, w.hi, w.n0 + wn, acc, reinterpret_cast<float *>(lds) + wave * finish_floats<4, 4>());
 }
 
 template <class T> tt_status launch(const TTGemm &g, hipStream_t s) {

@@ -24,10 +24,25 @@ struct Mats {
 
 // ---- norm and scaling ------------------------------------------------------------------------------
 // Sums of squares in 64 bits: neither 1e-25 nor 1e25 leaves the range, and the scale is not what limits the result.
-constexpr int kMaxParts = 64;
+constexpr int kMaxParts = 1024;
 int parts_of(long long elems) {
-  long long p = (elems + 8191) / 8192;
+  long long p = (elems + 4095) / 4096;
   return (int)(p < 1 ? 1 : p > kMaxParts ? kMaxParts : p);
+}
+// the place of element e of a matrix (a 64-bit division costs as much as the rest)
+__device__ __forceinline__ long long place_of(const Mats &m, long long e, bool small) {
+  const long long r = small ? (long long)((unsigned)e / (unsigned)m.cols) : e / m.cols;
+  return r * m.r_step + (e - r * m.cols);
+}
+__device__ __forceinline__ double block_sum(double s) {
+  __shared__ double red[TT_BLOCK];
+  red[threadIdx.x] = s;
+  __syncthreads();
+  for (int o = TT_BLOCK / 2; o > 0; o >>= 1) {
+    if ((int)threadIdx.x < o) red[threadIdx.x] += red[threadIdx.x + o];
+    __syncthreads();
+  }
+  return red[0];
 }
 
 template <class T>
@@ -35,20 +50,14 @@ __global__ void __launch_bounds__(TT_BLOCK) k_sum_squares(const T *__restrict__ 
   const long long z = blockIdx.x / (unsigned)parts;
   const int p = (int)(blockIdx.x % (unsigned)parts);
   const long long elems = (long long)m.rows * m.cols;
+  const bool small = elems < 2147483648LL;
   double s = 0;
   for (long long e = (long long)p * TT_BLOCK + threadIdx.x; e < elems; e += (long long)parts * TT_BLOCK) {
-    const long long r = e / m.cols;
-    const double v = (double)to_f32(g[z * m.b_step + r * m.r_step + (e - r * m.cols)]);
+    const double v = (double)to_f32(g[z * m.b_step + place_of(m, e, small)]);
     s += v * v;
   }
-  __shared__ double red[TT_BLOCK];
-  red[threadIdx.x] = s;
-  __syncthreads();
-  for (int o = TT_BLOCK / 2; o > 0; o >>= 1) {
-    if (threadIdx.x < o) red[threadIdx.x] += red[threadIdx.x + o];
-    __syncthreads();
-  }
-  if (threadIdx.x == 0) partial[z * parts + p] = red[0];
+  s = block_sum(s);
+  if (threadIdx.x == 0) partial[z * parts + p] = s;
 }
 
 // x = g * s in fp32, packed.  A matrix whose squares do not sum to a number is NaN as a whole.
@@ -58,14 +67,14 @@ __global__ void __launch_bounds__(TT_BLOCK) k_scale_in(const T *__restrict__ g, 
   const long long z = blockIdx.x / (unsigned)parts;
   const int p = (int)(blockIdx.x % (unsigned)parts);
   const long long elems = (long long)m.rows * m.cols;
+  const bool small = elems < 2147483648LL;
   double sum = 0;
-  for (int i = 0; i < parts; ++i) sum += partial[z * parts + i];
+  for (int i = threadIdx.x; i < parts; i += TT_BLOCK) sum += partial[z * parts + i];
+  sum = block_sum(sum);
   double scale = 1.0 / (sqrt(sum) + (double)eps);
   if (!(sum <= 1.7976931348623157e308)) scale = (double)NAN;
-  for (long long e = (long long)p * TT_BLOCK + threadIdx.x; e < elems; e += (long long)parts * TT_BLOCK) {
-    const long long r = e / m.cols;
-    x[z * elems + e] = (float)((double)to_f32(g[z * m.b_step + r * m.r_step + (e - r * m.cols)]) * scale);
-  }
+  for (long long e = (long long)p * TT_BLOCK + threadIdx.x; e < elems; e += (long long)parts * TT_BLOCK)
+    x[z * elems + e] = (float)((double)to_f32(g[z * m.b_step + place_of(m, e, small)]) * scale);
 }
 
 // The three products of a step, without their operands' addresses.  For results in 16 bits two bf16 parts of each operand are

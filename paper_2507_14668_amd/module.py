@@ -118,7 +118,9 @@ def tt_dense(x, w, bias=None, residual=None, activation="none", offsets=None):
     is left out too."""
     if residual is not None and offsets is not None and residual.requires_grad and torch.is_grad_enabled():
         residual = _GroupRows.apply(residual, offsets)
-    return _DenseFunction.apply(_row_major(x), w.contiguous(), None if bias is None else bias.contiguous(), _row_major(residual), activation, offsets)
+    if bias is not None and not bias.is_contiguous():
+        bias = bias.contiguous()
+    return _DenseFunction.apply(_row_major(x), w if w.is_contiguous() else w.contiguous(), bias, _row_major(residual), activation, offsets)
 
 
 class _GroupRows(torch.autograd.Function):

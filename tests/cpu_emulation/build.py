@@ -25,7 +25,7 @@ ROOT = os.path.dirname(os.path.dirname(HERE))
 CSRC = os.path.join(ROOT, "paper_2507_14668_amd", "csrc")
 CLANG = os.environ.get("TT_EMU_CXX", "/opt/rocm/llvm/bin/clang++")
 UNITS = ("tt_api", "tt_reorder", "tt_forward", "tt_forward_mfma", "tt_forward_sample", "tt_bf16", "tt_index_graph", "tt_fuse", "tt_backward",
-         "tt_backward_mfma", "tt_gemm", "tt_gemm_direct", "tt_dense", "tt_ortho", "tt_ortho_slice")
+         "tt_backward_mfma", "tt_gemm", "tt_gemm_direct", "tt_gemm_rows", "tt_dense", "tt_ortho", "tt_ortho_slice")
 
 
 def available() -> bool:

@@ -18,12 +18,14 @@ DT = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 GUARD = 512
 
 
-VARIANTS = {"small tiles": ("dense", []), "large tiles": ("dense_large", ["-DTT_GEMM_LARGE_TILES=1"]), "direct tiles": ("dense_direct", ["-DTT_GEMM_DIRECT_TILES=1"])}
+TILES = "-DTT_GEMM_FEW_ROWS=0"
+VARIANTS = {"as it is": ("dense", []), "small tiles": ("dense_small", [TILES]), "large tiles": ("dense_large", [TILES, "-DTT_GEMM_LARGE_TILES=1"]),
+            "direct tiles": ("dense_direct", [TILES, "-DTT_GEMM_DIRECT_TILES=1"])}
 
 
 @pytest.fixture(scope="module", params=VARIANTS)
 def lib(request):
-    """The library as it is (these sizes take the small tiles), and with the larger kinds from the first tile on."""
+    """The library as it is (few rows mostly), without the kernel for few rows, and with the larger tiles from the first one on."""
     lib = ctypes.CDLL(emu_build.build_shared(BUILD_DIR, *VARIANTS[request.param]))
     vp, sz, f32 = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_float
     lib.tt_dense_workspace_bytes.restype = lib.tt_orthogonalize_workspace_bytes.restype = lib.tt_core_ortho_workspace_bytes.restype = sz

@@ -286,7 +286,7 @@ extern "C" tt_status tt_orthogonalize(const tt_matrices *m, const void *g, void 
     TTSlices p = slices_of(in, m->dtype, Steps{steps, coefficients}, eps);
     p.in = g; p.in_b = in.b_step; p.in_s = tall ? 1 : in.r_step; p.in_l = tall ? in.r_step : 1;
     p.out = out; p.out_b = o_step; p.out_s = tall ? 1 : ldo; p.out_l = tall ? ldo : 1;
-    return ttk_slices(p, s);
+    return ttk_slices(&p, 1, s);
   }
   tt_status st = m->dtype == TT_F32    ? scale_in<float>(g, in, eps, ws, w, s)
                  : m->dtype == TT_BF16 ? scale_in<ttg::bf16>(g, in, eps, ws, w, s)
@@ -319,7 +319,11 @@ extern "C" tt_status tt_core_ortho_update(const tt_table *table, const float *co
   if (need == 0) return TT_ERR_SHAPE;
   if (!workspace || ((uintptr_t)workspace & 255) != 0 || workspace_bytes < need) return TT_ERR_WORKSPACE;
   hipStream_t s = (hipStream_t)stream;
-  for (int k = 0; k < 3; ++k) {
+  TTSlices jobs[3];  // the cores whose slices stay on chip go into one launch, core 1 first
+  int n = 0;
+  const int order[3] = {1, 0, 2};
+  for (int i = 0; i < 3; ++i) {
+    const int k = order[i];
     const Mats m = slices(table, k);
     const Scratch w = scratch(m.batch, m.rows, m.cols, TT_F32);
     char *ws = (char *)workspace;
@@ -333,15 +337,14 @@ extern "C" tt_status tt_core_ortho_update(const tt_table *table, const float *co
     const float rate = (float)((double)lr * sqrt(m.rows > m.cols ? (double)m.rows / m.cols : 1.0));
     const bool tall = m.rows > m.cols;
     if (ttk_slices_serves(tall ? m.cols : m.rows, tall ? m.rows : m.cols)) {
-      TTSlices p = slices_of(m, TT_F32, Steps{steps, coefficients}, eps);
+      TTSlices &p = jobs[n++];
+      p = slices_of(m, TT_F32, Steps{steps, coefficients}, eps);
       const long long row = k == 0 ? m.cols : (long long)m.batch * m.cols;  // between a slice's rows; slices are a row apart, in core 0 whole
       p.in = grad; p.out = core; p.mom = mom;
       p.in_b = p.out_b = k == 0 ? m.b_step : m.cols;
       p.in_s = p.out_s = tall ? 1 : row;
       p.in_l = p.out_l = tall ? row : 1;
       p.mu = mu; p.rate = rate; p.nesterov = nesterov;
-      const tt_status st = ttk_slices(p, s);
-      if (st != TT_OK) return st;
       continue;
     }
     hipLaunchKernelGGL(k_core_momentum, dim3((unsigned)blocks), dim3(TT_BLOCK), 0, s, d, grad, mom, mu, nesterov, u);
@@ -352,5 +355,5 @@ extern "C" tt_status tt_core_ortho_update(const tt_table *table, const float *co
     st = tt_launch_status();
     if (st != TT_OK) return st;
   }
-  return TT_OK;
+  return ttk_slices(jobs, n, s);
 }

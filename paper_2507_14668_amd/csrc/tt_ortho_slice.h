@@ -3,7 +3,7 @@
 
 #include "tt_gemm.h"
 
-#define TT_SLICE_MAX_STEPS 32
+#define TT_SLICE_MAX_STEPS TT_ORTHO_MAX_STEPS
 
 // Matrix z: element (s, l) of its short and its long side at z * b_step + s * s_step + l * l_step.
 struct TTSlices {
@@ -24,4 +24,4 @@ struct TTSlices {
 };
 
 bool ttk_slices_serves(long long shorter, long long longer);
-tt_status ttk_slices(const TTSlices &p, hipStream_t s);
+tt_status ttk_slices(const TTSlices *p, int n, hipStream_t s);  // n <= 3 batches of one dtype side by side

@@ -1,4 +1,6 @@
 // Newton-Schulz steps on small matrices that stay on chip from the first to the last step: read once, written once.
+#include <string.h>
+
 #include "tt_gemm_device.h"
 #include "tt_ortho_slice.h"
 
@@ -19,6 +21,54 @@ template <class T> __device__ __forceinline__ void give(const TTSlices &p, long 
   if (!p.mom) *o = from_f32<T>(v);
   else *o = from_f32<T>(to_f32(*o) - p.rate * v);
 }
+// C neighbours along l (ALONG_L) or along s from (s, l) on, in one access where they all exist and lie next to each other.
+template <class T, int C, bool ALONG_L> __device__ __forceinline__ void take_n(const TTSlices &p, long long z, int s, int l, float v[C]) {
+  const long long e = z * p.in_b + s * p.in_s + l * p.in_l;
+  const bool whole = ALONG_L ? s < p.shorter && l + C <= p.longer : s + C <= p.shorter && l < p.longer;
+  if constexpr (C == 4) {
+    if (whole && (ALONG_L ? p.in_l : p.in_s) == 1) {
+      load4((const T *)p.in + e, 4, v);
+      if (p.mom) {
+        float m[4];
+        load4(p.mom + e, 4, m);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          m[i] = p.mu * m[i] + v[i];
+          v[i] = p.nesterov ? v[i] + p.mu * m[i] : m[i];
+        }
+        store4(p.mom + e, 4, m);
+      }
+      return;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < C; ++i) {
+    const int si = ALONG_L ? s : s + i, li = ALONG_L ? l + i : l;
+    v[i] = si < p.shorter && li < p.longer ? take<T>(p, z, si, li) : 0.f;
+  }
+}
+template <class T, int C, bool ALONG_L> __device__ __forceinline__ void give_n(const TTSlices &p, long long z, int s, int l, float v[C]) {
+  const long long e = z * p.out_b + s * p.out_s + l * p.out_l;
+  const bool whole = ALONG_L ? s < p.shorter && l + C <= p.longer : s + C <= p.shorter && l < p.longer;
+  if constexpr (C == 4) {
+    if (whole && (ALONG_L ? p.out_l : p.out_s) == 1) {
+      T *o = (T *)p.out + e;
+      if (p.mom) {
+        float m[4];
+        load4(o, 4, m);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = m[i] - p.rate * v[i];
+      }
+      store4(o, 4, v);
+      return;
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < C; ++i) {
+    const int si = ALONG_L ? s : s + i, li = ALONG_L ? l + i : l;
+    if (si < p.shorter && li < p.longer) give<T>(p, z, si, li, v[i]);
+  }
+}
 // 1 / (norm + eps); NaN for a sum of squares that is no number or infinite, so that the whole matrix is NaN
 __device__ __forceinline__ double scale_of(double sum, float eps) {
   return sum <= 1.7976931348623157e308 ? 1.0 / (sqrt(sum) + (double)eps) : (double)NAN;
@@ -36,9 +86,8 @@ __device__ __forceinline__ double wave_sum64(double v) {
 // ---- short side up to 8: a wavefront per matrix, all in registers -----------------------------------
 // Lane l has the columns l, l + 64, ... of the long side; A is summed over the lanes and every lane has all of it.  Bound by the
 // reads and writes (and by latency where there are few matrices): the arithmetic of a 4 x 64 slice is 5 steps of 10 sums over the wavefront.
-template <class T, int S, int LC> __global__ void __launch_bounds__(TT_BLOCK) k_slices_small(TTSlices p) {
+template <class T, int S, int LC> __device__ __forceinline__ void slices_small(const TTSlices &p, long long z) {
   const int lane = threadIdx.x & 63;
-  const long long z = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (z >= p.batch) return;
   float x[LC][S];
   double sum = 0;
@@ -100,7 +149,7 @@ template <class T, int S, int LC> __global__ void __launch_bounds__(TT_BLOCK) k_
 
 // ---- short side up to 64, long side up to 512: a workgroup of eight wavefronts per matrix ------------
 // Each wavefront keeps 16 CT columns of X in registers, as results of the matrix instruction: lane (q, j) has rows 16 t + 4 q + i of
-// column j of each 16 x 16 tile.  fp32 products are six products of bf16 parts, as in tt_gemm.hip; X is at most one in norm,
+// column j of each 16 x 16 tile.  Columns are dealt so that a lane's are neighbours in memory (their order does not matter to X X^T).  fp32 products are six products of bf16 parts, as in tt_gemm.hip; X is at most one in norm,
 // so nothing over- or underflows that counts.
 //   A = X X^T: K runs over columns, of which a lane has one, so X's parts go through LDS, 32 columns at a time, [column][row], and come
 //     back by the transposing read.  Each wavefront sums over its own columns; the eight sums are added in order.
@@ -135,26 +184,40 @@ __device__ __forceinline__ f32x4 mma3(const u16x8 a[3], const u16x8 b[3], f32x4 
   return d;
 }
 
-template <class T, int MT, int CT> __global__ void __launch_bounds__(512, 1) k_slices_mid(TTSlices p) {
+template <class T, int MT, int CT> __device__ __forceinline__ void slices_mid(const TTSlices &p, long long z, unsigned short *lds, double *norms) {
   typedef Mid<MT, CT> G;
   constexpr int KS = (MT + 1) / 2;  // steps of 32 over the short side
-  __shared__ __align__(16) unsigned short lds[G::HALVES];
-  __shared__ double norms[8];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, q = lane >> 4, j = lane & 15;
-  const long long z = blockIdx.x;
   unsigned short *region = lds + wave * G::REGION, *pa = lds + 8 * G::REGION, *pb = lds;
+  const int l0 = (wave * 16 + j) * CT;  // the lane's columns are l0 + c
   f32x4 x[MT][CT];
+  if (p.in_l == 1) {
+#pragma unroll
+    for (int t = 0; t < MT; ++t)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float v[CT];
+        take_n<T, CT, true>(p, z, 16 * t + 4 * q + i, l0, v);
+#pragma unroll
+        for (int c = 0; c < CT; ++c) x[t][c][i] = v[c];
+      }
+  } else {
+#pragma unroll
+    for (int t = 0; t < MT; ++t)
+#pragma unroll
+      for (int c = 0; c < CT; ++c) {
+        float v[4];
+        take_n<T, 4, false>(p, z, 16 * t + 4 * q, l0 + c, v);
+        x[t][c] = f32x4{v[0], v[1], v[2], v[3]};
+      }
+  }
   double sum = 0;
 #pragma unroll
   for (int t = 0; t < MT; ++t)
 #pragma unroll
     for (int c = 0; c < CT; ++c)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int s = 16 * t + 4 * q + i, l = (wave * CT + c) * 16 + j;
-        x[t][c][i] = s < p.shorter && l < p.longer ? take<T>(p, z, s, l) : 0.f;
-        sum += (double)x[t][c][i] * x[t][c][i];
-      }
+      for (int i = 0; i < 4; ++i) sum += (double)x[t][c][i] * x[t][c][i];
   sum = wave_sum64(sum);
   if (lane == 0) norms[wave] = sum;
   __syncthreads();
@@ -167,10 +230,7 @@ template <class T, int MT, int CT> __global__ void __launch_bounds__(512, 1) k_s
 #pragma unroll
     for (int c = 0; c < CT; ++c)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int s = 16 * t + 4 * q + i, l = (wave * CT + c) * 16 + j;
-        x[t][c][i] = s < p.shorter && l < p.longer ? (float)((double)x[t][c][i] * scale) : 0.f;
-      }
+      for (int i = 0; i < 4; ++i) x[t][c][i] = (float)((double)x[t][c][i] * scale);  // (zeros outside: of a matrix that is NaN they are NaN too, and not stored)
 
   // rows 16 t .. + 15 of A or B: lane (q, j) has row j at k = 32 s + 4 q + i and 32 s + 16 + 4 q + i
   auto read = [&](const unsigned short *base, int t, int s, u16x8 f[3]) {
@@ -213,6 +273,7 @@ template <class T, int MT, int CT> __global__ void __launch_bounds__(512, 1) k_s
       for (int a = 0; a < MT; ++a)
 #pragma unroll
         for (int b = a; b < MT; ++b, ++n) sums[n] = mma3(f[b], f[a], sums[n]);  // lane (q, j): row 16 a + j, columns 16 b + 4 q + i
+      __builtin_amdgcn_sched_barrier(0);  // (one pair of column tiles after the other: with both at once the registers do not suffice)
     }
 #pragma unroll
     for (int n = 0; n < G::TILES; ++n) *reinterpret_cast<f32x4 *>(reinterpret_cast<float *>(region) + n * 256 + lane * 4) = sums[n];
@@ -292,54 +353,106 @@ template <class T, int MT, int CT> __global__ void __launch_bounds__(512, 1) k_s
         for (int h = 0; h < 2; ++h)
 #pragma unroll
           for (int i = 0; i < 4; ++i) x[t][c + h][i] = fmaf(ca, x[t][c + h][i], v[h][i]);
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
     __syncthreads();  // B is read no more: X's parts take its place
   }
+  if (p.out_l == 1) {
 #pragma unroll
-  for (int t = 0; t < MT; ++t)
-#pragma unroll
-    for (int c = 0; c < CT; ++c)
+    for (int t = 0; t < MT; ++t)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const int s = 16 * t + 4 * q + i, l = (wave * CT + c) * 16 + j;
-        if (s < p.shorter && l < p.longer) give<T>(p, z, s, l, x[t][c][i]);
+        float v[CT];
+#pragma unroll
+        for (int c = 0; c < CT; ++c) v[c] = x[t][c][i];
+        give_n<T, CT, true>(p, z, 16 * t + 4 * q + i, l0, v);
       }
+  } else {
+#pragma unroll
+    for (int t = 0; t < MT; ++t)
+#pragma unroll
+      for (int c = 0; c < CT; ++c) {
+        float v[4] = {x[t][c][0], x[t][c][1], x[t][c][2], x[t][c][3]};
+        give_n<T, 4, false>(p, z, 16 * t + 4 * q, l0 + c, v);
+      }
+  }
 }
 
-template <class T> tt_status launch(const TTSlices &p, hipStream_t s) {
-  if (p.shorter <= 8 && p.longer <= 512) {
-    const dim3 grid((unsigned)((p.batch + 3) / 4)), block(TT_BLOCK);
-    if (p.shorter <= 4) {
-      if (p.longer <= 64) hipLaunchKernelGGL((k_slices_small<T, 4, 1>), grid, block, 0, s, p);
-      else if (p.longer <= 128) hipLaunchKernelGGL((k_slices_small<T, 4, 2>), grid, block, 0, s, p);
-      else hipLaunchKernelGGL((k_slices_small<T, 4, 8>), grid, block, 0, s, p);
-    } else {
-      if (p.longer <= 128) hipLaunchKernelGGL((k_slices_small<T, 8, 2>), grid, block, 0, s, p);
-      else hipLaunchKernelGGL((k_slices_small<T, 8, 8>), grid, block, 0, s, p);
-    }
-    return tt_launch_status();
-  }
-  const dim3 grid((unsigned)p.batch), block(512);
-  const bool wide = p.longer > 256;
-  if (p.shorter <= 16) {
-    if (wide) hipLaunchKernelGGL((k_slices_mid<T, 1, 4>), grid, block, 0, s, p);
-    else hipLaunchKernelGGL((k_slices_mid<T, 1, 2>), grid, block, 0, s, p);
-  } else if (p.shorter <= 32) {
-    if (wide) hipLaunchKernelGGL((k_slices_mid<T, 2, 4>), grid, block, 0, s, p);
-    else hipLaunchKernelGGL((k_slices_mid<T, 2, 2>), grid, block, 0, s, p);
+// ---- launches --------------------------------------------------------------------------------------
+// A batch with a short side above 8 and two of smaller matrices in one launch, in workgroups of 512 threads: the small slices of a
+// table's cores 0 and 2 run beside the last slices of core 1, which has the launch's length.
+struct Jobs {
+  TTSlices mid, small[2];
+  int mid_blocks, small_blocks;  // of the first small batch
+};
+template <class T> __device__ __forceinline__ void small_job(const TTSlices &p, int block) {
+  const long long z = (long long)block * 8 + (threadIdx.x >> 6);
+  if (p.shorter <= 4) {
+    if (p.longer <= 64) slices_small<T, 4, 1>(p, z);
+    else if (p.longer <= 128) slices_small<T, 4, 2>(p, z);
+    else slices_small<T, 4, 8>(p, z);
   } else {
-    if (wide) hipLaunchKernelGGL((k_slices_mid<T, 4, 4>), grid, block, 0, s, p);
-    else hipLaunchKernelGGL((k_slices_mid<T, 4, 2>), grid, block, 0, s, p);
+    if (p.longer <= 128) slices_small<T, 8, 2>(p, z);
+    else slices_small<T, 8, 8>(p, z);
   }
-  return tt_launch_status();
+}
+template <class T, int MT, int CT> __global__ void __launch_bounds__(512, 1) k_slices(Jobs jobs) {
+  __shared__ __align__(16) unsigned short lds[Mid<MT, CT>::HALVES];
+  __shared__ double norms[8];
+  int block = (int)blockIdx.x;
+  if (block < jobs.mid_blocks) {
+    slices_mid<T, MT, CT>(jobs.mid, block, lds, norms);
+    return;
+  }
+  block -= jobs.mid_blocks;
+  if (block < jobs.small_blocks) small_job<T>(jobs.small[0], block);
+  else small_job<T>(jobs.small[1], block - jobs.small_blocks);
+}
+
+template <class T> tt_status launch(const TTSlices *p, int n, hipStream_t s) {
+  Jobs jobs;
+  for (int first = 0; first < n;) {  // each launch: as many as fit of those that follow each other
+    int mids = 0, smalls = 0, next = first;
+    long long blocks = 0;
+    memset(&jobs, 0, sizeof(jobs));
+    for (; next < n; ++next) {
+      const TTSlices &q = p[next];
+      const long long b = q.shorter > 8 ? q.batch : (q.batch + 7) / 8;
+      if (b > TT_MAX_WORKGROUPS / 4) return TT_ERR_SHAPE;
+      if (q.shorter > 8) {
+        if (mids || smalls) break;
+        jobs.mid = q;
+        jobs.mid_blocks = (int)b;
+        ++mids;
+      } else {
+        if (smalls == 2 || blocks + b > TT_MAX_WORKGROUPS / 2) break;
+        jobs.small[smalls++] = q;
+        if (smalls == 1) jobs.small_blocks = (int)b;
+      }
+      blocks += b;
+    }
+    first = next;
+    const int tall = mids ? jobs.mid.shorter : 0, wide = mids ? jobs.mid.longer : 0;
+    const dim3 grid((unsigned)blocks), block(512);
+    if (blocks == 0) continue;
+    if (tall <= 16 && wide <= 256) hipLaunchKernelGGL((k_slices<T, 1, 2>), grid, block, 0, s, jobs);
+    else if (tall <= 16) hipLaunchKernelGGL((k_slices<T, 1, 4>), grid, block, 0, s, jobs);
+    else if (tall <= 32 && wide <= 256) hipLaunchKernelGGL((k_slices<T, 2, 2>), grid, block, 0, s, jobs);
+    else if (tall <= 32) hipLaunchKernelGGL((k_slices<T, 2, 4>), grid, block, 0, s, jobs);
+    else if (wide <= 256) hipLaunchKernelGGL((k_slices<T, 4, 2>), grid, block, 0, s, jobs);
+    else hipLaunchKernelGGL((k_slices<T, 4, 4>), grid, block, 0, s, jobs);
+    const tt_status st = tt_launch_status();
+    if (st != TT_OK) return st;
+  }
+  return TT_OK;
 }
 
 }  // namespace
 
 bool ttk_slices_serves(long long shorter, long long longer) { return shorter <= 64 && longer <= 512; }
 
-tt_status ttk_slices(const TTSlices &p, hipStream_t s) {
-  if (p.batch > TT_MAX_WORKGROUPS / 2) return TT_ERR_SHAPE;  // (512 threads a matrix)
-  return p.dtype == TT_F32 ? launch<float>(p, s) : p.dtype == TT_BF16 ? launch<ttg::bf16>(p, s) : launch<ttg::f16>(p, s);
+tt_status ttk_slices(const TTSlices *p, int n, hipStream_t s) {
+  if (n < 1) return TT_OK;
+  return p->dtype == TT_F32 ? launch<float>(p, n, s) : p->dtype == TT_BF16 ? launch<ttg::bf16>(p, n, s) : launch<ttg::f16>(p, n, s);
 }

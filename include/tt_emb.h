@@ -434,11 +434,11 @@ typedef enum {
  * HOST struct, read during the call only.
  */
 #define TT_DENSE_MAX_DIM (1 << 20)
-#define TT_DENSE_MAX_GROUPS 65536
+#define TT_DENSE_MAX_GROUPS 32768
 typedef struct {
   int32_t dtype;       /* tt_dtype of every tensor of the call                                   */
   int32_t activation;  /* tt_activation                                                          */
-  int64_t rows;        /* rows of x, fewer than 2^31 - 2^17 - 1                                  */
+  int64_t rows;        /* rows of x, fewer than 2^31 - 2^16 - 1                                  */
   int32_t in_dim, out_dim; /* 1 .. TT_DENSE_MAX_DIM                                              */
   int32_t groups;      /* 0, or 1 .. TT_DENSE_MAX_GROUPS                                         */
   int32_t zero_rest;   /* rows of no group: 0 left as they were, 1 cleared                       */

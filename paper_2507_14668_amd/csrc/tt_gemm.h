@@ -24,6 +24,7 @@ struct TTGemm {
   int M, N, K;                 // RAGGED_M: M rows in all; RAGGED_K: K stored rows in all
   int batch;                   // members or groups
   const int64_t *offsets;      // DEVICE [batch + 1], ragged modes
+  int symmetric;               // BATCH: out is symmetric (A and B are one operand, res is symmetric): half its tiles are computed
   int zero_rest;               // RAGGED_M: rows of out outside every group are cleared (else left as they were)
   const void *bias;            // [N], nullable
   const void *res;             // nullable
@@ -37,13 +38,19 @@ struct TTGemm {
 
 // Long sums over few tiles of out are cut into pieces of K that run side by side; the pieces' sums go to `partial` and a
 // second launch adds them in order.  How many follows from types and sizes alone, so that a caller's workspace query knows.
-size_t ttk_gemm_partial_bytes(const TTGemm &g);  // 0: not split
+size_t ttk_gemm_partial_bytes(const TTGemm &g);  // 0: not cut (addresses are not looked at: enough for any)
 // Enqueues the product.  partial: ttk_gemm_partial_bytes(g) bytes of DEVICE memory, 256-byte aligned.
 tt_status ttk_gemm(const TTGemm &g, void *partial, hipStream_t s);
 
+// Rows of a group from which its sum is cut, for tiles of e x e (RAGGED_K); `least` steps of bk at least.
+int ttk_gemm_chunk(const TTGemm &g, int e, int bk, int least);
+size_t ttk_gemm_chunk_bytes(const TTGemm &g, int chunk);  // of the pieces' sums
+tt_status ttk_gemm_join_groups(const TTGemm &g, int chunk, int bk, const float *partial, hipStream_t s);
 // Large 16-bit products on aligned operands (tt_gemm_direct.hip); ttk_gemm passes them on.
 bool ttk_gemm_direct_serves(const TTGemm &g);
-tt_status ttk_gemm_direct(const TTGemm &g, hipStream_t s);
+int ttk_gemm_direct_chunk(const TTGemm &g);  // 0: nothing is cut
+size_t ttk_gemm_direct_bytes(const TTGemm &g);
+tt_status ttk_gemm_direct(const TTGemm &g, void *partial, hipStream_t s);
 // Few rows with a K-contiguous weight (tt_gemm_rows.hip); likewise.
 bool ttk_gemm_rows_serves(const TTGemm &g);
 tt_status ttk_gemm_rows(const TTGemm &g, hipStream_t s);

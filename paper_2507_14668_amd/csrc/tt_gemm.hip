@@ -28,8 +28,51 @@ template <class T> struct Unit;
 template <> struct Unit<float> { f32x4 a, b; };
 template <> struct Unit<bf16> { u16x8 v; };
 template <> struct Unit<f16> { u16x8 v; };
-template <class T> __device__ __forceinline__ Unit<T> load_unit(const T *p, int valid) {
+// `valid` of them exist.  A row of 8 and more has its last ones by a load that ends with them (one at a time, the lanes at the end of
+// a row had the whole step wait for them).
+template <class T> __device__ __forceinline__ Unit<T> load_unit(const T *p, int valid, bool long_row) {
   Unit<T> u;
+  if (long_row && valid > 0 && valid < 8) {
+    const int by = 8 - valid;
+    unsigned d[sizeof(T) * 2];
+    if constexpr (sizeof(T) == 4) {
+      u.a = *reinterpret_cast<const typename Vec<float>::v4 *>(p - by);
+      u.b = *reinterpret_cast<const typename Vec<float>::v4 *>(p - by + 4);
+    } else {
+      u.v = *reinterpret_cast<const typename Vec<T>::v16b *>(p - by);
+    }
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        d[i] = __float_as_uint(u.a[i]);
+        d[4 + i] = __float_as_uint(u.b[i]);
+      }
+#pragma unroll
+      for (int s = 1; s < 8; s *= 2)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) d[i] = (by & s) ? (i + s < 8 ? d[i + s] : 0u) : d[i];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        u.a[i] = __uint_as_float(d[i]);
+        u.b[i] = __uint_as_float(d[4 + i]);
+      }
+    } else {
+      typedef unsigned u4 __attribute__((ext_vector_type(4)));
+      const u4 w = __builtin_bit_cast(u4, u.v);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) d[i] = w[i];
+      if (by & 1) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) d[i] = (d[i] >> 16) | (i < 3 ? d[i + 1] << 16 : 0u);
+      }
+#pragma unroll
+      for (int s = 1; s < 4; s *= 2)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) d[i] = (by & (2 * s)) ? (i + s < 4 ? d[i + s] : 0u) : d[i];
+      u.v = __builtin_bit_cast(u16x8, u4{d[0], d[1], d[2], d[3]});
+    }
+    return u;
+  }
   if constexpr (sizeof(T) == 4) {
     u.a = u.b = f32x4{0.f, 0.f, 0.f, 0.f};
     if (valid >= 8) {
@@ -59,8 +102,10 @@ template <class T, bool KC, int E> struct Carrier {
   static constexpr int BK = Step<T>::BK, N = E * BK / 8 / TT_BLOCK;
   const T *p[N];
   int valid[N];
+  bool long_row;
   long long step;
-  __device__ __forceinline__ void start(const T *base, long long ld, int row0, int rows, int k_first) {
+  __device__ __forceinline__ void start(const T *base, long long ld, int row0, int rows, int k_first, int k_end) {
+    long_row = (KC ? k_end - k_first : rows - row0) >= 8;
     step = KC ? BK : (long long)BK * ld;
 #pragma unroll
     for (int i = 0; i < N; ++i) {
@@ -82,7 +127,7 @@ template <class T, bool KC, int E> struct Carrier {
     for (int i = 0; i < N; ++i) {
       const int n = threadIdx.x + i * TT_BLOCK;
       const int left = K - k0 - (KC ? (n % (BK / 8)) * 8 : n / (E / 8));
-      u[i] = load_unit(p[i], KC ? (left < valid[i] ? left : valid[i]) : (left > 0 ? valid[i] : 0));
+      u[i] = load_unit<T>(p[i], KC ? (left < valid[i] ? left : valid[i]) : (left > 0 ? valid[i] : 0), long_row);
       p[i] += step;
     }
   }
@@ -148,11 +193,10 @@ template <bool KC, int LD32> __device__ __forceinline__ f32x4 frag32(const float
 // a sum that is not finite, or with a sum below 2^-80 beside operands whose smallest product is that small, is done
 // again with the fp32 instruction.  (P = 2 is for operands that are scaled to at most one, with no such products that count.)
 template <class T, class O, int P, bool AKC, bool BKC, int E>
-__global__ void __launch_bounds__(TT_BLOCK, 2) k_gemm(TTGemm g, int m_tiles, int n_tiles, int split, float *partial) {
+__global__ void __launch_bounds__(TT_BLOCK, 2) k_gemm(TTGemm g, int m_tiles, int n_tiles, int split, int chunk, float *partial) {
   typedef Carrier<T, AKC, E> CA;
   typedef Carrier<T, BKC, E> CB;
-  constexpr int D = 1;
-  constexpr int BK = Step<T>::BK, PLANE = E * BK, F = E / 32, BUF = P == 1 ? 2 : 1;  // fp32's planes fill the LDS of two workgroups with one buffer
+    constexpr int BK = Step<T>::BK, PLANE = E * BK, F = E / 32, BUF = P == 1 ? 2 : 1;  // fp32's planes fill the LDS of two workgroups with one buffer
   constexpr int HALVES = 2 * BUF * P * PLANE, REDO = P == 3 ? 2 * (CA::SIZE32 + CB::SIZE32) : 0,
                 FINISH = 8 * finish_floats<F, 2>();
   __shared__ __align__(16) unsigned short lds[HALVES > REDO ? (HALVES > FINISH ? HALVES : FINISH) : (REDO > FINISH ? REDO : FINISH)];
@@ -160,11 +204,12 @@ __global__ void __launch_bounds__(TT_BLOCK, 2) k_gemm(TTGemm g, int m_tiles, int
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int members = (int)gridDim.y / split, cut = (int)blockIdx.y / members;  // which piece of K
   unsigned mt, nt;
-  tile_order(blockIdx.x, (unsigned)m_tiles, (unsigned)n_tiles, mt, nt);
+  tile_order(blockIdx.x, (unsigned)m_tiles, (unsigned)n_tiles, g.symmetric, mt, nt);
   Place w;
   w.n0 = (int)nt * E;
   w.k_lo = 0;
   w.k_hi = g.K;
+  float *piece = nullptr;
   if (g.mode == TT_GEMM_RAGGED_M) {
     const int there = find_tile<E>(g.offsets, g.batch, g.M, (int)mt, w.z, w.lo, w.hi);
     if (w.z < 0) {
@@ -175,9 +220,15 @@ __global__ void __launch_bounds__(TT_BLOCK, 2) k_gemm(TTGemm g, int m_tiles, int
     w.z = (int)blockIdx.y - cut * members;
     w.lo = (int)mt * E;
     w.hi = g.M < w.lo + E ? g.M : w.lo + E;
-    if (g.mode == TT_GEMM_RAGGED_K) group_rows(g.offsets, w.z, g.K, w.k_lo, w.k_hi);
+    if (g.mode == TT_GEMM_RAGGED_K) {
+      int pieces = 1, number = 0;
+      find_slot(g.offsets, g.batch, g.K, chunk, BK, (int)blockIdx.y, w.z, w.k_lo, w.k_hi, pieces, number);
+      if (w.z < 0) return;
+      if (pieces > 1) piece = partial + number * piece_floats(g);
+    }
   }
   if (split > 1) {  // whole steps to each piece
+    piece = partial + ((long long)cut * g.batch + w.z) * piece_floats(g);
     const int steps = (w.k_hi - w.k_lo + BK - 1) / BK, per = (steps + split - 1) / split;
     const long long a = (long long)w.k_lo + (long long)cut * per * BK, b = a + (long long)per * BK;
     if (a < w.k_hi) w.k_lo = (int)a;
@@ -189,9 +240,9 @@ __global__ void __launch_bounds__(TT_BLOCK, 2) k_gemm(TTGemm g, int m_tiles, int
   const int K = w.k_hi;
   CA ca;
   CB cb;
-  ca.start(a, g.lda, w.lo, w.hi, w.k_lo);
-  cb.start(b, g.ldb, w.n0, g.N, w.k_lo);
-  Unit<T> ua[D][CA::N], ub[D][CB::N];
+  ca.start(a, g.lda, w.lo, w.hi, w.k_lo, K);
+  cb.start(b, g.ldb, w.n0, g.N, w.k_lo, K);
+  Unit<T> ua[CA::N], ub[CB::N];
   const int wm = (wave >> 1) * (E / 2), wn = (wave & 1) * (E / 2);
   f32x4 acc[F][F] = {}, rs[F] = {};  // [m][n]; sums of A's rows
   const bool sums = g.rowsum && w.n0 == 0;
@@ -250,46 +301,33 @@ __global__ void __launch_bounds__(TT_BLOCK, 2) k_gemm(TTGemm g, int m_tiles, int
     }
   };
   if (w.k_lo < K) {
-#pragma unroll
-    for (int d = 0; d < D; ++d)
-      if (w.k_lo + d * BK < K) {
-        ca.load(ua[d], w.k_lo + d * BK, K);
-        cb.load(ub[d], w.k_lo + d * BK, K);
-      }
+    ca.load(ua, w.k_lo, K);
+    cb.load(ub, w.k_lo, K);
     if constexpr (BUF == 2) {
-      ca.template store<P>(ua[0], plane_a(0, 0));
-      cb.template store<P>(ub[0], plane_b(0, 0));
+      ca.template store<P>(ua, plane_a(0, 0));
+      cb.template store<P>(ub, plane_b(0, 0));
     }
     int buf = 0;
-    for (int k1 = w.k_lo; k1 < K; k1 += D * BK) {
-#pragma unroll
-      for (int d = 0; d < D; ++d) {
-        const int k0 = k1 + d * BK;
-        if (k0 >= K) break;
-        if constexpr (BUF == 2) {
-          __syncthreads();  // this step's tiles are whole, and nobody reads the other buffer any more
-          if (k0 + D * BK < K) {
-            ca.load(ua[d], k0 + D * BK, K);
-            cb.load(ub[d], k0 + D * BK, K);
-          }
-          multiply(buf);
-          if (k0 + BK < K) {
-            ca.template store<P>(ua[(d + 1) % D], plane_a(buf ^ 1, 0));
-            cb.template store<P>(ub[(d + 1) % D], plane_b(buf ^ 1, 0));
-          }
-          buf ^= 1;
-        } else {
-          __syncthreads();
-          note(ua[d], CA::N, small_a);
-          note(ub[d], CB::N, small_b);
-          ca.template store<P>(ua[d], plane_a(0, 0));
-          cb.template store<P>(ub[d], plane_b(0, 0));
-          __syncthreads();
-          if (k0 + D * BK < K) {
-            ca.load(ua[d], k0 + D * BK, K);
-            cb.load(ub[d], k0 + D * BK, K);
-          }
-          multiply(0);
+    for (int k0 = w.k_lo; k0 < K; k0 += BK) {
+      const bool more = k0 + BK < K;
+      __syncthreads();  // two buffers: this step's tiles are whole, and nobody reads the other buffer any more
+      if constexpr (BUF == 1) {
+        note(ua, CA::N, small_a);
+        note(ub, CB::N, small_b);
+        ca.template store<P>(ua, plane_a(0, 0));
+        cb.template store<P>(ub, plane_b(0, 0));
+        __syncthreads();
+      }
+      if (more) {
+        ca.load(ua, k0 + BK, K);
+        cb.load(ub, k0 + BK, K);
+      }
+      multiply(buf);
+      if constexpr (BUF == 2) {
+        buf ^= 1;
+        if (more) {
+          ca.template store<P>(ua, plane_a(buf, 0));
+          cb.template store<P>(ub, plane_b(buf, 0));
         }
       }
     }
@@ -340,14 +378,14 @@ __global__ void __launch_bounds__(TT_BLOCK, 2) k_gemm(TTGemm g, int m_tiles, int
 #pragma unroll
         for (int y = 0; y < F; ++y) acc[x][y] = f32x4{0.f, 0.f, 0.f, 0.f};
       }
-      ca.start(a, g.lda, w.lo, w.hi, w.k_lo);
-      cb.start(b, g.ldb, w.n0, g.N, w.k_lo);
+      ca.start(a, g.lda, w.lo, w.hi, w.k_lo, K);
+      cb.start(b, g.ldb, w.n0, g.N, w.k_lo, K);
       for (int k0 = w.k_lo; k0 < K; k0 += BK) {
-        ca.load(ua[0], k0, K);
-        cb.load(ub[0], k0, K);
+        ca.load(ua, k0, K);
+        cb.load(ub, k0, K);
         __syncthreads();
-        ca.store32(ua[0], l32a);
-        cb.store32(ub[0], l32b);
+        ca.store32(ua, l32a);
+        cb.store32(ub, l32b);
         __syncthreads();
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -372,52 +410,41 @@ __global__ void __launch_bounds__(TT_BLOCK, 2) k_gemm(TTGemm g, int m_tiles, int
     }
   }
   const int q = lane >> 4, j = lane & 15;
-  if (split > 1) {
-    float *piece = partial + ((long long)cut * g.batch + w.z) * g.M * (g.N + 1LL);  // [M][N] sums, then [M] sums of A's rows
-#pragma unroll
-    for (int x = 0; x < F; ++x) {
-      const int m = w.lo + wm + 16 * x + j;
-      if (m >= w.hi) continue;
-#pragma unroll
-      for (int y = 0; y < F; ++y) {
-        const int n = w.n0 + wn + 16 * y + 4 * q, valid = g.N - n < 4 ? g.N - n : 4;
-        const float v[4] = {acc[x][y][0], acc[x][y][1], acc[x][y][2], acc[x][y][3]};
-        if (valid > 0) store4(piece + (long long)m * g.N + n, valid, v);
-      }
-      if (sums && wn == 0 && q == 0) piece[(long long)g.M * g.N + m] = rs[x][0];
-    }
-    return;
-  }
   if (sums && wn == 0 && q == 0) {
 #pragma unroll
     for (int x = 0; x < F; ++x) {
       const int m = w.lo + wm + 16 * x + j;
-      if (m < w.hi) ((O *)g.rowsum)[w.z * g.rs_step + m] = from_f32<O>(rs[x][0]);
+      if (m >= w.hi) continue;
+      if (piece) piece[(long long)g.M * g.N + m] = rs[x][0];
+      else ((O *)g.rowsum)[w.z * g.rs_step + m] = from_f32<O>(rs[x][0]);
     }
   }
   __syncthreads();  // nobody reads the operands any more
-  finish_tile<T, O, F, F, 2>(g, w.z, w.lo + wm, w.hi, w.n0 + wn, acc, reinterpret_cast<float *>(lds) + wave * finish_floats<F, 2>());
+  float *room = reinterpret_cast<float *>(lds) + wave * finish_floats<F, 2>();
+  const bool mirror = g.symmetric && mt != nt;
+  if (piece) finish_tile<T, float, F, F, 2>(as_piece(g, piece), 0, w.lo + wm, w.hi, w.n0 + wn, acc, room, mirror);
+  else finish_tile<T, O, F, F, 2>(g, w.z, w.lo + wm, w.hi, w.n0 + wn, acc, room, mirror);
 }
 
-// The pieces of a split product, added in order; four columns of a row per thread.
-template <class T, class O> __global__ void __launch_bounds__(TT_BLOCK) k_join(TTGemm g, int split, const float *__restrict__ partial) {
-  const int per = (g.N + 3) / 4, z = (int)blockIdx.y;
-  const long long total = (long long)g.M * per, piece = (long long)g.M * (g.N + 1LL);
-  const float *p = partial + z * piece;
+// The pieces of a cut product, added in order; four columns of a row per thread.
+template <class T, class O> __device__ __forceinline__ void join_pieces(const TTGemm &g, int z, int pieces, const float *p, long long step) {
+  const int per = (g.N + 3) / 4;
+  const long long total = (long long)g.M * per;
   for (long long e = (long long)blockIdx.x * TT_BLOCK + threadIdx.x; e < total + g.M; e += (long long)gridDim.x * TT_BLOCK) {
     if (e >= total) {
       if (!g.rowsum) continue;
       const long long m = e - total;
       float s = 0.f;
-      for (int i = 0; i < split; ++i) s += p[i * g.batch * piece + (long long)g.M * g.N + m];
+      for (int i = 0; i < pieces; ++i) s += p[i * step + (long long)g.M * g.N + m];
       ((O *)g.rowsum)[z * g.rs_step + m] = from_f32<O>(s);
       continue;
     }
     const int m = (int)(e / per), n = (int)(e - (long long)m * per) * 4, valid = g.N - n < 4 ? g.N - n : 4;
     f32x4 s = {0.f, 0.f, 0.f, 0.f};
-    for (int i = 0; i < split; ++i) {
+#pragma unroll 4
+    for (int i = 0; i < pieces; ++i) {
       float t[4];
-      load4(p + i * g.batch * piece + (long long)m * g.N + n, valid, t);
+      load4(p + i * step + (long long)m * g.N + n, valid, t);
 #pragma unroll
       for (int c = 0; c < 4; ++c) s[c] += t[c];
     }
@@ -425,13 +452,22 @@ template <class T, class O> __global__ void __launch_bounds__(TT_BLOCK) k_join(T
     finish<T, O, 4>(g, z, m, n, valid, v);
   }
 }
+template <class T, class O> __global__ void __launch_bounds__(TT_BLOCK) k_join(TTGemm g, int split, const float *__restrict__ partial) {
+  const int z = (int)blockIdx.y;
+  join_pieces<T, O>(g, z, split, partial + z * piece_floats(g), g.batch * piece_floats(g));
+}
+template <class T> __global__ void __launch_bounds__(TT_BLOCK) k_join_groups(TTGemm g, int chunk, int bk, const float *__restrict__ partial) {
+  int z = (int)blockIdx.y, lo = 0, hi = 0, pieces = 1, first = 0;
+  find_slot(g.offsets, g.batch, g.K, chunk, bk, -1, z, lo, hi, pieces, first);
+  if (z >= 0) join_pieces<T, T>(g, z, pieces, partial + first * piece_floats(g), piece_floats(g));
+}
 
 // ---- host ------------------------------------------------------------------------------------------
 #ifndef TT_GEMM_LARGE_TILES
 #define TT_GEMM_LARGE_TILES 256  // tiles of 128 from which they are taken
 #endif
 struct Shape {
-  int e, split;
+  int e, split, chunk;
   long long m_tiles, n_tiles, members;
 };
 Shape shape_of(const TTGemm &g) {
@@ -444,52 +480,99 @@ Shape shape_of(const TTGemm &g) {
     h.n_tiles = tt_ceil_div(g.N, e);
     h.members = g.mode == TT_GEMM_RAGGED_M ? 1 : g.batch;
     h.e = e;
-    return (long long)tt_ceil_div(g.M, e) * tt_ceil_div(g.like_N ? g.like_N : g.N, e) * h.members;
+    const long long n = (long long)tt_ceil_div(g.M, e) * tt_ceil_div(g.like_N ? g.like_N : g.N, e) * h.members;
+    return n;
   };
   long long n = tiles(128);
   if (n < TT_GEMM_LARGE_TILES) n = tiles(64);
+  if (g.symmetric) n = (n + h.members * h.m_tiles) / 2;
   // two workgroups and more run on a compute unit: long sums in pieces up to 512 workgroups in all, of eight steps at least
+  // (of four where even so most compute units have none)
   h.split = 1;
-  if (g.mode != TT_GEMM_RAGGED_M) {
-    long long steps = tt_ceil_div(g.K, bk);
-    if (g.mode == TT_GEMM_RAGGED_K) steps = tt_ceil_div(steps, g.batch);  // of a group of the average size
+  h.chunk = 0;
+  if (g.mode == TT_GEMM_BATCH) {
+    const long long steps = tt_ceil_div(g.K, bk);
     long long split = 512 / n;
-    if (split > steps / 8) split = steps / 8;
+    const long long least = n * (steps / 4) <= 128 ? 4 : 8;
+    if (split > steps / least) split = steps / least;
     if (split > 64) split = 64;
     if (split > 1) h.split = (int)split;
+  } else if (g.mode == TT_GEMM_RAGGED_K) {
+    h.chunk = ttk_gemm_chunk(g, h.e, bk, h.e == 64 ? 8 : 32);
+    if (g.like_N && g.N != g.like_N) {  // (cut as the whole product of aligned operands would be)
+      TTGemm whole = g;
+      whole.N = g.like_N;
+      whole.b = g.a;
+      whole.ldb = 8;
+      if (ttk_gemm_direct_serves(whole)) h.chunk = ttk_gemm_direct_chunk(whole);
+    }
+    h.members = tt_ceil_div(g.K, h.chunk) + g.batch;  // slots
   }
   return h;
 }
 
 template <class T, class O, int P, int E> void launch_e(const TTGemm &g, const Shape &h, float *part, hipStream_t s) {
-  const dim3 grid((unsigned)(h.m_tiles * h.n_tiles), (unsigned)(h.members * h.split));
-  const int mti = (int)h.m_tiles, nti = (int)h.n_tiles, split = h.split;
-  if (g.a_kc && g.b_kc) hipLaunchKernelGGL((k_gemm<T, O, P, true, true, E>), grid, dim3(TT_BLOCK), 0, s, g, mti, nti, split, part);
-  else if (g.a_kc) hipLaunchKernelGGL((k_gemm<T, O, P, true, false, E>), grid, dim3(TT_BLOCK), 0, s, g, mti, nti, split, part);
-  else hipLaunchKernelGGL((k_gemm<T, O, P, false, false, E>), grid, dim3(TT_BLOCK), 0, s, g, mti, nti, split, part);
+  const long long per_member = g.symmetric ? h.n_tiles * (h.n_tiles + 1) / 2 : h.m_tiles * h.n_tiles;
+  const dim3 grid((unsigned)per_member, (unsigned)(h.members * h.split));
+  const int mti = (int)h.m_tiles, nti = (int)h.n_tiles, split = h.split, chunk = h.chunk;
+  if (g.a_kc && g.b_kc) hipLaunchKernelGGL((k_gemm<T, O, P, true, true, E>), grid, dim3(TT_BLOCK), 0, s, g, mti, nti, split, chunk, part);
+  else if (g.a_kc) hipLaunchKernelGGL((k_gemm<T, O, P, true, false, E>), grid, dim3(TT_BLOCK), 0, s, g, mti, nti, split, chunk, part);
+  else hipLaunchKernelGGL((k_gemm<T, O, P, false, false, E>), grid, dim3(TT_BLOCK), 0, s, g, mti, nti, split, chunk, part);
+}
+unsigned join_blocks(const TTGemm &g) {
+  long long blocks = ((long long)g.M * ((g.N + 3) / 4) + g.M + TT_BLOCK - 1) / TT_BLOCK;
+  return (unsigned)(blocks > 4096 ? 4096 : blocks);
 }
 template <class T, class O, int P> tt_status launch(const TTGemm &g, void *partial, hipStream_t s) {
   const Shape h = shape_of(g);
   if (h.m_tiles * h.n_tiles > TT_MAX_WORKGROUPS || h.m_tiles * h.n_tiles * h.members * h.split > TT_MAX_WORKGROUPS || h.members * h.split > 65535)
     return TT_ERR_SHAPE;
-  if (h.split > 1 && !partial) return TT_ERR_WORKSPACE;
+  if ((h.split > 1 || h.chunk) && !partial) return TT_ERR_WORKSPACE;
   float *part = (float *)partial;
   if (h.e == 128) launch_e<T, O, P, 128>(g, h, part, s);
   else launch_e<T, O, P, 64>(g, h, part, s);
   if (h.split > 1) {
-    long long blocks = ((long long)g.M * ((g.N + 3) / 4) + g.M + TT_BLOCK - 1) / TT_BLOCK;
-    if (blocks > 4096) blocks = 4096;
     const int split = h.split;
-    hipLaunchKernelGGL((k_join<T, O>), dim3((unsigned)blocks, (unsigned)h.members), dim3(TT_BLOCK), 0, s, g, split, (const float *)part);
+    hipLaunchKernelGGL((k_join<T, O>), dim3(join_blocks(g), (unsigned)h.members), dim3(TT_BLOCK), 0, s, g, split, (const float *)part);
   }
-  return tt_launch_status();
+  const tt_status st = tt_launch_status();
+  return st == TT_OK && h.chunk ? ttk_gemm_join_groups(g, h.chunk, g.dtype == TT_F32 ? 32 : 64, part, s) : st;
 }
 
 }  // namespace
 
+// About as many workgroups as run at once, and pieces long enough that writing and adding their sums does not count: a tile of 256
+// costs as much as 24 steps of it.
+int ttk_gemm_chunk(const TTGemm &g, int e, int bk, int least) {
+  const long long tiles = (long long)tt_ceil_div(g.M, e) * tt_ceil_div(g.like_N ? g.like_N : g.N, e), steps = tt_ceil_div(g.K, bk);
+  long long per = (steps * tiles + 511) / 512;
+  if (per < least) per = least;
+  if (per < steps / 16384) per = steps / 16384;  // slots are a grid's second side
+  const long long chunk = per * bk;
+  return (int)(chunk > 1073741824LL ? 1073741824LL : chunk);
+}
+size_t ttk_gemm_chunk_bytes(const TTGemm &g, int chunk) {
+  // groups of several pieces have fewer than 2 rows / chunk each, the rest none
+  const long long slots = 2 * ((long long)g.K / chunk);
+  return ((size_t)slots * g.M * (g.N + 1LL) * 4 + 255) & ~(size_t)255;
+}
+tt_status ttk_gemm_join_groups(const TTGemm &g, int chunk, int bk, const float *partial, hipStream_t s) {
+  const int most = g.K / chunk < g.batch ? g.K / chunk : g.batch;  // groups that can have two pieces
+  if (most < 1) return TT_OK;
+  const dim3 grid(join_blocks(g), (unsigned)most);
+  if (g.dtype == TT_F32) hipLaunchKernelGGL(k_join_groups<float>, grid, dim3(TT_BLOCK), 0, s, g, chunk, bk, partial);
+  else if (g.dtype == TT_BF16) hipLaunchKernelGGL(k_join_groups<ttg::bf16>, grid, dim3(TT_BLOCK), 0, s, g, chunk, bk, partial);
+  else hipLaunchKernelGGL(k_join_groups<ttg::f16>, grid, dim3(TT_BLOCK), 0, s, g, chunk, bk, partial);
+  return tt_launch_status();
+}
+
 size_t ttk_gemm_partial_bytes(const TTGemm &g) {
   if (g.M < 1 || g.N < 1 || g.batch < 1 || ttk_gemm_rows_serves(g)) return 0;
   const Shape h = shape_of(g);
+  if (h.chunk) {
+    const size_t a = ttk_gemm_chunk_bytes(g, h.chunk), b = ttk_gemm_direct_bytes(g);
+    return a > b ? a : b;
+  }
   return h.split < 2 ? 0 : (((size_t)h.split * g.batch * g.M * (g.N + 1LL) * 4) + 255) & ~(size_t)255;
 }
 
@@ -497,7 +580,7 @@ tt_status ttk_gemm(const TTGemm &g, void *partial, hipStream_t s) {
   if (g.M < 1 || g.N < 1 || g.batch < 1) return TT_OK;
   if (!g.a_kc && g.b_kc) return TT_ERR_INVALID_ARG;  // no caller needs it
   if (ttk_gemm_rows_serves(g)) return ttk_gemm_rows(g, s);
-  if (ttk_gemm_direct_serves(g)) return ttk_gemm_direct(g, s);
+  if (ttk_gemm_direct_serves(g)) return ttk_gemm_direct(g, partial, s);
   if (g.dtype == TT_BF16 && g.out_dtype == TT_BF16) return launch<ttg::bf16, ttg::bf16, 1>(g, partial, s);
   if (g.dtype == TT_F16 && g.out_dtype == TT_F16) return launch<ttg::f16, ttg::f16, 1>(g, partial, s);
   if (g.dtype != TT_F32) return TT_ERR_INVALID_ARG;

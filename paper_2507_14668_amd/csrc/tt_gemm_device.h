@@ -179,19 +179,6 @@ __device__ __forceinline__ int wave_max_scan(int v) {
 }
 __device__ __forceinline__ int clamp_row(int64_t o, int rows) { return o < 0 ? 0 : (o > rows ? rows : (int)o); }
 
-// Rows [lo, hi) of group z (the whole wavefront calls it).
-__device__ __forceinline__ void group_rows(const int64_t *off, int z, int rows, int &lo, int &hi) {
-  const int lane = threadIdx.x & 63;
-  int m = 0;
-  for (int g = lane; g <= z; g += 64) {
-    const int v = clamp_row(off[g], rows);
-    if (v > m) m = v;
-  }
-  lo = __shfl(wave_max_scan(m), 63, 64);
-  const int e = clamp_row(off[z + 1], rows);
-  hi = e > lo ? e : lo;
-}
-
 // Tile t of the row tiles of TM rows, counted group after group: its group and rows [lo, lo + count).  Returns the tiles there
 // are; for t at or behind that, `lo` and `hi` are the first and the end of the rows that groups cover.
 template <int TM>
@@ -225,6 +212,45 @@ __device__ __forceinline__ int find_tile(const int64_t *off, int groups, int row
   return tiles;
 }
 
+// Sums over a group's rows are cut into pieces: ceil(rows / chunk) of them, of equal size in whole steps of `bk`, at least one. Slot t of all
+// the groups' pieces: its group (-1: there is no such slot) and rows [lo, hi), the group's number of pieces, and the slot's number
+// among those of groups that have several, which is where its sums go.  With `t` < 0: the group that is number `group` of those that have
+// several (-1: there is none), and its first slot's number.
+__device__ __forceinline__ void find_slot(const int64_t *off, int groups, int rows, int chunk, int bk, int t, int &group, int &lo, int &hi, int &pieces, int &number) {
+  const int lane = threadIdx.x & 63, asked = group;
+  int start = clamp_row(off[0], rows), slots = 0, several = 0, cut = 0;
+  group = -1;
+  for (int g0 = 0; g0 < groups; g0 += 64) {
+    const int g = g0 + lane;
+    int e = wave_max_scan(g < groups ? clamp_row(off[g + 1], rows) : 0);
+    if (e < start) e = start;
+    int b = __shfl_up(e, 1, 64);
+    if (lane == 0) b = start;
+    int mine = g < groups ? (int)(((long long)e - b + chunk - 1) / chunk) : 0;
+    if (g < groups && mine < 1) mine = 1;
+    const int incl = tt_wave_incl_scan(mine), incl2 = tt_wave_incl_scan(mine > 1 ? mine : 0);
+    const unsigned long long many = __ballot(mine > 1);
+    const int rank = cut + __popcll(many & ((1ull << lane) - 1));
+    const unsigned long long has = __ballot(t >= 0 ? t < slots + incl : mine > 1 && rank == asked);
+    cut += __popcll(many);
+    if (has) {
+      const int l = __ffsll(has) - 1, first = slots + __shfl(incl - mine, l, 64);
+      group = g0 + l;
+      pieces = __shfl(mine, l, 64);
+      const int nth = t >= 0 ? t - first : 0, from = __shfl(b, l, 64), to = __shfl(e, l, 64);
+      number = several + __shfl(incl2 - (mine > 1 ? mine : 0), l, 64) + nth;
+      const int steps = (to - from + bk - 1) / bk, per = (steps + pieces - 1) / pieces;
+      const long long x = from + (long long)nth * per * bk, y = x + (long long)per * bk;
+      lo = x < to ? (int)x : to;
+      hi = y < to ? (int)y : to;
+      return;
+    }
+    slots += __shfl(incl, 63, 64);
+    several += __shfl(incl2, 63, 64);
+    start = __shfl(e, 63, 64);
+  }
+}
+
 // ---- matrix instructions -------------------------------------------------------------------------
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 // D[16 x 16] += A[16 x 32] B[32 x 16]: lane l holds A[l % 16][8 (l / 16) + i], B[8 (l / 16) + i][l % 16], D[4 (l / 16) + i][l % 16]
@@ -250,9 +276,17 @@ struct Place {
 };
 // Workgroups go round the eight dies by their number; each die gets neighbouring tiles, and within them eight row tiles
 // take a column tile together, so that what they read of both operands is in the die's L2.
-__device__ __forceinline__ void tile_order(unsigned t, unsigned m_tiles, unsigned n_tiles, unsigned &mt, unsigned &nt) {
-  const unsigned total = m_tiles * n_tiles, per = total / 8, left = total % 8, die = t % 8;
+// Of a symmetric result only the tiles with mt <= nt, n (n + 1) / 2 of them.
+__device__ __forceinline__ void tile_order(unsigned t, unsigned m_tiles, unsigned n_tiles, bool symmetric, unsigned &mt, unsigned &nt) {
+  const unsigned total = symmetric ? n_tiles * (n_tiles + 1) / 2 : m_tiles * n_tiles, per = total / 8, left = total % 8, die = t % 8;
   t = die * per + (die < left ? die : left) + t / 8;
+  if (symmetric) {
+    nt = (unsigned)((sqrtf(8.f * (float)t + 1.f) - 1.f) * 0.5f);
+    while (nt * (nt + 1) / 2 > t) --nt;
+    while ((nt + 1) * (nt + 2) / 2 <= t) ++nt;
+    mt = t - nt * (nt + 1) / 2;
+    return;
+  }
   const unsigned band = t / (8 * n_tiles), rows = m_tiles - 8 * band < 8 ? m_tiles - 8 * band : 8, in = t - band * 8 * n_tiles;
   mt = 8 * band + in % rows;
   nt = in / rows;
@@ -297,9 +331,22 @@ __device__ __forceinline__ void finish(const TTGemm &g, int z, int m, int n, int
 // four columns of a row, 8 bytes of a 16-bit row at a time; through 16 XB rows of LDS (`lds`: finish_floats of the wavefront's own) a lane
 // gets eight, and what is read and written is whole lines of 128 bytes.  The loop over the rows is not unrolled: with all activations in it
 // 16 times, the code is longer than the instruction cache.
+// A product's description with its sums themselves as the result: piece `number` of a cut product, [M][N] and then [M] sums of A's rows.
+__device__ __forceinline__ long long piece_floats(const TTGemm &g) { return (long long)g.M * (g.N + 1LL); }
+__device__ __forceinline__ TTGemm as_piece(const TTGemm &g, float *piece) {
+  TTGemm p = g;
+  p.out = piece;
+  p.ldo = g.N;
+  p.o_step = 0;
+  p.alpha = 1.f;
+  p.bias = p.res = nullptr;
+  p.pre = nullptr;
+  p.act = TT_ACT_NONE;
+  return p;
+}
 template <int FY, int XB> constexpr int finish_floats() { return 16 * XB * (16 * FY + 4); }
 template <class T, class O, int FX, int FY, int XB>
-__device__ __forceinline__ void finish_tile(const TTGemm &g, int z, int m0, int end, int n0, const f32x4 (&acc)[FX][FY], float *lds) {
+__device__ __forceinline__ void finish_tile(const TTGemm &g, int z, int m0, int end, int n0, const f32x4 (&acc)[FX][FY], float *lds, bool mirror = false) {
   constexpr int LD = 16 * FY + 4, PER = 2 * FY, ROWS = 64 / PER;  // lanes of a row, rows at a time
   const int lane = threadIdx.x & 63, q = lane >> 4, j = lane & 15, c = 8 * (lane % PER), r = lane / PER;
   const int valid = g.N - n0 - c;
@@ -316,6 +363,16 @@ __device__ __forceinline__ void finish_tile(const TTGemm &g, int z, int m0, int 
       const f32x4 a = *reinterpret_cast<const f32x4 *>(lds + row * LD + c), b = *reinterpret_cast<const f32x4 *>(lds + row * LD + c + 4);
       float v[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
       if (m < end && valid > 0) finish<T, O, 8>(g, z, m, n0 + c, valid, v);
+    }
+    if (mirror) {  // the same results as rows n of columns m (only products without a bias)
+#pragma unroll 1
+      for (int e = lane; e < 16 * FY * 2 * XB; e += 64) {
+        const int row = e / (2 * XB), col = 8 * (e % (2 * XB)), n = n0 + row, m = m0 + 16 * x0 + col;
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = lds[(col + i) * LD + row];
+        if (n < g.N && m < end) finish<T, O, 8>(g, z, n, m, end - m, v);
+      }
     }
     tt_wave_lds_order();
   }

@@ -114,16 +114,17 @@ __device__ __forceinline__ void step_of(unsigned short *__restrict__ now, const 
   half_step<T, AKC, BKC>(next, 0, wm, wn, sums, fa, fb, acc, rs);
 }
 
-template <class T, bool AKC, bool BKC> __global__ void __launch_bounds__(THREADS, 2) k_gemm_direct(TTGemm g, int m_tiles, int n_tiles) {
+template <class T, bool AKC, bool BKC> __global__ void __launch_bounds__(THREADS, 2) k_gemm_direct(TTGemm g, int m_tiles, int n_tiles, int chunk, float *partial) {
   __shared__ __align__(16) unsigned short lds[16 * finish_floats<4, 4>()];  // (more than two buffers take)
   static_assert(16 * finish_floats<4, 4>() >= STAGES * 2 * OPERAND, "LDS");
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   unsigned mt, nt;
-  tile_order(blockIdx.x, (unsigned)m_tiles, (unsigned)n_tiles, mt, nt);
+  tile_order(blockIdx.x, (unsigned)m_tiles, (unsigned)n_tiles, false, mt, nt);
   Place w;
   w.n0 = (int)nt * E;
   w.k_lo = 0;
   w.k_hi = g.K;
+  float *piece = nullptr;
   if (g.mode == TT_GEMM_RAGGED_M) {
     const int there = find_tile<E>(g.offsets, g.batch, g.M, (int)mt, w.z, w.lo, w.hi);
     if (w.z < 0) {
@@ -134,7 +135,12 @@ template <class T, bool AKC, bool BKC> __global__ void __launch_bounds__(THREADS
     w.z = (int)blockIdx.y;
     w.lo = (int)mt * E;
     w.hi = g.M < w.lo + E ? g.M : w.lo + E;
-    if (g.mode == TT_GEMM_RAGGED_K) group_rows(g.offsets, w.z, g.K, w.k_lo, w.k_hi);
+    if (g.mode == TT_GEMM_RAGGED_K) {
+      int pieces = 1, number = 0;
+      find_slot(g.offsets, g.batch, g.K, chunk, BK, (int)blockIdx.y, w.z, w.k_lo, w.k_hi, pieces, number);
+      if (w.z < 0) return;
+      if (pieces > 1) piece = partial + (long long)__builtin_amdgcn_readfirstlane(number) * piece_floats(g);
+    }
   }
   w.z = __builtin_amdgcn_readfirstlane(w.z);
   w.lo = __builtin_amdgcn_readfirstlane(w.lo);
@@ -180,25 +186,38 @@ template <class T, bool AKC, bool BKC> __global__ void __launch_bounds__(THREADS
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int m = w.lo + wm + 16 * (4 * (lane >> 4) + i) + (lane & 15);
-        if (m < w.hi) ((T *)g.rowsum)[w.z * g.rs_step + m] = from_f32<T>(rs[i]);
+        if (m >= w.hi) continue;
+        if (piece) piece[(long long)g.M * g.N + m] = rs[i];
+        else ((T *)g.rowsum)[w.z * g.rs_step + m] = from_f32<T>(rs[i]);
       }
     }
   }
   __syncthreads();  // nobody reads the operands any more
-  finish_tile<T, T, 8, 4, 4>(g, w.z, w.lo + wm, w.hi, w.n0 + wn, acc, reinterpret_cast<float *>(lds) + wave * finish_floats<4, 4>());
+  float *room = reinterpret_cast<float *>(lds) + wave * finish_floats<4, 4>();
+  if constexpr (!AKC) {  // (only sums over stored rows are cut)
+    if (piece) {
+      finish_tile<T, float, 8, 4, 4>(as_piece(g, piece), 0, w.lo + wm, w.hi, w.n0 + wn, acc, room);
+      return;
+    }
+  }
+  finish_tile<T, T, 8, 4, 4>(g, w.z, w.lo + wm, w.hi, w.n0 + wn, acc, room);
 }
 
-template <class T> tt_status launch(const TTGemm &g, hipStream_t s) {
+template <class T> tt_status launch(const TTGemm &g, void *partial, hipStream_t s) {
   const long long n_tiles = tt_ceil_div(g.N, E);
   const long long m_tiles = g.mode == TT_GEMM_RAGGED_M ? (long long)tt_ceil_div(g.M, E) + g.batch + 1 : tt_ceil_div(g.M, E);
-  const long long members = g.mode == TT_GEMM_RAGGED_M ? 1 : g.batch;
+  const int chunk = ttk_gemm_direct_chunk(g);
+  const long long members = g.mode == TT_GEMM_RAGGED_M ? 1 : chunk ? (long long)tt_ceil_div(g.K, chunk) + g.batch : g.batch;
   if (m_tiles * n_tiles > TT_MAX_WORKGROUPS / 2 || m_tiles * n_tiles * members > TT_MAX_WORKGROUPS / 2 || members > 65535) return TT_ERR_SHAPE;
+  if (chunk && !partial) return TT_ERR_WORKSPACE;
   const dim3 grid((unsigned)(m_tiles * n_tiles), (unsigned)members);
   const int mti = (int)m_tiles, nti = (int)n_tiles;
-  if (g.a_kc && g.b_kc) hipLaunchKernelGGL((k_gemm_direct<T, true, true>), grid, dim3(THREADS), 0, s, g, mti, nti);
-  else if (g.a_kc) hipLaunchKernelGGL((k_gemm_direct<T, true, false>), grid, dim3(THREADS), 0, s, g, mti, nti);
-  else hipLaunchKernelGGL((k_gemm_direct<T, false, false>), grid, dim3(THREADS), 0, s, g, mti, nti);
-  return tt_launch_status();
+  float *part = (float *)partial;
+  if (g.a_kc && g.b_kc) hipLaunchKernelGGL((k_gemm_direct<T, true, true>), grid, dim3(THREADS), 0, s, g, mti, nti, chunk, part);
+  else if (g.a_kc) hipLaunchKernelGGL((k_gemm_direct<T, true, false>), grid, dim3(THREADS), 0, s, g, mti, nti, chunk, part);
+  else hipLaunchKernelGGL((k_gemm_direct<T, false, false>), grid, dim3(THREADS), 0, s, g, mti, nti, chunk, part);
+  const tt_status st = tt_launch_status();
+  return st == TT_OK && chunk ? ttk_gemm_join_groups(g, chunk, BK, part, s) : st;
 }
 
 }  // namespace
@@ -207,7 +226,7 @@ template <class T> tt_status launch(const TTGemm &g, hipStream_t s) {
 #define TT_GEMM_DIRECT_TILES 192  // tiles of 256 from which they are taken
 #endif
 bool ttk_gemm_direct_serves(const TTGemm &g) {
-  if (g.dtype == TT_F32 || g.out_dtype != g.dtype) return false;
+  if (g.dtype == TT_F32 || g.out_dtype != g.dtype || g.symmetric) return false;
   const uintptr_t addresses = (uintptr_t)g.a | (uintptr_t)g.b;
   if ((addresses & 15) || ((g.lda | g.ldb | g.a_step | g.b_step) & 7)) return false;
   if (((g.a_kc || g.b_kc) && (g.K & 7)) || (!g.a_kc && (g.M & 7)) || (!g.b_kc && (g.N & 7))) return false;
@@ -216,4 +235,8 @@ bool ttk_gemm_direct_serves(const TTGemm &g) {
   return tiles >= TT_GEMM_DIRECT_TILES;
 }
 
-tt_status ttk_gemm_direct(const TTGemm &g, hipStream_t s) { return g.dtype == TT_BF16 ? launch<ttg::bf16>(g, s) : launch<ttg::f16>(g, s); }
+int ttk_gemm_direct_chunk(const TTGemm &g) { return g.mode == TT_GEMM_RAGGED_K ? ttk_gemm_chunk(g, E, BK, 64) : 0; }
+size_t ttk_gemm_direct_bytes(const TTGemm &g) { return g.mode == TT_GEMM_RAGGED_K && g.dtype != TT_F32 ? ttk_gemm_chunk_bytes(g, ttk_gemm_direct_chunk(g)) : 0; }
+tt_status ttk_gemm_direct(const TTGemm &g, void *partial, hipStream_t s) {
+  return g.dtype == TT_BF16 ? launch<ttg::bf16>(g, partial, s) : launch<ttg::f16>(g, partial, s);
+}

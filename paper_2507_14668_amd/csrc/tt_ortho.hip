@@ -96,12 +96,14 @@ Products products(const Mats &m, int dtype) {
   g.parts = dtype == TT_F32 ? 3 : 2;
   // A = X X^T, or X^T X
   p.gram = g;
+  p.gram.symmetric = 1;
   p.gram.a_kc = p.gram.b_kc = tall ? 0 : 1;
   p.gram.M = p.gram.N = side; p.gram.K = tall ? m.rows : m.cols;
   p.gram.lda = p.gram.ldb = m.cols; p.gram.a_step = p.gram.b_step = elems;
   p.gram.ldo = side; p.gram.o_step = sq;
   // B = b A + c A A (A is symmetric)
   p.square = g;
+  p.square.symmetric = 1;
   p.square.a_kc = p.square.b_kc = 1;
   p.square.M = p.square.N = p.square.K = side;
   p.square.lda = p.square.ldb = p.square.ldo = p.square.ldr = side;

@@ -105,6 +105,7 @@ CASES = [
     (90, 9, 33, torch.float16, "gelu", [5, 8, 80], 2, 1),
     (30, 16, 16, torch.float32, "none", [0, 20, 10, 25], 0, 0),      # not in order: the running maximum counts
     (30, 16, 16, torch.bfloat16, "none", [-4, 12, 99], 0, 0),        # outside: clamped
+    (600, 9, 12, torch.float32, "silu", [0, 20, 570, 600], 0, 0),    # a group whose sum over rows is cut
     (300, 72, 264, torch.bfloat16, "silu", [0, 130, 130, 299], 8, 0),
     (270, 136, 40, torch.float16, "relu", None, 0, 0),
     (20, 8, 8, torch.float32, "relu", [20, 20], 0, 0),               # one group, without rows
@@ -207,7 +208,7 @@ def test_dense_refusals(lib):
     assert call(ok()) == 0
     assert lib.tt_dense_forward(None, gx.ptr, gw.ptr, None, None, out.ptr, None, ws.ptr, 4096, None) == binding.TT_ERR_INVALID_ARG
     for name, bad, status in (("dtype", 3, -1), ("dtype", -1, -1), ("activation", 5, -1), ("rows", -1, -1), ("rows", 2 ** 31, -2), ("in_dim", 0, -2),
-                              ("out_dim", 0, -2), ("in_dim", 2 ** 20 + 1, -2), ("out_dim", 2 ** 20 + 1, -2), ("groups", -1, -1), ("groups", 65537, -2),
+                              ("out_dim", 0, -2), ("in_dim", 2 ** 20 + 1, -2), ("out_dim", 2 ** 20 + 1, -2), ("groups", -1, -1), ("groups", 32769, -2),
                               ("ld_x", 7, -2), ("ld_out", 3, -2), ("ld_residual", 3, -2), ("ld_grad", 3, -2), ("ld_dx", 7, -2), ("ld_x", -8, -2),
                               ("ld_x", 2 ** 41, -2)):
         op = ok()

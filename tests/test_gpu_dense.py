@@ -67,6 +67,9 @@ SIZES = [
     (8200, 2056, 520, None, 8, 0),
     (6000, 96, 700, (2500, 0, 1, 3499), 0, 0),
     (5000, 328, 1030, (130, 2700, 5, 2100), 6, 0),
+    (12000, 1024, 1024, (9300, 0, 3, 257, 1000, 64, 700, 128, 300, 1, 100, 147), 0, 0),
+    (9000, 64, 40, (8000, 10, 990), 0, 0),
+    (9000, 33, 47, (10, 8000, 0, 990), 1, 1),
     (30, 128, 512, (3, 0, 1, 26), 0, 0),
     (100, 64, 72, (1,) * 100, 0, 0),
     (515, 128, 128, (0, 256, 0, 1, 258, 0), 0, 0),
@@ -360,7 +363,7 @@ def test_refusals(tt):
 
 # ---- orthogonalised updates ------------------------------------------------------------------------
 ORTHO = [(1, 1, 1), (3, 1, 40), (2, 40, 1), (7, 4, 64), (7, 64, 4), (2, 64, 512), (1, 512, 128), (3, 100, 260), (1, 129, 129), (2, 128, 700), (1, 300, 290),
-         (1, 700, 333), (40, 33, 17), (1, 16, 3000), (1, 2500, 24), (2, 130, 1000), (1, 1024, 768)]
+         (1, 700, 333), (40, 33, 17), (1, 16, 3000), (1, 2500, 24), (2, 130, 1000), (1, 1024, 768), (1, 1200, 1500)]
 
 
 @pytest.mark.parametrize("dtype", DTYPES, ids=str)

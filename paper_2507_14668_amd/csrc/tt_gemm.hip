@@ -463,8 +463,11 @@ template <class T> __global__ void __launch_bounds__(TT_BLOCK) k_join_groups(TTG
 }
 
 // ---- host ------------------------------------------------------------------------------------------
+// Tiles of 128 from which they are taken.  These / tiles of 64, us: fp32 4096 x 2048 x 512 (512 tiles) 57 / 71 and its gradients 69 / 87 and
+// 72 / 93, 2048 x 2048 x 512 (256) 45 / 38, 42 / 49 and 43 / 51, 2048 x 1024 x 1024 (128) 46 / 44; fp16 2048 x 2048 x 520 18 / 15, 26 / 28 and
+// 26 / 30, 2048 x 1024 x 1024 27 / 15.
 #ifndef TT_GEMM_LARGE_TILES
-#define TT_GEMM_LARGE_TILES 256  // tiles of 128 from which they are taken
+#define TT_GEMM_LARGE_TILES 256
 #endif
 struct Shape {
   int e, split, chunk;

@@ -222,8 +222,11 @@ template <class T> tt_status launch(const TTGemm &g, void *partial, hipStream_t 
 
 }  // namespace
 
+// Tiles of 256 from which they are taken: a workgroup fills a compute unit, and fewer leave too many without.  bf16, these / tiles of 128
+// and 64, us: 2048 x 2048 x 2048 (64 tiles) 52 / 46, 2048 x 4096 x 1024 (128) 33 / 32, 4096 x 2560 x 1024 (160) 35 / 52, 4096 x 4096 x 1024
+// (256) 37 / 61; 64 weights of 1024 x 1024 over 32768 uneven rows 157 / 204.
 #ifndef TT_GEMM_DIRECT_TILES
-#define TT_GEMM_DIRECT_TILES 192  // tiles of 256 from which they are taken
+#define TT_GEMM_DIRECT_TILES 144
 #endif
 bool ttk_gemm_direct_serves(const TTGemm &g) {
   if (g.dtype == TT_F32 || g.out_dtype != g.dtype || g.symmetric) return false;

@@ -122,12 +122,18 @@ template <class T> tt_status launch_t(const TTGemm &g, hipStream_t s) {
 
 }  // namespace
 
+// Up to 32 rows (of a group of the average size) always; more while there are few workgroups and the rows that each of them reads are
+// short.  These / tiles, us: bf16 16 x 512 x 512 3.4 / 8.3, 64 x 4096 x 1024 7.5 / 11.8, 256 x 512 x 512 4.9 / 8.8, 128 x 1024 x 1024 7.0 / 9.5,
+// 96 x 4096 x 1024 11.8 / 12.7, 64 x 4096 x 4096 21.7 / 17.1, 128 x 4096 x 4096 41 / 22; fp32 64 x 512 x 512 8.0 / 10.8, 128 x 1024 x 1024 14.4 / 15.0.
 #ifndef TT_GEMM_FEW_ROWS
-#define TT_GEMM_FEW_ROWS 64  // up to this many rows (of a group of the average size)
+#define TT_GEMM_FEW_ROWS 32
 #endif
 bool ttk_gemm_rows_serves(const TTGemm &g) {
-  if (g.out_dtype != g.dtype || !g.a_kc || !g.b_kc || g.rowsum || g.mode == TT_GEMM_RAGGED_K || g.parts == 2) return false;
-  return (g.mode == TT_GEMM_RAGGED_M ? tt_ceil_div(g.M, g.batch) : g.M) <= TT_GEMM_FEW_ROWS;
+  if (g.out_dtype != g.dtype || !g.a_kc || !g.b_kc || g.rowsum || g.symmetric || g.mode == TT_GEMM_RAGGED_K || g.parts == 2) return false;
+  const int rows = g.mode == TT_GEMM_RAGGED_M ? tt_ceil_div(g.M, g.batch) : g.M;
+  if (rows <= TT_GEMM_FEW_ROWS) return true;
+  const long long bytes = (long long)g.K * (g.dtype == TT_F32 ? 4 : 2), groups = (long long)tt_ceil_div(rows, 64) * tt_ceil_div(g.N, 16) * g.batch;
+  return TT_GEMM_FEW_ROWS > 0 && rows <= 256 && bytes <= 4096 && groups <= 256;
 }
 tt_status ttk_gemm_rows(const TTGemm &g, hipStream_t s) {
   return g.dtype == TT_F32 ? launch_t<float>(g, s) : g.dtype == TT_BF16 ? launch_t<ttg::bf16>(g, s) : launch_t<ttg::f16>(g, s);

@@ -193,12 +193,13 @@ bool steps_ok(int steps, const float *coefficients, float eps) {
   return true;
 }
 bool size_ok(int64_t batch, int64_t rows, int64_t cols) {
-  if (rows < 1 || cols < 1 || rows > TT_ORTHO_MAX_SIDE || cols > TT_ORTHO_MAX_SIDE) return false;
-  const int64_t side = rows < cols ? rows : cols;
-  // the largest launch is that of 64 x 64 tiles of the matrices
-  return batch >= 0 && batch * (rows * cols) < ((int64_t)1 << 36) && batch * (side * side) < ((int64_t)1 << 36) &&
-         batch * tt_ceil_div(rows, 64) * tt_ceil_div(cols, 64) <= TT_MAX_WORKGROUPS && batch * kMaxParts <= TT_MAX_WORKGROUPS &&
-         (batch <= 65535 || (side <= 64 && (rows > cols ? rows : cols) <= 512));  // (larger matrices: one of a grid's second side each)
+  if (rows < 1 || cols < 1 || batch < 0 || rows > TT_ORTHO_MAX_SIDE || cols > TT_ORTHO_MAX_SIDE) return false;
+  const int64_t side = rows < cols ? rows : cols, most = (int64_t)1 << 36;
+  if (batch > most / (rows * cols) || batch > most / (side * side)) return false;
+  if (ttk_slices_serves(side, rows < cols ? cols : rows)) return batch <= TT_MAX_WORKGROUPS / 4;
+  // a matrix is one of a grid's second side (and is cut along K only where there are few); the norm's launch has all parts of all matrices
+  return batch <= 65535 && batch * parts_of(rows * cols) <= TT_MAX_WORKGROUPS &&
+         batch * tt_ceil_div(rows, 64) * tt_ceil_div(cols, 64) <= TT_MAX_WORKGROUPS;
 }
 
 // ---- TT cores --------------------------------------------------------------------------------------

@@ -116,11 +116,15 @@ def tt_dense(x, w, bias=None, residual=None, activation="none", offsets=None):
     """`act(x w^T + bias) + residual`, differentiable in its four tensors; grouped by `offsets` as in
     `binding.tt_dense_forward`.  Rows of no group give zeros and get none: their residual is not added, and its gradient there
     is left out too."""
-    if residual is not None and offsets is not None and residual.requires_grad and torch.is_grad_enabled():
+    train = torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (x, w, bias, residual))
+    if train and residual is not None and offsets is not None and residual.requires_grad:
         residual = _GroupRows.apply(residual, offsets)
     if bias is not None and not bias.is_contiguous():
         bias = bias.contiguous()
-    return _DenseFunction.apply(_row_major(x), w if w.is_contiguous() else w.contiguous(), bias, _row_major(residual), activation, offsets)
+    x, w, residual = _row_major(x), w if w.is_contiguous() else w.contiguous(), _row_major(residual)
+    if not train:  # nothing is kept for a backward pass
+        return binding.tt_dense_forward(x, w, bias, residual, activation, offsets=offsets)
+    return _DenseFunction.apply(x, w, bias, residual, activation, offsets)
 
 
 class _GroupRows(torch.autograd.Function):
@@ -335,6 +339,7 @@ class TTFusedEmbeddingBags(torch.nn.Module):
             for b in bags:
                 ends.append(ends[-1] + b)
             self._table_rows = ((bags, device), torch.tensor(ends, dtype=torch.int64, device=device))
+        self._table_rows[1].record_stream(torch.cuda.current_stream(device))  # (it may be replaced while this call's work is under way)
         return self._table_rows[1]
 
     def member_core(self, t: int, k: int, core=None):
@@ -500,7 +505,15 @@ class TTOrthoSGD(torch.optim.Optimizer):
         rest = [p for p in model.parameters() if id(p) not in taken]
         groups = [dict(params=ps, kind=kind, lr=rate) for ps, kind, rate in
                   ((cores, "cores", lr), (matrices, "matrices", lr), (rest, "rest", lr if other_lr is None else other_lr)) if ps]
-        super().__init__(groups, dict(momentum=momentum, nesterov=nesterov, steps=steps, coefficients=coefficients, eps=eps))
+        super().__init__(groups, dict(kind="rest", momentum=momentum, nesterov=nesterov, steps=steps, coefficients=coefficients, eps=eps))
+
+    def load_state_dict(self, state_dict):
+        super().load_state_dict(state_dict)  # casts what it loads to the parameters' types
+        for mine, saved in zip(self.param_groups, state_dict["param_groups"]):
+            for p, name in zip(mine["params"], saved["params"]):
+                if name in state_dict["state"]:
+                    m = state_dict["state"][name]["momentum"]
+                    self.state[p]["momentum"] = m.to(device=p.device, dtype=torch.float32, copy=True).contiguous()
 
     def _momentum(self, p):
         state = self.state[p]

@@ -175,6 +175,13 @@ def test_dense_without_rows(lib):
     ws, dw, db = Guarded((1, need), torch.uint8), Guarded((4, 8), torch.float32), Guarded((1, 4), torch.float32)
     assert lib.tt_dense_backward(ctypes.byref(op), None, None, None, None, None, dw.ptr, db.ptr, ws.ptr, need, None) == 0
     assert bool((dw.t == 0).all()) and bool((db.t == 0).all()) and dw.intact() and db.intact()
+    # ... and of groups
+    x, w, bias, _, _ = make(0, 8, 4, torch.bfloat16, 3)
+    op = dense_op(x, w, "none", torch.zeros(4, dtype=torch.int64))
+    need = lib.tt_dense_workspace_bytes(ctypes.byref(op), 1)
+    ws, dw, db = Guarded((1, need), torch.uint8), Guarded((3, 4, 8), torch.bfloat16), Guarded((3, 4), torch.bfloat16)
+    assert lib.tt_dense_backward(ctypes.byref(op), None, None, None, None, None, dw.ptr, db.ptr, ws.ptr, need, None) == 0
+    assert bool((dw.t == 0).all()) and bool((db.t == 0).all()) and dw.intact() and db.intact()
 
 
 def test_dense_special_values(lib):

@@ -556,3 +556,56 @@ def test_dense_module(tt):
     with pytest.raises(ValueError):
         tt.TTDense(4, 4, dtype=torch.float64)
     assert tt.TTDense(4, 4, bias=False).bias is None
+
+
+def test_no_graph_is_built_without_gradients(tt):
+    x, w, bias, res, _ = make(9, 16, 8, torch.float32)
+    assert not tt.tt_dense(x, w, bias, res, "gelu").requires_grad
+    w.requires_grad_(True)
+    with torch.no_grad():
+        assert not tt.tt_dense(x, w, bias, res, "gelu").requires_grad
+    assert tt.tt_dense(x, w, bias, res, "gelu").requires_grad
+
+
+def test_optimizer_state_keeps_its_precision(tt):
+    layer = tt.TTDense(24, 16, dtype=torch.bfloat16)
+    opt = tt.TTOrthoSGD(layer, lr=0.01)
+    for i in range(3):
+        layer(torch.randn(40, 24, device="cuda").bfloat16()).float().square().mean().backward()
+        opt.step()
+    other = tt.TTDense(24, 16, dtype=torch.bfloat16)
+    again = tt.TTOrthoSGD(other, lr=0.5)
+    again.load_state_dict(opt.state_dict())
+    for a, b in ((layer.weight, other.weight), (layer.bias, other.bias)):
+        m = again.state[b]["momentum"]
+        assert m.dtype == torch.float32 and torch.equal(m, opt.state[a]["momentum"]) and m.data_ptr() != opt.state[a]["momentum"].data_ptr()
+    assert again.param_groups[0]["lr"] == 0.01
+
+
+def test_many_small_matrices(tt):
+    g = torch.randn(70000, 4, 6, generator=torch.Generator().manual_seed(1)) * 1e-2
+    out = tt.tt_orthogonalize(g.cuda()).cpu()
+    ref.check_ortho(out[::5000], g[::5000], "many")
+    ref.check_ortho(out[-3:], g[-3:], "many, the last")
+
+
+def test_rows_past_32_bits(tt):
+    """Rows whose elements lie beyond 2^31: the last rows of a tall operand, forward and backward."""
+    rows, k, n = (1 << 31) // 72 + 1000, 72, 8
+    x = torch.zeros(rows, k, dtype=torch.bfloat16, device="cuda")
+    x[-5:] = torch.randn(5, k, device="cuda").bfloat16()
+    w = torch.randn(n, k, device="cuda").bfloat16()
+    out = tt.tt_dense_forward(x, w)
+    want, tol, _, _ = ref.forward64(x[-5:].cpu(), w.cpu())
+    ref.check(out[-5:].cpu(), want, tol, "the last rows")
+    assert float(out[:-5].abs().max()) == 0
+    grad = torch.zeros(rows, n, dtype=torch.bfloat16, device="cuda")
+    grad[-5:] = torch.randn(5, n, device="cuda").bfloat16()
+    dx, dw, db = tt.tt_dense_backward(x, w, grad)
+    (wx, ww, wb), (tx, tw, tb) = ref.backward64(x[-5:].cpu(), w.cpu(), grad[-5:].cpu())
+    ref.check(dx[-5:].cpu(), wx, tx, "dx")
+    ref.check(dw.cpu(), ww, tw, "dw")
+    ref.check(db.cpu(), wb, tb, "dbias")
+    off = torch.tensor([0, rows - 3, rows], device="cuda")
+    g2 = tt.tt_dense_forward(x, torch.stack([w, -w]), offsets=off)
+    assert torch.equal(g2[-5:-3], out[-5:-3]) and torch.equal(g2[-3:], -out[-3:])

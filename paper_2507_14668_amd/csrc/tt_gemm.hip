@@ -102,9 +102,10 @@ template <class T, bool KC, int E> struct Carrier {
   static constexpr int BK = Step<T>::BK, N = E * BK / 8 / TT_BLOCK;
   const T *p[N];
   int valid[N];
-  bool long_row;
+  bool long_row, whole;  // whole: all rows of the tile are there
   long long step;
   __device__ __forceinline__ void start(const T *base, long long ld, int row0, int rows, int k_first, int k_end) {
+    whole = rows - row0 >= E;
     long_row = (KC ? k_end - k_first : rows - row0) >= 8;
     step = KC ? BK : (long long)BK * ld;
 #pragma unroll
@@ -123,6 +124,19 @@ template <class T, bool KC, int E> struct Carrier {
   }
   // the units of the step at k0 (K: the end), and on to the next step
   __device__ __forceinline__ void load(Unit<T> u[N], int k0, int K) {
+    if (whole && K - k0 >= BK) {  // the same for all lanes, and most steps
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        if constexpr (sizeof(T) == 4) {
+          u[i].a = *reinterpret_cast<const typename Vec<float>::v4 *>(p[i]);
+          u[i].b = *reinterpret_cast<const typename Vec<float>::v4 *>(p[i] + 4);
+        } else {
+          u[i].v = *reinterpret_cast<const typename Vec<T>::v16b *>(p[i]);
+        }
+        p[i] += step;
+      }
+      return;
+    }
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const int n = threadIdx.x + i * TT_BLOCK;
@@ -196,7 +210,7 @@ template <class T, class O, int P, bool AKC, bool BKC, int E>
 __global__ void __launch_bounds__(TT_BLOCK, 2) k_gemm(TTGemm g, int m_tiles, int n_tiles, int split, int chunk, float *partial) {
   typedef Carrier<T, AKC, E> CA;
   typedef Carrier<T, BKC, E> CB;
-    constexpr int BK = Step<T>::BK, PLANE = E * BK, F = E / 32, BUF = P == 1 ? 2 : 1;  // fp32's planes fill the LDS of two workgroups with one buffer
+    constexpr int BK = Step<T>::BK, PLANE = E * BK, F = E / 32, BUF = P == 1 ? 2 : 1;  // fp32's planes fill the LDS of two workgroups with one buffer (two planes: two buffers are no faster)
   constexpr int HALVES = 2 * BUF * P * PLANE, REDO = P == 3 ? 2 * (CA::SIZE32 + CB::SIZE32) : 0,
                 FINISH = 8 * finish_floats<F, 2>();
   __shared__ __align__(16) unsigned short lds[HALVES > REDO ? (HALVES > FINISH ? HALVES : FINISH) : (REDO > FINISH ? REDO : FINISH)];
@@ -246,7 +260,7 @@ __global__ void __launch_bounds__(TT_BLOCK, 2) k_gemm(TTGemm g, int m_tiles, int
   const int wm = (wave >> 1) * (E / 2), wn = (wave & 1) * (E / 2);
   f32x4 acc[F][F] = {}, rs[F] = {};  // [m][n]; sums of A's rows
   const bool sums = g.rowsum && w.n0 == 0;
-  unsigned small_a = ~0u, small_b = ~0u;  // twice the bits of the smallest number that is not zero, less one
+  // the smallest number that is not zero, as twice its bits less one
   auto note = [&](const Unit<T> *u, int n, unsigned &small) {
     if constexpr (P == 3) {
 #pragma unroll
@@ -312,8 +326,6 @@ __global__ void __launch_bounds__(TT_BLOCK, 2) k_gemm(TTGemm g, int m_tiles, int
       const bool more = k0 + BK < K;
       __syncthreads();  // two buffers: this step's tiles are whole, and nobody reads the other buffer any more
       if constexpr (BUF == 1) {
-        note(ua, CA::N, small_a);
-        note(ub, CB::N, small_b);
         ca.template store<P>(ua, plane_a(0, 0));
         cb.template store<P>(ub, plane_b(0, 0));
         __syncthreads();
@@ -336,41 +348,59 @@ __global__ void __launch_bounds__(TT_BLOCK, 2) k_gemm(TTGemm g, int m_tiles, int
     bool odd = false, tiny = false;
 #pragma unroll
     for (int x = 0; x < F; ++x) {
+      const bool in = w.lo + wm + 16 * x + (lane & 15) < w.hi;
 #pragma unroll
       for (int y = 0; y < F; ++y)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           odd |= !(fabsf(acc[x][y][i]) < INFINITY);
-          tiny |= fabsf(acc[x][y][i]) < 0x1p-80f;
+          tiny |= in && w.n0 + wn + 16 * y + 4 * (lane >> 4) + i < g.N && fabsf(acc[x][y][i]) < 0x1p-80f;
         }
       if (sums) {
         odd |= !(fabsf(rs[x][0]) < INFINITY);
-        tiny |= fabsf(rs[x][0]) < 0x1p-80f;
+        tiny |= in && fabsf(rs[x][0]) < 0x1p-80f;
       }
     }
-    // exponents of the smallest numbers of the workgroup; the two floats' product is below 2^-92 if the exponents' sum (each 127 too many) is
-    unsigned ea = small_a == ~0u ? 255 : small_a >> 24, eb = small_b == ~0u ? 255 : small_b >> 24;
+    // what any lane of the workgroup has seen: bits 0 and 1
+    auto any = [&](int mine) {
+      const int both = (__ballot(mine & 1) ? 1 : 0) | (__ballot(mine & 2) ? 2 : 0);
+      __syncthreads();
+      if (lane == 0) flags[wave] = both;
+      __syncthreads();
+      return flags[0] | flags[1] | flags[2] | flags[3];
+    };
+    int seen = any((odd ? 1 : 0) | (tiny ? 2 : 0));
+    if (seen == 2) {  // small sums (of rows of zeros, mostly): whether small operands are the reason takes another look at them
+      unsigned small_a = ~0u, small_b = ~0u;
+      ca.start(a, g.lda, w.lo, w.hi, w.k_lo, K);
+      cb.start(b, g.ldb, w.n0, g.N, w.k_lo, K);
+      for (int k0 = w.k_lo; k0 < K; k0 += BK) {
+        ca.load(ua, k0, K);
+        cb.load(ub, k0, K);
+        note(ua, CA::N, small_a);
+        note(ub, CB::N, small_b);
+      }
+      unsigned ea = small_a == ~0u ? 255 : small_a >> 24, eb = small_b == ~0u ? 255 : small_b >> 24;  // exponents
 #pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const unsigned x = (unsigned)__shfl((int)ea, lane ^ o, 64), y = (unsigned)__shfl((int)eb, lane ^ o, 64);
-      ea = x < ea ? x : ea;
-      eb = y < eb ? y : eb;
-    }
-    const int mine = (__ballot(odd) ? 1 << 16 : 0) | (__ballot(tiny) ? 1 << 17 : 0) | (int)ea << 8 | (int)eb;
-    if (lane == 0) flags[wave] = mine;
-    __syncthreads();
-    int all = 0;
-    ea = eb = 255;
+      for (int o = 1; o < 64; o <<= 1) {
+        const unsigned x = (unsigned)__shfl((int)ea, lane ^ o, 64), y = (unsigned)__shfl((int)eb, lane ^ o, 64);
+        ea = x < ea ? x : ea;
+        eb = y < eb ? y : eb;
+      }
+      __syncthreads();
+      if (lane == 0) flags[wave] = (int)(ea << 8 | eb);
+      __syncthreads();
+      ea = eb = 255;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int f = flags[i];
-      all |= f & (3 << 16);
-      ea = (unsigned)(f >> 8 & 255) < ea ? (unsigned)(f >> 8 & 255) : ea;
-      eb = (unsigned)(f & 255) < eb ? (unsigned)(f & 255) : eb;
+      for (int i = 0; i < 4; ++i) {
+        const unsigned x = (unsigned)flags[i] >> 8, y = (unsigned)flags[i] & 255;
+        ea = x < ea ? x : ea;
+        eb = y < eb ? y : eb;
+      }
+      // the smallest product is below 2^-92 if the exponents' sum (each 127 too many) is; parts themselves are whole down to 2^-100
+      if ((int)(ea + eb) - 254 < -92 || ea < 27 || eb < 27) seen = 1;
     }
-    // parts themselves are whole down to 2^-100
-    const bool under = (int)(ea + eb) - 254 < -92 || ea < 27 || eb < 27;
-    if ((all & (1 << 16)) || ((all & (1 << 17)) && under)) {
+    if (seen & 1) {
       float *l32a = reinterpret_cast<float *>(lds), *l32b = l32a + CA::SIZE32;
 #pragma unroll
       for (int x = 0; x < F; ++x) {

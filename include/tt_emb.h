@@ -410,7 +410,10 @@ tt_status tt_index_graph_edges(const int64_t *indices, const int64_t *offsets, i
 /*
  * Dense side.  What a model does with pooled rows right behind the bags, and how cores and dense weights
  * are updated by their orthogonalised gradients.  These calls take fp32, bf16 or fp16 data; sums are fp32
- * on the matrix cores and reproducible (no atomics); they allocate nothing and follow the conventions above.
+ * on the matrix cores and reproducible: the same call gives the same bits (no atomics; the order of a sum
+ * follows types, sizes and alignment).  fp32 operands are multiplied as three bf16 parts each, six products of
+ * them, no less exact than the fp32 instruction, which takes over where infinities, NaN or products near the ends of
+ * the range are met.  The calls allocate nothing and follow the conventions above.
  */
 typedef enum { TT_F32 = 0, TT_BF16 = 1, TT_F16 = 2 } tt_dtype;
 typedef enum {
@@ -460,7 +463,7 @@ typedef struct {
  * Backward, from grad_out = dL/d out:
  *   dz = grad_out act'(z), dx = dz W, dW = dz^T x (per group, zeros for an empty one), dbias = sums of dz;
  *   any of dx, dw, dbias may be NULL.  dL/d residual is grad_out itself.  dz is rounded to the dtype
- *   before the products.  x is needed for dw, w for dx, pre if there is an activation.
+ *   before the products and dbias's sums.  x is needed for dw, w for dx, pre if there is an activation.
  *   workspace  tt_dense_workspace_bytes(op, 1) bytes, as above.
  * tt_dense_workspace_bytes returns 0 on invalid arguments too.
  */
@@ -476,7 +479,8 @@ tt_status tt_dense_backward(const tt_dense *op, const void *x, const void *w, co
  *   X = G / (|G| + eps) with the Frobenius norm;  for each step, with its coefficients (a, b, c):
  *   X <- a X + (b A + c A^2) X,  A = X X^T           (a tall X from the other side: the same polynomial)
  * which takes every singular value s to a s + b s^3 + c s^5, step after step.  fp32 arithmetic whatever the
- * dtype (norms in 64 bits), the result rounded once.  A zero matrix gives zeros; one with an infinity or
+ * dtype (norms in 64 bits), the result rounded once; for 16-bit dtypes the factors of the products have 16
+ * bits of significand, for fp32 24.  A zero matrix gives zeros (NaN if eps is 0); one with an infinity or
  * a NaN gives NaN in all its entries and does not touch the others of the batch.
  *   coefficients HOST float[steps][3], finite; steps 1 .. TT_ORTHO_MAX_STEPS; eps >= 0
  *   g, out       DEVICE; out may be g itself (with the same steps).
@@ -486,7 +490,8 @@ tt_status tt_dense_backward(const tt_dense *op, const void *x, const void *w, co
 #define TT_ORTHO_MAX_SIDE (1 << 20)
 typedef struct {
   int32_t dtype;              /* tt_dtype of g and out                                           */
-  int64_t batch, rows, cols;  /* sides 1 .. TT_ORTHO_MAX_SIDE, batch * rows * cols < 2^36        */
+  int64_t batch, rows, cols;  /* sides 1 .. TT_ORTHO_MAX_SIDE, batch * rows * cols <= 2^36;
+                                 batch <= 65535 above 64 x 512                                  */
   int64_t batch_step, row_step;         /* elements between matrices / rows of g; 0: packed       */
   int64_t out_batch_step, out_row_step; /* ... of out                                            */
 } tt_matrices;

@@ -4,14 +4,19 @@
 namespace {
 using namespace ttg;
 
-// 256 x 256 of out per workgroup of eight wavefronts (128 x 64 each), in steps of 32 values of K through four buffers of 32 KB.  Every
+// 256 x 256 of out per workgroup of eight wavefronts (128 x 64 each), in steps of 64 values of K through two buffers of 64 KB.  Every
 // element is fetched once per tile and never passes through a register on its way to LDS: a tile of 128 x 128 through registers
-// (tt_gemm.hip) is bound by LDS, whose reads and writes take longer than its matrix instructions.  Loads are three steps ahead: 64 KB take
-// 0.9 us from a full L2, which is what they multiply in, so with two buffers of 64 values the matrix cores waited at every step.
+// (tt_gemm.hip) is bound by LDS, whose reads and writes take longer than its matrix instructions.  A step has two halves: while one
+// half's operands multiply, the next half's are read from LDS into the registers that fall free, and between the halves a step's buffer is
+// handed to the loads of the step after the next, which have a whole step to land.
 // A load puts 16 bytes a lane at consecutive places in LDS, so the order that spreads the reads over the banks is made
 // by which 16 bytes each lane fetches.  Needs 16-byte aligned rows and a K (K-contiguous) or a number of rows (row-contiguous) that is
 // a multiple of 8: pieces of 16 bytes are whole or outside.  Rows outside are read from a row inside (their results are not stored),
 // values of K outside from a piece of zeros.
+// Measured in bf16: 16384 x 4096 x 4096 527 us (1044 TFLOP/s; x W, both from rows 577, dz^T x 530), 8192^3 875 us (1257); the library's product
+// without an epilogue 353 and 757.  Without its last part the first takes 412 us: a tile's results are written while nothing multiplies
+// (one workgroup fills the LDS), and that is what bounds it now.  Tried and no faster: steps of 32 through four buffers (half lines of 128
+// bytes for K-contiguous operands, 590), touching lines of later steps so that they are in the L2 (517 / 654 / 655).
 constexpr int E = 256, BK = 64, THREADS = 512, OPERAND = E * BK;  // halves of an operand in a buffer
 constexpr int STAGES = 2, PIECES = 4;                             // loads of a thread for an operand and step
 __device__ __align__(16) unsigned short g_zeros[8];
@@ -234,6 +239,7 @@ bool ttk_gemm_direct_serves(const TTGemm &g) {
   if ((addresses & 15) || ((g.lda | g.ldb | g.a_step | g.b_step) & 7)) return false;
   if (((g.a_kc || g.b_kc) && (g.K & 7)) || (!g.a_kc && (g.M & 7)) || (!g.b_kc && (g.N & 7))) return false;
   if (g.lda > (1 << 23) || g.ldb > (1 << 23)) return false;  // offsets within a tile are 32 bits
+  if ((g.mode != TT_GEMM_RAGGED_M && g.M <= 128) || (g.like_N ? g.like_N : g.N) <= 128) return false;  // half a tile would be empty
   const long long tiles = (long long)tt_ceil_div(g.M, E) * tt_ceil_div(g.like_N ? g.like_N : g.N, E) * (g.mode == TT_GEMM_RAGGED_M ? 1 : g.batch);
   return tiles >= TT_GEMM_DIRECT_TILES;
 }

@@ -85,7 +85,7 @@ __device__ __forceinline__ double wave_sum64(double v) {
 
 // ---- short side up to 8: a wavefront per matrix, all in registers -----------------------------------
 // Lane l has the columns l, l + 64, ... of the long side; A is summed over the lanes and every lane has all of it.  Bound by the
-// reads and writes (and by latency where there are few matrices): the arithmetic of a 4 x 64 slice is 5 steps of 10 sums over the wavefront.
+// reads and writes, and by latency where there are few matrices: 5 steps of 10 sums over the wavefront for a 4 x 64 slice, 9 us for 342 of them.
 template <class T, int S, int LC> __device__ __forceinline__ void slices_small(const TTSlices &p, long long z) {
   const int lane = threadIdx.x & 63;
   if (z >= p.batch) return;
@@ -156,6 +156,9 @@ template <class T, int S, int LC> __device__ __forceinline__ void slices_small(c
 //   B = b A + c A A: 16 x 16 tiles dealt to the wavefronts.
 //   X <- a X + B X: K runs over rows: a lane's own rows are its operand as they are, in the order 16 t + 4 q + i of K, in
 //     which B is read too.
+// Measured: 342 slices of 64 x 512 (and 684 of 4 x 64) with momentum and the update of the cores 164 us, 42 of it reading and writing (228 MB: 47 us
+// at 4.9 TB/s with nothing else).  A workgroup takes a compute unit (150 KB of LDS, 256 registers), so 342 slices go in two rounds of
+// 256, the second a third full, and 12 us a step; of a step 5 us are X, 5 B and the adding of A's sums, which wait for LDS and barriers.
 template <int MT, int CT> struct Mid {
   static constexpr int ROWS = 16 * MT, TILES = MT * (MT + 1) / 2;
   static constexpr int XP = MT == 4 ? 80 : MT == 2 ? 48 : 16;  // halves between columns: four of them meet different banks

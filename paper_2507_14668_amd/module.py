@@ -115,7 +115,9 @@ def _row_major(t):
 def tt_dense(x, w, bias=None, residual=None, activation="none", offsets=None):
     """`act(x w^T + bias) + residual`, differentiable in its four tensors; grouped by `offsets` as in
     `binding.tt_dense_forward`.  Rows of no group give zeros and get none: their residual is not added, and its gradient there
-    is left out too."""
+    is left out too.  With an activation in training the pre-activation is kept in x's type for the backward pass.  (As with any autograd
+    function: a backward pass that is captured into a graph should accumulate into no leaf that an eager graph still holds;
+    `torch.autograd.grad` does not.)"""
     train = torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (x, w, bias, residual))
     if train and residual is not None and offsets is not None and residual.requires_grad:
         residual = _GroupRows.apply(residual, offsets)

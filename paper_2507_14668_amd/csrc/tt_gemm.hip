@@ -455,8 +455,8 @@ __global__ void __launch_bounds__(TT_BLOCK, 2) k_gemm(TTGemm g, int m_tiles, int
   __syncthreads();  // nobody reads the operands any more
   float *room = reinterpret_cast<float *>(lds) + wave * finish_floats<F, 2>();
   const bool mirror = g.symmetric && mt != nt;
-  if (piece) finish_tile<T, float, F, F, 2>(as_piece(g, piece), 0, w.lo + wm, w.hi, w.n0 + wn, acc, room, mirror);
-  else finish_tile<T, O, F, F, 2>(g, w.z, w.lo + wm, w.hi, w.n0 + wn, acc, room, mirror);
+  if (piece) finish_tile<T, float, F, F, 2, false>(as_piece(g, piece), 0, w.lo + wm, w.hi, w.n0 + wn, acc, room, mirror);
+  else finish_tile<T, O, F, F, 2, false>(g, w.z, w.lo + wm, w.hi, w.n0 + wn, acc, room, mirror);
 }
 
 // The pieces of a cut product, added in order; four columns of a row per thread.

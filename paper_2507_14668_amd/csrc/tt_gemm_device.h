@@ -40,7 +40,7 @@ template <class T> __device__ __forceinline__ void load4(const T *p, int valid, 
     for (int i = 0; i < 4; ++i) v[i] = i < valid ? to_f32(p[i]) : 0.f;
   }
 }
-template <class T> __device__ __forceinline__ void store4(T *p, int valid, const float v[4]) {
+template <class T, bool STREAM = false> __device__ __forceinline__ void store4(T *p, int valid, const float v[4]) {  // STREAM: past the caches
   if (valid >= 4) {
     typename Vec<T>::v4 r;
 #pragma unroll
@@ -48,7 +48,8 @@ template <class T> __device__ __forceinline__ void store4(T *p, int valid, const
       if constexpr (sizeof(T) == 4) r[i] = v[i];
       else r[i] = __builtin_bit_cast(unsigned short, from_f32<T>(v[i]));
     }
-    *reinterpret_cast<typename Vec<T>::v4 *>(p) = r;
+    if constexpr (STREAM) __builtin_nontemporal_store(r, reinterpret_cast<typename Vec<T>::v4 *>(p));
+    else *reinterpret_cast<typename Vec<T>::v4 *>(p) = r;
   } else {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
@@ -56,10 +57,12 @@ template <class T> __device__ __forceinline__ void store4(T *p, int valid, const
   }
 }
 
-template <class T, int C> __device__ __forceinline__ void load_n(const T *p, int valid, float v[C]) {
+template <class T, int C, bool STREAM = false> __device__ __forceinline__ void load_n(const T *p, int valid, float v[C]) {
   if constexpr (C == 8 && sizeof(T) == 2) {
     if (valid >= 8) {
-      const typename Vec<T>::v16b r = *reinterpret_cast<const typename Vec<T>::v16b *>(p);
+      typename Vec<T>::v16b r;
+      if constexpr (STREAM) r = __builtin_nontemporal_load(reinterpret_cast<const typename Vec<T>::v16b *>(p));
+      else r = *reinterpret_cast<const typename Vec<T>::v16b *>(p);
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] = to_f32(__builtin_bit_cast(T, (unsigned short)r[i]));
       return;
@@ -68,18 +71,19 @@ template <class T, int C> __device__ __forceinline__ void load_n(const T *p, int
 #pragma unroll
   for (int i = 0; i < C; i += 4) load4(p + i, valid - i, v + i);
 }
-template <class T, int C> __device__ __forceinline__ void store_n(T *p, int valid, const float v[C]) {
+template <class T, int C, bool STREAM = false> __device__ __forceinline__ void store_n(T *p, int valid, const float v[C]) {
   if constexpr (C == 8 && sizeof(T) == 2) {
     if (valid >= 8) {
       typename Vec<T>::v16b r;
 #pragma unroll
       for (int i = 0; i < 8; ++i) r[i] = __builtin_bit_cast(unsigned short, from_f32<T>(v[i]));
-      *reinterpret_cast<typename Vec<T>::v16b *>(p) = r;
+      if constexpr (STREAM) __builtin_nontemporal_store(r, reinterpret_cast<typename Vec<T>::v16b *>(p));
+      else *reinterpret_cast<typename Vec<T>::v16b *>(p) = r;
       return;
     }
   }
 #pragma unroll
-  for (int i = 0; i < C; i += 4) store4(p + i, valid - i, v + i);
+  for (int i = 0; i < C; i += 4) store4<T, STREAM>(p + i, valid - i, v + i);
 }
 
 // ---- activations ---------------------------------------------------------------------------------
@@ -302,13 +306,17 @@ template <class O> __device__ __forceinline__ void clear_rest(const TTGemm &g, i
       store4((O *)g.out + (r < above ? r : r - above + covered) * g.ldo + c, end - c < 4 ? end - c : 4, zero);
 }
 
-// out[m][n .. n + C - 1] from C = 4 or 8 sums, of which `valid` columns exist
-template <class T, class O, int C>
-__device__ __forceinline__ void finish(const TTGemm &g, int z, int m, int n, int valid, float v[C]) {
+// out[m][n .. n + C - 1] from C = 4 or 8 sums, of which `valid` columns exist.  `bias` and `res`: these columns' values where the caller
+// has them already (null: they are read here).
+template <class T, class O, int C, bool STREAM = false>
+__device__ __forceinline__ void finish(const TTGemm &g, int z, int m, int n, int valid, float v[C], const float *bias = nullptr, const float *res = nullptr) {
   float t[C];
 #pragma unroll
   for (int i = 0; i < C; ++i) v[i] *= g.alpha;
-  if (g.bias) {
+  if (bias) {
+#pragma unroll
+    for (int i = 0; i < C; ++i) v[i] += bias[i];
+  } else if (g.bias) {
     load_n<T, C>((const T *)g.bias + z * g.bias_step + n, valid, t);
 #pragma unroll
     for (int i = 0; i < C; ++i) v[i] += t[i];
@@ -316,15 +324,18 @@ __device__ __forceinline__ void finish(const TTGemm &g, int z, int m, int n, int
   if (g.pre) {
 #pragma unroll
     for (int i = 0; i < C; ++i) t[i] = keep_sign<O>(v[i]);
-    store_n<O, C>((O *)g.pre + z * g.p_step + (long long)m * g.ldp + n, valid, t);
+    store_n<O, C, STREAM>((O *)g.pre + z * g.p_step + (long long)m * g.ldp + n, valid, t);
   }
   act_of<O, C>(v, g.act);
-  if (g.res) {
+  if (res) {
+#pragma unroll
+    for (int i = 0; i < C; ++i) v[i] = fmaf(g.beta, res[i], v[i]);
+  } else if (g.res) {
     load_n<T, C>((const T *)g.res + z * g.r_step + (long long)m * g.ldr + n, valid, t);
 #pragma unroll
     for (int i = 0; i < C; ++i) v[i] = fmaf(g.beta, t[i], v[i]);
   }
-  store_n<O, C>((O *)g.out + z * g.o_step + (long long)m * g.ldo + n, valid, v);
+  store_n<O, C, STREAM>((O *)g.out + z * g.o_step + (long long)m * g.ldo + n, valid, v);
 }
 
 // The results of a wavefront, 16 FX x 16 FY of out from row m0 and column n0, rows below `end`.  The instruction leaves a lane
@@ -345,11 +356,30 @@ __device__ __forceinline__ TTGemm as_piece(const TTGemm &g, float *piece) {
   return p;
 }
 template <int FY, int XB> constexpr int finish_floats() { return 16 * XB * (16 * FY + 4); }
-template <class T, class O, int FX, int FY, int XB>
+// STREAM (16-bit tiles of 256): results are written and the residual is read past the caches, which keep the operands instead (16384 x 4096
+// x 4096 bf16 without residual 543 -> 423 us), and the residual is read four rows ahead: one at a time, its latency had each tile's end
+// take as long as a quarter of its product.
+template <class T, class O, int FX, int FY, int XB, bool STREAM>
 __device__ __forceinline__ void finish_tile(const TTGemm &g, int z, int m0, int end, int n0, const f32x4 (&acc)[FX][FY], float *lds, bool mirror = false) {
   constexpr int LD = 16 * FY + 4, PER = 2 * FY, ROWS = 64 / PER;  // lanes of a row, rows at a time
   const int lane = threadIdx.x & 63, q = lane >> 4, j = lane & 15, c = 8 * (lane % PER), r = lane / PER;
   const int valid = g.N - n0 - c;
+  float bias[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  if (g.bias && valid > 0) load_n<T, 8>((const T *)g.bias + z * g.bias_step + n0 + c, valid, bias);
+  constexpr int AHEAD = 4;
+  typename Vec<T>::v16b ahead[AHEAD];
+  auto residual = [&](int row) {
+    typename Vec<T>::v16b v = {};
+    if (row < 16 * FX && m0 + row < end && valid >= 8)
+      v = __builtin_nontemporal_load(reinterpret_cast<const typename Vec<T>::v16b *>((const T *)g.res + z * g.r_step + (long long)(m0 + row) * g.ldr + n0 + c));
+    return v;
+  };
+  if constexpr (STREAM) {
+    if (g.res) {
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i) ahead[i] = residual(r + i * ROWS);
+    }
+  }
 #pragma unroll
   for (int x0 = 0; x0 < FX; x0 += XB) {
 #pragma unroll
@@ -357,12 +387,38 @@ __device__ __forceinline__ void finish_tile(const TTGemm &g, int z, int m0, int 
 #pragma unroll
       for (int y = 0; y < FY; ++y) *reinterpret_cast<f32x4 *>(lds + (16 * x + j) * LD + 16 * y + 4 * q) = acc[x0 + x][y];
     tt_wave_lds_order();
-#pragma unroll 1
-    for (int row = r; row < 16 * XB; row += ROWS) {
-      const int m = m0 + 16 * x0 + row;
+    auto sums = [&](int row, float v[8]) {
       const f32x4 a = *reinterpret_cast<const f32x4 *>(lds + row * LD + c), b = *reinterpret_cast<const f32x4 *>(lds + row * LD + c + 4);
-      float v[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
-      if (m < end && valid > 0) finish<T, O, 8>(g, z, m, n0 + c, valid, v);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        v[i] = a[i];
+        v[4 + i] = b[i];
+      }
+    };
+    if (STREAM && g.res) {
+      if constexpr (STREAM) {
+#pragma unroll 1
+        for (int row = r; row < 16 * XB; row += ROWS) {
+          const int m = m0 + 16 * x0 + row;
+          float v[8], res[8];
+          sums(row, v);
+#pragma unroll
+          for (int i = 0; i < 8; ++i) res[i] = to_f32(__builtin_bit_cast(T, (unsigned short)ahead[0][i]));
+#pragma unroll
+          for (int i = 0; i + 1 < AHEAD; ++i) ahead[i] = ahead[i + 1];
+          ahead[AHEAD - 1] = residual(16 * x0 + row + AHEAD * ROWS);
+          if (m < end && valid >= 8) finish<T, O, 8, true>(g, z, m, n0 + c, 8, v, bias, res);
+          else if (m < end && valid > 0) finish<T, O, 8, true>(g, z, m, n0 + c, valid, v, bias);
+        }
+      }
+    } else {
+#pragma unroll 1
+      for (int row = r; row < 16 * XB; row += ROWS) {
+        const int m = m0 + 16 * x0 + row;
+        float v[8];
+        sums(row, v);
+        if (m < end && valid > 0) finish<T, O, 8, STREAM>(g, z, m, n0 + c, valid, v, bias);
+      }
     }
     if (mirror) {  // the same results as rows n of columns m (only products without a bias)
 #pragma unroll 1

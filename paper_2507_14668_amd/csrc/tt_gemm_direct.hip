@@ -13,10 +13,10 @@ using namespace ttg;
 // by which 16 bytes each lane fetches.  Needs 16-byte aligned rows and a K (K-contiguous) or a number of rows (row-contiguous) that is
 // a multiple of 8: pieces of 16 bytes are whole or outside.  Rows outside are read from a row inside (their results are not stored),
 // values of K outside from a piece of zeros.
-// Measured in bf16: 16384 x 4096 x 4096 527 us (1044 TFLOP/s; x W, both from rows 577, dz^T x 530), 8192^3 875 us (1257); the library's product
-// without an epilogue 353 and 757.  Without its last part the first takes 412 us: a tile's results are written while nothing multiplies
+// Measured in bf16: 16384 x 4096 x 4096 426 us (1290 TFLOP/s; x W, both from rows 446, dz^T x 464), 8192^3 815 us (1350); the library's product
+// without an epilogue 353 and 757.  With bias, gelu and residual the first takes 490: a tile's results are finished while nothing multiplies
 // (one workgroup fills the LDS), and that is what bounds it now.  Tried and no faster: steps of 32 through four buffers (half lines of 128
-// bytes for K-contiguous operands, 590), touching lines of later steps so that they are in the L2 (517 / 654 / 655).
+// bytes for K-contiguous operands), touching lines of later steps so that they are in the L2.
 constexpr int E = 256, BK = 64, THREADS = 512, OPERAND = E * BK;  // halves of an operand in a buffer
 constexpr int STAGES = 2, PIECES = 4;                             // loads of a thread for an operand and step
 __device__ __align__(16) unsigned short g_zeros[8];
@@ -201,11 +201,11 @@ template <class T, bool AKC, bool BKC> __global__ void __launch_bounds__(THREADS
   float *room = reinterpret_cast<float *>(lds) + wave * finish_floats<4, 4>();
   if constexpr (!AKC) {  // (only sums over stored rows are cut)
     if (piece) {
-      finish_tile<T, float, 8, 4, 4>(as_piece(g, piece), 0, w.lo + wm, w.hi, w.n0 + wn, acc, room);
+      finish_tile<T, float, 8, 4, 4, false>(as_piece(g, piece), 0, w.lo + wm, w.hi, w.n0 + wn, acc, room);
       return;
     }
   }
-  finish_tile<T, T, 8, 4, 4>(g, w.z, w.lo + wm, w.hi, w.n0 + wn, acc, room);
+  finish_tile<T, T, 8, 4, 4, true>(g, w.z, w.lo + wm, w.hi, w.n0 + wn, acc, room);
 }
 
 template <class T> tt_status launch(const TTGemm &g, void *partial, hipStream_t s) {
@@ -229,9 +229,12 @@ template <class T> tt_status launch(const TTGemm &g, void *partial, hipStream_t 
 
 // Tiles of 256 from which they are taken: a workgroup fills a compute unit, and fewer leave too many without.  bf16, these / tiles of 128
 // and 64, us: 2048 x 2048 x 2048 (64 tiles) 52 / 46, 2048 x 4096 x 1024 (128) 33 / 32, 4096 x 2560 x 1024 (160) 35 / 52, 4096 x 4096 x 1024
-// (256) 37 / 61; 64 weights of 1024 x 1024 over 32768 uneven rows 157 / 204.
+// (256) 37 / 61; 64 weights of 1024 x 1024 over 32768 uneven rows 146 / 204.
 #ifndef TT_GEMM_DIRECT_TILES
 #define TT_GEMM_DIRECT_TILES 144
+#endif
+#ifndef TT_GEMM_DIRECT_LEAST
+#define TT_GEMM_DIRECT_LEAST 128  // of a side of out
 #endif
 bool ttk_gemm_direct_serves(const TTGemm &g) {
   if (g.dtype == TT_F32 || g.out_dtype != g.dtype || g.symmetric) return false;
@@ -239,7 +242,8 @@ bool ttk_gemm_direct_serves(const TTGemm &g) {
   if ((addresses & 15) || ((g.lda | g.ldb | g.a_step | g.b_step) & 7)) return false;
   if (((g.a_kc || g.b_kc) && (g.K & 7)) || (!g.a_kc && (g.M & 7)) || (!g.b_kc && (g.N & 7))) return false;
   if (g.lda > (1 << 23) || g.ldb > (1 << 23)) return false;  // offsets within a tile are 32 bits
-  if ((g.mode != TT_GEMM_RAGGED_M && g.M <= 128) || (g.like_N ? g.like_N : g.N) <= 128) return false;  // half a tile would be empty
+  // half a tile would be empty
+  if ((g.mode != TT_GEMM_RAGGED_M && g.M <= TT_GEMM_DIRECT_LEAST) || (g.like_N ? g.like_N : g.N) <= TT_GEMM_DIRECT_LEAST) return false;
   const long long tiles = (long long)tt_ceil_div(g.M, E) * tt_ceil_div(g.like_N ? g.like_N : g.N, E) * (g.mode == TT_GEMM_RAGGED_M ? 1 : g.batch);
   return tiles >= TT_GEMM_DIRECT_TILES;
 }

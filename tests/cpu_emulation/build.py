@@ -5,6 +5,7 @@ nothing in the product path loads what is built here.
 
   build_shared(out_dir)            -> libtt_emb_emu.so, driven through ctypes by the CPU tests
   build_harness(out_dir, sanitize) -> harness executable under "address" (+UBSan), "memory" or "thread"
+  build_dense(out_dir, tag)        -> library of the dense operators' units (matrix products, orthogonalised updates)
   build_unit(out_dir, name)        -> executable of one unit test over tt_internal.h
 
 Two textual changes are made to the copies that are compiled: `extern __shared__ float x[];`
@@ -25,18 +26,19 @@ ROOT = os.path.dirname(os.path.dirname(HERE))
 CSRC = os.path.join(ROOT, "paper_2507_14668_amd", "csrc")
 CLANG = os.environ.get("TT_EMU_CXX", "/opt/rocm/llvm/bin/clang++")
 UNITS = ("tt_api", "tt_reorder", "tt_forward", "tt_forward_mfma", "tt_forward_sample", "tt_bf16", "tt_index_graph", "tt_fuse", "tt_backward",
-         "tt_backward_mfma", "tt_gemm", "tt_gemm_direct", "tt_gemm_rows", "tt_dense", "tt_ortho", "tt_ortho_slice")
+         "tt_backward_mfma")
+DENSE_UNITS = ("tt_gemm", "tt_gemm_direct", "tt_gemm_rows", "tt_dense", "tt_ortho", "tt_ortho_slice")
 
 
 def available() -> bool:
     return os.path.exists(CLANG)
 
 
-def _generate(gen: str) -> list:
+def _generate(gen: str, units=UNITS) -> list:
     shutil.rmtree(gen, ignore_errors=True)
     os.makedirs(gen)
     out = []
-    for u in UNITS:
+    for u in units:
         text = open(os.path.join(CSRC, u + ".hip")).read()
         text = re.sub(r"extern __shared__ (?:__align__\(16\) )?float (\w+)\[\];", r"float *\1 = (float *)emu::dyn_lds();", text)
         text = text.replace("kBatchedCallsEnabled = false", "kBatchedCallsEnabled = true")
@@ -47,7 +49,8 @@ def _generate(gen: str) -> list:
         path = os.path.join(gen, u + ".cpp")
         open(path, "w").write(text)
         out.append(path)
-    for header in ("tt_internal.h", "tt_gemm.h", "tt_gemm_device.h", "tt_ortho_slice.h"):
+    headers = ("tt_internal.h",) if units == UNITS else ("tt_internal.h", "tt_gemm.h", "tt_gemm_device.h", "tt_ortho_slice.h")
+    for header in headers:
         shutil.copy(os.path.join(CSRC, header), gen)
     return out
 
@@ -74,6 +77,37 @@ def build_shared(out_dir: str, tag: str = "so", defines=()) -> str:
     objs, base = _compile(srcs, ["-O2", "-fPIC"] + list(defines), out_dir, tag)
     lib = os.path.join(out_dir, "libtt_emb_emu%s.so" % ("" if tag == "so" else "_" + tag))
     subprocess.run(base + ["-O2", "-fPIC", "-shared"] + objs + ["-o", lib], check=True)
+    return lib
+
+
+_dense_objects = {}  # (unit, its defines): object of this process's build
+
+
+def build_dense(out_dir: str, tag: str, defines=None) -> str:
+    """The dense operators' units as a library of their own; `defines` gives units flags ("-DNAME=value") of their own.  An
+    object is compiled once for every set of flags."""
+    os.makedirs(out_dir, exist_ok=True)
+    gen = os.path.join(out_dir, "gen_dense")
+    if not _dense_objects:
+        _generate(gen, DENSE_UNITS)
+    base = [CLANG, "-std=c++17", "-O1", "-fPIC", "-D__HIPCC__", "-I" + HERE, "-I" + gen, "-I" + os.path.join(ROOT, "include"), "-pthread",
+            "-Wno-unused-value"]
+
+    def one(unit):
+        flags = tuple((defines or {}).get(unit, ()))
+        if (unit, flags) not in _dense_objects:
+            src = os.path.join(HERE if unit == "emu_runtime" else gen, unit + ".cpp")
+            obj = os.path.join(gen, "%s_%d.o" % (unit, sum(1 for u, _ in list(_dense_objects) if u == unit)))
+            res = subprocess.run(base + list(flags) + ["-c", src, "-o", obj], capture_output=True, text=True)
+            if res.returncode != 0:
+                raise RuntimeError("compiling %s failed:\n%s" % (src, res.stderr[-4000:]))
+            _dense_objects[unit, flags] = obj
+        return _dense_objects[unit, flags]
+
+    with ThreadPoolExecutor(max_workers=8) as pool:
+        objs = list(pool.map(one, DENSE_UNITS + ("emu_runtime",)))
+    lib = os.path.join(out_dir, "libtt_dense_emu_%s.so" % tag)
+    subprocess.run(base + ["-shared"] + objs + ["-o", lib], check=True)
     return lib
 
 

@@ -18,15 +18,15 @@ DT = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 GUARD = 512
 
 
-TILES = "-DTT_GEMM_FEW_ROWS=0"
-VARIANTS = {"as it is": ("dense", []), "small tiles": ("dense_small", [TILES]), "large tiles": ("dense_large", [TILES, "-DTT_GEMM_LARGE_TILES=1"]),
-            "direct tiles": ("dense_direct", [TILES, "-DTT_GEMM_DIRECT_TILES=1"])}
+NO_ROWS = {"tt_gemm_rows": ["-DTT_GEMM_FEW_ROWS=0"]}
+VARIANTS = {"as it is": ("as_it_is", {}), "small tiles": ("small", NO_ROWS), "large tiles": ("large", dict(NO_ROWS, tt_gemm=["-DTT_GEMM_LARGE_TILES=1"])),
+            "direct tiles": ("direct", dict(NO_ROWS, tt_gemm_direct=["-DTT_GEMM_DIRECT_TILES=1", "-DTT_GEMM_DIRECT_LEAST=0"]))}
 
 
 @pytest.fixture(scope="module", params=VARIANTS)
 def lib(request):
     """The library as it is (few rows mostly), without the kernel for few rows, and with the larger tiles from the first one on."""
-    lib = ctypes.CDLL(emu_build.build_shared(BUILD_DIR, *VARIANTS[request.param]))
+    lib = ctypes.CDLL(emu_build.build_dense(BUILD_DIR, *VARIANTS[request.param]))
     vp, sz, f32 = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_float
     lib.tt_dense_workspace_bytes.restype = lib.tt_orthogonalize_workspace_bytes.restype = lib.tt_core_ortho_workspace_bytes.restype = sz
     lib.tt_dense_workspace_bytes.argtypes = [vp, ctypes.c_int]

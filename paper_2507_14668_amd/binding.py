@@ -624,11 +624,11 @@ class _On:
         return False
 
     def empty(self, shape, dtype):
-        """Memory for this call: freed early or late, it is not handed out again before the call's stream is done with it."""
-        t = torch.empty(shape, dtype=dtype, device=self.index)
-        if self.stream is not None:
-            t.record_stream(self.stream)
-        return t
+        """Memory of the call's stream: what was freed there is reused in its order."""
+        if self.stream is None:
+            return torch.empty(shape, dtype=dtype, device=self.index)
+        with torch.cuda.stream(self.stream):
+            return torch.empty(shape, dtype=dtype, device=self.index)
 
 
 def _index(t, name, dtype, at):

@@ -67,6 +67,9 @@ SIZES = [
     (8200, 2056, 520, None, 8, 0),
     (6000, 96, 700, (2500, 0, 1, 3499), 0, 0),
     (5000, 328, 1030, (130, 2700, 5, 2100), 6, 0),
+    (4100, 136, 2600, None, 8, 0),    # the largest tiles: forward, gradient of x, gradient of w
+    (4100, 2600, 200, None, 8, 0),
+    (300, 4096, 2568, None, 0, 0),
     (12000, 1024, 1024, (9300, 0, 3, 257, 1000, 64, 700, 128, 300, 1, 100, 147), 0, 0),
     (9000, 64, 40, (8000, 10, 990), 0, 0),
     (9000, 33, 47, (10, 8000, 0, 990), 1, 1),
@@ -609,3 +612,66 @@ def test_rows_past_32_bits(tt):
     off = torch.tensor([0, rows - 3, rows], device="cuda")
     g2 = tt.tt_dense_forward(x, torch.stack([w, -w]), offsets=off)
     assert torch.equal(g2[-5:-3], out[-5:-3]) and torch.equal(g2[-3:], -out[-3:])
+
+
+def test_autograd_in_a_graph(tt):
+    """A training pass through autograd, captured and replayed over new inputs with eager passes between."""
+    x, w, bias, res, grad = make(500, 64, 96, torch.bfloat16, 2)
+    off = torch.tensor([0, 200, 500], device="cuda")
+    leaves = [t.detach().clone().requires_grad_(True) for t in (x, w, bias, res)]
+
+    def step():
+        out = tt.tt_dense(*leaves, "gelu", offsets=off)
+        return (out.detach(),) + torch.autograd.grad(out, leaves, grad)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = step()
+    for i in range(3):
+        with torch.no_grad():
+            leaves[0].copy_(torch.randn(500, 64, generator=torch.Generator(device="cuda").manual_seed(i), device="cuda"))
+        want = [t.clone() for t in step()]
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(held, want)), i
+
+
+def test_update_in_a_graph(tt):
+    n, d, r = (5, 40, 6), (4, 8, 4), (1, 64, 64, 1)
+    gen = torch.Generator(device="cuda").manual_seed(0)
+    mk = lambda std: [torch.randn(r[k] * n[k] * d[k] * r[k + 1], generator=gen, device="cuda") * std for k in range(3)]
+    cores, grads, momenta = mk(0.05), mk(1e-3), mk(1e-2)
+    copies = [[t.clone() for t in ts] for ts in (cores, momenta)]
+    table, other = tt.Table(n[0] * n[1] * n[2], n, d, r, cores), tt.Table(n[0] * n[1] * n[2], n, d, r, copies[0])
+    tt.tt_core_ortho_update(table, grads, momenta, 0.0, momentum=1.0, nesterov=False)  # (before the capture)
+    for t, c in zip(momenta, copies[1]):
+        t.copy_(c)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        tt.tt_core_ortho_update(table, grads, momenta, 0.01)
+    for i in range(3):
+        for g in grads:
+            g.mul_(-0.7)
+        tt.tt_core_ortho_update(other, grads, copies[1], 0.01)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(table.cores + momenta, other.cores + copies[1])), i
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=str)
+def test_thin_sides(tt, dtype):
+    """One column in or out, one row of very many columns."""
+    for rows, k, n in ((3000, 1, 5), (3000, 5, 1), (1, 1, 70000), (1, 70000, 1), (70, 3, 300), (2000, 300, 3)):
+        x, w, bias, res, grad = make(rows, k, n, dtype)
+        want, tol, z, _ = ref.forward64(*cpu(x, w, bias, res), "silu")
+        ref.check(tt.tt_dense_forward(x, w, bias, res, "silu").cpu(), want, tol, "out")
+        pre = z.to(dtype)
+        wants, tols = ref.backward64(*cpu(x, w, grad), pre, "silu")
+        for got, want, tol, name in zip(tt.tt_dense_backward(x, w, grad, pre.cuda(), "silu"), wants, tols, ("dx", "dw", "dbias")):
+            ref.check(got.cpu(), want, tol, (name, rows, k, n))

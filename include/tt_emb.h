@@ -418,7 +418,8 @@ tt_status tt_index_graph_edges(const int64_t *indices, const int64_t *offsets, i
 typedef enum { TT_F32 = 0, TT_BF16 = 1, TT_F16 = 2 } tt_dtype;
 typedef enum {
   TT_ACT_NONE = 0,
-  TT_ACT_RELU = 1,   /* z <= 0 ? 0 : z, slope 0 at 0                                            */
+  TT_ACT_RELU = 1,   /* z <= 0 ? 0 : z, slope 0 at 0; a z of fp32 tensors that rounding could take to
+                        the other side of 0 is formed in 64 bits                                */
   TT_ACT_GELU = 2,   /* z Phi(z), with the normal distribution's Phi                            */
   TT_ACT_SILU = 3,   /* z / (1 + exp(-z))                                                       */
   TT_ACT_SIGMOID = 4 /* 1 / (1 + exp(-z))                                                       */

@@ -218,6 +218,8 @@ __global__ void __launch_bounds__(TT_BLOCK, 2) k_gemm(TTGemm g, int m_tiles, int
                 FINISH = 8 * finish_floats<F, 2>();
   __shared__ __align__(16) unsigned short lds[HALVES > REDO ? (HALVES > FINISH ? HALVES : FINISH) : (REDO > FINISH ? REDO : FINISH)];
   __shared__ int flags[4];
+  constexpr bool SETTLES = P == 3 && AKC && BKC;
+  __shared__ float sizes[SETTLES ? E : 1], largest[SETTLES ? E : 1];  // sums of |A|'s rows, the largest of |B|'s
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int members = (int)gridDim.y / split, cut = (int)blockIdx.y / members;  // which piece of K
   unsigned mt, nt;
@@ -241,11 +243,11 @@ __global__ void __launch_bounds__(TT_BLOCK, 2) k_gemm(TTGemm g, int m_tiles, int
       int pieces = 1, number = 0;
       find_slot(g.offsets, g.batch, g.K, chunk, BK, (int)blockIdx.y, w.z, w.k_lo, w.k_hi, pieces, number);
       if (w.z < 0) return;
-      if (pieces > 1) piece = partial + number * piece_floats(g);
+      if (pieces > 1) piece = partial + number * ttk_gemm_piece_floats(g);
     }
   }
   if (split > 1) {  // whole steps to each piece
-    piece = partial + ((long long)cut * g.batch + w.z) * piece_floats(g);
+    piece = partial + ((long long)cut * g.batch + w.z) * ttk_gemm_piece_floats(g);
     const int steps = (w.k_hi - w.k_lo + BK - 1) / BK, per = (steps + split - 1) / split;
     const long long a = (long long)w.k_lo + (long long)cut * per * BK, b = a + (long long)per * BK;
     if (a < w.k_hi) w.k_lo = (int)a;
@@ -263,6 +265,22 @@ __global__ void __launch_bounds__(TT_BLOCK, 2) k_gemm(TTGemm g, int m_tiles, int
   const int wm = (wave >> 1) * (E / 2), wn = (wave & 1) * (E / 2);
   f32x4 acc[F][F] = {}, rs[F] = {};  // [m][n]; sums of A's rows
   const bool sums = g.rowsum && w.n0 == 0;
+  const bool settles = SETTLES && ttk_gemm_settles(g);
+  float size[CA::N] = {}, most[CB::N] = {};  // of the rows that the thread carries (its units are of one row each, all along K)
+  auto measure = [&]() {
+    if constexpr (SETTLES) {
+      if (settles) {
+#pragma unroll
+        for (int i = 0; i < CA::N; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) size[i] += fabsf(ua[i].a[e]) + fabsf(ua[i].b[e]);
+#pragma unroll
+        for (int i = 0; i < CB::N; ++i)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) most[i] = fmaxf(most[i], fmaxf(fabsf(ub[i].a[e]), fabsf(ub[i].b[e])));
+      }
+    }
+  };
   // the smallest number that is not zero, as twice its bits less one
   auto note = [&](const Unit<T> *u, int n, unsigned &small) {
     if constexpr (P == 3) {
@@ -327,6 +345,7 @@ __global__ void __launch_bounds__(TT_BLOCK, 2) k_gemm(TTGemm g, int m_tiles, int
     int buf = 0;
     for (int k0 = w.k_lo; k0 < K; k0 += BK) {
       const bool more = k0 + BK < K;
+      measure();
       __syncthreads();  // two buffers: this step's tiles are whole, and nobody reads the other buffer any more
       if constexpr (BUF == 1) {
         ca.template store<P>(ua, plane_a(0, 0));
@@ -442,6 +461,29 @@ __global__ void __launch_bounds__(TT_BLOCK, 2) k_gemm(TTGemm g, int m_tiles, int
       }
     }
   }
+  if constexpr (SETTLES) {
+    if (settles) {
+      constexpr int PER = BK / 8;  // lanes of a row
+#pragma unroll
+      for (int i = 0; i < CA::N; ++i) {
+#pragma unroll
+        for (int o = 1; o < PER; o *= 2) {
+          size[i] += __shfl(size[i], lane ^ o, 64);
+          most[i] = fmaxf(most[i], __shfl(most[i], lane ^ o, 64));
+        }
+        const int r = ((int)threadIdx.x + i * TT_BLOCK) / PER;
+        if (lane % PER == 0) {
+          sizes[r] = size[i];
+          largest[r] = most[i];
+          if (piece) {
+            float *rows = piece + (long long)g.M * (g.N + 1LL);
+            if (w.n0 == 0 && w.lo + r < w.hi) rows[w.lo + r] = size[i];
+            if (w.lo == 0 && w.n0 + r < g.N) rows[g.M + w.n0 + r] = most[i];
+          }
+        }
+      }
+    }
+  }
   const int q = lane >> 4, j = lane & 15;
   if (sums && wn == 0 && q == 0) {
 #pragma unroll
@@ -456,23 +498,26 @@ __global__ void __launch_bounds__(TT_BLOCK, 2) k_gemm(TTGemm g, int m_tiles, int
   float *room = reinterpret_cast<float *>(lds) + wave * finish_floats<F, 2>();
   const bool mirror = g.symmetric && mt != nt;
   if (piece) finish_tile<T, float, F, F, 2, false>(as_piece(g, piece), 0, w.lo + wm, w.hi, w.n0 + wn, acc, room, mirror);
-  else finish_tile<T, O, F, F, 2, false>(g, w.z, w.lo + wm, w.hi, w.n0 + wn, acc, room, mirror);
+  else finish_tile<T, O, F, F, 2, false>(g, w.z, w.lo + wm, w.hi, w.n0 + wn, acc, room, mirror, settles ? sizes + wm : nullptr,
+                                                  settles ? largest + wn : nullptr);
 }
 
 // The pieces of a cut product, added in order; four columns of a row per thread.
 template <class T, class O> __device__ __forceinline__ void join_pieces(const TTGemm &g, int z, int pieces, const float *p, long long step) {
   const int per = (g.N + 3) / 4;
   const long long total = (long long)g.M * per;
-  for (long long e = (long long)blockIdx.x * TT_BLOCK + threadIdx.x; e < total + g.M; e += (long long)gridDim.x * TT_BLOCK) {
-    if (e >= total) {
-      if (!g.rowsum) continue;
+  const int lane = threadIdx.x & 63;
+  for (long long e0 = (long long)blockIdx.x * TT_BLOCK + (threadIdx.x - lane); e0 < total + g.M; e0 += (long long)gridDim.x * TT_BLOCK) {
+    const long long e = e0 + lane;  // (whole wavefronts, for settle_signs)
+    if (e >= total && e < total + g.M && g.rowsum) {
       const long long m = e - total;
       float s = 0.f;
       for (int i = 0; i < pieces; ++i) s += p[i * step + (long long)g.M * g.N + m];
       ((O *)g.rowsum)[z * g.rs_step + m] = from_f32<O>(s);
-      continue;
     }
-    const int m = (int)(e / per), n = (int)(e - (long long)m * per) * 4, valid = g.N - n < 4 ? g.N - n : 4;
+    if (e0 >= total) continue;
+    const int m = e < total ? (int)(e / per) : 0, n = e < total ? (int)(e - (long long)m * per) * 4 : 0;
+    const int valid = e >= total ? 0 : g.N - n < 4 ? g.N - n : 4;
     f32x4 s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
     for (int i = 0; i < pieces; ++i) {
@@ -482,17 +527,34 @@ template <class T, class O> __device__ __forceinline__ void join_pieces(const TT
       for (int c = 0; c < 4; ++c) s[c] += t[c];
     }
     float v[4] = {s[0], s[1], s[2], s[3]};
-    finish<T, O, 4>(g, z, m, n, valid, v);
+    if constexpr (std::is_same<T, float>::value && std::is_same<O, float>::value) {
+      if (ttk_gemm_settles(g)) {
+        const float none[4] = {0.f, 0.f, 0.f, 0.f};  // (bias is in v)
+        float size = 0.f, most[4] = {0.f, 0.f, 0.f, 0.f};
+        for (int i = 0; i < pieces; ++i) {
+          const float *rows = p + i * step + (long long)g.M * (g.N + 1LL);
+          float t[4];
+          size += rows[m];
+          load4(rows + g.M + n, valid, t);
+#pragma unroll
+          for (int c = 0; c < 4; ++c) most[c] = fmaxf(most[c], t[c]);
+        }
+        settle_signs<4>(g, z, m, n, valid, v, size, most);
+        if (valid > 0) finish<T, O, 4>(g, z, m, n, valid, v, none);
+        continue;
+      }
+    }
+    if (valid > 0) finish<T, O, 4>(g, z, m, n, valid, v);
   }
 }
 template <class T, class O> __global__ void __launch_bounds__(TT_BLOCK) k_join(TTGemm g, int split, const float *__restrict__ partial) {
   const int z = (int)blockIdx.y;
-  join_pieces<T, O>(g, z, split, partial + z * piece_floats(g), g.batch * piece_floats(g));
+  join_pieces<T, O>(g, z, split, partial + z * ttk_gemm_piece_floats(g), g.batch * ttk_gemm_piece_floats(g));
 }
 template <class T> __global__ void __launch_bounds__(TT_BLOCK) k_join_groups(TTGemm g, int chunk, int bk, const float *__restrict__ partial) {
   int z = (int)blockIdx.y, lo = 0, hi = 0, pieces = 1, first = 0;
   find_slot(g.offsets, g.batch, g.K, chunk, bk, -1, z, lo, hi, pieces, first);
-  if (z >= 0) join_pieces<T, T>(g, z, pieces, partial + first * piece_floats(g), piece_floats(g));
+  if (z >= 0) join_pieces<T, T>(g, z, pieces, partial + first * ttk_gemm_piece_floats(g), ttk_gemm_piece_floats(g));
 }
 
 // ---- host ------------------------------------------------------------------------------------------
@@ -590,7 +652,7 @@ int ttk_gemm_chunk(const TTGemm &g, int e, int bk, int least) {
 size_t ttk_gemm_chunk_bytes(const TTGemm &g, int chunk) {
   // groups of several pieces have fewer than 2 rows / chunk each, the rest none
   const long long slots = 2 * ((long long)g.K / chunk);
-  return ((size_t)slots * g.M * (g.N + 1LL) * 4 + 255) & ~(size_t)255;
+  return ((size_t)slots * ttk_gemm_piece_floats(g) * 4 + 255) & ~(size_t)255;
 }
 tt_status ttk_gemm_join_groups(const TTGemm &g, int chunk, int bk, const float *partial, hipStream_t s) {
   const int most = g.K / chunk < g.batch ? g.K / chunk : g.batch;  // groups that can have two pieces
@@ -609,7 +671,7 @@ size_t ttk_gemm_partial_bytes(const TTGemm &g) {
     const size_t a = ttk_gemm_chunk_bytes(g, h.chunk), b = ttk_gemm_direct_bytes(g);
     return a > b ? a : b;
   }
-  return h.split < 2 ? 0 : (((size_t)h.split * g.batch * g.M * (g.N + 1LL) * 4) + 255) & ~(size_t)255;
+  return h.split < 2 ? 0 : (((size_t)h.split * g.batch * ttk_gemm_piece_floats(g) * 4) + 255) & ~(size_t)255;
 }
 
 tt_status ttk_gemm(const TTGemm &g, void *partial, hipStream_t s) {

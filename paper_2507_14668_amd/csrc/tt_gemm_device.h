@@ -338,12 +338,59 @@ __device__ __forceinline__ void finish(const TTGemm &g, int z, int m, int n, int
   store_n<O, C, STREAM>((O *)g.out + z * g.o_step + (long long)m * g.ldo + n, valid, v);
 }
 
+__device__ __forceinline__ double wave_sum64(double v) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    const long long b = __builtin_bit_cast(long long, v);
+    const int lo = __shfl((int)b, (threadIdx.x & 63) ^ o, 64), hi = __shfl((int)(b >> 32), (threadIdx.x & 63) ^ o, 64);
+    v += __builtin_bit_cast(double, ((long long)hi << 32) | (unsigned)lo);
+  }
+  return v;
+}
+// relu of an fp32 product (K-contiguous operands): v becomes alpha v + bias.  A sum of K products is off by at most
+// 2 (K + 2) 2^-24 sum |terms|, and sum |terms| <= size |b| with `size` the sum of |A|'s row and |b| the largest of |B|'s row: where v is below
+// that (a quarter more, for the sums of absolute values' own rounding), all 64 lanes form it in 64 bits, and so its sign is the exact value's.  One in
+// ten thousand results of a layer as it is initialised; about a microsecond each for a wavefront.  Zero rows have nothing to settle.
+// All lanes of the wavefront call it, with one z; `valid` <= 0: a lane without results.
+template <int C>
+__device__ __forceinline__ void settle_signs(const TTGemm &g, int z, int m, int n, int valid, float v[C], float size, const float largest[C]) {
+  const int lane = threadIdx.x & 63;
+  const float *bias = g.bias ? (const float *)g.bias + z * g.bias_step : nullptr;
+  const float share = 2.5f * 0x1p-24f * (float)(g.K + 2) * size;
+  unsigned near = 0;
+#pragma unroll
+  for (int i = 0; i < C; ++i) {
+    v[i] = g.alpha * v[i] + (bias && i < valid ? bias[n + i] : 0.f);
+    near |= i < valid && fabsf(v[i]) < share * largest[i] ? 1u << i : 0u;
+  }
+  for (unsigned long long lanes = __ballot(near != 0); lanes; lanes = __ballot(near != 0)) {
+    const int l = __ffsll(lanes) - 1, which = __ffs(__shfl((int)near, l, 64)) - 1;
+    const int row = __shfl(m, l, 64), col = __shfl(n, l, 64) + which;
+    const float *a = (const float *)g.a + (g.mode == TT_GEMM_BATCH ? z * g.a_step : 0) + (long long)row * g.lda;
+    const float *b = (const float *)g.b + z * g.b_step + (long long)col * g.ldb;
+    double s = 0;
+    for (int k = 4 * lane; k < g.K; k += 256) {
+      float x[4], y[4];
+      load4(a + k, g.K - k, x);
+      load4(b + k, g.K - k, y);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s += (double)x[i] * y[i];
+    }
+    s = g.alpha * wave_sum64(s) + (bias ? bias[col] : 0.f);
+    const float r = s != 0 && fabs(s) < 0x1p-149 ? (s < 0 ? -0x1p-149f : 0x1p-149f) : (float)s;
+    if (lane == l) {
+      near &= near - 1;
+#pragma unroll
+      for (int i = 0; i < C; ++i) v[i] = i == which ? r : v[i];
+    }
+  }
+}
+
 // The results of a wavefront, 16 FX x 16 FY of out from row m0 and column n0, rows below `end`.  The instruction leaves a lane
 // four columns of a row, 8 bytes of a 16-bit row at a time; through 16 XB rows of LDS (`lds`: finish_floats of the wavefront's own) a lane
 // gets eight, and what is read and written is whole lines of 128 bytes.  The loop over the rows is not unrolled: with all activations in it
 // 16 times, the code is longer than the instruction cache.
-// A product's description with its sums themselves as the result: piece `number` of a cut product, [M][N] and then [M] sums of A's rows.
-__device__ __forceinline__ long long piece_floats(const TTGemm &g) { return (long long)g.M * (g.N + 1LL); }
+// A product's description with its sums themselves as the result: a piece of a cut product.
 __device__ __forceinline__ TTGemm as_piece(const TTGemm &g, float *piece) {
   TTGemm p = g;
   p.out = piece;
@@ -359,8 +406,10 @@ template <int FY, int XB> constexpr int finish_floats() { return 16 * XB * (16 *
 // STREAM (16-bit tiles of 256): results are written and the residual is read past the caches, which keep the operands instead (16384 x 4096
 // x 4096 bf16 without residual 543 -> 423 us), and the residual is read four rows ahead: one at a time, its latency had each tile's end
 // take as long as a quarter of its product.
+// `sizes` and `largest` (LDS, null: nothing is settled): of the wavefront's rows of A and of B, for settle_signs.
 template <class T, class O, int FX, int FY, int XB, bool STREAM>
-__device__ __forceinline__ void finish_tile(const TTGemm &g, int z, int m0, int end, int n0, const f32x4 (&acc)[FX][FY], float *lds, bool mirror = false) {
+__device__ __forceinline__ void finish_tile(const TTGemm &g, int z, int m0, int end, int n0, const f32x4 (&acc)[FX][FY], float *lds, bool mirror = false,
+                                            const float *sizes = nullptr, const float *largest = nullptr) {
   constexpr int LD = 16 * FY + 4, PER = 2 * FY, ROWS = 64 / PER;  // lanes of a row, rows at a time
   const int lane = threadIdx.x & 63, q = lane >> 4, j = lane & 15, c = 8 * (lane % PER), r = lane / PER;
   const int valid = g.N - n0 - c;
@@ -417,6 +466,14 @@ __device__ __forceinline__ void finish_tile(const TTGemm &g, int z, int m0, int 
         const int m = m0 + 16 * x0 + row;
         float v[8];
         sums(row, v);
+        if constexpr (std::is_same<T, float>::value && std::is_same<O, float>::value) {
+          if (sizes) {
+            const float none[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};  // (bias is in v)
+            settle_signs<8>(g, z, m, n0 + c, m < end ? valid : 0, v, sizes[16 * x0 + row], largest + c);
+            if (m < end && valid > 0) finish<T, O, 8, STREAM>(g, z, m, n0 + c, valid, v, none);
+            continue;
+          }
+        }
         if (m < end && valid > 0) finish<T, O, 8, STREAM>(g, z, m, n0 + c, valid, v, bias);
       }
     }

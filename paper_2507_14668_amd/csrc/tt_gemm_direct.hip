@@ -144,7 +144,7 @@ template <class T, bool AKC, bool BKC> __global__ void __launch_bounds__(THREADS
       int pieces = 1, number = 0;
       find_slot(g.offsets, g.batch, g.K, chunk, BK, (int)blockIdx.y, w.z, w.k_lo, w.k_hi, pieces, number);
       if (w.z < 0) return;
-      if (pieces > 1) piece = partial + (long long)__builtin_amdgcn_readfirstlane(number) * piece_floats(g);
+      if (pieces > 1) piece = partial + (long long)__builtin_amdgcn_readfirstlane(number) * ttk_gemm_piece_floats(g);
     }
   }
   w.z = __builtin_amdgcn_readfirstlane(w.z);

@@ -46,6 +46,8 @@ template <class T, int MT> __global__ void __launch_bounds__(THREADS) k_gemm_row
   typedef Chunk<T> C;
   typedef typename Piece<T>::type P;
   __shared__ __align__(16) float sums[WAVES * MT * 256];
+  constexpr bool F32 = sizeof(T) == 4;
+  __shared__ __align__(16) float sizes[F32 ? WAVES * MT * 16 : 4], largest[F32 ? WAVES * 16 : 4];  // for settle_signs: of every wavefront's part of K
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, q = lane >> 4, j = lane & 15;
   const int n0 = (int)(blockIdx.x % (unsigned)n_tiles) * 16, mt = (int)(blockIdx.x / (unsigned)n_tiles);
   int z, lo, hi;
@@ -80,6 +82,8 @@ template <class T, int MT> __global__ void __launch_bounds__(THREADS) k_gemm_row
       for (int x = 0; x < MT; ++x) la[x][i] = load_piece<T>(a[x] + k, left);
     }
   };
+  const bool settles = F32 && ttk_gemm_settles(g);
+  float size[MT] = {}, most = 0.f;  // of the lane's values of rows j
   const int first = wave * C::K;
   if (first < K) load(fb[0], fa[0], first);
   if (first + skip < K) load(fb[1], fa[1], first + skip);
@@ -91,11 +95,38 @@ template <class T, int MT> __global__ void __launch_bounds__(THREADS) k_gemm_row
       for (int i = 0; i < C::LOADS; ++i)
 #pragma unroll
         for (int x = 0; x < MT; ++x) acc[x] = multiply<T>(fb[d][i], fa[d][x][i], acc[x]);  // lane (q, j): row j, columns 4 q + i
+      if constexpr (F32) {
+        if (settles) {
+#pragma unroll
+          for (int i = 0; i < C::LOADS; ++i)
+#pragma unroll
+            for (int e = 0; e < C::E; ++e) {
+              most = fmaxf(most, fabsf(fb[d][i][e]));
+#pragma unroll
+              for (int x = 0; x < MT; ++x) size[x] += fabsf(fa[d][x][i][e]);
+            }
+        }
+      }
       if (k0 + (d + 2) * skip < K) load(fb[d], fa[d], k0 + (d + 2) * skip);
     }
   }
 #pragma unroll
   for (int x = 0; x < MT; ++x) *reinterpret_cast<f32x4 *>(sums + (wave * MT + x) * 256 + lane * 4) = acc[x];
+  if constexpr (F32) {
+    if (settles) {
+#pragma unroll
+      for (int o = 16; o < 64; o *= 2) {
+        most = fmaxf(most, __shfl(most, lane ^ o, 64));
+#pragma unroll
+        for (int x = 0; x < MT; ++x) size[x] += __shfl(size[x], lane ^ o, 64);
+      }
+      if (q == 0) {
+        largest[wave * 16 + j] = most;
+#pragma unroll
+        for (int x = 0; x < MT; ++x) sizes[(wave * MT + x) * 16 + j] = size[x];
+      }
+    }
+  }
   __syncthreads();
   for (int e = threadIdx.x; e < MT * 64; e += THREADS) {
     f32x4 s = {0.f, 0.f, 0.f, 0.f};
@@ -103,6 +134,22 @@ template <class T, int MT> __global__ void __launch_bounds__(THREADS) k_gemm_row
     for (int v = 0; v < WAVES; ++v) s += *reinterpret_cast<const f32x4 *>(sums + v * MT * 256 + e * 4);
     const int m = lo + 16 * (e >> 6) + (e & 15), n = n0 + 4 * ((e >> 4) & 3);
     float v[4] = {s[0], s[1], s[2], s[3]};
+    if constexpr (F32) {
+      if (settles) {  // (a wavefront has a whole turn of this loop or none)
+        const float none[4] = {0.f, 0.f, 0.f, 0.f};  // (bias is in v)
+        float whole = 0.f, top[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+          whole += sizes[(w * MT + (e >> 6)) * 16 + (e & 15)];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) top[i] = fmaxf(top[i], largest[w * 16 + 4 * ((e >> 4) & 3) + i]);
+        }
+        const int valid = m < hi ? (g.N - n < 4 ? g.N - n : 4) : 0;
+        settle_signs<4>(g, z, m, n, valid, v, whole, top);
+        if (valid > 0) finish<T, T, 4>(g, z, m, n, valid, v, none);
+        continue;
+      }
+    }
     if (m < hi && n < g.N) finish<T, T, 4>(g, z, m, n, g.N - n < 4 ? g.N - n : 4, v);
   }
 }

@@ -73,15 +73,6 @@ template <class T, int C, bool ALONG_L> __device__ __forceinline__ void give_n(c
 __device__ __forceinline__ double scale_of(double sum, float eps) {
   return sum <= 1.7976931348623157e308 ? 1.0 / (sqrt(sum) + (double)eps) : (double)NAN;
 }
-__device__ __forceinline__ double wave_sum64(double v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) {
-    const long long b = __builtin_bit_cast(long long, v);
-    const int lo = __shfl((int)b, (threadIdx.x & 63) ^ o, 64), hi = __shfl((int)(b >> 32), (threadIdx.x & 63) ^ o, 64);
-    v += __builtin_bit_cast(double, ((long long)hi << 32) | (unsigned)lo);
-  }
-  return v;
-}
 
 // ---- short side up to 8: a wavefront per matrix, all in registers -----------------------------------
 // Lane l has the columns l, l + 64, ... of the long side; A is summed over the lanes and every lane has all of it.  Bound by the

@@ -373,3 +373,38 @@ def test_core_update_values(lib, n, d, R, nesterov):
     assert ws.intact()
     t.r[1] = 129
     assert lib.tt_core_ortho_workspace_bytes(ctypes.byref(t)) == 0 and call() == binding.TT_ERR_SHAPE
+
+
+@pytest.mark.parametrize("rows,k,n,groups", [(1, 8, 1, 0), (70, 64, 66, 0), (33, 21, 40, 0), (40, 600, 40, 0), (130, 48, 130, 0), (90, 64, 70, 3)])
+def test_relu_decides_the_sign_exactly(lib, rows, k, n, groups):
+    """fp32 relu: biases that cancel a column's sum for one row down to its last bits, so that fp32 sums have any sign: the stored
+    pre-activation is the exact value's, to half a step of it and 64-bit rounding of the terms."""
+    x, w, _, _, grad = make(rows, k, n, torch.float32, groups, seed=rows + k)
+    offsets = torch.tensor([0, 25, 25, 80]) if groups else None
+    where = [(min(c, rows - 1), c, 0) for c in range(n)]  # the row that each column's bias cancels, and its group
+    if groups:
+        where = [(lo + c % (hi - lo), c, g) for g, (lo, hi) in enumerate(ref.ranges(offsets, 3, rows)) if hi > lo for c in range(n)]
+    bias = torch.zeros(w.shape[:-1])
+    exact = {}
+    for m, c, g in where:
+        wg, bg = (w[g], bias[g]) if groups else (w, bias)
+        s = float((x[m].double() * wg[c].double()).sum())
+        bg[c] = -s
+        exact[m, c] = s + float(bg[c]), float((x[m].double() * wg[c].double()).abs().sum())
+    gx, gw, gb, out, pre = place(x), place(w), place(bias), Guarded((rows, n), torch.float32), Guarded((rows, n), torch.float32)
+    op = dense_op(x, w, "relu", offsets)
+    need = lib.tt_dense_workspace_bytes(ctypes.byref(op), 0)
+    ws = Guarded((1, max(1, need)), torch.uint8)
+    assert lib.tt_dense_forward(ctypes.byref(op), gx.ptr, gw.ptr, gb.ptr, None, out.ptr, pre.ptr, ws.ptr, need, None) == 0
+    assert any(z != 0 for z, _ in exact.values())
+    for (m, c), (z, size) in exact.items():
+        got = float(pre.t[m, c])
+        assert abs(got - z) <= ref.U * abs(z) + 2 * k * 2.0 ** -53 * size, (m, c, got, z)
+        if abs(z) > 2 * k * 2.0 ** -53 * size:
+            assert (got > 0) == (z > 0) and (float(out.t[m, c]) > 0) == (z > 0), (m, c, got, z)
+    want, tol, z, tz = ref.forward64(x, w, bias, None, "relu", offsets)
+    member = ~torch.isnan(z[:, 0])
+    ref.check(out.t[member], want[member], tol[member], "out")
+    ref.check(pre.t[member], z[member], tz[member], "pre")
+    for g in (gx, gw, gb, out, pre, ws):
+        assert g.intact()

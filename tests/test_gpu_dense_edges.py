@@ -1,0 +1,67 @@
+"""The dense operators on the GPU where a last bit, a special value or a second caller decides: relu's sign, numbers near the ends of the
+range, NaN beside sums, gelu's tail, kept state."""
+import math
+
+import pytest
+import torch
+
+import dense_ref as ref
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def tt():
+    import paper_2507_14668_amd as tt
+    return tt
+
+
+def normal(*shape, seed=0, std=1.0, dtype=torch.float32):
+    return (torch.randn(*shape, generator=torch.Generator().manual_seed(seed)) * std).to(dtype)
+
+
+@pytest.mark.parametrize("rows,k,n,sizes", [(1, 128, 512, None), (48, 200, 96, None), (300, 128, 130, None), (300, 3000, 260, None), (4096, 128, 2048, None),
+                                            (5000, 77, 1500, None), (3000, 96, 640, (1000, 0, 7, 1993))])
+def test_relu_decides_the_sign_exactly(tt, rows, k, n, sizes):
+    """Biases that cancel a column's sum for one row of the first group down to its last bits: the stored pre-activation has the exact value's sign,
+    and the output and the gradients follow it."""
+    groups = 0 if sizes is None else len(sizes)
+    lead = (groups,) if groups else ()
+    x, w, bias = normal(rows, k, seed=rows), normal(*lead, n, k, seed=k, std=k ** -0.5), normal(*lead, n, seed=n)
+    off = None if sizes is None else torch.tensor([0] + list(sizes)).cumsum(0)
+    cols = torch.arange(n)
+    at = cols % (sizes[0] if groups else rows)
+    w0, b0 = (w[0], bias[0]) if groups else (w, bias)
+    terms = x[at].double() * w0.double()
+    b0.copy_(-terms.sum(1).float())
+    exact, noise = terms.sum(1) + b0.double(), 2 * k * 2.0 ** -53 * terms.abs().sum(1)
+    dx, dw, db, doff = x.cuda(), w.cuda(), bias.cuda(), None if off is None else off.cuda()
+    pre = torch.empty(rows, n, device="cuda")
+    out = tt.tt_dense_forward(dx, dw, db, None, "relu", offsets=doff, pre=pre)
+    got, value = pre.cpu()[at, cols].double(), out.cpu()[at, cols]
+    assert bool(((got - exact).abs() <= ref.U * exact.abs() + noise).all())
+    clear = exact.abs() > noise
+    assert int(clear.sum()) > 0.5 * n and torch.equal((value > 0)[clear], (exact > 0)[clear])
+    grad = torch.zeros(rows, n)
+    grad[at, cols] = 1.0
+    db = tt.tt_dense_backward(dx, dw, grad.cuda(), pre, "relu", offsets=doff, needs=(False, False, True))[2].cpu()
+    assert torch.equal(((db[0] if groups else db) == 1)[clear], (exact > 0)[clear])
+    assert torch.equal(tt.tt_dense_forward(dx, dw, db.cuda() * 0 + bias.cuda(), None, "relu", offsets=doff), out)
+
+
+@pytest.mark.parametrize("seed", range(4))
+def test_relu_gradients_of_a_large_batch(tt, seed):
+    """16384 x 128 -> 512: every one of 8 million signs is that of 64 bits, and the gradients are the formula's to fp32 rounding."""
+    rows, k, n = 16384, 128, 512
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    x, w, bias, grad = (torch.randn(*s, generator=gen, device="cuda") for s in ((rows, k), (n, k), (n,), (rows, n)))
+    w, bias = w * k ** -0.5, bias * 0.1
+    leaves = [t.requires_grad_(True) for t in (x, w, bias)]
+    got = torch.autograd.grad(tt.tt_dense(x, w, bias, None, "relu"), leaves, grad)
+    with torch.no_grad():
+        z = x.double() @ w.double().t() + bias.double()
+        dz = torch.where(z > 0, grad.double(), torch.zeros((), dtype=torch.float64, device="cuda"))
+        want = (dz @ w.double(), dz.t() @ x.double(), dz.sum(0))
+    for g, v, name in zip(got, want, ("dx", "dw", "dbias")):
+        # one sign the other way moves a row of dx by about 5e-4 of the whole; sums of up to 16384 terms in fp32 are off by a few 1e-6 in 2-norm
+        assert float((g.double() - v).norm() / v.norm()) < 2e-5, name

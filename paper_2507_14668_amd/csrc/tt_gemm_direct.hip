@@ -119,6 +119,28 @@ __device__ __forceinline__ void step_of(unsigned short *__restrict__ now, const 
   half_step<T, AKC, BKC>(next, 0, wm, wn, sums, fa, fb, acc, rs);
 }
 
+// Sums of A's rows wm .. + 127 from memory, in the order of the steps above: for tiles where the one result that keeps all eight of a lane's
+// sums is of no use (a NaN or an infinity times its zeros is NaN, in the sums of seven other rows).  Eight results of their own do not fit the
+// registers beside the product, and such tiles are the exception; the bits of the other sums are the same either way.
+template <class T> __device__ __forceinline__ void row_sums(const T *a, long long lda, int rows, int K, int wm, f32x4 (&rs)[8]) {
+  const int lane = threadIdx.x & 63, q = lane >> 4, j = lane & 15;
+  const unsigned short one = std::is_same<T, f16>::value ? 0x3c00 : 0x3f80;
+#pragma unroll 1
+  for (int k0 = 0; k0 < K; k0 += 32) {
+#pragma unroll
+    for (int x = 0; x < 8; ++x) {
+      const int c = wm + 16 * x + j;
+      u16x8 v;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int k = k0 + 8 * q + i;
+        v[i] = k < K && c < rows ? __builtin_bit_cast(unsigned short, a[k * lda + c]) : (unsigned short)0;
+      }
+      rs[x] = mma(T(), u16x8{one, one, one, one, one, one, one, one}, v, rs[x]);
+    }
+  }
+}
+
 template <class T, bool AKC, bool BKC> __global__ void __launch_bounds__(THREADS, 2) k_gemm_direct(TTGemm g, int m_tiles, int n_tiles, int chunk, float *partial) {
   __shared__ __align__(16) unsigned short lds[16 * finish_floats<4, 4>()];  // (more than two buffers take)
   static_assert(16 * finish_floats<4, 4>() >= STAGES * 2 * OPERAND, "LDS");
@@ -186,26 +208,37 @@ template <class T, bool AKC, bool BKC> __global__ void __launch_bounds__(THREADS
     }
     wait_loads<0>();  // the zeros too, before LDS is used for something else
   }
+  auto give_sum = [&](int m, float v) {
+    if (m >= w.hi) return;
+    if (piece) piece[(long long)g.M * g.N + m] = v;
+    else ((T *)g.rowsum)[w.z * g.rs_step + m] = from_f32<T>(v);
+  };
+  bool odd = false;  // a sum that is not finite, in any lane
   if constexpr (!AKC) {
-    if (sums && lane < 32) {
+    if (sums) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const int m = w.lo + wm + 16 * (4 * (lane >> 4) + i) + (lane & 15);
-        if (m >= w.hi) continue;
-        if (piece) piece[(long long)g.M * g.N + m] = rs[i];
-        else ((T *)g.rowsum)[w.z * g.rs_step + m] = from_f32<T>(rs[i]);
+        odd |= lane < 32 && !(fabsf(rs[i]) < INFINITY);
+        if (lane < 32) give_sum(w.lo + wm + 16 * (4 * (lane >> 4) + i) + (lane & 15), rs[i]);
       }
+      odd = __ballot(odd) != 0;
     }
   }
   __syncthreads();  // nobody reads the operands any more
   float *room = reinterpret_cast<float *>(lds) + wave * finish_floats<4, 4>();
   if constexpr (!AKC) {  // (only sums over stored rows are cut)
-    if (piece) {
-      finish_tile<T, float, 8, 4, 4, false>(as_piece(g, piece), 0, w.lo + wm, w.hi, w.n0 + wn, acc, room);
-      return;
+    if (piece) finish_tile<T, float, 8, 4, 4, false>(as_piece(g, piece), 0, w.lo + wm, w.hi, w.n0 + wn, acc, room);
+    else finish_tile<T, T, 8, 4, 4, true>(g, w.z, w.lo + wm, w.hi, w.n0 + wn, acc, room);
+    if (odd) {
+      f32x4 whole[8] = {};
+      row_sums<T>(a, g.lda, w.hi - w.lo, K, wm, whole);
+#pragma unroll
+      for (int x = 0; x < 8; ++x)
+        if (lane < 16) give_sum(w.lo + wm + 16 * x + lane, whole[x][0]);
     }
+  } else {
+    finish_tile<T, T, 8, 4, 4, true>(g, w.z, w.lo + wm, w.hi, w.n0 + wn, acc, room);
   }
-  finish_tile<T, T, 8, 4, 4, true>(g, w.z, w.lo + wm, w.hi, w.n0 + wn, acc, room);
 }
 
 template <class T> tt_status launch(const TTGemm &g, void *partial, hipStream_t s) {

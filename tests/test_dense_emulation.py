@@ -408,3 +408,40 @@ def test_relu_decides_the_sign_exactly(lib, rows, k, n, groups):
     ref.check(pre.t[member], z[member], tz[member], "pre")
     for g in (gx, gw, gb, out, pre, ws):
         assert g.intact()
+
+
+@pytest.mark.parametrize("dtype", DT, ids=str)
+@pytest.mark.parametrize("offs", [None, [0, 20, 64], [0, 64, 64]])
+def test_bias_gradient_beside_special_values(lib, dtype, offs):
+    """A NaN or an infinity in a column of the gradient reaches that column's sum only, with and without the weights' gradient beside it, and the
+    other sums have the bits that they have without it (fp32: they may be formed by another instruction then)."""
+    rows, k, n = 64, 264, 264
+    groups = 0 if offs is None else len(offs) - 1
+    offsets = None if offs is None else torch.tensor(offs, dtype=torch.int64)
+    x, w, _, _, grad = make(rows, k, n, dtype, groups)
+    op = dense_op(x, w, "none", offsets)
+    need = lib.tt_dense_workspace_bytes(ctypes.byref(op), 1)
+    gx, ws = place(x), Guarded((1, need), torch.uint8)
+
+    def dbias(g, with_dw):
+        gg, ow, ob = place(g), Guarded(tuple(w.shape), dtype), Guarded(tuple(w.shape[:-1]), dtype)
+        assert lib.tt_dense_backward(ctypes.byref(op), gx.ptr, None, None, gg.ptr, None, ow.ptr if with_dw else None, ob.ptr, ws.ptr, need, None) == 0
+        assert ow.intact() and ob.intact() and ws.intact()
+        return ob.t.clone().view(-1, n)
+    clean = dbias(grad, True)
+    # fp32 sums of m terms are each within 2 (m + 2) u sum |terms| of the exact one, so two of them within twice that of each other
+    most = 0.0 if dtype != torch.float32 else 4 * (rows + 2) * ref.U * float(grad.double().abs().sum(0).max())
+    assert torch.equal(dbias(grad, False), clean)
+    for value, cols in ((float("nan"), (7,)), (float("inf"), (7,)), (float("-inf"), (130, 263)), (float("inf"), (0, 16))):
+        bad = grad.clone()
+        bad[rows - 1, list(cols)] = value
+        want = clean.clone()
+        member = [(lo, hi) for lo, hi in ref.ranges(offsets, max(groups, 1), rows)]
+        for g, (lo, hi) in enumerate(member):
+            if lo <= rows - 1 < hi:
+                want[g, list(cols)] = value
+        for with_dw in (True, False):
+            got = dbias(bad, with_dw)
+            assert torch.equal(got.isnan(), want.isnan()), (value, cols, with_dw)
+            off = (got.nan_to_num(3.0, 4.0, 5.0).double() - want.nan_to_num(3.0, 4.0, 5.0).double()).abs()
+            assert bool((off <= most).all()), (value, cols, with_dw)

@@ -65,3 +65,24 @@ def test_relu_gradients_of_a_large_batch(tt, seed):
     for g, v, name in zip(got, want, ("dx", "dw", "dbias")):
         # one sign the other way moves a row of dx by about 5e-4 of the whole; sums of up to 16384 terms in fp32 are off by a few 1e-6 in 2-norm
         assert float((g.double() - v).norm() / v.norm()) < 2e-5, name
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16], ids=str)
+@pytest.mark.parametrize("rows,k,n,groups", [(520, 4096, 2560, 0), (5000, 1024, 1024, 12), (300, 256, 264, 0)])
+def test_bias_gradient_beside_special_values(tt, rows, k, n, groups, dtype):
+    """A NaN or an infinity in a column of the gradient reaches that column's sum only, whatever else is asked for (the first two sizes are those
+    of the largest tiles, whole and cut along the rows)."""
+    lead = (groups,) if groups else ()
+    x, w, grad = normal(rows, k, dtype=dtype).cuda(), torch.zeros(*lead, n, k, dtype=dtype, device="cuda"), normal(rows, n, seed=1, dtype=dtype).cuda()
+    off = None
+    if groups:
+        off = torch.tensor([0] + [rows - 8 * (groups - 1) + 8 * g for g in range(groups)], device="cuda")
+    clean = tt.tt_dense_backward(x, w, grad, offsets=off)[2]
+    for value, cols in ((math.nan, (7,)), (math.inf, (7, n - 1)), (-math.inf, (130,))):
+        bad = grad.clone()
+        bad[11, list(cols)] = value
+        want = clean.clone()
+        want[(0, list(cols)) if groups else list(cols)] = value
+        for needs in ((False, True, True), (False, False, True)):
+            got = tt.tt_dense_backward(x, w, bad, offsets=off, needs=needs)[2]
+            assert torch.equal(got.isnan(), want.isnan()) and torch.equal(got.nan_to_num(3.0, 4.0, 5.0), want.nan_to_num(3.0, 4.0, 5.0)), (value, cols, needs)

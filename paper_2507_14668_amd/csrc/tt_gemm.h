@@ -36,10 +36,10 @@ struct TTGemm {
   int parts;                   // fp32 operands: bf16 parts of each that are multiplied (3: fp32's precision, 2: 16 bits)
 };
 
-// relu in fp32: which side of its kink a result lies on decides whole rows of gradients, so the sums that fp32 cannot tell from -bias
-// are formed again in 64 bits (settle_signs in tt_gemm_device.h).
+// relu in fp32: which side of its kink a result lies on decides whole rows of gradients, so results that rounding could have taken to the
+// other side are formed again in 64 bits (settle_signs in tt_gemm_device.h).
 __host__ __device__ inline bool ttk_gemm_settles(const TTGemm &g) { return g.dtype == TT_F32 && g.act == TT_ACT_RELU; }
-// A piece of a cut product: sums [M][N], then sums of A's rows [M]; with settled signs also sums of |A|'s rows [M] and the largest of |B|'s rows [N].
+// A piece of a cut product: sums [M][N], then sums of A's rows [M]; with settled signs also squares of A's rows [M] and of B's [N].
 __host__ __device__ inline long long ttk_gemm_piece_floats(const TTGemm &g) {
   return (long long)g.M * (g.N + 1LL) + (ttk_gemm_settles(g) ? (long long)g.M + g.N : 0);
 }

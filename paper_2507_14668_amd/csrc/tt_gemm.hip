@@ -219,7 +219,7 @@ __global__ void __launch_bounds__(TT_BLOCK, 2) k_gemm(TTGemm g, int m_tiles, int
   __shared__ __align__(16) unsigned short lds[HALVES > REDO ? (HALVES > FINISH ? HALVES : FINISH) : (REDO > FINISH ? REDO : FINISH)];
   __shared__ int flags[4];
   constexpr bool SETTLES = P == 3 && AKC && BKC;
-  __shared__ float sizes[SETTLES ? E : 1], largest[SETTLES ? E : 1];  // sums of |A|'s rows, the largest of |B|'s
+  __shared__ float norms_a[SETTLES ? E : 1], norms_b[SETTLES ? E : 1];  // sums of squares of A's and B's rows
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int members = (int)gridDim.y / split, cut = (int)blockIdx.y / members;  // which piece of K
   unsigned mt, nt;
@@ -266,18 +266,17 @@ __global__ void __launch_bounds__(TT_BLOCK, 2) k_gemm(TTGemm g, int m_tiles, int
   f32x4 acc[F][F] = {}, rs[F] = {};  // [m][n]; sums of A's rows
   const bool sums = g.rowsum && w.n0 == 0;
   const bool settles = SETTLES && ttk_gemm_settles(g);
-  float size[CA::N] = {}, most[CB::N] = {};  // of the rows that the thread carries (its units are of one row each, all along K)
+  float squares_a[CA::N] = {}, squares_b[CB::N] = {};  // of the rows that the thread carries (its units are of one row each, all along K)
   auto measure = [&]() {
     if constexpr (SETTLES) {
       if (settles) {
 #pragma unroll
         for (int i = 0; i < CA::N; ++i)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) size[i] += fabsf(ua[i].a[e]) + fabsf(ua[i].b[e]);
-#pragma unroll
-        for (int i = 0; i < CB::N; ++i)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) most[i] = fmaxf(most[i], fmaxf(fabsf(ub[i].a[e]), fabsf(ub[i].b[e])));
+          for (int e = 0; e < 4; ++e) {
+            squares_a[i] = fmaf(ua[i].a[e], ua[i].a[e], fmaf(ua[i].b[e], ua[i].b[e], squares_a[i]));
+            squares_b[i] = fmaf(ub[i].a[e], ub[i].a[e], fmaf(ub[i].b[e], ub[i].b[e], squares_b[i]));
+          }
       }
     }
   };
@@ -345,9 +344,9 @@ __global__ void __launch_bounds__(TT_BLOCK, 2) k_gemm(TTGemm g, int m_tiles, int
     int buf = 0;
     for (int k0 = w.k_lo; k0 < K; k0 += BK) {
       const bool more = k0 + BK < K;
-      measure();
       __syncthreads();  // two buffers: this step's tiles are whole, and nobody reads the other buffer any more
       if constexpr (BUF == 1) {
+        measure();
         ca.template store<P>(ua, plane_a(0, 0));
         cb.template store<P>(ub, plane_b(0, 0));
         __syncthreads();
@@ -468,17 +467,17 @@ __global__ void __launch_bounds__(TT_BLOCK, 2) k_gemm(TTGemm g, int m_tiles, int
       for (int i = 0; i < CA::N; ++i) {
 #pragma unroll
         for (int o = 1; o < PER; o *= 2) {
-          size[i] += __shfl(size[i], lane ^ o, 64);
-          most[i] = fmaxf(most[i], __shfl(most[i], lane ^ o, 64));
+          squares_a[i] += __shfl(squares_a[i], lane ^ o, 64);
+          squares_b[i] += __shfl(squares_b[i], lane ^ o, 64);
         }
         const int r = ((int)threadIdx.x + i * TT_BLOCK) / PER;
         if (lane % PER == 0) {
-          sizes[r] = size[i];
-          largest[r] = most[i];
+          norms_a[r] = squares_a[i];
+          norms_b[r] = squares_b[i];
           if (piece) {
             float *rows = piece + (long long)g.M * (g.N + 1LL);
-            if (w.n0 == 0 && w.lo + r < w.hi) rows[w.lo + r] = size[i];
-            if (w.lo == 0 && w.n0 + r < g.N) rows[g.M + w.n0 + r] = most[i];
+            if (w.n0 == 0 && w.lo + r < w.hi) rows[w.lo + r] = squares_a[i];
+            if (w.lo == 0 && w.n0 + r < g.N) rows[g.M + w.n0 + r] = squares_b[i];
           }
         }
       }
@@ -498,8 +497,8 @@ __global__ void __launch_bounds__(TT_BLOCK, 2) k_gemm(TTGemm g, int m_tiles, int
   float *room = reinterpret_cast<float *>(lds) + wave * finish_floats<F, 2>();
   const bool mirror = g.symmetric && mt != nt;
   if (piece) finish_tile<T, float, F, F, 2, false>(as_piece(g, piece), 0, w.lo + wm, w.hi, w.n0 + wn, acc, room, mirror);
-  else finish_tile<T, O, F, F, 2, false>(g, w.z, w.lo + wm, w.hi, w.n0 + wn, acc, room, mirror, settles ? sizes + wm : nullptr,
-                                                  settles ? largest + wn : nullptr);
+  else finish_tile<T, O, F, F, 2, false>(g, w.z, w.lo + wm, w.hi, w.n0 + wn, acc, room, mirror, settles ? norms_a + wm : nullptr,
+                                                  settles ? norms_b + wn : nullptr);
 }
 
 // The pieces of a cut product, added in order; four columns of a row per thread.
@@ -530,16 +529,18 @@ template <class T, class O> __device__ __forceinline__ void join_pieces(const TT
     if constexpr (std::is_same<T, float>::value && std::is_same<O, float>::value) {
       if (ttk_gemm_settles(g)) {
         const float none[4] = {0.f, 0.f, 0.f, 0.f};  // (bias is in v)
-        float size = 0.f, most[4] = {0.f, 0.f, 0.f, 0.f};
+        float a = 0.f, b[4] = {0.f, 0.f, 0.f, 0.f};
         for (int i = 0; i < pieces; ++i) {
           const float *rows = p + i * step + (long long)g.M * (g.N + 1LL);
           float t[4];
-          size += rows[m];
+          a += rows[m];
           load4(rows + g.M + n, valid, t);
 #pragma unroll
-          for (int c = 0; c < 4; ++c) most[c] = fmaxf(most[c], t[c]);
+          for (int c = 0; c < 4; ++c) b[c] += t[c];
         }
-        settle_signs<4>(g, z, m, n, valid, v, size, most);
+        float bias[4] = {0.f, 0.f, 0.f, 0.f};
+        if (g.bias) load4((const float *)g.bias + z * g.bias_step + n, valid, bias);
+        settle_signs<4>(g, z, m, n, valid, v, bias, a, b);
         if (valid > 0) finish<T, O, 4>(g, z, m, n, valid, v, none);
         continue;
       }

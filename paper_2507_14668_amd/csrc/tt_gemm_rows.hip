@@ -47,7 +47,7 @@ template <class T, int MT> __global__ void __launch_bounds__(THREADS) k_gemm_row
   typedef typename Piece<T>::type P;
   __shared__ __align__(16) float sums[WAVES * MT * 256];
   constexpr bool F32 = sizeof(T) == 4;
-  __shared__ __align__(16) float sizes[F32 ? WAVES * MT * 16 : 4], largest[F32 ? WAVES * 16 : 4];  // for settle_signs: of every wavefront's part of K
+  __shared__ __align__(16) float norms_a[F32 ? WAVES * MT * 16 : 4], norms_b[F32 ? WAVES * 16 : 4];  // for settle_signs: squares of every wavefront's part of K
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, q = lane >> 4, j = lane & 15;
   const int n0 = (int)(blockIdx.x % (unsigned)n_tiles) * 16, mt = (int)(blockIdx.x / (unsigned)n_tiles);
   int z, lo, hi;
@@ -83,7 +83,7 @@ template <class T, int MT> __global__ void __launch_bounds__(THREADS) k_gemm_row
     }
   };
   const bool settles = F32 && ttk_gemm_settles(g);
-  float size[MT] = {}, most = 0.f;  // of the lane's values of rows j
+  float squares_a[MT] = {}, squares_b = 0.f;  // of the lane's values of rows j
   const int first = wave * C::K;
   if (first < K) load(fb[0], fa[0], first);
   if (first + skip < K) load(fb[1], fa[1], first + skip);
@@ -101,9 +101,9 @@ template <class T, int MT> __global__ void __launch_bounds__(THREADS) k_gemm_row
           for (int i = 0; i < C::LOADS; ++i)
 #pragma unroll
             for (int e = 0; e < C::E; ++e) {
-              most = fmaxf(most, fabsf(fb[d][i][e]));
+              squares_b = fmaf(fb[d][i][e], fb[d][i][e], squares_b);
 #pragma unroll
-              for (int x = 0; x < MT; ++x) size[x] += fabsf(fa[d][x][i][e]);
+              for (int x = 0; x < MT; ++x) squares_a[x] = fmaf(fa[d][x][i][e], fa[d][x][i][e], squares_a[x]);
             }
         }
       }
@@ -116,14 +116,14 @@ template <class T, int MT> __global__ void __launch_bounds__(THREADS) k_gemm_row
     if (settles) {
 #pragma unroll
       for (int o = 16; o < 64; o *= 2) {
-        most = fmaxf(most, __shfl(most, lane ^ o, 64));
+        squares_b += __shfl(squares_b, lane ^ o, 64);
 #pragma unroll
-        for (int x = 0; x < MT; ++x) size[x] += __shfl(size[x], lane ^ o, 64);
+        for (int x = 0; x < MT; ++x) squares_a[x] += __shfl(squares_a[x], lane ^ o, 64);
       }
       if (q == 0) {
-        largest[wave * 16 + j] = most;
+        norms_b[wave * 16 + j] = squares_b;
 #pragma unroll
-        for (int x = 0; x < MT; ++x) sizes[(wave * MT + x) * 16 + j] = size[x];
+        for (int x = 0; x < MT; ++x) norms_a[(wave * MT + x) * 16 + j] = squares_a[x];
       }
     }
   }
@@ -137,15 +137,17 @@ template <class T, int MT> __global__ void __launch_bounds__(THREADS) k_gemm_row
     if constexpr (F32) {
       if (settles) {  // (a wavefront has a whole turn of this loop or none)
         const float none[4] = {0.f, 0.f, 0.f, 0.f};  // (bias is in v)
-        float whole = 0.f, top[4] = {0.f, 0.f, 0.f, 0.f};
+        float sa = 0.f, sb[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) {
-          whole += sizes[(w * MT + (e >> 6)) * 16 + (e & 15)];
+          sa += norms_a[(w * MT + (e >> 6)) * 16 + (e & 15)];
 #pragma unroll
-          for (int i = 0; i < 4; ++i) top[i] = fmaxf(top[i], largest[w * 16 + 4 * ((e >> 4) & 3) + i]);
+          for (int i = 0; i < 4; ++i) sb[i] += norms_b[w * 16 + 4 * ((e >> 4) & 3) + i];
         }
         const int valid = m < hi ? (g.N - n < 4 ? g.N - n : 4) : 0;
-        settle_signs<4>(g, z, m, n, valid, v, whole, top);
+        float bias[4] = {0.f, 0.f, 0.f, 0.f};
+        if (g.bias) load4((const float *)g.bias + z * g.bias_step + n, valid, bias);
+        settle_signs<4>(g, z, m, n, valid, v, bias, sa, sb);
         if (valid > 0) finish<T, T, 4>(g, z, m, n, valid, v, none);
         continue;
       }

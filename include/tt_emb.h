@@ -412,8 +412,8 @@ tt_status tt_index_graph_edges(const int64_t *indices, const int64_t *offsets, i
  * are updated by their orthogonalised gradients.  These calls take fp32, bf16 or fp16 data; sums are fp32
  * on the matrix cores and reproducible: the same call gives the same bits (no atomics; the order of a sum
  * follows types, sizes and alignment).  fp32 operands are multiplied as three bf16 parts each, six products of
- * them, no less exact than the fp32 instruction, which takes over where infinities, NaN or products near the ends of
- * the range are met.  The calls allocate nothing and follow the conventions above.
+ * them, no less exact than the fp32 instruction, which takes over where infinities, NaN or numbers or products near the
+ * ends of the range would cost precision.  The calls allocate nothing and follow the conventions above.
  */
 typedef enum { TT_F32 = 0, TT_BF16 = 1, TT_F16 = 2 } tt_dtype;
 typedef enum {

@@ -203,9 +203,9 @@ template <bool KC, int LD32> __device__ __forceinline__ f32x4 frag32(const float
 // neighbours in a row of out.
 // P planes: 1 (16-bit operands), 2 or 3 (fp32 operands in bf16 parts).  Three parts hold all 24 bits; of the nine products
 // the six with hi * hi, hi * mid, hi * lo and mid * mid count, the rest is below 2^-24 of the product.  What parts cannot do:
-// infinities, NaN and numbers that round to a bf16 infinity give NaN sums, and products below 2^-92 lose parts to underflow.  A tile with
-// a sum that is not finite, or with a sum below 2^-80 beside operands whose smallest product is that small, is done
-// again with the fp32 instruction.  (P = 2 is for operands that are scaled to at most one, with no such products that count.)
+// infinities, NaN and numbers that round to a bf16 infinity give NaN sums, products below 2^-92 lose parts to underflow, and so do
+// numbers below 2^-100 by themselves.  A tile with a sum that is not finite, or with one so small that such a loss would
+// count beside operands that have it, is done again with the fp32 instruction.  (P = 2 is for operands that are scaled to at most one, with no such products that count.)
 // Measured: fp32 4096 x 4096 x 1024 198 us (174 TFLOP/s, 1040 of bf16 products; the fp32 instruction's rate is 154), 106496 x 128 x 128 40 us (22 by
 // its bytes); two parts 2048 x 4096 x 2048 106 us (975 of bf16 products).  Without the matrix instructions the first takes 169, without the split
 // of P = 2 the last 93: splitting, LDS and barriers bound it.  Loads two or four steps ahead in registers, and two buffers for P = 2, are no faster.
@@ -218,6 +218,7 @@ __global__ void __launch_bounds__(TT_BLOCK, 2) k_gemm(TTGemm g, int m_tiles, int
                 FINISH = 8 * finish_floats<F, 2>();
   __shared__ __align__(16) unsigned short lds[HALVES > REDO ? (HALVES > FINISH ? HALVES : FINISH) : (REDO > FINISH ? REDO : FINISH)];
   __shared__ int flags[4];
+  __shared__ float ends[4][2];
   constexpr bool SETTLES = P == 3 && AKC && BKC;
   __shared__ float norms_a[SETTLES ? E : 1], norms_b[SETTLES ? E : 1];  // sums of squares of A's and B's rows
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -280,8 +281,17 @@ __global__ void __launch_bounds__(TT_BLOCK, 2) k_gemm(TTGemm g, int m_tiles, int
       }
     }
   };
+  float large = 0.f;  // the largest number of both operands
+  auto note = [&](const Unit<T> *u, int n) {
+    if constexpr (P == 3) {
+#pragma unroll
+      for (int i = 0; i < n; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) large = tt_max3_abs(large, u[i].a[e], u[i].b[e]);
+    }
+  };
   // the smallest number that is not zero, as twice its bits less one
-  auto note = [&](const Unit<T> *u, int n, unsigned &small) {
+  auto note_small = [&](const Unit<T> *u, int n, unsigned &small) {
     if constexpr (P == 3) {
 #pragma unroll
       for (int i = 0; i < n; ++i)
@@ -347,6 +357,8 @@ __global__ void __launch_bounds__(TT_BLOCK, 2) k_gemm(TTGemm g, int m_tiles, int
       __syncthreads();  // two buffers: this step's tiles are whole, and nobody reads the other buffer any more
       if constexpr (BUF == 1) {
         measure();
+        note(ua, CA::N);
+        note(ub, CB::N);
         ca.template store<P>(ua, plane_a(0, 0));
         cb.template store<P>(ub, plane_b(0, 0));
         __syncthreads();
@@ -366,7 +378,11 @@ __global__ void __launch_bounds__(TT_BLOCK, 2) k_gemm(TTGemm g, int m_tiles, int
     }
   }
   if constexpr (P == 3) {
-    bool odd = false, tiny = false;
+    // A number below 2^-100 loses less than 2^-125 of itself to parts that are no normal numbers: nothing to a sum of more than 2^-98 K times
+    // the largest number.  That is below 2^-80 unless there are large numbers; smaller sums are of rows of zeros, mostly.
+    const float terms = (float)(K - w.k_lo);
+    bool odd = false;
+    float least = INFINITY;  // of the sums
 #pragma unroll
     for (int x = 0; x < F; ++x) {
       const bool in = w.lo + wm + 16 * x + (lane & 15) < w.hi;
@@ -374,32 +390,54 @@ __global__ void __launch_bounds__(TT_BLOCK, 2) k_gemm(TTGemm g, int m_tiles, int
       for (int y = 0; y < F; ++y)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          odd |= !(fabsf(acc[x][y][i]) < INFINITY);
-          tiny |= in && w.n0 + wn + 16 * y + 4 * (lane >> 4) + i < g.N && fabsf(acc[x][y][i]) < 0x1p-80f;
+          const float v = fabsf(acc[x][y][i]);
+          odd |= !(v < INFINITY);
+          if (in && w.n0 + wn + 16 * y + 4 * (lane >> 4) + i < g.N && v < least) least = v;
         }
-      if (sums) {
+      if (sums) {  // (sums of A's rows are of products with one)
         odd |= !(fabsf(rs[x][0]) < INFINITY);
-        tiny |= in && fabsf(rs[x][0]) < 0x1p-80f;
+        if (in && fabsf(rs[x][0]) < least) least = fabsf(rs[x][0]);
+        large = tt_max3_abs(large, large, 1.f);
       }
     }
-    // what any lane of the workgroup has seen: bits 0 and 1
+    // what any lane of the workgroup has seen
     auto any = [&](int mine) {
-      const int both = (__ballot(mine & 1) ? 1 : 0) | (__ballot(mine & 2) ? 2 : 0);
+      const int all = (__ballot(mine & 1) ? 1 : 0) | (__ballot(mine & 2) ? 2 : 0) | (__ballot(mine & 4) ? 4 : 0);
       __syncthreads();
-      if (lane == 0) flags[wave] = both;
+      if (lane == 0) flags[wave] = all;
       __syncthreads();
       return flags[0] | flags[1] | flags[2] | flags[3];
     };
-    int seen = any((odd ? 1 : 0) | (tiny ? 2 : 0));
-    if (seen == 2) {  // small sums (of rows of zeros, mostly): whether small operands are the reason takes another look at them
+    const int found = any((odd ? 1 : 0) | (least < 0x1p-80f ? 2 : 0) | (large * terms > 0x1p18f ? 4 : 0));
+    bool redo = found & 1, look = found & 2;
+    if (found == 4) {
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const float x = __shfl(least, lane ^ o, 64), y = __shfl(large, lane ^ o, 64);
+        least = x < least ? x : least;
+        large = y > large ? y : large;
+      }
+      if (lane == 0) {
+        ends[wave][0] = least;
+        ends[wave][1] = large;
+      }
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        least = ends[i][0] < least ? ends[i][0] : least;
+        large = ends[i][1] > large ? ends[i][1] : large;
+      }
+      look = least < 0x1p-98f * terms * large;
+    }
+    if (look && !redo) {  // whether small operands are the reason takes another look at them
       unsigned small_a = ~0u, small_b = ~0u;
       ca.start(a, g.lda, w.lo, w.hi, w.k_lo, K);
       cb.start(b, g.ldb, w.n0, g.N, w.k_lo, K);
       for (int k0 = w.k_lo; k0 < K; k0 += BK) {
         ca.load(ua, k0, K);
         cb.load(ub, k0, K);
-        note(ua, CA::N, small_a);
-        note(ub, CB::N, small_b);
+        note_small(ua, CA::N, small_a);
+        note_small(ub, CB::N, small_b);
       }
       unsigned ea = small_a == ~0u ? 255 : small_a >> 24, eb = small_b == ~0u ? 255 : small_b >> 24;  // exponents
 #pragma unroll
@@ -419,9 +457,9 @@ __global__ void __launch_bounds__(TT_BLOCK, 2) k_gemm(TTGemm g, int m_tiles, int
         eb = y < eb ? y : eb;
       }
       // the smallest product is below 2^-92 if the exponents' sum (each 127 too many) is; parts themselves are whole down to 2^-100
-      if ((int)(ea + eb) - 254 < -92 || ea < 27 || eb < 27) seen = 1;
+      redo = ea < 27 || eb < 27 || ((found & 2) && (int)(ea + eb) - 254 < -92);
     }
-    if (seen & 1) {
+    if (redo) {
       float *l32a = reinterpret_cast<float *>(lds), *l32b = l32a + CA::SIZE32;
 #pragma unroll
       for (int x = 0; x < F; ++x) {

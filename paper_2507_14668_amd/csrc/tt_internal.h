@@ -160,6 +160,14 @@ __device__ __forceinline__ float tt_min3_abs(float m, float x, float y) {
   return fminf(m, fminf(fabsf(x), fabsf(y)));
 #endif
 }
+__device__ __forceinline__ float tt_max3_abs(float m, float x, float y) {  // likewise the largest (NaN does not count)
+#ifdef __HIP_DEVICE_COMPILE__
+  asm("v_max3_f32 %0, %0, |%1|, |%2|" : "+v"(m) : "v"(x), "v"(y));
+  return m;
+#else
+  return fmaxf(m, fmaxf(fabsf(x), fabsf(y)));
+#endif
+}
 // x, as a value that the compiler does not know to be x
 __device__ __forceinline__ int tt_anew(int x) {
 #ifdef __HIP_DEVICE_COMPILE__

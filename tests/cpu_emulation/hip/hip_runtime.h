@@ -89,6 +89,7 @@ static inline int __shfl_up(int v, int delta, int = 64) {
 static inline int __shfl(int v, int src, int width = 64) {  // src counts inside the lane's segment of `width` lanes
   return (int)(uint32_t)emu::wave_exchange((uint32_t)v, (__lane() & ~(width - 1)) | (src & (width - 1)));
 }
+static inline int __clz(int v) { return v ? __builtin_clz((unsigned)v) : 32; }
 static inline int __ffs(int v) { return __builtin_ffs(v); }
 static inline int __ffsll(unsigned long long v) { return __builtin_ffsll((long long)v); }
 static inline float __shfl_xor(float v, int mask, int = 64) {

@@ -445,3 +445,31 @@ def test_bias_gradient_beside_special_values(lib, dtype, offs):
             assert torch.equal(got.isnan(), want.isnan()), (value, cols, with_dw)
             off = (got.nan_to_num(3.0, 4.0, 5.0).double() - want.nan_to_num(3.0, 4.0, 5.0).double()).abs()
             assert bool((off <= most).all()), (value, cols, with_dw)
+
+
+@pytest.mark.parametrize("small,large", [(2.0 ** -115, 2.0 ** 105), (1e-35, 1e20), (2e-38, 1e25), (1e-36, 1.0), (3e-32, 1e38), (1e-30, 1e-6), (2.0 ** -90, 2.0 ** 3)])
+@pytest.mark.parametrize("rows,k,n", [(40, 32, 40), (70, 300, 66)])
+def test_small_numbers_beside_large_ones(lib, small, large, rows, k, n):
+    """Normal fp32 numbers near the lower end, in all of one operand or in a single entry of it, keep their 24 bits whatever they are multiplied by:
+    within 2 (K + 2) u sum |terms|, as everywhere."""
+    x, w, _, _, grad = make(rows, k, n, torch.float32, seed=3)
+    one = lambda t: torch.where(t == 0, torch.ones(()), t)
+    for a, b in ((small * one(x), large * one(w)), (large * one(x), small * one(w))):
+        for single in (False, True):
+            if single:  # one small number in each row (each column of the weight's), beside ones that sum to nothing
+                a, b = a.clone(), b.clone()
+                t = a if small * 100 > float(a.abs().max()) else b
+                keep = torch.zeros_like(t)
+                keep[torch.arange(t.shape[0]), torch.arange(t.shape[0]) % k] = 1.0
+                t.mul_(keep)
+            ga, gb, out = place(a), place(b), Guarded((rows, n), torch.float32)
+            op = dense_op(a, b, "none", None)
+            need = lib.tt_dense_workspace_bytes(ctypes.byref(op), 0)
+            ws = Guarded((1, max(1, need)), torch.uint8)
+            assert lib.tt_dense_forward(ctypes.byref(op), ga.ptr, gb.ptr, None, None, out.ptr, None, ws.ptr, need, None) == 0
+            want, size = a.double() @ b.double().t(), a.double().abs() @ b.double().abs().t()
+            # (and half of the smallest number for each term, where results are that small)
+            fine = torch.isfinite(size)  # (1e38 times three and more is an infinity: those rows have infinities and NaN where the formula has them)
+            ref.check(out.t[fine], want[fine], (2 * (k + 2) * ref.U * size + (k + 1) * 2.0 ** -149)[fine], "small beside large")
+            assert torch.equal(out.t[~fine].double().nan_to_num(7.0), want[~fine].nan_to_num(7.0))
+            assert out.intact() and ws.intact()

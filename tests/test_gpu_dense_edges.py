@@ -86,3 +86,28 @@ def test_bias_gradient_beside_special_values(tt, rows, k, n, groups, dtype):
         for needs in ((False, True, True), (False, False, True)):
             got = tt.tt_dense_backward(x, w, bad, offsets=off, needs=needs)[2]
             assert torch.equal(got.isnan(), want.isnan()) and torch.equal(got.nan_to_num(3.0, 4.0, 5.0), want.nan_to_num(3.0, 4.0, 5.0)), (value, cols, needs)
+
+
+@pytest.mark.parametrize("small,large", [(2.0 ** -115, 2.0 ** 100), (1e-35, 1e20), (2e-38, 1e25), (1e-30, 1e-6), (2.0 ** -101, 1.0)])
+@pytest.mark.parametrize("rows,k,n", [(8, 64, 96), (300, 256, 512), (2000, 96, 2100), (500, 4096, 130)])
+def test_small_numbers_beside_large_ones(tt, rows, k, n, small, large):
+    """Normal fp32 numbers near the lower end, all of an operand or one of each row, keep their 24 bits whatever they are multiplied by: within
+    2 (K + 2) u sum |terms| (and half of the smallest number for each term), forward and backward."""
+    x, w = normal(rows, k, seed=1).clamp(-3, 3), normal(n, k, seed=2).clamp(-3, 3)
+    for a, b in ((small * x, large * w), (large * x, small * w)):
+        for single in (False, True):
+            if single:
+                a, b = a.clone(), b.clone()
+                t = a if small * 100 > float(a.abs().max()) else b
+                keep = torch.zeros_like(t)
+                keep[torch.arange(t.shape[0]), torch.arange(t.shape[0]) % k] = 1.0
+                t.mul_(keep)
+            got = tt.tt_dense_forward(a.cuda(), b.cuda()).cpu()
+            bound = lambda k, size: 2 * (k + 2) * ref.U * size + (k + 1) * 2.0 ** -149
+            ref.check(got, a.double() @ b.double().t(), bound(k, a.double().abs() @ b.double().abs().t()), "out")
+            grad = b[:rows % n + 1, :1].expand(-1, rows).t().contiguous() if n > rows else b[:, :1].t().expand(rows, -1).contiguous()
+            grad = grad[:, :n] if grad.shape[1] >= n else grad.repeat(1, -(-n // grad.shape[1]))[:, :n].contiguous()
+            weight = a[:1].expand(n, -1).contiguous()
+            dx, dw, _ = tt.tt_dense_backward(a.cuda(), weight.cuda(), grad.cuda())
+            ref.check(dx.cpu(), grad.double() @ weight.double(), bound(n, grad.double().abs() @ weight.double().abs()), "dx")
+            ref.check(dw.cpu(), grad.double().t() @ a.double(), bound(rows, grad.double().abs().t() @ a.double().abs()), "dw")

@@ -366,6 +366,10 @@ tt_status tt_core_sgd_update_batched(int num_tables, tt_batch_item *items, float
  *
  * tt_fuse_lookups_starts is the same for members whose offsets hold the bag STARTS only
  * (int64[num_bags[t]], torch.nn.EmbeddingBag's default): member t's last bag ends at nnz[t].
+ *
+ * tt_fuse_lookups_ranges is one or the other (`starts` != 0: the offsets are starts) and also writes
+ * bag_ranges, DEVICE int64[num_tables + 1]: the first row of every member in the fused `out`, and the
+ * end -- the `offsets` with which tt_dense gives every member's rows a weight of their own.
  */
 #define TT_FUSE_MAX_TABLES 32
 typedef struct {
@@ -383,6 +387,10 @@ tt_status tt_fuse_lookups_starts(const tt_fuse_members *members, const int64_t *
                                  const int64_t *const *starts, const int64_t *const *remaps,
                                  const int64_t *nnz, const int64_t *num_bags, int64_t *fused_indices,
                                  int64_t *fused_offsets, void *stream);
+tt_status tt_fuse_lookups_ranges(const tt_fuse_members *members, const int64_t *const *indices,
+                                 const int64_t *const *offsets, int starts, const int64_t *const *remaps,
+                                 const int64_t *nnz, const int64_t *num_bags, int64_t *fused_indices,
+                                 int64_t *fused_offsets, int64_t *bag_ranges, void *stream);
 
 /*
  * Index-graph edges of one batch (Section III-G, index-graph generation algorithm): the weighted

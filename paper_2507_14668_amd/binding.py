@@ -27,7 +27,7 @@ EXPORTS = ("tt_workspace_bytes", "tt_index_reorder", "tt_emb_bag_forward", "tt_e
            "tt_core_sgd_update", "tt_emb_bag_backward_sgd", "tt_emb_bag_forward_static", "tt_reuse_buffer_bytes", "tt_emb_bag_forward_sample",
            "tt_bf16_cores_bytes", "tt_cores_to_bf16", "tt_emb_bag_forward_bf16",
            "tt_forward_bf16_direct_pays", "tt_emb_bag_forward_bf16_direct",
-           "tt_index_graph_workspace_bytes", "tt_index_graph_edges", "tt_fuse_shape", "tt_fuse_lookups", "tt_fuse_lookups_starts", "tt_plan_status", "tt_strerror", "tt_prof_create", "tt_prof_destroy",
+           "tt_index_graph_workspace_bytes", "tt_index_graph_edges", "tt_fuse_shape", "tt_fuse_lookups", "tt_fuse_lookups_starts", "tt_fuse_lookups_ranges", "tt_plan_status", "tt_strerror", "tt_prof_create", "tt_prof_destroy",
            "tt_prof_collect", "tt_kernel_name", "tt_batch_desc_bytes", "tt_index_reorder_batched",
            "tt_emb_bag_forward_batched", "tt_emb_bag_backward_batched", "tt_core_sgd_update_batched",
            "tt_dense_workspace_bytes", "tt_dense_forward", "tt_dense_backward", "tt_orthogonalize_workspace_bytes", "tt_orthogonalize",
@@ -144,6 +144,8 @@ def load_library():
         lib.tt_fuse_lookups.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp]
         lib.tt_fuse_lookups_starts.restype = ctypes.c_int
         lib.tt_fuse_lookups_starts.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp]
+        lib.tt_fuse_lookups_ranges.restype = ctypes.c_int
+        lib.tt_fuse_lookups_ranges.argtypes = [vp, vp, vp, ctypes.c_int, vp, vp, vp, vp, vp, vp, vp]
         lib.tt_plan_status.restype = ctypes.c_int
         lib.tt_plan_status.argtypes = [vp, vp, vp]
         lib.tt_prof_create.restype = vp
@@ -510,10 +512,11 @@ class FusedLayout:
             b0 += int(nb)
         return out
 
-    def fuse_lookups(self, indices, offsets, remaps=None, out=None, stream=None, starts=False):
+    def fuse_lookups(self, indices, offsets, remaps=None, out=None, stream=None, starts=False, ranges=None):
         """Maps the members' `(indices[t], offsets[t])` (CSR offsets, `bags + 1` long) into the fused
         table: returns `(fused_indices, fused_offsets)`; `out` may bring the two tensors to write.
-        `starts=True`: the offsets hold the bag starts only (`bags` long)."""
+        `starts=True`: the offsets hold the bag starts only (`bags` long).  `ranges` (int64, `members + 1`
+        long) receives the members' first rows in the fused output, and the end."""
         T = len(self.members)
         if len(indices) != T or len(offsets) != T:
             raise ValueError("one (indices, offsets) pair per member table")
@@ -531,9 +534,16 @@ class FusedLayout:
             raise ValueError("fused_indices / fused_offsets have the wrong length")
         ptrs = lambda ts: (ctypes.c_void_p * T)(*[None if x is None or x.numel() == 0 else x.data_ptr() for x in ts])
         i64s = lambda vs: (ctypes.c_int64 * T)(*vs)
-        call = load_library().tt_fuse_lookups_starts if starts else load_library().tt_fuse_lookups
-        st = call(ctypes.byref(self.c), ptrs(idx), ptrs(off), ptrs(rm) if remaps is not None else None,
-                  i64s(nnz), i64s(nb), _ptr(f_idx), _ptr(f_off), _stream(stream))
+        lib, p_rm = load_library(), ptrs(rm) if remaps is not None else None
+        if ranges is not None:
+            if _dev_i64(ranges, "ranges").numel() != T + 1:
+                raise ValueError("ranges has one entry a member, and one more")
+            st = lib.tt_fuse_lookups_ranges(ctypes.byref(self.c), ptrs(idx), ptrs(off), int(starts), p_rm, i64s(nnz), i64s(nb),
+                                            _ptr(f_idx), _ptr(f_off), _ptr(ranges), _stream(stream))
+        else:
+            call = lib.tt_fuse_lookups_starts if starts else lib.tt_fuse_lookups
+            st = call(ctypes.byref(self.c), ptrs(idx), ptrs(off), p_rm, i64s(nnz), i64s(nb), _ptr(f_idx), _ptr(f_off),
+                      _stream(stream))
         _check(st, "tt_fuse_lookups")
         return f_idx, f_off
 

@@ -455,7 +455,7 @@ tt_status tt_fuse_lookups(const tt_fuse_members *members, const int64_t *const *
                           const int64_t *nnz, const int64_t *num_bags, int64_t *fused_indices,
                           int64_t *fused_offsets, void *stream) {
   return ttk_fuse_lookups(members, indices, offsets, remaps, nnz, num_bags, false, fused_indices, fused_offsets,
-                          (hipStream_t)stream);
+                          nullptr, (hipStream_t)stream);
 }
 
 tt_status tt_fuse_lookups_starts(const tt_fuse_members *members, const int64_t *const *indices,
@@ -463,7 +463,16 @@ tt_status tt_fuse_lookups_starts(const tt_fuse_members *members, const int64_t *
                                  const int64_t *nnz, const int64_t *num_bags, int64_t *fused_indices,
                                  int64_t *fused_offsets, void *stream) {
   return ttk_fuse_lookups(members, indices, starts, remaps, nnz, num_bags, true, fused_indices, fused_offsets,
-                          (hipStream_t)stream);
+                          nullptr, (hipStream_t)stream);
+}
+
+tt_status tt_fuse_lookups_ranges(const tt_fuse_members *members, const int64_t *const *indices,
+                                 const int64_t *const *offsets, int starts, const int64_t *const *remaps,
+                                 const int64_t *nnz, const int64_t *num_bags, int64_t *fused_indices,
+                                 int64_t *fused_offsets, int64_t *bag_ranges, void *stream) {
+  if (!bag_ranges) return TT_ERR_INVALID_ARG;
+  return ttk_fuse_lookups(members, indices, offsets, remaps, nnz, num_bags, starts != 0, fused_indices, fused_offsets,
+                          bag_ranges, (hipStream_t)stream);
 }
 
 size_t tt_index_graph_workspace_bytes(int64_t num_bags, int64_t max_pairs) {

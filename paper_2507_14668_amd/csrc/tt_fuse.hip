@@ -26,7 +26,7 @@ static_assert(sizeof(FuseArgs) <= 3600, "the members travel as kernel arguments"
 
 // grid (tiles, members): thread p of member t maps lookup p and offset p of that member
 __global__ void __launch_bounds__(TT_BLOCK)
-k_fuse_lookups(FuseArgs a, int64_t *__restrict__ fused_idx, int64_t *__restrict__ fused_off) {
+k_fuse_lookups(FuseArgs a, int64_t *__restrict__ fused_idx, int64_t *__restrict__ fused_off, int64_t *__restrict__ ranges) {
   const FuseMember &m = a.m[blockIdx.y];
   const long long span = m.nnz > m.bags ? m.nnz : m.bags;
   for (long long p = (long long)blockIdx.x * blockDim.x + threadIdx.x; p < span;
@@ -49,7 +49,13 @@ k_fuse_lookups(FuseArgs a, int64_t *__restrict__ fused_idx, int64_t *__restrict_
       fused_off[m.b0 + p] = ok ? m.l0 + o : -1;
     }
   }
-  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0) fused_off[a.total_bags] = a.total_nnz;
+  if (blockIdx.x == 0 && threadIdx.x == 0) {
+    if (blockIdx.y == 0) fused_off[a.total_bags] = a.total_nnz;
+    if (ranges) {
+      ranges[blockIdx.y] = m.b0;
+      if (blockIdx.y == 0) ranges[a.T] = a.total_bags;
+    }
+  }
 }
 
 }  // namespace
@@ -75,7 +81,7 @@ tt_status ttk_fuse_shape(const tt_fuse_members *mem, long long N[3]) {
 tt_status ttk_fuse_lookups(const tt_fuse_members *mem, const int64_t *const *indices,
                            const int64_t *const *offsets, const int64_t *const *remaps,
                            const int64_t *nnz, const int64_t *num_bags, bool starts_only, int64_t *fused_indices,
-                           int64_t *fused_offsets, hipStream_t s) {
+                           int64_t *fused_offsets, int64_t *bag_ranges, hipStream_t s) {
   long long N[3];
   tt_status st = ttk_fuse_shape(mem, N);
   if (st != TT_OK) return st;
@@ -106,6 +112,6 @@ tt_status ttk_fuse_lookups(const tt_fuse_members *mem, const int64_t *const *ind
   long long tiles = tt_ceil_div(span, TT_BLOCK);
   if (tiles > 4096) tiles = 4096;
   hipLaunchKernelGGL(k_fuse_lookups, dim3((unsigned)tiles, (unsigned)a.T), dim3(TT_BLOCK), 0, s, a,
-                     fused_indices, fused_offsets);
+                     fused_indices, fused_offsets, bag_ranges);
   return tt_launch_status();
 }

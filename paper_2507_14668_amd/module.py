@@ -330,19 +330,9 @@ class TTFusedEmbeddingBags(torch.nn.Module):
             self.register_parameter("core%d" % k, torch.nn.Parameter(w))
         self.projection = None if projection is None else TTDense(embedding_dim, projection, activation=projection_activation,
                                                                   groups=len(tables), device=device, generator=generator)
-        self._table_rows = (None, None)  # bags of every table, and the device tensor of their running sums: kept while the counts stay
 
     def cores(self):
         return [self.core0, self.core1, self.core2]
-
-    def _row_offsets(self, bags, device):
-        if self._table_rows[0] != (bags, device):
-            ends = [0]
-            for b in bags:
-                ends.append(ends[-1] + b)
-            self._table_rows = ((bags, device), torch.tensor(ends, dtype=torch.int64, device=device))
-        self._table_rows[1].record_stream(torch.cuda.current_stream(device))  # (it may be replaced while this call's work is under way)
-        return self._table_rows[1]
 
     def member_core(self, t: int, k: int, core=None):
         """Table t's part of fused core k (or of a tensor of its size, e.g. `.grad`): a strided view
@@ -370,11 +360,13 @@ class TTFusedEmbeddingBags(torch.nn.Module):
             off.append(o)
         if self._fused is None:
             self._fused = binding.FusedLayout(self.tables)
-        f_idx, f_off = self._fused.fuse_lookups(idx, off, starts=not self.include_last_offset)
+        # (a call's own, written on the device: a captured call keeps its memory, and no other call sees it)
+        ranges = None if self.projection is None else torch.empty(len(self.tables) + 1, dtype=torch.int64, device=off[0].device)
+        f_idx, f_off = self._fused.fuse_lookups(idx, off, starts=not self.include_last_offset, ranges=ranges)
         out = _TTBagFunction.apply(self.core0, self.core1, self.core2, f_idx, f_off, self)
         bags = tuple(o.numel() - (1 if self.include_last_offset else 0) for o in off)
         if self.projection is not None:
-            out = self.projection(out, self._row_offsets(bags, out.device))
+            out = self.projection(out, ranges)
         return list(torch.split(out, bags))
 
     def _bag_offsets(self, input, offsets):

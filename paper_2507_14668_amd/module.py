@@ -117,14 +117,16 @@ def tt_dense(x, w, bias=None, residual=None, activation="none", offsets=None):
     `binding.tt_dense_forward`.  Rows of no group give zeros and get none: their residual is not added, and its gradient there
     is left out too.  With an activation in training the pre-activation is kept in x's type for the backward pass.  (As with any autograd
     function: a backward pass that is captured into a graph should accumulate into no leaf that an eager graph still holds;
-    `torch.autograd.grad` does not.)"""
+    `torch.autograd.grad` does not.  There is no forward-mode derivative: tensors with tangents are refused.)"""
     train = torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (x, w, bias, residual))
+    # inside a level of forward-mode differentiation the autograd function is asked, which refuses tensors with tangents
+    dual = torch.autograd.forward_ad._current_level >= 0
     if train and residual is not None and offsets is not None and residual.requires_grad:
         residual = _GroupRows.apply(residual, offsets)
     if bias is not None and not bias.is_contiguous():
         bias = bias.contiguous()
     x, w, residual = _row_major(x), w if w.is_contiguous() else w.contiguous(), _row_major(residual)
-    if not train:  # nothing is kept for a backward pass
+    if not train and not dual:  # nothing is kept for a backward pass
         return binding.tt_dense_forward(x, w, bias, residual, activation, offsets=offsets)
     return _DenseFunction.apply(x, w, bias, residual, activation, offsets)
 

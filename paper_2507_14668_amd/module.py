@@ -484,7 +484,8 @@ class TTOrthoSGD(torch.optim.Optimizer):
     """Gradient descent whose updates are orthogonalised (`binding.tt_orthogonalize`): momentum, then
     `W <- W - lr sqrt(max(1, rows / cols)) ortho(u)` for every dense weight of the model's `TTDense` layers (every group's own)
     and for every slice of the cores of its TT bags (`binding.tt_core_ortho_update`).  Whatever else the model has (biases,
-    other layers) takes plain steps of `other_lr` with the same momentum.  Momenta are float32.
+    other layers) takes plain steps of `other_lr` with the same momentum.  Momenta are float32, and so are the updates up to the
+    step itself, which is rounded to the parameter's type once.
 
     model   a module; its parameters are sorted by the layers that own them
     Tables without gradients (unused in this step, or with `fused_sgd_lr`) stay as they are.
@@ -541,7 +542,9 @@ class TTOrthoSGD(torch.optim.Optimizer):
                 u = torch.add(g, buf, alpha=mu) if group["nesterov"] else buf
                 if group["kind"] == "matrices":
                     rows, cols = p.shape[-2:]
-                    p.add_(binding.tt_orthogonalize(u.to(p.dtype), **how), alpha=-lr * math.sqrt(max(1.0, rows / cols)))
+                    # (in float32: rounded to 16 bits first, a sum of gradients leaves float16's range, and bfloat16's 8 bits are what the
+                    # steps take up to 485 times)
+                    p.add_(binding.tt_orthogonalize(u, **how), alpha=-lr * math.sqrt(max(1.0, rows / cols)))
                 else:
-                    p.add_(u.to(p.dtype), alpha=-lr)
+                    p.add_(u, alpha=-lr)
         return loss

@@ -17,7 +17,13 @@ def tt(monkeypatch):
         if pre is not None:
             pre.copy_(z)
         return y.to(x.dtype)
+
+    def orthogonalize(g, steps=5, coefficients=binding.ORTHO_COEFFICIENTS, eps=1e-7, out=None, workspace=None, stream=None):
+        assert g.stride(-1) == 1 and g.stride(-2) >= g.shape[-1]
+        x = g.reshape((-1,) + g.shape[-2:])
+        return ref.ortho(x, steps=steps, coefficients=coefficients, eps=eps).reshape(g.shape).to(g.dtype)
     monkeypatch.setattr(binding, "tt_dense_forward", forward)
+    monkeypatch.setattr(binding, "tt_orthogonalize", orthogonalize)
     return tt
 
 
@@ -34,3 +40,34 @@ def test_forward_mode_is_refused(tt):
                     tt.tt_dense(*args)
         assert torch.allclose(tt.tt_dense(x, w), x @ w.t())  # no tangents: as ever
     assert torch.allclose(tt.tt_dense(x, w), x @ w.t())
+
+
+def ortho_step64(p, g, m, lr, mu, matrix, eps):
+    """One step in 64 bits: (new parameter, new momentum)."""
+    m = mu * m.double() + g.double()
+    u = g.double() + mu * m
+    if matrix:
+        u = max(1.0, p.shape[-2] / p.shape[-1]) ** 0.5 * ref.ortho(u.reshape((-1,) + u.shape[-2:]), eps=eps).reshape(u.shape)
+    return p.double() - lr * u, m
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16], ids=str)
+@pytest.mark.parametrize("groups", [None, 3])
+@pytest.mark.parametrize("scale", [1e-9, 1e-8, 1.0, 1e5])
+def test_optimizer_steps_at_any_scale(tt, dtype, groups, scale):
+    """Momenta far below and above the range of half precision: the step is that of 64 bits, rounded to the parameter's type once."""
+    layer = tt.TTDense(24, 16, groups=groups, device="cpu", dtype=dtype, generator=torch.Generator().manual_seed(0))
+    opt = tt.TTOrthoSGD(layer, lr=0.01, momentum=0.95, eps=0.0)
+    gen = torch.Generator().manual_seed(1)
+    for p in (layer.weight, layer.bias):
+        opt.state[p]["momentum"] = torch.randn(p.shape, generator=gen) * scale
+        p.grad = (torch.randn(p.shape, generator=gen) * min(scale, 1e3)).to(dtype)
+    want = [ortho_step64(p.detach(), p.grad, opt.state[p]["momentum"], 0.01, 0.95, p is layer.weight, 0.0) for p in (layer.weight, layer.bias)]
+    opt.step()
+    for p, (new, m) in zip((layer.weight, layer.bias), want):
+        assert bool(torch.isfinite(new.to(dtype)).all()) == bool(torch.isfinite(p).all())
+        fine = torch.isfinite(new.to(dtype))
+        # half a step of the type, and the step itself in fp32: its singular values are near one, and errors of 2^-23 of u are taken 485 times at most
+        off = 485 * 2.0 ** -22 * 0.01 if p is layer.weight else 2.0 ** -21 * 0.01 * float(m.abs().max()) * 2
+        ref.check(p.detach()[fine], new[fine], ref.rounding(new, dtype)[fine] + off, "parameter")
+        ref.check(opt.state[p]["momentum"], m, 2.0 ** -22 * m.abs().max().expand(m.shape), "momentum")

@@ -488,7 +488,7 @@ class TTOrthoSGD(torch.optim.Optimizer):
     step itself, which is rounded to the parameter's type once.
 
     model   a module; its parameters are sorted by the layers that own them
-    Tables without gradients (unused in this step, or with `fused_sgd_lr`) stay as they are.
+    Cores and weights without gradients (frozen, unused in this step, or of tables with `fused_sgd_lr`) stay as they are.
     """
 
     def __init__(self, model, lr: float, momentum: float = 0.95, nesterov: bool = True, steps: int = 5,
@@ -529,9 +529,13 @@ class TTOrthoSGD(torch.optim.Optimizer):
             if group["kind"] == "cores":
                 for t in self._tables:
                     cores = t.cores()
-                    if any(c.grad is None for c in cores):
+                    steps = [c.grad is not None for c in cores]
+                    if not any(steps):
                         continue
-                    binding.tt_core_ortho_update(t._table(cores), [c.grad.contiguous() for c in cores], [self._momentum(c) for c in cores], lr,
+                    # cores are updated each by itself: one without a gradient (a frozen one) has a copy stand in for it
+                    binding.tt_core_ortho_update(t._table([c if s else c.clone() for c, s in zip(cores, steps)]),
+                                                 [c.grad.contiguous() if s else torch.zeros_like(c) for c, s in zip(cores, steps)],
+                                                 [self._momentum(c) if s else torch.zeros_like(c) for c, s in zip(cores, steps)], lr,
                                                  momentum=mu, nesterov=group["nesterov"], **how)
                 continue
             for p in group["params"]:

@@ -24,6 +24,22 @@ def tt(monkeypatch):
         return ref.ortho(x, steps=steps, coefficients=coefficients, eps=eps).reshape(g.shape).to(g.dtype)
     monkeypatch.setattr(binding, "tt_dense_forward", forward)
     monkeypatch.setattr(binding, "tt_orthogonalize", orthogonalize)
+
+    def core_update(table, dcores, momenta, lr, momentum=0.95, nesterov=True, steps=5, coefficients=binding.ORTHO_COEFFICIENTS, eps=1e-7, workspace=None,
+                    stream=None):
+        r, n, d = table.r, table.n, table.d
+        for k, (c, g, m) in enumerate(zip(table.cores, dcores, momenta)):
+            m.mul_(momentum).add_(g)
+            u = (g + momentum * m if nesterov else m).view(r[k], n[k], d[k] * r[k + 1]).transpose(0, 1)
+            u = u.reshape(n[k], d[0], r[1]) if k == 0 else u
+            o = ref.ortho(u, steps=steps, coefficients=coefficients, eps=eps) * max(1.0, u.shape[1] / u.shape[2]) ** 0.5
+            c.sub_((lr * o).float().reshape(n[k], r[k], -1).transpose(0, 1).reshape(-1))
+    monkeypatch.setattr(binding, "tt_core_ortho_update", core_update)
+
+    class Table:
+        def __init__(self, num_rows, n, d, r, cores):
+            self.n, self.d, self.r, self.cores = n, d, r, cores
+    monkeypatch.setattr(binding, "Table", Table)
     return tt
 
 
@@ -71,3 +87,26 @@ def test_optimizer_steps_at_any_scale(tt, dtype, groups, scale):
         off = 485 * 2.0 ** -22 * 0.01 if p is layer.weight else 2.0 ** -21 * 0.01 * float(m.abs().max()) * 2
         ref.check(p.detach()[fine], new[fine], ref.rounding(new, dtype)[fine] + off, "parameter")
         ref.check(opt.state[p]["momentum"], m, 2.0 ** -22 * m.abs().max().expand(m.shape), "momentum")
+
+
+def one_bag(tt, seed=0):
+    bag = tt.TTEmbeddingBag(24, 16, n=(2, 3, 4), d=(2, 2, 4), ranks=(4, 3), device="cpu", generator=torch.Generator().manual_seed(seed))
+    for c in bag.cores():
+        c.grad = torch.randn(c.shape, generator=torch.Generator().manual_seed(9))
+    return bag
+
+
+@pytest.mark.parametrize("frozen", [(0,), (1,), (0, 2), (0, 1, 2)])
+def test_frozen_cores_do_not_hold_up_the_others(tt, frozen):
+    bag, other = one_bag(tt), one_bag(tt)
+    for k in frozen:
+        bag.cores()[k].requires_grad_(False)
+        bag.cores()[k].grad = None
+    for m in (bag, other):
+        opt = tt.TTOrthoSGD(m, lr=0.01)
+        opt.step()
+        opt.step()
+    start = one_bag(tt)
+    for k in range(3):
+        assert torch.equal(bag.cores()[k], (start if k in frozen else other).cores()[k])
+        assert torch.equal(other.cores()[k], start.cores()[k]) is False

@@ -496,8 +496,9 @@ class TTOrthoSGD(torch.optim.Optimizer):
         if lr < 0 or not 0 <= momentum < 1:
             raise ValueError("lr must not be negative, momentum is in [0, 1)")
         self._tables = [m for m in model.modules() if isinstance(m, (TTEmbeddingBag, TTFusedEmbeddingBags))]
-        matrices = [m.weight for m in model.modules() if isinstance(m, TTDense)]
-        cores = [c for t in self._tables for c in t.cores()]
+        once = lambda ps: list({id(p): p for p in ps}.values())  # layers may share a parameter
+        matrices = once(m.weight for m in model.modules() if isinstance(m, TTDense))
+        cores = once(c for t in self._tables for c in t.cores())
         taken = {id(p) for p in matrices + cores}
         rest = [p for p in model.parameters() if id(p) not in taken]
         groups = [dict(params=ps, kind=kind, lr=rate) for ps, kind, rate in
@@ -527,12 +528,15 @@ class TTOrthoSGD(torch.optim.Optimizer):
         for group in self.param_groups:
             lr, mu, how = group["lr"], group["momentum"], dict(steps=group["steps"], coefficients=group["coefficients"], eps=group["eps"])
             if group["kind"] == "cores":
+                done = set()
                 for t in self._tables:
                     cores = t.cores()
-                    steps = [c.grad is not None for c in cores]
+                    steps = [c.grad is not None and id(c) not in done for c in cores]
                     if not any(steps):
                         continue
-                    # cores are updated each by itself: one without a gradient (a frozen one) has a copy stand in for it
+                    done.update(id(c) for c in cores)
+                    # cores are updated each by itself: one without a gradient (a frozen one), or that another table has too, has a copy stand
+                    # in for it
                     binding.tt_core_ortho_update(t._table([c if s else c.clone() for c, s in zip(cores, steps)]),
                                                  [c.grad.contiguous() if s else torch.zeros_like(c) for c, s in zip(cores, steps)],
                                                  [self._momentum(c) if s else torch.zeros_like(c) for c, s in zip(cores, steps)], lr,

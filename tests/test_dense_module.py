@@ -110,3 +110,28 @@ def test_frozen_cores_do_not_hold_up_the_others(tt, frozen):
     for k in range(3):
         assert torch.equal(bag.cores()[k], (start if k in frozen else other).cores()[k])
         assert torch.equal(other.cores()[k], start.cores()[k]) is False
+
+
+def test_shared_parameters_take_one_step(tt):
+    class Model(torch.nn.Module):
+        def __init__(self, shared):
+            super().__init__()
+            gen = torch.Generator().manual_seed(0)
+            self.a, self.b = (tt.TTDense(12, 8, device="cpu", generator=gen) for _ in range(2))
+            self.s, self.t = one_bag(tt, 1), one_bag(tt, 2)
+            if shared:
+                self.b.weight = self.a.weight
+                self.t.core1 = self.s.core1
+            for layer in (self.a, self.b):
+                layer.weight.grad = torch.ones_like(layer.weight)
+    models = [Model(True), Model(False)]
+    for m in models:
+        opt = tt.TTOrthoSGD(m, lr=0.01)
+        for group in opt.param_groups:
+            assert len({id(p) for p in group["params"]}) == len(group["params"])
+        opt.step()
+    both, apart = models
+    assert torch.equal(both.a.weight, apart.a.weight) and both.b.weight is both.a.weight
+    for k in range(3):
+        assert torch.equal(both.s.cores()[k], apart.s.cores()[k])
+        assert torch.equal(both.t.cores()[k], both.s.cores()[k] if k == 1 else apart.t.cores()[k])

@@ -552,7 +552,7 @@ class TTOrthoSGD(torch.optim.Optimizer):
                     rows, cols = p.shape[-2:]
                     # (in float32: rounded to 16 bits first, a sum of gradients leaves float16's range, and bfloat16's 8 bits are what the
                     # steps take up to 485 times)
-                    p.add_(binding.tt_orthogonalize(u, **how), alpha=-lr * math.sqrt(max(1.0, rows / cols)))
+                    p.add_(binding.tt_orthogonalize(u.contiguous(), **how), alpha=-lr * math.sqrt(max(1.0, rows / cols)))
                 else:
                     p.add_(u, alpha=-lr)
         return loss

@@ -135,3 +135,16 @@ def test_shared_parameters_take_one_step(tt):
     for k in range(3):
         assert torch.equal(both.s.cores()[k], apart.s.cores()[k])
         assert torch.equal(both.t.cores()[k], both.s.cores()[k] if k == 1 else apart.t.cores()[k])
+
+
+@pytest.mark.parametrize("nesterov", [True, False])
+def test_gradients_of_any_strides(tt, nesterov):
+    """A gradient that a caller set, with its columns apart, gives the step of the same numbers in a row."""
+    layers = [tt.TTDense(12, 8, groups=2, device="cpu", generator=torch.Generator().manual_seed(0)) for _ in range(2)]
+    g = torch.randn(2, 8, 12, generator=torch.Generator().manual_seed(1))
+    layers[0].weight.grad, layers[1].weight.grad = g, g.transpose(1, 2).contiguous().transpose(1, 2)
+    for layer in layers:
+        opt = tt.TTOrthoSGD(layer, lr=0.01, nesterov=nesterov)
+        opt.step()
+        opt.step()
+    assert torch.equal(layers[0].weight, layers[1].weight)

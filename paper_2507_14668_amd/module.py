@@ -513,6 +513,9 @@ class TTOrthoSGD(torch.optim.Optimizer):
                     m = state_dict["state"][name]["momentum"]
                     self.state[p]["momentum"] = m.to(device=p.device, dtype=torch.float32, copy=True).contiguous()
 
+    def __getstate__(self):  # copies and pickles have the tables too
+        return dict(super().__getstate__(), _tables=self._tables)
+
     def _momentum(self, p):
         state = self.state[p]
         if "momentum" not in state:

@@ -1,5 +1,7 @@
 """The dense layers' module side on the CPU: what reaches the library, what is refused, what an optimizer step computes.  The library's calls are
 replaced by their plain forms."""
+import copy
+
 import pytest
 import torch
 import torch.autograd.forward_ad as fw
@@ -148,3 +150,15 @@ def test_gradients_of_any_strides(tt, nesterov):
         opt.step()
         opt.step()
     assert torch.equal(layers[0].weight, layers[1].weight)
+
+
+def test_copies_of_model_and_optimizer(tt):
+    bag = one_bag(tt)
+    opt = tt.TTOrthoSGD(bag, lr=0.01)
+    opt.step()
+    bag2, opt2 = copy.deepcopy((bag, opt))
+    for c, c2 in zip(bag.cores(), bag2.cores()):
+        c2.grad = c.grad.clone()
+    opt.step()
+    opt2.step()
+    assert all(torch.equal(a, b) and a is not b for a, b in zip(bag.cores(), bag2.cores()))

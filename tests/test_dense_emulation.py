@@ -1,6 +1,7 @@
 """The dense operators' host code and kernels compiled for the CPU (tests/cpu_emulation): values against 64 bits through the C
 ABI, and every refusal of an argument.  Buffers sit between guards of ones that nothing may touch."""
 import ctypes
+import math
 import os
 import sys
 
@@ -473,3 +474,24 @@ def test_small_numbers_beside_large_ones(lib, small, large, rows, k, n):
             ref.check(out.t[fine], want[fine], (2 * (k + 2) * ref.U * size + (k + 1) * 2.0 ** -149)[fine], "small beside large")
             assert torch.equal(out.t[~fine].double().nan_to_num(7.0), want[~fine].nan_to_num(7.0))
             assert out.intact() and ws.intact()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16], ids=str)
+def test_gelu_of_16_bits_over_its_tail(lib, dtype):
+    """Value and slope to half a step of the type, relative to themselves, down to where they leave its range."""
+    z = torch.arange(-2 ** 15, 2 ** 15, dtype=torch.int32).to(torch.int16).view(dtype)
+    z = z[torch.isfinite(z) & (z >= -12.75) & (z <= 8) & (z.float().abs() >= 2.0 ** -8)][::7]
+    # Phi to 2e-6, the rounding of z^2 / 2 and of exp's argument, a few units for the rest; then half a step of the type
+    z64 = z.double()
+    phi, bell = 0.5 * torch.erfc(-z64 / math.sqrt(2)), torch.exp(-0.5 * z64 * z64) / math.sqrt(2 * math.pi)
+    near = 2e-6 + (z64 * z64 + 8) * ref.U
+    gx, gw, out, one, dx = place(z[:, None]), place(torch.ones(1, 1, dtype=dtype)), Guarded((len(z), 1), dtype), place(torch.ones(len(z), 1, dtype=dtype)), Guarded((len(z), 1), dtype)
+    op = dense_op(gx.t, gw.t, "gelu", None)
+    need = lib.tt_dense_workspace_bytes(ctypes.byref(op), 1)
+    ws = Guarded((1, need), torch.uint8)
+    assert lib.tt_dense_forward(ctypes.byref(op), gx.ptr, gw.ptr, None, None, out.ptr, None, ws.ptr, need, None) == 0
+    want = z64 * phi
+    ref.check(out.t[:, 0], want, near * want.abs() + ref.rounding(want, dtype), "gelu")
+    assert lib.tt_dense_backward(ctypes.byref(op), gx.ptr, gw.ptr, gx.ptr, one.ptr, dx.ptr, None, None, ws.ptr, need, None) == 0
+    want = phi + z64 * bell
+    ref.check(dx.t[:, 0], want, near * (phi + z64.abs() * bell) + ref.rounding(want, dtype), "slope")

@@ -111,3 +111,20 @@ def test_small_numbers_beside_large_ones(tt, rows, k, n, small, large):
             dx, dw, _ = tt.tt_dense_backward(a.cuda(), weight.cuda(), grad.cuda())
             ref.check(dx.cpu(), grad.double() @ weight.double(), bound(n, grad.double().abs() @ weight.double().abs()), "dx")
             ref.check(dw.cpu(), grad.double().t() @ a.double(), bound(rows, grad.double().abs().t() @ a.double().abs()), "dw")
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16], ids=str)
+def test_gelu_of_16_bits_over_its_tail(tt, dtype):
+    """Value and slope to half a step of the type, relative to themselves, down to where they leave its range."""
+    z = torch.arange(-2 ** 15, 2 ** 15, dtype=torch.int32).to(torch.int16).view(dtype)
+    z = z[torch.isfinite(z) & (z >= -12.75) & (z <= 8) & (z.float().abs() >= 2.0 ** -8)]
+    # Phi to 2e-6, the rounding of z^2 / 2 and of exp's argument, a few units for the rest; then half a step of the type
+    z64 = z.double()
+    phi, bell = 0.5 * torch.erfc(-z64 / math.sqrt(2)), torch.exp(-0.5 * z64 * z64) / math.sqrt(2 * math.pi)
+    near = 2e-6 + (z64 * z64 + 8) * ref.U
+    x, one = z[:, None].cuda(), torch.ones(1, 1, dtype=dtype, device="cuda")
+    want = z64 * phi
+    ref.check(tt.tt_dense_forward(x, one, activation="gelu").cpu()[:, 0], want, near * want.abs() + ref.rounding(want, dtype), "gelu")
+    want = phi + z64 * bell
+    got = tt.tt_dense_backward(x, one, torch.ones_like(x), x, "gelu", needs=(True, False, False))[0]
+    ref.check(got.cpu()[:, 0], want, near * (phi + z64.abs() * bell) + ref.rounding(want, dtype), "slope")

@@ -692,10 +692,13 @@ def _dense_op(x, w, activation, offsets):
         raise ValueError("x must be [rows, %d], got %s" % (k, tuple(x.shape)))
     _packed(w, "w", dtype, at, shape)
     rows, groups, starts = x.shape[0], 0, None
+    step = _rows_of(x, "x", dtype, at, rows, k)
     if offsets is not None:
         groups = shape[0]
         starts = _packed(offsets, "offsets", torch.int64, at, (groups + 1,))
-    return CDense(DTYPES[dtype], ACTIVATIONS[activation], rows, k, n, groups, 0, starts, _rows_of(x, "x", dtype, at, rows, k)), at
+    if max(k, n, groups) > 0x7fffffff:  # the library's fields would take it modulo 2^32
+        raise TTError(TT_ERR_SHAPE, "tt_dense")
+    return CDense(DTYPES[dtype], ACTIVATIONS[activation], rows, k, n, groups, 0, starts, step), at
 
 
 def _workspace(t, at):

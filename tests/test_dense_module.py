@@ -162,3 +162,16 @@ def test_copies_of_model_and_optimizer(tt):
     opt.step()
     opt2.step()
     assert all(torch.equal(a, b) and a is not b for a, b in zip(bag.cores(), bag2.cores()))
+
+
+@pytest.mark.parametrize("x,w,groups", [((1, 2 ** 32 + 16), (8, 2 ** 32 + 16), 0), ((1, 8), (2 ** 32 + 16, 8), 0), ((4, 8), (2 ** 32 + 1, 1, 8), 2 ** 32 + 1),
+                                        ((1, 2 ** 31 + 8), (4, 2 ** 31 + 8), 0)])
+def test_sizes_past_32_bits_are_refused(tt, monkeypatch, x, w, groups):
+    """Sizes go to the library in 32 bits: larger ones must not arrive there as what is left of them (tensors without memory)."""
+    from paper_2507_14668_amd import binding
+    monkeypatch.setattr(binding, "_index", lambda t, name, dtype, at: 0)
+    make = lambda shape: torch.empty(shape, dtype=torch.bfloat16, device="meta")
+    off = torch.empty(groups + 1, dtype=torch.int64, device="meta") if groups else None
+    with pytest.raises(binding.TTError) as e:
+        binding._dense_op(make(x), make(w), "none", off)
+    assert e.value.status == binding.TT_ERR_SHAPE

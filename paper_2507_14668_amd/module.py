@@ -270,7 +270,7 @@ class TTEmbeddingBag(torch.nn.Module):
     def extra_repr(self) -> str:
         return "%d x %d, n=%s, d=%s, ranks=%s, %.1fx smaller than dense%s" % (
             self.num_embeddings, self.embedding_dim, self.n, self.d, self.r[1:3],
-            self.num_embeddings * self.embedding_dim / float(sum(p.numel() for p in self.parameters())),
+            self.num_embeddings * self.embedding_dim / float(sum(c.numel() for c in self.cores())),
             ", fused SGD lr=%g" % self.fused_sgd_lr if self.fused_sgd_lr is not None else "")
 
     @staticmethod

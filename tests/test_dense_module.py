@@ -175,3 +175,9 @@ def test_sizes_past_32_bits_are_refused(tt, monkeypatch, x, w, groups):
     with pytest.raises(binding.TTError) as e:
         binding._dense_op(make(x), make(w), "none", off)
     assert e.value.status == binding.TT_ERR_SHAPE
+
+
+def test_compression_ratio_is_the_cores(tt):
+    make = lambda **kw: tt.TTEmbeddingBag(1000, 16, n=(10, 10, 10), d=(2, 2, 4), ranks=(4, 4), device="cpu", **kw)
+    ratio = "%.1fx smaller than dense" % (1000 * 16 / (10 * 2 * 4 + 4 * 10 * 2 * 4 + 4 * 10 * 4))
+    assert ratio in repr(make()) and ratio in repr(make(projection=512))

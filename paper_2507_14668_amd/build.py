@@ -41,7 +41,7 @@ def build(verbose: bool = False) -> str:
     with tempfile.TemporaryDirectory() as tmp:
         jobs = [(src, os.path.join(tmp, os.path.basename(src) + ".o")) for src in sources()]
         compile_flags = [f for f in HIPCC_FLAGS if f != "-shared"]
-        workers = int(os.environ.get("MAX_JOBS", "0")) or min(8, os.cpu_count() or 1)
+        workers = int(os.environ.get("MAX_JOBS") or 0) or min(8, os.cpu_count() or 1)
         with ThreadPoolExecutor(max_workers=workers) as pool:
             list(pool.map(lambda job: run([hipcc] + compile_flags + include + ["-c", job[0], "-o", job[1]]), jobs))
         run([hipcc, "-shared", "-fPIC", "--offload-arch=gfx950", "-o", LIB] + [obj for _, obj in jobs])

@@ -128,3 +128,59 @@ def test_gelu_of_16_bits_over_its_tail(tt, dtype):
     want = phi + z64 * bell
     got = tt.tt_dense_backward(x, one, torch.ones_like(x), x, "gelu", needs=(True, False, False))[0]
     ref.check(got.cpu()[:, 0], want, near * (phi + z64.abs() * bell) + ref.rounding(want, dtype), "slope")
+
+
+@pytest.mark.parametrize("rows,k,n", [(8, 64, 96), (300, 256, 512), (60, 5000, 70), (2000, 96, 2100)])
+def test_float32_overflows_to_infinity(tt, rows, k, n):
+    """Positive terms only: a sum clearly past the range is an infinity (no NaN, no number), one clearly within it is a number."""
+    x, w = normal(rows, k, seed=1).abs() + 0.1, normal(n, k, seed=2).abs() + 0.1
+    size = x.double() @ w.double().t()
+    x = x * float(3.4028e38 / size.median())  # half of the results are past the range
+    want = x.double() @ w.double().t()
+    for act in ("none", "relu"):
+        got = tt.tt_dense_forward(x.cuda(), w.cuda(), activation=act).cpu()
+        margin = 2 * (k + 2) * ref.U
+        over, within = want > 3.4028236e38 * (1 + margin), want < 3.4028234e38 * (1 - margin)
+        assert int(over.sum()) > rows * n // 4 and bool((got[over] == math.inf).all())
+        ref.check(got[within], want[within], margin * want[within], act)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16, torch.float16], ids=str)
+@pytest.mark.parametrize("groups", [None, 3])
+@pytest.mark.parametrize("scale", [1e-9, 1.0, 1e5])
+def test_optimizer_steps_at_any_scale(tt, dtype, groups, scale):
+    """Momenta far below and above the range of half precision: the step is that of 64 bits, rounded to the parameter's type once."""
+    layer = tt.TTDense(24, 16, groups=groups, dtype=dtype, generator=torch.Generator(device="cuda").manual_seed(0))
+    opt = tt.TTOrthoSGD(layer, lr=0.01, momentum=0.95, eps=0.0)
+    want = []
+    for i, p in enumerate((layer.weight, layer.bias)):
+        m, g = normal(*p.shape, seed=i, std=scale), normal(*p.shape, seed=9 + i, std=min(scale, 1e3)).to(dtype)
+        opt.state[p]["momentum"], p.grad = m.cuda(), g.cuda()
+        m64 = 0.95 * m.double() + g.double()
+        u = g.double() + 0.95 * m64
+        if p is layer.weight:
+            u = ref.ortho(u.reshape((-1,) + u.shape[-2:]), eps=0.0).reshape(u.shape)
+        want.append((p.detach().cpu().double() - 0.01 * u, m64))
+    opt.step()
+    for p, (new, m) in zip((layer.weight, layer.bias), want):
+        fine = torch.isfinite(new.to(dtype))
+        assert torch.equal(torch.isfinite(p.detach().cpu()), fine)
+        # half a step of the type, and the step itself in fp32: its singular values are near one, and errors of 2^-22 of u are taken 485 times at most
+        off = 485 * 2.0 ** -22 * 0.01 if p is layer.weight else 2.0 ** -21 * 0.01 * float(m.abs().max()) * 2
+        ref.check(p.detach().cpu()[fine], new[fine], ref.rounding(new, dtype)[fine] + off, "parameter")
+        ref.check(opt.state[p]["momentum"].cpu(), m, 2.0 ** -22 * m.abs().max().expand(m.shape), "momentum")
+
+
+def test_frozen_core_on_the_gpu(tt):
+    """A table whose middle core is frozen trains the other two as it would beside a trained one."""
+    bags = [tt.TTEmbeddingBag(24, 16, n=(2, 3, 4), d=(2, 2, 4), ranks=(4, 3), generator=torch.Generator(device="cuda").manual_seed(0)) for _ in range(2)]
+    bags[0].core1.requires_grad_(False)
+    idx, off = torch.arange(24, device="cuda"), torch.arange(0, 24, 3, device="cuda")
+    start = [c.detach().clone() for c in bags[0].cores()]
+    for bag in bags:
+        opt = tt.TTOrthoSGD(bag, lr=0.01)
+        bag(idx, off).square().sum().backward()
+        opt.step()
+    assert bags[0].core1.grad is None and torch.equal(bags[0].core1, start[1]) and not torch.equal(bags[1].core1, start[1])
+    for k in (0, 2):
+        assert torch.equal(bags[0].cores()[k], bags[1].cores()[k]) and not torch.equal(bags[0].cores()[k], start[k])

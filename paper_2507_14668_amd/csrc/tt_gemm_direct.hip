@@ -217,11 +217,12 @@ template <class T, bool AKC, bool BKC> __global__ void __launch_bounds__(THREADS
   if constexpr (!AKC) {
     if (sums) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        odd |= lane < 32 && !(fabsf(rs[i]) < INFINITY);
-        if (lane < 32) give_sum(w.lo + wm + 16 * (4 * (lane >> 4) + i) + (lane & 15), rs[i]);
-      }
+      for (int i = 0; i < 4; ++i) odd |= lane < 32 && !(fabsf(rs[i]) < INFINITY);
       odd = __ballot(odd) != 0;
+      if (!odd && lane < 32) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) give_sum(w.lo + wm + 16 * (4 * (lane >> 4) + i) + (lane & 15), rs[i]);
+      }
     }
   }
   __syncthreads();  // nobody reads the operands any more

@@ -176,7 +176,16 @@ class TTDense(torch.nn.Module):
         return "%d -> %d%s, %s" % (self.in_features, self.out_features, "" if self.groups is None else ", %d groups" % self.groups, self.activation)
 
 
-class TTEmbeddingBag(torch.nn.Module):
+class _Projected(torch.nn.Module):
+    """A module that may have a `projection`; one that was pickled before there were any has none."""
+
+    def __setstate__(self, state):
+        super().__setstate__(state)
+        if "projection" not in self.__dict__ and "projection" not in self._modules:
+            self.projection = None
+
+
+class TTEmbeddingBag(_Projected):
     """Sum-pooling embedding bag whose table of `num_embeddings x embedding_dim` is held as three
     TT cores `G_k[r_k][n_k][d_k][r_{k+1}]` (flat float32 parameters `core0..core2`).
 
@@ -286,7 +295,7 @@ class TTEmbeddingBag(torch.nn.Module):
         return (n1, n2, n3)
 
 
-class TTFusedEmbeddingBags(torch.nn.Module):
+class TTFusedEmbeddingBags(_Projected):
     """Several sum-pooling embedding bags of one embedding_dim, one set of column factors `d` and one
     pair of ranks, held as ONE fused TT table: core k is `[r_k][sum of the tables' n_k][d_k][r_k+1]`
     and table t owns a range of the middle axis of every core.  A row of table t is the product of

@@ -181,3 +181,18 @@ def test_compression_ratio_is_the_cores(tt):
     make = lambda **kw: tt.TTEmbeddingBag(1000, 16, n=(10, 10, 10), d=(2, 2, 4), ranks=(4, 4), device="cpu", **kw)
     ratio = "%.1fx smaller than dense" % (1000 * 16 / (10 * 2 * 4 + 4 * 10 * 2 * 4 + 4 * 10 * 4))
     assert ratio in repr(make()) and ratio in repr(make(projection=512))
+
+
+@pytest.mark.parametrize("projection", [None, 12])
+def test_modules_pickled_without_a_projection(tt, projection):
+    """A module whose pickle knows of no projection has none; others keep theirs."""
+    fused = tt.TTFusedEmbeddingBags([(24, (2, 3, 4)), (6, (1, 2, 3))], 16, (2, 2, 4), (4, 3), device="cpu", projection=projection)
+    bag = tt.TTEmbeddingBag(24, 16, n=(2, 3, 4), d=(2, 2, 4), ranks=(4, 3), device="cpu", projection=projection)
+    for m in (bag, fused):
+        state = dict(m.__dict__)
+        if projection is None:
+            del state["projection"]
+        again = type(m).__new__(type(m))
+        again.__setstate__(state)
+        assert again.projection is m.projection
+        assert torch.equal(copy.deepcopy(m).core0, m.core0)

@@ -513,7 +513,8 @@ tt_status tt_orthogonalize(const tt_matrices *m, const void *g, void *out, int s
  *   m <- mu m + dG,  u = nesterov ? dG + mu m : m,
  *   G <- G - lr sqrt(max(1, rows / cols)) ortho(u)   for each slice G of each core,
  * the slices being the matrices that multiply in a row of the table: G1[i1] d1 x R1, G2[i2] R1 x (d2 R2),
- * G3[i3] R2 x d3.  A slice whose u is zero stays as it is.  table->core[] and momentum[] are updated in place.
+ * G3[i3] R2 x d3.  A slice whose u is zero stays as it is (eps > 0; else it
+ * becomes NaN).  table->core[] and momentum[] are updated in place.
  *   dcore, momentum  HOST arrays of 3 DEVICE pointers, core-shaped
  *   workspace        DEVICE, 256-byte aligned, tt_core_ortho_workspace_bytes(table) (0 on invalid arguments)
  */

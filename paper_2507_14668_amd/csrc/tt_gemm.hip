@@ -206,9 +206,9 @@ template <bool KC, int LD32> __device__ __forceinline__ f32x4 frag32(const float
 // infinities, NaN and numbers that round to a bf16 infinity give NaN sums, products below 2^-92 lose parts to underflow, and so do
 // numbers below 2^-100 by themselves.  A tile with a sum that is not finite, or with one so small that such a loss would
 // count beside operands that have it, is done again with the fp32 instruction.  (P = 2 is for operands that are scaled to at most one, with no such products that count.)
-// Measured: fp32 4096 x 4096 x 1024 198 us (174 TFLOP/s, 1040 of bf16 products; the fp32 instruction's rate is 154), 106496 x 128 x 128 40 us (22 by
-// its bytes); two parts 2048 x 4096 x 2048 106 us (975 of bf16 products).  Without the matrix instructions the first takes 169, without the split
-// of P = 2 the last 93: splitting, LDS and barriers bound it.  Loads two or four steps ahead in registers, and two buffers for P = 2, are no faster.
+// Measured: fp32 4096 x 4096 x 1024 188 us (183 TFLOP/s, 1100 of bf16 products; the fp32 instruction's rate is 154), 106496 x 128 x 128 39 us (22 by
+// its bytes), 2 % of both for the largest number; two parts 2048 x 4096 x 2048 106 us (975 of bf16 products).  Without the matrix instructions the first took 169 of 198,
+// without the split of P = 2 the last 93 of 106: splitting, LDS and barriers bound it.  Loads two or four steps ahead in registers, and two buffers for P = 2, are no faster.
 template <class T, class O, int P, bool AKC, bool BKC, int E>
 __global__ void __launch_bounds__(TT_BLOCK, 2) k_gemm(TTGemm g, int m_tiles, int n_tiles, int split, int chunk, float *partial) {
   typedef Carrier<T, AKC, E> CA;

@@ -79,8 +79,9 @@ __global__ void __launch_bounds__(TT_BLOCK) k_scale_in(const T *__restrict__ g, 
 
 // The three products of a step, without their operands' addresses.  For results in 16 bits two bf16 parts of each operand are
 // multiplied (16 bits of significand: five steps take errors up 485 times at most, in a few directions), for fp32 three.  A and B are
-// symmetric: the tiles on one side of the diagonal are computed.  Measured, 4096 x 2048 bf16: 1.30 ms, a step 84 + 14 us for A, 46 + 14 for B, 115
-// for X (900 to 980 TFLOP/s of bf16 products); 512 x 128 fp32: 153 us, bound by four launches a step of 3 to 8 us.
+// symmetric: the tiles on one side of the diagonal are computed.  Measured, 4096 x 2048 bf16: 1.27 ms a
+// call among others; under the profiler, where launches do not follow each other closely, 1.40 ms: norm and scaling 35 us, a step 83 + 15 for A, 46 + 15 for B,
+// 115 for X (900 to 980 TFLOP/s of bf16 products).  512 x 128 fp32: 158 us, bound by four launches a step of 4 to 10 us.
 struct Products {
   TTGemm gram, square, move;
 };

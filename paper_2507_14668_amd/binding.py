@@ -608,6 +608,7 @@ def fusion_groups(members, groups=None, max_factor_sum=1023):
 # ------------------------------------------------------------------ dense side
 DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "silu": 3, "sigmoid": 4}
+TT_ORTHO_MAX_STEPS = 32
 # the Muon optimiser's coefficients (K. Jordan and others, 2024): steep at zero, so that five steps do
 ORTHO_COEFFICIENTS = (3.4445, -4.7750, 2.0315)
 
@@ -773,10 +774,12 @@ def tt_dense_backward(x, w, grad_out, pre=None, activation="none", offsets=None,
 
 def _coefficients(steps, coefficients):
     steps = int(steps)
+    if not 1 <= steps <= TT_ORTHO_MAX_STEPS:
+        raise ValueError("steps: 1 to %d" % TT_ORTHO_MAX_STEPS)
     c = [float(v) for row in coefficients for v in (row if isinstance(row, (tuple, list)) else (row,))]
     if len(c) == 3:
         c = c * steps
-    if steps < 1 or len(c) != 3 * steps:
+    if len(c) != 3 * steps:
         raise ValueError("coefficients: one (a, b, c) for all steps, or one for each")
     return (ctypes.c_float * len(c))(*c)
 

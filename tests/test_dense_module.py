@@ -196,3 +196,16 @@ def test_modules_pickled_without_a_projection(tt, projection):
         again.__setstate__(state)
         assert again.projection is m.projection
         assert torch.equal(copy.deepcopy(m).core0, m.core0)
+
+
+def test_steps_are_checked_before_coefficients_are_laid_out(tt):
+    """A number of steps that the library would refuse is refused before a list of that length is made."""
+    import os
+    import re
+    from paper_2507_14668_amd import binding
+    header = open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "tt_emb.h")).read()
+    assert binding.TT_ORTHO_MAX_STEPS == int(re.search(r"#define TT_ORTHO_MAX_STEPS (\d+)", header).group(1))
+    assert len(binding._coefficients(32, (1, 2, 3))) == 96
+    for steps in (0, -1, 33, 10 ** 6):
+        with pytest.raises(ValueError):
+            binding._coefficients(steps, (1, 2, 3))

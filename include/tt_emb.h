@@ -466,7 +466,7 @@ typedef struct {
  * Forward.  bias and residual may be NULL.  pre (nullable) receives z, [rows][out_dim] packed, rounded to
  * the dtype (in fp16 a z that would round to zero keeps its sign as the smallest number): what
  * tt_dense_backward needs if there is an activation.  out may be the residual's own memory with the same
- * row step; otherwise outputs overlap nothing.  Tensors need the alignment of an element only.
+ * row step; otherwise outputs overlap nothing (TT_ERR_INVALID_ARG where one starts where another tensor does).  Tensors need the alignment of an element only.
  *   workspace  DEVICE, 256-byte aligned, tt_dense_workspace_bytes(op, 0) bytes (NULL if that is 0), borrowed
  *              until the work has finished: calls that may overlap need one each.
  * Backward, from grad_out = dL/d out:

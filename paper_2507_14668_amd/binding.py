@@ -717,7 +717,7 @@ def tt_dense_forward(x, w, bias=None, residual=None, activation="none", offsets=
     """`act(x w^T + bias) + residual`, of x [rows, in] and w [out, in]; with `offsets` (int64 [groups + 1], on the device) of w
     [groups, out, in] and bias [groups, out], group g's for the rows offsets[g] .. offsets[g + 1].  One dtype throughout (float32,
     bfloat16 or float16); x, residual and out may be views into wider rows.  `pre` (packed, [rows, out]) receives the
-    pre-activation that `tt_dense_backward` takes.  Rows of no group are left as they were in a given `out`, zeros in a new one."""
+    pre-activation that `tt_dense_backward` takes.  `out` may be the residual and overlaps nothing else.  Rows of no group are left as they were in a given `out`, zeros in a new one."""
     op, at = _dense_op(x, w, activation, offsets)
     rows, n, dtype = op.rows, op.out_dim, x.dtype
     on = _On(at, stream)

@@ -145,6 +145,9 @@ extern "C" tt_status tt_dense_forward(const tt_dense *op, const void *x, const v
   if (!aligned(x, op->dtype) || !aligned(w, op->dtype) || !aligned(bias, op->dtype) || !aligned(residual, op->dtype) || !aligned(out, op->dtype) ||
       !aligned(pre, op->dtype))
     return TT_ERR_INVALID_ARG;
+  // outputs over inputs that other workgroups still read; a residual that shares out's memory is read where it is written
+  if (out == x || out == w || out == bias || (pre && (pre == x || pre == w || pre == bias || pre == residual || pre == out))) return TT_ERR_INVALID_ARG;
+  if (out == residual && op->rows > 1 && step(op->ld_out, op->out_dim) != step(op->ld_residual, op->out_dim)) return TT_ERR_INVALID_ARG;
   const Scratch need = scratch(op, false);
   if (need.total && (!workspace || ((uintptr_t)workspace & 255) != 0 || workspace_bytes < need.total)) return TT_ERR_WORKSPACE;
   TTGemm g = of_out(op);
@@ -161,8 +164,11 @@ extern "C" tt_status tt_dense_backward(const tt_dense *op, const void *x, const 
   if (!dx && !dw && !dbias) return TT_OK;
   if (some && (!grad_out || (dw && !x) || (dx && !w) || (bent && !pre))) return TT_ERR_INVALID_ARG;
   const void *ptrs[7] = {x, w, pre, grad_out, dx, dw, dbias};
-  for (int i = 0; i < 7; ++i)
+  for (int i = 0; i < 7; ++i) {
     if (!aligned(ptrs[i], op->dtype)) return TT_ERR_INVALID_ARG;
+    for (int j = 4; j < 7; ++j)  // outputs over inputs
+      if (i < 4 && ptrs[j] && ptrs[i] == ptrs[j]) return TT_ERR_INVALID_ARG;
+  }
   const Scratch need = scratch(op, true);
   if (!workspace || ((uintptr_t)workspace & 255) != 0 || workspace_bytes < need.total) return TT_ERR_WORKSPACE;
   hipStream_t s = (hipStream_t)stream;

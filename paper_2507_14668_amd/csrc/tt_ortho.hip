@@ -283,6 +283,7 @@ extern "C" tt_status tt_orthogonalize(const tt_matrices *m, const void *g, void 
   in.b_step = m->batch_step ? m->batch_step : in.r_step * m->rows;
   const long long ldo = m->out_row_step ? m->out_row_step : m->cols, o_step = m->out_batch_step ? m->out_batch_step : ldo * m->rows;
   if (in.r_step < m->cols || ldo < m->cols || in.b_step < 0 || o_step < ldo * (m->rows - 1) + m->cols) return TT_ERR_SHAPE;
+  if (g == out && ((m->rows > 1 && in.r_step != ldo) || (m->batch > 1 && in.b_step != o_step))) return TT_ERR_INVALID_ARG;  // in place, from other places
   const Scratch w = scratch(m->batch, m->rows, m->cols, m->dtype);
   if (!workspace || ((uintptr_t)workspace & 255) != 0 || workspace_bytes < w.total) return TT_ERR_WORKSPACE;
   hipStream_t s = (hipStream_t)stream;

@@ -495,3 +495,28 @@ def test_gelu_of_16_bits_over_its_tail(lib, dtype):
     assert lib.tt_dense_backward(ctypes.byref(op), gx.ptr, gw.ptr, gx.ptr, one.ptr, dx.ptr, None, None, ws.ptr, need, None) == 0
     want = phi + z64 * bell
     ref.check(dx.t[:, 0], want, near * (phi + z64.abs() * bell) + ref.rounding(want, dtype), "slope")
+
+
+def test_outputs_over_inputs_are_refused(lib):
+    """Workgroups read what others have written by then: no output starts where an input does, but for the residual's own rows."""
+    from paper_2507_14668_amd import binding
+    x, w, bias, res, _ = make(4, 4, 4, torch.float32)
+    gx, gw, gb, gr, out, pre, ws = place(x), place(w), place(bias), place(res), Guarded((4, 4), torch.float32), Guarded((4, 4), torch.float32), Guarded((1, 8192), torch.uint8)
+    f = lambda op, out, pre=None, res=gr.ptr: lib.tt_dense_forward(ctypes.byref(op), gx.ptr, gw.ptr, gb.ptr, res, out, pre, ws.ptr, 8192, None)
+    op = dense_op(x, w, "relu", None)
+    bad = binding.TT_ERR_INVALID_ARG
+    assert [f(op, o.ptr) for o in (gx, gw, gb)] == [bad] * 3 and [f(op, out.ptr, p.ptr) for p in (gx, gw, gb, gr, out)] == [bad] * 5
+    assert f(op, gr.ptr, pre.ptr) == 0 and f(op, out.ptr) == 0 and f(op, out.ptr, pre.ptr, None) == 0
+    assert f(dense_op(x, w, "relu", None, ld_out=8, ld_residual=4), gr.ptr) == bad
+    gg = place(res)
+    b = lambda dx, dw, db: lib.tt_dense_backward(ctypes.byref(op), gx.ptr, gw.ptr, pre.ptr, gg.ptr, dx, dw, db, ws.ptr, 8192, None)
+    for t in (gx, gw, pre, gg):
+        assert b(t.ptr, None, None) == bad and b(None, t.ptr, None) == bad and b(None, None, t.ptr) == bad
+    assert b(out.ptr, None, None) == 0
+    g = torch.randn(2, 4, 4)
+    src, c = place(g), coefs(*(3.4445, -4.7750, 2.0315) * 5)
+    ortho = lambda m: lib.tt_orthogonalize(ctypes.byref(m), src.ptr, src.ptr, 5, c, 1e-7, ws.ptr, 8192, None)
+    assert ortho(matrices(g, batch=1, row_step=8)) == bad and ortho(matrices(g, batch_step=8, out_batch_step=16, row_step=4)) == bad
+    assert ortho(matrices(g)) == 0
+    for t in (gx, gw, gb, gr, out, pre, ws, gg, src):
+        assert t.intact()

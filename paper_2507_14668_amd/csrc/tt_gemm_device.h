@@ -354,7 +354,9 @@ __device__ __forceinline__ double wave_sum64(double v) {
 // the two rows; squares_a and squares_b are theirs): as errors of either sign they come to sqrt(K) 2^-24 |a| |b|.  Below four times
 // that v is formed again; measured errors of random operands are a thousandth of it.  (Operands beyond 2^+-60, whose squares leave the range,
 // have all results formed again, or keep the sign that they have.)  At K = 128 one result in 40000, at 4096 one in 1200.
-// 16384 x 128 -> 512 takes 26.9 us with relu, 24.8 without; 4096 x 4096 -> 1024 214 and 188.
+// 16384 x 128 -> 512 takes 26.9 us with relu, 24.8 without; 4096 x 4096 -> 1024 214 and 188.  Data of few values, whose sums cancel exactly, have
+// more of them at a microsecond each: 0 and 1 by -1 and 1, 5 % of the first product's results, 222 us.  Four at a time by 16 lanes each take 107 there, but the
+// products above 28.6 and 251.
 // All lanes of the wavefront call it, with one z; `valid` <= 0: a lane without results.
 template <int C>
 __device__ __forceinline__ void settle_signs(const TTGemm &g, int z, int m, int n, int valid, float v[C], const float bias[C], float squares_a,

@@ -524,6 +524,147 @@ tt_status tt_core_ortho_update(const tt_table *table, const float *const dcore[3
                                void *workspace, size_t workspace_bytes, void *stream);
 
 /*
+ * The top of a model.  Layer norm, a router that deals rows to experts, and the softmax loss over a
+ * catalogue.  fp32, bf16 or fp16 data with fp32 arithmetic (64 bits where said), rounded once; reproducible, no
+ * floating-point atomics; nothing is allocated.  Tensors need the alignment of an element only; outputs
+ * overlap nothing (TT_ERR_INVALID_ARG where one starts where another tensor of the call does).
+ *
+ * Layer norm of each row of x [rows][dim], mean and variance (of dim, not dim - 1) over the row:
+ *   y = (x - mean) rstd weight + bias,  rstd = 1 / sqrt(variance + eps)
+ * weight and bias [dim] may be NULL (one and zero).  Backward, with h = grad weight and x^ = (x - mean) rstd:
+ *   dx = rstd (h - mean(h) - x^ mean(h x^)),  dweight = sum over rows of grad x^,  dbias = sum of grad
+ * A row of equal values has rstd = 1 / sqrt(eps) (infinite if eps is 0); infinities and NaN stay in their
+ * row of out and dx.
+ *   stats      DEVICE float[rows][2]: mean and rstd, written by the forward (may be NULL), read by the backward
+ *   workspace  DEVICE, 256-byte aligned, tt_layer_norm_workspace_bytes(op) bytes; only for dweight and dbias
+ */
+#define TT_NORM_MAX_DIM (1 << 20)
+typedef struct {
+  int32_t dtype;  /* tt_dtype of every tensor but stats                                         */
+  int32_t dim;    /* 1 .. TT_NORM_MAX_DIM                                                       */
+  int64_t rows;   /* fewer than 2^31 - 1                                                        */
+  int64_t ld_x;   /* elements between rows of x; 0: dim                                         */
+  int64_t ld_out; /* ... of out; 0: dim                                                         */
+  int64_t ld_grad; /* ... of grad_out; 0: dim                                                   */
+  int64_t ld_dx;  /* ... of dx; 0: dim                                                          */
+  float eps;      /* >= 0                                                                       */
+} tt_norm;
+size_t tt_layer_norm_workspace_bytes(const tt_norm *op);
+tt_status tt_layer_norm_forward(const tt_norm *op, const void *x, const void *weight, const void *bias, void *out, float *stats, void *stream);
+tt_status tt_layer_norm_backward(const tt_norm *op, const void *x, const void *weight, const float *stats, const void *grad_out,
+                                 void *dx, void *dweight, void *dbias, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Routing.  For each row of logits z [rows][experts]:
+ *   s = softmax(z), or sigmoid of each z;  c = s + bias[e] (bias chooses only, it is not in the weights)
+ *   groups > 1: the experts are `groups` equal runs; the top_groups with the largest sum of their two best c
+ *     (one, where a group has one) stay
+ *   the `choices` experts with the largest c, largest first; equal ones by number, lowest first
+ *   weights[j] = scale s, divided by the sum of the row's chosen s if renormalize (0 if that sum is 0)
+ * Scores and comparisons are in 64 bits: which experts a row gets does not hang on rounding.  An expert whose
+ * logit or c is -infinity is masked: never chosen, and no group's strength.  Where fewer than `choices` are left the numbers
+ * are -1 and the weights 0 (a row of -infinity, as padding has, goes nowhere).  A NaN counts as the
+ * largest (so it shows in the weights); a logit of +infinity makes a softmax row NaN.
+ * Backward: from grad_weights the gradient of the logits through the weights (s only; numbers are fixed).
+ *   experts DEVICE int64[rows][choices]; weights, grad_weights float[rows][choices]; bias float[experts], nullable
+ */
+#define TT_ROUTE_MAX_EXPERTS 1024
+#define TT_ROUTE_MAX_CHOICES 64
+#define TT_ROUTE_MAX_GROUPS 64
+typedef enum { TT_SCORES_SOFTMAX = 0, TT_SCORES_SIGMOID = 1 } tt_scores;
+typedef struct {
+  int32_t dtype;       /* tt_dtype of logits and dlogits                                         */
+  int32_t scores;      /* tt_scores                                                              */
+  int64_t rows;        /* rows * choices fewer than 2^31 - 2^16 - 1                              */
+  int32_t experts;     /* 1 .. TT_ROUTE_MAX_EXPERTS                                              */
+  int32_t choices;     /* 1 .. min(TT_ROUTE_MAX_CHOICES, experts of top_groups groups)           */
+  int32_t groups;      /* 1 .. TT_ROUTE_MAX_GROUPS, a divisor of experts                         */
+  int32_t top_groups;  /* 1 .. groups                                                            */
+  int32_t renormalize; /* 0 or 1                                                                 */
+  float scale;         /* finite                                                                 */
+  int64_t ld_logits;   /* elements between rows of logits; 0: experts                            */
+  int64_t ld_dlogits;  /* ... of dlogits; 0: experts                                             */
+} tt_route;
+tt_status tt_route_forward(const tt_route *op, const void *logits, const float *bias, int64_t *experts, float *weights, void *stream);
+tt_status tt_route_backward(const tt_route *op, const void *logits, const int64_t *experts, const float *grad_weights, void *dlogits,
+                            void *stream);
+
+/*
+ * The experts' order of n choices (the numbers above, row after row): the choices of one expert stand next to
+ * each other, in the order in which they come.  Numbers outside [0, num_experts) go nowhere.
+ *   offsets DEVICE int64[num_experts + 1]: each expert's first place, and the end (what tt_dense takes)
+ *   slots   DEVICE int32[n]: each choice's place, -1 for none
+ *   sources DEVICE int32[n]: each place's choice, -1 for places behind the end
+ *   workspace DEVICE, 256-byte aligned, tt_expert_order_workspace_bytes(n, num_experts) (0: none needed, or invalid)
+ */
+size_t tt_expert_order_workspace_bytes(int64_t n, int32_t num_experts);
+tt_status tt_expert_order(const int64_t *experts, int64_t n, int32_t num_experts, int64_t *offsets, int32_t *slots, int32_t *sources,
+                          void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Rows to their experts and back.  slots [rows][choices] and sources [rows * choices] as above; places outside
+ * [0, rows * choices) count as none.
+ *   tt_expert_rows:     out[slots[r][j]] = x[r];  places without a source: left as they were, zeros with zero_rest
+ *   tt_expert_combine:  out[r] = residual[r] + sum over j of weights[r][j] y[slots[r][j]]   (weights NULL: ones; what a
+ *                       choice without a place would weigh is left out).  Also the gradient of tt_expert_rows.
+ *   tt_expert_combine_backward:  dy[slots[r][j]] = weights[r][j] grad[r], zeros in places without a source;
+ *                       dweights[r][j] = <grad[r], y[slots[r][j]]>, 0 without a place.  dy or dweights may be NULL.
+ *                       The residual's gradient is grad itself.
+ * out may be the residual's own memory with the same row step.
+ */
+typedef struct {
+  int32_t dtype;       /* tt_dtype of the rows; weights are float                                */
+  int32_t dim;         /* columns, 1 .. TT_NORM_MAX_DIM                                          */
+  int64_t rows;        /* of x, and of combine's out and grad; rows * choices as in tt_route     */
+  int32_t choices;     /* 1 .. TT_ROUTE_MAX_CHOICES                                              */
+  int32_t zero_rest;
+  int64_t ld_rows;     /* elements between rows of x, of combine's out and of grad; 0: dim       */
+  int64_t ld_residual; /* ... of residual; 0: dim                                                */
+  int64_t ld_places;   /* ... of tt_expert_rows' out and of y; 0: dim                            */
+  int64_t ld_dy;       /* ... of dy; 0: dim                                                      */
+} tt_deal;
+tt_status tt_expert_rows(const tt_deal *op, const void *x, const int32_t *slots, const int32_t *sources, void *out, void *stream);
+tt_status tt_expert_combine(const tt_deal *op, const void *y, const int32_t *slots, const float *weights, const void *residual, void *out,
+                            void *stream);
+tt_status tt_expert_combine_backward(const tt_deal *op, const void *y, const int32_t *slots, const int32_t *sources, const float *weights,
+                                     const void *grad, void *dy, float *dweights, void *stream);
+
+/*
+ * Softmax cross entropy of rows against a catalogue of classes, without keeping the logits:
+ *   z = x W^T + bias,  loss[r] = log(sum over classes of exp(z[r])) - z[r][label[r]]     x [rows][dim], W [classes][dim]
+ * Rows whose label is ignore_index count for nothing: their loss and gradients are zero, whatever x holds
+ * there.  A label that is neither that nor in [0, classes) gives a loss of NaN, and gradients with it.  A class whose bias is -infinity
+ * is left out; a row with a logit of NaN or +infinity, or without a class, has the loss NaN.
+ *   loss: TT_REDUCE_NONE float[rows]; TT_REDUCE_SUM, TT_REDUCE_MEAN float[1], the mean over the rows that count (0 if
+ *     there are none)
+ * Backward, from grad_loss (float[rows], or float[1]): with G = (softmax(z) - onehot(label)) times the row's share of it
+ *   dx = G W,  dW = G^T x,  dbias = sums of G's columns;  any of dx, dw, dbias may be NULL.
+ * G is formed again, a piece of the classes at a time, and rounded to the dtype before the products (fp16: scaled by a power of two
+ * so that its largest gradient is near the top of the range, in and out of the products).  Losses and lse are float whatever the dtype.
+ *   labels DEVICE int64[rows];  lse DEVICE float[rows]: log of the sum, 0 in rows that do not count; written by the
+ *   forward (not NULL), read by the backward
+ *   workspace DEVICE, 256-byte aligned, tt_cross_entropy_workspace_bytes(op, backward) (0 on invalid arguments)
+ */
+typedef enum { TT_REDUCE_NONE = 0, TT_REDUCE_SUM = 1, TT_REDUCE_MEAN = 2 } tt_reduce;
+#define TT_LOSS_MAX_CLASSES (1 << 30)
+typedef struct {
+  int32_t dtype;        /* tt_dtype of x, w, bias and their gradients                            */
+  int32_t reduce;       /* tt_reduce                                                             */
+  int64_t rows;         /* fewer than 2^31 - 2^16 - 1                                            */
+  int32_t dim;          /* 1 .. TT_DENSE_MAX_DIM                                                 */
+  int32_t classes;      /* 1 .. TT_LOSS_MAX_CLASSES                                              */
+  int64_t ignore_index;
+  int64_t ld_x;         /* elements between rows of x; 0: dim                                    */
+  int64_t ld_dx;        /* ... of dx; 0: dim                                                     */
+} tt_loss;
+size_t tt_cross_entropy_workspace_bytes(const tt_loss *op, int backward);
+tt_status tt_cross_entropy_forward(const tt_loss *op, const void *x, const void *w, const void *bias, const int64_t *labels, float *loss, float *lse,
+                                   void *workspace, size_t workspace_bytes, void *stream);
+tt_status tt_cross_entropy_backward(const tt_loss *op, const void *x, const void *w, const void *bias, const int64_t *labels, const float *lse,
+                                    const float *grad_loss, void *dx, void *dw, void *dbias, void *workspace, size_t workspace_bytes,
+                                    void *stream);
+
+/*
  * Waits for `stream`, copies the plan's device-side counters to the host and
  * reports deferred errors.  counts_out (HOST, nullable) receives
  * {U_r, U_p, valid lookups, status bits}.  Returns TT_ERR_INDEX_RANGE if any

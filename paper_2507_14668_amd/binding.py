@@ -31,7 +31,10 @@ EXPORTS = ("tt_workspace_bytes", "tt_index_reorder", "tt_emb_bag_forward", "tt_e
            "tt_prof_collect", "tt_kernel_name", "tt_batch_desc_bytes", "tt_index_reorder_batched",
            "tt_emb_bag_forward_batched", "tt_emb_bag_backward_batched", "tt_core_sgd_update_batched",
            "tt_dense_workspace_bytes", "tt_dense_forward", "tt_dense_backward", "tt_orthogonalize_workspace_bytes", "tt_orthogonalize",
-           "tt_core_ortho_workspace_bytes", "tt_core_ortho_update")
+           "tt_core_ortho_workspace_bytes", "tt_core_ortho_update",
+           "tt_layer_norm_workspace_bytes", "tt_layer_norm_forward", "tt_layer_norm_backward", "tt_route_forward", "tt_route_backward",
+           "tt_expert_order_workspace_bytes", "tt_expert_order", "tt_expert_rows", "tt_expert_combine", "tt_expert_combine_backward",
+           "tt_cross_entropy_workspace_bytes", "tt_cross_entropy_forward", "tt_cross_entropy_backward")
 KERNELS = {"fwd_contract": 0, "bag_sum": 1, "grad_merge": 2, "bwd_contract": 3, "sort_scatter": 4, "sgd": 5,
            "p12_fill": 6, "bag_chains": 7}
 
@@ -91,6 +94,28 @@ class CMatrices(ctypes.Structure):
     _fields_ = [("dtype", ctypes.c_int32), ("batch", ctypes.c_int64), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64),
                 ("batch_step", ctypes.c_int64), ("row_step", ctypes.c_int64), ("out_batch_step", ctypes.c_int64),
                 ("out_row_step", ctypes.c_int64)]
+
+
+class CNorm(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("dim", ctypes.c_int32), ("rows", ctypes.c_int64), ("ld_x", ctypes.c_int64), ("ld_out", ctypes.c_int64),
+                ("ld_grad", ctypes.c_int64), ("ld_dx", ctypes.c_int64), ("eps", ctypes.c_float)]
+
+
+class CRoute(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("scores", ctypes.c_int32), ("rows", ctypes.c_int64), ("experts", ctypes.c_int32),
+                ("choices", ctypes.c_int32), ("groups", ctypes.c_int32), ("top_groups", ctypes.c_int32), ("renormalize", ctypes.c_int32),
+                ("scale", ctypes.c_float), ("ld_logits", ctypes.c_int64), ("ld_dlogits", ctypes.c_int64)]
+
+
+class CDeal(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("dim", ctypes.c_int32), ("rows", ctypes.c_int64), ("choices", ctypes.c_int32),
+                ("zero_rest", ctypes.c_int32), ("ld_rows", ctypes.c_int64), ("ld_residual", ctypes.c_int64), ("ld_places", ctypes.c_int64),
+                ("ld_dy", ctypes.c_int64)]
+
+
+class CLoss(ctypes.Structure):
+    _fields_ = [("dtype", ctypes.c_int32), ("reduce", ctypes.c_int32), ("rows", ctypes.c_int64), ("dim", ctypes.c_int32),
+                ("classes", ctypes.c_int32), ("ignore_index", ctypes.c_int64), ("ld_x", ctypes.c_int64), ("ld_dx", ctypes.c_int64)]
 
 
 _lib = None
@@ -181,6 +206,18 @@ def load_library():
         lib.tt_core_ortho_workspace_bytes.argtypes = [vp]
         lib.tt_core_ortho_update.restype = ctypes.c_int
         lib.tt_core_ortho_update.argtypes = [vp, vp, vp, f32, f32, ctypes.c_int, ctypes.c_int, vp, f32, vp, sz, vp]
+        for name, res, args in (
+                ("tt_layer_norm_workspace_bytes", sz, [vp]), ("tt_layer_norm_forward", ctypes.c_int, [vp] * 7),
+                ("tt_layer_norm_backward", ctypes.c_int, [vp] * 9 + [sz, vp]),
+                ("tt_route_forward", ctypes.c_int, [vp] * 6), ("tt_route_backward", ctypes.c_int, [vp] * 6),
+                ("tt_expert_order_workspace_bytes", sz, [i64, ctypes.c_int32]),
+                ("tt_expert_order", ctypes.c_int, [vp, i64, ctypes.c_int32, vp, vp, vp, vp, sz, vp]),
+                ("tt_expert_rows", ctypes.c_int, [vp] * 6), ("tt_expert_combine", ctypes.c_int, [vp] * 7),
+                ("tt_expert_combine_backward", ctypes.c_int, [vp] * 9),
+                ("tt_cross_entropy_workspace_bytes", sz, [vp, ctypes.c_int]),
+                ("tt_cross_entropy_forward", ctypes.c_int, [vp] * 8 + [sz, vp]),
+                ("tt_cross_entropy_backward", ctypes.c_int, [vp] * 11 + [sz, vp])):
+            getattr(lib, name).restype, getattr(lib, name).argtypes = res, args
         _lib = lib
     return _lib
 
@@ -852,6 +889,305 @@ def tt_core_ortho_update(table: Table, dcores, momenta, lr: float, momentum=0.95
         st = lib.tt_core_ortho_update(ctypes.byref(table.c), ptrs(dcores), ptrs(momenta), ctypes.c_float(lr), ctypes.c_float(momentum), int(bool(nesterov)),
                                       int(steps), coef, eps, p_work, size, s)
     _check(st, "tt_core_ortho_update")
+
+
+# ------------------------------------------------------------------ a model's top
+SCORES = {"softmax": 0, "sigmoid": 1}
+REDUCTIONS = {"none": 0, "sum": 1, "mean": 2}
+TT_ROUTE_MAX_EXPERTS, TT_ROUTE_MAX_CHOICES, TT_ROUTE_MAX_GROUPS = 1024, 64, 64
+
+
+def _int32(v, name, where):
+    if not 0 <= v <= 0x7fffffff:  # the library's field would take it modulo 2^32
+        raise TTError(TT_ERR_SHAPE, "%s (%s)" % (where, name))
+    return v
+
+
+def _matrix(t, name):
+    """A 2-D tensor of one of the library's types; its dtype and device."""
+    if not isinstance(t, torch.Tensor) or t.dtype not in DTYPES:
+        raise TypeError("%s must be a CUDA tensor of float32, bfloat16 or float16" % name)
+    if t.dim() != 2:
+        raise ValueError("%s must have two dimensions, got %s" % (name, tuple(t.shape)))
+    return t.dtype, _index(t, name, t.dtype, None)
+
+
+def _norm_op(x, eps):
+    dtype, at = _matrix(x, "x")
+    rows, n = x.shape
+    op = CNorm(DTYPES[dtype], _int32(n, "columns", "tt_layer_norm"), rows, eps=float(eps))
+    op.ld_x = _rows_of(x, "x", dtype, at, rows, n)
+    return op, dtype, at
+
+
+def tt_layer_norm_forward(x, weight=None, bias=None, eps=1e-5, out=None, stats=None, stream=None):
+    """`(x - mean) / sqrt(variance + eps) * weight + bias` of each row of x [rows, dim]; weight and bias [dim] of x's type
+    (None: one and zero); x and out may be views into wider rows.  `stats` (float32 [rows, 2]) receives what
+    `tt_layer_norm_backward` takes.  `out` overlaps nothing."""
+    op, dtype, at = _norm_op(x, eps)
+    on = _On(at, stream)
+    p_w = None if weight is None else _packed(weight, "weight", dtype, at, (op.dim,))
+    p_b = None if bias is None else _packed(bias, "bias", dtype, at, (op.dim,))
+    p_s = None if stats is None else _packed(stats, "stats", torch.float32, at, (op.rows, 2))
+    if out is None:
+        out = on.empty(x.shape, dtype)
+    else:
+        op.ld_out = _rows_of(out, "out", dtype, at, op.rows, op.dim)
+    lib = load_library()
+    with on as s:
+        st = lib.tt_layer_norm_forward(ctypes.byref(op), x.data_ptr(), p_w, p_b, out.data_ptr(), p_s, s)
+    if st != TT_OK:
+        raise TTError(st, "tt_layer_norm_forward")
+    return out
+
+
+def tt_layer_norm_backward(x, weight, stats, grad_out, needs=(True, True, True), workspace=None, stream=None):
+    """Gradients `(dx, dweight, dbias)` of `tt_layer_norm_forward` from grad_out [rows, dim] and the forward's stats (None where
+    `needs` says so)."""
+    op, dtype, at = _norm_op(x, 0.0)
+    rows, n = op.rows, op.dim
+    on = _On(at, stream)
+    op.ld_grad = _rows_of(grad_out, "grad_out", dtype, at, rows, n)
+    p_w = None if weight is None else _packed(weight, "weight", dtype, at, (n,))
+    p_s = _packed(stats, "stats", torch.float32, at, (rows, 2))
+    dx = on.empty((rows, n), dtype) if needs[0] else None
+    dw = on.empty((n,), dtype) if needs[1] else None
+    db = on.empty((n,), dtype) if needs[2] else None
+    lib, ref = load_library(), ctypes.byref(op)
+    p_work, size = None, 0
+    if workspace is None and (needs[1] or needs[2]):
+        workspace = on.empty(lib.tt_layer_norm_workspace_bytes(ref), torch.uint8)
+    if workspace is not None:
+        p_work, size = _workspace(workspace, at)
+    with on as s:
+        st = lib.tt_layer_norm_backward(ref, x.data_ptr(), p_w, p_s, grad_out.data_ptr(), _null(dx), _null(dw), _null(db), p_work, size, s)
+    if st != TT_OK:
+        raise TTError(st, "tt_layer_norm_backward")
+    return dx, dw, db
+
+
+def _null(t):
+    return None if t is None else t.data_ptr()
+
+
+def _route_op(logits, k, scores, groups, top_groups, renormalize, scale):
+    dtype, at = _matrix(logits, "logits")
+    if scores not in SCORES:
+        raise ValueError("scores is one of %s" % ", ".join(SCORES))
+    rows, num = logits.shape
+    k, groups = int(k), int(groups)
+    top_groups = groups if top_groups is None else int(top_groups)
+    for v, name in ((num, "experts"), (k, "k"), (groups, "groups"), (top_groups, "top_groups")):
+        _int32(v, name, "tt_route")
+    op = CRoute(DTYPES[dtype], SCORES[scores], rows, num, k, groups, top_groups, int(bool(renormalize)), float(scale))
+    op.ld_logits = _rows_of(logits, "logits", dtype, at, rows, num)
+    return op, dtype, at
+
+
+def tt_route_forward(logits, k, bias=None, scores="softmax", groups=1, top_groups=None, renormalize=False, scale=1.0, experts=None, weights=None,
+                     stream=None):
+    """`(experts, weights)` of each row of logits [rows, experts]: the numbers (int64 [rows, k]) of the k experts with the largest
+    softmax or sigmoid score plus `bias` (float32 [experts]; it chooses only) and their weights (float32 [rows, k]).  With
+    groups the k are of the `top_groups` groups (None: all of them) with the largest sums of two best scores.  An expert whose
+    logit is -inf is masked; where fewer than k are left the number is -1 and the weight 0 (include/tt_emb.h has the rest)."""
+    op, dtype, at = _route_op(logits, k, scores, groups, top_groups, renormalize, scale)
+    on = _On(at, stream)
+    p_b = None if bias is None else _packed(bias, "bias", torch.float32, at, (op.experts,))
+    experts = on.empty((op.rows, op.choices), torch.int64) if experts is None else experts
+    weights = on.empty((op.rows, op.choices), torch.float32) if weights is None else weights
+    p_e = _packed(experts, "experts", torch.int64, at, (op.rows, op.choices))
+    p_w = _packed(weights, "weights", torch.float32, at, (op.rows, op.choices))
+    lib = load_library()
+    with on as s:
+        st = lib.tt_route_forward(ctypes.byref(op), logits.data_ptr(), p_b, p_e, p_w, s)
+    if st != TT_OK:
+        raise TTError(st, "tt_route_forward")
+    return experts, weights
+
+
+def tt_route_backward(logits, experts, grad_weights, scores="softmax", renormalize=False, scale=1.0, stream=None):
+    """The logits' gradient from that of the weights (float32 [rows, k]); `experts` are the numbers that the forward gave."""
+    if not isinstance(experts, torch.Tensor) or experts.dim() != 2:
+        raise TypeError("experts must be a CUDA tensor of int64, [rows, k]")
+    op, dtype, at = _route_op(logits, experts.shape[1], scores, 1, 1, renormalize, scale)
+    on = _On(at, stream)
+    p_e = _packed(experts, "experts", torch.int64, at, (op.rows, op.choices))
+    p_g = _packed(grad_weights, "grad_weights", torch.float32, at, (op.rows, op.choices))
+    out = on.empty(logits.shape, dtype)
+    lib = load_library()
+    with on as s:
+        st = lib.tt_route_backward(ctypes.byref(op), logits.data_ptr(), p_e, p_g, out.data_ptr(), s)
+    if st != TT_OK:
+        raise TTError(st, "tt_route_backward")
+    return out
+
+
+def tt_expert_order(experts, num_experts, workspace=None, stream=None):
+    """`(offsets, slots, sources)`: the choices (int64 [rows, k], numbers outside [0, num_experts) go nowhere) in the experts'
+    order.  offsets (int64 [num_experts + 1]) are what `tt_dense_forward` takes; slots (int32 [rows, k]) each choice's place, -1
+    for none; sources (int32 [rows * k]) each place's choice, -1 behind the last one."""
+    at = _index(experts, "experts", torch.int64, None)
+    if experts.dim() != 2 or not experts.is_contiguous():
+        raise ValueError("experts must be [rows, k] and contiguous")
+    n, num = experts.numel(), _int32(int(num_experts), "num_experts", "tt_expert_order")
+    on = _On(at, stream)
+    offsets, slots, sources = on.empty((num + 1,), torch.int64), on.empty(experts.shape, torch.int32), on.empty((n,), torch.int32)
+    lib = load_library()
+    need = lib.tt_expert_order_workspace_bytes(n, num)
+    if workspace is None and need:
+        workspace = on.empty(need, torch.uint8)
+    p_work, size = (None, 0) if workspace is None else _workspace(workspace, at)
+    with on as s:
+        st = lib.tt_expert_order(experts.data_ptr(), n, num, offsets.data_ptr(), slots.data_ptr(), sources.data_ptr(), p_work, size, s)
+    if st != TT_OK:
+        raise TTError(st, "tt_expert_order")
+    return offsets, slots, sources
+
+
+def _deal_op(dtype, dim, slots, sources, at):
+    _index(slots, "slots", torch.int32, at)
+    if slots.dim() != 2:
+        raise ValueError("slots must be [rows, k]")
+    rows, k = slots.shape
+    p_slots = _packed(slots, "slots", torch.int32, at, (rows, k))
+    p_sources = None if sources is None else _packed(sources, "sources", torch.int32, at, (rows * k,))
+    op = CDeal(DTYPES[dtype], _int32(dim, "columns", "tt_expert_rows"), rows, _int32(k, "k", "tt_expert_rows"))
+    return op, p_slots, p_sources
+
+
+def tt_expert_rows(x, slots, sources, out=None, stream=None):
+    """The rows of x [rows, dim] in the experts' order: `out[slots[r, j]] = x[r]`, out [rows * k, dim].  Places without a source
+    are left as they were in a given `out`, zeros in a new one."""
+    dtype, at = _matrix(x, "x")
+    op, p_slots, p_sources = _deal_op(dtype, x.shape[1], slots, sources, at)
+    on = _On(at, stream)
+    op.ld_rows = _rows_of(x, "x", dtype, at, op.rows, op.dim)
+    if out is None:
+        out = on.empty((op.rows * op.choices, op.dim), dtype)
+        op.zero_rest = 1
+    else:
+        op.ld_places = _rows_of(out, "out", dtype, at, op.rows * op.choices, op.dim)
+    lib = load_library()
+    with on as s:
+        st = lib.tt_expert_rows(ctypes.byref(op), x.data_ptr(), p_slots, p_sources, out.data_ptr(), s)
+    if st != TT_OK:
+        raise TTError(st, "tt_expert_rows")
+    return out
+
+
+def tt_expert_combine(y, slots, weights=None, residual=None, out=None, stream=None):
+    """`out[r] = residual[r] + sum_j weights[r, j] y[slots[r, j]]` of y [rows * k, dim] (weights float32 [rows, k], None: ones;
+    choices without a place are left out).  `out` may be the residual."""
+    dtype, at = _matrix(y, "y")
+    op, p_slots, _ = _deal_op(dtype, y.shape[1], slots, None, at)
+    rows, n = op.rows, op.dim
+    on = _On(at, stream)
+    op.ld_places = _rows_of(y, "y", dtype, at, rows * op.choices, n)
+    p_w = None if weights is None else _packed(weights, "weights", torch.float32, at, slots.shape)
+    p_res = None
+    if residual is not None:
+        op.ld_residual = _rows_of(residual, "residual", dtype, at, rows, n)
+        p_res = residual.data_ptr()
+    if out is None:
+        out = on.empty((rows, n), dtype)
+    else:
+        op.ld_rows = _rows_of(out, "out", dtype, at, rows, n)
+    lib = load_library()
+    with on as s:
+        st = lib.tt_expert_combine(ctypes.byref(op), y.data_ptr(), p_slots, p_w, p_res, out.data_ptr(), s)
+    if st != TT_OK:
+        raise TTError(st, "tt_expert_combine")
+    return out
+
+
+def tt_expert_combine_backward(y, slots, sources, weights, grad_out, needs=(True, True), stream=None):
+    """Gradients `(dy, dweights)` of `tt_expert_combine` from grad_out [rows, dim]; dy has zeros in places without a source."""
+    dtype, at = _matrix(y, "y")
+    op, p_slots, p_sources = _deal_op(dtype, y.shape[1], slots, sources, at)
+    rows, n = op.rows, op.dim
+    on = _On(at, stream)
+    op.ld_places = _rows_of(y, "y", dtype, at, rows * op.choices, n)
+    op.ld_rows = _rows_of(grad_out, "grad_out", dtype, at, rows, n)
+    p_w = None if weights is None else _packed(weights, "weights", torch.float32, at, slots.shape)
+    dy = on.empty((rows * op.choices, n), dtype) if needs[0] else None
+    dw = on.empty(slots.shape, torch.float32) if needs[1] else None
+    lib = load_library()
+    with on as s:
+        st = lib.tt_expert_combine_backward(ctypes.byref(op), y.data_ptr(), p_slots, p_sources, p_w, grad_out.data_ptr(), _null(dy), _null(dw), s)
+    if st != TT_OK:
+        raise TTError(st, "tt_expert_combine_backward")
+    return dy, dw
+
+
+def _loss_op(x, w, labels, bias, ignore_index, reduction):
+    dtype, at = _matrix(x, "x")
+    if reduction not in REDUCTIONS:
+        raise ValueError("reduction is one of %s" % ", ".join(REDUCTIONS))
+    rows, n = x.shape
+    _index(w, "w", dtype, at)
+    if w.dim() != 2 or w.shape[1] != n:
+        raise ValueError("w must be [classes, %d], got %s" % (n, tuple(w.shape)))
+    classes = w.shape[0]
+    if not -2 ** 63 <= ignore_index < 2 ** 63:
+        raise ValueError("ignore_index is a 64-bit integer")
+    op = CLoss(DTYPES[dtype], REDUCTIONS[reduction], rows, _int32(n, "columns", "tt_cross_entropy"), _int32(classes, "classes", "tt_cross_entropy"),
+               ignore_index)
+    op.ld_x = _rows_of(x, "x", dtype, at, rows, n)
+    return (op, dtype, at, _packed(w, "w", dtype, at, (classes, n)), None if bias is None else _packed(bias, "bias", dtype, at, (classes,)),
+            _packed(labels, "labels", torch.int64, at, (rows,)))
+
+
+def tt_cross_entropy_workspace_bytes(x, w, labels, bias=None, ignore_index=-100, reduction="mean", backward=False) -> int:
+    """Bytes of workspace the calls below take for these operands (they allocate it if none is given)."""
+    op = _loss_op(x, w, labels, bias, ignore_index, reduction)[0]
+    return int(load_library().tt_cross_entropy_workspace_bytes(ctypes.byref(op), int(backward)))
+
+
+def _loss_workspace(lib, op, backward, workspace, on, at):
+    if workspace is None:
+        need = lib.tt_cross_entropy_workspace_bytes(ctypes.byref(op), backward)
+        if need == 0:
+            raise TTError(TT_ERR_SHAPE, "tt_cross_entropy_workspace_bytes")
+        workspace = on.empty(need, torch.uint8)
+    return workspace, *_workspace(workspace, at)
+
+
+def tt_cross_entropy_forward(x, w, labels, bias=None, ignore_index=-100, reduction="mean", workspace=None, stream=None):
+    """`(loss, lse)` of x [rows, dim] against the classes of w [classes, dim] (and bias [classes]): float32, [rows] without a
+    reduction, else one number; labels int64 [rows].  Rows labelled ignore_index have a loss of zero and are not counted by "mean" (0
+    if there is no other).  lse [rows] is what the backward takes."""
+    op, dtype, at, p_w, p_b, p_l = _loss_op(x, w, labels, bias, ignore_index, reduction)
+    on = _On(at, stream)
+    loss = on.empty((op.rows,) if reduction == "none" else (), torch.float32)
+    lse = on.empty((op.rows,), torch.float32)
+    lib = load_library()
+    workspace, p_work, size = _loss_workspace(lib, op, 0, workspace, on, at)
+    with on as s:
+        st = lib.tt_cross_entropy_forward(ctypes.byref(op), x.data_ptr(), p_w, p_b, p_l, loss.data_ptr(), lse.data_ptr(), p_work, size, s)
+    if st != TT_OK:
+        raise TTError(st, "tt_cross_entropy_forward")
+    return loss, lse
+
+
+def tt_cross_entropy_backward(x, w, labels, lse, grad_loss, bias=None, ignore_index=-100, reduction="mean", needs=(True, True, True), workspace=None,
+                              stream=None):
+    """Gradients `(dx, dw, dbias)` of `tt_cross_entropy_forward` from grad_loss (float32, of the loss's shape)."""
+    op, dtype, at, p_w, p_b, p_l = _loss_op(x, w, labels, bias, ignore_index, reduction)
+    on = _On(at, stream)
+    p_lse = _packed(lse, "lse", torch.float32, at, (op.rows,))
+    p_g = _packed(grad_loss, "grad_loss", torch.float32, at, (op.rows,) if reduction == "none" else ())
+    dx = on.empty(x.shape, dtype) if needs[0] else None
+    dw = on.empty(w.shape, dtype) if needs[1] else None
+    db = on.empty((op.classes,), dtype) if needs[2] else None
+    if dx is None and dw is None and db is None:
+        return dx, dw, db
+    lib = load_library()
+    workspace, p_work, size = _loss_workspace(lib, op, 1, workspace, on, at)
+    with on as s:
+        st = lib.tt_cross_entropy_backward(ctypes.byref(op), x.data_ptr(), p_w, p_b, p_l, p_lse, p_g, _null(dx), _null(dw), _null(db), p_work, size, s)
+    if st != TT_OK:
+        raise TTError(st, "tt_cross_entropy_backward")
+    return dx, dw, db
 
 
 # ------------------------------------------------------------------ batched calls

@@ -13,6 +13,15 @@
 #define TT_GEMM_RAGGED_M 1  // rows [start(z), end(z)) of A, res and out belong to group z, whose B and bias are at z * step
 #define TT_GEMM_RAGGED_K 2  // group z sums over the stored rows [start(z), end(z)) of A and B; its out is at z * step
 
+// What becomes of the sums z = alpha * sum + bias of a tile, beside what the fields bias, pre, act and res say (PLAIN); the others
+// are the softmax loss's (tt_loss.hip), each for the layouts that it needs: rows of z by K-contiguous operands, ACC with a
+// row-contiguous B, SCALED with both row-contiguous.
+#define TT_GEMM_PLAIN 0
+#define TT_GEMM_STATS 1    // nothing is stored but, of each row's columns in the tile, the largest z and the sum of exp(z - it), and the label's z
+#define TT_GEMM_SOFTMAX 2  // out = (exp(z - lse[m]) - (n is the label)) * row_grad[m], zeros in columns N .. n_padded - 1
+#define TT_GEMM_ACC 3      // acc[m][n] = z, plus what is there if acc_add, in fp32
+#define TT_GEMM_SCALED 4   // out and rowsum times *scale
+
 struct TTGemm {
   int dtype, out_dtype;        // of the operands, bias, res; of out
   int a_kc, b_kc;              // 1: K-contiguous
@@ -33,6 +42,17 @@ struct TTGemm {
   long long bias_step, ldr, r_step, ldp, p_step, rs_step;
   int act;
   float alpha, beta;
+  int epilogue;                // TT_GEMM_PLAIN ...
+  int a_padded;                // 16-bit A whose rows go on with zeros (K-contiguous) or anything (else) up to a multiple of 8
+  float *stats;                // STATS: pairs [column tile][M]
+  float *picked;               // STATS: [M]
+  const int32_t *labels;       // STATS, SOFTMAX: [M], first + the label's column; others are no column's
+  int first;
+  const float *lse, *row_grad; // SOFTMAX: [M]
+  int n_padded;                // SOFTMAX
+  float *acc;                  // ACC: [M][N], fp32
+  int acc_add;
+  const float *scale;          // SCALED: DEVICE
   int parts;                   // fp32 operands: bf16 parts of each that are multiplied (3: fp32's precision, 2: 16 bits)
 };
 
@@ -49,6 +69,8 @@ __host__ __device__ inline long long ttk_gemm_piece_floats(const TTGemm &g) {
 size_t ttk_gemm_partial_bytes(const TTGemm &g);  // 0: not cut (addresses are not looked at: enough for any)
 // Enqueues the product.  partial: ttk_gemm_partial_bytes(g) bytes of DEVICE memory, 256-byte aligned.
 tt_status ttk_gemm(const TTGemm &g, void *partial, hipStream_t s);
+
+int ttk_gemm_tile(const TTGemm &g);  // the side of its tiles: the columns of a tile of stats
 
 // Rows of a group from which its sum is cut, for tiles of e x e (RAGGED_K); `least` steps of bk at least.
 int ttk_gemm_chunk(const TTGemm &g, int e, int bk, int least);

@@ -209,7 +209,7 @@ template <bool KC, int LD32> __device__ __forceinline__ f32x4 frag32(const float
 // Measured: fp32 4096 x 4096 x 1024 188 us (183 TFLOP/s, 1100 of bf16 products; the fp32 instruction's rate is 154), 106496 x 128 x 128 39 us (22 by
 // its bytes), 2 % of both for the largest number; two parts 2048 x 4096 x 2048 106 us (975 of bf16 products).  Without the matrix instructions the first took 169 of 198,
 // without the split of P = 2 the last 93 of 106: splitting, LDS and barriers bound it.  Loads two or four steps ahead in registers, and two buffers for P = 2, are no faster.
-template <class T, class O, int P, bool AKC, bool BKC, int E>
+template <class T, class O, int P, bool AKC, bool BKC, int E, int EPI>
 __global__ void __launch_bounds__(TT_BLOCK, 2) k_gemm(TTGemm g, int m_tiles, int n_tiles, int split, int chunk, float *partial) {
   typedef Carrier<T, AKC, E> CA;
   typedef Carrier<T, BKC, E> CB;
@@ -528,19 +528,27 @@ __global__ void __launch_bounds__(TT_BLOCK, 2) k_gemm(TTGemm g, int m_tiles, int
       const int m = w.lo + wm + 16 * x + j;
       if (m >= w.hi) continue;
       if (piece) piece[(long long)g.M * g.N + m] = rs[x][0];
-      else ((O *)g.rowsum)[w.z * g.rs_step + m] = from_f32<O>(rs[x][0]);
+      else ((O *)g.rowsum)[w.z * g.rs_step + m] = from_f32<O>(EPI == TT_GEMM_SCALED ? rs[x][0] * *g.scale : rs[x][0]);
     }
   }
   __syncthreads();  // nobody reads the operands any more
+  if constexpr (EPI == TT_GEMM_STATS) {
+    float2 *stats = reinterpret_cast<float2 *>(lds);  // [left, right half of the columns][row]
+    tile_stats<T, F, F>(g, w.z, w.lo + wm, w.hi, w.n0 + wn, acc, stats + (wave & 1) * E + wm);
+    __syncthreads();
+    const int r = (int)threadIdx.x;
+    if (r < E && w.lo + r < w.hi) reinterpret_cast<float2 *>(g.stats)[(long long)nt * g.M + w.lo + r] = join_stats(stats[r], stats[E + r]);
+    return;
+  }
   float *room = reinterpret_cast<float *>(lds) + wave * finish_floats<F, 2>();
   const bool mirror = g.symmetric && mt != nt;
   if (piece) finish_tile<T, float, F, F, 2, false>(as_piece(g, piece), 0, w.lo + wm, w.hi, w.n0 + wn, acc, room, mirror);
-  else finish_tile<T, O, F, F, 2, false>(g, w.z, w.lo + wm, w.hi, w.n0 + wn, acc, room, mirror, settles ? norms_a + wm : nullptr,
+  else finish_tile<T, O, F, F, 2, false, EPI>(g, w.z, w.lo + wm, w.hi, w.n0 + wn, acc, room, mirror, settles ? norms_a + wm : nullptr,
                                                   settles ? norms_b + wn : nullptr);
 }
 
 // The pieces of a cut product, added in order; four columns of a row per thread.
-template <class T, class O> __device__ __forceinline__ void join_pieces(const TTGemm &g, int z, int pieces, const float *p, long long step) {
+template <class T, class O, int EPI> __device__ __forceinline__ void join_pieces(const TTGemm &g, int z, int pieces, const float *p, long long step) {
   const int per = (g.N + 3) / 4;
   const long long total = (long long)g.M * per;
   const int lane = threadIdx.x & 63;
@@ -550,7 +558,7 @@ template <class T, class O> __device__ __forceinline__ void join_pieces(const TT
       const long long m = e - total;
       float s = 0.f;
       for (int i = 0; i < pieces; ++i) s += p[i * step + (long long)g.M * g.N + m];
-      ((O *)g.rowsum)[z * g.rs_step + m] = from_f32<O>(s);
+      ((O *)g.rowsum)[z * g.rs_step + m] = from_f32<O>(EPI == TT_GEMM_SCALED ? s * *g.scale : s);
     }
     if (e0 >= total) continue;
     const int m = e < total ? (int)(e / per) : 0, n = e < total ? (int)(e - (long long)m * per) * 4 : 0;
@@ -583,17 +591,28 @@ template <class T, class O> __device__ __forceinline__ void join_pieces(const TT
         continue;
       }
     }
-    if (valid > 0) finish<T, O, 4>(g, z, m, n, valid, v);
+    if constexpr (EPI == TT_GEMM_ACC) {
+      if (valid > 0) {
+        float *to = g.acc + (long long)m * g.N + n;
+        float t[4] = {0.f, 0.f, 0.f, 0.f};
+        if (g.acc_add) load4(to, valid, t);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) t[c] = fmaf(g.alpha, v[c], t[c]);
+        store4(to, valid, t);
+      }
+    } else {
+      if (valid > 0) finish<T, O, 4, false, EPI == TT_GEMM_SCALED>(g, z, m, n, valid, v);
+    }
   }
 }
-template <class T, class O> __global__ void __launch_bounds__(TT_BLOCK) k_join(TTGemm g, int split, const float *__restrict__ partial) {
+template <class T, class O, int EPI> __global__ void __launch_bounds__(TT_BLOCK) k_join(TTGemm g, int split, const float *__restrict__ partial) {
   const int z = (int)blockIdx.y;
-  join_pieces<T, O>(g, z, split, partial + z * ttk_gemm_piece_floats(g), g.batch * ttk_gemm_piece_floats(g));
+  join_pieces<T, O, EPI>(g, z, split, partial + z * ttk_gemm_piece_floats(g), g.batch * ttk_gemm_piece_floats(g));
 }
 template <class T> __global__ void __launch_bounds__(TT_BLOCK) k_join_groups(TTGemm g, int chunk, int bk, const float *__restrict__ partial) {
   int z = (int)blockIdx.y, lo = 0, hi = 0, pieces = 1, first = 0;
   find_slot(g.offsets, g.batch, g.K, chunk, bk, -1, z, lo, hi, pieces, first);
-  if (z >= 0) join_pieces<T, T>(g, z, pieces, partial + first * ttk_gemm_piece_floats(g), ttk_gemm_piece_floats(g));
+  if (z >= 0) join_pieces<T, T, TT_GEMM_PLAIN>(g, z, pieces, partial + first * ttk_gemm_piece_floats(g), ttk_gemm_piece_floats(g));
 }
 
 // ---- host ------------------------------------------------------------------------------------------
@@ -652,9 +671,17 @@ template <class T, class O, int P, int E> void launch_e(const TTGemm &g, const S
   const long long per_member = g.symmetric ? h.n_tiles * (h.n_tiles + 1) / 2 : h.m_tiles * h.n_tiles;
   const dim3 grid((unsigned)per_member, (unsigned)(h.members * h.split));
   const int mti = (int)h.m_tiles, nti = (int)h.n_tiles, split = h.split, chunk = h.chunk;
-  if (g.a_kc && g.b_kc) hipLaunchKernelGGL((k_gemm<T, O, P, true, true, E>), grid, dim3(TT_BLOCK), 0, s, g, mti, nti, split, chunk, part);
-  else if (g.a_kc) hipLaunchKernelGGL((k_gemm<T, O, P, true, false, E>), grid, dim3(TT_BLOCK), 0, s, g, mti, nti, split, chunk, part);
-  else hipLaunchKernelGGL((k_gemm<T, O, P, false, false, E>), grid, dim3(TT_BLOCK), 0, s, g, mti, nti, split, chunk, part);
+#define TT_TILES(AKC, BKC, EPI) hipLaunchKernelGGL((k_gemm<T, O, P, AKC, BKC, E, EPI>), grid, dim3(TT_BLOCK), 0, s, g, mti, nti, split, chunk, part)
+  if constexpr (std::is_same<T, O>::value && P != 2) {
+    if (g.epilogue == TT_GEMM_STATS) { TT_TILES(true, true, TT_GEMM_STATS); return; }
+    if (g.epilogue == TT_GEMM_SOFTMAX) { TT_TILES(true, true, TT_GEMM_SOFTMAX); return; }
+    if (g.epilogue == TT_GEMM_ACC) { TT_TILES(true, false, TT_GEMM_ACC); return; }
+    if (g.epilogue == TT_GEMM_SCALED) { TT_TILES(false, false, TT_GEMM_SCALED); return; }
+  }
+  if (g.a_kc && g.b_kc) TT_TILES(true, true, TT_GEMM_PLAIN);
+  else if (g.a_kc) TT_TILES(true, false, TT_GEMM_PLAIN);
+  else TT_TILES(false, false, TT_GEMM_PLAIN);
+#undef TT_TILES
 }
 unsigned join_blocks(const TTGemm &g) {
   long long blocks = ((long long)g.M * ((g.N + 3) / 4) + g.M + TT_BLOCK - 1) / TT_BLOCK;
@@ -670,7 +697,14 @@ template <class T, class O, int P> tt_status launch(const TTGemm &g, void *parti
   else launch_e<T, O, P, 64>(g, h, part, s);
   if (h.split > 1) {
     const int split = h.split;
-    hipLaunchKernelGGL((k_join<T, O>), dim3(join_blocks(g), (unsigned)h.members), dim3(TT_BLOCK), 0, s, g, split, (const float *)part);
+    const dim3 grid(join_blocks(g), (unsigned)h.members);
+    if constexpr (std::is_same<T, O>::value && P != 2) {
+      if (g.epilogue == TT_GEMM_ACC) hipLaunchKernelGGL((k_join<T, O, TT_GEMM_ACC>), grid, dim3(TT_BLOCK), 0, s, g, split, (const float *)part);
+      else if (g.epilogue == TT_GEMM_SCALED) hipLaunchKernelGGL((k_join<T, O, TT_GEMM_SCALED>), grid, dim3(TT_BLOCK), 0, s, g, split, (const float *)part);
+      else hipLaunchKernelGGL((k_join<T, O, TT_GEMM_PLAIN>), grid, dim3(TT_BLOCK), 0, s, g, split, (const float *)part);
+    } else {
+      hipLaunchKernelGGL((k_join<T, O, TT_GEMM_PLAIN>), grid, dim3(TT_BLOCK), 0, s, g, split, (const float *)part);
+    }
   }
   const tt_status st = tt_launch_status();
   return st == TT_OK && h.chunk ? ttk_gemm_join_groups(g, h.chunk, g.dtype == TT_F32 ? 32 : 64, part, s) : st;
@@ -703,6 +737,8 @@ tt_status ttk_gemm_join_groups(const TTGemm &g, int chunk, int bk, const float *
   return tt_launch_status();
 }
 
+int ttk_gemm_tile(const TTGemm &g) { return ttk_gemm_direct_serves(g) ? 256 : shape_of(g).e; }
+
 size_t ttk_gemm_partial_bytes(const TTGemm &g) {
   if (g.M < 1 || g.N < 1 || g.batch < 1 || ttk_gemm_rows_serves(g)) return 0;
   const Shape h = shape_of(g);
@@ -716,6 +752,7 @@ size_t ttk_gemm_partial_bytes(const TTGemm &g) {
 tt_status ttk_gemm(const TTGemm &g, void *partial, hipStream_t s) {
   if (g.M < 1 || g.N < 1 || g.batch < 1) return TT_OK;
   if (!g.a_kc && g.b_kc) return TT_ERR_INVALID_ARG;  // no caller needs it
+  if (g.epilogue != TT_GEMM_PLAIN && (g.out_dtype != g.dtype || g.parts == 2 || g.mode == TT_GEMM_RAGGED_K || g.symmetric)) return TT_ERR_INVALID_ARG;
   if (ttk_gemm_rows_serves(g)) return ttk_gemm_rows(g, s);
   if (ttk_gemm_direct_serves(g)) return ttk_gemm_direct(g, partial, s);
   if (g.dtype == TT_BF16 && g.out_dtype == TT_BF16) return launch<ttg::bf16, ttg::bf16, 1>(g, partial, s);

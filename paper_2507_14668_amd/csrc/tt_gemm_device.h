@@ -302,7 +302,7 @@ __device__ __forceinline__ void tile_order(unsigned t, unsigned m_tiles, unsigne
 template <class O> __device__ __forceinline__ void clear_rest(const TTGemm &g, int above, int covered, int idx, int n, int n0, int width) {
   const float zero[4] = {0.f, 0.f, 0.f, 0.f};
   const long long rest = (long long)above + g.M - covered;
-  const int end = g.N < n0 + width ? g.N : n0 + width;
+  const int cols = g.n_padded > g.N ? g.n_padded : g.N, end = cols < n0 + width ? cols : n0 + width;
   for (long long r = (long long)idx * 4 + (threadIdx.x >> 6); r < rest; r += (long long)n * 4)
     for (int c = n0 + 4 * (threadIdx.x & 63); c < end; c += 256)
       store4((O *)g.out + (r < above ? r : r - above + covered) * g.ldo + c, end - c < 4 ? end - c : 4, zero);
@@ -310,11 +310,16 @@ template <class O> __device__ __forceinline__ void clear_rest(const TTGemm &g, i
 
 // out[m][n .. n + C - 1] from C = 4 or 8 sums, of which `valid` columns exist.  `bias` and `res`: these columns' values where the caller
 // has them already (null: they are read here).
-template <class T, class O, int C, bool STREAM = false>
+template <class T, class O, int C, bool STREAM = false, bool SCALED = false>
 __device__ __forceinline__ void finish(const TTGemm &g, int z, int m, int n, int valid, float v[C], const float *bias = nullptr, const float *res = nullptr) {
   float t[C];
 #pragma unroll
   for (int i = 0; i < C; ++i) v[i] *= g.alpha;
+  if constexpr (SCALED) {
+    const float scale = *g.scale;
+#pragma unroll
+    for (int i = 0; i < C; ++i) v[i] *= scale;
+  }
   if (bias) {
 #pragma unroll
     for (int i = 0; i < C; ++i) v[i] += bias[i];
@@ -392,6 +397,70 @@ __device__ __forceinline__ void settle_signs(const TTGemm &g, int z, int m, int 
   }
 }
 
+// Eight columns of a row of the softmax's gradient: of `valid` columns, and zeros behind them up to the padding.
+template <class T> __device__ __forceinline__ void finish_softmax(const TTGemm &g, int m, int n, float v[8], const float bias[8]) {
+  const float lse = g.lse[m], grad = g.row_grad[m];
+  const int label = g.labels[m] - g.first - n, valid = g.N - n;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const float p = __expf(fmaf(g.alpha, v[i], bias[i]) - lse);
+    v[i] = i < valid ? grad * (i == label ? p - 1.f : p) : 0.f;
+  }
+  store_n<T, 8>((T *)g.out + (long long)m * g.ldo + n, g.n_padded - n, v);
+}
+// Eight columns of a row, added to what earlier products left there.
+__device__ __forceinline__ void finish_acc(const TTGemm &g, int m, int n, int valid, float v[8]) {
+  float *to = g.acc + (long long)m * g.N + n;
+  float t[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  if (g.acc_add) load_n<float, 8>(to, valid, t);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) t[i] = fmaf(g.alpha, v[i], t[i]);
+  store_n<float, 8>(to, valid, t);
+}
+// Of each row of a wavefront's results (as in finish_tile, in its registers still) the largest z and the sum of exp(z - it), over its columns,
+// to `stats` (LDS, a pair for each of the wavefront's rows); the label's z to picked.  A lane has 4 FY columns of FX rows, four lanes a row.
+// Columns of -infinity count as nothing; a NaN is in the sum.
+template <class T, int FX, int FY> __device__ __forceinline__ void tile_stats(const TTGemm &g, int z, int m0, int end, int n0, const f32x4 (&acc)[FX][FY], float2 *stats) {
+  const int lane = threadIdx.x & 63, q = lane >> 4, j = lane & 15;
+  f32x4 bias[FY];
+#pragma unroll
+  for (int y = 0; y < FY; ++y) {
+    const int n = n0 + 16 * y + 4 * q;
+    float t[4] = {0.f, 0.f, 0.f, 0.f};
+    if (g.bias) load4((const T *)g.bias + z * g.bias_step + n, g.N - n, t);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) bias[y][i] = n + i < g.N ? t[i] : -INFINITY;
+  }
+#pragma unroll
+  for (int x = 0; x < FX; ++x) {
+    const int m = m0 + 16 * x + j, label = (m < end ? g.labels[m] : -1) - g.first - n0 - 4 * q;
+    float top = -INFINITY, sum = 0.f;
+    f32x4 v[FY];
+#pragma unroll
+    for (int y = 0; y < FY; ++y)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        v[y][i] = fmaf(g.alpha, acc[x][y][i], bias[y][i]);
+        if (label == 16 * y + i && n0 + 16 * y + 4 * q + i < g.N) g.picked[m] = v[y][i];
+        top = fmaxf(top, v[y][i]);
+      }
+    top = fmaxf(top, __shfl(top, lane ^ 16, 64));
+    top = fmaxf(top, __shfl(top, lane ^ 32, 64));
+    const float base = top == -INFINITY ? 0.f : top;
+#pragma unroll
+    for (int y = 0; y < FY; ++y)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sum += __expf(v[y][i] - base);
+    sum += __shfl(sum, lane ^ 16, 64);
+    sum += __shfl(sum, lane ^ 32, 64);
+    if (q == 0) stats[16 * x + j] = float2{top, sum};
+  }
+}
+__device__ __forceinline__ float2 join_stats(float2 a, float2 b) {
+  const float top = fmaxf(a.x, b.x), base = top == -INFINITY ? 0.f : top;
+  return float2{top, a.y * __expf(a.x - base) + b.y * __expf(b.x - base)};
+}
+
 // The results of a wavefront, 16 FX x 16 FY of out from row m0 and column n0, rows below `end`.  The instruction leaves a lane
 // four columns of a row, 8 bytes of a 16-bit row at a time; through 16 XB rows of LDS (`lds`: finish_floats of the wavefront's own) a lane
 // gets eight, and what is read and written is whole lines of 128 bytes.  The loop over the rows is not unrolled: with all activations in it
@@ -413,7 +482,7 @@ template <int FY, int XB> constexpr int finish_floats() { return 16 * XB * (16 *
 // x 4096 bf16 without residual 543 -> 423 us), and the residual is read four rows ahead: one at a time, its latency had each tile's end
 // take as long as a quarter of its product.
 // `squares_a` and `squares_b` (LDS, null: nothing is settled): of the wavefront's rows of A and of B, for settle_signs.
-template <class T, class O, int FX, int FY, int XB, bool STREAM>
+template <class T, class O, int FX, int FY, int XB, bool STREAM, int EPI = TT_GEMM_PLAIN>
 __device__ __forceinline__ void finish_tile(const TTGemm &g, int z, int m0, int end, int n0, const f32x4 (&acc)[FX][FY], float *lds, bool mirror = false,
                                             const float *squares_a = nullptr, const float *squares_b = nullptr) {
   constexpr int LD = 16 * FY + 4, PER = 2 * FY, ROWS = 64 / PER;  // lanes of a row, rows at a time
@@ -455,7 +524,19 @@ __device__ __forceinline__ void finish_tile(const TTGemm &g, int z, int m0, int 
         v[4 + i] = b[i];
       }
     };
-    if (STREAM && g.res) {
+    if constexpr (EPI == TT_GEMM_SOFTMAX || EPI == TT_GEMM_ACC) {
+#pragma unroll 1
+      for (int row = r; row < 16 * XB; row += ROWS) {
+        const int m = m0 + 16 * x0 + row;
+        float v[8];
+        sums(row, v);
+        if constexpr (EPI == TT_GEMM_SOFTMAX) {
+          if (m < end && n0 + c < g.n_padded) finish_softmax<T>(g, m, n0 + c, v, bias);
+        } else {
+          if (m < end && valid > 0) finish_acc(g, m, n0 + c, valid, v);
+        }
+      }
+    } else if (STREAM && g.res) {
       if constexpr (STREAM) {
 #pragma unroll 1
         for (int row = r; row < 16 * XB; row += ROWS) {
@@ -467,8 +548,8 @@ __device__ __forceinline__ void finish_tile(const TTGemm &g, int z, int m0, int 
 #pragma unroll
           for (int i = 0; i + 1 < AHEAD; ++i) ahead[i] = ahead[i + 1];
           ahead[AHEAD - 1] = residual(16 * x0 + row + AHEAD * ROWS);
-          if (m < end && valid >= 8) finish<T, O, 8, true>(g, z, m, n0 + c, 8, v, bias, res);
-          else if (m < end && valid > 0) finish<T, O, 8, true>(g, z, m, n0 + c, valid, v, bias);
+          if (m < end && valid >= 8) finish<T, O, 8, true, EPI == TT_GEMM_SCALED>(g, z, m, n0 + c, 8, v, bias, res);
+          else if (m < end && valid > 0) finish<T, O, 8, true, EPI == TT_GEMM_SCALED>(g, z, m, n0 + c, valid, v, bias);
         }
       }
     } else {
@@ -481,11 +562,11 @@ __device__ __forceinline__ void finish_tile(const TTGemm &g, int z, int m0, int 
           if (squares_a) {
             const float none[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};  // (bias is in v)
             settle_signs<8>(g, z, m, n0 + c, m < end ? valid : 0, v, bias, squares_a[16 * x0 + row], squares);
-            if (m < end && valid > 0) finish<T, O, 8, STREAM>(g, z, m, n0 + c, valid, v, none);
+            if (m < end && valid > 0) finish<T, O, 8, STREAM, EPI == TT_GEMM_SCALED>(g, z, m, n0 + c, valid, v, none);
             continue;
           }
         }
-        if (m < end && valid > 0) finish<T, O, 8, STREAM>(g, z, m, n0 + c, valid, v, bias);
+        if (m < end && valid > 0) finish<T, O, 8, STREAM, EPI == TT_GEMM_SCALED>(g, z, m, n0 + c, valid, v, bias);
       }
     }
     if (mirror) {  // the same results as rows n of columns m (only products without a bias)

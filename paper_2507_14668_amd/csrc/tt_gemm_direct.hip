@@ -141,7 +141,7 @@ template <class T> __device__ __forceinline__ void row_sums(const T *a, long lon
   }
 }
 
-template <class T, bool AKC, bool BKC> __global__ void __launch_bounds__(THREADS, 2) k_gemm_direct(TTGemm g, int m_tiles, int n_tiles, int chunk, float *partial) {
+template <class T, bool AKC, bool BKC, int EPI> __global__ void __launch_bounds__(THREADS, 2) k_gemm_direct(TTGemm g, int m_tiles, int n_tiles, int chunk, float *partial) {
   __shared__ __align__(16) unsigned short lds[16 * finish_floats<4, 4>()];  // (more than two buffers take)
   static_assert(16 * finish_floats<4, 4>() >= STAGES * 2 * OPERAND, "LDS");
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -211,7 +211,7 @@ template <class T, bool AKC, bool BKC> __global__ void __launch_bounds__(THREADS
   auto give_sum = [&](int m, float v) {
     if (m >= w.hi) return;
     if (piece) piece[(long long)g.M * g.N + m] = v;
-    else ((T *)g.rowsum)[w.z * g.rs_step + m] = from_f32<T>(v);
+    else ((T *)g.rowsum)[w.z * g.rs_step + m] = from_f32<T>(EPI == TT_GEMM_SCALED ? v * *g.scale : v);
   };
   bool odd = false;  // a sum that is not finite, in any lane
   if constexpr (!AKC) {
@@ -226,10 +226,20 @@ template <class T, bool AKC, bool BKC> __global__ void __launch_bounds__(THREADS
     }
   }
   __syncthreads();  // nobody reads the operands any more
+  if constexpr (EPI == TT_GEMM_STATS) {
+    float2 *stats = reinterpret_cast<float2 *>(lds);  // [columns 0, 64, 128, 192][row]
+    tile_stats<T, 8, 4>(g, w.z, w.lo + wm, w.hi, w.n0 + wn, acc, stats + (wave & 3) * E + wm);
+    __syncthreads();
+    const int r = (int)threadIdx.x;
+    if (r < E && w.lo + r < w.hi)
+      reinterpret_cast<float2 *>(g.stats)[(long long)nt * g.M + w.lo + r] =
+          join_stats(join_stats(stats[r], stats[E + r]), join_stats(stats[2 * E + r], stats[3 * E + r]));
+    return;
+  }
   float *room = reinterpret_cast<float *>(lds) + wave * finish_floats<4, 4>();
   if constexpr (!AKC) {  // (only sums over stored rows are cut)
     if (piece) finish_tile<T, float, 8, 4, 4, false>(as_piece(g, piece), 0, w.lo + wm, w.hi, w.n0 + wn, acc, room);
-    else finish_tile<T, T, 8, 4, 4, true>(g, w.z, w.lo + wm, w.hi, w.n0 + wn, acc, room);
+    else finish_tile<T, T, 8, 4, 4, true, EPI>(g, w.z, w.lo + wm, w.hi, w.n0 + wn, acc, room);
     if (odd) {
       f32x4 whole[8] = {};
       row_sums<T>(a, g.lda, w.hi - w.lo, K, wm, whole);
@@ -238,7 +248,7 @@ template <class T, bool AKC, bool BKC> __global__ void __launch_bounds__(THREADS
         if (lane < 16) give_sum(w.lo + wm + 16 * x + lane, whole[x][0]);
     }
   } else {
-    finish_tile<T, T, 8, 4, 4, true>(g, w.z, w.lo + wm, w.hi, w.n0 + wn, acc, room);
+    finish_tile<T, T, 8, 4, 4, EPI == TT_GEMM_PLAIN, EPI>(g, w.z, w.lo + wm, w.hi, w.n0 + wn, acc, room);
   }
 }
 
@@ -252,9 +262,15 @@ template <class T> tt_status launch(const TTGemm &g, void *partial, hipStream_t 
   const dim3 grid((unsigned)(m_tiles * n_tiles), (unsigned)members);
   const int mti = (int)m_tiles, nti = (int)n_tiles;
   float *part = (float *)partial;
-  if (g.a_kc && g.b_kc) hipLaunchKernelGGL((k_gemm_direct<T, true, true>), grid, dim3(THREADS), 0, s, g, mti, nti, chunk, part);
-  else if (g.a_kc) hipLaunchKernelGGL((k_gemm_direct<T, true, false>), grid, dim3(THREADS), 0, s, g, mti, nti, chunk, part);
-  else hipLaunchKernelGGL((k_gemm_direct<T, false, false>), grid, dim3(THREADS), 0, s, g, mti, nti, chunk, part);
+#define TT_DIRECT(AKC, BKC, EPI) hipLaunchKernelGGL((k_gemm_direct<T, AKC, BKC, EPI>), grid, dim3(THREADS), 0, s, g, mti, nti, chunk, part)
+  if (g.epilogue == TT_GEMM_STATS) TT_DIRECT(true, true, TT_GEMM_STATS);
+  else if (g.epilogue == TT_GEMM_SOFTMAX) TT_DIRECT(true, true, TT_GEMM_SOFTMAX);
+  else if (g.epilogue == TT_GEMM_ACC) TT_DIRECT(true, false, TT_GEMM_ACC);
+  else if (g.epilogue == TT_GEMM_SCALED) TT_DIRECT(false, false, TT_GEMM_SCALED);
+  else if (g.a_kc && g.b_kc) TT_DIRECT(true, true, TT_GEMM_PLAIN);
+  else if (g.a_kc) TT_DIRECT(true, false, TT_GEMM_PLAIN);
+  else TT_DIRECT(false, false, TT_GEMM_PLAIN);
+#undef TT_DIRECT
   const tt_status st = tt_launch_status();
   return st == TT_OK && chunk ? ttk_gemm_join_groups(g, chunk, BK, part, s) : st;
 }
@@ -274,7 +290,8 @@ bool ttk_gemm_direct_serves(const TTGemm &g) {
   if (g.dtype == TT_F32 || g.out_dtype != g.dtype || g.symmetric) return false;
   const uintptr_t addresses = (uintptr_t)g.a | (uintptr_t)g.b;
   if ((addresses & 15) || ((g.lda | g.ldb | g.a_step | g.b_step) & 7)) return false;
-  if (((g.a_kc || g.b_kc) && (g.K & 7)) || (!g.a_kc && (g.M & 7)) || (!g.b_kc && (g.N & 7))) return false;
+  if (((g.a_kc || g.b_kc) && (g.K & 7) && !(g.a_padded && !g.b_kc)) || (!g.a_kc && (g.M & 7) && !g.a_padded) || (!g.b_kc && (g.N & 7))) return false;
+  if (g.epilogue != TT_GEMM_PLAIN && g.M <= TT_GEMM_DIRECT_LEAST) return false;
   if (g.lda > (1 << 23) || g.ldb > (1 << 23)) return false;  // offsets within a tile are 32 bits
   // half a tile would be empty
   if ((g.mode != TT_GEMM_RAGGED_M && g.M <= TT_GEMM_DIRECT_LEAST) || (g.like_N ? g.like_N : g.N) <= TT_GEMM_DIRECT_LEAST) return false;

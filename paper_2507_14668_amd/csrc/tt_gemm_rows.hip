@@ -179,7 +179,7 @@ template <class T> tt_status launch_t(const TTGemm &g, hipStream_t s) {
 #define TT_GEMM_FEW_ROWS 32
 #endif
 bool ttk_gemm_rows_serves(const TTGemm &g) {
-  if (g.out_dtype != g.dtype || !g.a_kc || !g.b_kc || g.rowsum || g.symmetric || g.mode == TT_GEMM_RAGGED_K || g.parts == 2) return false;
+  if (g.out_dtype != g.dtype || !g.a_kc || !g.b_kc || g.rowsum || g.symmetric || g.mode == TT_GEMM_RAGGED_K || g.parts == 2 || g.epilogue != TT_GEMM_PLAIN) return false;
   const int rows = g.mode == TT_GEMM_RAGGED_M ? tt_ceil_div(g.M, g.batch) : g.M;
   if (rows <= TT_GEMM_FEW_ROWS) return true;
   const long long bytes = (long long)g.K * (g.dtype == TT_F32 ? 4 : 2), groups = (long long)tt_ceil_div(rows, 64) * tt_ceil_div(g.N, 16) * g.batch;

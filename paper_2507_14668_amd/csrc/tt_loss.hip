@@ -1,0 +1,406 @@
+// Softmax cross entropy against a catalogue, and its gradients, in pieces of the classes.
+#include <string.h>
+
+#include "tt_gemm_device.h"
+
+namespace {
+using namespace ttg;
+
+// Rows that count stand next to each other in the work: the products leave the others out, and whatever those hold (padding
+// may hold anything) meets nothing.
+struct Rows {
+  int32_t *of, *at;    // [rows]: row of each place, place of each row (-1: does not count)
+  int32_t *label;      // [rows] of each place; -1: no class
+  float *lse, *share;  // [rows] of each place: backward
+  float *scale;        // [2]: of G in fp16, and back
+  int64_t *offsets;    // {0, places}
+};
+
+// One workgroup: places in the order of the rows.  In the backward also each place's lse and share of the loss's gradient.
+constexpr int SCAN = 512;
+__global__ void __launch_bounds__(SCAN) k_loss_rows(const int64_t *labels, long long rows, int classes, long long ignored, int reduce, const float *lse,
+                                                    const float *grad, int half, Rows w) {
+  __shared__ int tmp[SCAN / 64 + 1];
+  __shared__ float tops[SCAN / 64];
+  int places = 0;
+  for (long long r0 = 0; r0 < rows; r0 += SCAN) {
+    const long long r = r0 + threadIdx.x;
+    const int64_t label = r < rows ? labels[r] : ignored;
+    const bool counts = label != ignored;
+    int total;
+    const int at = places + tt_block_excl_scan_n<SCAN>(counts ? 1 : 0, tmp, &total);
+    if (r < rows) w.at[r] = counts ? at : -1;
+    if (counts) {
+      w.of[at] = (int32_t)r;
+      w.label[at] = label >= 0 && label < classes ? (int32_t)label : -1;
+      if (lse) w.lse[at] = lse[r];
+    }
+    places += total;
+  }
+  if (threadIdx.x == 0) {
+    w.offsets[0] = 0;
+    w.offsets[1] = places;
+  }
+  if (!lse) return;
+  __syncthreads();
+  const float all = reduce == TT_REDUCE_NONE ? 0.f : reduce == TT_REDUCE_MEAN && places > 0 ? grad[0] / (float)places : grad[0];
+  float top = 0.f;  // the largest finite share
+  for (int i = threadIdx.x; i < places; i += SCAN) {
+    const float g = fabsf(reduce == TT_REDUCE_NONE ? grad[w.of[i]] : all);
+    top = g < INFINITY && g > top ? g : top;
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+  if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < SCAN / 64; ++i) top = fmaxf(top, tops[i]);
+  float scale = 1.f, back = 1.f;
+  if (half && top > 0.f) {  // the power of two that takes it to 2^13 .. 2^14, as far as that and its inverse are normal numbers
+    int e = (int)(__float_as_uint(top) >> 23);
+    e = e < 14 ? 14 : e > 240 ? 240 : e;
+    scale = __uint_as_float((unsigned)(127 + 13 + 127 - e) << 23);
+    back = __uint_as_float((unsigned)(e - 13) << 23);
+  }
+  if (threadIdx.x == 0) {
+    w.scale[0] = scale;
+    w.scale[1] = back;
+  }
+  for (int i = threadIdx.x; i < places; i += SCAN) w.share[i] = scale * (reduce == TT_REDUCE_NONE ? grad[w.of[i]] : all);
+}
+
+// x's rows that count next to each other, `ld` apart (padded with zeros), zeros behind the last one.
+template <class T> __global__ void __launch_bounds__(TT_BLOCK) k_loss_gather(const T *x, long long ld_x, long long rows, int dim, Rows w, T *to, int ld) {
+  constexpr int C = 16 / sizeof(T);
+  const long long places = w.offsets[1];
+  const int per = (ld + C - 1) / C;
+  for (long long e = (long long)blockIdx.x * TT_BLOCK + threadIdx.x; e < rows * per; e += (long long)gridDim.x * TT_BLOCK) {
+    const long long i = e / per;
+    const int c = (int)(e - i * per) * C;
+    float v[C] = {};
+    if (i < places) load_n<T, C>(x + w.of[i] * ld_x + c, dim - c, v);
+    store_n<T, C>(to + i * ld + c, ld - c, v);
+  }
+}
+
+// A piece's tiles into each row's running pair (largest logit, sum of exp(logit - it)); a wavefront takes 64 rows and a share of the tiles.
+__global__ void __launch_bounds__(TT_BLOCK) k_loss_fold(const float2 *__restrict__ stats, int tiles, long long rows, int first, Rows w, float2 *run) {
+  __shared__ float2 part[TT_BLOCK];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const long long i = (long long)blockIdx.x * 64 + lane, places = w.offsets[1];
+  float2 s = {-INFINITY, 0.f};
+  if (i < places)
+    for (int t = wave; t < tiles; t += TT_BLOCK / 64) s = join_stats(s, stats[t * rows + i]);
+  part[threadIdx.x] = s;
+  __syncthreads();
+  if (wave != 0 || i >= places) return;
+  for (int k = 1; k < TT_BLOCK / 64; ++k) s = join_stats(s, part[64 * k + lane]);
+  run[i] = first ? s : join_stats(run[i], s);
+}
+__global__ void __launch_bounds__(TT_BLOCK) k_loss_of_rows(long long rows, Rows w, const float2 *run, const float *picked, float *loss, float *lse) {
+  const long long r = (long long)blockIdx.x * TT_BLOCK + threadIdx.x;
+  if (r >= rows) return;
+  const int at = w.at[r];
+  float l = 0.f, v = 0.f;
+  if (at >= 0) {
+    const float2 s = run[at];
+    const bool bad = w.label[at] < 0;
+    l = bad ? NAN : s.x + logf(s.y);
+    // (the sum of the label's own and the others: near a loss of zero the difference of two large numbers would be their rounding)
+    v = bad ? NAN : (s.x - picked[at]) + logf(s.y);
+  }
+  lse[r] = l;
+  loss[r] = v;
+}
+// One workgroup: the sum or the mean, in 64 bits.
+__global__ void __launch_bounds__(SCAN) k_loss_sum(const float *each, long long rows, Rows w, int reduce, float *loss) {
+  __shared__ double sums[SCAN / 64];
+  double s = 0;
+  for (long long r = threadIdx.x; r < rows; r += SCAN) s += (double)each[r];
+  s = wave_sum64(s);
+  if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = s;
+  __syncthreads();
+  if (threadIdx.x != 0) return;
+  s = 0;
+  for (int i = 0; i < SCAN / 64; ++i) s += sums[i];
+  const int64_t places = w.offsets[1];
+  loss[0] = (float)(reduce == TT_REDUCE_MEAN && places > 0 ? s / (double)places : s);
+}
+
+// dx from its sums in the order of the places; zeros in rows that do not count
+template <class T> __global__ void __launch_bounds__(TT_BLOCK) k_loss_dx(const float *acc, long long rows, int dim, Rows w, T *dx, long long ld) {
+  const int per = (dim + 3) / 4;
+  const float back = w.scale[1];
+  for (long long e = (long long)blockIdx.x * TT_BLOCK + threadIdx.x; e < rows * per; e += (long long)gridDim.x * TT_BLOCK) {
+    const long long r = e / per;
+    const int c = (int)(e - r * per) * 4, at = w.at[r];
+    float v[4] = {0.f, 0.f, 0.f, 0.f};
+    if (at >= 0) load4(acc + (long long)at * dim + c, dim - c, v);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] *= back;
+    store4(dx + r * ld + c, dim - c, v);
+  }
+}
+template <class T> __global__ void __launch_bounds__(TT_BLOCK) k_loss_clear(T *p, long long n) {
+  for (long long i = (long long)blockIdx.x * TT_BLOCK + threadIdx.x; i < n; i += (long long)gridDim.x * TT_BLOCK) p[i] = from_f32<T>(0.f);
+}
+
+// ---- host ------------------------------------------------------------------------------------------
+size_t pad256(size_t n) { return (n + 255) & ~(size_t)255; }
+size_t elem(int dtype) { return dtype == TT_F32 ? 4 : 2; }
+bool aligned(const void *p, size_t size) { return ((uintptr_t)p & (size - 1)) == 0; }
+
+tt_status check(const tt_loss *op) {
+  if (!op || op->dtype < TT_F32 || op->dtype > TT_F16 || op->reduce < TT_REDUCE_NONE || op->reduce > TT_REDUCE_MEAN || op->rows < 0) return TT_ERR_INVALID_ARG;
+  if (op->dim < 1 || op->dim > TT_DENSE_MAX_DIM || op->classes < 1 || op->classes > TT_LOSS_MAX_CLASSES || op->rows >= 2147483647LL - 2 * TT_DENSE_MAX_GROUPS)
+    return TT_ERR_SHAPE;
+  const int64_t ld[2] = {op->ld_x, op->ld_dx};
+  for (int i = 0; i < 2; ++i)
+    if (ld[i] != 0 && (ld[i] < op->dim || ld[i] > ((int64_t)1 << 40))) return TT_ERR_SHAPE;
+  return TT_OK;
+}
+
+// Classes of a piece, whole tiles of 256: of a forward one the statistics, of a backward one G has `room` bytes, about half of what the
+// last-level cache holds, so that the products that read a piece find it there.
+#ifndef TT_LOSS_ROOM
+#define TT_LOSS_ROOM (128 << 20)
+#endif
+long long piece_of(const tt_loss *op, bool backward) {
+  const long long each = backward ? op->rows * (long long)elem(op->dtype) : tt_ceil_div(op->rows * 8, 64);
+  long long most = (long long)TT_LOSS_ROOM / (each > 0 ? each : 1) / 256 * 256;
+  if (most < 256) most = 256;
+  const long long pieces = (op->classes + most - 1) / most;
+  return ((op->classes + pieces - 1) / pieces + 255) / 256 * 256;
+}
+int padded(int dim) { return (dim + 7) & ~7; }
+
+void describe(const tt_loss *op, TTGemm *g) {
+  memset(g, 0, sizeof(*g));
+  g->dtype = g->out_dtype = op->dtype;
+  g->batch = 1;
+  g->alpha = g->beta = 1.f;
+  g->parts = 3;
+}
+TTGemm of_logits(const tt_loss *op, int classes, bool backward, long long ldg) {  // rows that count by W of a piece
+  TTGemm g;
+  describe(op, &g);
+  g.a_kc = g.b_kc = 1;
+  g.mode = TT_GEMM_RAGGED_M;
+  g.M = (int)op->rows; g.N = classes; g.K = op->dim;
+  g.lda = padded(op->dim); g.ldb = op->dim; g.ldo = ldg;
+  g.epilogue = backward ? TT_GEMM_SOFTMAX : TT_GEMM_STATS;
+  g.zero_rest = backward;
+  g.n_padded = (classes + 7) & ~7;
+  return g;
+}
+TTGemm of_dx(const tt_loss *op, int classes, long long ldg) {  // G W
+  TTGemm g;
+  describe(op, &g);
+  g.a_kc = 1; g.b_kc = 0;
+  g.M = (int)op->rows; g.N = op->dim; g.K = classes;
+  g.lda = ldg; g.ldb = op->dim; g.ldo = op->dim;
+  g.a_padded = 1;
+  g.epilogue = TT_GEMM_ACC;
+  return g;
+}
+TTGemm of_dw(const tt_loss *op, int classes, long long ldg, bool column) {  // G^T x, or one column of G^T G
+  TTGemm g;
+  describe(op, &g);
+  g.a_kc = g.b_kc = 0;
+  g.M = classes; g.N = column ? 1 : op->dim; g.K = (int)op->rows;
+  g.like_N = op->dim;
+  g.lda = ldg; g.ldb = column ? ldg : padded(op->dim); g.ldo = g.N;
+  g.a_padded = 1;
+  g.epilogue = op->dtype == TT_F16 ? TT_GEMM_SCALED : TT_GEMM_PLAIN;
+  return g;
+}
+
+struct Scratch {
+  size_t of, at, label, lse, share, scale, offsets, x, stats, run, picked, each, grads, acc, column, pieces, total;
+};
+Scratch scratch(const tt_loss *op, bool backward) {
+  Scratch w = {};
+  const size_t rows = (size_t)op->rows, es = elem(op->dtype);
+  const long long piece = piece_of(op, backward);
+  auto take = [&](size_t &at, size_t bytes) {
+    at = w.total;
+    w.total += pad256(bytes);
+  };
+  take(w.of, rows * 4);
+  take(w.at, rows * 4);
+  take(w.label, rows * 4);
+  take(w.scale, 8);
+  take(w.offsets, 16);
+  take(w.x, rows * padded(op->dim) * es);
+  if (!backward) {
+    take(w.stats, (size_t)tt_ceil_div(piece, 64) * rows * 8);
+    take(w.run, rows * 8);
+    take(w.picked, rows * 4);
+    take(w.each, rows * 4);
+    return w;
+  }
+  take(w.lse, rows * 4);
+  take(w.share, rows * 4);
+  take(w.grads, rows * piece * es);
+  take(w.acc, rows * op->dim * 4);
+  take(w.column, (size_t)piece * es);
+  size_t most = 0;
+  const int last = (int)(op->classes - (op->classes - 1) / piece * piece);
+  for (int i = 0; i < 2; ++i) {
+    const int n = i ? last : (int)(piece < op->classes ? piece : op->classes);
+    const size_t need[3] = {ttk_gemm_partial_bytes(of_dx(op, n, piece)), ttk_gemm_partial_bytes(of_dw(op, n, piece, false)),
+                            ttk_gemm_partial_bytes(of_dw(op, n, piece, true))};
+    for (int k = 0; k < 3; ++k) most = need[k] > most ? need[k] : most;
+  }
+  take(w.pieces, most);
+  return w;
+}
+Rows rows_of(char *ws, const Scratch &w) {
+  return Rows{(int32_t *)(ws + w.of), (int32_t *)(ws + w.at), (int32_t *)(ws + w.label), (float *)(ws + w.lse), (float *)(ws + w.share), (float *)(ws + w.scale),
+              (int64_t *)(ws + w.offsets)};
+}
+unsigned grid_of(long long items) {
+  const long long blocks = (items + TT_BLOCK - 1) / TT_BLOCK;
+  return (unsigned)(blocks < 1 ? 1 : blocks > 16384 ? 16384 : blocks);
+}
+template <class T> tt_status gather(const tt_loss *op, const void *x, const Rows &r, void *to, hipStream_t s) {
+  const int ld = padded(op->dim), dim = op->dim;
+  const long long rows = op->rows, ld_x = op->ld_x ? op->ld_x : op->dim;
+  hipLaunchKernelGGL(k_loss_gather<T>, dim3(grid_of(rows * tt_ceil_div(ld, 16 / (int)sizeof(T)))), dim3(TT_BLOCK), 0, s, (const T *)x, ld_x, rows, dim, r,
+                     (T *)to, ld);
+  return tt_launch_status();
+}
+template <class T> tt_status write_dx(const tt_loss *op, const float *acc, const Rows &r, void *dx, hipStream_t s) {
+  const int dim = op->dim;
+  const long long rows = op->rows, ld = op->ld_dx ? op->ld_dx : op->dim;
+  hipLaunchKernelGGL(k_loss_dx<T>, dim3(grid_of(rows * tt_ceil_div(dim, 4))), dim3(TT_BLOCK), 0, s, acc, rows, dim, r, (T *)dx, ld);
+  return tt_launch_status();
+}
+template <class T> tt_status clear(void *p, long long n, hipStream_t s) {
+  hipLaunchKernelGGL(k_loss_clear<T>, dim3(grid_of(n)), dim3(TT_BLOCK), 0, s, (T *)p, n);
+  return tt_launch_status();
+}
+#define TT_BY_TYPE(call, dtype, ...) \
+  ((dtype) == TT_F32 ? call<float>(__VA_ARGS__) : (dtype) == TT_BF16 ? call<ttg::bf16>(__VA_ARGS__) : call<ttg::f16>(__VA_ARGS__))
+
+}  // namespace
+
+extern "C" size_t tt_cross_entropy_workspace_bytes(const tt_loss *op, int backward) {
+  if (check(op) != TT_OK) return 0;
+  return scratch(op, backward != 0).total;
+}
+
+extern "C" tt_status tt_cross_entropy_forward(const tt_loss *op, const void *x, const void *w, const void *bias, const int64_t *labels, float *loss, float *lse,
+                                              void *workspace, size_t workspace_bytes, void *stream) {
+  tt_status st = check(op);
+  if (st != TT_OK) return st;
+  const bool some = op->rows > 0, whole = op->reduce != TT_REDUCE_NONE;
+  if (!some && !whole) return TT_OK;
+  const size_t es = elem(op->dtype);
+  if (!loss || (some && (!x || !w || !labels || !lse))) return TT_ERR_INVALID_ARG;
+  const void *ptrs[6] = {x, w, bias, labels, loss, lse};
+  const size_t sizes[6] = {es, es, es, 8, 4, 4};
+  for (int i = 0; i < 6; ++i) {
+    if (!aligned(ptrs[i], sizes[i])) return TT_ERR_INVALID_ARG;
+    for (int j = 4; j < 6; ++j)
+      if (i < j && ptrs[j] && ptrs[i] == ptrs[j]) return TT_ERR_INVALID_ARG;
+  }
+  const Scratch need = scratch(op, false);
+  if (!workspace || ((uintptr_t)workspace & 255) != 0 || workspace_bytes < need.total) return TT_ERR_WORKSPACE;
+  hipStream_t s = (hipStream_t)stream;
+  char *ws = (char *)workspace;
+  const Rows r = rows_of(ws, need);
+  const long long rows = op->rows, ignored = op->ignore_index, piece = piece_of(op, false);
+  const int classes = op->classes, reduce = op->reduce;
+  float *each = whole ? (float *)(ws + need.each) : loss;
+  hipLaunchKernelGGL(k_loss_rows, dim3(1), dim3(SCAN), 0, s, labels, rows, classes, ignored, reduce, (const float *)nullptr, (const float *)nullptr, 0, r);
+  if ((st = tt_launch_status()) != TT_OK) return st;
+  if (some) {
+    if ((st = TT_BY_TYPE(gather, op->dtype, op, x, r, ws + need.x, s)) != TT_OK) return st;
+    float2 *run = (float2 *)(ws + need.run);
+    for (long long c = 0; c < classes; c += piece) {
+      const int n = (int)(classes - c < piece ? classes - c : piece);
+      TTGemm g = of_logits(op, n, false, 0);
+      g.a = ws + need.x;
+      g.b = (const char *)w + (size_t)c * op->dim * es;
+      g.bias = bias ? (const char *)bias + (size_t)c * es : nullptr;
+      g.offsets = r.offsets;
+      g.stats = (float *)(ws + need.stats);
+      g.picked = (float *)(ws + need.picked);
+      g.labels = r.label;
+      g.first = (int)c;
+      if ((st = ttk_gemm(g, nullptr, s)) != TT_OK) return st;
+      const int tiles = tt_ceil_div(n, ttk_gemm_tile(g)), first = c == 0;
+      hipLaunchKernelGGL(k_loss_fold, dim3((unsigned)tt_ceil_div(rows, 64)), dim3(TT_BLOCK), 0, s, (const float2 *)g.stats, tiles, rows, first, r, run);
+    }
+    hipLaunchKernelGGL(k_loss_of_rows, dim3((unsigned)tt_ceil_div(rows, TT_BLOCK)), dim3(TT_BLOCK), 0, s, rows, r, (const float2 *)run,
+                       (const float *)(ws + need.picked), each, lse);
+  }
+  if (whole) hipLaunchKernelGGL(k_loss_sum, dim3(1), dim3(SCAN), 0, s, (const float *)each, rows, r, reduce, loss);
+  return tt_launch_status();
+}
+
+extern "C" tt_status tt_cross_entropy_backward(const tt_loss *op, const void *x, const void *w, const void *bias, const int64_t *labels, const float *lse,
+                                               const float *grad_loss, void *dx, void *dw, void *dbias, void *workspace, size_t workspace_bytes,
+                                               void *stream) {
+  tt_status st = check(op);
+  if (st != TT_OK) return st;
+  if (!dx && !dw && !dbias) return TT_OK;
+  const bool some = op->rows > 0;
+  const size_t es = elem(op->dtype);
+  if (some && (!x || !w || !labels || !lse || !grad_loss)) return TT_ERR_INVALID_ARG;
+  const void *ptrs[9] = {x, w, bias, labels, lse, grad_loss, dx, dw, dbias};
+  const size_t sizes[9] = {es, es, es, 8, 4, 4, es, es, es};
+  for (int i = 0; i < 9; ++i) {
+    if (!aligned(ptrs[i], sizes[i])) return TT_ERR_INVALID_ARG;
+    for (int j = 6; j < 9; ++j)
+      if (i < j && ptrs[j] && ptrs[i] == ptrs[j]) return TT_ERR_INVALID_ARG;
+  }
+  hipStream_t s = (hipStream_t)stream;
+  if (!some) {
+    if (dw && (st = TT_BY_TYPE(clear, op->dtype, dw, (long long)op->classes * op->dim, s)) != TT_OK) return st;
+    return dbias ? TT_BY_TYPE(clear, op->dtype, dbias, (long long)op->classes, s) : TT_OK;
+  }
+  const Scratch need = scratch(op, true);
+  if (!workspace || ((uintptr_t)workspace & 255) != 0 || workspace_bytes < need.total) return TT_ERR_WORKSPACE;
+  char *ws = (char *)workspace;
+  const Rows r = rows_of(ws, need);
+  const long long rows = op->rows, ignored = op->ignore_index, piece = piece_of(op, true);
+  const int classes = op->classes, reduce = op->reduce, half = op->dtype == TT_F16;
+  hipLaunchKernelGGL(k_loss_rows, dim3(1), dim3(SCAN), 0, s, labels, rows, classes, ignored, reduce, lse, grad_loss, half, r);
+  if ((st = tt_launch_status()) != TT_OK) return st;
+  if ((st = TT_BY_TYPE(gather, op->dtype, op, x, r, ws + need.x, s)) != TT_OK) return st;
+  for (long long c = 0; c < classes; c += piece) {
+    const int n = (int)(classes - c < piece ? classes - c : piece);
+    const char *wc = (const char *)w + (size_t)c * op->dim * es;
+    TTGemm g = of_logits(op, n, true, piece);
+    g.a = ws + need.x;
+    g.b = wc;
+    g.bias = bias ? (const char *)bias + (size_t)c * es : nullptr;
+    g.offsets = r.offsets;
+    g.out = ws + need.grads;
+    g.labels = r.label;
+    g.lse = r.lse;
+    g.row_grad = r.share;
+    g.first = (int)c;
+    if ((st = ttk_gemm(g, nullptr, s)) != TT_OK) return st;
+    if (dx) {
+      TTGemm d = of_dx(op, n, piece);
+      d.a = ws + need.grads;
+      d.b = wc;
+      d.acc = (float *)(ws + need.acc);
+      d.acc_add = c > 0;
+      if ((st = ttk_gemm(d, ws + need.pieces, s)) != TT_OK) return st;
+    }
+    if (dw || dbias) {  // as in the dense operators: the sums of G's columns come beside a product
+      TTGemm d = of_dw(op, n, piece, !dw);
+      d.a = ws + need.grads;
+      d.b = dw ? ws + need.x : ws + need.grads;
+      d.out = dw ? (char *)dw + (size_t)c * op->dim * es : ws + need.column;
+      d.rowsum = dbias ? (char *)dbias + (size_t)c * es : nullptr;
+      d.scale = r.scale + 1;
+      if ((st = ttk_gemm(d, ws + need.pieces, s)) != TT_OK) return st;
+    }
+  }
+  return dx ? TT_BY_TYPE(write_dx, op->dtype, op, (const float *)(ws + need.acc), r, dx, s) : TT_OK;
+}

@@ -23,6 +23,9 @@ Two more forward routes of the library are selectable:
 product with bias, activation and residual in one kernel, and in a fused module the product grouped by table.  `tt_dense` is
 the differentiable call, `TTOrthoSGD` the optimizer whose updates of cores and dense weights are orthogonalised.
 
+What a model puts on top of the pooled rows: `tt_layer_norm` (`TTLayerNorm`), `tt_route`, `tt_expert_rows` and `tt_expert_combine`
+around products grouped by expert (`TTExperts`), and `tt_cross_entropy` against a catalogue (`TTSoftmaxLoss`).
+
 `TTFusedEmbeddingBags` holds SEVERAL tables of equal column factors and ranks as one fused TT table
 (cores side by side along the row-factor axis) and serves all of them with one reorder, one forward
 and one backward: what a model with many small tables needs to fill the GPU.
@@ -30,6 +33,7 @@ and one backward: what a model with many small tables needs to fill the GPU.
 from __future__ import annotations
 
 import math
+from typing import NamedTuple
 
 import torch
 
@@ -174,6 +178,246 @@ class TTDense(torch.nn.Module):
 
     def extra_repr(self) -> str:
         return "%d -> %d%s, %s" % (self.in_features, self.out_features, "" if self.groups is None else ", %d groups" % self.groups, self.activation)
+
+
+def _dual():
+    """Inside a level of forward-mode differentiation: the autograd functions are asked, which refuse tensors with tangents."""
+    return torch.autograd.forward_ad._current_level >= 0
+
+
+def _trained(*ts):
+    return torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in ts)
+
+
+def _packed(t):
+    return t if t is None or t.is_contiguous() else t.contiguous()
+
+
+class _NormFunction(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, eps):
+        stats = torch.empty((x.shape[0], 2), dtype=torch.float32, device=x.device)
+        out = binding.tt_layer_norm_forward(x, weight, bias, eps, stats=stats)
+        ctx.save_for_backward(x, weight, stats)
+        return out
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, grad_out):
+        x, weight, stats = ctx.saved_tensors
+        need = ctx.needs_input_grad
+        return (*binding.tt_layer_norm_backward(x, weight, stats, _row_major(grad_out), needs=need[:3]), None)
+
+
+def tt_layer_norm(x, weight=None, bias=None, eps=1e-5):
+    """Layer norm over the last dimension of x, `(x - mean) / sqrt(variance + eps) * weight + bias`, differentiable in its three
+    tensors; weight and bias have x's type.  For training the mean and the deviation of each row are kept in float32."""
+    rows = x if x.dim() == 2 else x.reshape(-1, x.shape[-1])
+    rows, weight, bias = _row_major(rows), _packed(weight), _packed(bias)
+    if not _trained(x, weight, bias) and not _dual():
+        out = binding.tt_layer_norm_forward(rows, weight, bias, eps)
+    else:
+        out = _NormFunction.apply(rows, weight, bias, eps)
+    return out if x.dim() == 2 else out.view(x.shape)
+
+
+class TTLayerNorm(torch.nn.Module):
+    """Layer norm over the last dimension, of `features` elements: float32, bfloat16 or float16."""
+
+    def __init__(self, features: int, eps: float = 1e-5, affine: bool = True, device="cuda", dtype=torch.float32):
+        super().__init__()
+        if dtype not in binding.DTYPES:
+            raise ValueError("dtype is float32, bfloat16 or float16")
+        self.features, self.eps = int(features), float(eps)
+        self.weight = torch.nn.Parameter(torch.ones(self.features, dtype=dtype, device=device)) if affine else None
+        self.bias = torch.nn.Parameter(torch.zeros(self.features, dtype=dtype, device=device)) if affine else None
+
+    def forward(self, x):
+        if x.shape[-1] != self.features:
+            raise ValueError("the last dimension must be %d, got %d" % (self.features, x.shape[-1]))
+        return tt_layer_norm(x, self.weight, self.bias, self.eps)
+
+    def extra_repr(self) -> str:
+        return "%d, eps=%g%s" % (self.features, self.eps, "" if self.weight is not None else ", no weight")
+
+
+class Routes(NamedTuple):
+    """Where the rows of a batch go: `weights` (float32) and `experts` (int64, -1: none) [rows, k], and the choices in the experts'
+    order: `offsets` (int64 [experts + 1]), `slots` (int32 [rows, k], each choice's place, -1: none) and `sources` (int32
+    [rows * k], each place's choice, -1 behind the last one)."""
+    weights: torch.Tensor
+    experts: torch.Tensor
+    offsets: torch.Tensor
+    slots: torch.Tensor
+    sources: torch.Tensor
+
+
+class _RouteFunction(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, logits, k, bias, scores, groups, top_groups, renormalize, scale):
+        experts, weights = binding.tt_route_forward(logits, k, bias, scores, groups, top_groups, renormalize, scale)
+        ctx.how = dict(scores=scores, renormalize=renormalize, scale=scale)
+        ctx.save_for_backward(logits, experts)
+        ctx.mark_non_differentiable(experts)
+        return weights, experts
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, grad_weights, _):
+        logits, experts = ctx.saved_tensors
+        return (binding.tt_route_backward(logits, experts, grad_weights.contiguous(), **ctx.how),) + (None,) * 7
+
+
+def tt_route(logits, k: int, bias=None, scores: str = "softmax", groups: int = 1, top_groups=None, renormalize: bool = False, scale: float = 1.0) -> Routes:
+    """The `Routes` of rows by their logits [rows, experts], as `binding.tt_route_forward` chooses them; the weights are
+    differentiable in the logits (`bias`, float32 [experts], chooses only and gets no gradient)."""
+    logits = _row_major(logits)
+    bias = None if bias is None else _packed(bias.detach())
+    if not _trained(logits) and not _dual():
+        experts, weights = binding.tt_route_forward(logits, k, bias, scores, groups, top_groups, renormalize, scale)
+    else:
+        weights, experts = _RouteFunction.apply(logits, k, bias, scores, groups, top_groups, renormalize, scale)
+    return Routes(weights, experts, *binding.tt_expert_order(experts, logits.shape[1]))
+
+
+class _RowsFunction(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, slots, sources):
+        ctx.save_for_backward(slots)
+        return binding.tt_expert_rows(x, slots, sources)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, grad_out):
+        (slots,) = ctx.saved_tensors
+        return binding.tt_expert_combine(_row_major(grad_out), slots), None, None
+
+
+def tt_expert_rows(x, routes: Routes):
+    """The rows of x [rows, dim] in the experts' order, [rows * k, dim]: what `tt_dense` takes with `routes.offsets`.  Places without
+    a source are zeros."""
+    x = _row_major(x)
+    if not _trained(x) and not _dual():
+        return binding.tt_expert_rows(x, routes.slots, routes.sources)
+    return _RowsFunction.apply(x, routes.slots, routes.sources)
+
+
+class _CombineFunction(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, y, weights, residual, slots, sources):
+        ctx.has_residual = residual is not None
+        ctx.save_for_backward(y, weights, slots, sources)
+        return binding.tt_expert_combine(y, slots, weights, residual)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, grad_out):
+        y, weights, slots, sources = ctx.saved_tensors
+        need = ctx.needs_input_grad
+        dy = dw = None
+        if need[0] or need[1]:
+            dy, dw = binding.tt_expert_combine_backward(y, slots, sources, weights, _row_major(grad_out), needs=need[:2])
+        return dy, dw, grad_out if ctx.has_residual and need[2] else None, None, None
+
+
+def tt_expert_combine(y, routes: Routes, residual=None):
+    """`residual + sum_j weights[:, j] y[slots[:, j]]`, rows of the experts back in the batch's order; differentiable in y
+    [rows * k, dim], the weights and the residual."""
+    y, weights, residual = _row_major(y), _packed(routes.weights), _row_major(residual)
+    if not _trained(y, weights, residual) and not _dual():
+        return binding.tt_expert_combine(y, routes.slots, weights, residual)
+    return _CombineFunction.apply(y, weights, residual, routes.slots, routes.sources)
+
+
+class TTExperts(torch.nn.Module):
+    """A layer of experts: `x + sum of weight_e expert_e(norm(x))` over the `choices` experts that each row is sent to, an expert being
+    act(x W1^T + b1) W2^T + b2 of its own (`TTDense` grouped by expert: one product for all).
+
+    features, hidden   width of the rows, and between an expert's two products
+    experts, choices   experts there are, and how many a row gets
+    scores, groups, top_groups, renormalize, scale   as in `tt_route`
+    balance   a buffer that is added to the scores for choosing (zeros; a training loop may move it, it has no gradient)
+    norm, residual   layer norm before the router and the experts; the row itself added to the result
+    forward(x, mask=None): x [rows, features]; rows where mask (bool [rows]) is False go to no expert.
+    """
+
+    def __init__(self, features: int, hidden: int, experts: int, choices: int, activation: str = "silu", scores: str = "softmax", groups: int = 1,
+                 top_groups=None, renormalize: bool = True, scale: float = 1.0, balance: bool = False, norm: bool = True, residual: bool = True,
+                 device="cuda", dtype=torch.float32, generator=None):
+        super().__init__()
+        self.features, self.choices, self.residual = int(features), int(choices), bool(residual)
+        self.route = dict(scores=scores, groups=int(groups), top_groups=None if top_groups is None else int(top_groups), renormalize=bool(renormalize),
+                          scale=float(scale))
+        make = dict(device=device, dtype=dtype, generator=generator)
+        self.norm = TTLayerNorm(features, device=device, dtype=dtype) if norm else None
+        self.router = TTDense(features, experts, bias=False, **make)
+        self.up = TTDense(features, hidden, activation=activation, groups=experts, **make)
+        self.down = TTDense(hidden, features, groups=experts, **make)
+        self.register_buffer("balance", torch.zeros(experts, dtype=torch.float32, device=device) if balance else None)
+
+    def forward(self, x, mask=None):
+        h = x if self.norm is None else self.norm(x)
+        logits = self.router(h)
+        if mask is not None:
+            logits = logits.masked_fill(~mask[:, None], -math.inf)
+        routes = tt_route(logits, self.choices, bias=self.balance, **self.route)
+        y = self.down(self.up(tt_expert_rows(h, routes), routes.offsets), routes.offsets)
+        return tt_expert_combine(y, routes, x if self.residual else None)
+
+    def extra_repr(self) -> str:
+        return "%d of %d experts, %s" % (self.choices, self.router.out_features, self.route["scores"])
+
+
+class _LossFunction(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, w, bias, labels, ignore_index, reduction):
+        loss, lse = binding.tt_cross_entropy_forward(x, w, labels, bias, ignore_index, reduction)
+        ctx.how = dict(ignore_index=ignore_index, reduction=reduction)
+        ctx.save_for_backward(x, w, bias, labels, lse)
+        return loss
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, grad_loss):
+        x, w, bias, labels, lse = ctx.saved_tensors
+        need = ctx.needs_input_grad
+        grads = binding.tt_cross_entropy_backward(x, w, labels, lse, grad_loss.contiguous(), bias, needs=need[:3], **ctx.how)
+        return (*grads, None, None, None)
+
+
+def tt_cross_entropy(x, w, labels, bias=None, ignore_index: int = -100, reduction: str = "mean"):
+    """Softmax cross entropy of rows x [rows, dim] against the classes of w [classes, dim]: `logsumexp(x w^T + bias)` less the
+    label's logit, float32, differentiable in x, w and bias.  The logits are never stored: the gradients form them again, a piece of
+    the classes at a time.  reduction "none" gives [rows], "sum" and "mean" one number (the mean over rows whose label is
+    not ignore_index, 0 if there are none)."""
+    x, w, bias, labels = _row_major(x), _packed(w), _packed(bias), _packed(labels)
+    if not _trained(x, w, bias) and not _dual():
+        return binding.tt_cross_entropy_forward(x, w, labels, bias, ignore_index, reduction)[0]
+    return _LossFunction.apply(x, w, bias, labels, ignore_index, reduction)
+
+
+class TTSoftmaxLoss(torch.nn.Module):
+    """Softmax cross entropy against a catalogue of `classes` rows of its own: weight [classes, features], with `bias` [classes].
+    forward(x, labels) is `tt_cross_entropy`."""
+
+    def __init__(self, features: int, classes: int, bias: bool = False, ignore_index: int = -100, reduction: str = "mean", device="cuda",
+                 dtype=torch.float32, generator=None):
+        super().__init__()
+        if dtype not in binding.DTYPES:
+            raise ValueError("dtype is float32, bfloat16 or float16")
+        if reduction not in binding.REDUCTIONS:
+            raise ValueError("reduction is one of %s" % ", ".join(binding.REDUCTIONS))
+        self.ignore_index, self.reduction = int(ignore_index), reduction
+        w = torch.empty((int(classes), int(features)), dtype=torch.float32, device=device)
+        w.normal_(0.0, int(features) ** -0.5, generator=generator)
+        self.weight = torch.nn.Parameter(w.to(dtype))
+        self.bias = torch.nn.Parameter(torch.zeros(int(classes), dtype=dtype, device=device)) if bias else None
+
+    def forward(self, x, labels):
+        return tt_cross_entropy(x, self.weight, labels, self.bias, self.ignore_index, self.reduction)
+
+    def extra_repr(self) -> str:
+        return "%d classes, %d features, %s" % (*self.weight.shape, self.reduction)
 
 
 class _Projected(torch.nn.Module):

@@ -5,7 +5,8 @@ nothing in the product path loads what is built here.
 
   build_shared(out_dir)            -> libtt_emb_emu.so, driven through ctypes by the CPU tests
   build_harness(out_dir, sanitize) -> harness executable under "address" (+UBSan), "memory" or "thread"
-  build_dense(out_dir, tag)        -> library of the dense operators' units (matrix products, orthogonalised updates)
+  build_dense(out_dir, tag)        -> library of the dense operators' units (matrix products, orthogonalised updates; top=True: and of
+                                      norm, routing and loss)
   build_unit(out_dir, name)        -> executable of one unit test over tt_internal.h
 
 Two textual changes are made to the copies that are compiled: `extern __shared__ float x[];`
@@ -27,6 +28,7 @@ CSRC = os.path.join(ROOT, "paper_2507_14668_amd", "csrc")
 CLANG = os.environ.get("TT_EMU_CXX", "/opt/rocm/llvm/bin/clang++")
 UNITS = ("tt_api", "tt_reorder", "tt_forward", "tt_forward_mfma", "tt_forward_sample", "tt_bf16", "tt_index_graph", "tt_fuse", "tt_backward",
          "tt_backward_mfma")
+TOP_UNITS = ("tt_norm", "tt_route", "tt_expert_rows", "tt_loss")
 DENSE_UNITS = ("tt_gemm", "tt_gemm_direct", "tt_gemm_rows", "tt_dense", "tt_ortho", "tt_ortho_slice")
 
 
@@ -83,13 +85,13 @@ def build_shared(out_dir: str, tag: str = "so", defines=()) -> str:
 _dense_objects = {}  # (unit, its defines): object of this process's build
 
 
-def build_dense(out_dir: str, tag: str, defines=None) -> str:
-    """The dense operators' units as a library of their own; `defines` gives units flags ("-DNAME=value") of their own.  An
+def build_dense(out_dir: str, tag: str, defines=None, top=False) -> str:
+    """The dense operators' units as a library of their own, with `top` also those of a model's top (norm, routing, loss); `defines` gives units flags ("-DNAME=value") of their own.  An
     object is compiled once for every set of flags."""
     os.makedirs(out_dir, exist_ok=True)
     gen = os.path.join(out_dir, "gen_dense")
     if not _dense_objects:
-        _generate(gen, DENSE_UNITS)
+        _generate(gen, DENSE_UNITS + TOP_UNITS)
     base = [CLANG, "-std=c++17", "-O1", "-fPIC", "-D__HIPCC__", "-I" + HERE, "-I" + gen, "-I" + os.path.join(ROOT, "include"), "-pthread",
             "-Wno-unused-value"]
 
@@ -105,7 +107,7 @@ def build_dense(out_dir: str, tag: str, defines=None) -> str:
         return _dense_objects[unit, flags]
 
     with ThreadPoolExecutor(max_workers=8) as pool:
-        objs = list(pool.map(one, DENSE_UNITS + ("emu_runtime",)))
+        objs = list(pool.map(one, DENSE_UNITS + (TOP_UNITS if top else ()) + ("emu_runtime",)))
     lib = os.path.join(out_dir, "libtt_dense_emu_%s.so" % tag)
     subprocess.run(base + ["-shared"] + objs + ["-o", lib], check=True)
     return lib

@@ -89,6 +89,11 @@ static inline int __shfl_up(int v, int delta, int = 64) {
 static inline int __shfl(int v, int src, int width = 64) {  // src counts inside the lane's segment of `width` lanes
   return (int)(uint32_t)emu::wave_exchange((uint32_t)v, (__lane() & ~(width - 1)) | (src & (width - 1)));
 }
+static inline float __shfl(float v, int src, int width = 64) {
+  int u; memcpy(&u, &v, 4);
+  u = __shfl(u, src, width);
+  float r; memcpy(&r, &u, 4); return r;
+}
 static inline int __clz(int v) { return v ? __builtin_clz((unsigned)v) : 32; }
 static inline int __ffs(int v) { return __builtin_ffs(v); }
 static inline int __ffsll(unsigned long long v) { return __builtin_ffsll((long long)v); }
@@ -101,6 +106,17 @@ static inline unsigned long long __ballot(bool p) { return emu::wave_ballot(p); 
 static inline int __popcll(unsigned long long v) { return __builtin_popcountll(v); }
 static inline int __builtin_amdgcn_readfirstlane(int v) { return (int)(uint32_t)emu::wave_exchange((uint32_t)v, -2); }
 static inline int __builtin_amdgcn_readlane(int v, int lane) { return (int)(uint32_t)emu::wave_exchange((uint32_t)v, lane); }
+// data-parallel moves within a wavefront: from 1 to 15 lanes before in a row of 16, or the end of a row to the next row (0x142), of the
+// first half to the second (0x143); lanes without a source, and rows outside the mask, keep `old`
+static inline int __builtin_amdgcn_update_dpp(int old, int src, int ctrl, int row_mask, int, bool) {
+  const int lane = __lane(), row = lane >> 4;
+  int from = -1;
+  if (ctrl >= 0x111 && ctrl <= 0x11f) from = (lane & 15) >= (ctrl & 15) ? lane - (ctrl & 15) : -1;
+  else if (ctrl == 0x142) from = row > 0 ? 16 * row - 1 : -1;
+  else if (ctrl == 0x143) from = row > 1 ? 31 : -1;
+  const int v = (int)(uint32_t)emu::wave_exchange((uint32_t)src, from < 0 ? lane : from);
+  return from >= 0 && (row_mask >> row & 1) ? v : old;
+}
 // lanes are fibers that run one after the other between collectives: a point that orders LDS
 // accesses inside a wavefront has to be one
 static inline void __builtin_amdgcn_wave_barrier() { emu::wave_exchange(0, -1); }

@@ -1,0 +1,454 @@
+"""Layer norm, routing, the experts' rows and the softmax loss on the GPU: values against 64 bits over sizes, types and layouts; autograd,
+modules, a run of them together, streams, graphs, reproducibility and refusals."""
+import math
+
+import pytest
+import torch
+
+import top_ref as ref
+from test_top_emulation import LOSSES, ROUTES, routed
+
+pytestmark = pytest.mark.gpu
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+
+
+@pytest.fixture(scope="module")
+def tt():
+    import paper_2507_14668_amd as tt
+    return tt
+
+
+def put(t, pad=0, shift=0):
+    """t on the GPU, in rows `pad` longer and `shift` elements behind an aligned address."""
+    if t is None:
+        return None
+    wide = (*t.shape[:-1], t.shape[-1] + pad)
+    flat = torch.empty(math.prod(wide) + shift, dtype=t.dtype, device="cuda")[shift:].view(wide)
+    view = flat[..., :t.shape[-1]]
+    view.copy_(t)
+    return view
+
+
+def randn(gen, *s, std=1.0, dtype=F32):
+    return (torch.randn(*s, generator=gen) * std).to(dtype)
+
+
+def cpu(*ts):
+    return [None if t is None else t.detach().cpu() for t in ts]
+
+
+def check(got, pair, what):
+    ref.check(got.detach().cpu(), *pair, what)
+
+
+# ---- layer norm
+@pytest.mark.parametrize("rows,n", [(1, 1), (1, 512), (3, 130), (33, 128), (1000, 128), (257, 264), (7, 1024), (65, 1500), (9, 2048), (20, 4096),
+                                    (6, 8192), (5, 8193), (3, 16384), (2, 20001), (5000, 72)])
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("pad,shift", [(0, 0), (5, 1)])
+def test_layer_norm(tt, rows, n, dtype, pad, shift):
+    gen = torch.Generator().manual_seed(rows + n)
+    x, g = (randn(gen, rows, n, std=2) + randn(gen, rows, 1)).to(dtype), randn(gen, rows, n, dtype=dtype)
+    w, b = randn(gen, n, dtype=dtype), randn(gen, n, dtype=dtype)
+    want = ref.norm64(x, w, b, 1e-5, g)
+    dx, dw, db = put(x, pad, shift).requires_grad_(), put(w, 0, shift).requires_grad_(), put(b, 0, shift).requires_grad_()
+    y = tt.tt_layer_norm(dx, dw, db)
+    check(y, want["out"], "out")
+    grads = torch.autograd.grad(y, [dx, dw, db], put(g, pad, shift))
+    for got, name in zip(grads, ("dx", "dweight", "dbias")):
+        check(got, want[name], name)
+    out = torch.full((rows, n + 3), 7.0, dtype=dtype, device="cuda")
+    tt.tt_layer_norm_forward(dx, dw, db, out=out[:, :n])
+    assert torch.equal(out[:, :n], y) and bool((out[:, n:] == 7).all())
+    again = torch.autograd.grad(tt.tt_layer_norm(dx, dw, db), [dx, dw, db], put(g, pad, shift))
+    assert all(torch.equal(p, q) for p, q in zip(grads, again))
+
+
+def test_layer_norm_many_rows(tt):
+    """More rows than workgroups take at a time; the sums over rows against 64 bits."""
+    x = torch.randn(100003, 40, device="cuda")
+    g = torch.randn_like(x)
+    w = torch.randn(40, device="cuda").requires_grad_()
+    y = tt.tt_layer_norm(x, w)
+    (dw,) = torch.autograd.grad(y, w, g)
+    want = ref.norm64(x.cpu(), w.detach().cpu(), grad=g.cpu())
+    check(y, want["out"], "out")
+    check(dw, want["dweight"], "dweight")
+
+
+def test_layer_norm_of_more_dimensions_and_views(tt):
+    x = torch.randn(4, 6, 16, device="cuda").transpose(0, 1).requires_grad_()
+    y = tt.tt_layer_norm(x)
+    assert y.shape == x.shape
+    want = ref.norm64(x.detach().cpu().reshape(-1, 16), grad=torch.ones(24, 16))
+    check(y.reshape(-1, 16), want["out"], "out")
+    y.sum().backward()  # an expanded gradient
+    check(x.grad.reshape(-1, 16), want["dx"], "dx")
+    assert tt.tt_layer_norm(torch.randn(5, device="cuda")).shape == (5,)
+    assert tt.tt_layer_norm(torch.empty(0, 8, device="cuda")).shape == (0, 8)
+
+
+def differences(f, leaves, grads, eps=1e-3):
+    """Directional derivatives of f (a float64 scalar of float32 leaves) by central differences, in random directions."""
+    for leaf, grad in zip(leaves, grads):
+        d = torch.randn_like(leaf)
+        with torch.no_grad():
+            was = leaf.clone()
+            leaf.copy_(was + eps * d)
+            up = f()
+            leaf.copy_(was - eps * d)
+            down = f()
+            leaf.copy_(was)
+        yield float((up - down) / (2 * eps)), float((grad.double() * d.double()).sum()), float((grad.double() * d.double()).abs().sum())
+
+
+def test_gradients_by_differences(tt):
+    """fp32 values are good to about 1e-6 of their size, so differences over 2e-3 to about 1e-3 of a sum's terms, and the third derivative adds
+    eps^2: a hundredth of the sum of the terms' sizes is allowed."""
+    gen = torch.Generator(device="cuda").manual_seed(0)
+    f = lambda *s: torch.randn(*s, generator=gen, device="cuda")
+    x, w, b, r = f(12, 24).requires_grad_(), f(24).requires_grad_(), f(24).requires_grad_(), f(12, 24)
+    norm = lambda: (tt.tt_layer_norm(x, w, b).double() * r).sum()
+    for got, want, size in differences(norm, [x, w, b], torch.autograd.grad(norm(), [x, w, b])):
+        assert abs(got - want) < 0.01 * size
+    z, g = (4 * f(10, 8)).requires_grad_(), f(10, 3)
+    for scores in ("softmax", "sigmoid"):
+        for renorm in (True, False):
+            route = lambda: (tt.tt_route(z, 3, scores=scores, renormalize=renorm).weights.double() * g).sum()
+            for got, want, size in differences(route, [z], torch.autograd.grad(route(), [z])):
+                assert abs(got - want) < 0.01 * size
+    x, w, b = f(10, 16).requires_grad_(), f(50, 16).requires_grad_(), f(50).requires_grad_()
+    labels = torch.randint(0, 50, (10,), device="cuda", generator=gen)
+    loss = lambda: tt.tt_cross_entropy(x, w, labels, b).double()
+    for got, want, size in differences(loss, [x, w, b], torch.autograd.grad(loss(), [x, w, b]), eps=1e-2):
+        assert abs(got - want) < 0.01 * size
+
+
+# ---- routing
+@pytest.mark.parametrize("rows,num,k,dtype,scores,biased,groups,top,renorm,scale,pad", ROUTES + [
+    (500, 64, 2, F32, "softmax", False, 1, 1, True, 1.0, 0), (301, 256, 8, F32, "sigmoid", True, 8, 4, True, 2.5, 8), (700, 160, 6, BF16, "softmax", True, 8, 3, False, 16.0, 0),
+    (300, 512, 8, F16, "sigmoid", True, 16, 5, True, 1.0, 0)])
+def test_route(tt, rows, num, k, dtype, scores, biased, groups, top, renorm, scale, pad):
+    gen = torch.Generator().manual_seed(num + rows)
+    z = routed(gen, rows, num, dtype)
+    bias = torch.randint(-50, 51, (num,), generator=gen).float() * 1e-3 if biased else None
+    if biased and num > 8:
+        bias[4] = -math.inf
+    how = dict(scores=scores, renormalize=renorm, scale=scale)
+    want_w, want_e = ref.route64(z, k, bias, groups=groups, top_groups=top, **how)
+    dz = put(z, pad).requires_grad_()
+    r = tt.tt_route(dz, k, bias=put(bias), groups=groups, top_groups=top, **how)
+    assert torch.equal(r.experts.cpu(), want_e)
+    check(r.weights, (want_w, ref.weights_tol(want_w)), "weights")
+    for got, want in zip(r[2:], ref.order_ref(want_e, num)):
+        assert torch.equal(got.cpu(), want)
+    g = randn(gen, rows, k)
+    (grad,) = torch.autograd.grad(r.weights, dz, g.cuda())
+    check(grad, ref.route_backward64(z, want_e, g, **how), "dlogits")
+
+
+def test_close_scores_are_told_apart(tt):
+    """Scores whose order single precision cannot tell: the larger logit wins by one unit in its last place, whatever the bias' size."""
+    rows, num = 64, 40
+    gen = torch.Generator().manual_seed(1)
+    z = torch.randn(rows, 1, generator=gen).expand(rows, num).clone()
+    best = torch.randint(0, num, (rows,), generator=gen)
+    at = torch.arange(rows)
+    z[at, best] = torch.nextafter(z[at, best], torch.full((rows,), 9.0))
+    for scores in ("softmax", "sigmoid"):
+        r = tt.tt_route(z.cuda(), 2, bias=torch.full((num,), 0.25, device="cuda"), scores=scores)
+        assert torch.equal(r.experts[:, 0].cpu(), best)
+        assert torch.equal(r.experts[:, 1].cpu(), torch.where(best == 0, 1, 0))
+
+
+@pytest.mark.parametrize("rows,k,num", [(0, 2, 5), (1, 1, 1), (8192, 1, 64), (8193, 1, 64), (5000, 8, 256), (70001, 2, 1000), (40000, 3, 7)])
+def test_expert_order(tt, rows, k, num):
+    e = torch.randint(-1, num, (rows, k), generator=torch.Generator().manual_seed(rows))
+    if rows > 100:
+        e[7] = 2 ** 40
+        e[: rows // 2] = torch.where(e[: rows // 2] >= 0, num - 1, -1)  # crowded
+    got = tt.tt_expert_order(e.cuda(), num)
+    for g, want in zip(got, ref.order_ref(e, num)):
+        assert torch.equal(g.cpu(), want)
+
+
+# ---- the experts' rows
+@pytest.mark.parametrize("rows,k,num,n", [(1, 1, 1, 1), (1, 2, 64, 512), (48, 2, 64, 1024), (300, 3, 26, 130), (33, 8, 16, 2047), (5, 4, 9, 5000), (2000, 4, 64, 64)])
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("pad,shift", [(0, 0), (3, 1)])
+def test_expert_rows_and_combine(tt, rows, k, num, n, dtype, pad, shift):
+    gen = torch.Generator().manual_seed(rows + n)
+    e = torch.randint(-1, num, (rows, k), generator=gen)
+    offsets, slots, sources = ref.order_ref(e, num)
+    x, y, res, g, gxs = (randn(gen, r, n, dtype=dtype) for r in (rows, rows * k, rows, rows, rows * k))
+    w, some = torch.rand(rows, k, generator=gen), sources >= 0
+    y[~some] = math.nan
+    gxs[~some] = math.nan
+    leaves = [put(t, pad, shift).requires_grad_() for t in (x, y, res)] + [put(w).requires_grad_()]
+    r = tt.Routes(leaves[3], *(t.cuda() for t in (e, offsets, slots, sources)))
+    xs = tt.tt_expert_rows(leaves[0], r)
+    assert torch.equal(xs.detach().cpu()[some], ref.rows_ref(x, slots)[some]) and not xs.detach().cpu()[~some].any()
+    out = tt.tt_expert_combine(leaves[1], r, leaves[2])
+    want = ref.combine64(y, slots, w, res, g)
+    check(out, want["out"], "out")
+    dx, dy, dres, dw = torch.autograd.grad([xs, out], leaves, [put(gxs, pad, shift), put(g, pad, shift)])
+    check(dx, ref.combine64(gxs, slots)["out"], "dx")
+    ref.check(dy.cpu()[some], want["dy"][0][some], want["dy"][1][some], "dy")
+    assert not dy.cpu()[~some].any() and torch.equal(dres.cpu(), g)
+    check(dw, want["dweights"], "dweights")
+    left = torch.full((rows * k, n), 3.0, dtype=dtype, device="cuda")
+    from paper_2507_14668_amd import binding
+    binding.tt_expert_rows(leaves[0], r.slots, r.sources, out=left)
+    assert bool((left.cpu()[~some] == 3).all()) and torch.equal(left.cpu()[some], xs.detach().cpu()[some])
+
+
+# ---- the loss
+BIG = [(1, 128, 1000, F32, True, "mean", 0, 0, 0), (300, 128, 2000, F32, True, "mean", 7, 0, 0), (257, 64, 5001, BF16, True, "none", 30, 0, 0),
+       (513, 128, 20001, BF16, True, "mean", 50, 0, 0), (500, 136, 4099, F16, False, "none", 3, 8, 0), (700, 479, 1501, BF16, True, "sum", 1, 0, 1),
+       (2048, 256, 6000, BF16, False, "mean", 200, 0, 0), (1500, 72, 9001, F16, True, "mean", 0, 0, 0), (2, 1024, 3000, BF16, True, "mean", 0, 0, 0)]
+
+
+@pytest.mark.parametrize("rows,dim,classes,dtype,biased,reduction,ignored,pad,shift", LOSSES + BIG)
+def test_cross_entropy(tt, rows, dim, classes, dtype, biased, reduction, ignored, pad, shift):
+    gen = torch.Generator().manual_seed(rows + classes)
+    x, w = randn(gen, rows, dim, dtype=dtype), randn(gen, classes, dim, std=2 * dim ** -0.5, dtype=dtype)
+    b = randn(gen, classes, dtype=dtype) if biased else None
+    if biased and classes > 8:
+        b[3] = -math.inf
+    labels = torch.randint(0, classes, (rows,), generator=gen)
+    labels[labels == 3] = 0
+    skip = torch.randperm(rows, generator=gen)[:ignored]
+    labels[skip] = -7
+    x[skip] = math.nan
+    grad = randn(gen, rows) if reduction == "none" else torch.tensor(1.0 if dtype != F16 else 300.0)
+    leaves = [put(x, pad, shift), put(w, 0, shift)] + ([put(b, 0, shift)] if biased else [])
+    call = lambda: tt.tt_cross_entropy(leaves[0], leaves[1], labels.cuda(), leaves[2] if biased else None, -7, reduction)
+    evaluated = call()
+    for t in leaves:
+        t.requires_grad_()
+    loss = call()
+    assert torch.equal(loss, evaluated) and loss.dtype == F32
+    grads = torch.autograd.grad(loss, leaves, grad.cuda())
+    if rows == 0:
+        assert loss == 0 and not grads[1].any()
+        return
+    want = ref.loss64(torch.where(torch.isnan(x), torch.zeros_like(x), x), w, labels, b, -7, reduction, grad)
+    check(loss, want["loss"], "loss")
+    for got, name in zip(grads, ("dx", "dw", "dbias")):
+        check(got, want[name], name)
+    assert not grads[0][skip.cuda()].any()
+    again = torch.autograd.grad(call(), leaves, grad.cuda())
+    assert all(torch.equal(p, q) for p, q in zip(grads, again))
+
+
+def test_cross_entropy_of_frozen_parts(tt):
+    """Each leaf alone gets what it gets beside the others."""
+    gen = torch.Generator().manual_seed(3)
+    x, w, b = randn(gen, 300, 64, dtype=BF16).cuda(), randn(gen, 1000, 64, dtype=BF16).cuda(), randn(gen, 1000, dtype=BF16).cuda()
+    labels = torch.randint(0, 1000, (300,), generator=gen).cuda()
+    together = None
+    for pick in ((0, 1, 2), (0,), (1,), (0, 2)):
+        leaves = [t.clone().requires_grad_(i in pick) for i, t in enumerate((x, w, b))]
+        grads = torch.autograd.grad(tt.tt_cross_entropy(leaves[0], leaves[1], labels, leaves[2]), [leaves[i] for i in pick])
+        together = together or grads
+        for i, g in zip(pick, grads):
+            assert torch.equal(g, together[i])
+
+
+# ---- together
+def layer64(m, x, mask):
+    """TTExperts in 64 bits with autograd, from its parameters."""
+    p = {k: v.detach().double().cpu().requires_grad_() for k, v in m.named_parameters()}
+    x = x.detach().double().cpu().requires_grad_()
+    h = x
+    if m.norm is not None:
+        h = (x - x.mean(1, keepdim=True)) / (x.var(1, correction=0, keepdim=True) + m.norm.eps).sqrt() * p["norm.weight"] + p["norm.bias"]
+    logits = h @ p["router.weight"].t()
+    if mask is not None:
+        logits = logits.masked_fill(~mask.cpu()[:, None], -math.inf)
+    s = torch.sigmoid(logits) if m.route["scores"] == "sigmoid" else torch.softmax(logits, 1).nan_to_num(0.0)
+    how = dict(m.route)
+    renorm, scale = how.pop("renormalize"), how.pop("scale")
+    _, e = ref.route64(logits.detach(), m.choices, None if m.balance is None else m.balance.cpu(), **how)
+    there = e >= 0
+    pick = torch.gather(s, 1, e.clamp(min=0)) * there
+    w = scale * (pick / pick.sum(1, keepdim=True).clamp(min=1e-300) if renorm else pick)
+    out = x if m.residual else torch.zeros_like(x)
+    for j in range(m.choices):
+        for r in range(x.shape[0]):
+            if there[r, j]:
+                k = e[r, j]
+                z = h[r] @ p["up.weight"][k].t() + p["up.bias"][k]
+                y = (z * torch.sigmoid(z)) @ p["down.weight"][k].t() + p["down.bias"][k]
+                out = out + torch.zeros_like(x).index_put((torch.tensor([r]),), (w[r, j] * y)[None])
+    return out, x, p
+
+
+@pytest.mark.parametrize("how", [dict(), dict(scores="sigmoid", groups=4, top_groups=2, balance=True, scale=2.0), dict(norm=False, residual=False, renormalize=False)])
+def test_experts_layer(tt, how):
+    """norm, router, choice, the experts' products and the way back, with all gradients.  fp32 throughout: each of the seven steps is good to
+    about 1e-6 of the largest of its terms, and steps pass errors on by factors of a few (the norm of the small matrices): 1e-4 of the
+    largest value is allowed."""
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    m = tt.TTExperts(24, 40, 8, 3, generator=gen, **how)
+    if m.balance is not None:
+        m.balance.copy_(0.05 * torch.randn(8, device="cuda", generator=gen))
+    x = torch.randn(37, 24, device="cuda", generator=gen).requires_grad_()
+    mask = torch.rand(37, device="cuda", generator=gen) > 0.2
+    g = torch.randn(37, 24, device="cuda", generator=gen)
+    y = m(x, mask)
+    y.backward(g)
+    want, x64, p = layer64(m, x, mask)
+    want.backward(g.double().cpu())
+    near = lambda a, b: float((a.detach().cpu().double() - b).abs().max()) <= 1e-4 * float(b.abs().max() + 1e-3)
+    assert near(y, want.detach()) and near(x.grad, x64.grad)
+    for name, v in m.named_parameters():
+        assert near(v.grad, p[name].grad), name
+    if not m.residual:
+        assert not y[~mask].any()
+
+
+def test_a_model_of_them_learns_in_the_right_direction(tt):
+    """Bags, experts and the loss, one step of each kind of optimizer: runs, and every parameter gets a gradient."""
+    gen = torch.Generator(device="cuda").manual_seed(0)
+    bag = tt.TTEmbeddingBag(1000, 32, n=(10, 10, 10), d=(2, 4, 4), ranks=(8, 8), projection=48)
+    experts = tt.TTExperts(48, 64, 4, 2, generator=gen)
+    head = tt.TTSoftmaxLoss(48, 500, bias=True, generator=gen)
+    model = torch.nn.ModuleList([bag, experts, head])
+    opt = tt.TTOrthoSGD(model, lr=0.02)
+    idx = torch.randint(0, 1000, (64, 5), device="cuda", generator=gen)
+    labels = torch.randint(0, 500, (64,), device="cuda", generator=gen)
+    loss = head(experts(bag(idx)), labels)
+    loss.backward()
+    assert all(p.grad is not None and bool(p.grad.isfinite().all()) for p in model.parameters())
+    opt.step()
+    assert bool(head(experts(bag(idx)), labels).isfinite())
+
+
+# ---- streams, devices, graphs
+def test_another_stream(tt):
+    """Work on a given stream waits for what that stream waits for, and its memory is that stream's."""
+    side = torch.cuda.Stream()
+    x, w = torch.randn(300, 96, device="cuda"), torch.randn(700, 96, device="cuda")
+    labels = torch.randint(0, 700, (300,), device="cuda")
+    z = torch.randn(300, 64, device="cuda")
+    stats = torch.empty(300, 2, device="cuda")
+    want = [tt.tt_layer_norm_forward(x, stats=stats), *tt.tt_layer_norm_backward(x, None, stats, x, (True, True, True)), *tt.tt_cross_entropy_forward(x, w, labels),
+            *tt.tt_route_forward(z, 4)]
+    side.wait_stream(torch.cuda.current_stream())
+    got = [tt.tt_layer_norm_forward(x, stats=stats, stream=side), *tt.tt_layer_norm_backward(x, None, stats, x, (True, True, True), stream=side),
+           *tt.tt_cross_entropy_forward(x, w, labels, stream=side), *tt.tt_route_forward(z, 4, stream=side)]
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(want, got))
+    with torch.cuda.stream(side):
+        loss = tt.tt_cross_entropy(x.clone().requires_grad_(), w, labels)
+        loss.backward()
+    side.synchronize()
+    assert torch.equal(loss.detach(), want[4])
+
+
+def test_captured_and_replayed(tt):
+    """A step of norm, routing, experts and loss with its gradients in a graph: each replay, with eager work in between, gives what the eager call
+    gives on the same data."""
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    m = tt.TTExperts(64, 96, 16, 2, generator=gen, balance=True)
+    head = torch.randn(3001, 64, device="cuda", generator=gen).requires_grad_()
+    leaves = list(m.parameters()) + [head]
+    x = torch.randn(200, 64, device="cuda", generator=gen)
+    labels = torch.randint(0, 3001, (200,), device="cuda", generator=gen)
+
+    def step():
+        loss = tt.tt_cross_entropy(m(x), head, labels)
+        return [loss.detach()] + list(torch.autograd.grad(loss, leaves))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for _ in range(2):
+            step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = step()
+    for i in range(4):
+        x.copy_(torch.randn(200, 64, device="cuda", generator=gen))
+        labels.copy_(torch.randint(0, 3001, (200,), device="cuda", generator=gen))
+        labels[:i] = -100
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in captured]
+        want = step()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), i
+
+
+def test_two_graphs_share_no_memory(tt):
+    """Two captured losses replayed side by side on two streams, each with the workspace of its own capture."""
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    w = torch.randn(2000, 64, device="cuda", generator=gen)
+    calls, graphs, outs = [], [], []
+    for i in range(2):
+        x = torch.randn(300, 64, device="cuda", generator=gen).requires_grad_()
+        labels = torch.randint(0, 2000, (300,), device="cuda", generator=gen)
+        calls.append((x, labels))
+    run = lambda x, labels: torch.autograd.grad(tt.tt_cross_entropy(x, w, labels), x)[0]
+    want = [run(*c) for c in calls]
+    torch.cuda.synchronize()
+    for c in calls:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            outs.append(run(*c))
+        graphs.append(graph)
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for _ in range(5):
+        for s, graph in zip(streams, graphs):
+            with torch.cuda.stream(s):
+                graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs, want))
+
+
+def test_refusals(tt):
+    x, w = torch.randn(4, 8, device="cuda"), torch.randn(10, 8, device="cuda")
+    labels, z = torch.zeros(4, dtype=torch.int64, device="cuda"), torch.randn(4, 6, device="cuda")
+    r = tt.tt_route(z, 2)
+    with pytest.raises(TypeError):
+        tt.tt_layer_norm(x.cpu())
+    with pytest.raises(TypeError):
+        tt.tt_layer_norm(x, torch.ones(8, dtype=BF16, device="cuda"))
+    with pytest.raises(TypeError):
+        tt.tt_layer_norm(x.double())
+    with pytest.raises(ValueError):
+        tt.tt_layer_norm(x, torch.ones(9, device="cuda"))
+    with pytest.raises(tt.TTError):
+        tt.tt_layer_norm(x, eps=-1.0)
+    with pytest.raises(tt.TTError):
+        tt.tt_layer_norm_forward(x, out=x)
+    with pytest.raises(ValueError):
+        tt.tt_route(z, 2, scores="tanh")
+    for bad in (dict(k=7), dict(k=0), dict(k=2, groups=4), dict(k=2, groups=2, top_groups=3), dict(k=2, scale=math.nan), dict(k=4, groups=2, top_groups=1)):
+        with pytest.raises(tt.TTError):
+            tt.tt_route(z, **bad)
+    with pytest.raises((TypeError, ValueError)):
+        tt.tt_route(z, 2, bias=torch.zeros(5, device="cuda"))
+    with pytest.raises(TypeError):
+        tt.tt_route(z, 2, bias=torch.zeros(6, dtype=BF16, device="cuda"))
+    with pytest.raises(ValueError):
+        tt.tt_expert_rows(torch.randn(5, 8, device="cuda"), r)
+    with pytest.raises(ValueError):
+        tt.tt_expert_combine(torch.randn(4, 8, device="cuda"), r)
+    with pytest.raises(TypeError):
+        tt.tt_expert_combine(torch.randn(8, 8, device="cuda"), r, torch.randn(4, 8, dtype=F16, device="cuda"))
+    with pytest.raises(ValueError):
+        tt.tt_cross_entropy(x, w[:, :7], labels)
+    with pytest.raises(TypeError):
+        tt.tt_cross_entropy(x, w, labels.int())
+    with pytest.raises(ValueError):
+        tt.tt_cross_entropy(x, w, labels[:3])
+    with pytest.raises(ValueError):
+        tt.tt_cross_entropy(x, w, labels, reduction="max")
+    with pytest.raises(TypeError):
+        tt.tt_cross_entropy(x, w.bfloat16(), labels)
+    with pytest.raises(tt.TTError):
+        tt.tt_cross_entropy_forward(x, w, labels, workspace=torch.empty(256, dtype=torch.uint8, device="cuda"))
+    with pytest.raises(tt.TTError):
+        tt.tt_cross_entropy(x, w[:0], labels)

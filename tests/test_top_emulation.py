@@ -1,0 +1,510 @@
+"""Layer norm, routing, the experts' rows and the softmax loss compiled for the CPU (tests/cpu_emulation): values against 64 bits through the
+C ABI, and every refusal of an argument.  Buffers sit between guards that nothing may touch."""
+import ctypes
+import math
+import os
+import sys
+
+import pytest
+import torch
+
+import top_ref as ref
+from test_dense_emulation import BUILD_DIR, DT, Guarded, emu_build, place, ptr
+
+pytestmark = pytest.mark.skipif(not emu_build.available(), reason="host clang++ of the ROCm toolchain not found")
+ROOM = ["-DTT_LOSS_ROOM=40000"]  # several pieces of the classes
+VARIANTS = {"as it is": ("top", {}), "pieces, large tiles": ("top_large", dict(tt_loss=ROOM, tt_gemm=["-DTT_GEMM_LARGE_TILES=1"])),
+            "pieces, direct tiles": ("top_direct", dict(tt_loss=ROOM, tt_gemm_direct=["-DTT_GEMM_DIRECT_TILES=1", "-DTT_GEMM_DIRECT_LEAST=0"]))}
+F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
+
+
+def load(tag):
+    from paper_2507_14668_amd import binding
+    lib = ctypes.CDLL(emu_build.build_dense(BUILD_DIR, *VARIANTS[tag], top=True))
+    real = binding.load_library()
+    for name in binding.EXPORTS:
+        if hasattr(lib, name) and any(name.startswith("tt_" + s) for s in ("layer", "route", "expert", "cross")):
+            getattr(lib, name).restype, getattr(lib, name).argtypes = getattr(real, name).restype, getattr(real, name).argtypes
+    return lib
+
+
+@pytest.fixture(scope="module")
+def lib():
+    return load("as it is")
+
+
+@pytest.fixture(scope="module", params=VARIANTS)
+def loss_lib(request):
+    return load(request.param)
+
+
+def randn(gen, *s, std=1.0, dtype=F32):
+    return (torch.randn(*s, generator=gen) * std).to(dtype)
+
+
+def intact(*gs):
+    assert all(g is None or g.intact() for g in gs)
+
+
+# ---- layer norm
+@pytest.mark.parametrize("rows,n,dtype,affine,pad,shift", [
+    (1, 1, F32, True, 0, 0), (3, 7, BF16, True, 1, 1), (5, 64, F32, True, 0, 0), (70, 128, F32, True, 0, 0), (19, 130, F16, True, 3, 1),
+    (9, 128, BF16, False, 0, 0), (6, 256, BF16, True, 8, 0), (4, 300, F32, True, 0, 3), (3, 1025, F32, True, 0, 0), (3, 2047, BF16, True, 5, 1),
+    (2, 2050, F32, True, 0, 0), (2, 4100, F16, True, 0, 0), (2, 8200, BF16, True, 0, 0), (2, 8200, F32, True, 1, 0), (2, 16400, BF16, True, 0, 1),
+    (600, 24, F32, True, 0, 0), (0, 16, F32, True, 0, 0)])
+def test_layer_norm(lib, rows, n, dtype, affine, pad, shift):
+    from paper_2507_14668_amd import binding
+    gen = torch.Generator().manual_seed(rows * 7 + n)
+    x, grad = (randn(gen, rows, n, std=2) + randn(gen, rows, 1)).to(dtype), randn(gen, rows, n, dtype=dtype)
+    w, b = (randn(gen, n, dtype=dtype), randn(gen, n, dtype=dtype)) if affine else (None, None)
+    gx, gg, gw, gb = place(x, n + pad, shift), place(grad, n + pad, shift), place(w, None, shift), place(b, None, shift)
+    out, dx = Guarded((rows, n), dtype, n + pad, offset=shift), Guarded((rows, n), dtype, n + pad, offset=shift)
+    dw, db, stats = Guarded((1, n), dtype, offset=shift), Guarded((1, n), dtype, offset=shift), Guarded((max(rows, 1), 2), F32)
+    op = binding.CNorm(DT[dtype], n, rows, n + pad, n + pad, n + pad, n + pad, 1e-5)
+    want = ref.norm64(x, w, b, 1e-5, grad)
+    assert lib.tt_layer_norm_forward(ctypes.byref(op), gx.ptr, ptr(gw), ptr(gb), out.ptr, stats.ptr, None) == 0
+    ws = Guarded((1, max(1, lib.tt_layer_norm_workspace_bytes(ctypes.byref(op)))), torch.uint8)
+    assert lib.tt_layer_norm_backward(ctypes.byref(op), gx.ptr, ptr(gw), stats.ptr, gg.ptr, dx.ptr, dw.ptr, db.ptr, ws.ptr, ws.cols, None) == 0
+    if rows:
+        ref.check(out.t, *want["out"], "out")
+        ref.check(dx.t, *want["dx"], "dx")
+        ref.check(dw.t[0], *want["dweight"], "dweight")
+        ref.check(db.t[0], *want["dbias"], "dbias")
+        alone = Guarded((1, n), dtype)
+        assert lib.tt_layer_norm_backward(ctypes.byref(op), gx.ptr, ptr(gw), stats.ptr, gg.ptr, None, alone.ptr, None, ws.ptr, ws.cols, None) == 0
+        assert torch.equal(alone.t, dw.t)
+        alone = Guarded((rows, n), dtype, n + pad)
+        assert lib.tt_layer_norm_backward(ctypes.byref(op), gx.ptr, ptr(gw), stats.ptr, gg.ptr, alone.ptr, None, None, None, 0, None) == 0
+        assert torch.equal(alone.t, dx.t)
+        intact(alone)
+    else:
+        assert not dw.t.any() and not db.t.any()
+    intact(gx, gg, gw, gb, out, dx, dw, db, stats, ws)
+
+
+def test_layer_norm_special_rows(lib):
+    """Rows of equal values, infinities, NaN, numbers at the type's ends: each in its own row only."""
+    from paper_2507_14668_amd import binding
+    n = 40
+    x = torch.randn(6, n, generator=torch.Generator().manual_seed(0))
+    x[1], x[2, 3], x[3, 5], x[4] = 7.0, math.inf, math.nan, 0.0
+    out, op = torch.empty_like(x), binding.CNorm(0, n, 6, eps=1e-5)
+    assert lib.tt_layer_norm_forward(ctypes.byref(op), x.data_ptr(), None, None, out.data_ptr(), None, None) == 0
+    good = torch.tensor([0, 1, 4, 5])
+    want = ref.norm64(x[good], eps=1e-5)
+    ref.check(out[good], *want["out"], "out")
+    assert not out[1].any() and not out[4].any()
+    assert out[3].isnan().all() and out[2].isnan().any()
+
+
+def test_layer_norm_refusals(lib):
+    from paper_2507_14668_amd import binding
+    x, out, st, ws = torch.zeros(4, 8), torch.zeros(4, 8), torch.zeros(4, 2), torch.zeros(1 << 16, dtype=torch.uint8)
+    w = torch.zeros(8)
+    at = ws.data_ptr() + -ws.data_ptr() % 256
+
+    def forward(x=x.data_ptr(), w=w.data_ptr(), b=None, out=out.data_ptr(), stats=None, **kw):
+        op = binding.CNorm(0, 8, 4, eps=1e-5)
+        for k, v in kw.items():
+            setattr(op, k, v)
+        return lib.tt_layer_norm_forward(ctypes.byref(op), x, w, b, out, stats, None)
+    assert forward() == 0
+    for bad in (dict(x=None), dict(out=None), dict(out=x.data_ptr()), dict(out=w.data_ptr()), dict(x=x.data_ptr() + 2), dict(dtype=3), dict(dtype=-1), dict(rows=-1),
+                dict(eps=-1.0), dict(eps=math.nan), dict(eps=math.inf), dict(stats=out.data_ptr()), dict(stats=x.data_ptr())):
+        assert forward(**bad) == binding.TT_ERR_INVALID_ARG, bad
+    for bad in (dict(dim=0), dict(dim=(1 << 20) + 1), dict(rows=2 ** 31 - 1), dict(ld_x=7), dict(ld_out=7), dict(ld_out=1 << 41)):
+        assert forward(**bad) == binding.TT_ERR_SHAPE, bad
+    assert lib.tt_layer_norm_forward(None, None, None, None, None, None, None) == binding.TT_ERR_INVALID_ARG
+    dx, dw = torch.zeros(4, 8), torch.zeros(8)
+
+    def backward(x=x.data_ptr(), stats=st.data_ptr(), g=out.data_ptr(), dx=dx.data_ptr(), dw=dw.data_ptr(), db=None, ws=at, size=4096):
+        op = binding.CNorm(0, 8, 4, eps=1e-5)
+        return lib.tt_layer_norm_backward(ctypes.byref(op), x, w.data_ptr(), stats, g, dx, dw, db, ws, size, None)
+    assert backward() == 0
+    for bad in (dict(x=None), dict(stats=None), dict(g=None), dict(dx=out.data_ptr()), dict(dw=dx.data_ptr()), dict(db=dw.data_ptr()), dict(dw=st.data_ptr())):
+        assert backward(**bad) == binding.TT_ERR_INVALID_ARG, bad
+    for bad in (dict(ws=None), dict(ws=at + 16), dict(size=8)):
+        assert backward(**bad) == binding.TT_ERR_WORKSPACE, bad
+
+
+# ---- routing
+ROUTES = [
+    # rows, experts, k, dtype, scores, bias, groups, top, renorm, scale, pad
+    (1, 1, 1, F32, "softmax", False, 1, 1, True, 1.0, 0),
+    (9, 5, 5, F32, "softmax", False, 1, 1, False, 1.0, 0),
+    (33, 26, 3, BF16, "softmax", True, 1, 1, False, 1.0, 3),
+    (17, 64, 2, F32, "sigmoid", True, 1, 1, True, 2.5, 0),
+    (12, 65, 4, F16, "softmax", False, 1, 1, True, 1.0, 1),
+    (10, 128, 8, BF16, "sigmoid", False, 4, 2, True, 1.0, 0),
+    (14, 256, 8, F32, "sigmoid", True, 8, 4, True, 2.5, 0),
+    (8, 300, 64, F32, "softmax", True, 1, 1, True, 1.0, 0),
+    (9, 36, 4, F32, "softmax", True, 4, 1, False, 1.0, 0),
+    (6, 64, 3, F32, "softmax", True, 64, 5, True, 1.0, 0),     # groups of one
+    (5, 1024, 7, BF16, "sigmoid", True, 2, 1, False, 1.0, 0),
+    (7, 51, 6, F32, "softmax", True, 3, 3, True, 1.0, 0),      # all groups stay
+    (11, 264, 2, F16, "sigmoid", True, 33, 2, True, 1.0, 0),   # more groups than half a wavefront
+]
+
+
+def routed(gen, rows, num, dtype, masked=True):
+    z = randn(gen, rows, num, std=1.5) + randn(gen, num, std=0.5)
+    if masked and rows > 4:
+        z[torch.rand(rows, num, generator=gen) < 0.2] = -math.inf
+        z[1] = -math.inf                       # padding
+        z[2, 1:] = -math.inf                   # one expert is left
+        z[3] = 0.25                            # all the same
+    return z.to(dtype)
+
+
+@pytest.mark.parametrize("rows,num,k,dtype,scores,biased,groups,top,renorm,scale,pad", ROUTES)
+def test_route(lib, rows, num, k, dtype, scores, biased, groups, top, renorm, scale, pad):
+    from paper_2507_14668_amd import binding
+    gen = torch.Generator().manual_seed(num + rows)
+    z = routed(gen, rows, num, dtype)
+    bias = torch.randint(-50, 51, (num,), generator=gen).float() * 1e-3 if biased else None
+    if biased and num > 8:
+        bias[4] = -math.inf
+    how = dict(scores=scores, renormalize=renorm, scale=scale)
+    want_w, want_e = ref.route64(z, k, bias, groups=groups, top_groups=top, **how)
+    op = binding.CRoute(DT[dtype], binding.SCORES[scores], rows, num, k, groups, top, int(renorm), scale, num + pad, num + pad)
+    gz, gb = place(z, num + pad), place(bias[None] if biased else None)
+    e, w = Guarded((rows, k), torch.int64), Guarded((rows, k), F32)
+    assert lib.tt_route_forward(ctypes.byref(op), gz.ptr, ptr(gb), e.ptr, w.ptr, None) == 0
+    assert torch.equal(e.t, want_e)
+    ref.check(w.t, want_w, ref.weights_tol(want_w), "weights")
+    g = randn(gen, rows, k)
+    gg, dz = place(g), Guarded((rows, num), dtype, num + pad)
+    assert lib.tt_route_backward(ctypes.byref(op), gz.ptr, e.ptr, gg.ptr, dz.ptr, None) == 0
+    ref.check(dz.t, *ref.route_backward64(z, e.t, g, **how), "dlogits")
+    intact(gz, gb, e, w, gg, dz)
+
+
+def test_route_specials(lib):
+    """Ties to the lowest number, NaN first and seen, +infinity, scores that underflow, scores that differ in their last bits."""
+    from paper_2507_14668_amd import binding
+    z = torch.zeros(6, 8)
+    z[1, 5] = math.nan
+    z[2, 5] = math.inf
+    z[3] = torch.tensor([0.0, -1e4, -1e4, -1e4, -math.inf, -1e4, -1e4, -1e4])
+    z[4] = torch.tensor([1.0, 1.0 + 2.0 ** -23, 1.0, 1.0 + 2.0 ** -23, 0, 0, 0, 0])
+    z[5, 2], z[5, 6] = math.nan, 3.0
+    bias = torch.zeros(8)
+    for scores in ("softmax", "sigmoid"):
+        op = binding.CRoute(0, binding.SCORES[scores], 6, 8, 3, 1, 1, 0, 1.0)
+        e, w = torch.empty(6, 3, dtype=torch.int64), torch.empty(6, 3)
+        assert lib.tt_route_forward(ctypes.byref(op), z.data_ptr(), bias.data_ptr(), e.data_ptr(), w.data_ptr(), None) == 0
+        assert e[0].tolist() == [0, 1, 2] and e[4].tolist() == [1, 3, 0] and e[3].tolist() == [0, 1, 2]
+        if scores == "sigmoid":
+            assert e[1].tolist() == [5, 0, 1] and w[1, 0].isnan() and not w[1, 1:].isnan().any()
+            assert e[2].tolist() == [5, 0, 1] and w[2, 0] == 1
+            assert e[5].tolist() == [2, 6, 0]
+        else:
+            assert w[1].isnan().all() and w[2].isnan().all() and w[5].isnan().all()
+            assert w[3].tolist() == [1.0, 0.0, 0.0]
+    # a number twice in the caller's own choice: both gradients
+    op = binding.CRoute(0, 1, 1, 4, 3, 1, 1, 0, 1.0)
+    e, g, z, dz = torch.tensor([[2, 2, 7]]), torch.tensor([[1.0, 2.0, 4.0]]), torch.zeros(1, 4), torch.empty(1, 4)
+    assert lib.tt_route_backward(ctypes.byref(op), z.data_ptr(), e.data_ptr(), g.data_ptr(), dz.data_ptr(), None) == 0
+    assert dz.tolist() == [[0.0, 0.0, 0.75, 0.0]]
+
+
+def test_route_refusals(lib):
+    from paper_2507_14668_amd import binding
+    z, b, e, w, dz = torch.zeros(4, 8), torch.zeros(8), torch.zeros(4, 2, dtype=torch.int64), torch.zeros(4, 2), torch.zeros(4, 8)
+    inval, shape = binding.TT_ERR_INVALID_ARG, binding.TT_ERR_SHAPE
+
+    def call(z=z.data_ptr(), b=b.data_ptr(), e=e.data_ptr(), w=w.data_ptr(), **kw):
+        op = binding.CRoute(0, 0, 4, 8, 2, 1, 1, 1, 1.0)
+        for k, v in kw.items():
+            setattr(op, k, v)
+        return lib.tt_route_forward(ctypes.byref(op), z, b, e, w, None)
+    assert call() == 0
+    for bad in (dict(z=None), dict(e=None), dict(w=None), dict(z=z.data_ptr() + 1), dict(e=e.data_ptr() + 4), dict(b=b.data_ptr() + 2), dict(w=b.data_ptr()),
+                dict(e=z.data_ptr()), dict(w=e.data_ptr()), dict(dtype=7), dict(scores=2), dict(rows=-1), dict(renormalize=2), dict(scale=math.inf), dict(scale=math.nan)):
+        assert call(**bad) == inval, bad
+    for bad in (dict(experts=0), dict(experts=1025), dict(choices=0), dict(choices=9), dict(groups=3), dict(groups=0), dict(top_groups=2), dict(top_groups=0),
+                dict(groups=8, top_groups=1), dict(ld_logits=7), dict(rows=2 ** 30)):
+        assert call(**bad) == shape, bad
+    op = binding.CRoute(0, 0, 4, 8, 2, 1, 1, 1, 1.0)
+    back = lambda z=z.data_ptr(), e=e.data_ptr(), g=w.data_ptr(), d=dz.data_ptr(): lib.tt_route_backward(ctypes.byref(op), z, e, g, d, None)
+    assert back() == 0
+    for bad in (dict(z=None), dict(e=None), dict(g=None), dict(d=None), dict(d=z.data_ptr()), dict(d=w.data_ptr())):
+        assert back(**bad) == inval, bad
+
+
+@pytest.mark.parametrize("rows,k,num", [(0, 3, 5), (1, 1, 1), (1, 2, 64), (40, 4, 7), (700, 3, 26), (300, 8, 1024), (8192, 1, 3), (2049, 4, 100), (4500, 3, 1000)])
+@pytest.mark.parametrize("spread", [True, False])
+def test_expert_order(lib, rows, k, num, spread):
+    gen = torch.Generator().manual_seed(rows + num)
+    e = torch.randint(-1, num + 1, (rows, k), generator=gen) if spread else torch.full((rows, k), num // 2, dtype=torch.int64)
+    if spread and rows > 10:
+        e[3], e[4] = 2 ** 40, -2 ** 63
+    offsets, slots, sources = (Guarded((1, max(1, n)), t) for n, t in ((num + 1, torch.int64), (rows * k, torch.int32), (rows * k, torch.int32)))
+    need = lib.tt_expert_order_workspace_bytes(rows * k, num)
+    assert (need > 0) == (rows * k > 8192)
+    ge, ws = place(e) if rows else Guarded((1, 1), torch.int64), Guarded((1, max(1, need)), torch.uint8)
+    assert lib.tt_expert_order(ge.ptr, rows * k, num, offsets.ptr, slots.ptr, sources.ptr, ws.ptr, need, None) == 0
+    want = ref.order_ref(e, num)
+    assert torch.equal(offsets.t[0], want[0])
+    if rows:
+        assert torch.equal(slots.t[0].view(rows, k), want[1]) and torch.equal(sources.t[0], want[2])
+    intact(offsets, slots, sources, ge, ws)
+
+
+def test_expert_order_refusals(lib):
+    from paper_2507_14668_amd import binding
+    e, o = torch.zeros(20000, dtype=torch.int64), torch.zeros(9, dtype=torch.int64)
+    s, t, ws = torch.zeros(20000, dtype=torch.int32), torch.zeros(20000, dtype=torch.int32), torch.zeros(1 << 16, dtype=torch.uint8)
+    at = ws.data_ptr() + -ws.data_ptr() % 256
+
+    def call(e=e.data_ptr(), n=20000, num=8, o=o.data_ptr(), s=s.data_ptr(), t=t.data_ptr(), ws=at, size=1 << 15):
+        return lib.tt_expert_order(e, n, num, o, s, t, ws, size, None)
+    assert call() == 0
+    for bad in (dict(e=None), dict(o=None), dict(s=None), dict(t=None), dict(n=-1), dict(t=s.data_ptr()), dict(o=e.data_ptr()), dict(s=e.data_ptr()), dict(e=e.data_ptr() + 4)):
+        assert call(**bad) == binding.TT_ERR_INVALID_ARG, bad
+    for bad in (dict(num=0), dict(num=1025), dict(n=2 ** 31 - 1)):
+        assert call(**bad) == binding.TT_ERR_SHAPE, bad
+    for bad in (dict(ws=None), dict(ws=at + 8), dict(size=64)):
+        assert call(**bad) == binding.TT_ERR_WORKSPACE, bad
+
+
+# ---- the experts' rows
+@pytest.mark.parametrize("rows,k,num,n,dtype,pad,shift", [
+    (1, 1, 1, 1, F32, 0, 0), (5, 2, 3, 16, BF16, 0, 0), (37, 3, 5, 33, F16, 3, 1), (20, 4, 6, 130, F32, 0, 0), (9, 8, 16, 1000, BF16, 8, 0),
+    (3, 2, 4, 2100, F32, 0, 0), (70, 1, 9, 64, F32, 0, 0)])
+@pytest.mark.parametrize("weighted", [True, False])
+def test_expert_rows_and_combine(lib, rows, k, num, n, dtype, pad, shift, weighted):
+    from paper_2507_14668_amd import binding
+    gen = torch.Generator().manual_seed(rows + n)
+    e = torch.randint(-1, num, (rows, k), generator=gen)
+    if rows == 1:
+        e[0, 0] = 0
+    _, slots, sources = ref.order_ref(e, num)
+    x, y, res, grad = (randn(gen, r, n, dtype=dtype) for r in (rows, rows * k, rows, rows))
+    w = torch.rand(rows, k, generator=gen) if weighted else None
+    y[(sources < 0)] = math.nan  # behind the last place: read by nobody
+    op = binding.CDeal(DT[dtype], n, rows, k, 1, n + pad, n + pad, n + pad, n + pad)
+    gx, gy, gr, gg = (place(t, n + pad, shift) for t in (x, y, res, grad))
+    gs, gt, gw = place(slots), place(sources[None]), place(w)
+    out = Guarded((rows * k, n), dtype, n + pad, offset=shift)
+    want, some = ref.rows_ref(x, slots), sources >= 0
+    assert lib.tt_expert_rows(ctypes.byref(op), gx.ptr, gs.ptr, gt.ptr, out.ptr, None) == 0
+    assert torch.equal(out.t[some], want[some]) and not out.t[~some].any()
+    op.zero_rest = 0
+    left = Guarded((rows * k, n), dtype, n + pad)
+    assert lib.tt_expert_rows(ctypes.byref(op), gx.ptr, gs.ptr, None, left.ptr, None) == 0
+    assert torch.equal(left.t[some], want[some]) and bool((left.t[~some].contiguous().view(torch.uint8) == 0xFF).all())
+    c = Guarded((rows, n), dtype, n + pad, offset=shift)
+    want = ref.combine64(y, slots, w, res, grad)
+    assert lib.tt_expert_combine(ctypes.byref(op), gy.ptr, gs.ptr, ptr(gw), gr.ptr, c.ptr, None) == 0
+    ref.check(c.t, *want["out"], "out")
+    assert lib.tt_expert_combine(ctypes.byref(op), gy.ptr, gs.ptr, ptr(gw), gr.ptr, gr.ptr, None) == 0  # in place of the residual
+    assert torch.equal(gr.t, c.t)
+    dy, dw = Guarded((rows * k, n), dtype, n + pad, offset=shift), Guarded((rows, k), F32)
+    assert lib.tt_expert_combine_backward(ctypes.byref(op), gy.ptr, gs.ptr, gt.ptr, ptr(gw), gg.ptr, dy.ptr, dw.ptr, None) == 0
+    ref.check(dy.t[some], want["dy"][0][some], want["dy"][1][some], "dy")
+    assert not dy.t[~some].any()
+    ref.check(dw.t, *want["dweights"], "dweights")
+    alone = Guarded((rows, k), F32)
+    assert lib.tt_expert_combine_backward(ctypes.byref(op), gy.ptr, gs.ptr, None, ptr(gw), gg.ptr, None, alone.ptr, None) == 0
+    assert torch.equal(alone.t, dw.t)
+    alone = Guarded((rows * k, n), dtype, n + pad)
+    assert lib.tt_expert_combine_backward(ctypes.byref(op), None, gs.ptr, gt.ptr, ptr(gw), gg.ptr, alone.ptr, None, None) == 0
+    assert torch.equal(alone.t, dy.t)
+    intact(gx, gy, gr, gg, gs, gt, gw, out, left, c, dy, dw)
+
+
+def test_places_outside_count_as_none(lib):
+    from paper_2507_14668_amd import binding
+    x, slots = torch.randn(2, 8), torch.tensor([[0, 99], [-7, 2]], dtype=torch.int32)
+    sources = torch.tensor([0, -1, 3, 99], dtype=torch.int32)
+    op = binding.CDeal(0, 8, 2, 2, 1)
+    out, c = Guarded((4, 8), F32), Guarded((2, 8), F32)
+    assert lib.tt_expert_rows(ctypes.byref(op), x.data_ptr(), slots.data_ptr(), sources.data_ptr(), out.ptr, None) == 0
+    assert torch.equal(out.t, torch.stack([x[0], 0 * x[0], x[1], 0 * x[0]]))
+    assert lib.tt_expert_combine(ctypes.byref(op), out.ptr, slots.data_ptr(), None, None, c.ptr, None) == 0
+    assert torch.equal(c.t, x)
+    intact(out, c)
+
+
+def test_expert_rows_refusals(lib):
+    from paper_2507_14668_amd import binding
+    x, y, s, t, w = torch.zeros(4, 8), torch.zeros(8, 8), torch.zeros(4, 2, dtype=torch.int32), torch.zeros(8, dtype=torch.int32), torch.zeros(4, 2)
+    out, dw = torch.zeros(8, 8), torch.zeros(4, 2)
+    p = lambda v: v if v is None or isinstance(v, int) else v.data_ptr()
+
+    def op(kw):
+        o = binding.CDeal(0, 8, 4, 2, 1)
+        for k in list(kw):
+            if hasattr(o, k):
+                setattr(o, k, kw.pop(k))
+        return ctypes.byref(o)
+
+    def rows(**kw):
+        o = op(kw)
+        a = dict(x=x, s=s, t=t, out=out, **{})
+        a.update(kw)
+        return lib.tt_expert_rows(o, p(a["x"]), p(a["s"]), p(a["t"]), p(a["out"]), None)
+
+    def combine(**kw):
+        o = op(kw)
+        a = dict(y=y, s=s, w=w, r=None, out=out)
+        a.update(kw)
+        return lib.tt_expert_combine(o, p(a["y"]), p(a["s"]), p(a["w"]), p(a["r"]), p(a["out"]), None)
+
+    def back(**kw):
+        o = op(kw)
+        a = dict(y=y, s=s, t=t, w=w, g=x, dy=out, dw=dw)
+        a.update(kw)
+        return lib.tt_expert_combine_backward(o, p(a["y"]), p(a["s"]), p(a["t"]), p(a["w"]), p(a["g"]), p(a["dy"]), p(a["dw"]), None)
+    assert rows() == combine() == back() == 0
+    inval, shape = binding.TT_ERR_INVALID_ARG, binding.TT_ERR_SHAPE
+    for call in (rows, combine, back):
+        for bad in (dict(dim=0), dict(dim=(1 << 20) + 1), dict(choices=0), dict(choices=65), dict(ld_rows=7), dict(ld_places=7), dict(ld_dy=3), dict(rows=2 ** 30)):
+            assert call(**bad) == shape, (call, bad)
+        for bad in (dict(dtype=3), dict(rows=-1), dict(s=None), dict(s=s.data_ptr() + 2)):
+            assert call(**bad) == inval, (call, bad)
+    for bad in (dict(x=None), dict(out=None), dict(t=None), dict(out=x), dict(out=s), dict(x=x.data_ptr() + 1)):
+        assert rows(**bad) == inval, bad
+    for bad in (dict(y=None), dict(out=None), dict(out=y), dict(out=w), dict(r=out, ld_residual=16), dict(w=w.data_ptr() + 1)):
+        assert combine(**bad) == inval, bad
+    for bad in (dict(y=None), dict(g=None), dict(t=None), dict(dy=y), dict(dy=x), dict(dw=w), dict(dw=out)):
+        assert back(**bad) == inval, bad
+
+
+# ---- the loss
+LOSSES = [
+    # rows, dim, classes, dtype, bias, reduction, ignored, pad, shift
+    (1, 1, 1, F32, False, "mean", 0, 0, 0),
+    (1, 16, 70, BF16, True, "sum", 0, 0, 0),
+    (5, 24, 300, F32, True, "mean", 2, 0, 0),
+    (33, 33, 129, F16, True, "none", 5, 3, 1),
+    (70, 16, 65, BF16, False, "mean", 10, 8, 0),
+    (130, 64, 600, BF16, True, "mean", 20, 0, 0),
+    (130, 40, 521, F16, False, "none", 0, 0, 0),
+    (66, 20, 40, F32, False, "none", 60, 1, 0),
+    (9, 8, 20, F32, True, "mean", 9, 0, 0),       # no row counts
+    (300, 72, 264, F16, True, "sum", 3, 0, 0),
+    (0, 8, 20, F32, True, "mean", 0, 0, 0),
+]
+
+
+@pytest.mark.parametrize("rows,dim,classes,dtype,biased,reduction,ignored,pad,shift", LOSSES)
+def test_cross_entropy(loss_lib, rows, dim, classes, dtype, biased, reduction, ignored, pad, shift):
+    from paper_2507_14668_amd import binding
+    lib, gen = loss_lib, torch.Generator().manual_seed(rows + classes)
+    x, w = randn(gen, rows, dim, dtype=dtype), randn(gen, classes, dim, std=2 * dim ** -0.5, dtype=dtype)
+    b = randn(gen, classes, dtype=dtype) if biased else None
+    if biased and classes > 8:
+        b[3] = -math.inf  # a class that is left out
+    labels = torch.randint(0, classes, (rows,), generator=gen)
+    labels[labels == 3] = 0
+    skip = torch.randperm(rows, generator=gen)[:ignored]
+    labels[skip] = -7
+    x[skip] = math.nan  # nobody looks at them
+    grad = randn(gen, rows) if reduction == "none" else torch.tensor(1.0 if dtype != F16 else 300.0)
+    op = binding.CLoss(DT[dtype], binding.REDUCTIONS[reduction], rows, dim, classes, -7, dim + pad, dim + pad)
+    gx, gw, gb, gl = place(x, dim + pad, shift), place(w, None, shift), place(b[None] if biased else None, None, shift), place(labels[None])
+    gg = place(grad.reshape(1, -1))
+    loss, lse = Guarded((1, max(1, rows if reduction == "none" else 1)), F32), Guarded((1, max(1, rows)), F32)
+    want = ref.loss64(torch.where(torch.isnan(x), torch.zeros_like(x), x), w, labels, b, -7, reduction, grad) if rows else None
+    ws = Guarded((1, lib.tt_cross_entropy_workspace_bytes(ctypes.byref(op), 0)), torch.uint8)
+    assert lib.tt_cross_entropy_forward(ctypes.byref(op), gx.ptr, gw.ptr, ptr(gb), gl.ptr, loss.ptr, lse.ptr, ws.ptr, ws.cols, None) == 0
+    ws2 = Guarded((1, lib.tt_cross_entropy_workspace_bytes(ctypes.byref(op), 1)), torch.uint8)
+    dx, dw, db = Guarded((rows, dim), dtype, dim + pad, offset=shift), Guarded((classes, dim), dtype, offset=shift), Guarded((1, classes), dtype, offset=shift)
+    back = lambda dx, dw, db: lib.tt_cross_entropy_backward(ctypes.byref(op), gx.ptr, gw.ptr, ptr(gb), gl.ptr, lse.ptr, gg.ptr, dx, dw, db, ws2.ptr, ws2.cols, None)
+    assert back(dx.ptr, dw.ptr, db.ptr) == 0
+    if rows:
+        ref.check(loss.t[0] if reduction == "none" else loss.t[0, 0], *want["loss"], "loss")
+        ref.check(lse.t[0], *want["lse"], "lse")
+        ref.check(dx.t, *want["dx"], "dx")
+        ref.check(dw.t, *want["dw"], "dw")
+        ref.check(db.t[0], *want["dbias"], "dbias")
+        assert not dx.t[skip].any()
+        for which in range(3):  # each by itself gives the same
+            alone = [Guarded(tuple(t.t.shape), dtype, t.ld) if i == which else None for i, t in enumerate((dx, dw, db))]
+            assert back(*[ptr(t) for t in alone]) == 0
+            got, was = alone[which].t, (dx, dw, db)[which].t
+            assert torch.equal(got, was) or which == 2 and torch.allclose(got.float(), was.float(), rtol=2 * torch.finfo(dtype).eps, atol=1e-6)
+    else:
+        assert loss.t[0, 0] == 0 and not dw.t.any() and not db.t.any()
+    intact(gx, gw, gb, gl, gg, loss, lse, ws, ws2, dx, dw, db)
+
+
+def test_cross_entropy_bad_labels(lib):
+    """A label outside gives NaN, in its row's loss and in the gradients; ignore_index inside the classes is ignored."""
+    from paper_2507_14668_amd import binding
+    gen = torch.Generator().manual_seed(0)
+    x, w = randn(gen, 4, 8), randn(gen, 10, 8)
+    op = binding.CLoss(0, 0, 4, 8, 10, 3)
+    ws = Guarded((1, max(lib.tt_cross_entropy_workspace_bytes(ctypes.byref(op), i) for i in (0, 1))), torch.uint8)
+    for bad in (10, -1, 2 ** 40, -2 ** 63):
+        labels, loss, lse = torch.tensor([1, bad, 3, 9]), torch.empty(4), torch.empty(4)
+        call = (ctypes.byref(op), x.data_ptr(), w.data_ptr(), None, labels.data_ptr())
+        assert lib.tt_cross_entropy_forward(*call, loss.data_ptr(), lse.data_ptr(), ws.ptr, ws.cols, None) == 0
+        want = ref.loss64(x[[0, 3]], w, labels[[0, 3]], ignore_index=3, reduction="none")
+        ref.check(loss[[0, 3]], *want["loss"], "loss")
+        assert loss[1].isnan() and loss[2] == 0
+        grad, dx, dw = torch.ones(4), torch.empty(4, 8), torch.empty(10, 8)
+        assert lib.tt_cross_entropy_backward(*call, lse.data_ptr(), grad.data_ptr(), dx.data_ptr(), dw.data_ptr(), None, ws.ptr, ws.cols, None) == 0
+        assert dx[1].isnan().all() and not dx[[0, 2, 3]].isnan().any() and dw.isnan().all() and not dx[2].any()
+
+
+def test_cross_entropy_special_logits(lib):
+    """Large logits, a masked label, no class at all, NaN and infinities in a row."""
+    from paper_2507_14668_amd import binding
+    w, b = torch.eye(4), torch.tensor([0.0, 0.0, 0.0, -math.inf])
+    x = torch.tensor([[1e4, 0, 0, 0], [1e4, 0, 0, 0], [0, 0, 0, 5], [0, math.nan, 0, 0], [0, math.inf, 0, 0], [-3e38, 3e38, 0, 0]])
+    labels = torch.tensor([0, 1, 3, 0, 0, 1])
+    op = binding.CLoss(0, 0, 6, 4, 4, -100)
+    ws = Guarded((1, lib.tt_cross_entropy_workspace_bytes(ctypes.byref(op), 0)), torch.uint8)
+    loss, lse = torch.empty(6), torch.empty(6)
+    assert lib.tt_cross_entropy_forward(ctypes.byref(op), x.data_ptr(), w.data_ptr(), b.data_ptr(), labels.data_ptr(), loss.data_ptr(), lse.data_ptr(), ws.ptr,
+                                        ws.cols, None) == 0
+    assert loss[0] == 0 and loss[1] == 1e4 and loss[2] == math.inf and loss[3].isnan() and loss[4].isnan() and loss[5] == 0
+    b[:] = -math.inf
+    assert lib.tt_cross_entropy_forward(ctypes.byref(op), x.data_ptr(), w.data_ptr(), b.data_ptr(), labels.data_ptr(), loss.data_ptr(), lse.data_ptr(), ws.ptr,
+                                        ws.cols, None) == 0
+    assert loss.isnan().all()
+
+
+def test_cross_entropy_refusals(lib):
+    from paper_2507_14668_amd import binding
+    x, w, b, lab, loss, lse = torch.zeros(4, 8), torch.zeros(10, 8), torch.zeros(10), torch.zeros(4, dtype=torch.int64), torch.zeros(4), torch.zeros(4)
+    ws = Guarded((1, 1 << 20), torch.uint8)
+    p = lambda v: v if v is None or isinstance(v, int) else v.data_ptr()
+    inval, shape, work = binding.TT_ERR_INVALID_ARG, binding.TT_ERR_SHAPE, binding.TT_ERR_WORKSPACE
+
+    def make(kw):
+        o = binding.CLoss(0, 0, 4, 8, 10, -100)
+        for k in list(kw):
+            if hasattr(o, k):
+                setattr(o, k, kw.pop(k))
+        return ctypes.byref(o)
+
+    def forward(**kw):
+        o = make(kw)
+        a = dict(x=x, w=w, b=b, lab=lab, loss=loss, lse=lse, ws=ws.ptr, size=ws.cols)
+        a.update(kw)
+        return lib.tt_cross_entropy_forward(o, *(p(a[k]) for k in ("x", "w", "b", "lab", "loss", "lse", "ws")), a["size"], None)
+    dx, dw, db, grad = torch.zeros(4, 8), torch.zeros(10, 8), torch.zeros(10), torch.zeros(4)
+
+    def backward(**kw):
+        o = make(kw)
+        a = dict(x=x, w=w, b=b, lab=lab, lse=lse, grad=grad, dx=dx, dw=dw, db=db, ws=ws.ptr, size=ws.cols)
+        a.update(kw)
+        return lib.tt_cross_entropy_backward(o, *(p(a[k]) for k in ("x", "w", "b", "lab", "lse", "grad", "dx", "dw", "db", "ws")), a["size"], None)
+    assert forward() == backward() == 0
+    for call in (forward, backward):
+        for bad in (dict(dim=0), dict(dim=(1 << 20) + 1), dict(classes=0), dict(classes=2 ** 30 + 1), dict(rows=2 ** 31 - 1), dict(ld_x=7), dict(ld_dx=7)):
+            assert call(**bad) == shape, (call, bad)
+        for bad in (dict(dtype=3), dict(reduce=3), dict(rows=-1), dict(x=None), dict(w=None), dict(lab=None), dict(lse=None), dict(x=x.data_ptr() + 1),
+                    dict(lab=lab.data_ptr() + 4), dict(b=b.data_ptr() + 1)):
+            assert call(**bad) == inval, (call, bad)
+        for bad in (dict(ws=None), dict(ws=ws.ptr + 16), dict(size=100)):
+            assert call(**bad) == work, (call, bad)
+    for bad in (dict(loss=None), dict(loss=lse), dict(loss=x), dict(lse=w), dict(loss=lab)):
+        assert forward(**bad) == inval, bad
+    for bad in (dict(grad=None), dict(dx=x), dict(dw=w), dict(db=b), dict(dx=lse), dict(dw=dx), dict(db=dw), dict(dx=grad)):
+        assert backward(**bad) == inval, bad
+    assert lib.tt_cross_entropy_workspace_bytes(None, 0) == 0

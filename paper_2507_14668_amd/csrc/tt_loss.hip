@@ -2,24 +2,17 @@
 #include <string.h>
 
 #include "tt_gemm_device.h"
+#include "tt_loss.h"
 
 namespace {
 using namespace ttg;
 
-// Rows that count stand next to each other in the work: the products leave the others out, and whatever those hold (padding
-// may hold anything) meets nothing.
-struct Rows {
-  int32_t *of, *at;    // [rows]: row of each place, place of each row (-1: does not count)
-  int32_t *label;      // [rows] of each place; -1: no class
-  float *lse, *share;  // [rows] of each place: backward
-  float *scale;        // [2]: of G in fp16, and back
-  int64_t *offsets;    // {0, places}
-};
+typedef TTLossRows Rows;
 
 // One workgroup: places in the order of the rows.  In the backward also each place's lse and share of the loss's gradient.
 constexpr int SCAN = 512;
 __global__ void __launch_bounds__(SCAN) k_loss_rows(const int64_t *labels, long long rows, int classes, long long ignored, int reduce, const float *lse,
-                                                    const float *grad, int half, Rows w) {
+                                                    const float *grad, int bits, int half, Rows w) {
   __shared__ int tmp[SCAN / 64 + 1];
   __shared__ float tops[SCAN / 64];
   int places = 0;
@@ -55,18 +48,24 @@ __global__ void __launch_bounds__(SCAN) k_loss_rows(const int64_t *labels, long 
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < SCAN / 64; ++i) top = fmaxf(top, tops[i]);
+  // fp32 takes G as it is.  In 16 bits a share that all rows have is left for the end (rounded into each term it would be the same error in
+  // all of them); shares of their own are part of G, in fp16 times the power of two that takes the largest to 2^13 .. 2^14, as far as that and its
+  // inverse are normal numbers.  2^13 for the same reason: fp16 has a short range.
+  const bool own = reduce == TT_REDUCE_NONE;
   float scale = 1.f, back = 1.f;
-  if (half && top > 0.f) {  // the power of two that takes it to 2^13 .. 2^14, as far as that and its inverse are normal numbers
+  if (bits == 16 && own && half && top > 0.f) {
     int e = (int)(__float_as_uint(top) >> 23);
     e = e < 14 ? 14 : e > 240 ? 240 : e;
     scale = __uint_as_float((unsigned)(127 + 13 + 127 - e) << 23);
     back = __uint_as_float((unsigned)(e - 13) << 23);
   }
-  if (threadIdx.x == 0) {
-    w.scale[0] = scale;
-    w.scale[1] = back;
+  if (bits == 16 && !own) back = all * 0x1p-13f;
+  if (threadIdx.x == 0) w.back[0] = back;
+  for (int i = threadIdx.x; i < places; i += SCAN) {
+    const float share = own ? grad[w.of[i]] : all;
+    w.share[i] = share;
+    w.weight[i] = bits == 16 && !own ? 8192.f : scale * share;
   }
-  for (int i = threadIdx.x; i < places; i += SCAN) w.share[i] = scale * (reduce == TT_REDUCE_NONE ? grad[w.of[i]] : all);
 }
 
 // x's rows that count next to each other, `ld` apart (padded with zeros), zeros behind the last one.
@@ -130,7 +129,7 @@ __global__ void __launch_bounds__(SCAN) k_loss_sum(const float *each, long long 
 // dx from its sums in the order of the places; zeros in rows that do not count
 template <class T> __global__ void __launch_bounds__(TT_BLOCK) k_loss_dx(const float *acc, long long rows, int dim, Rows w, T *dx, long long ld) {
   const int per = (dim + 3) / 4;
-  const float back = w.scale[1];
+  const float back = w.back[0];
   for (long long e = (long long)blockIdx.x * TT_BLOCK + threadIdx.x; e < rows * per; e += (long long)gridDim.x * TT_BLOCK) {
     const long long r = e / per;
     const int c = (int)(e - r * per) * 4, at = w.at[r];
@@ -172,7 +171,8 @@ long long piece_of(const tt_loss *op, bool backward) {
   const long long pieces = (op->classes + most - 1) / most;
   return ((op->classes + pieces - 1) / pieces + 255) / 256 * 256;
 }
-int padded(int dim) { return (dim + 7) & ~7; }
+bool narrow(const tt_loss *op) { return ttk_narrow_serves(op->dtype, op->dim); }
+int padded(const tt_loss *op) { return narrow(op) ? ttk_narrow_padded(op->dim) : (op->dim + 7) & ~7; }
 
 void describe(const tt_loss *op, TTGemm *g) {
   memset(g, 0, sizeof(*g));
@@ -187,7 +187,7 @@ TTGemm of_logits(const tt_loss *op, int classes, bool backward, long long ldg) {
   g.a_kc = g.b_kc = 1;
   g.mode = TT_GEMM_RAGGED_M;
   g.M = (int)op->rows; g.N = classes; g.K = op->dim;
-  g.lda = padded(op->dim); g.ldb = op->dim; g.ldo = ldg;
+  g.lda = padded(op); g.ldb = op->dim; g.ldo = ldg;
   g.epilogue = backward ? TT_GEMM_SOFTMAX : TT_GEMM_STATS;
   g.zero_rest = backward;
   g.n_padded = (classes + 7) & ~7;
@@ -209,14 +209,14 @@ TTGemm of_dw(const tt_loss *op, int classes, long long ldg, bool column) {  // G
   g.a_kc = g.b_kc = 0;
   g.M = classes; g.N = column ? 1 : op->dim; g.K = (int)op->rows;
   g.like_N = op->dim;
-  g.lda = ldg; g.ldb = column ? ldg : padded(op->dim); g.ldo = g.N;
+  g.lda = ldg; g.ldb = column ? ldg : padded(op); g.ldo = g.N;
   g.a_padded = 1;
-  g.epilogue = op->dtype == TT_F16 ? TT_GEMM_SCALED : TT_GEMM_PLAIN;
+  g.epilogue = op->dtype == TT_F32 ? TT_GEMM_PLAIN : TT_GEMM_SCALED;
   return g;
 }
 
 struct Scratch {
-  size_t of, at, label, lse, share, scale, offsets, x, stats, run, picked, each, grads, acc, column, pieces, total;
+  size_t of, at, label, lse, share, weight, back, offsets, x, stats, run, picked, each, grads, acc, column, pieces, parts, total;
 };
 Scratch scratch(const tt_loss *op, bool backward) {
   Scratch w = {};
@@ -229,11 +229,11 @@ Scratch scratch(const tt_loss *op, bool backward) {
   take(w.of, rows * 4);
   take(w.at, rows * 4);
   take(w.label, rows * 4);
-  take(w.scale, 8);
+  take(w.back, 4);
   take(w.offsets, 16);
-  take(w.x, rows * padded(op->dim) * es);
+  take(w.x, rows * padded(op) * es);
   if (!backward) {
-    take(w.stats, (size_t)tt_ceil_div(piece, 64) * rows * 8);
+    take(w.stats, (narrow(op) ? (size_t)ttk_narrow_runs(op->rows, op->classes) : (size_t)tt_ceil_div(piece, 64)) * rows * 8);
     take(w.run, rows * 8);
     take(w.picked, rows * 4);
     take(w.each, rows * 4);
@@ -241,6 +241,13 @@ Scratch scratch(const tt_loss *op, bool backward) {
   }
   take(w.lse, rows * 4);
   take(w.share, rows * 4);
+  take(w.weight, rows * 4);
+  if (narrow(op)) {
+    const size_t row_runs = ttk_narrow_row_runs(op->rows, op->classes);
+    const size_t dx = (size_t)ttk_narrow_runs(op->rows, op->classes) * rows * padded(op) * 4, dw = row_runs > 1 ? row_runs * op->classes * (padded(op) + 4) * 4 : 0;
+    take(w.parts, dx > dw ? dx : dw);
+    return w;
+  }
   take(w.grads, rows * piece * es);
   take(w.acc, rows * op->dim * 4);
   take(w.column, (size_t)piece * es);
@@ -256,15 +263,18 @@ Scratch scratch(const tt_loss *op, bool backward) {
   return w;
 }
 Rows rows_of(char *ws, const Scratch &w) {
-  return Rows{(int32_t *)(ws + w.of), (int32_t *)(ws + w.at), (int32_t *)(ws + w.label), (float *)(ws + w.lse), (float *)(ws + w.share), (float *)(ws + w.scale),
-              (int64_t *)(ws + w.offsets)};
+  return TTLossRows{(int32_t *)(ws + w.of), (int32_t *)(ws + w.at), (int32_t *)(ws + w.label), (float *)(ws + w.lse), (float *)(ws + w.share), (float *)(ws + w.weight),
+              (float *)(ws + w.back), (int64_t *)(ws + w.offsets)};
+}
+TTNarrow narrow_of(const tt_loss *op, const void *w, const void *bias, char *ws, const Scratch &need) {
+  return TTNarrow{op->dtype, op->dim, padded(op), op->classes, op->rows, ws + need.x, w, bias, rows_of(ws, need)};
 }
 unsigned grid_of(long long items) {
   const long long blocks = (items + TT_BLOCK - 1) / TT_BLOCK;
   return (unsigned)(blocks < 1 ? 1 : blocks > 16384 ? 16384 : blocks);
 }
 template <class T> tt_status gather(const tt_loss *op, const void *x, const Rows &r, void *to, hipStream_t s) {
-  const int ld = padded(op->dim), dim = op->dim;
+  const int ld = padded(op), dim = op->dim;
   const long long rows = op->rows, ld_x = op->ld_x ? op->ld_x : op->dim;
   hipLaunchKernelGGL(k_loss_gather<T>, dim3(grid_of(rows * tt_ceil_div(ld, 16 / (int)sizeof(T)))), dim3(TT_BLOCK), 0, s, (const T *)x, ld_x, rows, dim, r,
                      (T *)to, ld);
@@ -313,12 +323,18 @@ extern "C" tt_status tt_cross_entropy_forward(const tt_loss *op, const void *x, 
   const long long rows = op->rows, ignored = op->ignore_index, piece = piece_of(op, false);
   const int classes = op->classes, reduce = op->reduce;
   float *each = whole ? (float *)(ws + need.each) : loss;
-  hipLaunchKernelGGL(k_loss_rows, dim3(1), dim3(SCAN), 0, s, labels, rows, classes, ignored, reduce, (const float *)nullptr, (const float *)nullptr, 0, r);
+  hipLaunchKernelGGL(k_loss_rows, dim3(1), dim3(SCAN), 0, s, labels, rows, classes, ignored, reduce, (const float *)nullptr, (const float *)nullptr, 0, 0, r);
   if ((st = tt_launch_status()) != TT_OK) return st;
   if (some) {
     if ((st = TT_BY_TYPE(gather, op->dtype, op, x, r, ws + need.x, s)) != TT_OK) return st;
     float2 *run = (float2 *)(ws + need.run);
-    for (long long c = 0; c < classes; c += piece) {
+    if (narrow(op)) {
+      const TTNarrow n = narrow_of(op, w, bias, ws, need);
+      if ((st = ttk_narrow_stats(n, (float *)(ws + need.stats), s)) != TT_OK || (st = ttk_narrow_picked(n, (float *)(ws + need.picked), s)) != TT_OK) return st;
+      const int runs = ttk_narrow_runs(rows, classes), first = 1;
+      hipLaunchKernelGGL(k_loss_fold, dim3((unsigned)tt_ceil_div(rows, 64)), dim3(TT_BLOCK), 0, s, (const float2 *)(ws + need.stats), runs, rows, first, r, run);
+    }
+    for (long long c = 0; c < classes && !narrow(op); c += piece) {
       const int n = (int)(classes - c < piece ? classes - c : piece);
       TTGemm g = of_logits(op, n, false, 0);
       g.a = ws + need.x;
@@ -366,10 +382,16 @@ extern "C" tt_status tt_cross_entropy_backward(const tt_loss *op, const void *x,
   char *ws = (char *)workspace;
   const Rows r = rows_of(ws, need);
   const long long rows = op->rows, ignored = op->ignore_index, piece = piece_of(op, true);
-  const int classes = op->classes, reduce = op->reduce, half = op->dtype == TT_F16;
-  hipLaunchKernelGGL(k_loss_rows, dim3(1), dim3(SCAN), 0, s, labels, rows, classes, ignored, reduce, lse, grad_loss, half, r);
+  const int classes = op->classes, reduce = op->reduce, bits = op->dtype == TT_F32 ? 32 : 16, half = op->dtype == TT_F16;
+  hipLaunchKernelGGL(k_loss_rows, dim3(1), dim3(SCAN), 0, s, labels, rows, classes, ignored, reduce, lse, grad_loss, bits, half, r);
   if ((st = tt_launch_status()) != TT_OK) return st;
   if ((st = TT_BY_TYPE(gather, op->dtype, op, x, r, ws + need.x, s)) != TT_OK) return st;
+  if (narrow(op)) {
+    const TTNarrow n = narrow_of(op, w, bias, ws, need);
+    float *parts = (float *)(ws + need.parts);
+    if (dx && (st = ttk_narrow_dx(n, parts, dx, op->ld_dx ? op->ld_dx : op->dim, s)) != TT_OK) return st;
+    return dw || dbias ? ttk_narrow_dw(n, reduce == TT_REDUCE_NONE, parts, dw, dbias, s) : TT_OK;
+  }
   for (long long c = 0; c < classes; c += piece) {
     const int n = (int)(classes - c < piece ? classes - c : piece);
     const char *wc = (const char *)w + (size_t)c * op->dim * es;
@@ -381,7 +403,7 @@ extern "C" tt_status tt_cross_entropy_backward(const tt_loss *op, const void *x,
     g.out = ws + need.grads;
     g.labels = r.label;
     g.lse = r.lse;
-    g.row_grad = r.share;
+    g.row_grad = r.weight;
     g.first = (int)c;
     if ((st = ttk_gemm(g, nullptr, s)) != TT_OK) return st;
     if (dx) {
@@ -398,7 +420,7 @@ extern "C" tt_status tt_cross_entropy_backward(const tt_loss *op, const void *x,
       d.b = dw ? ws + need.x : ws + need.grads;
       d.out = dw ? (char *)dw + (size_t)c * op->dim * es : ws + need.column;
       d.rowsum = dbias ? (char *)dbias + (size_t)c * es : nullptr;
-      d.scale = r.scale + 1;
+      d.scale = r.back;
       if ((st = ttk_gemm(d, ws + need.pieces, s)) != TT_OK) return st;
     }
   }

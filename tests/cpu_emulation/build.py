@@ -28,7 +28,7 @@ CSRC = os.path.join(ROOT, "paper_2507_14668_amd", "csrc")
 CLANG = os.environ.get("TT_EMU_CXX", "/opt/rocm/llvm/bin/clang++")
 UNITS = ("tt_api", "tt_reorder", "tt_forward", "tt_forward_mfma", "tt_forward_sample", "tt_bf16", "tt_index_graph", "tt_fuse", "tt_backward",
          "tt_backward_mfma")
-TOP_UNITS = ("tt_norm", "tt_route", "tt_expert_rows", "tt_loss")
+TOP_UNITS = ("tt_norm", "tt_route", "tt_expert_rows", "tt_loss", "tt_loss_narrow")
 DENSE_UNITS = ("tt_gemm", "tt_gemm_direct", "tt_gemm_rows", "tt_dense", "tt_ortho", "tt_ortho_slice")
 
 
@@ -51,7 +51,7 @@ def _generate(gen: str, units=UNITS) -> list:
         path = os.path.join(gen, u + ".cpp")
         open(path, "w").write(text)
         out.append(path)
-    headers = ("tt_internal.h",) if units == UNITS else ("tt_internal.h", "tt_gemm.h", "tt_gemm_device.h", "tt_ortho_slice.h")
+    headers = ("tt_internal.h",) if units == UNITS else ("tt_internal.h", "tt_gemm.h", "tt_gemm_device.h", "tt_ortho_slice.h", "tt_loss.h")
     for header in headers:
         shutil.copy(os.path.join(CSRC, header), gen)
     return out

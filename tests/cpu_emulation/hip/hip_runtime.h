@@ -212,6 +212,7 @@ static inline void emu_global_load_lds(const void *src, void *lds, int size, int
 #define __builtin_amdgcn_global_load_lds(src, lds, size, offset, aux) \
   emu_global_load_lds((const void *)(uintptr_t)(src), (void *)(uintptr_t)(lds), size, offset, aux)
 #define __builtin_amdgcn_rcpf(x) (1.f / (x))
+#define __builtin_amdgcn_exp2f(x) exp2f(x)
 #define __expf(x) expf(x)
 static inline void emu_waitcnt(int) {}  // loads are done at once
 #define __builtin_amdgcn_s_waitcnt(n) emu_waitcnt(n)

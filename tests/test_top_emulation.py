@@ -12,9 +12,9 @@ import top_ref as ref
 from test_dense_emulation import BUILD_DIR, DT, Guarded, emu_build, place, ptr
 
 pytestmark = pytest.mark.skipif(not emu_build.available(), reason="host clang++ of the ROCm toolchain not found")
-ROOM = ["-DTT_LOSS_ROOM=40000"]  # several pieces of the classes
-VARIANTS = {"as it is": ("top", {}), "pieces, large tiles": ("top_large", dict(tt_loss=ROOM, tt_gemm=["-DTT_GEMM_LARGE_TILES=1"])),
-            "pieces, direct tiles": ("top_direct", dict(tt_loss=ROOM, tt_gemm_direct=["-DTT_GEMM_DIRECT_TILES=1", "-DTT_GEMM_DIRECT_LEAST=0"]))}
+PIECES = dict(tt_loss=["-DTT_LOSS_ROOM=40000"], tt_loss_narrow=["-DTT_LOSS_NARROW=0"])  # several pieces of the classes, short rows among them
+VARIANTS = {"as it is": ("top", {}), "pieces, large tiles": ("top_large", dict(PIECES, tt_gemm=["-DTT_GEMM_LARGE_TILES=1"])),
+            "pieces, direct tiles": ("top_direct", dict(PIECES, tt_gemm_direct=["-DTT_GEMM_DIRECT_TILES=1", "-DTT_GEMM_DIRECT_LEAST=0"]))}
 F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
 
 
@@ -382,6 +382,8 @@ LOSSES = [
     (70, 16, 65, BF16, False, "mean", 10, 8, 0),
     (130, 64, 600, BF16, True, "mean", 20, 0, 0),
     (130, 40, 521, F16, False, "none", 0, 0, 0),
+    (270, 128, 300, BF16, True, "mean", 30, 0, 0),
+    (40, 100, 700, BF16, True, "none", 4, 0, 1),
     (66, 20, 40, F32, False, "none", 60, 1, 0),
     (9, 8, 20, F32, True, "mean", 9, 0, 0),       # no row counts
     (300, 72, 264, F16, True, "sum", 3, 0, 0),

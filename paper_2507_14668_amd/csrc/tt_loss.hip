@@ -12,7 +12,7 @@ typedef TTLossRows Rows;
 // One workgroup: places in the order of the rows.  In the backward also each place's lse and share of the loss's gradient.
 constexpr int SCAN = 512;
 __global__ void __launch_bounds__(SCAN) k_loss_rows(const int64_t *labels, long long rows, int classes, long long ignored, int reduce, const float *lse,
-                                                    const float *grad, int bits, int half, Rows w) {
+                                                    const float *grad, int bits, int half, int negative, Rows w) {
   __shared__ int tmp[SCAN / 64 + 1];
   __shared__ float tops[SCAN / 64];
   int places = 0;
@@ -26,7 +26,7 @@ __global__ void __launch_bounds__(SCAN) k_loss_rows(const int64_t *labels, long 
     if (counts) {
       w.of[at] = (int32_t)r;
       w.label[at] = label >= 0 && label < classes ? (int32_t)label : -1;
-      if (lse) w.lse[at] = lse[r];
+      if (lse) w.lse[at] = negative ? -lse[r] : lse[r];
     }
     places += total;
   }
@@ -65,6 +65,11 @@ __global__ void __launch_bounds__(SCAN) k_loss_rows(const int64_t *labels, long 
     const float share = own ? grad[w.of[i]] : all;
     w.share[i] = share;
     w.weight[i] = bits == 16 && !own ? 8192.f : scale * share;
+  }
+  if (negative && threadIdx.x < TT_LOSS_STEP && places + (int)threadIdx.x < (places + TT_LOSS_STEP - 1) / TT_LOSS_STEP * TT_LOSS_STEP) {
+    w.lse[places + threadIdx.x] = -INFINITY;  // up to a whole step: rows that add nothing
+    w.label[places + threadIdx.x] = -1;
+    w.weight[places + threadIdx.x] = 0.f;
   }
 }
 
@@ -216,36 +221,44 @@ TTGemm of_dw(const tt_loss *op, int classes, long long ldg, bool column) {  // G
 }
 
 struct Scratch {
-  size_t of, at, label, lse, share, weight, back, offsets, x, stats, run, picked, each, grads, acc, column, pieces, parts, total;
+  size_t of, at, label, lse, share, weight, back, offsets, x, stats, run, picked, each, grads, acc, column, pieces, parts, starts, copy, total;
 };
 Scratch scratch(const tt_loss *op, bool backward) {
   Scratch w = {};
-  const size_t rows = (size_t)op->rows, es = elem(op->dtype);
+  const size_t rows = (size_t)op->rows, whole = rows + TT_LOSS_STEP, es = elem(op->dtype);
   const long long piece = piece_of(op, backward);
+  TTNarrow n = {};
+  n.dtype = op->dtype;
+  n.dim = op->dim;
+  n.padded = padded(op);
+  n.classes = op->classes;
+  n.rows = op->rows;
   auto take = [&](size_t &at, size_t bytes) {
     at = w.total;
     w.total += pad256(bytes);
   };
   take(w.of, rows * 4);
   take(w.at, rows * 4);
-  take(w.label, rows * 4);
+  take(w.label, whole * 4);
   take(w.back, 4);
   take(w.offsets, 16);
   take(w.x, rows * padded(op) * es);
+  if (narrow(op)) {
+    take(w.starts, ((size_t)op->classes + TT_LOSS_STEP) * 4);
+    take(w.copy, (size_t)op->classes * padded(op) * es);  // (whether it is used is known with w's address only)
+  }
   if (!backward) {
-    take(w.stats, (narrow(op) ? (size_t)ttk_narrow_runs(op->rows, op->classes) : (size_t)tt_ceil_div(piece, 64)) * rows * 8);
+    take(w.stats, narrow(op) ? ttk_narrow_stats_bytes(n) : (size_t)tt_ceil_div(piece, 64) * rows * 8);
     take(w.run, rows * 8);
     take(w.picked, rows * 4);
     take(w.each, rows * 4);
     return w;
   }
-  take(w.lse, rows * 4);
+  take(w.lse, whole * 4);
   take(w.share, rows * 4);
-  take(w.weight, rows * 4);
+  take(w.weight, whole * 4);
   if (narrow(op)) {
-    const size_t row_runs = ttk_narrow_row_runs(op->rows, op->classes);
-    const size_t dx = (size_t)ttk_narrow_runs(op->rows, op->classes) * rows * padded(op) * 4, dw = row_runs > 1 ? row_runs * op->classes * (padded(op) + 4) * 4 : 0;
-    take(w.parts, dx > dw ? dx : dw);
+    take(w.parts, ttk_narrow_parts_bytes(n));
     return w;
   }
   take(w.grads, rows * piece * es);
@@ -267,7 +280,9 @@ Rows rows_of(char *ws, const Scratch &w) {
               (float *)(ws + w.back), (int64_t *)(ws + w.offsets)};
 }
 TTNarrow narrow_of(const tt_loss *op, const void *w, const void *bias, char *ws, const Scratch &need) {
-  return TTNarrow{op->dtype, op->dim, padded(op), op->classes, op->rows, ws + need.x, w, bias, rows_of(ws, need)};
+  const bool as_it_is = op->dim == padded(op) && aligned(w, 16);
+  return TTNarrow{op->dtype, op->dim, padded(op), op->classes, op->rows, ws + need.x, w, bias, rows_of(ws, need), (float *)(ws + need.starts),
+                  as_it_is ? nullptr : ws + need.copy};
 }
 unsigned grid_of(long long items) {
   const long long blocks = (items + TT_BLOCK - 1) / TT_BLOCK;
@@ -323,16 +338,15 @@ extern "C" tt_status tt_cross_entropy_forward(const tt_loss *op, const void *x, 
   const long long rows = op->rows, ignored = op->ignore_index, piece = piece_of(op, false);
   const int classes = op->classes, reduce = op->reduce;
   float *each = whole ? (float *)(ws + need.each) : loss;
-  hipLaunchKernelGGL(k_loss_rows, dim3(1), dim3(SCAN), 0, s, labels, rows, classes, ignored, reduce, (const float *)nullptr, (const float *)nullptr, 0, 0, r);
+  hipLaunchKernelGGL(k_loss_rows, dim3(1), dim3(SCAN), 0, s, labels, rows, classes, ignored, reduce, (const float *)nullptr, (const float *)nullptr, 0, 0, 0, r);
   if ((st = tt_launch_status()) != TT_OK) return st;
   if (some) {
     if ((st = TT_BY_TYPE(gather, op->dtype, op, x, r, ws + need.x, s)) != TT_OK) return st;
     float2 *run = (float2 *)(ws + need.run);
     if (narrow(op)) {
       const TTNarrow n = narrow_of(op, w, bias, ws, need);
-      if ((st = ttk_narrow_stats(n, (float *)(ws + need.stats), s)) != TT_OK || (st = ttk_narrow_picked(n, (float *)(ws + need.picked), s)) != TT_OK) return st;
-      const int runs = ttk_narrow_runs(rows, classes), first = 1;
-      hipLaunchKernelGGL(k_loss_fold, dim3((unsigned)tt_ceil_div(rows, 64)), dim3(TT_BLOCK), 0, s, (const float2 *)(ws + need.stats), runs, rows, first, r, run);
+      if ((st = ttk_narrow_classes(n, s)) != TT_OK) return st;
+      if ((st = ttk_narrow_stats(n, (float *)(ws + need.stats), (float *)run, (float *)(ws + need.picked), s)) != TT_OK) return st;
     }
     for (long long c = 0; c < classes && !narrow(op); c += piece) {
       const int n = (int)(classes - c < piece ? classes - c : piece);
@@ -382,13 +396,14 @@ extern "C" tt_status tt_cross_entropy_backward(const tt_loss *op, const void *x,
   char *ws = (char *)workspace;
   const Rows r = rows_of(ws, need);
   const long long rows = op->rows, ignored = op->ignore_index, piece = piece_of(op, true);
-  const int classes = op->classes, reduce = op->reduce, bits = op->dtype == TT_F32 ? 32 : 16, half = op->dtype == TT_F16;
-  hipLaunchKernelGGL(k_loss_rows, dim3(1), dim3(SCAN), 0, s, labels, rows, classes, ignored, reduce, lse, grad_loss, bits, half, r);
+  const int classes = op->classes, reduce = op->reduce, bits = op->dtype == TT_F32 ? 32 : 16, half = op->dtype == TT_F16, negative = narrow(op);
+  hipLaunchKernelGGL(k_loss_rows, dim3(1), dim3(SCAN), 0, s, labels, rows, classes, ignored, reduce, lse, grad_loss, bits, half, negative, r);
   if ((st = tt_launch_status()) != TT_OK) return st;
   if ((st = TT_BY_TYPE(gather, op->dtype, op, x, r, ws + need.x, s)) != TT_OK) return st;
   if (narrow(op)) {
     const TTNarrow n = narrow_of(op, w, bias, ws, need);
     float *parts = (float *)(ws + need.parts);
+    if ((st = ttk_narrow_classes(n, s)) != TT_OK) return st;
     if (dx && (st = ttk_narrow_dx(n, parts, dx, op->ld_dx ? op->ld_dx : op->dim, s)) != TT_OK) return st;
     return dw || dbias ? ttk_narrow_dw(n, reduce == TT_REDUCE_NONE, parts, dw, dbias, s) : TT_OK;
   }

@@ -17,24 +17,55 @@ using namespace ttg;
 // What is added to a logit comes for nothing: of the streamed vector (the class's bias, or a row's -lse) as the product's starting value, of the held
 // one in the multiply-add before exp2.
 // 512 registers of a SIMD's lane are two wavefronts of 256: 64 of the held operand, 128 of the sums, 32 of S.
-constexpr int WAVES = 4, THREADS = 64 * WAVES, STEP = 32;
+constexpr int WAVES = 4, THREADS = 64 * WAVES, STEP = TT_LOSS_STEP;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr float RAISE = 13.f;  // P is formed 2^13 times its size: fp16's smallest numbers then are of 2^-37, and P stays below 2^14
 enum Mode { STATS, ROWS, CLASSES };
 constexpr int held_tiles(int KP, Mode mode) { return mode != STATS && KP == 128 ? 3 : 4; }  // of 16 vectors, of a wavefront
 
+// How a launch is cut, from the number of held vectors (which the host does not know where they are rows that count) and of workgroups that run at once:
+// workgroup w has block w % blocks of the held vectors and run w / blocks of the streamed ones.  As many runs as fill the card once, or
+// twice where that wastes less; eight steps at least in each.
+struct Cut {
+  int blocks, runs;
+};
+__host__ __device__ inline Cut cut_of(long long held, long long streamed, int tile, int slots) {
+  const long long blocks = held < 1 ? 1 : (held + tile - 1) / tile, steps = (streamed + STEP - 1) / STEP;
+  const long long one = slots / blocks, two = 2LL * slots / blocks;
+  long long runs = 42 * one >= 20 * two ? one : two;
+  if (runs > steps / 8) runs = steps / 8;
+  return Cut{(int)blocks, (int)(runs < 1 ? 1 : runs)};
+}
+// Workgroups for any number of vectors up to these.
+__host__ __device__ inline long long grid_for(long long held, long long streamed, int tile, int slots) {
+  const long long blocks = held < 1 ? 1 : (held + tile - 1) / tile, most = blocks * ((streamed + 8 * STEP - 1) / (8 * STEP));
+  const long long twice = 2LL * slots < most ? 2LL * slots : most;
+  return blocks > twice ? blocks : twice;
+}
+constexpr int tile_of(int KP, Mode mode) { return 16 * held_tiles(KP, mode) * WAVES; }
+constexpr int slots_of(Mode mode) { return 256 * (mode == STATS ? 4 : 2); }
+
 struct Args {
   const void *held, *streamed;
-  const void *bias;          // [classes], nullable
-  const float *lse, *weight; // of places
-  const int32_t *label;
+  const float *starts;       // of streamed vectors, -infinity behind the last one, whole steps
+  const float *constants;    // of held vectors
+  const float *weight;       // CLASSES with shares: of the rows, whole steps
+  const int32_t *label;      // of the rows, whole steps
   const int64_t *offsets;
   void *out, *sums;          // CLASSES of one run: dW, dbias
   const float *back;
-  float *parts;
-  long long rows;
-  int dim, classes, runs;
+  float *parts;              // [workgroup][tile]...
+  int dim, classes;
 };
+
+typedef const __attribute__((address_space(1))) void *GlobalPtr;
+typedef __attribute__((address_space(3))) void *LdsPtr;
+// Waits for the wavefront's loads (into LDS too) and LDS reads.
+__device__ __forceinline__ void wait_loads() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(7 << 4);
+  asm volatile("" ::: "memory");
+}
 
 // 16-byte pieces of an LDS row are spread so that sixteen neighbouring rows at one piece, and eight at two neighbouring pieces (the transposing
 // read), meet every bank once.
@@ -52,161 +83,178 @@ template <int KP> __device__ __forceinline__ u16x8 frag_across(const unsigned sh
   const u16x4 x = lds_read_tr(at), y = lds_read_tr(at + 16 * KP);
   return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
 }
-// Eight elements of a vector, zeros where there are none.
-template <class T> __device__ __forceinline__ u16x8 load8(const T *p, int valid) {
-  u16x8 v;
-  if (valid >= 8) {
-    const typename Vec<T>::v16b r = *reinterpret_cast<const typename Vec<T>::v16b *>(p);
+
+// A step's LDS: the tile, then of its vectors what they start at and the shares.
+template <int KP> constexpr int step_bytes() { return STEP * KP * 2 + 2 * STEP * 4; }
+
+// What a thread fetches of a step.  The tile's 16-byte pieces go from memory into LDS, lane after lane; which piece a lane fetches makes their order
+// there.  A vector behind the last one is the last one again: it starts at -infinity, and its P is zero.
+template <class T, int KP, Mode MODE, bool SHARES> struct Fetcher {
+  const T *streamed;
+  const float *starts, *weight;
+  long long count;
+  int row, wave, lane;
+  unsigned offset;
+  __device__ __forceinline__ void fetch(long long t, char *to) const {
+    constexpr int PIECES = STEP * KP / 8 / THREADS, TILE = STEP * KP * 2;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = r[i];
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = i < valid ? __builtin_bit_cast(unsigned short, p[i]) : (unsigned short)0;
+    for (int i = 0; i < PIECES; ++i) {
+      const long long r = t + row + i * (THREADS / (KP / 8));
+      __builtin_amdgcn_global_load_lds((GlobalPtr)(streamed + (r < count ? r : count - 1) * KP + offset), (LdsPtr)(to + (i * THREADS + wave * 64) * 16), 16, 0, 0);
+    }
+    if (lane < STEP) {  // a wavefront each
+      if (wave == 0) __builtin_amdgcn_global_load_lds((GlobalPtr)(starts + t + lane), (LdsPtr)(to + TILE), 4, 0, 0);
+      if constexpr (SHARES)
+        if (wave == 1) __builtin_amdgcn_global_load_lds((GlobalPtr)(weight + t + lane), (LdsPtr)(to + TILE + STEP * 4), 4, 0, 0);
+    }
   }
-  return v;
+};
+
+// A step, from `now`, while the next one (`ahead`; behind the last: none) is on its way to `next`.  (The buffers are separate to the compiler,
+// which else has every read wait for the loads.)
+// hit: a label of the rows is among the classes here, which few steps have; one branch, since what is on its two sides is not
+// interleaved.  `label`: ROWS of the held rows, less the step's first class; CLASSES lane l's is row l's, less the first held class.
+// The one is taken off P before that is rounded: where a row is nearly sure of its label their difference is all that is left.
+template <class T, int KP, Mode MODE, bool SHARES, int H, int DO>
+__device__ __forceinline__ void step_of(const char *__restrict__ now, char *__restrict__ next, const Fetcher<T, KP, MODE, SHARES> &fetcher, long long ahead,
+                                        long long end, bool hit, const int (&label)[MODE == ROWS ? H : 1], const u16x8 (&held)[H][KP / 32], float (&constant)[H], f32x4 (&acc)[DO][H], float (&sums)[H]) {
+  constexpr int KS = KP / 32, D = KP / 16;
+  constexpr bool OUT = MODE != STATS, CLASS = MODE == CLASSES;
+  const int lane = threadIdx.x & 63, q = lane >> 4, j = lane & 15;
+  if (ahead < end) fetcher.fetch(ahead, next);
+  const unsigned short *tile = reinterpret_cast<const unsigned short *>(now);
+  const float *starts = reinterpret_cast<const float *>(now + STEP * KP * 2), *shares = starts + STEP;
+  f32x4 S[2][H];
+#pragma unroll
+  for (int half = 0; half < 2; ++half) {  // 16 streamed vectors
+    const f32x4 from = *reinterpret_cast<const f32x4 *>(starts + 16 * half + 4 * q);
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      const u16x8 f = frag<KP>(tile, 16 * half, s);
+#pragma unroll
+      for (int x = 0; x < H; ++x) S[half][x] = mma(T(), f, held[x][s], s ? S[half][x] : from);
+    }
+    if constexpr (MODE == STATS) {
+#pragma unroll
+      for (int x = 0; x < H; ++x) {
+        const float top = fmaxf(fmaxf(S[half][x][0], S[half][x][1]), fmaxf(S[half][x][2], S[half][x][3]));
+        // what exp2 gets stays below 16, so that the sum stays far from the range's end; seldom after the first steps
+        const bool above = fmaf(top, LOG2E, constant[x]) > 16.f;
+        if (__ballot(above)) {
+          const float now = above ? -top * LOG2E : constant[x];
+          sums[x] *= above ? __builtin_amdgcn_exp2f(now - constant[x]) : 1.f;
+          constant[x] = now;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sums[x] += __builtin_amdgcn_exp2f(fmaf(S[half][x][i], LOG2E, constant[x]));
+      }
+    } else {
+#pragma unroll
+      for (int x = 0; x < H; ++x)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) S[half][x][i] = __builtin_amdgcn_exp2f(fmaf(S[half][x][i], LOG2E, constant[x]));
+    }
+  }
+  if constexpr (OUT) {
+    if (hit) {
+#pragma unroll
+      for (int half = 0; half < 2; ++half)
+#pragma unroll
+        for (int x = 0; x < H; ++x)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int streamed = 16 * half + 4 * q + i;
+            const bool here = CLASS ? __shfl(label[0], streamed, 64) == 16 * x + j : label[CLASS ? 0 : x] == streamed;
+            S[half][x][i] -= here ? (SHARES ? 1.f : 8192.f) : 0.f;
+          }
+    }
+    u16x8 P[H];
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      f32x4 share = {1.f, 1.f, 1.f, 1.f};
+      if constexpr (SHARES) share = *reinterpret_cast<const f32x4 *>(shares + 16 * half + 4 * q);
+#pragma unroll
+      for (int x = 0; x < H; ++x)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if constexpr (SHARES) S[half][x][i] *= share[i];
+          if constexpr (CLASS) sums[x] += S[half][x][i];
+          P[x][4 * half + i] = __builtin_bit_cast(unsigned short, from_f32<T>(S[half][x][i]));
+        }
+    }
+#pragma unroll
+    for (int y = 0; y < D; ++y) {
+      const u16x8 f = frag_across<KP>(tile, 16 * y);
+#pragma unroll
+      for (int x = 0; x < H; ++x) acc[y][x] = mma(T(), f, P[x], acc[y][x]);
+    }
+  }
 }
 
 template <class T, int KP, Mode MODE, bool SHARES> __global__ void __launch_bounds__(THREADS, 2) k_narrow(Args a) {
-  constexpr int KS = KP / 32, H = held_tiles(KP, MODE), HELD = 16 * H, D = KP / 16, PIECES = STEP * KP / 8 / THREADS;
+  constexpr int KS = KP / 32, H = held_tiles(KP, MODE), HELD = 16 * H, D = KP / 16;
   constexpr bool OUT = MODE != STATS, CLASS = MODE == CLASSES;
-  __shared__ __align__(16) unsigned short tiles[2][STEP * KP];
-  __shared__ __align__(16) float starts[2][STEP], shares[SHARES ? 2 : 1][SHARES ? STEP : 4];
-  __shared__ int labels[CLASS ? 2 : 1][CLASS ? STEP : 4];
+  constexpr int BYTES = step_bytes<KP>(), GIVE = CLASS ? WAVES * 16 * (KP + 8) * 2 : 0;  // two steps, or what is given out through it
+  __shared__ __align__(16) char lds[GIVE > 2 * BYTES ? GIVE : 2 * BYTES];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), q = lane >> 4, j = lane & 15;
   const long long places = a.offsets[1];
   const long long held_count = CLASS ? a.classes : places, streamed_count = CLASS ? places : a.classes;
-  const long long h0 = (long long)blockIdx.x * (HELD * WAVES) + wave * HELD;
-  if ((long long)blockIdx.x * (HELD * WAVES) >= held_count) return;  // (the whole workgroup)
+  const Cut cut = cut_of(held_count, streamed_count, tile_of(KP, MODE), slots_of(MODE));
+  const int block = (int)(blockIdx.x % (unsigned)cut.blocks), run = (int)(blockIdx.x / (unsigned)cut.blocks);
+  if (run >= cut.runs || held_count == 0) return;
+  const long long h0 = (long long)block * tile_of(KP, MODE) + wave * HELD;
   // this run's share of the streamed vectors, whole steps
-  const long long steps = (streamed_count + STEP - 1) / STEP, per = (steps + a.runs - 1) / a.runs;
-  const long long s0 = blockIdx.y * per * STEP, s1 = s0 + per * STEP < streamed_count ? s0 + per * STEP : streamed_count;
-  // vectors of x are KP apart, padded with zeros; of W dim apart
-  const int ld_held = CLASS ? a.dim : KP, ld_streamed = CLASS ? KP : a.dim, held_dim = ld_held, streamed_dim = ld_streamed;
+  const long long steps = (streamed_count + STEP - 1) / STEP, per = (steps + cut.runs - 1) / cut.runs;
+  const long long s0 = run * per * STEP, s1 = s0 + per * STEP < streamed_count ? s0 + per * STEP : streamed_count;
 
   u16x8 held[H][KS];
   float constant[H];  // of the held vector, in units of log 2
 #pragma unroll
   for (int x = 0; x < H; ++x) {
-    const long long h = h0 + 16 * x + j;
-    const bool in = h < held_count;
+    const long long h = h0 + 16 * x + j < held_count ? h0 + 16 * x + j : held_count - 1;  // (of vectors outside nothing is written)
 #pragma unroll
-    for (int s = 0; s < KS; ++s) held[x][s] = load8((const T *)a.held + (in ? h : 0) * ld_held + 32 * s + 8 * q, in ? held_dim - 32 * s - 8 * q : 0);
-    if constexpr (MODE == ROWS) constant[x] = (in ? -a.lse[h] * LOG2E : 0.f) + RAISE;
-    else if constexpr (CLASS) constant[x] = (a.bias && in ? to_f32(((const T *)a.bias)[h]) * LOG2E : 0.f) + (SHARES ? 0.f : RAISE);
-    else constant[x] = 3e38f;  // less the largest so far: below all
+    for (int s = 0; s < KS; ++s) held[x][s] = *reinterpret_cast<const u16x8 *>((const T *)a.held + h * KP + 32 * s + 8 * q);
+    constant[x] = MODE == STATS ? 3e38f /* less the largest so far: below all */ : fmaf(a.constants[h], LOG2E, SHARES ? 0.f : RAISE);
   }
   f32x4 acc[OUT ? D : 1][H] = {};  // [columns][held]
   float sums[H] = {};
 
-  u16x8 next[PIECES];
-  float start_next = 0.f, share_next = 0.f;
-  int label_next = -1;
-  auto fetch = [&](long long t) {
+  const int row = (int)threadIdx.x / (KP / 8);
+  const Fetcher<T, KP, MODE, SHARES> fetcher = {(const T *)a.streamed, a.starts, a.weight, streamed_count, row, wave, lane,
+                                                ((threadIdx.x % (KP / 8)) ^ spread<KP>(row & 15)) * 8};
+  // Labels are a step ahead of their use, in a register: of the held rows less the first class, or of the streamed rows less the first held class.
+  int label[MODE == ROWS ? H : 1] = {}, label_next = 0;
+  if constexpr (MODE == ROWS) {
 #pragma unroll
-    for (int i = 0; i < PIECES; ++i) {
-      const int p = threadIdx.x + i * THREADS, r = p / (KP / 8), c = p % (KP / 8) * 8;
-      const bool in = t + r < s1;
-      next[i] = load8((const T *)a.streamed + (in ? t + r : 0) * ld_streamed + c, in ? streamed_dim - c : 0);
-    }
-    if (threadIdx.x < STEP) {
-      const long long r = t + threadIdx.x;
-      const bool in = r < s1;
-      if constexpr (CLASS) {
-        start_next = in ? -a.lse[r] : -INFINITY;
-        label_next = in ? a.label[r] : -1;
-        if constexpr (SHARES) share_next = in ? a.weight[r] : 0.f;
-      } else {
-        start_next = in ? (a.bias ? to_f32(((const T *)a.bias)[r]) : 0.f) : -INFINITY;
-      }
-    }
-  };
-  auto put = [&](int b) {
-#pragma unroll
-    for (int i = 0; i < PIECES; ++i) {
-      const int p = threadIdx.x + i * THREADS, r = p / (KP / 8), c8 = p % (KP / 8);
-      *reinterpret_cast<u16x8 *>(tiles[b] + r * KP + ((c8 ^ spread<KP>(r & 15)) << 3)) = next[i];
-    }
-    if (threadIdx.x < STEP) {
-      starts[b][threadIdx.x] = start_next;
-      if constexpr (CLASS) labels[b][threadIdx.x] = label_next;
-      if constexpr (SHARES) shares[b][threadIdx.x] = share_next;
-    }
-  };
-
+    for (int x = 0; x < H; ++x) label[x] = h0 + 16 * x + j < held_count ? a.label[h0 + 16 * x + j] - (int)s0 : -1;
+  }
   if (s0 < s1) {
-    fetch(s0);
-    put(0);
+    fetcher.fetch(s0, lds);
+    if constexpr (CLASS) label_next = a.label[s0 + (lane & 31)];
+    wait_loads();
   }
   int b = 0;
   for (long long t = s0; t < s1; t += STEP, b ^= 1) {
-    __syncthreads();  // this step's tile is whole, and nobody reads the other buffer any more
-    const bool more = t + STEP < s1;
-    if (more) fetch(t + STEP);
-    const unsigned short *tile = tiles[b];
-    bool hit = false;  // a label of these rows is among the wavefront's classes
-    if constexpr (CLASS) hit = __ballot(lane < STEP && (unsigned)(labels[b][lane & 31] - (int)h0) < (unsigned)HELD) != 0;
-    u16x8 P[OUT ? H : 1];
+    __syncthreads();  // this step has landed, everyone's part of it, and nobody reads the other buffer any more
+    bool hit = false;
+    if constexpr (MODE == ROWS) {
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {  // 16 streamed vectors
-      f32x4 S[H];
-      const f32x4 from = *reinterpret_cast<const f32x4 *>(&starts[b][16 * half + 4 * q]);
-#pragma unroll
-      for (int s = 0; s < KS; ++s) {
-        const u16x8 f = frag<KP>(tile, 16 * half, s);
-#pragma unroll
-        for (int x = 0; x < H; ++x) S[x] = mma(T(), f, held[x][s], s ? S[x] : from);
-      }
-      if constexpr (MODE == STATS) {
-#pragma unroll
-        for (int x = 0; x < H; ++x) {
-          const float top = fmaxf(fmaxf(S[x][0], S[x][1]), fmaxf(S[x][2], S[x][3]));
-          // what exp2 gets stays below 16, so that the sum stays far from the range's end; seldom after the first steps
-          const bool above = fmaf(top, LOG2E, constant[x]) > 16.f;
-          if (__ballot(above)) {
-            const float now = above ? -top * LOG2E : constant[x];
-            sums[x] *= above ? __builtin_amdgcn_exp2f(now - constant[x]) : 1.f;
-            constant[x] = now;
-          }
-#pragma unroll
-          for (int i = 0; i < 4; ++i) sums[x] += __builtin_amdgcn_exp2f(fmaf(S[x][i], LOG2E, constant[x]));
-        }
-      } else {
-        __builtin_amdgcn_sched_barrier(0);
-        f32x4 share;
-        if constexpr (SHARES) share = *reinterpret_cast<const f32x4 *>(&shares[b][16 * half + 4 * q]);
-#pragma unroll
-        for (int x = 0; x < H; ++x) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            S[x][i] = __builtin_amdgcn_exp2f(fmaf(S[x][i], LOG2E, constant[x]));
-            if constexpr (SHARES) S[x][i] *= share[i];
-          }
-          if constexpr (CLASS) {
-            if (hit) {
-#pragma unroll
-              for (int i = 0; i < 4; ++i)
-                if (labels[b][16 * half + 4 * q + i] == (int)(h0 + 16 * x + j)) S[x][i] -= SHARES ? share[i] : 8192.f;
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) sums[x] += S[x][i];
-          }
-#pragma unroll
-          for (int i = 0; i < 4; ++i) P[x][4 * half + i] = __builtin_bit_cast(unsigned short, from_f32<T>(S[x][i]));
-        }
-      }
+      for (int x = 0; x < H; ++x) hit |= (unsigned)label[x] < (unsigned)STEP;
     }
-    if constexpr (OUT) {
-      __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-      for (int y = 0; y < D; ++y) {
-        const u16x8 f = frag_across<KP>(tile, 16 * y);
-#pragma unroll
-        for (int x = 0; x < H; ++x) acc[y][x] = mma(T(), f, P[x], acc[y][x]);
-      }
+    if constexpr (CLASS) {
+      label[0] = label_next - (int)h0;
+      hit = (unsigned)label[0] < (unsigned)HELD;
+      if (t + STEP < s1) label_next = a.label[t + STEP + (lane & 31)];
     }
-    if (more) put(b ^ 1);
+    step_of<T, KP, MODE, SHARES>(lds + b * BYTES, lds + (b ^ 1) * BYTES, fetcher, t + STEP, s1, OUT && __ballot(hit) != 0, label, held, constant, acc, sums);
+    if constexpr (MODE == ROWS) {
+#pragma unroll
+      for (int x = 0; x < H; ++x) label[x] -= STEP;
+    }
+    wait_loads();
   }
 
+  const int first = wave * HELD;  // of the workgroup's tile
   if constexpr (MODE == STATS) {
 #pragma unroll
     for (int x = 0; x < H; ++x) {  // four lanes have a row's columns
@@ -214,36 +262,76 @@ template <class T, int KP, Mode MODE, bool SHARES> __global__ void __launch_boun
       if (constant[x] == 3e38f) mine = {-INFINITY, sums[x]};  // nothing but -infinity (or NaN, which the sum has)
 #pragma unroll
       for (int o = 16; o < 64; o *= 2) mine = join_stats(mine, float2{__shfl(mine.x, lane ^ o, 64), __shfl(mine.y, lane ^ o, 64)});
-      const long long h = h0 + 16 * x + j;
-      if (q == 0 && h < held_count) reinterpret_cast<float2 *>(a.parts)[blockIdx.y * a.rows + h] = mine;
+      if (q == 0) reinterpret_cast<float2 *>(a.parts)[(long long)blockIdx.x * tile_of(KP, MODE) + first + 16 * x + j] = mine;
     }
-  } else {
+  } else if (MODE == ROWS || cut.runs > 1) {
+    constexpr int LD = CLASS ? KP + 4 : KP;
+    float *to = a.parts + ((long long)blockIdx.x * tile_of(KP, MODE) + first) * LD;
 #pragma unroll
     for (int x = 0; x < H; ++x) {
-      const long long h = h0 + 16 * x + j;
+#pragma unroll
+      for (int y = 0; y < D; ++y) *reinterpret_cast<f32x4 *>(to + (16 * x + j) * LD + 16 * y + 4 * q) = acc[y][x];
       if constexpr (CLASS) {
         sums[x] += __shfl(sums[x], lane ^ 16, 64);
         sums[x] += __shfl(sums[x], lane ^ 32, 64);
-      }
-      if (h >= held_count) continue;
-      if (CLASS && a.runs == 1) {
-        const float back = *a.back;
-#pragma unroll
-        for (int y = 0; y < D; ++y) {
-          const int c = 16 * y + 4 * q;
-          float v[4] = {acc[y][x][0] * back, acc[y][x][1] * back, acc[y][x][2] * back, acc[y][x][3] * back};
-          if (a.out && c < a.dim) store4((T *)a.out + h * a.dim + c, a.dim - c, v);
-        }
-        if (a.sums && q == 0) ((T *)a.sums)[h] = from_f32<T>(sums[x] * back);
-      } else {
-        constexpr int LD = CLASS ? KP + 4 : KP;
-        float *to = a.parts + (blockIdx.y * (CLASS ? (long long)a.classes : a.rows) + h) * LD;
-#pragma unroll
-        for (int y = 0; y < D; ++y) *reinterpret_cast<f32x4 *>(to + 16 * y + 4 * q) = acc[y][x];
-        if (CLASS && q == 0) to[KP] = sums[x];
+        if (q == 0) to[(16 * x + j) * LD + KP] = sums[x];
       }
     }
+  } else if constexpr (CLASS) {
+    const float back = *a.back;
+    // through LDS, 16 classes at a time, so that whole lines are written
+    constexpr int LD = KP + 8, PER = KP / 8, ROWS_AT = 64 / PER;
+    __syncthreads();  // nobody reads a step any more
+    unsigned short *room = reinterpret_cast<unsigned short *>(lds) + wave * 16 * LD;
+#pragma unroll
+    for (int x = 0; x < H; ++x) {
+      sums[x] += __shfl(sums[x], lane ^ 16, 64);
+      sums[x] += __shfl(sums[x], lane ^ 32, 64);
+      const long long h = h0 + 16 * x;
+      if (a.sums && q == 0 && h + j < held_count) ((T *)a.sums)[h + j] = from_f32<T>(sums[x] * back);
+      if (!a.out) continue;
+#pragma unroll
+      for (int y = 0; y < D; ++y) {
+        u16x4 v;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = __builtin_bit_cast(unsigned short, from_f32<T>(acc[y][x][i] * back));
+        *reinterpret_cast<u16x4 *>(room + j * LD + 16 * y + 4 * q) = v;
+      }
+      tt_wave_lds_order();
+#pragma unroll
+      for (int r = lane / PER; r < 16; r += ROWS_AT) {
+        const int c = lane % PER * 8;
+        const u16x8 v = *reinterpret_cast<const u16x8 *>(room + r * LD + c);
+        if (h + r >= held_count || c >= a.dim) continue;
+        T *to = (T *)a.out + (h + r) * a.dim + c;
+        if (a.dim - c >= 8) {
+          typename Vec<T>::v16b o;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) o[i] = v[i];
+          *reinterpret_cast<typename Vec<T>::v16b *>(to) = o;
+        } else {
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if (i < a.dim - c) to[i] = __builtin_bit_cast(T, (unsigned short)v[i]);
+        }
+      }
+      tt_wave_lds_order();
+    }
   }
+}
+
+// The runs' statistics of each place together, a wavefront a place.
+__global__ void __launch_bounds__(TT_BLOCK) k_narrow_fold(const float2 *__restrict__ parts, const int64_t *offsets, int classes, int tile, int slots, float2 *run) {
+  const int lane = threadIdx.x & 63;
+  const long long i = (long long)blockIdx.x * (TT_BLOCK / 64) + (threadIdx.x >> 6), places = offsets[1];
+  if (i >= places) return;
+  const Cut cut = cut_of(places, classes, tile, slots);
+  const long long block = i / tile;
+  float2 s = {-INFINITY, 0.f};
+  for (int k = lane; k < cut.runs; k += 64) s = join_stats(s, parts[(k * (long long)cut.blocks + block) * tile + i % tile]);
+#pragma unroll
+  for (int o = 1; o < 64; o *= 2) s = join_stats(s, float2{__shfl(s.x, lane ^ o, 64), __shfl(s.y, lane ^ o, 64)});
+  if (lane == 0) run[i] = s;
 }
 
 // z of each place's label, as a product of its own: 16 lanes a place
@@ -265,89 +353,131 @@ template <class T> __global__ void __launch_bounds__(TT_BLOCK) k_narrow_picked(T
   if (in && lane == 0) picked[i] = s + (n.bias && label >= 0 ? to_f32(((const T *)n.bias)[label]) : 0.f);
 }
 
-// dx = share (sum of the runs' parts - W of the label), zeros in rows that do not count; four columns a thread
-template <class T> __global__ void __launch_bounds__(TT_BLOCK) k_narrow_dx(TTNarrow n, int runs, const float *__restrict__ parts, T *dx, long long ld) {
-  const int per = (n.dim + 3) / 4;
-  for (long long e = (long long)blockIdx.x * TT_BLOCK + threadIdx.x; e < n.rows * per; e += (long long)gridDim.x * TT_BLOCK) {
-    const long long r = e / per;
-    const int c = (int)(e - r * per) * 4, at = n.r.at[r];
-    float v[4] = {0.f, 0.f, 0.f, 0.f};
-    if (at >= 0) {
-      f32x4 s = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 8
-      for (int k = 0; k < runs; ++k) s += *reinterpret_cast<const f32x4 *>(parts + (k * n.rows + at) * n.padded + c);
-      const int label = n.r.label[at];
-      if (label >= 0) load4((const T *)n.w + (long long)label * n.dim + c, n.dim - c, v);
-      const float share = n.r.share[at];
+// A workgroup's sum of the runs' parts of one vector, `width` columns (of four a thread) in eight runs that are added in order: in the threads of the first.
+template <int KP> __device__ __forceinline__ f32x4 sum_runs(const float *__restrict__ parts, int ld, const Cut &cut, int tile, long long vector, float *room) {
+  constexpr int PER = KP / 4 + 1, SEGMENTS = TT_BLOCK / PER;  // the last four columns: the sums
+  const int c = (int)threadIdx.x % PER, seg = (int)threadIdx.x / PER, each = (cut.runs + SEGMENTS - 1) / SEGMENTS;
+  const long long block = vector / tile;
+  f32x4 s = {0.f, 0.f, 0.f, 0.f};
+  if (seg < SEGMENTS && 4 * c < ld) {
+    const int end = (seg + 1) * each < cut.runs ? (seg + 1) * each : cut.runs;
+#pragma unroll 4
+    for (int k = seg * each; k < end; ++k)
+      s += *reinterpret_cast<const f32x4 *>(parts + ((k * (long long)cut.blocks + block) * tile + vector % tile) * ld + 4 * c);
+  }
+  f32x4 *all = reinterpret_cast<f32x4 *>(room);
+  all[threadIdx.x] = s;
+  __syncthreads();
+  if (seg == 0) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) v[i] = share * (s[i] * 0x1p-13f - v[i]);
+    for (int k = 1; k < SEGMENTS; ++k) s += all[k * PER + c];
+  }
+  __syncthreads();
+  return s;
+}
+// dx = share times the sum, zeros in rows that do not count; a workgroup a row
+template <class T, int KP> __global__ void __launch_bounds__(TT_BLOCK) k_narrow_dx(TTNarrow n, const float *__restrict__ parts, T *dx, long long ld) {
+  __shared__ __align__(16) float room[TT_BLOCK * 4];
+  const long long places = n.r.offsets[1];
+  const Cut cut = cut_of(places, n.classes, tile_of(KP, ROWS), slots_of(ROWS));
+  const int c = 4 * (int)threadIdx.x;
+  for (long long r = blockIdx.x; r < n.rows; r += gridDim.x) {
+    const int at = n.r.at[r];
+    f32x4 s = {0.f, 0.f, 0.f, 0.f};
+    if (at >= 0) {
+      s = sum_runs<KP>(parts, KP, cut, tile_of(KP, ROWS), at, room);
+      s *= 0x1p-13f * n.r.share[at];
     }
-    store4(dx + r * ld + c, n.dim - c, v);
+    const float v[4] = {s[0], s[1], s[2], s[3]};
+    if (c < n.dim && c < KP) store4(dx + r * ld + c, n.dim - c, v);
   }
 }
-// dW and dbias of several runs of the rows
-template <class T> __global__ void __launch_bounds__(TT_BLOCK) k_narrow_dw(TTNarrow n, int runs, const float *__restrict__ parts, T *dw, T *db) {
-  const int per = (n.dim + 3) / 4 + 1, ld = n.padded + 4;
+// dW and dbias where the rows came in several runs; a workgroup a class
+template <class T, int KP> __global__ void __launch_bounds__(TT_BLOCK) k_narrow_dw(TTNarrow n, const float *__restrict__ parts, T *dw, T *db) {
+  __shared__ __align__(16) float room[TT_BLOCK * 4];
+  const Cut cut = cut_of(n.classes, n.r.offsets[1], tile_of(KP, CLASSES), slots_of(CLASSES));
+  if (cut.runs == 1) return;  // the products' kernel has written them
   const float back = *n.r.back;
-  for (long long e = (long long)blockIdx.x * TT_BLOCK + threadIdx.x; e < (long long)n.classes * per; e += (long long)gridDim.x * TT_BLOCK) {
-    const long long h = e / per;
-    const int c = (int)(e - h * per) * 4;
-    const bool sum = c >= n.dim;  // the last one: dbias
-    if (sum ? !db : !dw) continue;
-    f32x4 s = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 8
-    for (int k = 0; k < runs; ++k) {
-      const float *p = parts + (k * (long long)n.classes + h) * ld + (sum ? n.padded : c);
-      if (sum) s[0] += *p;
-      else s += *reinterpret_cast<const f32x4 *>(p);
-    }
-    float v[4] = {s[0] * back, s[1] * back, s[2] * back, s[3] * back};
-    if (sum) db[h] = from_f32<T>(v[0]);
-    else store4(dw + h * n.dim + c, n.dim - c, v);
+  const int c = 4 * (int)threadIdx.x;
+  for (long long h = blockIdx.x; h < n.classes; h += gridDim.x) {
+    const f32x4 s = sum_runs<KP>(parts, KP + 4, cut, tile_of(KP, CLASSES), h, room) * back;
+    const float v[4] = {s[0], s[1], s[2], s[3]};
+    if (dw && c < n.dim && c < KP) store4(dw + h * n.dim + c, n.dim - c, v);
+    if (db && c == KP) db[h] = from_f32<T>(v[0]);
+  }
+}
+
+// What the kernels above take of the classes: their biases as numbers of 32 bits (-infinity behind the last one, whole steps), and where W's rows are not `padded`
+// aligned elements as they are, a copy of which they are.
+template <class T> __global__ void __launch_bounds__(TT_BLOCK) k_narrow_classes(TTNarrow n, float *starts, T *copy) {
+  const long long whole = ((long long)n.classes + STEP - 1) / STEP * STEP, stride = (long long)gridDim.x * TT_BLOCK;
+  for (long long i = (long long)blockIdx.x * TT_BLOCK + threadIdx.x; i < whole; i += stride)
+    starts[i] = i >= n.classes ? -INFINITY : n.bias ? to_f32(((const T *)n.bias)[i]) : 0.f;
+  if (!copy) return;
+  const int per = n.padded / 8;
+  for (long long e = (long long)blockIdx.x * TT_BLOCK + threadIdx.x; e < (long long)n.classes * per; e += stride) {
+    const long long r = e / per;
+    const int c = (int)(e - r * per) * 8;
+    float v[8] = {};
+    load_n<T, 8>((const T *)n.w + r * n.dim + c, n.dim - c, v);
+    store_n<T, 8>(copy + r * n.padded + c, 8, v);
   }
 }
 
 // ---- host ------------------------------------------------------------------------------------------
 Args args_of(const TTNarrow &n, bool classes) {
   Args a = {};
-  a.held = classes ? n.w : n.x;
-  a.streamed = classes ? n.x : n.w;
-  a.bias = n.bias;
-  a.lse = n.r.lse;
+  const void *w = n.copy ? n.copy : n.w;
+  a.held = classes ? w : n.x;
+  a.streamed = classes ? n.x : w;
+  a.starts = classes ? n.r.lse : n.starts;
+  a.constants = classes ? n.starts : n.r.lse;
   a.weight = n.r.weight;
   a.label = n.r.label;
   a.offsets = n.r.offsets;
   a.back = n.r.back;
-  a.rows = n.rows;
   a.dim = n.dim;
   a.classes = n.classes;
   return a;
 }
-template <class T, int KP> tt_status launch(Mode mode, bool shares, const Args &a, long long held, hipStream_t s) {
-  const dim3 grid((unsigned)tt_ceil_div(held, 16 * held_tiles(KP, mode) * WAVES), (unsigned)a.runs), block(THREADS);
-  if (mode == STATS) hipLaunchKernelGGL((k_narrow<T, KP, STATS, false>), grid, block, 0, s, a);
-  else if (mode == ROWS) hipLaunchKernelGGL((k_narrow<T, KP, ROWS, false>), grid, block, 0, s, a);
-  else if (shares) hipLaunchKernelGGL((k_narrow<T, KP, CLASSES, true>), grid, block, 0, s, a);
-  else hipLaunchKernelGGL((k_narrow<T, KP, CLASSES, false>), grid, block, 0, s, a);
+template <Mode MODE> long long workgroups(const TTNarrow &n) {
+  const long long held = MODE == CLASSES ? n.classes : n.rows, streamed = MODE == CLASSES ? n.rows : n.classes;
+  return grid_for(held, streamed, n.padded == 64 ? tile_of(64, MODE) : tile_of(128, MODE), slots_of(MODE));
+}
+template <class T, int KP, Mode MODE> tt_status launch_as(const TTNarrow &n, bool shares, const Args &a, hipStream_t s) {
+  const dim3 grid((unsigned)workgroups<MODE>(n)), block(THREADS);
+  if constexpr (MODE == CLASSES) {
+    if (shares) hipLaunchKernelGGL((k_narrow<T, KP, MODE, true>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((k_narrow<T, KP, MODE, false>), grid, block, 0, s, a);
+  } else {
+    hipLaunchKernelGGL((k_narrow<T, KP, MODE, false>), grid, block, 0, s, a);
+  }
   return tt_launch_status();
 }
-tt_status launch(const TTNarrow &n, Mode mode, bool shares, const Args &a, hipStream_t s) {
-  const long long held = mode == CLASSES ? n.classes : n.rows;
-  if (n.dtype == TT_BF16) return n.padded == 64 ? launch<ttg::bf16, 64>(mode, shares, a, held, s) : launch<ttg::bf16, 128>(mode, shares, a, held, s);
-  return n.padded == 64 ? launch<ttg::f16, 64>(mode, shares, a, held, s) : launch<ttg::f16, 128>(mode, shares, a, held, s);
+template <Mode MODE> tt_status launch(const TTNarrow &n, bool shares, const Args &a, hipStream_t s) {
+  if (workgroups<MODE>(n) > TT_MAX_WORKGROUPS) return TT_ERR_SHAPE;
+  if (n.dtype == TT_BF16) return n.padded == 64 ? launch_as<ttg::bf16, 64, MODE>(n, shares, a, s) : launch_as<ttg::bf16, 128, MODE>(n, shares, a, s);
+  return n.padded == 64 ? launch_as<ttg::f16, 64, MODE>(n, shares, a, s) : launch_as<ttg::f16, 128, MODE>(n, shares, a, s);
 }
 unsigned grid_of(long long items) {
   const long long blocks = (items + TT_BLOCK - 1) / TT_BLOCK;
   return (unsigned)(blocks < 1 ? 1 : blocks > 16384 ? 16384 : blocks);
 }
-int runs_of(long long held, long long streamed) {
-  // about as many workgroups as two rounds of two on 256 compute units, eight steps at least in each
-  const long long blocks = (held + 255) / 256, steps = (streamed + STEP - 1) / STEP;
-  long long runs = 1024 / (blocks > 0 ? blocks : 1);
-  if (runs > steps / 8) runs = steps / 8;
-  if (runs > 256) runs = 256;
-  return (int)(runs < 1 ? 1 : runs);
+unsigned most_of(long long n) { return (unsigned)(n > 65536 ? 65536 : n); }
+template <class T> tt_status finish_dx(const TTNarrow &n, const float *parts, void *dx, long long ld, hipStream_t s) {
+  const dim3 grid(most_of(n.rows)), block(TT_BLOCK);
+  if (n.padded == 64) hipLaunchKernelGGL((k_narrow_dx<T, 64>), grid, block, 0, s, n, parts, (T *)dx, ld);
+  else hipLaunchKernelGGL((k_narrow_dx<T, 128>), grid, block, 0, s, n, parts, (T *)dx, ld);
+  return tt_launch_status();
 }
+template <class T> tt_status finish_dw(const TTNarrow &n, const float *parts, void *dw, void *db, hipStream_t s) {
+  const dim3 grid(most_of(n.classes)), block(TT_BLOCK);
+  if (n.padded == 64) hipLaunchKernelGGL((k_narrow_dw<T, 64>), grid, block, 0, s, n, parts, (T *)dw, (T *)db);
+  else hipLaunchKernelGGL((k_narrow_dw<T, 128>), grid, block, 0, s, n, parts, (T *)dw, (T *)db);
+  return tt_launch_status();
+}
+// Whether the classes are few enough for the rows to come in several runs (fewer rows that count never make it so).
+bool several(const TTNarrow &n) { return workgroups<CLASSES>(n) > (n.classes + (n.padded == 64 ? tile_of(64, CLASSES) : tile_of(128, CLASSES)) - 1) / (n.padded == 64 ? tile_of(64, CLASSES) : tile_of(128, CLASSES)); }
 
 }  // namespace
 
@@ -356,16 +486,28 @@ int runs_of(long long held, long long streamed) {
 #endif
 bool ttk_narrow_serves(int dtype, int dim) { return dtype != TT_F32 && dim <= TT_LOSS_NARROW; }
 int ttk_narrow_padded(int dim) { return dim <= 64 ? 64 : 128; }
-int ttk_narrow_runs(long long rows, int classes) { return runs_of(rows, classes); }
-int ttk_narrow_row_runs(long long rows, int classes) { return runs_of(classes, rows); }
 
-tt_status ttk_narrow_stats(const TTNarrow &n, float *stats, hipStream_t s) {
+size_t ttk_narrow_stats_bytes(const TTNarrow &n) { return (size_t)workgroups<STATS>(n) * (n.padded == 64 ? tile_of(64, STATS) : tile_of(128, STATS)) * 8; }
+size_t ttk_narrow_parts_bytes(const TTNarrow &n) {
+  const size_t dx = (size_t)workgroups<ROWS>(n) * (n.padded == 64 ? tile_of(64, ROWS) : tile_of(128, ROWS)) * n.padded * 4;
+  const size_t dw = several(n) ? (size_t)workgroups<CLASSES>(n) * (n.padded == 64 ? tile_of(64, CLASSES) : tile_of(128, CLASSES)) * (n.padded + 4) * 4 : 0;
+  return dx > dw ? dx : dw;
+}
+
+tt_status ttk_narrow_classes(const TTNarrow &n, hipStream_t s) {
+  const dim3 grid(grid_of((long long)n.classes * (n.copy ? n.padded / 8 : 1))), block(TT_BLOCK);
+  if (n.dtype == TT_BF16) hipLaunchKernelGGL(k_narrow_classes<ttg::bf16>, grid, block, 0, s, n, n.starts, (ttg::bf16 *)n.copy);
+  else hipLaunchKernelGGL(k_narrow_classes<ttg::f16>, grid, block, 0, s, n, n.starts, (ttg::f16 *)n.copy);
+  return tt_launch_status();
+}
+tt_status ttk_narrow_stats(const TTNarrow &n, float *stats, float *run, float *picked, hipStream_t s) {
   Args a = args_of(n, false);
   a.parts = stats;
-  a.runs = ttk_narrow_runs(n.rows, n.classes);
-  return launch(n, STATS, false, a, s);
-}
-tt_status ttk_narrow_picked(const TTNarrow &n, float *picked, hipStream_t s) {
+  tt_status st = launch<STATS>(n, false, a, s);
+  if (st != TT_OK) return st;
+  const int tile = n.padded == 64 ? tile_of(64, STATS) : tile_of(128, STATS), slots = slots_of(STATS), classes = n.classes;
+  hipLaunchKernelGGL(k_narrow_fold, dim3((unsigned)tt_ceil_div(n.rows, TT_BLOCK / 64)), dim3(TT_BLOCK), 0, s, (const float2 *)stats, (const int64_t *)n.r.offsets, classes,
+                     tile, slots, (float2 *)run);
   const dim3 grid((unsigned)tt_ceil_div(n.rows, TT_BLOCK / 16)), block(TT_BLOCK);
   if (n.dtype == TT_BF16) hipLaunchKernelGGL(k_narrow_picked<ttg::bf16>, grid, block, 0, s, n, picked);
   else hipLaunchKernelGGL(k_narrow_picked<ttg::f16>, grid, block, 0, s, n, picked);
@@ -374,26 +516,16 @@ tt_status ttk_narrow_picked(const TTNarrow &n, float *picked, hipStream_t s) {
 tt_status ttk_narrow_dx(const TTNarrow &n, float *parts, void *dx, long long ld_dx, hipStream_t s) {
   Args a = args_of(n, false);
   a.parts = parts;
-  a.runs = ttk_narrow_runs(n.rows, n.classes);
-  const tt_status st = launch(n, ROWS, false, a, s);
+  const tt_status st = launch<ROWS>(n, false, a, s);
   if (st != TT_OK) return st;
-  const dim3 grid(grid_of(n.rows * ((n.dim + 3) / 4))), block(TT_BLOCK);
-  const int runs = a.runs;
-  if (n.dtype == TT_BF16) hipLaunchKernelGGL(k_narrow_dx<ttg::bf16>, grid, block, 0, s, n, runs, (const float *)parts, (ttg::bf16 *)dx, ld_dx);
-  else hipLaunchKernelGGL(k_narrow_dx<ttg::f16>, grid, block, 0, s, n, runs, (const float *)parts, (ttg::f16 *)dx, ld_dx);
-  return tt_launch_status();
+  return n.dtype == TT_BF16 ? finish_dx<ttg::bf16>(n, parts, dx, ld_dx, s) : finish_dx<ttg::f16>(n, parts, dx, ld_dx, s);
 }
 tt_status ttk_narrow_dw(const TTNarrow &n, bool shares, float *parts, void *dw, void *dbias, hipStream_t s) {
   Args a = args_of(n, true);
   a.parts = parts;
   a.out = dw;
   a.sums = dbias;
-  a.runs = ttk_narrow_row_runs(n.rows, n.classes);
-  const tt_status st = launch(n, CLASSES, shares, a, s);
-  if (st != TT_OK || a.runs == 1) return st;
-  const dim3 grid(grid_of((long long)n.classes * ((n.dim + 3) / 4 + 1))), block(TT_BLOCK);
-  const int runs = a.runs;
-  if (n.dtype == TT_BF16) hipLaunchKernelGGL(k_narrow_dw<ttg::bf16>, grid, block, 0, s, n, runs, (const float *)parts, (ttg::bf16 *)dw, (ttg::bf16 *)dbias);
-  else hipLaunchKernelGGL(k_narrow_dw<ttg::f16>, grid, block, 0, s, n, runs, (const float *)parts, (ttg::f16 *)dw, (ttg::f16 *)dbias);
-  return tt_launch_status();
+  const tt_status st = launch<CLASSES>(n, shares, a, s);
+  if (st != TT_OK || !several(n)) return st;
+  return n.dtype == TT_BF16 ? finish_dw<ttg::bf16>(n, parts, dw, dbias, s) : finish_dw<ttg::f16>(n, parts, dw, dbias, s);
 }

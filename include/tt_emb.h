@@ -600,6 +600,9 @@ tt_status tt_route_backward(const tt_route *op, const void *logits, const int64_
 size_t tt_expert_order_workspace_bytes(int64_t n, int32_t num_experts);
 tt_status tt_expert_order(const int64_t *experts, int64_t n, int32_t num_experts, int64_t *offsets, int32_t *slots, int32_t *sources,
                           void *workspace, size_t workspace_bytes, void *stream);
+/* tt_route_forward and the order of what it gives, in one call (workspace: of tt_expert_order for rows * choices). */
+tt_status tt_route_order(const tt_route *op, const void *logits, const float *bias, int64_t *experts, float *weights, int64_t *offsets,
+                         int32_t *slots, int32_t *sources, void *workspace, size_t workspace_bytes, void *stream);
 
 /*
  * Rows to their experts and back.  slots [rows][choices] and sources [rows * choices] as above; places outside

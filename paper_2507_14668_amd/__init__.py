@@ -6,7 +6,7 @@ from .binding import (Plan, Prof, Table, alloc_batch_desc, tt_core_sgd_update_ba
 from .binding import (ORTHO_COEFFICIENTS, tt_core_ortho_update, tt_dense_backward, tt_dense_forward, tt_dense_workspace_bytes,  # noqa: F401
                       tt_orthogonalize)
 from .binding import (tt_cross_entropy_backward, tt_cross_entropy_forward, tt_cross_entropy_workspace_bytes, tt_expert_combine_backward,  # noqa: F401
-                      tt_expert_order, tt_layer_norm_backward, tt_layer_norm_forward, tt_route_backward, tt_route_forward)
+                      tt_expert_order, tt_layer_norm_backward, tt_layer_norm_forward, tt_route_backward, tt_route_forward, tt_route_order)
 from .module import (TTDense, TTEmbeddingBag, TTEmbeddingBagCollection, TTFusedEmbeddingBags, TTOrthoSGD, tt_dense)  # noqa: F401,E402
 from .module import (Routes, TTExperts, TTLayerNorm, TTSoftmaxLoss, tt_cross_entropy, tt_expert_combine, tt_expert_rows, tt_layer_norm,  # noqa: F401,E402
                      tt_route)

@@ -33,7 +33,7 @@ EXPORTS = ("tt_workspace_bytes", "tt_index_reorder", "tt_emb_bag_forward", "tt_e
            "tt_dense_workspace_bytes", "tt_dense_forward", "tt_dense_backward", "tt_orthogonalize_workspace_bytes", "tt_orthogonalize",
            "tt_core_ortho_workspace_bytes", "tt_core_ortho_update",
            "tt_layer_norm_workspace_bytes", "tt_layer_norm_forward", "tt_layer_norm_backward", "tt_route_forward", "tt_route_backward",
-           "tt_expert_order_workspace_bytes", "tt_expert_order", "tt_expert_rows", "tt_expert_combine", "tt_expert_combine_backward",
+           "tt_expert_order_workspace_bytes", "tt_expert_order", "tt_route_order", "tt_expert_rows", "tt_expert_combine", "tt_expert_combine_backward",
            "tt_cross_entropy_workspace_bytes", "tt_cross_entropy_forward", "tt_cross_entropy_backward")
 KERNELS = {"fwd_contract": 0, "bag_sum": 1, "grad_merge": 2, "bwd_contract": 3, "sort_scatter": 4, "sgd": 5,
            "p12_fill": 6, "bag_chains": 7}
@@ -212,6 +212,7 @@ def load_library():
                 ("tt_route_forward", ctypes.c_int, [vp] * 6), ("tt_route_backward", ctypes.c_int, [vp] * 6),
                 ("tt_expert_order_workspace_bytes", sz, [i64, ctypes.c_int32]),
                 ("tt_expert_order", ctypes.c_int, [vp, i64, ctypes.c_int32, vp, vp, vp, vp, sz, vp]),
+                ("tt_route_order", ctypes.c_int, [vp] * 9 + [sz, vp]),
                 ("tt_expert_rows", ctypes.c_int, [vp] * 6), ("tt_expert_combine", ctypes.c_int, [vp] * 7),
                 ("tt_expert_combine_backward", ctypes.c_int, [vp] * 9),
                 ("tt_cross_entropy_workspace_bytes", sz, [vp, ctypes.c_int]),
@@ -1042,6 +1043,30 @@ def tt_expert_order(experts, num_experts, workspace=None, stream=None):
     if st != TT_OK:
         raise TTError(st, "tt_expert_order")
     return offsets, slots, sources
+
+
+def tt_route_order(logits, k, bias=None, scores="softmax", groups=1, top_groups=None, renormalize=False, scale=1.0, workspace=None, stream=None):
+    """`tt_route_forward` and the `tt_expert_order` of what it gives in one call: `(weights, experts, offsets, slots, sources)`."""
+    op, dtype, at = _route_op(logits, k, scores, groups, top_groups, renormalize, scale)
+    on = _On(at, stream)
+    p_b = None if bias is None else _packed(bias, "bias", torch.float32, at, (op.experts,))
+    lib, shape, n = load_library(), (op.rows, op.choices), op.rows * op.choices
+    if max(n, op.experts) > 0x7fffffff:
+        raise TTError(TT_ERR_SHAPE, "tt_route_order")
+    experts, weights, offsets = on.empty(shape, torch.int64), on.empty(shape, torch.float32), on.empty((op.experts + 1,), torch.int64)
+    slots, sources = on.empty(shape, torch.int32), on.empty((n,), torch.int32)
+    p_work, size = None, 0
+    if workspace is not None:
+        p_work, size = _workspace(workspace, at)
+    elif n > 4096:  # fewer need none
+        workspace = on.empty(max(1, lib.tt_expert_order_workspace_bytes(n, op.experts)), torch.uint8)
+        p_work, size = workspace.data_ptr(), workspace.numel()
+    with on as s:
+        st = lib.tt_route_order(ctypes.byref(op), logits.data_ptr(), p_b, experts.data_ptr(), weights.data_ptr(), offsets.data_ptr(), slots.data_ptr(),
+                                sources.data_ptr(), p_work, size, s)
+    if st != TT_OK:
+        raise TTError(st, "tt_route_order")
+    return weights, experts, offsets, slots, sources
 
 
 def _deal_op(dtype, dim, slots, sources, at):

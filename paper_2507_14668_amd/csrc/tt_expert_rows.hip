@@ -81,67 +81,95 @@ template <class T, int LANES> __global__ void __launch_bounds__(TT_BLOCK) k_rows
   }
 }
 
-// out = residual + sum of weight * y, fp32, the choices in order.
-template <class T, int LANES> __global__ void __launch_bounds__(TT_BLOCK) k_combine(Deal p) {
-  constexpr int C = Chunk<T>::C, GROUPS = TT_BLOCK / LANES;
+// out = residual + sum of weight * y, fp32, the choices in order.  A lane has NV chunks of a row at a time (all of a row that they
+// cover), so that its loads for several choices are under way together.
+template <class T, int LANES, int NV> __global__ void __launch_bounds__(TT_BLOCK) k_combine(Deal p) {
+  constexpr int C = Chunk<T>::C, GROUPS = TT_BLOCK / LANES, WIDTH = LANES * C * NV;
   const int lane = threadIdx.x % LANES, group = threadIdx.x / LANES;
   for (long long r = (long long)blockIdx.x * GROUPS + group; r < p.rows; r += (long long)gridDim.x * GROUPS) {
-    for (int c = lane * C; c < p.n; c += LANES * C) {
-      float sum[C] = {};
+    for (int c0 = lane * C; c0 < p.n; c0 += WIDTH) {
+      float sum[NV][C] = {};
 #pragma unroll 4
       for (int j = 0; j < p.k; ++j) {
         const int s = place_of(p, r, j);
         if (s < 0) continue;
         const float w = p.weights ? p.weights[r * p.k + j] : 1.f;
-        Chunk<T> v;
-        v.load((const T *)p.y + s * p.ld_places + c, p.n - c);
+        Chunk<T> v[NV];
 #pragma unroll
-        for (int e = 0; e < C; ++e) sum[e] = fmaf(w, v.at(e), sum[e]);
-      }
-      if (p.residual) {
-        Chunk<T> v;
-        v.load((const T *)p.residual + r * p.ld_residual + c, p.n - c);
+        for (int i = 0; i < NV; ++i) v[i].load((const T *)p.y + s * p.ld_places + c0 + i * LANES * C, p.n - c0 - i * LANES * C);
 #pragma unroll
-        for (int e = 0; e < C; ++e) sum[e] += v.at(e);
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+          for (int e = 0; e < C; ++e) sum[i][e] = fmaf(w, v[i].at(e), sum[i][e]);
       }
-      store_n<T, C>((T *)p.out + r * p.ld_rows + c, p.n - c, sum);
+#pragma unroll
+      for (int i = 0; i < NV; ++i) {
+        const int c = c0 + i * LANES * C;
+        if (c >= p.n) break;
+        if (p.residual) {
+          Chunk<T> v;
+          v.load((const T *)p.residual + r * p.ld_residual + c, p.n - c);
+#pragma unroll
+          for (int e = 0; e < C; ++e) sum[i][e] += v.at(e);
+        }
+        store_n<T, C>((T *)p.out + r * p.ld_rows + c, p.n - c, sum[i]);
+      }
     }
   }
 }
 
-// dy = weight * grad in each place, dweight = <grad, y>.
-template <class T, int LANES> __global__ void __launch_bounds__(TT_BLOCK) k_combine_backward(Deal p) {
-  constexpr int C = Chunk<T>::C, GROUPS = TT_BLOCK / LANES;
+// dy = weight * grad in each place, dweight = <grad, y>.  With NV a row fits its lanes and its gradient is read once; without (0) it is read
+// for every choice.
+template <class T, int LANES, int NV> __global__ void __launch_bounds__(TT_BLOCK) k_combine_backward(Deal p) {
+  constexpr int C = Chunk<T>::C, GROUPS = TT_BLOCK / LANES, N = NV ? NV : 1;
   const int lane = threadIdx.x % LANES, group = threadIdx.x / LANES;
   for (long long r0 = (long long)blockIdx.x * GROUPS; r0 < p.rows; r0 += (long long)gridDim.x * GROUPS) {
     const bool live = r0 + group < p.rows;
     const long long r = live ? r0 + group : p.rows - 1;
+    Chunk<T> g[N];
+    if constexpr (NV != 0) {
+#pragma unroll
+      for (int i = 0; i < NV; ++i) g[i].load((const T *)p.grad + r * p.ld_rows + (i * LANES + lane) * C, p.n - (i * LANES + lane) * C);
+    }
+#pragma unroll 2
     for (int j = 0; j < p.k; ++j) {
       const int s = live ? place_of(p, r, j) : -1;
       const float w = s >= 0 && p.weights ? p.weights[r * p.k + j] : 1.f;
       const bool rest = live && p.dy && no_source(p, r * p.k + j);
       float dot = 0.f;
-      for (int c = lane * C; c < p.n; c += LANES * C) {
+      for (int c0 = lane * C; c0 < p.n; c0 += LANES * C * N) {
         if (s >= 0) {
-          Chunk<T> g;
-          g.load((const T *)p.grad + r * p.ld_rows + c, p.n - c);
+          if constexpr (NV == 0) g[0].load((const T *)p.grad + r * p.ld_rows + c0, p.n - c0);
+          Chunk<T> v[N];
           if (p.dweights) {
-            Chunk<T> v;
-            v.load((const T *)p.y + s * p.ld_places + c, p.n - c);
 #pragma unroll
-            for (int e = 0; e < C; ++e) dot = fmaf(g.at(e), v.at(e), dot);
+            for (int i = 0; i < N; ++i) v[i].load((const T *)p.y + s * p.ld_places + c0 + i * LANES * C, p.n - c0 - i * LANES * C);
           }
           if (p.dy) {
-            float d[C];
 #pragma unroll
-            for (int e = 0; e < C; ++e) d[e] = w * g.at(e);
-            store_n<T, C>((T *)p.dy + s * p.ld_dy + c, p.n - c, d);
+            for (int i = 0; i < N; ++i) {
+              const int c = c0 + i * LANES * C;
+              float d[C];
+#pragma unroll
+              for (int e = 0; e < C; ++e) d[e] = w * g[i].at(e);
+              if (c < p.n) store_n<T, C>((T *)p.dy + s * p.ld_dy + c, p.n - c, d);
+            }
+          }
+          if (p.dweights) {
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+#pragma unroll
+              for (int e = 0; e < C; ++e) dot = fmaf(g[i].at(e), v[i].at(e), dot);  // (zeros behind the row's end)
           }
         }
         if (rest) {
           Chunk<T> z;
           z.zero();
-          z.store((T *)p.dy + (r * p.k + j) * p.ld_dy + c, p.n - c);
+#pragma unroll
+          for (int i = 0; i < N; ++i) {
+            const int c = c0 + i * LANES * C;
+            if (c < p.n) z.store((T *)p.dy + (r * p.k + j) * p.ld_dy + c, p.n - c);
+          }
         }
       }
       if (p.dweights) {
@@ -181,17 +209,22 @@ Deal describe(const tt_deal *op) {
   return p;
 }
 enum Which { ROWS, COMBINE, BACKWARD };
-template <class T, int LANES> void launch_lanes(const Deal &p, Which which, hipStream_t s) {
+template <class T, int LANES, int NV> void launch_as(const Deal &p, Which which, hipStream_t s) {
   long long blocks = (p.rows + TT_BLOCK / LANES - 1) / (TT_BLOCK / LANES);
   if (blocks > 65536) blocks = 65536;
   const dim3 grid((unsigned)blocks), block(TT_BLOCK);
   if (which == ROWS) hipLaunchKernelGGL((k_rows<T, LANES>), grid, block, 0, s, p);
-  else if (which == COMBINE) hipLaunchKernelGGL((k_combine<T, LANES>), grid, block, 0, s, p);
-  else hipLaunchKernelGGL((k_combine_backward<T, LANES>), grid, block, 0, s, p);
+  else if (which == COMBINE) hipLaunchKernelGGL((k_combine<T, LANES, NV ? NV : 4>), grid, block, 0, s, p);
+  else hipLaunchKernelGGL((k_combine_backward<T, LANES, NV>), grid, block, 0, s, p);
 }
 template <class T> tt_status launch(const Deal &p, Which which, hipStream_t s) {
-  if (p.n <= 32 * Chunk<T>::C) launch_lanes<T, 16>(p, which, s);
-  else launch_lanes<T, 64>(p, which, s);
+  const int chunks = tt_ceil_div(p.n, Chunk<T>::C);
+  if (chunks <= 16) launch_as<T, 16, 1>(p, which, s);
+  else if (chunks <= 32) launch_as<T, 16, 2>(p, which, s);
+  else if (chunks <= 64) launch_as<T, 64, 1>(p, which, s);
+  else if (chunks <= 128) launch_as<T, 64, 2>(p, which, s);
+  else if (chunks <= 256) launch_as<T, 64, 4>(p, which, s);
+  else launch_as<T, 64, 0>(p, which, s);
   return tt_launch_status();
 }
 tt_status launch(int dtype, const Deal &p, Which which, hipStream_t s) {

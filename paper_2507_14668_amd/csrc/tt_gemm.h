@@ -44,6 +44,7 @@ struct TTGemm {
   float alpha, beta;
   int epilogue;                // TT_GEMM_PLAIN ...
   int a_padded;                // 16-bit A whose rows go on with zeros (K-contiguous) or anything (else) up to a multiple of 8
+  int b_padded;                // the same of a row-contiguous B whose rows go on with anything
   float *stats;                // STATS: pairs [column tile][M]
   float *picked;               // STATS: [M]
   const int32_t *labels;       // STATS, SOFTMAX: [M], first + the label's column; others are no column's

@@ -290,7 +290,7 @@ bool ttk_gemm_direct_serves(const TTGemm &g) {
   if (g.dtype == TT_F32 || g.out_dtype != g.dtype || g.symmetric) return false;
   const uintptr_t addresses = (uintptr_t)g.a | (uintptr_t)g.b;
   if ((addresses & 15) || ((g.lda | g.ldb | g.a_step | g.b_step) & 7)) return false;
-  if (((g.a_kc || g.b_kc) && (g.K & 7) && !(g.a_padded && !g.b_kc)) || (!g.a_kc && (g.M & 7) && !g.a_padded) || (!g.b_kc && (g.N & 7))) return false;
+  if (((g.a_kc || g.b_kc) && (g.K & 7) && !(g.a_padded && !g.b_kc)) || (!g.a_kc && (g.M & 7) && !g.a_padded) || (!g.b_kc && (g.N & 7) && !g.b_padded)) return false;
   if (g.epilogue != TT_GEMM_PLAIN && g.M <= TT_GEMM_DIRECT_LEAST) return false;
   if (g.lda > (1 << 23) || g.ldb > (1 << 23)) return false;  // offsets within a tile are 32 bits
   // half a tile would be empty

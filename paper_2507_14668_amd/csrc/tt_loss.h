@@ -18,6 +18,17 @@ struct TTLossRows {
 
 #define TT_LOSS_STEP 32
 
+#ifdef __HIPCC__
+// What place i's row has for its loss and lse: s is its largest logit (or one near it) and the sum of exp(logit - that).
+__device__ __forceinline__ void ttk_loss_of(const TTLossRows &w, long long i, float2 s, float picked, float *loss, float *lse) {
+  const bool bad = w.label[i] < 0;
+  const int r = w.of[i];
+  lse[r] = bad ? NAN : s.x + logf(s.y);
+  // (the difference of the logits first: near a loss of zero lse less the label's logit would be lse's rounding)
+  loss[r] = bad ? NAN : (s.x - picked) + logf(s.y);
+}
+#endif
+
 struct TTNarrow {
   int dtype, dim, padded, classes;
   long long rows;
@@ -33,7 +44,6 @@ int ttk_narrow_padded(int dim);
 size_t ttk_narrow_stats_bytes(const TTNarrow &n);  // (sizes alone are looked at)
 size_t ttk_narrow_parts_bytes(const TTNarrow &n);
 tt_status ttk_narrow_classes(const TTNarrow &n, hipStream_t s);  // writes starts and copy: before the others
-// run: of each place about its largest logit and the sum of exp(logit - that), pairs; picked: the label's logit
-tt_status ttk_narrow_stats(const TTNarrow &n, float *stats, float *run, float *picked, hipStream_t s);
+tt_status ttk_narrow_stats(const TTNarrow &n, float *stats, float *loss, float *lse, hipStream_t s);
 tt_status ttk_narrow_dx(const TTNarrow &n, float *parts, void *dx, long long ld_dx, hipStream_t s);
 tt_status ttk_narrow_dw(const TTNarrow &n, bool shares, float *parts, void *dw, void *dbias, hipStream_t s);

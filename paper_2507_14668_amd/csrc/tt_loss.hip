@@ -12,7 +12,7 @@ typedef TTLossRows Rows;
 // One workgroup: places in the order of the rows.  In the backward also each place's lse and share of the loss's gradient.
 constexpr int SCAN = 512;
 __global__ void __launch_bounds__(SCAN) k_loss_rows(const int64_t *labels, long long rows, int classes, long long ignored, int reduce, const float *lse,
-                                                    const float *grad, int bits, int half, int negative, Rows w) {
+                                                    const float *grad, int bits, int half, int negative, float *loss, float *lse_out, Rows w) {
   __shared__ int tmp[SCAN / 64 + 1];
   __shared__ float tops[SCAN / 64];
   int places = 0;
@@ -23,6 +23,7 @@ __global__ void __launch_bounds__(SCAN) k_loss_rows(const int64_t *labels, long 
     int total;
     const int at = places + tt_block_excl_scan_n<SCAN>(counts ? 1 : 0, tmp, &total);
     if (r < rows) w.at[r] = counts ? at : -1;
+    if (loss && r < rows && !counts) loss[r] = lse_out[r] = 0.f;
     if (counts) {
       w.of[at] = (int32_t)r;
       w.label[at] = label >= 0 && label < classes ? (int32_t)label : -1;
@@ -87,34 +88,26 @@ template <class T> __global__ void __launch_bounds__(TT_BLOCK) k_loss_gather(con
   }
 }
 
-// A piece's tiles into each row's running pair (largest logit, sum of exp(logit - it)); a wavefront takes 64 rows and a share of the tiles.
-__global__ void __launch_bounds__(TT_BLOCK) k_loss_fold(const float2 *__restrict__ stats, int tiles, long long rows, int first, Rows w, float2 *run) {
+// A piece's tiles into each place's running pair (largest logit, sum of exp(logit - it)), sixteen places a workgroup and sixteen runs of the tiles;
+// of the last piece the row's lse and loss.
+__global__ void __launch_bounds__(TT_BLOCK) k_loss_fold(const float2 *__restrict__ stats, int tiles, long long rows, int first, int last, Rows w, float2 *run,
+                                                        const float *picked, float *loss, float *lse) {
   __shared__ float2 part[TT_BLOCK];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const long long i = (long long)blockIdx.x * 64 + lane, places = w.offsets[1];
+  const int lane = threadIdx.x & 15, seg = threadIdx.x >> 4, per = (tiles + 15) / 16;
+  const long long i = (long long)blockIdx.x * 16 + lane, places = w.offsets[1];
   float2 s = {-INFINITY, 0.f};
-  if (i < places)
-    for (int t = wave; t < tiles; t += TT_BLOCK / 64) s = join_stats(s, stats[t * rows + i]);
+  if (i < places) {
+    const int end = (seg + 1) * per < tiles ? (seg + 1) * per : tiles;
+#pragma unroll 4
+    for (int t = seg * per; t < end; ++t) s = join_stats(s, stats[t * rows + i]);
+  }
   part[threadIdx.x] = s;
   __syncthreads();
-  if (wave != 0 || i >= places) return;
-  for (int k = 1; k < TT_BLOCK / 64; ++k) s = join_stats(s, part[64 * k + lane]);
-  run[i] = first ? s : join_stats(run[i], s);
-}
-__global__ void __launch_bounds__(TT_BLOCK) k_loss_of_rows(long long rows, Rows w, const float2 *run, const float *picked, float *loss, float *lse) {
-  const long long r = (long long)blockIdx.x * TT_BLOCK + threadIdx.x;
-  if (r >= rows) return;
-  const int at = w.at[r];
-  float l = 0.f, v = 0.f;
-  if (at >= 0) {
-    const float2 s = run[at];
-    const bool bad = w.label[at] < 0;
-    l = bad ? NAN : s.x + logf(s.y);
-    // (the sum of the label's own and the others: near a loss of zero the difference of two large numbers would be their rounding)
-    v = bad ? NAN : (s.x - picked[at]) + logf(s.y);
-  }
-  lse[r] = l;
-  loss[r] = v;
+  if (seg != 0 || i >= places) return;
+  for (int k = 1; k < 16; ++k) s = join_stats(s, part[16 * k + lane]);
+  if (!first) s = join_stats(run[i], s);
+  if (last) ttk_loss_of(w, i, s, picked[i], loss, lse);
+  else run[i] = s;
 }
 // One workgroup: the sum or the mean, in 64 bits.
 __global__ void __launch_bounds__(SCAN) k_loss_sum(const float *each, long long rows, Rows w, int reduce, float *loss) {
@@ -132,17 +125,28 @@ __global__ void __launch_bounds__(SCAN) k_loss_sum(const float *each, long long 
 }
 
 // dx from its sums in the order of the places; zeros in rows that do not count
-template <class T> __global__ void __launch_bounds__(TT_BLOCK) k_loss_dx(const float *acc, long long rows, int dim, Rows w, T *dx, long long ld) {
+template <class T> __global__ void __launch_bounds__(TT_BLOCK) k_loss_dx(const float *acc, int ld_acc, long long rows, int dim, Rows w, T *dx, long long ld) {
   const int per = (dim + 3) / 4;
   const float back = w.back[0];
   for (long long e = (long long)blockIdx.x * TT_BLOCK + threadIdx.x; e < rows * per; e += (long long)gridDim.x * TT_BLOCK) {
     const long long r = e / per;
     const int c = (int)(e - r * per) * 4, at = w.at[r];
     float v[4] = {0.f, 0.f, 0.f, 0.f};
-    if (at >= 0) load4(acc + (long long)at * dim + c, dim - c, v);
+    if (at >= 0) load4(acc + (long long)at * ld_acc + c, dim - c, v);
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[i] *= back;
     store4(dx + r * ld + c, dim - c, v);
+  }
+}
+// Rows of W with zeros up to a multiple of 8.
+template <class T> __global__ void __launch_bounds__(TT_BLOCK) k_loss_pad(const T *w, long long rows, int dim, T *to, int ld) {
+  const int per = ld / 8;
+  for (long long e = (long long)blockIdx.x * TT_BLOCK + threadIdx.x; e < rows * per; e += (long long)gridDim.x * TT_BLOCK) {
+    const long long r = e / per;
+    const int c = (int)(e - r * per) * 8;
+    float v[8];
+    load_n<T, 8>(w + r * dim + c, dim - c, v);
+    store_n<T, 8>(to + r * ld + c, 8, v);
   }
 }
 template <class T> __global__ void __launch_bounds__(TT_BLOCK) k_loss_clear(T *p, long long n) {
@@ -177,6 +181,13 @@ long long piece_of(const tt_loss *op, bool backward) {
   return ((op->classes + pieces - 1) / pieces + 255) / 256 * 256;
 }
 bool narrow(const tt_loss *op) { return ttk_narrow_serves(op->dtype, op->dim); }
+// 16-bit rows of a W whose length is no multiple of 8 elements are copied to ones that are, a piece at a time, so that the large tiles serve: the copy costs
+// four bytes an element at 4.5 TB/s, the tiles save the difference between 330 and 1100 TFLOP/s in every product; 1001 rows of 479 against
+// 50001 classes COPY us with it, 178 without.  Few rows do not pay for it.
+#ifndef TT_LOSS_COPY_ROWS
+#define TT_LOSS_COPY_ROWS 256
+#endif
+bool copies(const tt_loss *op) { return op->dtype != TT_F32 && !narrow(op) && (op->dim & 7) && op->rows >= TT_LOSS_COPY_ROWS; }
 int padded(const tt_loss *op) { return narrow(op) ? ttk_narrow_padded(op->dim) : (op->dim + 7) & ~7; }
 
 void describe(const tt_loss *op, TTGemm *g) {
@@ -191,8 +202,8 @@ TTGemm of_logits(const tt_loss *op, int classes, bool backward, long long ldg) {
   describe(op, &g);
   g.a_kc = g.b_kc = 1;
   g.mode = TT_GEMM_RAGGED_M;
-  g.M = (int)op->rows; g.N = classes; g.K = op->dim;
-  g.lda = padded(op); g.ldb = op->dim; g.ldo = ldg;
+  g.M = (int)op->rows; g.N = classes; g.K = copies(op) ? padded(op) : op->dim;
+  g.lda = padded(op); g.ldb = g.K; g.ldo = ldg;
   g.epilogue = backward ? TT_GEMM_SOFTMAX : TT_GEMM_STATS;
   g.zero_rest = backward;
   g.n_padded = (classes + 7) & ~7;
@@ -202,8 +213,8 @@ TTGemm of_dx(const tt_loss *op, int classes, long long ldg) {  // G W
   TTGemm g;
   describe(op, &g);
   g.a_kc = 1; g.b_kc = 0;
-  g.M = (int)op->rows; g.N = op->dim; g.K = classes;
-  g.lda = ldg; g.ldb = op->dim; g.ldo = op->dim;
+  g.M = (int)op->rows; g.N = copies(op) ? padded(op) : op->dim; g.K = classes;
+  g.lda = ldg; g.ldb = g.ldo = g.N;
   g.a_padded = 1;
   g.epilogue = TT_GEMM_ACC;
   return g;
@@ -215,7 +226,7 @@ TTGemm of_dw(const tt_loss *op, int classes, long long ldg, bool column) {  // G
   g.M = classes; g.N = column ? 1 : op->dim; g.K = (int)op->rows;
   g.like_N = op->dim;
   g.lda = ldg; g.ldb = column ? ldg : padded(op); g.ldo = g.N;
-  g.a_padded = 1;
+  g.a_padded = g.b_padded = 1;
   g.epilogue = op->dtype == TT_F32 ? TT_GEMM_PLAIN : TT_GEMM_SCALED;
   return g;
 }
@@ -243,6 +254,7 @@ Scratch scratch(const tt_loss *op, bool backward) {
   take(w.back, 4);
   take(w.offsets, 16);
   take(w.x, rows * padded(op) * es);
+  if (copies(op)) take(w.copy, (size_t)(piece < op->classes ? piece : op->classes) * padded(op) * es);
   if (narrow(op)) {
     take(w.starts, ((size_t)op->classes + TT_LOSS_STEP) * 4);
     take(w.copy, (size_t)op->classes * padded(op) * es);  // (whether it is used is known with w's address only)
@@ -262,7 +274,7 @@ Scratch scratch(const tt_loss *op, bool backward) {
     return w;
   }
   take(w.grads, rows * piece * es);
-  take(w.acc, rows * op->dim * 4);
+  take(w.acc, rows * (copies(op) ? padded(op) : op->dim) * 4);
   take(w.column, (size_t)piece * es);
   size_t most = 0;
   const int last = (int)(op->classes - (op->classes - 1) / piece * piece);
@@ -296,9 +308,15 @@ template <class T> tt_status gather(const tt_loss *op, const void *x, const Rows
   return tt_launch_status();
 }
 template <class T> tt_status write_dx(const tt_loss *op, const float *acc, const Rows &r, void *dx, hipStream_t s) {
-  const int dim = op->dim;
+  const int dim = op->dim, ld_acc = copies(op) ? padded(op) : op->dim;
   const long long rows = op->rows, ld = op->ld_dx ? op->ld_dx : op->dim;
-  hipLaunchKernelGGL(k_loss_dx<T>, dim3(grid_of(rows * tt_ceil_div(dim, 4))), dim3(TT_BLOCK), 0, s, acc, rows, dim, r, (T *)dx, ld);
+  hipLaunchKernelGGL(k_loss_dx<T>, dim3(grid_of(rows * tt_ceil_div(dim, 4))), dim3(TT_BLOCK), 0, s, acc, ld_acc, rows, dim, r, (T *)dx, ld);
+  return tt_launch_status();
+}
+template <class T> tt_status pad(const tt_loss *op, const void *w, int classes, void *to, hipStream_t s) {
+  const int dim = op->dim, ld = padded(op);
+  const long long rows = classes;
+  hipLaunchKernelGGL(k_loss_pad<T>, dim3(grid_of(rows * (ld / 8))), dim3(TT_BLOCK), 0, s, (const T *)w, rows, dim, (T *)to, ld);
   return tt_launch_status();
 }
 template <class T> tt_status clear(void *p, long long n, hipStream_t s) {
@@ -338,7 +356,7 @@ extern "C" tt_status tt_cross_entropy_forward(const tt_loss *op, const void *x, 
   const long long rows = op->rows, ignored = op->ignore_index, piece = piece_of(op, false);
   const int classes = op->classes, reduce = op->reduce;
   float *each = whole ? (float *)(ws + need.each) : loss;
-  hipLaunchKernelGGL(k_loss_rows, dim3(1), dim3(SCAN), 0, s, labels, rows, classes, ignored, reduce, (const float *)nullptr, (const float *)nullptr, 0, 0, 0, r);
+  hipLaunchKernelGGL(k_loss_rows, dim3(1), dim3(SCAN), 0, s, labels, rows, classes, ignored, reduce, (const float *)nullptr, (const float *)nullptr, 0, 0, 0, each, lse, r);
   if ((st = tt_launch_status()) != TT_OK) return st;
   if (some) {
     if ((st = TT_BY_TYPE(gather, op->dtype, op, x, r, ws + need.x, s)) != TT_OK) return st;
@@ -346,13 +364,17 @@ extern "C" tt_status tt_cross_entropy_forward(const tt_loss *op, const void *x, 
     if (narrow(op)) {
       const TTNarrow n = narrow_of(op, w, bias, ws, need);
       if ((st = ttk_narrow_classes(n, s)) != TT_OK) return st;
-      if ((st = ttk_narrow_stats(n, (float *)(ws + need.stats), (float *)run, (float *)(ws + need.picked), s)) != TT_OK) return st;
+      if ((st = ttk_narrow_stats(n, (float *)(ws + need.stats), each, lse, s)) != TT_OK) return st;
     }
     for (long long c = 0; c < classes && !narrow(op); c += piece) {
       const int n = (int)(classes - c < piece ? classes - c : piece);
       TTGemm g = of_logits(op, n, false, 0);
       g.a = ws + need.x;
       g.b = (const char *)w + (size_t)c * op->dim * es;
+      if (copies(op)) {
+        if ((st = TT_BY_TYPE(pad, op->dtype, op, g.b, n, ws + need.copy, s)) != TT_OK) return st;
+        g.b = ws + need.copy;
+      }
       g.bias = bias ? (const char *)bias + (size_t)c * es : nullptr;
       g.offsets = r.offsets;
       g.stats = (float *)(ws + need.stats);
@@ -360,11 +382,10 @@ extern "C" tt_status tt_cross_entropy_forward(const tt_loss *op, const void *x, 
       g.labels = r.label;
       g.first = (int)c;
       if ((st = ttk_gemm(g, nullptr, s)) != TT_OK) return st;
-      const int tiles = tt_ceil_div(n, ttk_gemm_tile(g)), first = c == 0;
-      hipLaunchKernelGGL(k_loss_fold, dim3((unsigned)tt_ceil_div(rows, 64)), dim3(TT_BLOCK), 0, s, (const float2 *)g.stats, tiles, rows, first, r, run);
+      const int tiles = tt_ceil_div(n, ttk_gemm_tile(g)), first = c == 0, last = c + n == classes;
+      hipLaunchKernelGGL(k_loss_fold, dim3((unsigned)tt_ceil_div(rows, 16)), dim3(TT_BLOCK), 0, s, (const float2 *)g.stats, tiles, rows, first, last, r, run,
+                         (const float *)g.picked, each, lse);
     }
-    hipLaunchKernelGGL(k_loss_of_rows, dim3((unsigned)tt_ceil_div(rows, TT_BLOCK)), dim3(TT_BLOCK), 0, s, rows, r, (const float2 *)run,
-                       (const float *)(ws + need.picked), each, lse);
   }
   if (whole) hipLaunchKernelGGL(k_loss_sum, dim3(1), dim3(SCAN), 0, s, (const float *)each, rows, r, reduce, loss);
   return tt_launch_status();
@@ -397,7 +418,7 @@ extern "C" tt_status tt_cross_entropy_backward(const tt_loss *op, const void *x,
   const Rows r = rows_of(ws, need);
   const long long rows = op->rows, ignored = op->ignore_index, piece = piece_of(op, true);
   const int classes = op->classes, reduce = op->reduce, bits = op->dtype == TT_F32 ? 32 : 16, half = op->dtype == TT_F16, negative = narrow(op);
-  hipLaunchKernelGGL(k_loss_rows, dim3(1), dim3(SCAN), 0, s, labels, rows, classes, ignored, reduce, lse, grad_loss, bits, half, negative, r);
+  hipLaunchKernelGGL(k_loss_rows, dim3(1), dim3(SCAN), 0, s, labels, rows, classes, ignored, reduce, lse, grad_loss, bits, half, negative, (float *)nullptr, (float *)nullptr, r);
   if ((st = tt_launch_status()) != TT_OK) return st;
   if ((st = TT_BY_TYPE(gather, op->dtype, op, x, r, ws + need.x, s)) != TT_OK) return st;
   if (narrow(op)) {
@@ -410,6 +431,10 @@ extern "C" tt_status tt_cross_entropy_backward(const tt_loss *op, const void *x,
   for (long long c = 0; c < classes; c += piece) {
     const int n = (int)(classes - c < piece ? classes - c : piece);
     const char *wc = (const char *)w + (size_t)c * op->dim * es;
+    if (copies(op)) {
+      if ((st = TT_BY_TYPE(pad, op->dtype, op, wc, n, ws + need.copy, s)) != TT_OK) return st;
+      wc = ws + need.copy;
+    }
     TTGemm g = of_logits(op, n, true, piece);
     g.a = ws + need.x;
     g.b = wc;

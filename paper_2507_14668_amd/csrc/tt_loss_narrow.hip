@@ -320,37 +320,28 @@ template <class T, int KP, Mode MODE, bool SHARES> __global__ void __launch_boun
   }
 }
 
-// The runs' statistics of each place together, a wavefront a place.
-__global__ void __launch_bounds__(TT_BLOCK) k_narrow_fold(const float2 *__restrict__ parts, const int64_t *offsets, int classes, int tile, int slots, float2 *run) {
+// Each place's statistics of all runs together, the label's logit as a product of its own, and what the row has of it: a wavefront a place.
+template <class T> __global__ void __launch_bounds__(TT_BLOCK) k_narrow_fold(TTNarrow n, const float2 *__restrict__ parts, int tile, int slots, float *loss, float *lse) {
   const int lane = threadIdx.x & 63;
-  const long long i = (long long)blockIdx.x * (TT_BLOCK / 64) + (threadIdx.x >> 6), places = offsets[1];
+  const long long i = (long long)blockIdx.x * (TT_BLOCK / 64) + (threadIdx.x >> 6), places = n.r.offsets[1];
   if (i >= places) return;
-  const Cut cut = cut_of(places, classes, tile, slots);
+  const Cut cut = cut_of(places, n.classes, tile, slots);
   const long long block = i / tile;
+  const int label = n.r.label[i];
   float2 s = {-INFINITY, 0.f};
   for (int k = lane; k < cut.runs; k += 64) s = join_stats(s, parts[(k * (long long)cut.blocks + block) * tile + i % tile]);
+  float z = 0.f;
+  if (label >= 0) {
 #pragma unroll
-  for (int o = 1; o < 64; o *= 2) s = join_stats(s, float2{__shfl(s.x, lane ^ o, 64), __shfl(s.y, lane ^ o, 64)});
-  if (lane == 0) run[i] = s;
-}
-
-// z of each place's label, as a product of its own: 16 lanes a place
-template <class T> __global__ void __launch_bounds__(TT_BLOCK) k_narrow_picked(TTNarrow n, float *picked) {
-  const int lane = threadIdx.x % 16;
-  const long long i = (long long)blockIdx.x * (TT_BLOCK / 16) + threadIdx.x / 16;
-  const bool in = i < n.r.offsets[1];
-  const int label = in ? n.r.label[i] : -1;
-  float v[8] = {}, w[8] = {}, s = 0.f;
-  const int left = label >= 0 ? n.dim - 8 * lane : 0;
-  if (left > 0) {
-    load_n<T, 8>((const T *)n.x + i * n.padded + 8 * lane, left, v);
-    load_n<T, 8>((const T *)n.w + (long long)label * n.dim + 8 * lane, left, w);
+    for (int c = lane; c < 128; c += 64)
+      if (c < n.dim) z = fmaf(to_f32(((const T *)n.x)[i * n.padded + c]), to_f32(((const T *)n.w)[(long long)label * n.dim + c]), z);
   }
 #pragma unroll
-  for (int e = 0; e < 8; ++e) s = fmaf(v[e], w[e], s);
-#pragma unroll
-  for (int o = 8; o > 0; o >>= 1) s += __shfl(s, (threadIdx.x & 63) ^ o, 64);
-  if (in && lane == 0) picked[i] = s + (n.bias && label >= 0 ? to_f32(((const T *)n.bias)[label]) : 0.f);
+  for (int o = 1; o < 64; o *= 2) {
+    s = join_stats(s, float2{__shfl(s.x, lane ^ o, 64), __shfl(s.y, lane ^ o, 64)});
+    z += __shfl(z, lane ^ o, 64);
+  }
+  if (lane == 0) ttk_loss_of(n.r, i, s, z + (label >= 0 ? n.starts[label] : 0.f), loss, lse);
 }
 
 // A workgroup's sum of the runs' parts of one vector, `width` columns (of four a thread) in eight runs that are added in order: in the threads of the first.
@@ -500,17 +491,16 @@ tt_status ttk_narrow_classes(const TTNarrow &n, hipStream_t s) {
   else hipLaunchKernelGGL(k_narrow_classes<ttg::f16>, grid, block, 0, s, n, n.starts, (ttg::f16 *)n.copy);
   return tt_launch_status();
 }
-tt_status ttk_narrow_stats(const TTNarrow &n, float *stats, float *run, float *picked, hipStream_t s) {
+tt_status ttk_narrow_stats(const TTNarrow &n, float *stats, float *loss, float *lse, hipStream_t s) {
   Args a = args_of(n, false);
   a.parts = stats;
   tt_status st = launch<STATS>(n, false, a, s);
   if (st != TT_OK) return st;
-  const int tile = n.padded == 64 ? tile_of(64, STATS) : tile_of(128, STATS), slots = slots_of(STATS), classes = n.classes;
-  hipLaunchKernelGGL(k_narrow_fold, dim3((unsigned)tt_ceil_div(n.rows, TT_BLOCK / 64)), dim3(TT_BLOCK), 0, s, (const float2 *)stats, (const int64_t *)n.r.offsets, classes,
-                     tile, slots, (float2 *)run);
-  const dim3 grid((unsigned)tt_ceil_div(n.rows, TT_BLOCK / 16)), block(TT_BLOCK);
-  if (n.dtype == TT_BF16) hipLaunchKernelGGL(k_narrow_picked<ttg::bf16>, grid, block, 0, s, n, picked);
-  else hipLaunchKernelGGL(k_narrow_picked<ttg::f16>, grid, block, 0, s, n, picked);
+  const int tile = n.padded == 64 ? tile_of(64, STATS) : tile_of(128, STATS), slots = slots_of(STATS);
+  const dim3 grid((unsigned)tt_ceil_div(n.rows, TT_BLOCK / 64)), block(TT_BLOCK);
+  const float2 *parts = (const float2 *)stats;
+  if (n.dtype == TT_BF16) hipLaunchKernelGGL(k_narrow_fold<ttg::bf16>, grid, block, 0, s, n, parts, tile, slots, loss, lse);
+  else hipLaunchKernelGGL(k_narrow_fold<ttg::f16>, grid, block, 0, s, n, parts, tile, slots, loss, lse);
   return tt_launch_status();
 }
 tt_status ttk_narrow_dx(const TTNarrow &n, float *parts, void *dx, long long ld_dx, hipStream_t s) {

@@ -533,3 +533,22 @@ extern "C" tt_status tt_expert_order(const int64_t *experts, int64_t n, int32_t 
                      offsets, slots, sources);
   return tt_launch_status();
 }
+
+extern "C" tt_status tt_route_order(const tt_route *op, const void *logits, const float *bias, int64_t *experts, float *weights, int64_t *offsets, int32_t *slots,
+                                    int32_t *sources, void *workspace, size_t workspace_bytes, void *stream) {
+  tt_status st = check(op);
+  if (st != TT_OK) return st;
+  const int64_t n = op->rows * op->choices;
+  // what the second call would refuse is refused before the first one has begun
+  if (!offsets || !aligned(offsets, 8) || (n > 0 && (!slots || !sources || !aligned(slots, 4) || !aligned(sources, 4)))) return TT_ERR_INVALID_ARG;
+  const void *outs[5] = {experts, weights, offsets, slots, sources};
+  for (int i = 0; i < 5; ++i) {
+    if (outs[i] && (outs[i] == logits || outs[i] == (const void *)bias)) return TT_ERR_INVALID_ARG;
+    for (int j = 0; j < i; ++j)
+      if (outs[i] && outs[i] == outs[j]) return TT_ERR_INVALID_ARG;
+  }
+  const size_t need = tt_expert_order_workspace_bytes(n, op->experts);
+  if (need && (!workspace || ((uintptr_t)workspace & 255) != 0 || workspace_bytes < need)) return TT_ERR_WORKSPACE;
+  st = tt_route_forward(op, logits, bias, experts, weights, stream);
+  return st == TT_OK ? tt_expert_order(experts, n, op->experts, offsets, slots, sources, workspace, workspace_bytes, stream) : st;
+}

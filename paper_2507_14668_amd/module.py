@@ -253,19 +253,19 @@ class Routes(NamedTuple):
 
 
 class _RouteFunction(torch.autograd.Function):
+    """The weights that the library has formed, with the logits' gradient behind them."""
+
     @staticmethod
-    def forward(ctx, logits, k, bias, scores, groups, top_groups, renormalize, scale):
-        experts, weights = binding.tt_route_forward(logits, k, bias, scores, groups, top_groups, renormalize, scale)
-        ctx.how = dict(scores=scores, renormalize=renormalize, scale=scale)
+    def forward(ctx, logits, weights, experts, how):
+        ctx.how = how
         ctx.save_for_backward(logits, experts)
-        ctx.mark_non_differentiable(experts)
-        return weights, experts
+        return weights.view_as(weights)
 
     @staticmethod
     @torch.autograd.function.once_differentiable
-    def backward(ctx, grad_weights, _):
+    def backward(ctx, grad_weights):
         logits, experts = ctx.saved_tensors
-        return (binding.tt_route_backward(logits, experts, grad_weights.contiguous(), **ctx.how),) + (None,) * 7
+        return binding.tt_route_backward(logits, experts, grad_weights.contiguous(), *ctx.how), None, None, None
 
 
 def tt_route(logits, k: int, bias=None, scores: str = "softmax", groups: int = 1, top_groups=None, renormalize: bool = False, scale: float = 1.0) -> Routes:
@@ -273,11 +273,10 @@ def tt_route(logits, k: int, bias=None, scores: str = "softmax", groups: int = 1
     differentiable in the logits (`bias`, float32 [experts], chooses only and gets no gradient)."""
     logits = _row_major(logits)
     bias = None if bias is None else _packed(bias.detach())
-    if not _trained(logits) and not _dual():
-        experts, weights = binding.tt_route_forward(logits, k, bias, scores, groups, top_groups, renormalize, scale)
-    else:
-        weights, experts = _RouteFunction.apply(logits, k, bias, scores, groups, top_groups, renormalize, scale)
-    return Routes(weights, experts, *binding.tt_expert_order(experts, logits.shape[1]))
+    weights, *rest = binding.tt_route_order(logits, k, bias, scores, groups, top_groups, renormalize, scale)
+    if _trained(logits) or _dual():
+        weights = _RouteFunction.apply(logits, weights, rest[0], (scores, renormalize, scale))
+    return Routes(weights, *rest)
 
 
 class _RowsFunction(torch.autograd.Function):

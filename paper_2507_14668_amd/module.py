@@ -193,6 +193,15 @@ def _packed(t):
     return t if t is None or t.is_contiguous() else t.contiguous()
 
 
+def _once(backward):
+    """`once_differentiable`, asked where a graph of the backward pass is made; elsewhere it would say nothing, and take 7 us on the host."""
+    asked = torch.autograd.function.once_differentiable(backward)
+
+    def call(ctx, *grads):
+        return asked(ctx, *grads) if torch.is_grad_enabled() else backward(ctx, *grads)
+    return call
+
+
 class _NormFunction(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight, bias, eps):
@@ -202,7 +211,7 @@ class _NormFunction(torch.autograd.Function):
         return out
 
     @staticmethod
-    @torch.autograd.function.once_differentiable
+    @_once
     def backward(ctx, grad_out):
         x, weight, stats = ctx.saved_tensors
         need = ctx.needs_input_grad
@@ -262,7 +271,7 @@ class _RouteFunction(torch.autograd.Function):
         return weights.view_as(weights)
 
     @staticmethod
-    @torch.autograd.function.once_differentiable
+    @_once
     def backward(ctx, grad_weights):
         logits, experts = ctx.saved_tensors
         return binding.tt_route_backward(logits, experts, grad_weights.contiguous(), *ctx.how), None, None, None
@@ -286,7 +295,7 @@ class _RowsFunction(torch.autograd.Function):
         return binding.tt_expert_rows(x, slots, sources)
 
     @staticmethod
-    @torch.autograd.function.once_differentiable
+    @_once
     def backward(ctx, grad_out):
         (slots,) = ctx.saved_tensors
         return binding.tt_expert_combine(_row_major(grad_out), slots), None, None
@@ -309,7 +318,7 @@ class _CombineFunction(torch.autograd.Function):
         return binding.tt_expert_combine(y, slots, weights, residual)
 
     @staticmethod
-    @torch.autograd.function.once_differentiable
+    @_once
     def backward(ctx, grad_out):
         y, weights, slots, sources = ctx.saved_tensors
         need = ctx.needs_input_grad
@@ -376,7 +385,7 @@ class _LossFunction(torch.autograd.Function):
         return loss
 
     @staticmethod
-    @torch.autograd.function.once_differentiable
+    @_once
     def backward(ctx, grad_loss):
         x, w, bias, labels, lse = ctx.saved_tensors
         need = ctx.needs_input_grad

@@ -642,8 +642,11 @@ tt_status tt_expert_combine_backward(const tt_deal *op, const void *y, const int
  *     there are none)
  * Backward, from grad_loss (float[rows], or float[1]): with G = (softmax(z) - onehot(label)) times the row's share of it
  *   dx = G W,  dW = G^T x,  dbias = sums of G's columns;  any of dx, dw, dbias may be NULL.
- * G is formed again, a piece of the classes at a time, and rounded to the dtype before the products (fp16: scaled by a power of two
- * so that its largest gradient is near the top of the range, in and out of the products).  Losses and lse are float whatever the dtype.
+ * G is formed again, a piece of the classes at a time (of rows of up to 128 elements it is never stored), and in 16 bits rounded to the
+ * dtype before the products: without the share that all rows have of a sum or a mean, which is multiplied in at the end, and in fp16 by
+ * powers of two that keep it in the range.  fp32 products are of three bf16 parts, as in tt_dense; those of rows of up to 128 elements do
+ * without the fp32 instruction where parts cannot do (numbers below 2^-100 have fewer bits, numbers that bf16 cannot hold give NaN, and a
+ * row with a logit beyond 2^127 has NaN gradients).  Losses and lse are float whatever the dtype.
  *   labels DEVICE int64[rows];  lse DEVICE float[rows]: log of the sum, 0 in rows that do not count; written by the
  *   forward (not NULL), read by the backward
  *   workspace DEVICE, 256-byte aligned, tt_cross_entropy_workspace_bytes(op, backward) (0 on invalid arguments)

@@ -12,7 +12,7 @@ typedef TTLossRows Rows;
 // One workgroup: places in the order of the rows.  In the backward also each place's lse and share of the loss's gradient.
 constexpr int SCAN = 512;
 __global__ void __launch_bounds__(SCAN) k_loss_rows(const int64_t *labels, long long rows, int classes, long long ignored, int reduce, const float *lse,
-                                                    const float *grad, int bits, int half, int negative, float *loss, float *lse_out, Rows w) {
+                                                    const float *grad, int apart, int half, int negative, float *loss, float *lse_out, Rows w) {
   __shared__ int tmp[SCAN / 64 + 1];
   __shared__ float tops[SCAN / 64];
   int places = 0;
@@ -27,7 +27,8 @@ __global__ void __launch_bounds__(SCAN) k_loss_rows(const int64_t *labels, long 
     if (counts) {
       w.of[at] = (int32_t)r;
       w.label[at] = label >= 0 && label < classes ? (int32_t)label : -1;
-      if (lse) w.lse[at] = negative ? -lse[r] : lse[r];
+      // (short rows multiply it by log2 e: beyond 2^127 it counts as NaN)
+      if (lse) w.lse[at] = !negative ? lse[r] : fabsf(lse[r]) < 0x1p127f ? -lse[r] : NAN;
     }
     places += total;
   }
@@ -49,23 +50,23 @@ __global__ void __launch_bounds__(SCAN) k_loss_rows(const int64_t *labels, long 
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < SCAN / 64; ++i) top = fmaxf(top, tops[i]);
-  // fp32 takes G as it is.  In 16 bits a share that all rows have is left for the end (rounded into each term it would be the same error in
+  // fp32 products take G as it is.  Else (`apart`: 16 bits, and short rows) a share that all rows have is left for the end (rounded into each term it would be the same error in
   // all of them); shares of their own are part of G, in fp16 times the power of two that takes the largest to 2^13 .. 2^14, as far as that and its
   // inverse are normal numbers.  2^13 for the same reason: fp16 has a short range.
   const bool own = reduce == TT_REDUCE_NONE;
   float scale = 1.f, back = 1.f;
-  if (bits == 16 && own && half && top > 0.f) {
+  if (own && half && top > 0.f) {
     int e = (int)(__float_as_uint(top) >> 23);
     e = e < 14 ? 14 : e > 240 ? 240 : e;
     scale = __uint_as_float((unsigned)(127 + 13 + 127 - e) << 23);
     back = __uint_as_float((unsigned)(e - 13) << 23);
   }
-  if (bits == 16 && !own) back = all * 0x1p-13f;
+  if (apart && !own) back = all * 0x1p-13f;
   if (threadIdx.x == 0) w.back[0] = back;
   for (int i = threadIdx.x; i < places; i += SCAN) {
     const float share = own ? grad[w.of[i]] : all;
     w.share[i] = share;
-    w.weight[i] = bits == 16 && !own ? 8192.f : scale * share;
+    w.weight[i] = apart && !own ? 8192.f : scale * share;
   }
   if (negative && threadIdx.x < TT_LOSS_STEP && places + (int)threadIdx.x < (places + TT_LOSS_STEP - 1) / TT_LOSS_STEP * TT_LOSS_STEP) {
     w.lse[places + threadIdx.x] = -INFINITY;  // up to a whole step: rows that add nothing
@@ -106,8 +107,15 @@ __global__ void __launch_bounds__(TT_BLOCK) k_loss_fold(const float2 *__restrict
   if (seg != 0 || i >= places) return;
   for (int k = 1; k < 16; ++k) s = join_stats(s, part[16 * k + lane]);
   if (!first) s = join_stats(run[i], s);
-  if (last) ttk_loss_of(w, i, s, picked[i], loss, lse);
-  else run[i] = s;
+  if (!last) {
+    run[i] = s;
+    return;
+  }
+  const bool bad = w.label[i] < 0;
+  const int r = w.of[i];
+  lse[r] = bad ? NAN : s.x + logf(s.y);
+  // (the difference of the logits first: near a loss of zero lse less the label's logit would be lse's rounding)
+  loss[r] = bad ? NAN : (s.x - picked[i]) + logf(s.y);
 }
 // One workgroup: the sum or the mean, in 64 bits.
 __global__ void __launch_bounds__(SCAN) k_loss_sum(const float *each, long long rows, Rows w, int reduce, float *loss) {
@@ -180,7 +188,7 @@ long long piece_of(const tt_loss *op, bool backward) {
   const long long pieces = (op->classes + most - 1) / most;
   return ((op->classes + pieces - 1) / pieces + 255) / 256 * 256;
 }
-bool narrow(const tt_loss *op) { return ttk_narrow_serves(op->dtype, op->dim); }
+bool narrow(const tt_loss *op) { return ttk_narrow_serves(op->dim); }
 // 16-bit rows of a W whose length is no multiple of 8 elements are copied to ones that are, a piece at a time, so that the large tiles serve: the copy costs
 // four bytes an element at 4.5 TB/s, the tiles save the difference between 330 and 1100 TFLOP/s in every product; 1001 rows of 479 against
 // 50001 classes COPY us with it, 178 without.  Few rows do not pay for it.
@@ -253,11 +261,12 @@ Scratch scratch(const tt_loss *op, bool backward) {
   take(w.label, whole * 4);
   take(w.back, 4);
   take(w.offsets, 16);
-  take(w.x, rows * padded(op) * es);
+  const size_t each = narrow(op) && op->dtype == TT_F32 ? 6 : es;  // (three planes of 16 bits)
+  take(w.x, rows * padded(op) * each);
   if (copies(op)) take(w.copy, (size_t)(piece < op->classes ? piece : op->classes) * padded(op) * es);
   if (narrow(op)) {
     take(w.starts, ((size_t)op->classes + TT_LOSS_STEP) * 4);
-    take(w.copy, (size_t)op->classes * padded(op) * es);  // (whether it is used is known with w's address only)
+    take(w.copy, (size_t)op->classes * padded(op) * each);  // (whether it is used is known with w's address only)
   }
   if (!backward) {
     take(w.stats, narrow(op) ? ttk_narrow_stats_bytes(n) : (size_t)tt_ceil_div(piece, 64) * rows * 8);
@@ -291,10 +300,10 @@ Rows rows_of(char *ws, const Scratch &w) {
   return TTLossRows{(int32_t *)(ws + w.of), (int32_t *)(ws + w.at), (int32_t *)(ws + w.label), (float *)(ws + w.lse), (float *)(ws + w.share), (float *)(ws + w.weight),
               (float *)(ws + w.back), (int64_t *)(ws + w.offsets)};
 }
-TTNarrow narrow_of(const tt_loss *op, const void *w, const void *bias, char *ws, const Scratch &need) {
-  const bool as_it_is = op->dim == padded(op) && aligned(w, 16);
-  return TTNarrow{op->dtype, op->dim, padded(op), op->classes, op->rows, ws + need.x, w, bias, rows_of(ws, need), (float *)(ws + need.starts),
-                  as_it_is ? nullptr : ws + need.copy};
+TTNarrow narrow_of(const tt_loss *op, const void *x, const void *w, const void *bias, char *ws, const Scratch &need) {
+  const bool as_it_is = op->dtype != TT_F32 && op->dim == padded(op) && aligned(w, 16);
+  return TTNarrow{op->dtype, op->dim, padded(op), op->classes, op->rows, x, op->ld_x ? op->ld_x : op->dim, w, bias, rows_of(ws, need), ws + need.x,
+                  as_it_is ? nullptr : ws + need.copy, (float *)(ws + need.starts)};
 }
 unsigned grid_of(long long items) {
   const long long blocks = (items + TT_BLOCK - 1) / TT_BLOCK;
@@ -359,11 +368,11 @@ extern "C" tt_status tt_cross_entropy_forward(const tt_loss *op, const void *x, 
   hipLaunchKernelGGL(k_loss_rows, dim3(1), dim3(SCAN), 0, s, labels, rows, classes, ignored, reduce, (const float *)nullptr, (const float *)nullptr, 0, 0, 0, each, lse, r);
   if ((st = tt_launch_status()) != TT_OK) return st;
   if (some) {
-    if ((st = TT_BY_TYPE(gather, op->dtype, op, x, r, ws + need.x, s)) != TT_OK) return st;
+    if (!narrow(op) && (st = TT_BY_TYPE(gather, op->dtype, op, x, r, ws + need.x, s)) != TT_OK) return st;
     float2 *run = (float2 *)(ws + need.run);
     if (narrow(op)) {
-      const TTNarrow n = narrow_of(op, w, bias, ws, need);
-      if ((st = ttk_narrow_classes(n, s)) != TT_OK) return st;
+      const TTNarrow n = narrow_of(op, x, w, bias, ws, need);
+      if ((st = ttk_narrow_take(n, s)) != TT_OK) return st;
       if ((st = ttk_narrow_stats(n, (float *)(ws + need.stats), each, lse, s)) != TT_OK) return st;
     }
     for (long long c = 0; c < classes && !narrow(op); c += piece) {
@@ -417,14 +426,14 @@ extern "C" tt_status tt_cross_entropy_backward(const tt_loss *op, const void *x,
   char *ws = (char *)workspace;
   const Rows r = rows_of(ws, need);
   const long long rows = op->rows, ignored = op->ignore_index, piece = piece_of(op, true);
-  const int classes = op->classes, reduce = op->reduce, bits = op->dtype == TT_F32 ? 32 : 16, half = op->dtype == TT_F16, negative = narrow(op);
-  hipLaunchKernelGGL(k_loss_rows, dim3(1), dim3(SCAN), 0, s, labels, rows, classes, ignored, reduce, lse, grad_loss, bits, half, negative, (float *)nullptr, (float *)nullptr, r);
+  const int classes = op->classes, reduce = op->reduce, apart = op->dtype != TT_F32 || narrow(op), half = op->dtype == TT_F16, negative = narrow(op);
+  hipLaunchKernelGGL(k_loss_rows, dim3(1), dim3(SCAN), 0, s, labels, rows, classes, ignored, reduce, lse, grad_loss, apart, half, negative, (float *)nullptr, (float *)nullptr, r);
   if ((st = tt_launch_status()) != TT_OK) return st;
-  if ((st = TT_BY_TYPE(gather, op->dtype, op, x, r, ws + need.x, s)) != TT_OK) return st;
+  if (!narrow(op) && (st = TT_BY_TYPE(gather, op->dtype, op, x, r, ws + need.x, s)) != TT_OK) return st;
   if (narrow(op)) {
-    const TTNarrow n = narrow_of(op, w, bias, ws, need);
+    const TTNarrow n = narrow_of(op, x, w, bias, ws, need);
     float *parts = (float *)(ws + need.parts);
-    if ((st = ttk_narrow_classes(n, s)) != TT_OK) return st;
+    if ((st = ttk_narrow_take(n, s)) != TT_OK) return st;
     if (dx && (st = ttk_narrow_dx(n, parts, dx, op->ld_dx ? op->ld_dx : op->dim, s)) != TT_OK) return st;
     return dw || dbias ? ttk_narrow_dw(n, reduce == TT_REDUCE_NONE, parts, dw, dbias, s) : TT_OK;
   }

@@ -1,4 +1,4 @@
-// Softmax cross entropy of short rows (up to 128 elements of 16 bits): nothing of the size rows x classes is ever stored.
+// Softmax cross entropy of short rows (up to 128 elements): nothing of the size rows x classes is ever stored.
 #include "tt_gemm_device.h"
 #include "tt_loss.h"
 
@@ -16,12 +16,15 @@ using namespace ttg;
 // rounding alone; it is never in memory.
 // What is added to a logit comes for nothing: of the streamed vector (the class's bias, or a row's -lse) as the product's starting value, of the held
 // one in the multiply-add before exp2.
-// 512 registers of a SIMD's lane are two wavefronts of 256: 64 of the held operand, 128 of the sums, 32 of S.
+// fp32 operands come in PARTS = 3 planes of bf16 (tt_split_bf16), P is split as it is formed, and six of the nine products count, as in the other fp32
+// products; what they redo with the fp32 instruction (numbers below 2^-100 in size, or near the range's end) has fewer bits here, or is NaN.
+// 512 registers of a SIMD's lane are two wavefronts of 256: 48 of the held operand (three tiles of 16), 96 of the sums, 24 of S.
 constexpr int WAVES = 4, THREADS = 64 * WAVES, STEP = TT_LOSS_STEP;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr float RAISE = 13.f;  // P is formed 2^13 times its size: fp16's smallest numbers then are of 2^-37, and P stays below 2^14
 enum Mode { STATS, ROWS, CLASSES };
-constexpr int held_tiles(int KP, Mode mode) { return mode != STATS && KP == 128 ? 3 : 4; }  // of 16 vectors, of a wavefront
+// of 16 vectors, of a wavefront: what fits the registers
+constexpr int held_tiles(int KP, Mode mode, int parts) { return parts == 1 ? (mode != STATS && KP == 128 ? 3 : 4) : KP == 128 ? (mode == STATS ? 3 : 2) : (mode == STATS ? 4 : 3); }
 
 // How a launch is cut, from the number of held vectors (which the host does not know where they are rows that count) and of workgroups that run at once:
 // workgroup w has block w % blocks of the held vectors and run w / blocks of the streamed ones.  As many runs as fill the card once, or
@@ -42,8 +45,8 @@ __host__ __device__ inline long long grid_for(long long held, long long streamed
   const long long twice = 2LL * slots < most ? 2LL * slots : most;
   return blocks > twice ? blocks : twice;
 }
-constexpr int tile_of(int KP, Mode mode) { return 16 * held_tiles(KP, mode) * WAVES; }
-constexpr int slots_of(Mode mode) { return 256 * (mode == STATS ? 4 : 2); }
+constexpr int tile_of(int KP, Mode mode, int parts) { return 16 * held_tiles(KP, mode, parts) * WAVES; }
+constexpr int slots_of(Mode mode, int parts) { return 256 * (mode == STATS && parts == 1 ? 4 : 2); }
 
 struct Args {
   const void *held, *streamed;
@@ -55,6 +58,7 @@ struct Args {
   void *out, *sums;          // CLASSES of one run: dW, dbias
   const float *back;
   float *parts;              // [workgroup][tile]...
+  long long held_plane, streamed_plane;  // elements between the planes of fp32 operands
   int dim, classes;
 };
 
@@ -85,22 +89,26 @@ template <int KP> __device__ __forceinline__ u16x8 frag_across(const unsigned sh
 }
 
 // A step's LDS: the tile, then of its vectors what they start at and the shares.
-template <int KP> constexpr int step_bytes() { return STEP * KP * 2 + 2 * STEP * 4; }
+template <int KP, int PARTS> constexpr int step_bytes() { return STEP * KP * 2 * PARTS + 2 * STEP * 4; }
 
 // What a thread fetches of a step.  The tile's 16-byte pieces go from memory into LDS, lane after lane; which piece a lane fetches makes their order
 // there.  A vector behind the last one is the last one again: it starts at -infinity, and its P is zero.
-template <class T, int KP, Mode MODE, bool SHARES> struct Fetcher {
-  const T *streamed;
+template <int KP, Mode MODE, bool SHARES, int PARTS> struct Fetcher {
+  const unsigned short *streamed;
+  long long plane;
   const float *starts, *weight;
   long long count;
   int row, wave, lane;
   unsigned offset;
   __device__ __forceinline__ void fetch(long long t, char *to) const {
-    constexpr int PIECES = STEP * KP / 8 / THREADS, TILE = STEP * KP * 2;
+    constexpr int PIECES = STEP * KP / 8 / THREADS, PLANE = STEP * KP * 2, TILE = PARTS * PLANE;
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
       const long long r = t + row + i * (THREADS / (KP / 8));
-      __builtin_amdgcn_global_load_lds((GlobalPtr)(streamed + (r < count ? r : count - 1) * KP + offset), (LdsPtr)(to + (i * THREADS + wave * 64) * 16), 16, 0, 0);
+      const unsigned short *from = streamed + (r < count ? r : count - 1) * KP + offset;
+#pragma unroll
+      for (int p = 0; p < PARTS; ++p)
+        __builtin_amdgcn_global_load_lds((GlobalPtr)(from + p * plane), (LdsPtr)(to + p * PLANE + (i * THREADS + wave * 64) * 16), 16, 0, 0);
     }
     if (lane < STEP) {  // a wavefront each
       if (wave == 0) __builtin_amdgcn_global_load_lds((GlobalPtr)(starts + t + lane), (LdsPtr)(to + TILE), 4, 0, 0);
@@ -115,24 +123,31 @@ template <class T, int KP, Mode MODE, bool SHARES> struct Fetcher {
 // hit: a label of the rows is among the classes here, which few steps have; one branch, since what is on its two sides is not
 // interleaved.  `label`: ROWS of the held rows, less the step's first class; CLASSES lane l's is row l's, less the first held class.
 // The one is taken off P before that is rounded: where a row is nearly sure of its label their difference is all that is left.
-template <class T, int KP, Mode MODE, bool SHARES, int H, int DO>
-__device__ __forceinline__ void step_of(const char *__restrict__ now, char *__restrict__ next, const Fetcher<T, KP, MODE, SHARES> &fetcher, long long ahead,
-                                        long long end, bool hit, const int (&label)[MODE == ROWS ? H : 1], const u16x8 (&held)[H][KP / 32], float (&constant)[H], f32x4 (&acc)[DO][H], float (&sums)[H]) {
+template <class T, int KP, Mode MODE, bool SHARES, int PARTS, int H, int DO>
+__device__ __forceinline__ void step_of(const char *__restrict__ now, char *__restrict__ next, const Fetcher<KP, MODE, SHARES, PARTS> &fetcher, long long ahead,
+                                        long long end, bool hit, const int (&label)[MODE == ROWS ? H : 1], const u16x8 (&held)[H][KP / 32][PARTS], float (&constant)[H], f32x4 (&acc)[DO][H], float (&sums)[H]) {
   constexpr int KS = KP / 32, D = KP / 16;
   constexpr bool OUT = MODE != STATS, CLASS = MODE == CLASSES;
   const int lane = threadIdx.x & 63, q = lane >> 4, j = lane & 15;
   if (ahead < end) fetcher.fetch(ahead, next);
   const unsigned short *tile = reinterpret_cast<const unsigned short *>(now);
-  const float *starts = reinterpret_cast<const float *>(now + STEP * KP * 2), *shares = starts + STEP;
+  const float *starts = reinterpret_cast<const float *>(now + STEP * KP * 2 * PARTS), *shares = starts + STEP;
   f32x4 S[2][H];
 #pragma unroll
   for (int half = 0; half < 2; ++half) {  // 16 streamed vectors
     const f32x4 from = *reinterpret_cast<const f32x4 *>(starts + 16 * half + 4 * q);
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
-      const u16x8 f = frag<KP>(tile, 16 * half, s);
+      u16x8 f[PARTS];
 #pragma unroll
-      for (int x = 0; x < H; ++x) S[half][x] = mma(T(), f, held[x][s], s ? S[half][x] : from);
+      for (int p = 0; p < PARTS; ++p) f[p] = frag<KP>(tile + p * STEP * KP, 16 * half, s);
+      // the smallest terms first
+#pragma unroll
+      for (int d = PARTS - 1; d >= 0; --d)
+#pragma unroll
+        for (int p = 0; p <= d; ++p)
+#pragma unroll
+          for (int x = 0; x < H; ++x) S[half][x] = mma(T(), f[d - p], held[x][s][p], s || d != PARTS - 1 || p ? S[half][x] : from);
     }
     if constexpr (MODE == STATS) {
 #pragma unroll
@@ -142,11 +157,16 @@ __device__ __forceinline__ void step_of(const char *__restrict__ now, char *__re
         const bool above = fmaf(top, LOG2E, constant[x]) > 16.f;
         if (__ballot(above)) {
           const float now = above ? -top * LOG2E : constant[x];
-          sums[x] *= above ? __builtin_amdgcn_exp2f(now - constant[x]) : 1.f;
+          const float by = above ? __builtin_amdgcn_exp2f(now - constant[x]) : 1.f;
+          sums[x] *= by;
+          acc[0][x][0] *= by;
+          acc[0][x][1] = above ? top : acc[0][x][1];
           constant[x] = now;
         }
+        float e[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) sums[x] += __builtin_amdgcn_exp2f(fmaf(S[half][x][i], LOG2E, constant[x]));
+        for (int i = 0; i < 4; ++i) e[i] = __builtin_amdgcn_exp2f(fmaf(S[half][x][i], LOG2E, constant[x]));
+        sums[x] += (e[0] + e[1]) + (e[2] + e[3]);
       }
     } else {
 #pragma unroll
@@ -168,7 +188,7 @@ __device__ __forceinline__ void step_of(const char *__restrict__ now, char *__re
             S[half][x][i] -= here ? (SHARES ? 1.f : 8192.f) : 0.f;
           }
     }
-    u16x8 P[H];
+    u16x8 P[H][PARTS];
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
       f32x4 share = {1.f, 1.f, 1.f, 1.f};
@@ -178,49 +198,83 @@ __device__ __forceinline__ void step_of(const char *__restrict__ now, char *__re
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           if constexpr (SHARES) S[half][x][i] *= share[i];
-          if constexpr (CLASS) sums[x] += S[half][x][i];
-          P[x][4 * half + i] = __builtin_bit_cast(unsigned short, from_f32<T>(S[half][x][i]));
+          if constexpr (PARTS == 1) P[x][0][4 * half + i] = __builtin_bit_cast(unsigned short, from_f32<T>(S[half][x][i]));
+          else if (i & 1) {
+            unsigned part[3];
+            tt_split_bf16(S[half][x][i - 1], S[half][x][i], part[0], part[1], part[2]);
+#pragma unroll
+            for (int p = 0; p < PARTS; ++p) {
+              P[x][p][4 * half + i - 1] = (unsigned short)part[p];
+              P[x][p][4 * half + i] = (unsigned short)(part[p] >> 16);
+            }
+          }
         }
+      if constexpr (CLASS) {
+#pragma unroll
+        for (int x = 0; x < H; ++x) sums[x] += (S[half][x][0] + S[half][x][1]) + (S[half][x][2] + S[half][x][3]);
+      }
     }
 #pragma unroll
     for (int y = 0; y < D; ++y) {
-      const u16x8 f = frag_across<KP>(tile, 16 * y);
+      u16x8 f[PARTS];
 #pragma unroll
-      for (int x = 0; x < H; ++x) acc[y][x] = mma(T(), f, P[x], acc[y][x]);
+      for (int p = 0; p < PARTS; ++p) f[p] = frag_across<KP>(tile + p * STEP * KP, 16 * y);
+#pragma unroll
+      for (int d = PARTS - 1; d >= 0; --d)
+#pragma unroll
+        for (int p = 0; p <= d; ++p)
+#pragma unroll
+          for (int x = 0; x < H; ++x) acc[y][x] = mma(T(), f[d - p], P[x][p], acc[y][x]);
     }
   }
 }
 
-template <class T, int KP, Mode MODE, bool SHARES> __global__ void __launch_bounds__(THREADS, 2) k_narrow(Args a) {
-  constexpr int KS = KP / 32, H = held_tiles(KP, MODE), HELD = 16 * H, D = KP / 16;
+// Statistics of two sets of a row's logits: m, about the largest in units of log 2, and s, the sum of 2^(logit - m).  Where a logit is so large that
+// its m is infinite, that logit alone counts and is what s holds.
+__device__ __forceinline__ float2 join_runs(float2 a, float2 b) {
+  if (a.x == INFINITY || b.x == INFINITY) {
+    const float y = a.x != INFINITY ? -INFINITY : a.y, z = b.x != INFINITY ? -INFINITY : b.y;
+    const bool bad = a.y != a.y || b.y != b.y;
+    return float2{INFINITY, bad ? NAN : fmaxf(y, z)};
+  }
+  const float top = fmaxf(a.x, b.x), base = top == -INFINITY ? 0.f : top;
+  return float2{top, a.y * __builtin_amdgcn_exp2f(a.x - base) + b.y * __builtin_amdgcn_exp2f(b.x - base)};
+}
+
+// T: of the products; O: of dW and dbias
+template <class T, class O, int KP, Mode MODE, bool SHARES> __global__ void __launch_bounds__(THREADS, 2) k_narrow(Args a) {
+  constexpr int PARTS = sizeof(O) == 4 ? 3 : 1, KS = KP / 32, H = held_tiles(KP, MODE, PARTS), HELD = 16 * H, D = KP / 16;
   constexpr bool OUT = MODE != STATS, CLASS = MODE == CLASSES;
-  constexpr int BYTES = step_bytes<KP>(), GIVE = CLASS ? WAVES * 16 * (KP + 8) * 2 : 0;  // two steps, or what is given out through it
+  constexpr int BYTES = step_bytes<KP, PARTS>(), GIVE = CLASS ? WAVES * 16 * (KP + 8) * 2 : 0;  // two steps, or what is given out through it
   __shared__ __align__(16) char lds[GIVE > 2 * BYTES ? GIVE : 2 * BYTES];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), q = lane >> 4, j = lane & 15;
   const long long places = a.offsets[1];
   const long long held_count = CLASS ? a.classes : places, streamed_count = CLASS ? places : a.classes;
-  const Cut cut = cut_of(held_count, streamed_count, tile_of(KP, MODE), slots_of(MODE));
+  const Cut cut = cut_of(held_count, streamed_count, tile_of(KP, MODE, PARTS), slots_of(MODE, PARTS));
   const int block = (int)(blockIdx.x % (unsigned)cut.blocks), run = (int)(blockIdx.x / (unsigned)cut.blocks);
   if (run >= cut.runs || held_count == 0) return;
-  const long long h0 = (long long)block * tile_of(KP, MODE) + wave * HELD;
+  const long long h0 = (long long)block * tile_of(KP, MODE, PARTS) + wave * HELD;
   // this run's share of the streamed vectors, whole steps
   const long long steps = (streamed_count + STEP - 1) / STEP, per = (steps + cut.runs - 1) / cut.runs;
   const long long s0 = run * per * STEP, s1 = s0 + per * STEP < streamed_count ? s0 + per * STEP : streamed_count;
 
-  u16x8 held[H][KS];
+  u16x8 held[H][KS][PARTS];
   float constant[H];  // of the held vector, in units of log 2
 #pragma unroll
   for (int x = 0; x < H; ++x) {
     const long long h = h0 + 16 * x + j < held_count ? h0 + 16 * x + j : held_count - 1;  // (of vectors outside nothing is written)
 #pragma unroll
-    for (int s = 0; s < KS; ++s) held[x][s] = *reinterpret_cast<const u16x8 *>((const T *)a.held + h * KP + 32 * s + 8 * q);
+    for (int s = 0; s < KS; ++s)
+#pragma unroll
+      for (int p = 0; p < PARTS; ++p)
+        held[x][s][p] = *reinterpret_cast<const u16x8 *>((const unsigned short *)a.held + p * a.held_plane + h * KP + 32 * s + 8 * q);
     constant[x] = MODE == STATS ? 3e38f /* less the largest so far: below all */ : fmaf(a.constants[h], LOG2E, SHARES ? 0.f : RAISE);
   }
-  f32x4 acc[OUT ? D : 1][H] = {};  // [columns][held]
+  f32x4 acc[OUT ? D : 1][H] = {};  // [columns][held]; STATS: [0] what sums were 16 steps ago and before (a chain of additions stays short), [1] the logit that constant is of
   float sums[H] = {};
 
   const int row = (int)threadIdx.x / (KP / 8);
-  const Fetcher<T, KP, MODE, SHARES> fetcher = {(const T *)a.streamed, a.starts, a.weight, streamed_count, row, wave, lane,
+  const Fetcher<KP, MODE, SHARES, PARTS> fetcher = {(const unsigned short *)a.streamed, a.streamed_plane, a.starts, a.weight, streamed_count, row, wave, lane,
                                                 ((threadIdx.x % (KP / 8)) ^ spread<KP>(row & 15)) * 8};
   // Labels are a step ahead of their use, in a register: of the held rows less the first class, or of the streamed rows less the first held class.
   int label[MODE == ROWS ? H : 1] = {}, label_next = 0;
@@ -246,10 +300,17 @@ template <class T, int KP, Mode MODE, bool SHARES> __global__ void __launch_boun
       hit = (unsigned)label[0] < (unsigned)HELD;
       if (t + STEP < s1) label_next = a.label[t + STEP + (lane & 31)];
     }
-    step_of<T, KP, MODE, SHARES>(lds + b * BYTES, lds + (b ^ 1) * BYTES, fetcher, t + STEP, s1, OUT && __ballot(hit) != 0, label, held, constant, acc, sums);
+    step_of<T, KP, MODE, SHARES, PARTS>(lds + b * BYTES, lds + (b ^ 1) * BYTES, fetcher, t + STEP, s1, OUT && __ballot(hit) != 0, label, held, constant, acc, sums);
     if constexpr (MODE == ROWS) {
 #pragma unroll
       for (int x = 0; x < H; ++x) label[x] -= STEP;
+    }
+    if (MODE == STATS && ((t - s0) / STEP & 15) == 15) {
+#pragma unroll
+      for (int x = 0; x < H; ++x) {
+        acc[0][x][0] += sums[x];
+        sums[x] = 0.f;
+      }
     }
     wait_loads();
   }
@@ -258,15 +319,17 @@ template <class T, int KP, Mode MODE, bool SHARES> __global__ void __launch_boun
   if constexpr (MODE == STATS) {
 #pragma unroll
     for (int x = 0; x < H; ++x) {  // four lanes have a row's columns
-      float2 mine = {-constant[x] * LN2, sums[x]};
-      if (constant[x] == 3e38f) mine = {-INFINITY, sums[x]};  // nothing but -infinity (or NaN, which the sum has)
+      sums[x] += acc[0][x][0];
+      float2 mine = {-constant[x], sums[x]};
+      if (constant[x] == 3e38f) mine.x = -INFINITY;  // nothing but -infinity (or NaN, which the sum has)
+      if (constant[x] == -INFINITY) mine.y = sums[x] == sums[x] ? acc[0][x][1] : sums[x];
 #pragma unroll
-      for (int o = 16; o < 64; o *= 2) mine = join_stats(mine, float2{__shfl(mine.x, lane ^ o, 64), __shfl(mine.y, lane ^ o, 64)});
-      if (q == 0) reinterpret_cast<float2 *>(a.parts)[(long long)blockIdx.x * tile_of(KP, MODE) + first + 16 * x + j] = mine;
+      for (int o = 16; o < 64; o *= 2) mine = join_runs(mine, float2{__shfl(mine.x, lane ^ o, 64), __shfl(mine.y, lane ^ o, 64)});
+      if (q == 0) reinterpret_cast<float2 *>(a.parts)[(long long)blockIdx.x * tile_of(KP, MODE, PARTS) + first + 16 * x + j] = mine;
     }
   } else if (MODE == ROWS || cut.runs > 1) {
     constexpr int LD = CLASS ? KP + 4 : KP;
-    float *to = a.parts + ((long long)blockIdx.x * tile_of(KP, MODE) + first) * LD;
+    float *to = a.parts + ((long long)blockIdx.x * tile_of(KP, MODE, PARTS) + first) * LD;
 #pragma unroll
     for (int x = 0; x < H; ++x) {
 #pragma unroll
@@ -288,8 +351,17 @@ template <class T, int KP, Mode MODE, bool SHARES> __global__ void __launch_boun
       sums[x] += __shfl(sums[x], lane ^ 16, 64);
       sums[x] += __shfl(sums[x], lane ^ 32, 64);
       const long long h = h0 + 16 * x;
-      if (a.sums && q == 0 && h + j < held_count) ((T *)a.sums)[h + j] = from_f32<T>(sums[x] * back);
+      if (a.sums && q == 0 && h + j < held_count) ((O *)a.sums)[h + j] = from_f32<O>(sums[x] * back);
       if (!a.out) continue;
+      if constexpr (PARTS == 3) {  // 64 bytes of a row at a time as they are
+#pragma unroll
+        for (int y = 0; y < D; ++y) {
+          const int c = 16 * y + 4 * q;
+          const float v[4] = {acc[y][x][0] * back, acc[y][x][1] * back, acc[y][x][2] * back, acc[y][x][3] * back};
+          if (h + j < held_count && c < a.dim) store4((float *)a.out + (h + j) * a.dim + c, a.dim - c, v);
+        }
+        continue;
+      }
 #pragma unroll
       for (int y = 0; y < D; ++y) {
         u16x4 v;
@@ -329,19 +401,25 @@ template <class T> __global__ void __launch_bounds__(TT_BLOCK) k_narrow_fold(TTN
   const long long block = i / tile;
   const int label = n.r.label[i];
   float2 s = {-INFINITY, 0.f};
-  for (int k = lane; k < cut.runs; k += 64) s = join_stats(s, parts[(k * (long long)cut.blocks + block) * tile + i % tile]);
+  for (int k = lane; k < cut.runs; k += 64) s = join_runs(s, parts[(k * (long long)cut.blocks + block) * tile + i % tile]);
   float z = 0.f;
   if (label >= 0) {
 #pragma unroll
     for (int c = lane; c < 128; c += 64)
-      if (c < n.dim) z = fmaf(to_f32(((const T *)n.x)[i * n.padded + c]), to_f32(((const T *)n.w)[(long long)label * n.dim + c]), z);
+      if (c < n.dim) z = fmaf(to_f32(((const T *)n.of_call)[n.r.of[i] * n.ld + c]), to_f32(((const T *)n.w)[(long long)label * n.dim + c]), z);
   }
 #pragma unroll
   for (int o = 1; o < 64; o *= 2) {
-    s = join_stats(s, float2{__shfl(s.x, lane ^ o, 64), __shfl(s.y, lane ^ o, 64)});
+    s = join_runs(s, float2{__shfl(s.x, lane ^ o, 64), __shfl(s.y, lane ^ o, 64)});
     z += __shfl(z, lane ^ o, 64);
   }
-  if (lane == 0) ttk_loss_of(n.r, i, s, z + (label >= 0 ? n.starts[label] : 0.f), loss, lse);
+  if (lane != 0) return;
+  z += label >= 0 ? n.starts[label] : 0.f;
+  const int r = n.r.of[i];
+  const float more = log2f(s.y);
+  // (the label's logit is taken off before the sum's logarithm is added: near a loss of zero lse less that logit would be lse's rounding)
+  lse[r] = label < 0 ? NAN : s.x == INFINITY ? s.y : (s.x + more) * LN2;
+  loss[r] = label < 0 ? NAN : s.x == INFINITY ? s.y - z : (fmaf(-z, LOG2E, s.x) + more) * LN2;
 }
 
 // A workgroup's sum of the runs' parts of one vector, `width` columns (of four a thread) in eight runs that are added in order: in the threads of the first.
@@ -370,13 +448,14 @@ template <int KP> __device__ __forceinline__ f32x4 sum_runs(const float *__restr
 template <class T, int KP> __global__ void __launch_bounds__(TT_BLOCK) k_narrow_dx(TTNarrow n, const float *__restrict__ parts, T *dx, long long ld) {
   __shared__ __align__(16) float room[TT_BLOCK * 4];
   const long long places = n.r.offsets[1];
-  const Cut cut = cut_of(places, n.classes, tile_of(KP, ROWS), slots_of(ROWS));
+  constexpr int PARTS = sizeof(T) == 4 ? 3 : 1;
+  const Cut cut = cut_of(places, n.classes, tile_of(KP, ROWS, PARTS), slots_of(ROWS, PARTS));
   const int c = 4 * (int)threadIdx.x;
   for (long long r = blockIdx.x; r < n.rows; r += gridDim.x) {
     const int at = n.r.at[r];
     f32x4 s = {0.f, 0.f, 0.f, 0.f};
     if (at >= 0) {
-      s = sum_runs<KP>(parts, KP, cut, tile_of(KP, ROWS), at, room);
+      s = sum_runs<KP>(parts, KP, cut, tile_of(KP, ROWS, PARTS), at, room);
       s *= 0x1p-13f * n.r.share[at];
     }
     const float v[4] = {s[0], s[1], s[2], s[3]};
@@ -386,32 +465,49 @@ template <class T, int KP> __global__ void __launch_bounds__(TT_BLOCK) k_narrow_
 // dW and dbias where the rows came in several runs; a workgroup a class
 template <class T, int KP> __global__ void __launch_bounds__(TT_BLOCK) k_narrow_dw(TTNarrow n, const float *__restrict__ parts, T *dw, T *db) {
   __shared__ __align__(16) float room[TT_BLOCK * 4];
-  const Cut cut = cut_of(n.classes, n.r.offsets[1], tile_of(KP, CLASSES), slots_of(CLASSES));
+  constexpr int PARTS = sizeof(T) == 4 ? 3 : 1;
+  const Cut cut = cut_of(n.classes, n.r.offsets[1], tile_of(KP, CLASSES, PARTS), slots_of(CLASSES, PARTS));
   if (cut.runs == 1) return;  // the products' kernel has written them
   const float back = *n.r.back;
   const int c = 4 * (int)threadIdx.x;
   for (long long h = blockIdx.x; h < n.classes; h += gridDim.x) {
-    const f32x4 s = sum_runs<KP>(parts, KP + 4, cut, tile_of(KP, CLASSES), h, room) * back;
+    const f32x4 s = sum_runs<KP>(parts, KP + 4, cut, tile_of(KP, CLASSES, PARTS), h, room) * back;
     const float v[4] = {s[0], s[1], s[2], s[3]};
     if (dw && c < n.dim && c < KP) store4(dw + h * n.dim + c, n.dim - c, v);
     if (db && c == KP) db[h] = from_f32<T>(v[0]);
   }
 }
 
-// What the kernels above take of the classes: their biases as numbers of 32 bits (-infinity behind the last one, whole steps), and where W's rows are not `padded`
-// aligned elements as they are, a copy of which they are.
-template <class T> __global__ void __launch_bounds__(TT_BLOCK) k_narrow_classes(TTNarrow n, float *starts, T *copy) {
-  const long long whole = ((long long)n.classes + STEP - 1) / STEP * STEP, stride = (long long)gridDim.x * TT_BLOCK;
-  for (long long i = (long long)blockIdx.x * TT_BLOCK + threadIdx.x; i < whole; i += stride)
-    starts[i] = i >= n.classes ? -INFINITY : n.bias ? to_f32(((const T *)n.bias)[i]) : 0.f;
-  if (!copy) return;
-  const int per = n.padded / 8;
-  for (long long e = (long long)blockIdx.x * TT_BLOCK + threadIdx.x; e < (long long)n.classes * per; e += stride) {
+// What the kernels above take: vectors `padded` apart with zeros behind their ends (fp32: three planes of their parts), those at `of` of them if that
+// is given, zeros behind the `there` that there are; and the classes' biases as numbers of 32 bits (-infinity behind the last one, whole steps).
+template <class T> __global__ void __launch_bounds__(TT_BLOCK) k_narrow_take(const T *from, long long ld, const int32_t *of, const int64_t *there, long long count, int dim,
+                                                                             unsigned short *to, int padded, const T *bias, float *starts) {
+  const long long stride = (long long)gridDim.x * TT_BLOCK, some = there ? there[1] : count, whole = (count + STEP - 1) / STEP * STEP, plane = count * padded;
+  if (starts)
+    for (long long i = (long long)blockIdx.x * TT_BLOCK + threadIdx.x; i < whole; i += stride) starts[i] = i >= count ? -INFINITY : bias ? to_f32(bias[i]) : 0.f;
+  if (!to) return;
+  const int per = padded / 8;
+  for (long long e = (long long)blockIdx.x * TT_BLOCK + threadIdx.x; e < count * per; e += stride) {
     const long long r = e / per;
     const int c = (int)(e - r * per) * 8;
     float v[8] = {};
-    load_n<T, 8>((const T *)n.w + r * n.dim + c, n.dim - c, v);
-    store_n<T, 8>(copy + r * n.padded + c, 8, v);
+    if (r < some) load_n<T, 8>(from + (of ? of[r] : r) * ld + c, dim - c, v);
+    if constexpr (sizeof(T) == 2) {
+      store_n<T, 8>((T *)to + r * padded + c, 8, v);
+    } else {
+      typedef unsigned u4 __attribute__((ext_vector_type(4)));
+      u4 part[3];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        unsigned h, m, l;
+        tt_split_bf16(v[2 * i], v[2 * i + 1], h, m, l);
+        part[0][i] = h;
+        part[1][i] = m;
+        part[2][i] = l;
+      }
+#pragma unroll
+      for (int p = 0; p < 3; ++p) *reinterpret_cast<u4 *>(to + p * plane + r * padded + c) = part[p];
+    }
   }
 }
 
@@ -427,29 +523,38 @@ Args args_of(const TTNarrow &n, bool classes) {
   a.label = n.r.label;
   a.offsets = n.r.offsets;
   a.back = n.r.back;
+  a.held_plane = (classes ? (long long)n.classes : n.rows) * n.padded;
+  a.streamed_plane = (classes ? n.rows : (long long)n.classes) * n.padded;
   a.dim = n.dim;
   a.classes = n.classes;
   return a;
 }
+int parts_of(const TTNarrow &n) { return n.dtype == TT_F32 ? 3 : 1; }
+template <Mode MODE> int tile_for(const TTNarrow &n) { return n.padded == 64 ? tile_of(64, MODE, parts_of(n)) : tile_of(128, MODE, parts_of(n)); }
 template <Mode MODE> long long workgroups(const TTNarrow &n) {
   const long long held = MODE == CLASSES ? n.classes : n.rows, streamed = MODE == CLASSES ? n.rows : n.classes;
-  return grid_for(held, streamed, n.padded == 64 ? tile_of(64, MODE) : tile_of(128, MODE), slots_of(MODE));
+  return grid_for(held, streamed, tile_for<MODE>(n), slots_of(MODE, parts_of(n)));
 }
-template <class T, int KP, Mode MODE> tt_status launch_as(const TTNarrow &n, bool shares, const Args &a, hipStream_t s) {
+template <class T, class O, int KP, Mode MODE> tt_status launch_as(const TTNarrow &n, bool shares, const Args &a, hipStream_t s) {
   const dim3 grid((unsigned)workgroups<MODE>(n)), block(THREADS);
   if constexpr (MODE == CLASSES) {
-    if (shares) hipLaunchKernelGGL((k_narrow<T, KP, MODE, true>), grid, block, 0, s, a);
-    else hipLaunchKernelGGL((k_narrow<T, KP, MODE, false>), grid, block, 0, s, a);
+    if (shares) hipLaunchKernelGGL((k_narrow<T, O, KP, MODE, true>), grid, block, 0, s, a);
+    else hipLaunchKernelGGL((k_narrow<T, O, KP, MODE, false>), grid, block, 0, s, a);
   } else {
-    hipLaunchKernelGGL((k_narrow<T, KP, MODE, false>), grid, block, 0, s, a);
+    hipLaunchKernelGGL((k_narrow<T, O, KP, MODE, false>), grid, block, 0, s, a);
   }
   return tt_launch_status();
 }
+template <class T, class O, Mode MODE> tt_status launch_padded(const TTNarrow &n, bool shares, const Args &a, hipStream_t s) {
+  return n.padded == 64 ? launch_as<T, O, 64, MODE>(n, shares, a, s) : launch_as<T, O, 128, MODE>(n, shares, a, s);
+}
 template <Mode MODE> tt_status launch(const TTNarrow &n, bool shares, const Args &a, hipStream_t s) {
   if (workgroups<MODE>(n) > TT_MAX_WORKGROUPS) return TT_ERR_SHAPE;
-  if (n.dtype == TT_BF16) return n.padded == 64 ? launch_as<ttg::bf16, 64, MODE>(n, shares, a, s) : launch_as<ttg::bf16, 128, MODE>(n, shares, a, s);
-  return n.padded == 64 ? launch_as<ttg::f16, 64, MODE>(n, shares, a, s) : launch_as<ttg::f16, 128, MODE>(n, shares, a, s);
+  if (n.dtype == TT_F32) return launch_padded<ttg::bf16, float, MODE>(n, shares, a, s);
+  return n.dtype == TT_BF16 ? launch_padded<ttg::bf16, ttg::bf16, MODE>(n, shares, a, s) : launch_padded<ttg::f16, ttg::f16, MODE>(n, shares, a, s);
 }
+#define TT_BY_TYPE(call, dtype, ...) \
+  ((dtype) == TT_F32 ? call<float>(__VA_ARGS__) : (dtype) == TT_BF16 ? call<ttg::bf16>(__VA_ARGS__) : call<ttg::f16>(__VA_ARGS__))
 unsigned grid_of(long long items) {
   const long long blocks = (items + TT_BLOCK - 1) / TT_BLOCK;
   return (unsigned)(blocks < 1 ? 1 : blocks > 16384 ? 16384 : blocks);
@@ -467,48 +572,55 @@ template <class T> tt_status finish_dw(const TTNarrow &n, const float *parts, vo
   else hipLaunchKernelGGL((k_narrow_dw<T, 128>), grid, block, 0, s, n, parts, (T *)dw, (T *)db);
   return tt_launch_status();
 }
+template <class T> tt_status take(const TTNarrow &n, bool classes, hipStream_t s) {
+  const long long count = classes ? n.classes : n.rows, ld = classes ? n.dim : n.ld;
+  const T *from = (const T *)(classes ? n.w : n.of_call), *bias = classes ? (const T *)n.bias : nullptr;
+  const int32_t *of = classes ? nullptr : n.r.of;
+  const int64_t *there = classes ? nullptr : n.r.offsets;
+  unsigned short *to = (unsigned short *)(classes ? n.copy : n.x);
+  float *starts = classes ? n.starts : nullptr;
+  const int dim = n.dim, padded = n.padded;
+  hipLaunchKernelGGL(k_narrow_take<T>, dim3(grid_of(count * (to ? padded / 8 : 1))), dim3(TT_BLOCK), 0, s, from, ld, of, there, count, dim, to, padded, bias, starts);
+  return tt_launch_status();
+}
+template <class T> tt_status fold(const TTNarrow &n, const float2 *parts, float *loss, float *lse, hipStream_t s) {
+  const int tile = tile_for<STATS>(n), slots = slots_of(STATS, parts_of(n));
+  hipLaunchKernelGGL(k_narrow_fold<T>, dim3((unsigned)tt_ceil_div(n.rows, TT_BLOCK / 64)), dim3(TT_BLOCK), 0, s, n, parts, tile, slots, loss, lse);
+  return tt_launch_status();
+}
 // Whether the classes are few enough for the rows to come in several runs (fewer rows that count never make it so).
-bool several(const TTNarrow &n) { return workgroups<CLASSES>(n) > (n.classes + (n.padded == 64 ? tile_of(64, CLASSES) : tile_of(128, CLASSES)) - 1) / (n.padded == 64 ? tile_of(64, CLASSES) : tile_of(128, CLASSES)); }
+bool several(const TTNarrow &n) { return workgroups<CLASSES>(n) > tt_ceil_div(n.classes, tile_for<CLASSES>(n)); }
 
 }  // namespace
 
 #ifndef TT_LOSS_NARROW
 #define TT_LOSS_NARROW 128
 #endif
-bool ttk_narrow_serves(int dtype, int dim) { return dtype != TT_F32 && dim <= TT_LOSS_NARROW; }
+bool ttk_narrow_serves(int dim) { return dim <= TT_LOSS_NARROW; }
 int ttk_narrow_padded(int dim) { return dim <= 64 ? 64 : 128; }
 
-size_t ttk_narrow_stats_bytes(const TTNarrow &n) { return (size_t)workgroups<STATS>(n) * (n.padded == 64 ? tile_of(64, STATS) : tile_of(128, STATS)) * 8; }
+size_t ttk_narrow_stats_bytes(const TTNarrow &n) { return (size_t)workgroups<STATS>(n) * tile_for<STATS>(n) * 8; }
 size_t ttk_narrow_parts_bytes(const TTNarrow &n) {
-  const size_t dx = (size_t)workgroups<ROWS>(n) * (n.padded == 64 ? tile_of(64, ROWS) : tile_of(128, ROWS)) * n.padded * 4;
-  const size_t dw = several(n) ? (size_t)workgroups<CLASSES>(n) * (n.padded == 64 ? tile_of(64, CLASSES) : tile_of(128, CLASSES)) * (n.padded + 4) * 4 : 0;
+  const size_t dx = (size_t)workgroups<ROWS>(n) * tile_for<ROWS>(n) * n.padded * 4;
+  const size_t dw = several(n) ? (size_t)workgroups<CLASSES>(n) * tile_for<CLASSES>(n) * (n.padded + 4) * 4 : 0;
   return dx > dw ? dx : dw;
 }
 
-tt_status ttk_narrow_classes(const TTNarrow &n, hipStream_t s) {
-  const dim3 grid(grid_of((long long)n.classes * (n.copy ? n.padded / 8 : 1))), block(TT_BLOCK);
-  if (n.dtype == TT_BF16) hipLaunchKernelGGL(k_narrow_classes<ttg::bf16>, grid, block, 0, s, n, n.starts, (ttg::bf16 *)n.copy);
-  else hipLaunchKernelGGL(k_narrow_classes<ttg::f16>, grid, block, 0, s, n, n.starts, (ttg::f16 *)n.copy);
-  return tt_launch_status();
+tt_status ttk_narrow_take(const TTNarrow &n, hipStream_t s) {
+  const tt_status st = TT_BY_TYPE(take, n.dtype, n, false, s);
+  return st == TT_OK ? TT_BY_TYPE(take, n.dtype, n, true, s) : st;
 }
 tt_status ttk_narrow_stats(const TTNarrow &n, float *stats, float *loss, float *lse, hipStream_t s) {
   Args a = args_of(n, false);
   a.parts = stats;
-  tt_status st = launch<STATS>(n, false, a, s);
-  if (st != TT_OK) return st;
-  const int tile = n.padded == 64 ? tile_of(64, STATS) : tile_of(128, STATS), slots = slots_of(STATS);
-  const dim3 grid((unsigned)tt_ceil_div(n.rows, TT_BLOCK / 64)), block(TT_BLOCK);
-  const float2 *parts = (const float2 *)stats;
-  if (n.dtype == TT_BF16) hipLaunchKernelGGL(k_narrow_fold<ttg::bf16>, grid, block, 0, s, n, parts, tile, slots, loss, lse);
-  else hipLaunchKernelGGL(k_narrow_fold<ttg::f16>, grid, block, 0, s, n, parts, tile, slots, loss, lse);
-  return tt_launch_status();
+  const tt_status st = launch<STATS>(n, false, a, s);
+  return st == TT_OK ? TT_BY_TYPE(fold, n.dtype, n, (const float2 *)stats, loss, lse, s) : st;
 }
 tt_status ttk_narrow_dx(const TTNarrow &n, float *parts, void *dx, long long ld_dx, hipStream_t s) {
   Args a = args_of(n, false);
   a.parts = parts;
   const tt_status st = launch<ROWS>(n, false, a, s);
-  if (st != TT_OK) return st;
-  return n.dtype == TT_BF16 ? finish_dx<ttg::bf16>(n, parts, dx, ld_dx, s) : finish_dx<ttg::f16>(n, parts, dx, ld_dx, s);
+  return st == TT_OK ? TT_BY_TYPE(finish_dx, n.dtype, n, (const float *)parts, dx, ld_dx, s) : st;
 }
 tt_status ttk_narrow_dw(const TTNarrow &n, bool shares, float *parts, void *dw, void *dbias, hipStream_t s) {
   Args a = args_of(n, true);
@@ -516,6 +628,5 @@ tt_status ttk_narrow_dw(const TTNarrow &n, bool shares, float *parts, void *dw, 
   a.out = dw;
   a.sums = dbias;
   const tt_status st = launch<CLASSES>(n, shares, a, s);
-  if (st != TT_OK || !several(n)) return st;
-  return n.dtype == TT_BF16 ? finish_dw<ttg::bf16>(n, parts, dw, dbias, s) : finish_dw<ttg::f16>(n, parts, dw, dbias, s);
+  return st == TT_OK && several(n) ? TT_BY_TYPE(finish_dw, n.dtype, n, (const float *)parts, dw, dbias, s) : st;
 }

@@ -51,7 +51,7 @@ struct TTGemm {
   int first;
   const float *lse, *row_grad; // SOFTMAX: [M]
   int n_padded;                // SOFTMAX
-  float *acc;                  // ACC: [M][N], fp32
+  float *acc;                  // ACC: [batch][M][N], fp32
   int acc_add;
   const float *scale;          // SCALED: DEVICE
   int parts;                   // fp32 operands: bf16 parts of each that are multiplied (3: fp32's precision, 2: 16 bits)

@@ -593,7 +593,7 @@ template <class T, class O, int EPI> __device__ __forceinline__ void join_pieces
     }
     if constexpr (EPI == TT_GEMM_ACC) {
       if (valid > 0) {
-        float *to = g.acc + (long long)m * g.N + n;
+        float *to = g.acc + ((long long)z * g.M + m) * g.N + n;
         float t[4] = {0.f, 0.f, 0.f, 0.f};
         if (g.acc_add) load4(to, valid, t);
 #pragma unroll

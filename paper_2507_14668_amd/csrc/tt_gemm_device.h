@@ -409,8 +409,8 @@ template <class T> __device__ __forceinline__ void finish_softmax(const TTGemm &
   store_n<T, 8>((T *)g.out + (long long)m * g.ldo + n, g.n_padded - n, v);
 }
 // Eight columns of a row, added to what earlier products left there.
-__device__ __forceinline__ void finish_acc(const TTGemm &g, int m, int n, int valid, float v[8]) {
-  float *to = g.acc + (long long)m * g.N + n;
+__device__ __forceinline__ void finish_acc(const TTGemm &g, int z, int m, int n, int valid, float v[8]) {
+  float *to = g.acc + ((long long)z * g.M + m) * g.N + n;
   float t[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
   if (g.acc_add) load_n<float, 8>(to, valid, t);
 #pragma unroll
@@ -533,7 +533,7 @@ __device__ __forceinline__ void finish_tile(const TTGemm &g, int z, int m0, int 
         if constexpr (EPI == TT_GEMM_SOFTMAX) {
           if (m < end && n0 + c < g.n_padded) finish_softmax<T>(g, m, n0 + c, v, bias);
         } else {
-          if (m < end && valid > 0) finish_acc(g, m, n0 + c, valid, v);
+          if (m < end && valid > 0) finish_acc(g, z, m, n0 + c, valid, v);
         }
       }
     } else if (STREAM && g.res) {

@@ -133,14 +133,22 @@ __global__ void __launch_bounds__(SCAN) k_loss_sum(const float *each, long long 
 }
 
 // dx from its sums in the order of the places; zeros in rows that do not count
-template <class T> __global__ void __launch_bounds__(TT_BLOCK) k_loss_dx(const float *acc, int ld_acc, long long rows, int dim, Rows w, T *dx, long long ld) {
+template <class T> __global__ void __launch_bounds__(TT_BLOCK) k_loss_dx(const float *acc, int ld_acc, int cuts, long long rows, int dim, Rows w, T *dx, long long ld) {
   const int per = (dim + 3) / 4;
   const float back = w.back[0];
   for (long long e = (long long)blockIdx.x * TT_BLOCK + threadIdx.x; e < rows * per; e += (long long)gridDim.x * TT_BLOCK) {
     const long long r = e / per;
     const int c = (int)(e - r * per) * 4, at = w.at[r];
     float v[4] = {0.f, 0.f, 0.f, 0.f};
-    if (at >= 0) load4(acc + (long long)at * ld_acc + c, dim - c, v);
+    if (at >= 0) {
+#pragma unroll 4
+      for (int k = 0; k < cuts; ++k) {
+        float t[4];
+        load4(acc + (k * rows + at) * ld_acc + c, dim - c, t);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] += t[i];
+      }
+    }
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[i] *= back;
     store4(dx + r * ld + c, dim - c, v);
@@ -191,7 +199,7 @@ long long piece_of(const tt_loss *op, bool backward) {
 bool narrow(const tt_loss *op) { return ttk_narrow_serves(op->dim); }
 // 16-bit rows of a W whose length is no multiple of 8 elements are copied to ones that are, a piece at a time, so that the large tiles serve: the copy costs
 // four bytes an element at 4.5 TB/s, the tiles save the difference between 330 and 1100 TFLOP/s in every product; 1001 rows of 479 against
-// 50001 classes COPY us with it, 178 without.  Few rows do not pay for it.
+// 50001 classes 111 us with it, 178 without.  Few rows do not pay for it.
 #ifndef TT_LOSS_COPY_ROWS
 #define TT_LOSS_COPY_ROWS 256
 #endif
@@ -217,12 +225,29 @@ TTGemm of_logits(const tt_loss *op, int classes, bool backward, long long ldg) {
   g.n_padded = (classes + 7) & ~7;
   return g;
 }
-TTGemm of_dx(const tt_loss *op, int classes, long long ldg) {  // G W
+// G W: few tiles of dx over many classes are cut into `cuts` equal members, whole steps of 64 classes, whose sums stand side by side until
+// the end; what is left over is a product of its own.  4000 rows of 513 (48 tiles of 256) against 16384 classes in fp16 250 us whole, 108 in
+// five; 2000 x 256 (8 tiles) against 33536 in bf16 98 whole (in tiles of 64, by four), 67 in sixteen.
+#ifndef TT_LOSS_CUT
+#define TT_LOSS_CUT 1024  // classes of a member at least
+#endif
+int cuts_of(const tt_loss *op) {
+  const int e = op->dtype == TT_F32 ? 128 : 256;
+  const long long tiles = (long long)tt_ceil_div(op->rows, e) * tt_ceil_div(op->dim, e), want = op->dtype == TT_F32 ? 512 : 256;
+  if (op->rows <= 128 || tiles * 2 > want) return 1;
+  long long cuts = want / tiles;
+  const long long piece = piece_of(op, true), most = (piece < op->classes ? piece : op->classes) / TT_LOSS_CUT;
+  if (cuts > most) cuts = most;
+  return (int)(cuts < 1 ? 1 : cuts > 16 ? 16 : cuts);
+}
+TTGemm of_dx(const tt_loss *op, int classes, int members, long long ldg) {
   TTGemm g;
   describe(op, &g);
   g.a_kc = 1; g.b_kc = 0;
+  g.batch = members;
   g.M = (int)op->rows; g.N = copies(op) ? padded(op) : op->dim; g.K = classes;
   g.lda = ldg; g.ldb = g.ldo = g.N;
+  g.a_step = classes; g.b_step = (long long)classes * g.ldb;
   g.a_padded = 1;
   g.epilogue = TT_GEMM_ACC;
   return g;
@@ -283,13 +308,16 @@ Scratch scratch(const tt_loss *op, bool backward) {
     return w;
   }
   take(w.grads, rows * piece * es);
-  take(w.acc, rows * (copies(op) ? padded(op) : op->dim) * 4);
+  take(w.acc, (size_t)cuts_of(op) * rows * (copies(op) ? padded(op) : op->dim) * 4);
   take(w.column, (size_t)piece * es);
   size_t most = 0;
   const int last = (int)(op->classes - (op->classes - 1) / piece * piece);
   for (int i = 0; i < 2; ++i) {
     const int n = i ? last : (int)(piece < op->classes ? piece : op->classes);
-    const size_t need[3] = {ttk_gemm_partial_bytes(of_dx(op, n, piece)), ttk_gemm_partial_bytes(of_dw(op, n, piece, false)),
+    const int cuts = cuts_of(op), each = n / cuts / 64 * 64;
+    const size_t whole = ttk_gemm_partial_bytes(cuts > 1 && each > 0 ? of_dx(op, each, cuts, piece) : of_dx(op, n, 1, piece));
+    const size_t rest = cuts > 1 && each > 0 && n > each * cuts ? ttk_gemm_partial_bytes(of_dx(op, n - each * cuts, 1, piece)) : 0;
+    const size_t need[3] = {whole > rest ? whole : rest, ttk_gemm_partial_bytes(of_dw(op, n, piece, false)),
                             ttk_gemm_partial_bytes(of_dw(op, n, piece, true))};
     for (int k = 0; k < 3; ++k) most = need[k] > most ? need[k] : most;
   }
@@ -317,9 +345,9 @@ template <class T> tt_status gather(const tt_loss *op, const void *x, const Rows
   return tt_launch_status();
 }
 template <class T> tt_status write_dx(const tt_loss *op, const float *acc, const Rows &r, void *dx, hipStream_t s) {
-  const int dim = op->dim, ld_acc = copies(op) ? padded(op) : op->dim;
+  const int dim = op->dim, ld_acc = copies(op) ? padded(op) : op->dim, cuts = cuts_of(op);
   const long long rows = op->rows, ld = op->ld_dx ? op->ld_dx : op->dim;
-  hipLaunchKernelGGL(k_loss_dx<T>, dim3(grid_of(rows * tt_ceil_div(dim, 4))), dim3(TT_BLOCK), 0, s, acc, ld_acc, rows, dim, r, (T *)dx, ld);
+  hipLaunchKernelGGL(k_loss_dx<T>, dim3(grid_of(rows * tt_ceil_div(dim, 4))), dim3(TT_BLOCK), 0, s, acc, ld_acc, cuts, rows, dim, r, (T *)dx, ld);
   return tt_launch_status();
 }
 template <class T> tt_status pad(const tt_loss *op, const void *w, int classes, void *to, hipStream_t s) {
@@ -456,12 +484,17 @@ extern "C" tt_status tt_cross_entropy_backward(const tt_loss *op, const void *x,
     g.first = (int)c;
     if ((st = ttk_gemm(g, nullptr, s)) != TT_OK) return st;
     if (dx) {
-      TTGemm d = of_dx(op, n, piece);
-      d.a = ws + need.grads;
-      d.b = wc;
-      d.acc = (float *)(ws + need.acc);
-      d.acc_add = c > 0;
-      if ((st = ttk_gemm(d, ws + need.pieces, s)) != TT_OK) return st;
+      const int cuts = cuts_of(op), size = n / cuts / 64 * 64, members = cuts > 1 && size > 0 ? cuts : 1, whole = members > 1 ? size : n;
+      for (int i = 0; i < 2; ++i) {
+        const int from = i ? whole * members : 0, classes_of = i ? n - from : whole;
+        if (classes_of == 0) continue;
+        TTGemm d = of_dx(op, classes_of, i ? 1 : members, piece);
+        d.a = ws + need.grads + (size_t)from * es;
+        d.b = wc + (size_t)from * d.ldb * es;
+        d.acc = (float *)(ws + need.acc);
+        d.acc_add = c > 0 || i;
+        if ((st = ttk_gemm(d, ws + need.pieces, s)) != TT_OK) return st;
+      }
     }
     if (dw || dbias) {  // as in the dense operators: the sums of G's columns come beside a product
       TTGemm d = of_dw(op, n, piece, !dw);

@@ -12,7 +12,7 @@ import top_ref as ref
 from test_dense_emulation import BUILD_DIR, DT, Guarded, emu_build, place, ptr
 
 pytestmark = pytest.mark.skipif(not emu_build.available(), reason="host clang++ of the ROCm toolchain not found")
-PIECES = dict(tt_loss=["-DTT_LOSS_ROOM=40000"], tt_loss_narrow=["-DTT_LOSS_NARROW=0"])  # several pieces of the classes, short rows among them
+PIECES = dict(tt_loss=["-DTT_LOSS_ROOM=40000", "-DTT_LOSS_CUT=64", "-DTT_LOSS_COPY_ROWS=100"], tt_loss_narrow=["-DTT_LOSS_NARROW=0"])  # several pieces of the classes, short rows among them
 VARIANTS = {"as it is": ("top", {}), "pieces, large tiles": ("top_large", dict(PIECES, tt_gemm=["-DTT_GEMM_LARGE_TILES=1"])),
             "pieces, direct tiles": ("top_direct", dict(PIECES, tt_gemm_direct=["-DTT_GEMM_DIRECT_TILES=1", "-DTT_GEMM_DIRECT_LEAST=0"]))}
 F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
@@ -384,6 +384,8 @@ LOSSES = [
     (130, 40, 521, F16, False, "none", 0, 0, 0),
     (270, 128, 300, BF16, True, "mean", 30, 0, 0),
     (40, 100, 700, BF16, True, "none", 4, 0, 1),
+    (140, 133, 500, F16, True, "mean", 4, 0, 1),  # a copy of W in longer rows
+    (150, 136, 450, F32, True, "sum", 4, 0, 0),
     (66, 20, 40, F32, False, "none", 60, 1, 0),
     (9, 8, 20, F32, True, "mean", 9, 0, 0),       # no row counts
     (300, 72, 264, F16, True, "sum", 3, 0, 0),

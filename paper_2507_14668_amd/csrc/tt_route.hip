@@ -17,19 +17,50 @@ struct Route {  // of a call, by value to the kernels
   float scale;
 };
 
-// ---- wavefront reductions without LDS: neighbours within rows of 16 lanes, then across the rows; lane 63 has the result.
+// ---- reductions and reads over the LANES (16 or 64) of a row ---------------------------------------
+__device__ __forceinline__ int row_lane(int lanes) { return threadIdx.x & (lanes - 1); }
+template <int LANES> __device__ __forceinline__ int from_lane(int v, int lane) {  // lane: the same in all of the row's
+  if constexpr (LANES == 64) return __builtin_amdgcn_readlane(v, lane);
+  else return __shfl(v, (threadIdx.x & 63 & ~(LANES - 1)) | lane, 64);
+}
+template <int LANES> __device__ __forceinline__ u64 ballot_of(bool p) {  // of the row's lanes
+  if constexpr (LANES == 64) return __ballot(p);
+  else return __ballot(p) >> (threadIdx.x & 63 & ~(LANES - 1)) & ((1ull << LANES) - 1);
+}
+// Neighbours within rows of 16 lanes, then across those, without LDS; the last lane has the result.
 template <int CTRL, int ROWS> __device__ __forceinline__ unsigned max_dpp(unsigned v) {
   const unsigned t = (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xf, false);
   return t > v ? t : v;
 }
-__device__ __forceinline__ unsigned wave_max_u32(unsigned v) {
+template <int LANES> __device__ __forceinline__ unsigned max_of(unsigned v) {
   v = max_dpp<0x111, 0xf>(v);  // from 1, 2, 4, 8 lanes before
   v = max_dpp<0x112, 0xf>(v);
   v = max_dpp<0x114, 0xf>(v);
   v = max_dpp<0x118, 0xf>(v);
-  v = max_dpp<0x142, 0xa>(v);  // the ends of rows 0 and 2 to rows 1 and 3
-  v = max_dpp<0x143, 0xc>(v);  // the end of row 1 to rows 2 and 3
-  return (unsigned)__builtin_amdgcn_readlane((int)v, 63);
+  if constexpr (LANES == 64) {
+    v = max_dpp<0x142, 0xa>(v);  // the ends of rows 0 and 2 to rows 1 and 3
+    v = max_dpp<0x143, 0xc>(v);  // the end of row 1 to rows 2 and 3
+  }
+  return (unsigned)from_lane<LANES>((int)v, LANES - 1);
+}
+template <int LANES> __device__ __forceinline__ float largest_of(float v) {  // NaN does not count
+#pragma unroll
+  for (int o = LANES / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
+  return v;
+}
+template <int LANES> __device__ __forceinline__ float sum_of(float v) {
+#pragma unroll
+  for (int o = LANES / 2; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+  return v;
+}
+template <int LANES> __device__ __forceinline__ double sum_of(double v) {
+#pragma unroll
+  for (int o = LANES / 2; o > 0; o >>= 1) {
+    const long long b = __builtin_bit_cast(long long, v);
+    const int lo = __shfl((int)b, (threadIdx.x & 63) ^ o, 64), hi = __shfl((int)(b >> 32), (threadIdx.x & 63) ^ o, 64);
+    v += __builtin_bit_cast(double, ((long long)hi << 32) | (unsigned)lo);
+  }
+  return v;
 }
 // The order of numbers as that of unsigned integers: -infinity and masked ones 0 (there is no choice), NaN the largest.
 __device__ __forceinline__ u64 key_of(double c) {
@@ -41,36 +72,29 @@ __device__ __forceinline__ u64 key_of(double c) {
 __device__ __forceinline__ double value_of(u64 key) {  // of keys other than 0; ~0 is a NaN as it is
   return __builtin_bit_cast(double, (long long)(key >> 63 ? key & 0x7fffffffffffffffull : ~key));
 }
-// The lane with the largest key, the first of them; its key is `best`.
-__device__ __forceinline__ int pick(u64 key, u64 &best) {
-  const unsigned hi = (unsigned)(key >> 32), top = wave_max_u32(hi);
-  u64 lanes = __ballot(hi == top);
-  unsigned low = 0;
-  if (__popcll(lanes) > 1) {
-    low = wave_max_u32(hi == top ? (unsigned)key : 0u);
-    lanes = __ballot(hi == top && (unsigned)key == low);
-    best = (u64)top << 32 | low;
-    return __ffsll(lanes) - 1;
+// The row's lane with the largest key, the first of them; its key is `best`.
+template <int LANES> __device__ __forceinline__ int pick(u64 key, u64 &best) {
+  const unsigned hi = (unsigned)(key >> 32), top = max_of<LANES>(hi);
+  u64 lanes = ballot_of<LANES>(hi == top);
+  unsigned low;
+  if (__ballot(__popcll(lanes) > 1)) {  // (of any row of the wavefront)
+    low = max_of<LANES>(hi == top ? (unsigned)key : 0u);
+    lanes = ballot_of<LANES>(hi == top && (unsigned)key == low);
+  } else {
+    low = (unsigned)from_lane<LANES>((int)(unsigned)key, __ffsll(lanes) - 1);
   }
-  const int lane = __ffsll(lanes) - 1;
-  low = (unsigned)__builtin_amdgcn_readlane((int)(unsigned)key, lane);
   best = (u64)top << 32 | low;
-  return lane;
+  return __ffsll(lanes) - 1;
 }
-__device__ __forceinline__ double read_lane64(double v, int lane) {
+template <int LANES> __device__ __forceinline__ double read_lane64(double v, int lane) {
   const long long b = __builtin_bit_cast(long long, v);
-  const unsigned lo = (unsigned)__builtin_amdgcn_readlane((int)b, lane), hi = (unsigned)__builtin_amdgcn_readlane((int)(b >> 32), lane);
+  const unsigned lo = (unsigned)from_lane<LANES>((int)b, lane), hi = (unsigned)from_lane<LANES>((int)(b >> 32), lane);
   return __builtin_bit_cast(double, (long long)((u64)hi << 32 | lo));
-}
-__device__ __forceinline__ float wave_max(float v) {  // NaN does not count
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
-  return v;
 }
 
 // The lane's EL logits, experts EL lane .. + EL - 1 (-infinity behind the last one).
-template <class T, int EL> __device__ __forceinline__ void load_logits(const Route &p, long long row, float z[EL]) {
-  const int first = EL * (threadIdx.x & 63), valid = p.num - first;
+template <class T, int LANES, int EL> __device__ __forceinline__ void load_logits(const Route &p, long long row, float z[EL]) {
+  const int first = EL * row_lane(LANES), valid = p.num - first;
   const T *src = (const T *)p.logits + row * p.ld + first;
   if constexpr (EL >= 4) {
     load_n<T, EL>(src, valid, z);
@@ -84,17 +108,23 @@ template <class T, int EL> __device__ __forceinline__ void load_logits(const Rou
 
 constexpr int ROUTE_WAVES = 4;
 
-// A wavefront takes a row: scores in 64 bits, then choice after choice the largest key of all lanes.
-template <class T, int EL, bool GROUPS> __global__ void __launch_bounds__(64 * ROUTE_WAVES) k_route(Route p) {
+// LANES lanes take a row (16: up to 64 experts and 16 choices, four rows a wavefront; 64: all others): scores in 64 bits, then choice after choice the largest
+// key of all lanes.  16384 rows of 256 experts, sigmoid, four of eight groups, eight choices 37 us: the 64-bit exp and division, and about 60 instructions a
+// choice.  65536 rows of 64 experts and four choices 21 us; the call with the order 57 us by 64 lanes a row, 43 by 16.
+template <class T, int LANES, int EL, bool GROUPS> __global__ void __launch_bounds__(64 * ROUTE_WAVES) k_route(Route p) {
+  static_assert(!GROUPS || LANES == 64, "groups");
+  constexpr int PER = 64 / LANES;  // rows a wavefront
   __shared__ u64 room[GROUPS ? ROUTE_WAVES : 1][GROUPS ? 64 * EL : 1];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, first = EL * lane;
+  const int lane = row_lane(LANES), wave = threadIdx.x >> 6, first = EL * lane;
   float bias[EL];
 #pragma unroll
   for (int i = 0; i < EL; ++i) bias[i] = p.bias && first + i < p.num ? p.bias[first + i] : 0.f;
-  for (long long r = (long long)blockIdx.x * ROUTE_WAVES + wave; r < p.rows; r += (long long)gridDim.x * ROUTE_WAVES) {
+  for (long long r0 = ((long long)blockIdx.x * ROUTE_WAVES + wave) * PER; r0 < p.rows; r0 += (long long)gridDim.x * ROUTE_WAVES * PER) {
+    const bool live = r0 + (threadIdx.x & 63) / LANES < p.rows;
+    const long long r = live ? r0 + (threadIdx.x & 63) / LANES : p.rows - 1;
     float z[EL];
     double s[EL];
-    load_logits<T, EL>(p, r, z);
+    load_logits<T, LANES, EL>(p, r, z);
     if (p.sigmoid) {
 #pragma unroll
       for (int i = 0; i < EL; ++i) s[i] = 1.0 / (1.0 + exp(-(double)z[i]));
@@ -102,7 +132,7 @@ template <class T, int EL, bool GROUPS> __global__ void __launch_bounds__(64 * R
       float top = z[0];
 #pragma unroll
       for (int i = 1; i < EL; ++i) top = fmaxf(top, z[i]);
-      top = wave_max(top);
+      top = largest_of<LANES>(top);
       if (top == -INFINITY) top = 0.f;
       double sum = 0;
 #pragma unroll
@@ -110,7 +140,7 @@ template <class T, int EL, bool GROUPS> __global__ void __launch_bounds__(64 * R
         s[i] = exp((double)z[i] - (double)top);
         sum += s[i];
       }
-      sum = wave_sum64(sum);
+      sum = sum_of<LANES>(sum);
       const double inv = sum == 0 ? 0.0 : 1.0 / sum;
 #pragma unroll
       for (int i = 0; i < EL; ++i) s[i] *= inv;
@@ -147,7 +177,7 @@ template <class T, int EL, bool GROUPS> __global__ void __launch_bounds__(64 * R
       u64 keep = 0;
       for (int t = 0; t < p.top_groups; ++t) {
         u64 best;
-        const int l = pick(strength, best);
+        const int l = pick<64>(strength, best);
         if (best == 0) break;
         keep |= 1ull << (l / per);
         strength = lane == l ? 0 : strength;
@@ -170,11 +200,9 @@ template <class T, int EL, bool GROUPS> __global__ void __launch_bounds__(64 * R
 #pragma unroll
       for (int i = 1; i < EL; ++i) sc = at == i ? s[i] : sc;
       u64 top;
-      const int l = pick(best, top);
-      if (top == 0) break;
-      const int which = __builtin_amdgcn_readlane(at, l);
-      sc = read_lane64(sc, l);
-      if (lane == j) {
+      const int l = pick<LANES>(best, top), which = from_lane<LANES>(at, l);
+      sc = read_lane64<LANES>(sc, l);
+      if (lane == j && top != 0) {  // (0: none is left)
         mine = EL * l + which;
         score = sc;
       }
@@ -182,10 +210,10 @@ template <class T, int EL, bool GROUPS> __global__ void __launch_bounds__(64 * R
       for (int i = 0; i < EL; ++i) key[i] = lane == l && which == i ? 0 : key[i];
     }
     if (p.renorm) {
-      const double sum = wave_sum64(score);
+      const double sum = sum_of<LANES>(score);
       score = sum == 0 ? 0.0 : score / sum;
     }
-    if (lane < p.k) {
+    if (live && lane < p.k) {
       p.experts[r * p.k + lane] = mine;
       p.weights[r * p.k + lane] = (float)((double)p.scale * score);
     }
@@ -194,12 +222,16 @@ template <class T, int EL, bool GROUPS> __global__ void __launch_bounds__(64 * R
 
 // dz = s (ds - sum ds s) (softmax) or ds s (1 - s), with ds of the chosen experts from the gradients of their weights:
 // scale g, or scale (g - sum g w') / sum s with the renormalised w' = s / sum s.
-template <class T, int EL> __global__ void __launch_bounds__(64 * ROUTE_WAVES) k_route_backward(Route p) {
-  __shared__ float room[ROUTE_WAVES][64 * EL];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, first = EL * lane;
-  for (long long r = (long long)blockIdx.x * ROUTE_WAVES + wave; r < p.rows; r += (long long)gridDim.x * ROUTE_WAVES) {
+template <class T, int LANES, int EL> __global__ void __launch_bounds__(64 * ROUTE_WAVES) k_route_backward(Route p) {
+  constexpr int PER = 64 / LANES;
+  __shared__ float room[ROUTE_WAVES * PER][LANES * EL];
+  const int lane = row_lane(LANES), wave = threadIdx.x >> 6, first = EL * lane;
+  float *mine_of = room[threadIdx.x / LANES];
+  for (long long r0 = ((long long)blockIdx.x * ROUTE_WAVES + wave) * PER; r0 < p.rows; r0 += (long long)gridDim.x * ROUTE_WAVES * PER) {
+    const bool live = r0 + (threadIdx.x & 63) / LANES < p.rows;
+    const long long r = live ? r0 + (threadIdx.x & 63) / LANES : p.rows - 1;
     float z[EL], s[EL];
-    load_logits<T, EL>(p, r, z);
+    load_logits<T, LANES, EL>(p, r, z);
     const int64_t asked = lane < p.k ? p.experts[r * p.k + lane] : -1;
     const int mine = asked >= 0 && asked < p.num ? (int)asked : -1;
     float g = mine >= 0 ? p.scale * p.grad[r * p.k + lane] : 0.f;
@@ -210,33 +242,33 @@ template <class T, int EL> __global__ void __launch_bounds__(64 * ROUTE_WAVES) k
       float top = z[0], sum = 0.f;
 #pragma unroll
       for (int i = 1; i < EL; ++i) top = fmaxf(top, z[i]);
-      top = wave_max(top);
+      top = largest_of<LANES>(top);
       if (top == -INFINITY) top = 0.f;
 #pragma unroll
       for (int i = 0; i < EL; ++i) {
         s[i] = expf(z[i] - top);
         sum += s[i];
       }
-      sum = tt_wave_sum(sum);
+      sum = sum_of<LANES>(sum);
       const float inv = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
       for (int i = 0; i < EL; ++i) s[i] *= inv;
     }
 #pragma unroll
-    for (int i = 0; i < EL; ++i) room[wave][first + i] = s[i];
+    for (int i = 0; i < EL; ++i) mine_of[first + i] = s[i];
     tt_wave_lds_order();
-    const float chosen = mine >= 0 ? room[wave][mine] : 0.f;
+    const float chosen = mine >= 0 ? mine_of[mine] : 0.f;
     tt_wave_lds_order();
     if (p.renorm) {
-      const float total = tt_wave_sum(chosen), inv = total == 0.f ? 0.f : 1.f / total;
-      const float mean = tt_wave_sum(g * chosen) * inv;
+      const float total = sum_of<LANES>(chosen), inv = total == 0.f ? 0.f : 1.f / total;
+      const float mean = sum_of<LANES>(g * chosen) * inv;
       g = mine >= 0 ? (g - mean) * inv : 0.f;
     }
-    const float dot = p.sigmoid ? 0.f : tt_wave_sum(g * chosen);
+    const float dot = p.sigmoid ? 0.f : sum_of<LANES>(g * chosen);
     float d[EL] = {};
     for (int j = 0; j < p.k; ++j) {  // one after the other: an expert named twice gets both
-      const int e = __builtin_amdgcn_readlane(mine, j) - first;
-      const float gj = __uint_as_float((unsigned)__builtin_amdgcn_readlane((int)__float_as_uint(g), j));
+      const int e = from_lane<LANES>(mine, j) - first;
+      const float gj = __uint_as_float((unsigned)from_lane<LANES>((int)__float_as_uint(g), j));
 #pragma unroll
       for (int i = 0; i < EL; ++i) d[i] += e == i ? gj : 0.f;
     }
@@ -245,6 +277,7 @@ template <class T, int EL> __global__ void __launch_bounds__(64 * ROUTE_WAVES) k
       if (p.sigmoid) d[i] = d[i] == 0.f ? 0.f : d[i] * s[i] * (1.f / (1.f + expf(z[i])));
       else d[i] = s[i] * (d[i] - dot);
     }
+    if (!live) continue;
     T *to = (T *)p.dlogits + r * p.ldd + first;
     const int valid = p.num - first;
     if constexpr (EL >= 4) {
@@ -446,21 +479,34 @@ Route describe(const tt_route *op) {
   p.scale = op->scale;
   return p;
 }
-template <class T, int EL> void launch_el(const Route &p, bool backward, hipStream_t s) {
-  long long blocks = (p.rows + ROUTE_WAVES - 1) / ROUTE_WAVES;
+template <class T, int LANES, int EL> void launch_el(const Route &p, bool backward, hipStream_t s) {
+  constexpr int ROWS = ROUTE_WAVES * 64 / LANES;
+  long long blocks = (p.rows + ROWS - 1) / ROWS;
   if (blocks > 8192) blocks = 8192;
   const dim3 grid((unsigned)blocks), block(64 * ROUTE_WAVES);
-  if (backward) hipLaunchKernelGGL((k_route_backward<T, EL>), grid, block, 0, s, p);
-  else if (p.top_groups < p.groups) hipLaunchKernelGGL((k_route<T, EL, true>), grid, block, 0, s, p);
-  else hipLaunchKernelGGL((k_route<T, EL, false>), grid, block, 0, s, p);
+  if (backward) {
+    hipLaunchKernelGGL((k_route_backward<T, LANES, EL>), grid, block, 0, s, p);
+    return;
+  }
+  if constexpr (LANES == 64) {
+    if (p.top_groups < p.groups) {
+      hipLaunchKernelGGL((k_route<T, LANES, EL, true>), grid, block, 0, s, p);
+      return;
+    }
+  }
+  hipLaunchKernelGGL((k_route<T, LANES, EL, false>), grid, block, 0, s, p);
 }
 template <class T> tt_status launch(const Route &p, bool backward, hipStream_t s) {
   const int el = tt_ceil_div(p.num, 64);
-  if (el <= 1) launch_el<T, 1>(p, backward, s);
-  else if (el <= 2) launch_el<T, 2>(p, backward, s);
-  else if (el <= 4) launch_el<T, 4>(p, backward, s);
-  else if (el <= 8) launch_el<T, 8>(p, backward, s);
-  else launch_el<T, 16>(p, backward, s);
+  if (p.num <= 64 && p.k <= 16 && (backward || p.top_groups == p.groups)) {
+    if (p.num <= 16) launch_el<T, 16, 1>(p, backward, s);
+    else if (p.num <= 32) launch_el<T, 16, 2>(p, backward, s);
+    else launch_el<T, 16, 4>(p, backward, s);
+  } else if (el <= 1) launch_el<T, 64, 1>(p, backward, s);
+  else if (el <= 2) launch_el<T, 64, 2>(p, backward, s);
+  else if (el <= 4) launch_el<T, 64, 4>(p, backward, s);
+  else if (el <= 8) launch_el<T, 64, 8>(p, backward, s);
+  else launch_el<T, 64, 16>(p, backward, s);
   return tt_launch_status();
 }
 tt_status launch(int dtype, const Route &p, bool backward, hipStream_t s) {

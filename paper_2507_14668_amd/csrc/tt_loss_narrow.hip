@@ -24,29 +24,36 @@ constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr float RAISE = 13.f;  // P is formed 2^13 times its size: fp16's smallest numbers then are of 2^-37, and P stays below 2^14
 enum Mode { STATS, ROWS, CLASSES };
 // of 16 vectors, of a wavefront: what fits the registers
-constexpr int held_tiles(int KP, Mode mode, int parts) { return parts == 1 ? (mode != STATS && KP == 128 ? 3 : 4) : KP == 128 ? (mode == STATS ? 3 : 2) : (mode == STATS ? 4 : 3); }
+__host__ __device__ constexpr int held_tiles(int KP, Mode mode, int parts) { return parts == 1 ? (mode != STATS && KP == 128 ? 3 : 4) : KP == 128 ? (mode == STATS ? 3 : 2) : (mode == STATS ? 4 : 3); }
 
 // How a launch is cut, from the number of held vectors (which the host does not know where they are rows that count) and of workgroups that run at once:
 // workgroup w has block w % blocks of the held vectors and run w / blocks of the streamed ones.  As many runs as fill the card once, or
-// twice where that wastes less; eight steps at least in each.
+// twice where that wastes less; `least` steps at least in each, since its parts are written and added at the end.
 struct Cut {
   int blocks, runs;
 };
-__host__ __device__ inline Cut cut_of(long long held, long long streamed, int tile, int slots) {
+struct Sizes {  // of a kernel's launches
+  int tile, slots, least;
+};
+__host__ __device__ inline Cut cut_of(long long held, long long streamed, const Sizes &z) {
+  const int tile = z.tile, slots = z.slots;
   const long long blocks = held < 1 ? 1 : (held + tile - 1) / tile, steps = (streamed + STEP - 1) / STEP;
   const long long one = slots / blocks, two = 2LL * slots / blocks;
   long long runs = 42 * one >= 20 * two ? one : two;
-  if (runs > steps / 8) runs = steps / 8;
+  if (runs > steps / z.least) runs = steps / z.least;
   return Cut{(int)blocks, (int)(runs < 1 ? 1 : runs)};
 }
 // Workgroups for any number of vectors up to these.
-__host__ __device__ inline long long grid_for(long long held, long long streamed, int tile, int slots) {
-  const long long blocks = held < 1 ? 1 : (held + tile - 1) / tile, most = blocks * ((streamed + 8 * STEP - 1) / (8 * STEP));
-  const long long twice = 2LL * slots < most ? 2LL * slots : most;
+inline long long grid_for(long long held, long long streamed, const Sizes &z) {
+  const long long blocks = held < 1 ? 1 : (held + z.tile - 1) / z.tile, most = blocks * ((streamed + z.least * STEP - 1) / (z.least * STEP));
+  const long long twice = 2LL * z.slots < most ? 2LL * z.slots : most;
   return blocks > twice ? blocks : twice;
 }
-constexpr int tile_of(int KP, Mode mode, int parts) { return 16 * held_tiles(KP, mode, parts) * WAVES; }
-constexpr int slots_of(Mode mode, int parts) { return 256 * (mode == STATS && parts == 1 ? 4 : 2); }
+__host__ __device__ constexpr int tile_of(int KP, Mode mode, int parts) { return 16 * held_tiles(KP, mode, parts) * WAVES; }
+// A step takes 0.4 us of a wavefront, of fp32 1.5; the statistics' parts are eight bytes a row.
+__host__ __device__ constexpr Sizes sizes_of(int KP, Mode mode, int parts) {
+  return Sizes{tile_of(KP, mode, parts), 256 * (mode == STATS && parts == 1 ? 4 : 2), parts == 3 ? (mode == STATS ? 2 : 3) : mode == STATS ? 4 : 8};
+}
 
 struct Args {
   const void *held, *streamed;
@@ -250,7 +257,7 @@ template <class T, class O, int KP, Mode MODE, bool SHARES> __global__ void __la
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), q = lane >> 4, j = lane & 15;
   const long long places = a.offsets[1];
   const long long held_count = CLASS ? a.classes : places, streamed_count = CLASS ? places : a.classes;
-  const Cut cut = cut_of(held_count, streamed_count, tile_of(KP, MODE, PARTS), slots_of(MODE, PARTS));
+  const Cut cut = cut_of(held_count, streamed_count, sizes_of(KP, MODE, PARTS));
   const int block = (int)(blockIdx.x % (unsigned)cut.blocks), run = (int)(blockIdx.x / (unsigned)cut.blocks);
   if (run >= cut.runs || held_count == 0) return;
   const long long h0 = (long long)block * tile_of(KP, MODE, PARTS) + wave * HELD;
@@ -393,85 +400,96 @@ template <class T, class O, int KP, Mode MODE, bool SHARES> __global__ void __la
 }
 
 // Each place's statistics of all runs together, the label's logit as a product of its own, and what the row has of it: a wavefront a place.
-template <class T> __global__ void __launch_bounds__(TT_BLOCK) k_narrow_fold(TTNarrow n, const float2 *__restrict__ parts, int tile, int slots, float *loss, float *lse) {
+template <class T> __global__ void __launch_bounds__(TT_BLOCK) k_narrow_fold(TTNarrow n, const float2 *__restrict__ parts, Sizes z, float *loss, float *lse) {
   const int lane = threadIdx.x & 63;
   const long long i = (long long)blockIdx.x * (TT_BLOCK / 64) + (threadIdx.x >> 6), places = n.r.offsets[1];
   if (i >= places) return;
-  const Cut cut = cut_of(places, n.classes, tile, slots);
+  const Cut cut = cut_of(places, n.classes, z);
+  const int tile = z.tile;
   const long long block = i / tile;
   const int label = n.r.label[i];
   float2 s = {-INFINITY, 0.f};
   for (int k = lane; k < cut.runs; k += 64) s = join_runs(s, parts[(k * (long long)cut.blocks + block) * tile + i % tile]);
-  float z = 0.f;
+  float logit = 0.f;  // the label's
   if (label >= 0) {
 #pragma unroll
     for (int c = lane; c < 128; c += 64)
-      if (c < n.dim) z = fmaf(to_f32(((const T *)n.of_call)[n.r.of[i] * n.ld + c]), to_f32(((const T *)n.w)[(long long)label * n.dim + c]), z);
+      if (c < n.dim) logit = fmaf(to_f32(((const T *)n.of_call)[n.r.of[i] * n.ld + c]), to_f32(((const T *)n.w)[(long long)label * n.dim + c]), logit);
   }
 #pragma unroll
   for (int o = 1; o < 64; o *= 2) {
     s = join_runs(s, float2{__shfl(s.x, lane ^ o, 64), __shfl(s.y, lane ^ o, 64)});
-    z += __shfl(z, lane ^ o, 64);
+    logit += __shfl(logit, lane ^ o, 64);
   }
   if (lane != 0) return;
-  z += label >= 0 ? n.starts[label] : 0.f;
+  logit += label >= 0 ? n.starts[label] : 0.f;
   const int r = n.r.of[i];
   const float more = log2f(s.y);
   // (the label's logit is taken off before the sum's logarithm is added: near a loss of zero lse less that logit would be lse's rounding)
   lse[r] = label < 0 ? NAN : s.x == INFINITY ? s.y : (s.x + more) * LN2;
-  loss[r] = label < 0 ? NAN : s.x == INFINITY ? s.y - z : (fmaf(-z, LOG2E, s.x) + more) * LN2;
+  loss[r] = label < 0 ? NAN : s.x == INFINITY ? s.y - logit : (fmaf(-logit, LOG2E, s.x) + more) * LN2;
 }
 
-// A workgroup's sum of the runs' parts of one vector, `width` columns (of four a thread) in eight runs that are added in order: in the threads of the first.
-template <int KP> __device__ __forceinline__ f32x4 sum_runs(const float *__restrict__ parts, int ld, const Cut &cut, int tile, long long vector, float *room) {
-  constexpr int PER = KP / 4 + 1, SEGMENTS = TT_BLOCK / PER;  // the last four columns: the sums
-  const int c = (int)threadIdx.x % PER, seg = (int)threadIdx.x / PER, each = (cut.runs + SEGMENTS - 1) / SEGMENTS;
-  const long long block = vector / tile;
-  f32x4 s = {0.f, 0.f, 0.f, 0.f};
-  if (seg < SEGMENTS && 4 * c < ld) {
-    const int end = (seg + 1) * each < cut.runs ? (seg + 1) * each : cut.runs;
-#pragma unroll 4
-    for (int k = seg * each; k < end; ++k)
-      s += *reinterpret_cast<const f32x4 *>(parts + ((k * (long long)cut.blocks + block) * tile + vector % tile) * ld + 4 * c);
-  }
-  f32x4 *all = reinterpret_cast<f32x4 *>(room);
-  all[threadIdx.x] = s;
-  __syncthreads();
-  if (seg == 0) {
-#pragma unroll
-    for (int k = 1; k < SEGMENTS; ++k) s += all[k * PER + c];
-  }
-  __syncthreads();
-  return s;
-}
-// dx = share times the sum, zeros in rows that do not count; a workgroup a row
-template <class T, int KP> __global__ void __launch_bounds__(TT_BLOCK) k_narrow_dx(TTNarrow n, const float *__restrict__ parts, T *dx, long long ld) {
-  __shared__ __align__(16) float room[TT_BLOCK * 4];
-  const long long places = n.r.offsets[1];
-  constexpr int PARTS = sizeof(T) == 4 ? 3 : 1;
-  const Cut cut = cut_of(places, n.classes, tile_of(KP, ROWS, PARTS), slots_of(ROWS, PARTS));
-  const int c = 4 * (int)threadIdx.x;
-  for (long long r = blockIdx.x; r < n.rows; r += gridDim.x) {
-    const int at = n.r.at[r];
+// The sums of the runs' parts of vectors, four columns a thread (the last four: the sums beside dW).  Up to eight runs: SEGMENTS vectors a workgroup, each by its own
+// threads; more: one vector, the runs in SEGMENTS shares that are then added in order (in the threads of the first).
+template <int KP> struct Summing {
+  static constexpr int PER = KP / 4 + 1, SEGMENTS = TT_BLOCK / PER;
+  __device__ static __forceinline__ bool together(const Cut &cut) { return cut.runs > 8; }
+  // `vector`: the workgroup's, or its threads' own (-1: none); all threads of the workgroup call it
+  __device__ static __forceinline__ f32x4 sum(const float *__restrict__ parts, int ld, const Cut &cut, int tile, long long vector, f32x4 *room) {
+    const int c = (int)threadIdx.x % PER, seg = (int)threadIdx.x / PER, each = together(cut) ? (cut.runs + SEGMENTS - 1) / SEGMENTS : cut.runs;
+    const int from = together(cut) ? seg * each : 0, end = from + each < cut.runs ? from + each : cut.runs;
     f32x4 s = {0.f, 0.f, 0.f, 0.f};
-    if (at >= 0) {
-      s = sum_runs<KP>(parts, KP, cut, tile_of(KP, ROWS, PARTS), at, room);
-      s *= 0x1p-13f * n.r.share[at];
+    if (vector >= 0 && seg < SEGMENTS && 4 * c < ld) {
+      const long long block = vector / tile;
+#pragma unroll 4
+      for (int k = from; k < end; ++k) s += *reinterpret_cast<const f32x4 *>(parts + ((k * (long long)cut.blocks + block) * tile + vector % tile) * ld + 4 * c);
     }
+    if (!together(cut)) return s;
+    __syncthreads();  // nobody reads the last vector's any more
+    room[threadIdx.x] = s;
+    __syncthreads();
+    if (seg == 0) {
+#pragma unroll
+      for (int k = 1; k < SEGMENTS; ++k) s += room[k * PER + c];
+    }
+    return s;
+  }
+};
+// dx = share times the sum, zeros in rows that do not count
+template <class T, int KP> __global__ void __launch_bounds__(TT_BLOCK) k_narrow_dx(TTNarrow n, const float *__restrict__ parts, T *dx, long long ld) {
+  typedef Summing<KP> S;
+  constexpr Sizes z = sizes_of(KP, ROWS, sizeof(T) == 4 ? 3 : 1);
+  __shared__ __align__(16) f32x4 room[TT_BLOCK];
+  const Cut cut = cut_of(n.r.offsets[1], n.classes, z);
+  const bool together = S::together(cut);
+  const int c = 4 * ((int)threadIdx.x % S::PER), seg = (int)threadIdx.x / S::PER, many = together ? 1 : S::SEGMENTS;
+  for (long long r0 = (long long)blockIdx.x * many; r0 < n.rows; r0 += (long long)gridDim.x * many) {
+    const long long r = r0 + (together ? 0 : seg);
+    const bool in = r < n.rows && seg < S::SEGMENTS;
+    const int at = in ? n.r.at[r] : -1;
+    f32x4 s = S::sum(parts, KP, cut, z.tile, at, room);
+    if (!in || (together && seg != 0) || c >= n.dim || c >= KP) continue;
+    if (at >= 0) s *= 0x1p-13f * n.r.share[at];
     const float v[4] = {s[0], s[1], s[2], s[3]};
-    if (c < n.dim && c < KP) store4(dx + r * ld + c, n.dim - c, v);
+    store4(dx + r * ld + c, n.dim - c, v);
   }
 }
-// dW and dbias where the rows came in several runs; a workgroup a class
+// dW and dbias where the rows came in several runs
 template <class T, int KP> __global__ void __launch_bounds__(TT_BLOCK) k_narrow_dw(TTNarrow n, const float *__restrict__ parts, T *dw, T *db) {
-  __shared__ __align__(16) float room[TT_BLOCK * 4];
-  constexpr int PARTS = sizeof(T) == 4 ? 3 : 1;
-  const Cut cut = cut_of(n.classes, n.r.offsets[1], tile_of(KP, CLASSES, PARTS), slots_of(CLASSES, PARTS));
+  typedef Summing<KP> S;
+  constexpr Sizes z = sizes_of(KP, CLASSES, sizeof(T) == 4 ? 3 : 1);
+  __shared__ __align__(16) f32x4 room[TT_BLOCK];
+  const Cut cut = cut_of(n.classes, n.r.offsets[1], z);
   if (cut.runs == 1) return;  // the products' kernel has written them
+  const bool together = S::together(cut);
   const float back = *n.r.back;
-  const int c = 4 * (int)threadIdx.x;
-  for (long long h = blockIdx.x; h < n.classes; h += gridDim.x) {
-    const f32x4 s = sum_runs<KP>(parts, KP + 4, cut, tile_of(KP, CLASSES, PARTS), h, room) * back;
+  const int c = 4 * ((int)threadIdx.x % S::PER), seg = (int)threadIdx.x / S::PER, many = together ? 1 : S::SEGMENTS;
+  for (long long h0 = (long long)blockIdx.x * many; h0 < n.classes; h0 += (long long)gridDim.x * many) {
+    const long long h = h0 + (together ? 0 : seg);
+    const bool in = h < n.classes && seg < S::SEGMENTS;
+    const f32x4 s = S::sum(parts, KP + 4, cut, z.tile, in ? h : -1, room) * back;
+    if (!in || (together && seg != 0)) continue;
     const float v[4] = {s[0], s[1], s[2], s[3]};
     if (dw && c < n.dim && c < KP) store4(dw + h * n.dim + c, n.dim - c, v);
     if (db && c == KP) db[h] = from_f32<T>(v[0]);
@@ -530,10 +548,11 @@ Args args_of(const TTNarrow &n, bool classes) {
   return a;
 }
 int parts_of(const TTNarrow &n) { return n.dtype == TT_F32 ? 3 : 1; }
-template <Mode MODE> int tile_for(const TTNarrow &n) { return n.padded == 64 ? tile_of(64, MODE, parts_of(n)) : tile_of(128, MODE, parts_of(n)); }
+template <Mode MODE> Sizes sizes_for(const TTNarrow &n) { return sizes_of(n.padded, MODE, parts_of(n)); }
+template <Mode MODE> int tile_for(const TTNarrow &n) { return sizes_for<MODE>(n).tile; }
 template <Mode MODE> long long workgroups(const TTNarrow &n) {
   const long long held = MODE == CLASSES ? n.classes : n.rows, streamed = MODE == CLASSES ? n.rows : n.classes;
-  return grid_for(held, streamed, tile_for<MODE>(n), slots_of(MODE, parts_of(n)));
+  return grid_for(held, streamed, sizes_for<MODE>(n));
 }
 template <class T, class O, int KP, Mode MODE> tt_status launch_as(const TTNarrow &n, bool shares, const Args &a, hipStream_t s) {
   const dim3 grid((unsigned)workgroups<MODE>(n)), block(THREADS);
@@ -584,8 +603,8 @@ template <class T> tt_status take(const TTNarrow &n, bool classes, hipStream_t s
   return tt_launch_status();
 }
 template <class T> tt_status fold(const TTNarrow &n, const float2 *parts, float *loss, float *lse, hipStream_t s) {
-  const int tile = tile_for<STATS>(n), slots = slots_of(STATS, parts_of(n));
-  hipLaunchKernelGGL(k_narrow_fold<T>, dim3((unsigned)tt_ceil_div(n.rows, TT_BLOCK / 64)), dim3(TT_BLOCK), 0, s, n, parts, tile, slots, loss, lse);
+  const Sizes z = sizes_for<STATS>(n);
+  hipLaunchKernelGGL(k_narrow_fold<T>, dim3((unsigned)tt_ceil_div(n.rows, TT_BLOCK / 64)), dim3(TT_BLOCK), 0, s, n, parts, z, loss, lse);
   return tt_launch_status();
 }
 // Whether the classes are few enough for the rows to come in several runs (fewer rows that count never make it so).

@@ -16,19 +16,29 @@ __global__ void __launch_bounds__(SCAN) k_loss_rows(const int64_t *labels, long 
   __shared__ int tmp[SCAN / 64 + 1];
   __shared__ float tops[SCAN / 64];
   int places = 0;
-  for (long long r0 = 0; r0 < rows; r0 += SCAN) {
-    const long long r = r0 + threadIdx.x;
-    const int64_t label = r < rows ? labels[r] : ignored;
-    const bool counts = label != ignored;
-    int total;
-    const int at = places + tt_block_excl_scan_n<SCAN>(counts ? 1 : 0, tmp, &total);
-    if (r < rows) w.at[r] = counts ? at : -1;
-    if (loss && r < rows && !counts) loss[r] = lse_out[r] = 0.f;
-    if (counts) {
+  constexpr int EACH = 8;  // rows of a thread at a time
+  for (long long r0 = 0; r0 < rows; r0 += SCAN * EACH) {
+    const long long r1 = r0 + threadIdx.x * EACH;
+    int64_t label[EACH];
+    int mine = 0;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+      label[i] = r1 + i < rows ? labels[r1 + i] : ignored;
+      mine += label[i] != ignored;
+    }
+    int total, at = places + tt_block_excl_scan_n<SCAN>(mine, tmp, &total);
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+      const long long r = r1 + i;
+      const bool counts = label[i] != ignored;
+      if (r < rows) w.at[r] = counts ? at : -1;
+      if (loss && r < rows && !counts) loss[r] = lse_out[r] = 0.f;
+      if (!counts) continue;
       w.of[at] = (int32_t)r;
-      w.label[at] = label >= 0 && label < classes ? (int32_t)label : -1;
+      w.label[at] = label[i] >= 0 && label[i] < classes ? (int32_t)label[i] : -1;
       // (short rows multiply it by log2 e: beyond 2^127 it counts as NaN)
       if (lse) w.lse[at] = !negative ? lse[r] : fabsf(lse[r]) < 0x1p127f ? -lse[r] : NAN;
+      ++at;
     }
     places += total;
   }
@@ -39,10 +49,13 @@ __global__ void __launch_bounds__(SCAN) k_loss_rows(const int64_t *labels, long 
   if (!lse) return;
   __syncthreads();
   const float all = reduce == TT_REDUCE_NONE ? 0.f : reduce == TT_REDUCE_MEAN && places > 0 ? grad[0] / (float)places : grad[0];
-  float top = 0.f;  // the largest finite share
-  for (int i = threadIdx.x; i < places; i += SCAN) {
-    const float g = fabsf(reduce == TT_REDUCE_NONE ? grad[w.of[i]] : all);
-    top = g < INFINITY && g > top ? g : top;
+  float top = 0.f;  // the largest finite share: what fp16 asks for
+  if (half && reduce == TT_REDUCE_NONE) {
+#pragma unroll 4
+    for (int i = threadIdx.x; i < places; i += SCAN) {
+      const float g = fabsf(grad[w.of[i]]);
+      top = g < INFINITY && g > top ? g : top;
+    }
   }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
@@ -63,6 +76,7 @@ __global__ void __launch_bounds__(SCAN) k_loss_rows(const int64_t *labels, long 
   }
   if (apart && !own) back = all * 0x1p-13f;
   if (threadIdx.x == 0) w.back[0] = back;
+#pragma unroll 4
   for (int i = threadIdx.x; i < places; i += SCAN) {
     const float share = own ? grad[w.of[i]] : all;
     w.share[i] = share;
@@ -121,6 +135,7 @@ __global__ void __launch_bounds__(TT_BLOCK) k_loss_fold(const float2 *__restrict
 __global__ void __launch_bounds__(SCAN) k_loss_sum(const float *each, long long rows, Rows w, int reduce, float *loss) {
   __shared__ double sums[SCAN / 64];
   double s = 0;
+#pragma unroll 8
   for (long long r = threadIdx.x; r < rows; r += SCAN) s += (double)each[r];
   s = wave_sum64(s);
   if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = s;

@@ -205,7 +205,9 @@ def test_expert_rows_and_combine(tt, rows, k, num, n, dtype, pad, shift):
 # ---- the loss
 BIG = [(1, 128, 1000, F32, True, "mean", 0, 0, 0), (300, 128, 2000, F32, True, "mean", 7, 0, 0), (257, 64, 5001, BF16, True, "none", 30, 0, 0),
        (513, 128, 20001, BF16, True, "mean", 50, 0, 0), (500, 136, 4099, F16, False, "none", 3, 8, 0), (700, 479, 1501, BF16, True, "sum", 1, 0, 1),
-       (2048, 256, 6000, BF16, False, "mean", 200, 0, 0), (1500, 72, 9001, F16, True, "mean", 0, 0, 0), (2, 1024, 3000, BF16, True, "mean", 0, 0, 0)]
+       (2048, 256, 6000, BF16, False, "mean", 200, 0, 0), (1500, 72, 9001, F16, True, "mean", 0, 0, 0), (2, 1024, 3000, BF16, True, "mean", 0, 0, 0),
+       (9001, 16, 40, F32, True, "none", 4000, 0, 0), (3000, 128, 5001, F32, False, "mean", 11, 0, 0), (700, 256, 9000, F32, True, "mean", 5, 0, 0),
+       (200, 520, 3001, F16, True, "sum", 9, 0, 0)]
 
 
 @pytest.mark.parametrize("rows,dim,classes,dtype,biased,reduction,ignored,pad,shift", LOSSES + BIG)
@@ -239,6 +241,39 @@ def test_cross_entropy(tt, rows, dim, classes, dtype, biased, reduction, ignored
     assert not grads[0][skip.cuda()].any()
     again = torch.autograd.grad(call(), leaves, grad.cuda())
     assert all(torch.equal(p, q) for p, q in zip(grads, again))
+
+
+@pytest.mark.parametrize("dim", [64, 100, 200])
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+def test_gradients_of_nearly_sure_rows(tt, dim, dtype):
+    """Rows whose label has almost all of the probability: what is left of the one after the label's share is taken off before anything is rounded to 16
+    bits, so the gradients keep their relative precision (against 64 bits, within the bounds that `loss64` derives)."""
+    gen = torch.Generator().manual_seed(dim)
+    w = randn(gen, 500, dim, std=dim ** -0.5, dtype=dtype)
+    labels = torch.randint(0, 500, (200,), generator=gen)
+    x = (w[labels].double() / w[labels].double().norm(dim=1, keepdim=True) ** 2 * 13).to(dtype)  # the label's logit about 13, others of deviation 1
+    grad = torch.tensor(1.0 if dtype != F16 else 200.0)
+    want = ref.loss64(x, w, labels, grad=grad)
+    p = torch.exp(-want["loss"][0])
+    assert 0.9 < float(p) < 1
+    leaves = [put(x).requires_grad_(), put(w).requires_grad_()]
+    loss = tt.tt_cross_entropy(leaves[0], leaves[1], labels.cuda())
+    check(loss, want["loss"], "loss")
+    for got, name in zip(torch.autograd.grad(loss, leaves, grad.cuda()), ("dx", "dw")):
+        check(got, want[name], name)
+        off = (got.double().cpu() - want[name][0]).norm() / want[name][0].norm()
+        assert off < 3 * torch.finfo(dtype).eps + 2e-6, (name, float(off))
+
+
+def test_no_rows(tt):
+    """An empty batch through all of them, with gradients."""
+    m = tt.TTExperts(16, 24, 8, 2)
+    head = tt.TTSoftmaxLoss(16, 50, bias=True)
+    x = torch.empty(0, 16, device="cuda").requires_grad_()
+    loss = head(m(x), torch.empty(0, dtype=torch.int64, device="cuda"))
+    loss.backward()
+    assert loss == 0 and x.grad.shape == (0, 16)
+    assert all(p.grad is not None and not p.grad.any() for p in list(m.parameters()) + list(head.parameters()))
 
 
 def test_cross_entropy_of_frozen_parts(tt):

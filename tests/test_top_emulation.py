@@ -388,6 +388,7 @@ LOSSES = [
     (150, 136, 450, F32, True, "sum", 4, 0, 0),
     (66, 20, 40, F32, False, "none", 60, 1, 0),
     (9, 8, 20, F32, True, "mean", 9, 0, 0),       # no row counts
+    (9, 8, 2000, BF16, True, "mean", 9, 0, 0),
     (300, 72, 264, F16, True, "sum", 3, 0, 0),
     (0, 8, 20, F32, True, "mean", 0, 0, 0),
 ]

@@ -647,8 +647,9 @@ tt_status tt_expert_combine_backward(const tt_deal *op, const void *y, const int
  * powers of two that keep it in the range.  fp32 products are of three bf16 parts, as in tt_dense; those of rows of up to 128 elements do
  * without the fp32 instruction where parts cannot do (numbers below 2^-100 have fewer bits, numbers that bf16 cannot hold give NaN, and a
  * row with a logit beyond 2^127 has NaN gradients).  Losses and lse are float whatever the dtype.
- *   labels DEVICE int64[rows];  lse DEVICE float[rows]: log of the sum, 0 in rows that do not count; written by the
- *   forward (not NULL), read by the backward
+ *   labels DEVICE int64[rows];  stats DEVICE float[rows][2]: the log of the sum and the loss of each row, 0 in rows that do not
+ *   count; written by the forward (not NULL), read by the backward (which forms the label's softmax - 1 from the loss: its
+ *   relative precision lasts where a row is nearly sure)
  *   workspace DEVICE, 256-byte aligned, tt_cross_entropy_workspace_bytes(op, backward) (0 on invalid arguments)
  */
 typedef enum { TT_REDUCE_NONE = 0, TT_REDUCE_SUM = 1, TT_REDUCE_MEAN = 2 } tt_reduce;
@@ -664,9 +665,9 @@ typedef struct {
   int64_t ld_dx;        /* ... of dx; 0: dim                                                     */
 } tt_loss;
 size_t tt_cross_entropy_workspace_bytes(const tt_loss *op, int backward);
-tt_status tt_cross_entropy_forward(const tt_loss *op, const void *x, const void *w, const void *bias, const int64_t *labels, float *loss, float *lse,
+tt_status tt_cross_entropy_forward(const tt_loss *op, const void *x, const void *w, const void *bias, const int64_t *labels, float *loss, float *stats,
                                    void *workspace, size_t workspace_bytes, void *stream);
-tt_status tt_cross_entropy_backward(const tt_loss *op, const void *x, const void *w, const void *bias, const int64_t *labels, const float *lse,
+tt_status tt_cross_entropy_backward(const tt_loss *op, const void *x, const void *w, const void *bias, const int64_t *labels, const float *stats,
                                     const float *grad_loss, void *dx, void *dw, void *dbias, void *workspace, size_t workspace_bytes,
                                     void *stream);
 

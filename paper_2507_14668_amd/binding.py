@@ -1178,28 +1178,28 @@ def _loss_workspace(lib, op, backward, workspace, on, at):
 
 
 def tt_cross_entropy_forward(x, w, labels, bias=None, ignore_index=-100, reduction="mean", workspace=None, stream=None):
-    """`(loss, lse)` of x [rows, dim] against the classes of w [classes, dim] (and bias [classes]): float32, [rows] without a
+    """`(loss, stats)` of x [rows, dim] against the classes of w [classes, dim] (and bias [classes]): float32, [rows] without a
     reduction, else one number; labels int64 [rows].  Rows labelled ignore_index have a loss of zero and are not counted by "mean" (0
-    if there is no other).  lse [rows] is what the backward takes."""
+    if there is no other).  stats [rows, 2] (the log of the sum and the loss of each row) is what the backward takes."""
     op, dtype, at, p_w, p_b, p_l = _loss_op(x, w, labels, bias, ignore_index, reduction)
     on = _On(at, stream)
     loss = on.empty((op.rows,) if reduction == "none" else (), torch.float32)
-    lse = on.empty((op.rows,), torch.float32)
+    stats = on.empty((op.rows, 2), torch.float32)
     lib = load_library()
     workspace, p_work, size = _loss_workspace(lib, op, 0, workspace, on, at)
     with on as s:
-        st = lib.tt_cross_entropy_forward(ctypes.byref(op), x.data_ptr(), p_w, p_b, p_l, loss.data_ptr(), lse.data_ptr(), p_work, size, s)
+        st = lib.tt_cross_entropy_forward(ctypes.byref(op), x.data_ptr(), p_w, p_b, p_l, loss.data_ptr(), stats.data_ptr(), p_work, size, s)
     if st != TT_OK:
         raise TTError(st, "tt_cross_entropy_forward")
-    return loss, lse
+    return loss, stats
 
 
-def tt_cross_entropy_backward(x, w, labels, lse, grad_loss, bias=None, ignore_index=-100, reduction="mean", needs=(True, True, True), workspace=None,
+def tt_cross_entropy_backward(x, w, labels, stats, grad_loss, bias=None, ignore_index=-100, reduction="mean", needs=(True, True, True), workspace=None,
                               stream=None):
     """Gradients `(dx, dw, dbias)` of `tt_cross_entropy_forward` from grad_loss (float32, of the loss's shape)."""
     op, dtype, at, p_w, p_b, p_l = _loss_op(x, w, labels, bias, ignore_index, reduction)
     on = _On(at, stream)
-    p_lse = _packed(lse, "lse", torch.float32, at, (op.rows,))
+    p_s = _packed(stats, "stats", torch.float32, at, (op.rows, 2))
     p_g = _packed(grad_loss, "grad_loss", torch.float32, at, (op.rows,) if reduction == "none" else ())
     dx = on.empty(x.shape, dtype) if needs[0] else None
     dw = on.empty(w.shape, dtype) if needs[1] else None
@@ -1209,7 +1209,7 @@ def tt_cross_entropy_backward(x, w, labels, lse, grad_loss, bias=None, ignore_in
     lib = load_library()
     workspace, p_work, size = _loss_workspace(lib, op, 1, workspace, on, at)
     with on as s:
-        st = lib.tt_cross_entropy_backward(ctypes.byref(op), x.data_ptr(), p_w, p_b, p_l, p_lse, p_g, _null(dx), _null(dw), _null(db), p_work, size, s)
+        st = lib.tt_cross_entropy_backward(ctypes.byref(op), x.data_ptr(), p_w, p_b, p_l, p_s, p_g, _null(dx), _null(dw), _null(db), p_work, size, s)
     if st != TT_OK:
         raise TTError(st, "tt_cross_entropy_backward")
     return dx, dw, db

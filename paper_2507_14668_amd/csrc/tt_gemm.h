@@ -18,7 +18,7 @@
 // row-contiguous B, SCALED with both row-contiguous.
 #define TT_GEMM_PLAIN 0
 #define TT_GEMM_STATS 1    // nothing is stored but, of each row's columns in the tile, the largest z and the sum of exp(z - it), and the label's z
-#define TT_GEMM_SOFTMAX 2  // out = (exp(z - lse[m]) - (n is the label)) * row_grad[m], zeros in columns N .. n_padded - 1
+#define TT_GEMM_SOFTMAX 2  // out = (n is the label ? hot[m] : exp(z - lse[m])) * row_grad[m], zeros in columns N .. n_padded - 1
 #define TT_GEMM_ACC 3      // acc[m][n] = z, plus what is there if acc_add, in fp32
 #define TT_GEMM_SCALED 4   // out and rowsum times *scale
 
@@ -50,6 +50,7 @@ struct TTGemm {
   const int32_t *labels;       // STATS, SOFTMAX: [M], first + the label's column; others are no column's
   int first;
   const float *lse, *row_grad; // SOFTMAX: [M]
+  const float *hot;            // SOFTMAX: [M], the label's softmax less one
   int n_padded;                // SOFTMAX
   float *acc;                  // ACC: [batch][M][N], fp32
   int acc_add;

@@ -402,9 +402,11 @@ template <class T> __device__ __forceinline__ void finish_softmax(const TTGemm &
   const float lse = g.lse[m], grad = g.row_grad[m];
   const int label = g.labels[m] - g.first - n, valid = g.N - n;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float p = __expf(fmaf(g.alpha, v[i], bias[i]) - lse);
-    v[i] = i < valid ? grad * (i == label ? p - 1.f : p) : 0.f;
+  for (int i = 0; i < 8; ++i) v[i] = i < valid ? grad * __expf(fmaf(g.alpha, v[i], bias[i]) - lse) : 0.f;
+  if ((unsigned)label < 8u) {
+    const float hot = grad * g.hot[m];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = i == label ? hot : v[i];
   }
   store_n<T, 8>((T *)g.out + (long long)m * g.ldo + n, g.n_padded - n, v);
 }

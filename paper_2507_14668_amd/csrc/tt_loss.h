@@ -12,6 +12,7 @@ struct TTLossRows {
   float *lse;               // [rows] of each place: backward.  (Short rows: of, label, lse and weight up to whole steps.)
   float *share;             // [rows]: what the loss's gradient gives each place
   float *weight;            // [rows]: what G is formed with instead of it
+  float *hot;               // [rows]: the label's softmax less one
   float *back;              // [1]: what that is multiplied by at the end
   int64_t *offsets;         // {0, places}
 };
@@ -35,6 +36,7 @@ int ttk_narrow_padded(int dim);
 size_t ttk_narrow_stats_bytes(const TTNarrow &n);  // (sizes alone are looked at)
 size_t ttk_narrow_parts_bytes(const TTNarrow &n);
 tt_status ttk_narrow_take(const TTNarrow &n, hipStream_t s);  // writes x, copy and starts: before the others
-tt_status ttk_narrow_stats(const TTNarrow &n, float *stats, float *loss, float *lse, hipStream_t s);
+// picked: [rows]; each: the rows' pairs (lse, loss); loss: the losses again, or null
+tt_status ttk_narrow_stats(const TTNarrow &n, float *stats, float *picked, float *each, float *loss, hipStream_t s);
 tt_status ttk_narrow_dx(const TTNarrow &n, float *parts, void *dx, long long ld_dx, hipStream_t s);
 tt_status ttk_narrow_dw(const TTNarrow &n, bool shares, float *parts, void *dw, void *dbias, hipStream_t s);

@@ -9,10 +9,10 @@ using namespace ttg;
 
 typedef TTLossRows Rows;
 
-// One workgroup: places in the order of the rows.  In the backward also each place's lse and share of the loss's gradient.
+// One workgroup: places in the order of the rows.  In the backward also each place's lse, hot and share of the loss's gradient.
 constexpr int SCAN = 512;
-__global__ void __launch_bounds__(SCAN) k_loss_rows(const int64_t *labels, long long rows, int classes, long long ignored, int reduce, const float *lse,
-                                                    const float *grad, int apart, int half, int negative, float *loss, float *lse_out, Rows w) {
+__global__ void __launch_bounds__(SCAN) k_loss_rows(const int64_t *labels, long long rows, int classes, long long ignored, int reduce, const float2 *of_rows,
+                                                    const float *grad, int apart, int half, int negative, float *loss, float2 *zeros, Rows w) {
   __shared__ int tmp[SCAN / 64 + 1];
   __shared__ float tops[SCAN / 64];
   int places = 0;
@@ -32,12 +32,19 @@ __global__ void __launch_bounds__(SCAN) k_loss_rows(const int64_t *labels, long 
       const long long r = r1 + i;
       const bool counts = label[i] != ignored;
       if (r < rows) w.at[r] = counts ? at : -1;
-      if (loss && r < rows && !counts) loss[r] = lse_out[r] = 0.f;
+      if (zeros && r < rows && !counts) {
+        zeros[r] = float2{0.f, 0.f};
+        if (loss) loss[r] = 0.f;
+      }
       if (!counts) continue;
       w.of[at] = (int32_t)r;
       w.label[at] = label[i] >= 0 && label[i] < classes ? (int32_t)label[i] : -1;
-      // (short rows multiply it by log2 e: beyond 2^127 it counts as NaN)
-      if (lse) w.lse[at] = !negative ? lse[r] : fabsf(lse[r]) < 0x1p127f ? -lse[r] : NAN;
+      if (of_rows) {
+        const float2 s = of_rows[r];
+        // (short rows multiply lse by log2 e: beyond 2^127 it counts as NaN)
+        w.lse[at] = !negative ? s.x : fabsf(s.x) < 0x1p127f ? -s.x : NAN;
+        w.hot[at] = expm1f(-s.y);
+      }
       ++at;
     }
     places += total;
@@ -46,7 +53,7 @@ __global__ void __launch_bounds__(SCAN) k_loss_rows(const int64_t *labels, long 
     w.offsets[0] = 0;
     w.offsets[1] = places;
   }
-  if (!lse) return;
+  if (!of_rows) return;
   __syncthreads();
   const float all = reduce == TT_REDUCE_NONE ? 0.f : reduce == TT_REDUCE_MEAN && places > 0 ? grad[0] / (float)places : grad[0];
   float top = 0.f;  // the largest finite share: what fp16 asks for
@@ -106,7 +113,7 @@ template <class T> __global__ void __launch_bounds__(TT_BLOCK) k_loss_gather(con
 // A piece's tiles into each place's running pair (largest logit, sum of exp(logit - it)), sixteen places a workgroup and sixteen runs of the tiles;
 // of the last piece the row's lse and loss.
 __global__ void __launch_bounds__(TT_BLOCK) k_loss_fold(const float2 *__restrict__ stats, int tiles, long long rows, int first, int last, Rows w, float2 *run,
-                                                        const float *picked, float *loss, float *lse) {
+                                                        const float *picked, float2 *each, float *loss) {
   __shared__ float2 part[TT_BLOCK];
   const int lane = threadIdx.x & 15, seg = threadIdx.x >> 4, per = (tiles + 15) / 16;
   const long long i = (long long)blockIdx.x * 16 + lane, places = w.offsets[1];
@@ -127,16 +134,17 @@ __global__ void __launch_bounds__(TT_BLOCK) k_loss_fold(const float2 *__restrict
   }
   const bool bad = w.label[i] < 0;
   const int r = w.of[i];
-  lse[r] = bad ? NAN : s.x + logf(s.y);
   // (the difference of the logits first: near a loss of zero lse less the label's logit would be lse's rounding)
-  loss[r] = bad ? NAN : (s.x - picked[i]) + logf(s.y);
+  const float more = logf(s.y);
+  each[r] = bad ? float2{NAN, NAN} : float2{s.x + more, (s.x - picked[i]) + more};
+  if (loss) loss[r] = each[r].y;
 }
 // One workgroup: the sum or the mean, in 64 bits.
-__global__ void __launch_bounds__(SCAN) k_loss_sum(const float *each, long long rows, Rows w, int reduce, float *loss) {
+__global__ void __launch_bounds__(SCAN) k_loss_sum(const float2 *each, long long rows, Rows w, int reduce, float *loss) {
   __shared__ double sums[SCAN / 64];
   double s = 0;
 #pragma unroll 8
-  for (long long r = threadIdx.x; r < rows; r += SCAN) s += (double)each[r];
+  for (long long r = threadIdx.x; r < rows; r += SCAN) s += (double)each[r].y;
   s = wave_sum64(s);
   if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = s;
   __syncthreads();
@@ -280,7 +288,7 @@ TTGemm of_dw(const tt_loss *op, int classes, long long ldg, bool column) {  // G
 }
 
 struct Scratch {
-  size_t of, at, label, lse, share, weight, back, offsets, x, stats, run, picked, each, grads, acc, column, pieces, parts, starts, copy, total;
+  size_t of, at, label, lse, share, weight, hot, back, offsets, x, stats, run, picked, grads, acc, column, pieces, parts, starts, copy, total;
 };
 Scratch scratch(const tt_loss *op, bool backward) {
   Scratch w = {};
@@ -312,12 +320,12 @@ Scratch scratch(const tt_loss *op, bool backward) {
     take(w.stats, narrow(op) ? ttk_narrow_stats_bytes(n) : (size_t)tt_ceil_div(piece, 64) * rows * 8);
     take(w.run, rows * 8);
     take(w.picked, rows * 4);
-    take(w.each, rows * 4);
     return w;
   }
   take(w.lse, whole * 4);
   take(w.share, rows * 4);
   take(w.weight, whole * 4);
+  take(w.hot, whole * 4);
   if (narrow(op)) {
     take(w.parts, ttk_narrow_parts_bytes(n));
     return w;
@@ -341,7 +349,7 @@ Scratch scratch(const tt_loss *op, bool backward) {
 }
 Rows rows_of(char *ws, const Scratch &w) {
   return TTLossRows{(int32_t *)(ws + w.of), (int32_t *)(ws + w.at), (int32_t *)(ws + w.label), (float *)(ws + w.lse), (float *)(ws + w.share), (float *)(ws + w.weight),
-              (float *)(ws + w.back), (int64_t *)(ws + w.offsets)};
+                    (float *)(ws + w.hot), (float *)(ws + w.back), (int64_t *)(ws + w.offsets)};
 }
 TTNarrow narrow_of(const tt_loss *op, const void *x, const void *w, const void *bias, char *ws, const Scratch &need) {
   const bool as_it_is = op->dtype != TT_F32 && op->dim == padded(op) && aligned(w, 16);
@@ -385,16 +393,16 @@ extern "C" size_t tt_cross_entropy_workspace_bytes(const tt_loss *op, int backwa
   return scratch(op, backward != 0).total;
 }
 
-extern "C" tt_status tt_cross_entropy_forward(const tt_loss *op, const void *x, const void *w, const void *bias, const int64_t *labels, float *loss, float *lse,
+extern "C" tt_status tt_cross_entropy_forward(const tt_loss *op, const void *x, const void *w, const void *bias, const int64_t *labels, float *loss, float *stats,
                                               void *workspace, size_t workspace_bytes, void *stream) {
   tt_status st = check(op);
   if (st != TT_OK) return st;
   const bool some = op->rows > 0, whole = op->reduce != TT_REDUCE_NONE;
   if (!some && !whole) return TT_OK;
   const size_t es = elem(op->dtype);
-  if (!loss || (some && (!x || !w || !labels || !lse))) return TT_ERR_INVALID_ARG;
-  const void *ptrs[6] = {x, w, bias, labels, loss, lse};
-  const size_t sizes[6] = {es, es, es, 8, 4, 4};
+  if (!loss || (some && (!x || !w || !labels || !stats))) return TT_ERR_INVALID_ARG;
+  const void *ptrs[6] = {x, w, bias, labels, loss, stats};
+  const size_t sizes[6] = {es, es, es, 8, 4, 8};
   for (int i = 0; i < 6; ++i) {
     if (!aligned(ptrs[i], sizes[i])) return TT_ERR_INVALID_ARG;
     for (int j = 4; j < 6; ++j)
@@ -407,8 +415,9 @@ extern "C" tt_status tt_cross_entropy_forward(const tt_loss *op, const void *x, 
   const Rows r = rows_of(ws, need);
   const long long rows = op->rows, ignored = op->ignore_index, piece = piece_of(op, false);
   const int classes = op->classes, reduce = op->reduce;
-  float *each = whole ? (float *)(ws + need.each) : loss;
-  hipLaunchKernelGGL(k_loss_rows, dim3(1), dim3(SCAN), 0, s, labels, rows, classes, ignored, reduce, (const float *)nullptr, (const float *)nullptr, 0, 0, 0, each, lse, r);
+  float2 *each = (float2 *)stats;
+  float *losses = whole ? nullptr : loss;
+  hipLaunchKernelGGL(k_loss_rows, dim3(1), dim3(SCAN), 0, s, labels, rows, classes, ignored, reduce, (const float2 *)nullptr, (const float *)nullptr, 0, 0, 0, losses, each, r);
   if ((st = tt_launch_status()) != TT_OK) return st;
   if (some) {
     if (!narrow(op) && (st = TT_BY_TYPE(gather, op->dtype, op, x, r, ws + need.x, s)) != TT_OK) return st;
@@ -416,7 +425,7 @@ extern "C" tt_status tt_cross_entropy_forward(const tt_loss *op, const void *x, 
     if (narrow(op)) {
       const TTNarrow n = narrow_of(op, x, w, bias, ws, need);
       if ((st = ttk_narrow_take(n, s)) != TT_OK) return st;
-      if ((st = ttk_narrow_stats(n, (float *)(ws + need.stats), each, lse, s)) != TT_OK) return st;
+      if ((st = ttk_narrow_stats(n, (float *)(ws + need.stats), (float *)(ws + need.picked), stats, losses, s)) != TT_OK) return st;
     }
     for (long long c = 0; c < classes && !narrow(op); c += piece) {
       const int n = (int)(classes - c < piece ? classes - c : piece);
@@ -436,14 +445,14 @@ extern "C" tt_status tt_cross_entropy_forward(const tt_loss *op, const void *x, 
       if ((st = ttk_gemm(g, nullptr, s)) != TT_OK) return st;
       const int tiles = tt_ceil_div(n, ttk_gemm_tile(g)), first = c == 0, last = c + n == classes;
       hipLaunchKernelGGL(k_loss_fold, dim3((unsigned)tt_ceil_div(rows, 16)), dim3(TT_BLOCK), 0, s, (const float2 *)g.stats, tiles, rows, first, last, r, run,
-                         (const float *)g.picked, each, lse);
+                         (const float *)g.picked, each, losses);
     }
   }
-  if (whole) hipLaunchKernelGGL(k_loss_sum, dim3(1), dim3(SCAN), 0, s, (const float *)each, rows, r, reduce, loss);
+  if (whole) hipLaunchKernelGGL(k_loss_sum, dim3(1), dim3(SCAN), 0, s, (const float2 *)each, rows, r, reduce, loss);
   return tt_launch_status();
 }
 
-extern "C" tt_status tt_cross_entropy_backward(const tt_loss *op, const void *x, const void *w, const void *bias, const int64_t *labels, const float *lse,
+extern "C" tt_status tt_cross_entropy_backward(const tt_loss *op, const void *x, const void *w, const void *bias, const int64_t *labels, const float *stats,
                                                const float *grad_loss, void *dx, void *dw, void *dbias, void *workspace, size_t workspace_bytes,
                                                void *stream) {
   tt_status st = check(op);
@@ -451,9 +460,9 @@ extern "C" tt_status tt_cross_entropy_backward(const tt_loss *op, const void *x,
   if (!dx && !dw && !dbias) return TT_OK;
   const bool some = op->rows > 0;
   const size_t es = elem(op->dtype);
-  if (some && (!x || !w || !labels || !lse || !grad_loss)) return TT_ERR_INVALID_ARG;
-  const void *ptrs[9] = {x, w, bias, labels, lse, grad_loss, dx, dw, dbias};
-  const size_t sizes[9] = {es, es, es, 8, 4, 4, es, es, es};
+  if (some && (!x || !w || !labels || !stats || !grad_loss)) return TT_ERR_INVALID_ARG;
+  const void *ptrs[9] = {x, w, bias, labels, stats, grad_loss, dx, dw, dbias};
+  const size_t sizes[9] = {es, es, es, 8, 8, 4, es, es, es};
   for (int i = 0; i < 9; ++i) {
     if (!aligned(ptrs[i], sizes[i])) return TT_ERR_INVALID_ARG;
     for (int j = 6; j < 9; ++j)
@@ -470,7 +479,7 @@ extern "C" tt_status tt_cross_entropy_backward(const tt_loss *op, const void *x,
   const Rows r = rows_of(ws, need);
   const long long rows = op->rows, ignored = op->ignore_index, piece = piece_of(op, true);
   const int classes = op->classes, reduce = op->reduce, apart = op->dtype != TT_F32 || narrow(op), half = op->dtype == TT_F16, negative = narrow(op);
-  hipLaunchKernelGGL(k_loss_rows, dim3(1), dim3(SCAN), 0, s, labels, rows, classes, ignored, reduce, lse, grad_loss, apart, half, negative, (float *)nullptr, (float *)nullptr, r);
+  hipLaunchKernelGGL(k_loss_rows, dim3(1), dim3(SCAN), 0, s, labels, rows, classes, ignored, reduce, (const float2 *)stats, grad_loss, apart, half, negative, (float *)nullptr, (float2 *)nullptr, r);
   if ((st = tt_launch_status()) != TT_OK) return st;
   if (!narrow(op) && (st = TT_BY_TYPE(gather, op->dtype, op, x, r, ws + need.x, s)) != TT_OK) return st;
   if (narrow(op)) {
@@ -496,6 +505,7 @@ extern "C" tt_status tt_cross_entropy_backward(const tt_loss *op, const void *x,
     g.labels = r.label;
     g.lse = r.lse;
     g.row_grad = r.weight;
+    g.hot = r.hot;
     g.first = (int)c;
     if ((st = ttk_gemm(g, nullptr, s)) != TT_OK) return st;
     if (dx) {

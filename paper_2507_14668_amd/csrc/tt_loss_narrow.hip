@@ -52,7 +52,7 @@ inline long long grid_for(long long held, long long streamed, const Sizes &z) {
 __host__ __device__ constexpr int tile_of(int KP, Mode mode, int parts) { return 16 * held_tiles(KP, mode, parts) * WAVES; }
 // A step takes 0.4 us of a wavefront, of fp32 1.5; the statistics' parts are eight bytes a row.
 __host__ __device__ constexpr Sizes sizes_of(int KP, Mode mode, int parts) {
-  return Sizes{tile_of(KP, mode, parts), 256 * (mode == STATS && parts == 1 ? 4 : 2), parts == 3 ? (mode == STATS ? 2 : 3) : mode == STATS ? 4 : 8};
+  return Sizes{tile_of(KP, mode, parts), 256 * (mode == STATS && parts == 1 ? 3 : 2), parts == 3 ? (mode == STATS ? 2 : 3) : mode == STATS ? 4 : 8};
 }
 
 struct Args {
@@ -61,6 +61,8 @@ struct Args {
   const float *constants;    // of held vectors
   const float *weight;       // CLASSES with shares: of the rows, whole steps
   const int32_t *label;      // of the rows, whole steps
+  const float *hot;          // of the rows: the label's softmax less one
+  float *picked;             // STATS: of the rows
   const int64_t *offsets;
   void *out, *sums;          // CLASSES of one run: dW, dbias
   const float *back;
@@ -128,11 +130,13 @@ template <int KP, Mode MODE, bool SHARES, int PARTS> struct Fetcher {
 // A step, from `now`, while the next one (`ahead`; behind the last: none) is on its way to `next`.  (The buffers are separate to the compiler,
 // which else has every read wait for the loads.)
 // hit: a label of the rows is among the classes here, which few steps have; one branch, since what is on its two sides is not
-// interleaved.  `label`: ROWS of the held rows, less the step's first class; CLASSES lane l's is row l's, less the first held class.
-// The one is taken off P before that is rounded: where a row is nearly sure of its label their difference is all that is left.
+// interleaved.  `label`: of the held rows, less the step's first class; CLASSES lane l's is row l's, less the first held class.
+// STATS gives the label's logit out there.  The others have the label's softmax less one, which the loss says to its last bits (`hot`, of the held rows or, CLASSES,
+// of the step's): where a row is nearly sure of its label, exp(z - lse) - 1 would be the rounding of lse.
 template <class T, int KP, Mode MODE, bool SHARES, int PARTS, int H, int DO>
 __device__ __forceinline__ void step_of(const char *__restrict__ now, char *__restrict__ next, const Fetcher<KP, MODE, SHARES, PARTS> &fetcher, long long ahead,
-                                        long long end, bool hit, const int (&label)[MODE == ROWS ? H : 1], const u16x8 (&held)[H][KP / 32][PARTS], float (&constant)[H], f32x4 (&acc)[DO][H], float (&sums)[H]) {
+                                        long long end, bool hit, const int (&label)[MODE == CLASSES ? 1 : H], const float *hot, float *picked,
+                                        const u16x8 (&held)[H][KP / 32][PARTS], float (&constant)[H], f32x4 (&acc)[DO][H], float (&sums)[H]) {
   constexpr int KS = KP / 32, D = KP / 16;
   constexpr bool OUT = MODE != STATS, CLASS = MODE == CLASSES;
   const int lane = threadIdx.x & 63, q = lane >> 4, j = lane & 15;
@@ -157,6 +161,13 @@ __device__ __forceinline__ void step_of(const char *__restrict__ now, char *__re
           for (int x = 0; x < H; ++x) S[half][x] = mma(T(), f[d - p], held[x][s][p], s || d != PARTS - 1 || p ? S[half][x] : from);
     }
     if constexpr (MODE == STATS) {
+      if (hit) {
+#pragma unroll
+        for (int x = 0; x < H; ++x)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (label[x] == 16 * half + 4 * q + i) picked[16 * x + j] = S[half][x][i];
+      }
 #pragma unroll
       for (int x = 0; x < H; ++x) {
         const float top = fmaxf(fmaxf(S[half][x][0], S[half][x][1]), fmaxf(S[half][x][2], S[half][x][3]));
@@ -191,8 +202,8 @@ __device__ __forceinline__ void step_of(const char *__restrict__ now, char *__re
 #pragma unroll
           for (int i = 0; i < 4; ++i) {
             const int streamed = 16 * half + 4 * q + i;
-            const bool here = CLASS ? __shfl(label[0], streamed, 64) == 16 * x + j : label[CLASS ? 0 : x] == streamed;
-            S[half][x][i] -= here ? (SHARES ? 1.f : 8192.f) : 0.f;
+            if (CLASS ? __shfl(label[0], streamed, 64) == 16 * x + j : label[CLASS ? 0 : x] == streamed)
+              S[half][x][i] = hot[CLASS ? streamed : 16 * x + j] * (SHARES ? 1.f : 8192.f);
           }
     }
     u16x8 P[H][PARTS];
@@ -249,7 +260,7 @@ __device__ __forceinline__ float2 join_runs(float2 a, float2 b) {
 }
 
 // T: of the products; O: of dW and dbias
-template <class T, class O, int KP, Mode MODE, bool SHARES> __global__ void __launch_bounds__(THREADS, 2) k_narrow(Args a) {
+template <class T, class O, int KP, Mode MODE, bool SHARES> __global__ void __launch_bounds__(THREADS, MODE == STATS && sizeof(O) == 2 ? 3 : 2) k_narrow(Args a) {
   constexpr int PARTS = sizeof(O) == 4 ? 3 : 1, KS = KP / 32, H = held_tiles(KP, MODE, PARTS), HELD = 16 * H, D = KP / 16;
   constexpr bool OUT = MODE != STATS, CLASS = MODE == CLASSES;
   constexpr int BYTES = step_bytes<KP, PARTS>(), GIVE = CLASS ? WAVES * 16 * (KP + 8) * 2 : 0;  // two steps, or what is given out through it
@@ -284,8 +295,8 @@ template <class T, class O, int KP, Mode MODE, bool SHARES> __global__ void __la
   const Fetcher<KP, MODE, SHARES, PARTS> fetcher = {(const unsigned short *)a.streamed, a.streamed_plane, a.starts, a.weight, streamed_count, row, wave, lane,
                                                 ((threadIdx.x % (KP / 8)) ^ spread<KP>(row & 15)) * 8};
   // Labels are a step ahead of their use, in a register: of the held rows less the first class, or of the streamed rows less the first held class.
-  int label[MODE == ROWS ? H : 1] = {}, label_next = 0;
-  if constexpr (MODE == ROWS) {
+  int label[CLASS ? 1 : H] = {}, label_next = 0;
+  if constexpr (!CLASS) {
 #pragma unroll
     for (int x = 0; x < H; ++x) label[x] = h0 + 16 * x + j < held_count ? a.label[h0 + 16 * x + j] - (int)s0 : -1;
   }
@@ -298,7 +309,7 @@ template <class T, class O, int KP, Mode MODE, bool SHARES> __global__ void __la
   for (long long t = s0; t < s1; t += STEP, b ^= 1) {
     __syncthreads();  // this step has landed, everyone's part of it, and nobody reads the other buffer any more
     bool hit = false;
-    if constexpr (MODE == ROWS) {
+    if constexpr (!CLASS) {
 #pragma unroll
       for (int x = 0; x < H; ++x) hit |= (unsigned)label[x] < (unsigned)STEP;
     }
@@ -307,8 +318,8 @@ template <class T, class O, int KP, Mode MODE, bool SHARES> __global__ void __la
       hit = (unsigned)label[0] < (unsigned)HELD;
       if (t + STEP < s1) label_next = a.label[t + STEP + (lane & 31)];
     }
-    step_of<T, KP, MODE, SHARES, PARTS>(lds + b * BYTES, lds + (b ^ 1) * BYTES, fetcher, t + STEP, s1, OUT && __ballot(hit) != 0, label, held, constant, acc, sums);
-    if constexpr (MODE == ROWS) {
+    step_of<T, KP, MODE, SHARES, PARTS>(lds + b * BYTES, lds + (b ^ 1) * BYTES, fetcher, t + STEP, s1, __ballot(hit) != 0, label, CLASS ? a.hot + t : a.hot + h0, a.picked + h0, held, constant, acc, sums);
+    if constexpr (!CLASS) {
 #pragma unroll
       for (int x = 0; x < H; ++x) label[x] -= STEP;
     }
@@ -399,35 +410,26 @@ template <class T, class O, int KP, Mode MODE, bool SHARES> __global__ void __la
   }
 }
 
-// Each place's statistics of all runs together, the label's logit as a product of its own, and what the row has of it: a wavefront a place.
-template <class T> __global__ void __launch_bounds__(TT_BLOCK) k_narrow_fold(TTNarrow n, const float2 *__restrict__ parts, Sizes z, float *loss, float *lse) {
+// Each place's statistics of all runs together, and what the row has of them: a wavefront a place.
+__global__ void __launch_bounds__(TT_BLOCK) k_narrow_fold(TTNarrow n, const float2 *__restrict__ parts, Sizes z, const float *picked, float2 *each, float *loss) {
   const int lane = threadIdx.x & 63;
   const long long i = (long long)blockIdx.x * (TT_BLOCK / 64) + (threadIdx.x >> 6), places = n.r.offsets[1];
   if (i >= places) return;
   const Cut cut = cut_of(places, n.classes, z);
-  const int tile = z.tile;
-  const long long block = i / tile;
-  const int label = n.r.label[i];
+  const long long block = i / z.tile;
   float2 s = {-INFINITY, 0.f};
-  for (int k = lane; k < cut.runs; k += 64) s = join_runs(s, parts[(k * (long long)cut.blocks + block) * tile + i % tile]);
-  float logit = 0.f;  // the label's
-  if (label >= 0) {
+  for (int k = lane; k < cut.runs; k += 64) s = join_runs(s, parts[(k * (long long)cut.blocks + block) * z.tile + i % z.tile]);
 #pragma unroll
-    for (int c = lane; c < 128; c += 64)
-      if (c < n.dim) logit = fmaf(to_f32(((const T *)n.of_call)[n.r.of[i] * n.ld + c]), to_f32(((const T *)n.w)[(long long)label * n.dim + c]), logit);
-  }
-#pragma unroll
-  for (int o = 1; o < 64; o *= 2) {
-    s = join_runs(s, float2{__shfl(s.x, lane ^ o, 64), __shfl(s.y, lane ^ o, 64)});
-    logit += __shfl(logit, lane ^ o, 64);
-  }
+  for (int o = 1; o < 64; o *= 2) s = join_runs(s, float2{__shfl(s.x, lane ^ o, 64), __shfl(s.y, lane ^ o, 64)});
   if (lane != 0) return;
-  logit += label >= 0 ? n.starts[label] : 0.f;
+  const bool bad = n.r.label[i] < 0;
   const int r = n.r.of[i];
-  const float more = log2f(s.y);
-  // (the label's logit is taken off before the sum's logarithm is added: near a loss of zero lse less that logit would be lse's rounding)
-  lse[r] = label < 0 ? NAN : s.x == INFINITY ? s.y : (s.x + more) * LN2;
-  loss[r] = label < 0 ? NAN : s.x == INFINITY ? s.y - logit : (fmaf(-logit, LOG2E, s.x) + more) * LN2;
+  const float more = log2f(s.y), logit = bad ? 0.f : picked[i];  // (of the same products: the largest logit less itself is zero)
+  float2 of = {(s.x + more) * LN2, (fmaf(-logit, LOG2E, s.x) + more) * LN2};
+  if (s.x == INFINITY) of = float2{s.y, s.y - logit};
+  if (bad) of = float2{NAN, NAN};
+  each[r] = of;
+  if (loss) loss[r] = of.y;
 }
 
 // The sums of the runs' parts of vectors, four columns a thread (the last four: the sums beside dW).  Up to eight runs: SEGMENTS vectors a workgroup, each by its own
@@ -539,6 +541,7 @@ Args args_of(const TTNarrow &n, bool classes) {
   a.constants = classes ? n.starts : n.r.lse;
   a.weight = n.r.weight;
   a.label = n.r.label;
+  a.hot = n.r.hot;
   a.offsets = n.r.offsets;
   a.back = n.r.back;
   a.held_plane = (classes ? (long long)n.classes : n.rows) * n.padded;
@@ -602,11 +605,6 @@ template <class T> tt_status take(const TTNarrow &n, bool classes, hipStream_t s
   hipLaunchKernelGGL(k_narrow_take<T>, dim3(grid_of(count * (to ? padded / 8 : 1))), dim3(TT_BLOCK), 0, s, from, ld, of, there, count, dim, to, padded, bias, starts);
   return tt_launch_status();
 }
-template <class T> tt_status fold(const TTNarrow &n, const float2 *parts, float *loss, float *lse, hipStream_t s) {
-  const Sizes z = sizes_for<STATS>(n);
-  hipLaunchKernelGGL(k_narrow_fold<T>, dim3((unsigned)tt_ceil_div(n.rows, TT_BLOCK / 64)), dim3(TT_BLOCK), 0, s, n, parts, z, loss, lse);
-  return tt_launch_status();
-}
 // Whether the classes are few enough for the rows to come in several runs (fewer rows that count never make it so).
 bool several(const TTNarrow &n) { return workgroups<CLASSES>(n) > tt_ceil_div(n.classes, tile_for<CLASSES>(n)); }
 
@@ -629,11 +627,16 @@ tt_status ttk_narrow_take(const TTNarrow &n, hipStream_t s) {
   const tt_status st = TT_BY_TYPE(take, n.dtype, n, false, s);
   return st == TT_OK ? TT_BY_TYPE(take, n.dtype, n, true, s) : st;
 }
-tt_status ttk_narrow_stats(const TTNarrow &n, float *stats, float *loss, float *lse, hipStream_t s) {
+tt_status ttk_narrow_stats(const TTNarrow &n, float *stats, float *picked, float *each, float *loss, hipStream_t s) {
   Args a = args_of(n, false);
   a.parts = stats;
+  a.picked = picked;
   const tt_status st = launch<STATS>(n, false, a, s);
-  return st == TT_OK ? TT_BY_TYPE(fold, n.dtype, n, (const float2 *)stats, loss, lse, s) : st;
+  if (st != TT_OK) return st;
+  const Sizes z = sizes_for<STATS>(n);
+  hipLaunchKernelGGL(k_narrow_fold, dim3((unsigned)tt_ceil_div(n.rows, TT_BLOCK / 64)), dim3(TT_BLOCK), 0, s, n, (const float2 *)stats, z, (const float *)picked,
+                     (float2 *)each, loss);
+  return tt_launch_status();
 }
 tt_status ttk_narrow_dx(const TTNarrow &n, float *parts, void *dx, long long ld_dx, hipStream_t s) {
   Args a = args_of(n, false);

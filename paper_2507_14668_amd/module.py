@@ -379,17 +379,17 @@ class TTExperts(torch.nn.Module):
 class _LossFunction(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, w, bias, labels, ignore_index, reduction):
-        loss, lse = binding.tt_cross_entropy_forward(x, w, labels, bias, ignore_index, reduction)
+        loss, stats = binding.tt_cross_entropy_forward(x, w, labels, bias, ignore_index, reduction)
         ctx.how = dict(ignore_index=ignore_index, reduction=reduction)
-        ctx.save_for_backward(x, w, bias, labels, lse)
+        ctx.save_for_backward(x, w, bias, labels, stats)
         return loss
 
     @staticmethod
     @_once
     def backward(ctx, grad_loss):
-        x, w, bias, labels, lse = ctx.saved_tensors
+        x, w, bias, labels, stats = ctx.saved_tensors
         need = ctx.needs_input_grad
-        grads = binding.tt_cross_entropy_backward(x, w, labels, lse, grad_loss.contiguous(), bias, needs=need[:3], **ctx.how)
+        grads = binding.tt_cross_entropy_backward(x, w, labels, stats, grad_loss.contiguous(), bias, needs=need[:3], **ctx.how)
         return (*grads, None, None, None)
 
 

@@ -411,7 +411,7 @@ def test_cross_entropy(loss_lib, rows, dim, classes, dtype, biased, reduction, i
     op = binding.CLoss(DT[dtype], binding.REDUCTIONS[reduction], rows, dim, classes, -7, dim + pad, dim + pad)
     gx, gw, gb, gl = place(x, dim + pad, shift), place(w, None, shift), place(b[None] if biased else None, None, shift), place(labels[None])
     gg = place(grad.reshape(1, -1))
-    loss, lse = Guarded((1, max(1, rows if reduction == "none" else 1)), F32), Guarded((1, max(1, rows)), F32)
+    loss, lse = Guarded((1, max(1, rows if reduction == "none" else 1)), F32), Guarded((max(1, rows), 2), F32)
     want = ref.loss64(torch.where(torch.isnan(x), torch.zeros_like(x), x), w, labels, b, -7, reduction, grad) if rows else None
     ws = Guarded((1, lib.tt_cross_entropy_workspace_bytes(ctypes.byref(op), 0)), torch.uint8)
     assert lib.tt_cross_entropy_forward(ctypes.byref(op), gx.ptr, gw.ptr, ptr(gb), gl.ptr, loss.ptr, lse.ptr, ws.ptr, ws.cols, None) == 0
@@ -421,7 +421,7 @@ def test_cross_entropy(loss_lib, rows, dim, classes, dtype, biased, reduction, i
     assert back(dx.ptr, dw.ptr, db.ptr) == 0
     if rows:
         ref.check(loss.t[0] if reduction == "none" else loss.t[0, 0], *want["loss"], "loss")
-        ref.check(lse.t[0], *want["lse"], "lse")
+        ref.check(lse.t[:, 0], *want["lse"], "lse")
         ref.check(dx.t, *want["dx"], "dx")
         ref.check(dw.t, *want["dw"], "dw")
         ref.check(db.t[0], *want["dbias"], "dbias")
@@ -444,7 +444,7 @@ def test_cross_entropy_bad_labels(lib):
     op = binding.CLoss(0, 0, 4, 8, 10, 3)
     ws = Guarded((1, max(lib.tt_cross_entropy_workspace_bytes(ctypes.byref(op), i) for i in (0, 1))), torch.uint8)
     for bad in (10, -1, 2 ** 40, -2 ** 63):
-        labels, loss, lse = torch.tensor([1, bad, 3, 9]), torch.empty(4), torch.empty(4)
+        labels, loss, lse = torch.tensor([1, bad, 3, 9]), torch.empty(4), torch.empty(4, 2)
         call = (ctypes.byref(op), x.data_ptr(), w.data_ptr(), None, labels.data_ptr())
         assert lib.tt_cross_entropy_forward(*call, loss.data_ptr(), lse.data_ptr(), ws.ptr, ws.cols, None) == 0
         want = ref.loss64(x[[0, 3]], w, labels[[0, 3]], ignore_index=3, reduction="none")
@@ -463,7 +463,7 @@ def test_cross_entropy_special_logits(lib):
     labels = torch.tensor([0, 1, 3, 0, 0, 1])
     op = binding.CLoss(0, 0, 6, 4, 4, -100)
     ws = Guarded((1, lib.tt_cross_entropy_workspace_bytes(ctypes.byref(op), 0)), torch.uint8)
-    loss, lse = torch.empty(6), torch.empty(6)
+    loss, lse = torch.empty(6), torch.empty(6, 2)
     assert lib.tt_cross_entropy_forward(ctypes.byref(op), x.data_ptr(), w.data_ptr(), b.data_ptr(), labels.data_ptr(), loss.data_ptr(), lse.data_ptr(), ws.ptr,
                                         ws.cols, None) == 0
     # a logit to units of log 2 and back is two constants and two products, each off by half a step of 2^-23, and the logarithm of a sum near
@@ -478,7 +478,7 @@ def test_cross_entropy_special_logits(lib):
 
 def test_cross_entropy_refusals(lib):
     from paper_2507_14668_amd import binding
-    x, w, b, lab, loss, lse = torch.zeros(4, 8), torch.zeros(10, 8), torch.zeros(10), torch.zeros(4, dtype=torch.int64), torch.zeros(4), torch.zeros(4)
+    x, w, b, lab, loss, lse = torch.zeros(4, 8), torch.zeros(10, 8), torch.zeros(10), torch.zeros(4, dtype=torch.int64), torch.zeros(4), torch.zeros(4, 2)
     ws = Guarded((1, 1 << 20), torch.uint8)
     p = lambda v: v if v is None or isinstance(v, int) else v.data_ptr()
     inval, shape, work = binding.TT_ERR_INVALID_ARG, binding.TT_ERR_SHAPE, binding.TT_ERR_WORKSPACE

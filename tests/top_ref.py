@@ -62,6 +62,7 @@ def scores64(logits, scores):
 
 def route64(logits, k, bias=None, scores="softmax", groups=1, top_groups=None, renormalize=False, scale=1.0):
     """(weights float64, experts), one row after the other."""
+    logits, bias = logits.detach(), None if bias is None else bias.detach()
     rows, num = logits.shape
     top_groups = groups if top_groups is None else top_groups
     s = scores64(logits, scores)

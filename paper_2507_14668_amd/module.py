@@ -24,7 +24,8 @@ product with bias, activation and residual in one kernel, and in a fused module 
 the differentiable call, `TTOrthoSGD` the optimizer whose updates of cores and dense weights are orthogonalised.
 
 What a model puts on top of the pooled rows: `tt_layer_norm` (`TTLayerNorm`), `tt_route`, `tt_expert_rows` and `tt_expert_combine`
-around products grouped by expert (`TTExperts`), and `tt_cross_entropy` against a catalogue (`TTSoftmaxLoss`).
+around products grouped by expert (`TTExperts`), and `tt_cross_entropy` against a catalogue (`TTSoftmaxLoss`).  What `tt_dense`
+says of backward passes that are captured into a graph holds for their gradients too.
 
 `TTFusedEmbeddingBags` holds SEVERAL tables of equal column factors and ranks as one fused TT table
 (cores side by side along the row-factor axis) and serves all of them with one reorder, one forward
@@ -346,7 +347,8 @@ class TTExperts(torch.nn.Module):
     scores, groups, top_groups, renormalize, scale   as in `tt_route`
     balance   a buffer that is added to the scores for choosing (zeros; a training loop may move it, it has no gradient)
     norm, residual   layer norm before the router and the experts; the row itself added to the result
-    forward(x, mask=None): x [rows, features]; rows where mask (bool [rows]) is False go to no expert.
+    forward(x, mask=None): x [rows, features]; rows where mask (bool [rows]) is False go to no expert, and no parameter's gradient
+    has anything of them, whatever they hold.
     """
 
     def __init__(self, features: int, hidden: int, experts: int, choices: int, activation: str = "silu", scores: str = "softmax", groups: int = 1,
@@ -364,7 +366,8 @@ class TTExperts(torch.nn.Module):
         self.register_buffer("balance", torch.zeros(experts, dtype=torch.float32, device=device) if balance else None)
 
     def forward(self, x, mask=None):
-        h = x if self.norm is None else self.norm(x)
+        h = x if mask is None else x.masked_fill(~mask[:, None], 0.0)  # (a zero gradient times a NaN would be one)
+        h = h if self.norm is None else self.norm(h)
         logits = self.router(h)
         if mask is not None:
             logits = logits.masked_fill(~mask[:, None], -math.inf)

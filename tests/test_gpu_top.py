@@ -345,6 +345,22 @@ def test_experts_layer(tt, how):
         assert not y[~mask].any()
 
 
+def test_experts_layer_whatever_masked_rows_hold(tt):
+    """NaN and infinities in masked rows: what the other rows get, and all gradients, have the bits that zeros there give."""
+    gen = torch.Generator(device="cuda").manual_seed(8)
+    m = tt.TTExperts(48, 40, 8, 2, generator=gen, residual=False, dtype=torch.bfloat16)
+    x = torch.randn(70, 48, device="cuda", generator=gen).bfloat16()
+    mask = torch.rand(70, device="cuda", generator=gen) > 0.3
+    runs = []
+    for fill in (0.0, math.nan, math.inf):
+        x[~mask] = fill
+        leaf = x.clone().requires_grad_()
+        y = m(leaf, mask)
+        runs.append([y.detach(), *torch.autograd.grad(y.float().square().sum(), [leaf, *m.parameters()])])
+        assert all(torch.equal(a, b) for a, b in zip(runs[0], runs[-1]))
+    assert not runs[0][0][~mask].any() and not runs[0][1][~mask].any() and all(bool(t.isfinite().all()) for t in runs[0])
+
+
 def test_a_model_of_them_learns_in_the_right_direction(tt):
     """Bags, experts and the loss, one step of each kind of optimizer: runs, and every parameter gets a gradient."""
     gen = torch.Generator(device="cuda").manual_seed(0)

@@ -171,6 +171,20 @@ def test_experts_layer_on_masked_rows(tt):
             tt.TTExperts(8, 12, 6, 2, device="cpu", **bad)
 
 
+def test_experts_layer_whatever_masked_rows_hold(tt):
+    m = tt.TTExperts(8, 12, 6, 2, device="cpu", residual=False)
+    x, mask = torch.randn(7, 8), torch.tensor([True, False] * 3 + [True])
+    grads = []
+    for fill in (0.0, math.nan, math.inf):
+        x[~mask] = fill
+        leaf = x.clone().requires_grad_()
+        y = m(leaf, mask)
+        assert not y[~mask].any()
+        grads.append(torch.autograd.grad(y[mask].square().sum(), [leaf, *m.parameters()]))
+        assert all(torch.equal(a, b) for a, b in zip(grads[0], grads[-1]))
+    assert not grads[0][0][~mask].any() and all(bool(g.isfinite().all()) for g in grads[0])
+
+
 def test_softmax_loss_module(tt):
     head = tt.TTSoftmaxLoss(6, 9, bias=True, ignore_index=2, reduction="sum", device="cpu")
     x = torch.randn(4, 6, requires_grad=True)

@@ -606,7 +606,7 @@ tt_status tt_route_order(const tt_route *op, const void *logits, const float *bi
 
 /*
  * Rows to their experts and back.  slots [rows][choices] and sources [rows * choices] as above; places outside
- * [0, rows * choices) count as none.
+ * [0, rows * choices) count as none, and a place is one choice's at most (of two, which one it gets is open).
  *   tt_expert_rows:     out[slots[r][j]] = x[r];  places without a source: left as they were, zeros with zero_rest
  *   tt_expert_combine:  out[r] = residual[r] + sum over j of weights[r][j] y[slots[r][j]]   (weights NULL: ones; what a
  *                       choice without a place would weigh is left out).  Also the gradient of tt_expert_rows.

@@ -86,8 +86,8 @@ _dense_objects = {}  # (unit, its defines): object of this process's build
 
 
 def build_dense(out_dir: str, tag: str, defines=None, top=False) -> str:
-    """The dense operators' units as a library of their own, with `top` also those of a model's top (norm, routing, loss); `defines` gives units flags ("-DNAME=value") of their own.  An
-    object is compiled once for every set of flags."""
+    """The dense operators' units as a library of their own, with `top` also those of a model's top (norm, routing, loss);
+    `defines` gives units flags ("-DNAME=value") of their own.  An object is compiled once for every set of flags."""
     os.makedirs(out_dir, exist_ok=True)
     gen = os.path.join(out_dir, "gen_dense")
     if not _dense_objects:

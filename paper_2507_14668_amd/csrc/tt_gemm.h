@@ -43,6 +43,7 @@ struct TTGemm {
   int act;
   float alpha, beta;
   int epilogue;                // TT_GEMM_PLAIN ...
+  int large;                   // tiles of 128 also where those are few but their sums can be cut into pieces for the whole card
   int a_padded;                // 16-bit A whose rows go on with zeros (K-contiguous) or anything (else) up to a multiple of 8
   int b_padded;                // the same of a row-contiguous B whose rows go on with anything
   float *stats;                // STATS: pairs [column tile][M]

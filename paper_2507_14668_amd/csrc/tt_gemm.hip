@@ -622,6 +622,14 @@ template <class T> __global__ void __launch_bounds__(TT_BLOCK) k_join_groups(TTG
 #ifndef TT_GEMM_LARGE_TILES
 #define TT_GEMM_LARGE_TILES 256
 #endif
+// Whether a product of n tiles of 128 keeps those because its sums are cut into pieces that fill the card: a workgroup of them does four times the work of one
+// of 64 in two and a half times its time.  The loss in fp32 and its gradients, with / without, us: 4000 rows of 4096 against 500 classes 612 / 683, 1000 x 2000 x 2000
+// 347 / 363, 70 x 4096 x 30000 1083 / 1336; where the pieces fill three quarters of it, 300 x 2000 x 8001 515 / 483, or half, 4000 x 512 x 500 231 / 187.
+bool large_pieces(const TTGemm &g, long long n, int bk) {
+  if (!g.large || g.mode != TT_GEMM_BATCH || g.M <= 64 || (g.like_N ? g.like_N : g.N) <= 64) return false;
+  const long long most = 512 / n, steps = tt_ceil_div(g.K, bk) / 8;
+  return n * (most < steps ? most : steps) >= 448;
+}
 struct Shape {
   int e, split, chunk;
   long long m_tiles, n_tiles, members;
@@ -640,7 +648,7 @@ Shape shape_of(const TTGemm &g) {
     return n;
   };
   long long n = tiles(128);
-  if (n < TT_GEMM_LARGE_TILES) n = tiles(64);
+  if (n < TT_GEMM_LARGE_TILES && !large_pieces(g, n, bk)) n = tiles(64);
   if (g.symmetric) n = (n + h.members * h.m_tiles) / 2;
   // two workgroups and more run on a compute unit: long sums in pieces up to 512 workgroups in all, of eight steps at least
   // (of four where even so most compute units have none)

@@ -110,6 +110,62 @@ template <class T> __global__ void __launch_bounds__(TT_BLOCK) k_loss_gather(con
   }
 }
 
+// The pieces of fp32 logits that went through memory: of each place's COLUMNS of them the pair that a tile of the product gives else, and the label's
+// logit; a wavefront each.  z: [rows][ld], 16-byte aligned rows.
+constexpr int COLUMNS = 1024;
+__global__ void __launch_bounds__(TT_BLOCK) k_loss_pairs(const float *__restrict__ z, long long ld, long long rows, int n, int first, Rows w, float2 *stats,
+                                                         float *picked) {
+  const long long i = (long long)blockIdx.x * (TT_BLOCK / 64) + (threadIdx.x >> 6);
+  if (i >= w.offsets[1]) return;
+  const int lane = threadIdx.x & 63, label = w.label[i] - first;
+  for (int t = (int)blockIdx.y; t * COLUMNS < n; t += (int)gridDim.y) {
+    const int c0 = t * COLUMNS + 4 * lane;
+    f32x4 v[COLUMNS / 256];
+    float top = -INFINITY, sum = 0.f;
+#pragma unroll
+    for (int k = 0; k < COLUMNS / 256; ++k) {
+      const int c = c0 + 256 * k;
+      float a[4] = {0.f, 0.f, 0.f, 0.f};
+      if (c < n) load4(z + i * ld + c, n - c, a);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        v[k][e] = c + e < n ? a[e] : -INFINITY;
+        if (c + e == label && c + e < n) picked[i] = a[e];
+        top = fmaxf(top, v[k][e]);
+      }
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+    const float base = top == -INFINITY ? 0.f : top;
+#pragma unroll
+    for (int k = 0; k < COLUMNS / 256; ++k)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum += __expf(v[k][e] - base);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
+    if (lane == 0) stats[t * rows + i] = float2{top, sum};
+  }
+}
+// ... and G in their place, zeros in the rows that do not count and in columns n .. padded - 1.
+__global__ void __launch_bounds__(TT_BLOCK) k_loss_softmax(float *z, long long ld, long long rows, int n, int padded, int first, Rows w) {
+  const long long places = w.offsets[1];
+  const int per = padded / 4;
+  for (long long e = (long long)blockIdx.x * TT_BLOCK + threadIdx.x; e < rows * per; e += (long long)gridDim.x * TT_BLOCK) {
+    const long long i = e / per;
+    const int c = (int)(e - i * per) * 4;
+    float *at = z + i * ld + c;
+    float v[4] = {0.f, 0.f, 0.f, 0.f};
+    if (i < places) {
+      load4(at, n - c, v);
+      const float lse = w.lse[i], grad = w.weight[i];
+      const int label = w.label[i] - first - c;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) v[k] = k < n - c ? grad * (k == label ? w.hot[i] : __expf(v[k] - lse)) : 0.f;
+    }
+    store4(at, 4, v);
+  }
+}
+
 // A piece's tiles into each place's running pair (largest logit, sum of exp(logit - it)), sixteen places a workgroup and sixteen runs of the tiles;
 // of the last piece the row's lse and loss.
 __global__ void __launch_bounds__(TT_BLOCK) k_loss_fold(const float2 *__restrict__ stats, int tiles, long long rows, int first, int last, Rows w, float2 *run,
@@ -207,13 +263,14 @@ tt_status check(const tt_loss *op) {
   return TT_OK;
 }
 
-// Classes of a piece, whole tiles of 256: of a forward one the statistics, of a backward one G has `room` bytes, about half of what the
-// last-level cache holds, so that the products that read a piece find it there.
+bool stored(const tt_loss *op);
+// Classes of a piece, whole tiles of 256: of a forward one the statistics, of a backward one G (and of both logits that go through memory) has
+// `room` bytes, about half of what the last-level cache holds, so that the products that read a piece find it there.
 #ifndef TT_LOSS_ROOM
 #define TT_LOSS_ROOM (128 << 20)
 #endif
 long long piece_of(const tt_loss *op, bool backward) {
-  const long long each = backward ? op->rows * (long long)elem(op->dtype) : tt_ceil_div(op->rows * 8, 64);
+  const long long each = backward || stored(op) ? op->rows * (long long)elem(op->dtype) : tt_ceil_div(op->rows * 8, 64);
   long long most = (long long)TT_LOSS_ROOM / (each > 0 ? each : 1) / 256 * 256;
   if (most < 256) most = 256;
   const long long pieces = (op->classes + most - 1) / most;
@@ -235,6 +292,7 @@ void describe(const tt_loss *op, TTGemm *g) {
   g->batch = 1;
   g->alpha = g->beta = 1.f;
   g->parts = 3;
+  g->large = op->dtype == TT_F32;
 }
 TTGemm of_logits(const tt_loss *op, int classes, bool backward, long long ldg) {  // rows that count by W of a piece
   TTGemm g;
@@ -247,6 +305,24 @@ TTGemm of_logits(const tt_loss *op, int classes, bool backward, long long ldg) {
   g.zero_rest = backward;
   g.n_padded = (classes + 7) & ~7;
   return g;
+}
+// The logits of a piece, or its G, in fp32 as an ordinary product that all rows take part in (zeros behind the last one that counts).
+TTGemm of_stored(const tt_loss *op, int classes, long long ldz) {
+  TTGemm g;
+  describe(op, &g);
+  g.a_kc = g.b_kc = 1;
+  g.M = (int)op->rows; g.N = classes; g.K = op->dim;
+  g.lda = padded(op); g.ldb = op->dim; g.ldo = ldz;
+  return g;
+}
+// Whether fp32 logits go through memory: where few tiles leave most compute units without one, which the ordinary product cuts along its sums, and for the
+// few rows that have a kernel of their own.  The loss alone, through memory / in the tiles' own statistics, us: 1000 rows of 4096 against 500 classes 87 / 154, 300 x
+// 4096 x 2000 97 / 143, 70 x 2000 x 30000 144 / 224, 16 x 4096 x 30000 163 / 229.  (In 16 bits the steps are four times as fast, and a rounded logit would not do.)
+bool stored(const tt_loss *op) {
+  if (op->dtype != TT_F32 || narrow(op) || op->rows < 1) return false;
+  const long long most = (long long)TT_LOSS_ROOM / (op->rows * 4);  // (a piece has so many, and 256 at least)
+  const TTGemm g = of_stored(op, op->classes < most ? op->classes : most < 256 ? 256 : (int)most, 0);
+  return ttk_gemm_rows_serves(g) || ttk_gemm_partial_bytes(g) > 0;
 }
 // G W: few tiles of dx over many classes are cut into `cuts` equal members, whole steps of 64 classes, whose sums stand side by side until
 // the end; what is left over is a product of its own.  4000 rows of 513 (48 tiles of 256) against 16384 classes in fp16 250 us whole, 108 in
@@ -283,13 +359,18 @@ TTGemm of_dw(const tt_loss *op, int classes, long long ldg, bool column) {  // G
   g.like_N = op->dim;
   g.lda = ldg; g.ldb = column ? ldg : padded(op); g.ldo = g.N;
   g.a_padded = g.b_padded = 1;
-  g.epilogue = op->dtype == TT_F32 ? TT_GEMM_PLAIN : TT_GEMM_SCALED;
+  g.epilogue = TT_GEMM_SCALED;
   return g;
 }
 
 struct Scratch {
   size_t of, at, label, lse, share, weight, hot, back, offsets, x, stats, run, picked, grads, acc, column, pieces, parts, starts, copy, total;
 };
+size_t stored_bytes(const tt_loss *op, long long piece) {
+  const int first = (int)(piece < op->classes ? piece : op->classes), last = (int)(op->classes - (op->classes - 1) / piece * piece);
+  const size_t a = ttk_gemm_partial_bytes(of_stored(op, first, piece)), b = ttk_gemm_partial_bytes(of_stored(op, last, piece));
+  return a > b ? a : b;
+}
 Scratch scratch(const tt_loss *op, bool backward) {
   Scratch w = {};
   const size_t rows = (size_t)op->rows, whole = rows + TT_LOSS_STEP, es = elem(op->dtype);
@@ -320,6 +401,10 @@ Scratch scratch(const tt_loss *op, bool backward) {
     take(w.stats, narrow(op) ? ttk_narrow_stats_bytes(n) : (size_t)tt_ceil_div(piece, 64) * rows * 8);
     take(w.run, rows * 8);
     take(w.picked, rows * 4);
+    if (stored(op)) {
+      take(w.grads, rows * piece * 4);
+      take(w.pieces, stored_bytes(op, piece));
+    }
     return w;
   }
   take(w.lse, whole * 4);
@@ -333,7 +418,7 @@ Scratch scratch(const tt_loss *op, bool backward) {
   take(w.grads, rows * piece * es);
   take(w.acc, (size_t)cuts_of(op) * rows * (copies(op) ? padded(op) : op->dim) * 4);
   take(w.column, (size_t)piece * es);
-  size_t most = 0;
+  size_t most = stored(op) ? stored_bytes(op, piece) : 0;
   const int last = (int)(op->classes - (op->classes - 1) / piece * piece);
   for (int i = 0; i < 2; ++i) {
     const int n = i ? last : (int)(piece < op->classes ? piece : op->classes);
@@ -383,6 +468,15 @@ template <class T> tt_status clear(void *p, long long n, hipStream_t s) {
   hipLaunchKernelGGL(k_loss_clear<T>, dim3(grid_of(n)), dim3(TT_BLOCK), 0, s, (T *)p, n);
   return tt_launch_status();
 }
+// The logits of n classes from c on, fp32, in `grads`.
+tt_status logits(const tt_loss *op, char *ws, const Scratch &need, const void *w, const void *bias, long long c, int n, long long piece, hipStream_t s) {
+  TTGemm g = of_stored(op, n, piece);
+  g.a = ws + need.x;
+  g.b = (const float *)w + c * op->dim;
+  g.bias = bias ? (const float *)bias + c : nullptr;
+  g.out = ws + need.grads;
+  return ttk_gemm(g, ws + need.pieces, s);
+}
 #define TT_BY_TYPE(call, dtype, ...) \
   ((dtype) == TT_F32 ? call<float>(__VA_ARGS__) : (dtype) == TT_BF16 ? call<ttg::bf16>(__VA_ARGS__) : call<ttg::f16>(__VA_ARGS__))
 
@@ -429,23 +523,34 @@ extern "C" tt_status tt_cross_entropy_forward(const tt_loss *op, const void *x, 
     }
     for (long long c = 0; c < classes && !narrow(op); c += piece) {
       const int n = (int)(classes - c < piece ? classes - c : piece);
-      TTGemm g = of_logits(op, n, false, 0);
-      g.a = ws + need.x;
-      g.b = (const char *)w + (size_t)c * op->dim * es;
-      if (copies(op)) {
-        if ((st = TT_BY_TYPE(pad, op->dtype, op, g.b, n, ws + need.copy, s)) != TT_OK) return st;
-        g.b = ws + need.copy;
+      const int first = c == 0, last = c + n == classes;
+      int tiles;
+      if (stored(op)) {
+        float *z = (float *)(ws + need.grads);
+        if ((st = logits(op, ws, need, w, bias, c, n, piece, s)) != TT_OK) return st;
+        tiles = tt_ceil_div(n, COLUMNS);
+        hipLaunchKernelGGL(k_loss_pairs, dim3((unsigned)tt_ceil_div(rows, TT_BLOCK / 64), (unsigned)(tiles < 65535 ? tiles : 65535)), dim3(TT_BLOCK), 0, s, (const float *)z, piece,
+                           rows, n, (int)c, r, (float2 *)(ws + need.stats), (float *)(ws + need.picked));
+        if ((st = tt_launch_status()) != TT_OK) return st;
+      } else {
+        TTGemm g = of_logits(op, n, false, 0);
+        g.a = ws + need.x;
+        g.b = (const char *)w + (size_t)c * op->dim * es;
+        if (copies(op)) {
+          if ((st = TT_BY_TYPE(pad, op->dtype, op, g.b, n, ws + need.copy, s)) != TT_OK) return st;
+          g.b = ws + need.copy;
+        }
+        g.bias = bias ? (const char *)bias + (size_t)c * es : nullptr;
+        g.offsets = r.offsets;
+        g.stats = (float *)(ws + need.stats);
+        g.picked = (float *)(ws + need.picked);
+        g.labels = r.label;
+        g.first = (int)c;
+        if ((st = ttk_gemm(g, nullptr, s)) != TT_OK) return st;
+        tiles = tt_ceil_div(n, ttk_gemm_tile(g));
       }
-      g.bias = bias ? (const char *)bias + (size_t)c * es : nullptr;
-      g.offsets = r.offsets;
-      g.stats = (float *)(ws + need.stats);
-      g.picked = (float *)(ws + need.picked);
-      g.labels = r.label;
-      g.first = (int)c;
-      if ((st = ttk_gemm(g, nullptr, s)) != TT_OK) return st;
-      const int tiles = tt_ceil_div(n, ttk_gemm_tile(g)), first = c == 0, last = c + n == classes;
-      hipLaunchKernelGGL(k_loss_fold, dim3((unsigned)tt_ceil_div(rows, 16)), dim3(TT_BLOCK), 0, s, (const float2 *)g.stats, tiles, rows, first, last, r, run,
-                         (const float *)g.picked, each, losses);
+      hipLaunchKernelGGL(k_loss_fold, dim3((unsigned)tt_ceil_div(rows, 16)), dim3(TT_BLOCK), 0, s, (const float2 *)(ws + need.stats), tiles, rows, first, last, r, run,
+                         (const float *)(ws + need.picked), each, losses);
     }
   }
   if (whole) hipLaunchKernelGGL(k_loss_sum, dim3(1), dim3(SCAN), 0, s, (const float2 *)each, rows, r, reduce, loss);
@@ -496,18 +601,25 @@ extern "C" tt_status tt_cross_entropy_backward(const tt_loss *op, const void *x,
       if ((st = TT_BY_TYPE(pad, op->dtype, op, wc, n, ws + need.copy, s)) != TT_OK) return st;
       wc = ws + need.copy;
     }
-    TTGemm g = of_logits(op, n, true, piece);
-    g.a = ws + need.x;
-    g.b = wc;
-    g.bias = bias ? (const char *)bias + (size_t)c * es : nullptr;
-    g.offsets = r.offsets;
-    g.out = ws + need.grads;
-    g.labels = r.label;
-    g.lse = r.lse;
-    g.row_grad = r.weight;
-    g.hot = r.hot;
-    g.first = (int)c;
-    if ((st = ttk_gemm(g, nullptr, s)) != TT_OK) return st;
+    if (stored(op)) {
+      if ((st = logits(op, ws, need, w, bias, c, n, piece, s)) != TT_OK) return st;
+      const int to = (n + 7) & ~7;
+      hipLaunchKernelGGL(k_loss_softmax, dim3(grid_of(rows * (to / 4))), dim3(TT_BLOCK), 0, s, (float *)(ws + need.grads), piece, rows, n, to, (int)c, r);
+      if ((st = tt_launch_status()) != TT_OK) return st;
+    } else {
+      TTGemm g = of_logits(op, n, true, piece);
+      g.a = ws + need.x;
+      g.b = wc;
+      g.bias = bias ? (const char *)bias + (size_t)c * es : nullptr;
+      g.offsets = r.offsets;
+      g.out = ws + need.grads;
+      g.labels = r.label;
+      g.lse = r.lse;
+      g.row_grad = r.weight;
+      g.hot = r.hot;
+      g.first = (int)c;
+      if ((st = ttk_gemm(g, nullptr, s)) != TT_OK) return st;
+    }
     if (dx) {
       const int cuts = cuts_of(op), size = n / cuts / 64 * 64, members = cuts > 1 && size > 0 ? cuts : 1, whole = members > 1 ? size : n;
       for (int i = 0; i < 2; ++i) {

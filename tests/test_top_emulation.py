@@ -391,6 +391,10 @@ LOSSES = [
     (9, 8, 2000, BF16, True, "mean", 9, 0, 0),
     (300, 72, 264, F16, True, "sum", 3, 0, 0),
     (0, 8, 20, F32, True, "mean", 0, 0, 0),
+    (20, 200, 1100, F32, True, "mean", 3, 0, 1),  # fp32 logits through memory: few rows, more classes than a wavefront takes,
+    (1, 133, 2049, F32, True, "sum", 0, 2, 0),
+    (70, 600, 130, F32, True, "none", 9, 0, 0),   # ... and sums in pieces
+    (90, 1030, 70, F32, False, "mean", 90, 0, 0),
 ]
 
 

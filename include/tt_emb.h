@@ -533,8 +533,8 @@ tt_status tt_core_ortho_update(const tt_table *table, const float *const dcore[3
  *   y = (x - mean) rstd weight + bias,  rstd = 1 / sqrt(variance + eps)
  * weight and bias [dim] may be NULL (one and zero).  Backward, with h = grad weight and x^ = (x - mean) rstd:
  *   dx = rstd (h - mean(h) - x^ mean(h x^)),  dweight = sum over rows of grad x^,  dbias = sum of grad
- * A row of equal values has rstd = 1 / sqrt(eps) (infinite if eps is 0); infinities and NaN stay in their
- * row of out and dx.
+ * A row of equal values gives the bias if eps > 0 (without eps it has no answer: NaN or the bias); infinities and
+ * NaN stay in their row of out and dx.
  *   stats      DEVICE float[rows][2]: mean and rstd, written by the forward (may be NULL), read by the backward
  *   workspace  DEVICE, 256-byte aligned, tt_layer_norm_workspace_bytes(op) bytes; only for dweight and dbias
  */

@@ -74,6 +74,12 @@ template <int LANES> __device__ __forceinline__ void row_sum(float &a, float &b,
 }
 template <int LANES> constexpr int threads_of() { return LANES > 256 ? LANES : 256; }
 
+// The mean of a row's sum is off by the rounding of that sum, in the size of its elements, which may be far above their spread: it is mended by the mean `off` of
+// what it leaves of them, whose rounding is in the size of the spread, and the mean of the squares of that by off's.  A NaN stays one.
+__device__ __forceinline__ float variance_of(float squares, float off) {
+  const float v = fmaf(-off, off, squares);
+  return v < 0.f ? 0.f : v;
+}
 // A row stays in the registers of LANES threads, NV pieces each: it is read once, and the variance is the mean of the squares of
 // what is left after the mean.  weight and bias stay in registers over a workgroup's rows.  Bound by memory: 106496 rows of 128 in fp32 18.2 us
 // (6.0 TB/s), 16384 of 4096 in bf16 50 (5.4), a large copy 5.1.
@@ -106,17 +112,19 @@ template <class T, int LANES, int NV> __global__ void __launch_bounds__(threads_
 #pragma unroll
       for (int e = 0; e < C; ++e) sum += x[i].at(e);
     row_sum<LANES>(sum, none, room, turn);
-    const float mean = sum * inv;
+    const float about = sum * inv;
+    float off = 0.f;
 #pragma unroll
     for (int i = 0; i < NV; ++i)
 #pragma unroll
       for (int e = 0; e < C; ++e) {
-        const float d = x[i].at(e) - mean;
-        squares += (i * LANES + lane) * C + e < p.n ? d * d : 0.f;
+        const float d = (i * LANES + lane) * C + e < p.n ? x[i].at(e) - about : 0.f;
+        squares = fmaf(d, d, squares);
+        off += d;
       }
-    none = 0.f;
-    row_sum<LANES>(squares, none, room, turn);
-    const float rstd = 1.f / sqrtf(squares * inv + p.eps);
+    row_sum<LANES>(squares, off, room, turn);
+    off *= inv;
+    const float mean = about + off, rstd = 1.f / sqrtf(variance_of(squares * inv, off) + p.eps);
     if (!live) continue;
     if (p.stats && lane == 0) {
       p.stats[2 * r] = mean;
@@ -229,16 +237,21 @@ template <class T> __global__ void __launch_bounds__(WIDE) k_norm_forward_wide(N
       for (int e = 0; e < C; ++e) sum += v[e];
     }
     row_sum<WIDE>(sum, none, room, turn);
-    const float mean = sum * inv;
+    const float about = sum * inv;
+    float off = 0.f;
     for (int c = threadIdx.x * C; c < p.n; c += WIDE * C) {
       float v[C];
       load_n<T, C>(x + c, p.n - c, v);
 #pragma unroll
-      for (int e = 0; e < C; ++e) squares += c + e < p.n ? (v[e] - mean) * (v[e] - mean) : 0.f;
+      for (int e = 0; e < C; ++e) {
+        const float d = c + e < p.n ? v[e] - about : 0.f;
+        squares = fmaf(d, d, squares);
+        off += d;
+      }
     }
-    none = 0.f;
-    row_sum<WIDE>(squares, none, room, turn);
-    const float rstd = 1.f / sqrtf(squares * inv + p.eps);
+    row_sum<WIDE>(squares, off, room, turn);
+    off *= inv;
+    const float mean = about + off, rstd = 1.f / sqrtf(variance_of(squares * inv, off) + p.eps);
     if (p.stats && threadIdx.x == 0) {
       p.stats[2 * r] = mean;
       p.stats[2 * r + 1] = rstd;

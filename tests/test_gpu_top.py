@@ -345,6 +345,17 @@ def test_experts_layer(tt, how):
         assert not y[~mask].any()
 
 
+@pytest.mark.parametrize("n", [3, 128, 1000, 4096, 20000])
+def test_layer_norm_of_equal_values(tt, n):
+    """The bias, whatever eps is above zero and however far from zero the row is; no gradient of the row reaches the weight."""
+    x = torch.tensor([1000.1, -0.1, 0.0, 77777.7], device="cuda")[:, None].expand(4, n).contiguous().requires_grad_()
+    w, b = torch.full((n,), 3.0, device="cuda", requires_grad=True), torch.randn(n, device="cuda")
+    y = tt.tt_layer_norm(x, w, b, eps=1e-12)
+    assert torch.equal(y, b.expand(4, n))
+    (dw,) = torch.autograd.grad(y.sum(), w)
+    assert not dw.any()
+
+
 def test_experts_layer_whatever_masked_rows_hold(tt):
     """NaN and infinities in masked rows: what the other rows get, and all gradients, have the bits that zeros there give."""
     gen = torch.Generator(device="cuda").manual_seed(8)

@@ -47,6 +47,31 @@ def intact(*gs):
 
 
 # ---- layer norm
+@pytest.mark.parametrize("n", [3, 100, 700, 2500, 4096, 9000])
+def test_layer_norm_of_rows_far_from_zero(lib, n):
+    """Rows of equal values give the bias, whatever eps is above zero; rows around 1000 and 3e5 what 64 bits give, as far as a mean of fp32 allows.  With
+    chains of at most 46 additions (32 in a thread, 14 across) the first mean is off by a = 46 u |mean| at most, in deviations d; the mean of what it leaves
+    by 46 u (1 + d), and u |mean| when it is added; the squares by 49 u (1 + d^2), what is taken off them by 92 u d (1 + d), half of both in the root;
+    three roundings more in y, one with the bias."""
+    from paper_2507_14668_amd import binding
+    gen = torch.Generator().manual_seed(n)
+    x = torch.stack([torch.full((n,), 1000.1), torch.full((n,), -0.1), 1000 + torch.randn(n, generator=gen), 3e5 + torch.randn(n, generator=gen)])
+    bias, out, stats = torch.randn(n, generator=gen), Guarded((4, n), F32), Guarded((4, 2), F32)
+    gx, gb = place(x), place(bias)
+    op = binding.CNorm(DT[F32], n, 4, eps=1e-12)
+    assert lib.tt_layer_norm_forward(ctypes.byref(op), gx.ptr, None, gb.ptr, out.ptr, stats.ptr, None) == 0
+    assert torch.equal(out.t[:2], bias.expand(2, n))
+    d = x[2:].double()
+    y = (d - d.mean(1, keepdim=True)) / torch.sqrt(d.var(1, unbiased=False, keepdim=True) + 1e-12)
+    mean, s, u = d.mean(1, keepdim=True), d.std(1, unbiased=False, keepdim=True), 2.0 ** -24
+    a = 46 * u * mean / s
+    most = u * (mean / s + 46 * (1 + a) + y.abs() * (4 + 24.5 * (1 + a * a) + 46 * a * (1 + a)) + (y + bias).abs())
+    off = (out.t[2:].double() - (y + bias)).abs() - most
+    assert float(off.max()) <= 0
+    assert bool(((stats.t[2:, :1] - mean).abs() <= u * (mean + 46 * s * (1 + a))).all())
+    intact(gx, gb, out, stats)
+
+
 @pytest.mark.parametrize("rows,n,dtype,affine,pad,shift", [
     (1, 1, F32, True, 0, 0), (3, 7, BF16, True, 1, 1), (5, 64, F32, True, 0, 0), (70, 128, F32, True, 0, 0), (19, 130, F16, True, 3, 1),
     (9, 128, BF16, False, 0, 0), (6, 256, BF16, True, 8, 0), (4, 300, F32, True, 0, 3), (3, 1025, F32, True, 0, 0), (3, 2047, BF16, True, 5, 1),

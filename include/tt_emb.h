@@ -565,7 +565,8 @@ tt_status tt_layer_norm_backward(const tt_norm *op, const void *x, const void *w
  * logit or c is -infinity is masked: never chosen, and no group's strength.  Where fewer than `choices` are left the numbers
  * are -1 and the weights 0 (a row of -infinity, as padding has, goes nowhere).  A NaN counts as the
  * largest (so it shows in the weights); a logit of +infinity makes a softmax row NaN.
- * Backward: from grad_weights the gradient of the logits through the weights (s only; numbers are fixed).
+ * Backward: from grad_weights the gradient of the logits through the weights (s only; numbers are fixed), in 64 bits as well.  Renormalised weights
+ * hang on the chosen logits alone, and the others' gradient is zero.
  *   experts DEVICE int64[rows][choices]; weights, grad_weights float[rows][choices]; bias float[experts], nullable
  */
 #define TT_ROUTE_MAX_EXPERTS 1024

@@ -220,72 +220,85 @@ template <class T, int LANES, int EL, bool GROUPS> __global__ void __launch_boun
   }
 }
 
-// dz = s (ds - sum ds s) (softmax) or ds s (1 - s), with ds of the chosen experts from the gradients of their weights:
-// scale g, or scale (g - sum g w') / sum s with the renormalised w' = s / sum s.
+// dz = s (ds - sum ds s) (softmax) or ds s (1 - s), with ds of the chosen experts from the gradients g of their weights, in 64 bits as the scores are: those of
+// chosen experts may be far below what fp32 holds.  Renormalised weights w = s / sum s have the gradient t = w (g - sum g w) beside them, which no small sum is divided into:
+// dz = t (softmax: the chosen scores' share of all others cancels) or t (1 - s).  Only softmax weights as they are need every expert's exp.
 template <class T, int LANES, int EL> __global__ void __launch_bounds__(64 * ROUTE_WAVES) k_route_backward(Route p) {
   constexpr int PER = 64 / LANES;
   __shared__ float room[ROUTE_WAVES * PER][LANES * EL];
   const int lane = row_lane(LANES), wave = threadIdx.x >> 6, first = EL * lane;
-  float *mine_of = room[threadIdx.x / LANES];
+  float *logits_of = room[threadIdx.x / LANES];
   for (long long r0 = ((long long)blockIdx.x * ROUTE_WAVES + wave) * PER; r0 < p.rows; r0 += (long long)gridDim.x * ROUTE_WAVES * PER) {
     const bool live = r0 + (threadIdx.x & 63) / LANES < p.rows;
     const long long r = live ? r0 + (threadIdx.x & 63) / LANES : p.rows - 1;
-    float z[EL], s[EL];
+    float z[EL];
     load_logits<T, LANES, EL>(p, r, z);
     const int64_t asked = lane < p.k ? p.experts[r * p.k + lane] : -1;
     const int mine = asked >= 0 && asked < p.num ? (int)asked : -1;
-    float g = mine >= 0 ? p.scale * p.grad[r * p.k + lane] : 0.f;
-    if (p.sigmoid) {
+    const double g = mine >= 0 ? (double)p.scale * (double)p.grad[r * p.k + lane] : 0.0;
 #pragma unroll
-      for (int i = 0; i < EL; ++i) s[i] = 1.f / (1.f + expf(-z[i]));
+    for (int i = 0; i < EL; ++i) logits_of[first + i] = z[i];
+    tt_wave_lds_order();
+    const float chosen = mine >= 0 ? logits_of[mine] : -INFINITY;
+    tt_wave_lds_order();
+    double s = 0, inv = 0, each[EL] = {};  // the chosen expert's score; softmax: one over the sum, and without renormalising the lane's exponentials
+    float top = 0.f;
+    if (p.sigmoid) {
+      s = mine >= 0 ? 1.0 / (1.0 + exp(-(double)chosen)) : 0.0;
     } else {
-      float top = z[0], sum = 0.f;
+      top = z[0];
 #pragma unroll
       for (int i = 1; i < EL; ++i) top = fmaxf(top, z[i]);
       top = largest_of<LANES>(top);
       if (top == -INFINITY) top = 0.f;
+      double sum = 0;
+      if (p.renorm) {  // (it only says whether scores are zero in 64 bits, or not numbers)
+        float about = 0.f;
 #pragma unroll
-      for (int i = 0; i < EL; ++i) {
-        s[i] = expf(z[i] - top);
-        sum += s[i];
+        for (int i = 0; i < EL; ++i) about += expf(z[i] - top);
+        sum = sum_of<LANES>(about);
+      } else {
+#pragma unroll
+        for (int i = 0; i < EL; ++i) {
+          each[i] = exp((double)z[i] - (double)top);
+          sum += each[i];
+        }
+        sum = sum_of<LANES>(sum);
       }
-      sum = sum_of<LANES>(sum);
-      const float inv = sum == 0.f ? 0.f : 1.f / sum;
-#pragma unroll
-      for (int i = 0; i < EL; ++i) s[i] *= inv;
+      inv = sum == 0 ? 0.0 : 1.0 / sum;
+      s = mine >= 0 ? exp((double)chosen - (double)top) * inv : 0.0;
     }
-#pragma unroll
-    for (int i = 0; i < EL; ++i) mine_of[first + i] = s[i];
-    tt_wave_lds_order();
-    const float chosen = mine >= 0 ? mine_of[mine] : 0.f;
-    tt_wave_lds_order();
+    double t;
     if (p.renorm) {
-      const float total = sum_of<LANES>(chosen), inv = total == 0.f ? 0.f : 1.f / total;
-      const float mean = sum_of<LANES>(g * chosen) * inv;
-      g = mine >= 0 ? (g - mean) * inv : 0.f;
+      const double total = sum_of<LANES>(s), w = total == 0 ? 0.0 : s / total;
+      t = w * (g - sum_of<LANES>(g * w));
+    } else {
+      t = g * s;
     }
-    const float dot = p.sigmoid ? 0.f : sum_of<LANES>(g * chosen);
-    float d[EL] = {};
+    if (p.sigmoid) t *= 1.0 / (1.0 + exp((double)chosen));
+    if (mine < 0) t = 0;
+    const double dot = p.sigmoid || p.renorm ? 0.0 : sum_of<LANES>(t);
+    double d[EL];
+#pragma unroll
+    for (int i = 0; i < EL; ++i) d[i] = p.sigmoid ? 0.0 : p.renorm ? 0.0 * inv : -(each[i] * inv) * dot;
     for (int j = 0; j < p.k; ++j) {  // one after the other: an expert named twice gets both
       const int e = from_lane<LANES>(mine, j) - first;
-      const float gj = __uint_as_float((unsigned)from_lane<LANES>((int)__float_as_uint(g), j));
+      const double tj = read_lane64<LANES>(t, j);
 #pragma unroll
-      for (int i = 0; i < EL; ++i) d[i] += e == i ? gj : 0.f;
-    }
-#pragma unroll
-    for (int i = 0; i < EL; ++i) {
-      if (p.sigmoid) d[i] = d[i] == 0.f ? 0.f : d[i] * s[i] * (1.f / (1.f + expf(z[i])));
-      else d[i] = s[i] * (d[i] - dot);
+      for (int i = 0; i < EL; ++i) d[i] += e == i ? tj : 0.0;
     }
     if (!live) continue;
+    float out[EL];
+#pragma unroll
+    for (int i = 0; i < EL; ++i) out[i] = (float)d[i];
     T *to = (T *)p.dlogits + r * p.ldd + first;
     const int valid = p.num - first;
     if constexpr (EL >= 4) {
-      store_n<T, EL>(to, valid, d);
+      store_n<T, EL>(to, valid, out);
     } else {
 #pragma unroll
       for (int i = 0; i < EL; ++i)
-        if (i < valid) to[i] = from_f32<T>(d[i]);
+        if (i < valid) to[i] = from_f32<T>(out[i]);
     }
   }
 }

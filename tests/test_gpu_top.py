@@ -6,7 +6,7 @@ import pytest
 import torch
 
 import top_ref as ref
-from test_top_emulation import LOSSES, ROUTES, routed
+from test_top_emulation import FAR_ROUTES, LOSSES, ROUTES, routed
 
 pytestmark = pytest.mark.gpu
 F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
@@ -145,6 +145,26 @@ def test_route(tt, rows, num, k, dtype, scores, biased, groups, top, renorm, sca
     g = randn(gen, rows, k)
     (grad,) = torch.autograd.grad(r.weights, dz, g.cuda())
     check(grad, ref.route_backward64(z, want_e, g, **how), "dlogits")
+
+
+@pytest.mark.parametrize("logits,bias,scores", FAR_ROUTES)
+@pytest.mark.parametrize("renorm", [True, False])
+@pytest.mark.parametrize("num,dtype", [(4, F32), (64, F16), (300, F32)])
+def test_route_of_scores_outside_single_precision(tt, logits, bias, scores, renorm, num, dtype):
+    """Where the chosen scores are too small for fp32, weights and gradients are those of 64 bits; the rest of the experts is masked."""
+    at = torch.arange(4) * (num // 4)
+    z, b = torch.full((5, num), -math.inf), torch.zeros(num)
+    z[:, at] = torch.tensor(logits)
+    b[at] = torch.tensor(bias or [0.0] * 4)
+    g = randn(torch.Generator().manual_seed(num), 5, 2)
+    leaf = put(z.to(dtype)).requires_grad_()
+    how = dict(scores=scores, renormalize=renorm, scale=2.5)
+    r = tt.tt_route(leaf, 2, bias=put(b), **how)
+    want_w, want_e = ref.route64(z.to(dtype), 2, b, **how)
+    assert torch.equal(r.experts.cpu(), want_e)
+    check(r.weights, (want_w, ref.weights_tol(want_w)), "weights")
+    (dz,) = torch.autograd.grad(r.weights, leaf, g.cuda())
+    check(dz, ref.route_backward_wide64(z.to(dtype), want_e, g, **how), "dlogits")
 
 
 def test_close_scores_are_told_apart(tt):

@@ -233,6 +233,52 @@ def test_route_specials(lib):
     assert dz.tolist() == [[0.0, 0.0, 0.75, 0.0]]
 
 
+# rows of logits whose scores leave the range of fp32, and what is added to choose them: (logits, bias, scores)
+FAR_ROUTES = [([-88.0, -87.5, -89.0, -90.0], None, "sigmoid"), ([-89.0, -90.0, -200.0, -201.0], None, "sigmoid"), ([-100.0, -100.5, -700.0, -99.0], None, "sigmoid"),
+              ([90.0, 101.0, 300.0, 89.0], None, "sigmoid"), ([0.0, -90.0, -90.5, -200.0], [-math.inf, 0, 0, 0], "softmax"),
+              ([0.0, -120.0, -121.0, -500.0], [-2.0, 0, 0, 0], "softmax"), ([0.0, -95.0, -95.25, -94.0], [-2.0, 0, 0, -2.0], "softmax"),
+              ([0.0, -600.0, -601.0, -650.0], [-2.0, 0, 0, 0], "softmax"), ([3.0, 2.5, -400.0, 1.0], None, "softmax"), ([500.0, 499.0, 0.0, -500.0], None, "softmax")]
+
+
+@pytest.mark.parametrize("logits,bias,scores", FAR_ROUTES)
+@pytest.mark.parametrize("renorm", [True, False])
+@pytest.mark.parametrize("num,dtype", [(4, F32), (26, F32), (64, BF16), (100, F32), (700, F32)])
+def test_route_of_scores_outside_single_precision(lib, logits, bias, scores, renorm, num, dtype):
+    """Weights and their gradient where the chosen scores are too small for fp32: what 64 bits give.  The rest of the experts is masked."""
+    from paper_2507_14668_amd import binding
+    at = torch.arange(4) * (num // 4)
+    z, b = torch.full((3, num), -math.inf), torch.zeros(num)
+    z[:, at] = torch.tensor(logits)
+    z = z.to(dtype)
+    b[at] = torch.tensor(bias or [0.0] * 4)
+    g = torch.tensor([[3.0, -2.0], [1e30, 1.0], [0.25, 0.25]])
+    op = binding.CRoute(DT[dtype], binding.SCORES[scores], 3, num, 2, 1, 1, int(renorm), 2.5)
+    how = dict(scores=scores, renormalize=renorm, scale=2.5)
+    e, w, dz = Guarded((3, 2), torch.int64), Guarded((3, 2), F32), Guarded((3, num), dtype)
+    gz, gb, gg = place(z), place(b[None]), place(g)
+    assert lib.tt_route_forward(ctypes.byref(op), gz.ptr, gb.ptr, e.ptr, w.ptr, None) == 0
+    want_w, want_e = ref.route64(z, 2, b, **how)
+    assert torch.equal(e.t, want_e)
+    ref.check(w.t, want_w, ref.weights_tol(want_w), "weights")
+    assert lib.tt_route_backward(ctypes.byref(op), gz.ptr, e.ptr, gg.ptr, dz.ptr, None) == 0
+    ref.check(dz.t, *ref.route_backward_wide64(z, e.t, g, **how), "dlogits")
+    intact(gz, gb, gg, e, w, dz)
+
+
+def test_route_gradients_show_what_is_not_a_number(lib):
+    """A NaN or +infinity among the logits: NaN in a softmax row's gradient, as in its weights; scores that are zero in 64 bits have none."""
+    from paper_2507_14668_amd import binding
+    z = torch.zeros(4, 8)
+    z[0, 5], z[1, 5], z[2, 1:] = math.nan, math.inf, -1e4
+    e, g, dz = torch.tensor([[0, 1], [0, 5], [2, 3], [2, 3]]), torch.ones(4, 2), torch.empty(4, 8)
+    g[:, 0] = 2.0
+    for renorm in (0, 1):
+        op = binding.CRoute(0, 0, 4, 8, 2, 1, 1, renorm, 1.0)
+        assert lib.tt_route_backward(ctypes.byref(op), z.data_ptr(), e.data_ptr(), g.data_ptr(), dz.data_ptr(), None) == 0
+        assert dz[0].isnan().all() and dz[1].isnan().all() and not dz[2].any()
+        ref.check(dz[3:], *ref.route_backward_wide64(z[3:], e[3:], g[3:], "softmax", bool(renorm)), "dlogits")
+
+
 def test_route_refusals(lib):
     from paper_2507_14668_amd import binding
     z, b, e, w, dz = torch.zeros(4, 8), torch.zeros(8), torch.zeros(4, 2, dtype=torch.int64), torch.zeros(4, 2), torch.zeros(4, 8)

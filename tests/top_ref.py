@@ -232,3 +232,31 @@ def loss64(x, w, labels, bias=None, ignore_index=-100, reduction="mean", grad=No
     result["dw"] = (dw, eG.t() @ x.abs() + 2 * (rows + 2) * U * (size.t() @ x.abs()) + rounding(dw, dtype))
     result["dbias"] = (db, eG.sum(0) + 2 * (rows + 2) * U * size.sum(0) + rounding(db, dtype))
     return result
+
+
+# ---- the router's gradient at any size of the scores
+def route_backward_wide64(logits, experts, grad, scores="softmax", renormalize=False, scale=1.0):
+    """dlogits and its tolerance from normalised weights by differences of logarithms, which no size of a score takes out of the range.  64-bit
+    arithmetic, 2^-44 of the terms' sizes (some hundred roundings of 2^-53 each), rounded to fp32 and from there to the type."""
+    z, there = logits.double(), experts >= 0
+    at = experts.clamp(min=0)
+    pick = lambda v: torch.where(there, torch.gather(v, 1, at), torch.full((), -math.inf, dtype=torch.float64))
+    softplus = lambda v: v.clamp(min=0) + torch.log1p(torch.exp(-v.abs()))
+    logs = z - torch.logsumexp(z, 1, keepdim=True) if scores == "softmax" else -softplus(-z)
+    chosen = pick(logs)
+    g = torch.where(there, scale * grad.double(), torch.zeros((), dtype=torch.float64))
+    if renormalize:
+        w = torch.softmax(chosen, 1).nan_to_num(0.0)
+        t = w * (g - (g * w).sum(1, keepdim=True))
+        size = w * (g.abs() + (g * w).abs().sum(1, keepdim=True))
+    else:
+        w = torch.exp(chosen)
+        t, size = g * w, (g * w).abs()
+    if scores == "sigmoid":
+        rest = torch.where(there, torch.exp(-softplus(torch.gather(z, 1, at))), torch.zeros((), dtype=torch.float64))
+        t, size = t * rest, size * rest
+    dz, tol = (torch.zeros_like(z).scatter_add_(1, at, v) for v in (t, size))
+    if scores == "softmax" and not renormalize:
+        s, dot = torch.exp(logs), t.sum(1, keepdim=True)
+        dz, tol = dz - s * dot, tol + s * size.sum(1, keepdim=True)
+    return dz, 2.0 ** -44 * tol + rounding(dz, torch.float32) + (rounding(dz, logits.dtype) if logits.dtype != torch.float32 else 0)

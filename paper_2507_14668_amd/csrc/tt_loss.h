@@ -18,6 +18,7 @@ struct TTLossRows {
 };
 
 #define TT_LOSS_STEP 32
+#define TT_LOSS_RAISE 8192.f  // what a G without its shares is formed with in fp16, whose range is short
 
 struct TTNarrow {
   int dtype, dim, padded, classes;

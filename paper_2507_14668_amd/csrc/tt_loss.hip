@@ -81,13 +81,14 @@ __global__ void __launch_bounds__(SCAN) k_loss_rows(const int64_t *labels, long 
     scale = __uint_as_float((unsigned)(127 + 13 + 127 - e) << 23);
     back = __uint_as_float((unsigned)(e - 13) << 23);
   }
-  if (apart && !own) back = all * 0x1p-13f;
+  const float raised = half ? TT_LOSS_RAISE : 1.f;  // (a bf16 G has the range, and its sums need theirs: of rows near 1e38 they would overflow)
+  if (apart && !own) back = all / raised;
   if (threadIdx.x == 0) w.back[0] = back;
 #pragma unroll 4
   for (int i = threadIdx.x; i < places; i += SCAN) {
     const float share = own ? grad[w.of[i]] : all;
     w.share[i] = share;
-    w.weight[i] = apart && !own ? 8192.f : scale * share;
+    w.weight[i] = apart && !own ? raised : scale * share;
   }
   if (negative && threadIdx.x < TT_LOSS_STEP && places + (int)threadIdx.x < (places + TT_LOSS_STEP - 1) / TT_LOSS_STEP * TT_LOSS_STEP) {
     w.lse[places + threadIdx.x] = -INFINITY;  // up to a whole step: rows that add nothing

@@ -25,7 +25,9 @@ using namespace ttg;
 // other half prefetched into registers does too, and loads through registers instead of straight into LDS took 742, 964 and 1052.
 constexpr int WAVES = 4, THREADS = 64 * WAVES, STEP = TT_LOSS_STEP;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
-constexpr float RAISE = 13.f;  // P is formed 2^13 times its size: fp16's smallest numbers then are of 2^-37, and P stays below 2^14
+// In fp16 P is formed 2^13 times its size: the smallest numbers then are of 2^-37, and P stays below 2^14.  bf16 has the range, and sums that need theirs.
+template <class T> constexpr float raise() { return std::is_same<T, f16>::value ? 13.f : 0.f; }
+template <class T> constexpr float raised() { return std::is_same<T, f16>::value ? TT_LOSS_RAISE : 1.f; }
 enum Mode { STATS, ROWS, CLASSES };
 // of 16 vectors, of a wavefront: what fits the registers
 __host__ __device__ constexpr int held_tiles(int KP, Mode mode, int parts) { return parts == 1 ? (mode != STATS && KP == 128 ? 3 : 4) : KP == 128 ? (mode == STATS ? 3 : 2) : (mode == STATS ? 4 : 3); }
@@ -208,7 +210,7 @@ __device__ __forceinline__ void step_of(const char *__restrict__ now, char *__re
           for (int i = 0; i < 4; ++i) {
             const int streamed = 16 * half + 4 * q + i;
             if (CLASS ? __shfl(label[0], streamed, 64) == 16 * x + j : label[CLASS ? 0 : x] == streamed)
-              S[half][x][i] = hot[CLASS ? streamed : 16 * x + j] * (SHARES ? 1.f : 8192.f);
+              S[half][x][i] = hot[CLASS ? streamed : 16 * x + j] * (SHARES ? 1.f : raised<T>());
           }
     }
     u16x8 P[H][PARTS];
@@ -291,7 +293,7 @@ template <class T, class O, int KP, Mode MODE, bool SHARES> __global__ void __la
 #pragma unroll
       for (int p = 0; p < PARTS; ++p)
         held[x][s][p] = *reinterpret_cast<const u16x8 *>((const unsigned short *)a.held + p * a.held_plane + h * KP + 32 * s + 8 * q);
-    constant[x] = MODE == STATS ? 3e38f /* less the largest so far: below all */ : fmaf(a.constants[h], LOG2E, SHARES ? 0.f : RAISE);
+    constant[x] = MODE == STATS ? 3e38f /* less the largest so far: below all */ : fmaf(a.constants[h], LOG2E, SHARES ? 0.f : raise<T>());
   }
   f32x4 acc[OUT ? D : 1][H] = {};  // [columns][held]; STATS: [0] what sums were 16 steps ago and before (a chain of additions stays short), [1] the logit that constant is of
   float sums[H] = {};
@@ -477,7 +479,7 @@ template <class T, int KP> __global__ void __launch_bounds__(TT_BLOCK) k_narrow_
     const int at = in ? n.r.at[r] : -1;
     f32x4 s = S::sum(parts, KP, cut, z.tile, at, room);
     if (!in || (together && seg != 0) || c >= n.dim || c >= KP) continue;
-    if (at >= 0) s *= 0x1p-13f * n.r.share[at];
+    if (at >= 0) s *= 1.f / raised<T>() * n.r.share[at];
     const float v[4] = {s[0], s[1], s[2], s[3]};
     store4(dx + r * ld + c, n.dim - c, v);
   }

@@ -551,6 +551,33 @@ def test_cross_entropy_special_logits(lib):
     assert loss.isnan().all()
 
 
+@pytest.mark.parametrize("reduction", ["none", "sum", "mean"])
+@pytest.mark.parametrize("dim,dtype", [(64, F32), (64, BF16), (100, BF16), (128, F32), (136, BF16), (200, F32), (200, BF16)])
+def test_cross_entropy_of_large_operands(lib, dim, dtype, reduction):
+    """Rows, then classes, near the type's largest number, and logits of ordinary size: gradients that the type holds are not lost on the way.  A row's numbers are `size` in one
+    column and 2 / size in another (a quarter for the second class), the classes' the other way round; each logit is one product of them, or two."""
+    from paper_2507_14668_amd import binding
+    size, up, classes = 2.0 ** 125, 2.0 ** -125, 9
+    for first, second in ((size, up), (up, size)):
+        x, w = torch.zeros(3, dim), torch.zeros(classes, dim)
+        x[0, 1], x[1, 1], x[2, 20] = first, -first, first / 2
+        w[2, 1], w[3, 1], w[4, 20] = 2 * second, -second, second / 2
+        labels = torch.tensor([2, 3, 4])
+        x, w = x.to(dtype), w.to(dtype)
+        grad = torch.ones(3 if reduction == "none" else 1)
+        want = ref.loss64(x, w, labels, reduction=reduction, grad=grad if reduction == "none" else grad[0])
+        op = binding.CLoss(DT[dtype], binding.REDUCTIONS[reduction], 3, dim, classes, -100)
+        ws = Guarded((1, max(lib.tt_cross_entropy_workspace_bytes(ctypes.byref(op), i) for i in (0, 1))), torch.uint8)
+        loss, stats, dx, dw, db = torch.empty(3), torch.empty(3, 2), torch.empty_like(x), torch.empty_like(w), torch.empty(classes, dtype=dtype)
+        call = (ctypes.byref(op), x.data_ptr(), w.data_ptr(), None, labels.data_ptr())
+        assert lib.tt_cross_entropy_forward(*call, loss.data_ptr(), stats.data_ptr(), ws.ptr, ws.cols, None) == 0
+        assert lib.tt_cross_entropy_backward(*call, stats.data_ptr(), grad.data_ptr(), dx.data_ptr(), dw.data_ptr(), db.data_ptr(), ws.ptr, ws.cols, None) == 0
+        ref.check(loss if reduction == "none" else loss[0], *want["loss"], "loss")
+        small = 2.0 ** -100 if dtype == F32 else 0.0  # (short fp32 rows: numbers below 2^-100 may have fewer bits)
+        for got, name in ((dx, "dx"), (dw, "dw"), (db, "dbias")):
+            ref.check(got, want[name][0], want[name][1] + small, name)
+
+
 def test_cross_entropy_refusals(lib):
     from paper_2507_14668_amd import binding
     x, w, b, lab, loss, lse = torch.zeros(4, 8), torch.zeros(10, 8), torch.zeros(10), torch.zeros(4, dtype=torch.int64), torch.zeros(4), torch.zeros(4, 2)

@@ -646,8 +646,8 @@ tt_status tt_expert_combine_backward(const tt_deal *op, const void *y, const int
  * G is formed again, a piece of the classes at a time (of rows of up to 128 elements it is never stored), and in 16 bits rounded to the
  * dtype before the products: without the share that all rows have of a sum or a mean, which is multiplied in at the end, and in fp16 by
  * powers of two that keep it in the range.  fp32 products are of three bf16 parts, as in tt_dense; those of rows of up to 128 elements do
- * without the fp32 instruction where parts cannot do (numbers below 2^-100 have fewer bits, numbers that bf16 cannot hold give NaN, and a
- * row with a logit beyond 2^127 has NaN gradients).  Losses and lse are float whatever the dtype.
+ * without the fp32 instruction where parts cannot do (numbers below 2^-100 have fewer bits, numbers that bf16 cannot hold give NaN).  Losses
+ * and lse are float whatever the dtype: lse is rounded by up to 2^-24 of itself, and G's probabilities are off by that, relative to their size.
  *   labels DEVICE int64[rows];  stats DEVICE float[rows][2]: the log of the sum and the loss of each row, 0 in rows that do not
  *   count; written by the forward (not NULL), read by the backward (which forms the label's softmax - 1 from the loss: its
  *   relative precision lasts where a row is nearly sure)

@@ -41,8 +41,7 @@ __global__ void __launch_bounds__(SCAN) k_loss_rows(const int64_t *labels, long 
       w.label[at] = label[i] >= 0 && label[i] < classes ? (int32_t)label[i] : -1;
       if (of_rows) {
         const float2 s = of_rows[r];
-        // (short rows multiply lse by log2 e: beyond 2^127 it counts as NaN)
-        w.lse[at] = !negative ? s.x : fabsf(s.x) < 0x1p127f ? -s.x : NAN;
+        w.lse[at] = negative ? -s.x : s.x;
         w.hot[at] = expm1f(-s.y);
       }
       ++at;

@@ -1,4 +1,6 @@
 // Softmax cross entropy of short rows (up to 128 elements): nothing of the size rows x classes is ever stored.
+#include <float.h>
+
 #include "tt_gemm_device.h"
 #include "tt_loss.h"
 
@@ -14,8 +16,9 @@ using namespace ttg;
 // over the streamed ones: two tiles of 16 of P = exp(S - ..) are, as they lie in the registers, an operand of 32 terms, whose order 4 q + i | 16 +
 // 4 q + i the transposing LDS reads of the other operand follow.  So P goes from matrix instruction to matrix instruction through exp and a
 // rounding alone; it is never in memory.
-// What is added to a logit comes for nothing: of the streamed vector (the class's bias, or a row's -lse) as the product's starting value, of the held
-// one in the multiply-add before exp2.
+// A class's bias is the product's starting value, in all three, so that all have the same bits of a logit.  What the row has (the reference of its statistics, or lse) is taken off
+// before the difference is scaled for exp2: in one multiply-add with that it would be rounded in the size of the logits, and e to the power of that is what all probabilities
+// are off by (14 % at logits of 2^20).
 // fp32 operands come in PARTS = 3 planes of bf16 (tt_split_bf16), P is split as it is formed, and six of the nine products count, as in the other fp32
 // products; what they redo with the fp32 instruction (numbers below 2^-100 in size, or near the range's end) has fewer bits here, or is NaN.
 // 512 registers of a SIMD's lane are two wavefronts of 256: 48 of the held operand (three tiles of 16), 96 of the sums, 24 of S.
@@ -24,7 +27,7 @@ using namespace ttg;
 // them, and two wavefronts a SIMD do not hide the one behind the other; the clock falls to 2.2 GHz.  Four held tiles spill, a step of the
 // other half prefetched into registers does too, and loads through registers instead of straight into LDS took 742, 964 and 1052.
 constexpr int WAVES = 4, THREADS = 64 * WAVES, STEP = TT_LOSS_STEP;
-constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+constexpr float LOG2E = 1.4426950408889634f;
 // In fp16 P is formed 2^13 times its size: the smallest numbers then are of 2^-37, and P stays below 2^14.  bf16 has the range, and sums that need theirs.
 template <class T> constexpr float raise() { return std::is_same<T, f16>::value ? 13.f : 0.f; }
 template <class T> constexpr float raised() { return std::is_same<T, f16>::value ? TT_LOSS_RAISE : 1.f; }
@@ -64,8 +67,8 @@ __host__ __device__ constexpr Sizes sizes_of(int KP, Mode mode, int parts) {
 
 struct Args {
   const void *held, *streamed;
-  const float *starts;       // of streamed vectors, -infinity behind the last one, whole steps
-  const float *constants;    // of held vectors
+  const float *starts;       // of streamed vectors: the bias, or a row's -lse; -infinity behind the last one, whole steps
+  const float *constants;    // of held vectors: a row's -lse, or the bias
   const float *weight;       // CLASSES with shares: of the rows, whole steps
   const int32_t *label;      // of the rows, whole steps
   const float *hot;          // of the rows: the label's softmax less one
@@ -104,11 +107,13 @@ template <int KP> __device__ __forceinline__ u16x8 frag_across(const unsigned sh
   return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
-// A step's LDS: the tile, then of its vectors what they start at and the shares.
+__device__ __forceinline__ f32x4 all_of(float v) { return f32x4{v, v, v, v}; }
+
+// A step's LDS: the tile, then of its vectors `starts` and the shares.
 template <int KP, int PARTS> constexpr int step_bytes() { return STEP * KP * 2 * PARTS + 2 * STEP * 4; }
 
 // What a thread fetches of a step.  The tile's 16-byte pieces go from memory into LDS, lane after lane; which piece a lane fetches makes their order
-// there.  A vector behind the last one is the last one again: it starts at -infinity, and its P is zero.
+// there.  A vector behind the last one is the last one again, with -infinity: its P is zero.
 template <int KP, Mode MODE, bool SHARES, int PARTS> struct Fetcher {
   const unsigned short *streamed;
   long long plane;
@@ -153,7 +158,7 @@ __device__ __forceinline__ void step_of(const char *__restrict__ now, char *__re
   f32x4 S[2][H];
 #pragma unroll
   for (int half = 0; half < 2; ++half) {  // 16 streamed vectors
-    const f32x4 from = *reinterpret_cast<const f32x4 *>(starts + 16 * half + 4 * q);
+    const f32x4 of_streamed = *reinterpret_cast<const f32x4 *>(starts + 16 * half + 4 * q);
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
       u16x8 f[PARTS];
@@ -165,7 +170,7 @@ __device__ __forceinline__ void step_of(const char *__restrict__ now, char *__re
 #pragma unroll
         for (int p = 0; p <= d; ++p)
 #pragma unroll
-          for (int x = 0; x < H; ++x) S[half][x] = mma(T(), f[d - p], held[x][s][p], s || d != PARTS - 1 || p ? S[half][x] : from);
+          for (int x = 0; x < H; ++x) S[half][x] = mma(T(), f[d - p], held[x][s][p], s || d != PARTS - 1 || p ? S[half][x] : CLASS ? all_of(constant[x]) : of_streamed);
     }
     if constexpr (MODE == STATS) {
       if (hit) {
@@ -178,26 +183,25 @@ __device__ __forceinline__ void step_of(const char *__restrict__ now, char *__re
 #pragma unroll
       for (int x = 0; x < H; ++x) {
         const float top = fmaxf(fmaxf(S[half][x][0], S[half][x][1]), fmaxf(S[half][x][2], S[half][x][3]));
-        // what exp2 gets stays below 16, so that the sum stays far from the range's end; seldom after the first steps
-        const bool above = fmaf(top, LOG2E, constant[x]) > 16.f;
+        // what is added up stays below e^11, so that the sum stays far from the range's end; seldom after the first steps
+        const bool above = top - constant[x] > 11.f;
         if (__ballot(above)) {
-          const float now = above ? -top * LOG2E : constant[x];
-          const float by = above ? __builtin_amdgcn_exp2f(now - constant[x]) : 1.f;
+          const float now = above ? top : constant[x];
+          const float by = above ? __builtin_amdgcn_exp2f((constant[x] - now) * LOG2E) : 1.f;
           sums[x] *= by;
           acc[0][x][0] *= by;
-          acc[0][x][1] = above ? top : acc[0][x][1];
           constant[x] = now;
         }
         float e[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) e[i] = __builtin_amdgcn_exp2f(fmaf(S[half][x][i], LOG2E, constant[x]));
+        for (int i = 0; i < 4; ++i) e[i] = __builtin_amdgcn_exp2f((S[half][x][i] - constant[x]) * LOG2E);
         sums[x] += (e[0] + e[1]) + (e[2] + e[3]);
       }
     } else {
 #pragma unroll
       for (int x = 0; x < H; ++x)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) S[half][x][i] = __builtin_amdgcn_exp2f(fmaf(S[half][x][i], LOG2E, constant[x]));
+        for (int i = 0; i < 4; ++i) S[half][x][i] = __builtin_amdgcn_exp2f(fmaf(S[half][x][i] + (CLASS ? of_streamed[i] : constant[x]), LOG2E, SHARES ? 0.f : raise<T>()));
     }
   }
   if constexpr (OUT) {
@@ -254,16 +258,10 @@ __device__ __forceinline__ void step_of(const char *__restrict__ now, char *__re
   }
 }
 
-// Statistics of two sets of a row's logits: m, about the largest in units of log 2, and s, the sum of 2^(logit - m).  Where a logit is so large that
-// its m is infinite, that logit alone counts and is what s holds.
+// Statistics of two sets of a row's logits: m, about the largest, and s, the sum of exp(logit - m).  (A NaN or +infinity among them makes s NaN.)
 __device__ __forceinline__ float2 join_runs(float2 a, float2 b) {
-  if (a.x == INFINITY || b.x == INFINITY) {
-    const float y = a.x != INFINITY ? -INFINITY : a.y, z = b.x != INFINITY ? -INFINITY : b.y;
-    const bool bad = a.y != a.y || b.y != b.y;
-    return float2{INFINITY, bad ? NAN : fmaxf(y, z)};
-  }
   const float top = fmaxf(a.x, b.x), base = top == -INFINITY ? 0.f : top;
-  return float2{top, a.y * __builtin_amdgcn_exp2f(a.x - base) + b.y * __builtin_amdgcn_exp2f(b.x - base)};
+  return float2{top, a.y * __builtin_amdgcn_exp2f((a.x - base) * LOG2E) + b.y * __builtin_amdgcn_exp2f((b.x - base) * LOG2E)};
 }
 
 // T: of the products; O: of dW and dbias
@@ -284,7 +282,7 @@ template <class T, class O, int KP, Mode MODE, bool SHARES> __global__ void __la
   const long long s0 = run * per * STEP, s1 = s0 + per * STEP < streamed_count ? s0 + per * STEP : streamed_count;
 
   u16x8 held[H][KS][PARTS];
-  float constant[H];  // of the held vector, in units of log 2
+  float constant[H];  // of the held vector
 #pragma unroll
   for (int x = 0; x < H; ++x) {
     const long long h = h0 + 16 * x + j < held_count ? h0 + 16 * x + j : held_count - 1;  // (of vectors outside nothing is written)
@@ -293,9 +291,9 @@ template <class T, class O, int KP, Mode MODE, bool SHARES> __global__ void __la
 #pragma unroll
       for (int p = 0; p < PARTS; ++p)
         held[x][s][p] = *reinterpret_cast<const u16x8 *>((const unsigned short *)a.held + p * a.held_plane + h * KP + 32 * s + 8 * q);
-    constant[x] = MODE == STATS ? 3e38f /* less the largest so far: below all */ : fmaf(a.constants[h], LOG2E, SHARES ? 0.f : raise<T>());
+    constant[x] = MODE == STATS ? -FLT_MAX /* the largest so far, about: below all */ : a.constants[h];
   }
-  f32x4 acc[OUT ? D : 1][H] = {};  // [columns][held]; STATS: [0] what sums were 16 steps ago and before (a chain of additions stays short), [1] the logit that constant is of
+  f32x4 acc[OUT ? D : 1][H] = {};  // [columns][held]; STATS: [0] what sums were 16 steps ago and before (a chain of additions stays short)
   float sums[H] = {};
 
   const int row = (int)threadIdx.x / (KP / 8);
@@ -345,9 +343,7 @@ template <class T, class O, int KP, Mode MODE, bool SHARES> __global__ void __la
 #pragma unroll
     for (int x = 0; x < H; ++x) {  // four lanes have a row's columns
       sums[x] += acc[0][x][0];
-      float2 mine = {-constant[x], sums[x]};
-      if (constant[x] == 3e38f) mine.x = -INFINITY;  // nothing but -infinity (or NaN, which the sum has)
-      if (constant[x] == -INFINITY) mine.y = sums[x] == sums[x] ? acc[0][x][1] : sums[x];
+      float2 mine = {sums[x] == 0.f ? -INFINITY : constant[x], sums[x]};  // (0: nothing but -infinity)
 #pragma unroll
       for (int o = 16; o < 64; o *= 2) mine = join_runs(mine, float2{__shfl(mine.x, lane ^ o, 64), __shfl(mine.y, lane ^ o, 64)});
       if (q == 0) reinterpret_cast<float2 *>(a.parts)[(long long)blockIdx.x * tile_of(KP, MODE, PARTS) + first + 16 * x + j] = mine;
@@ -431,10 +427,8 @@ __global__ void __launch_bounds__(TT_BLOCK) k_narrow_fold(TTNarrow n, const floa
   if (lane != 0) return;
   const bool bad = n.r.label[i] < 0;
   const int r = n.r.of[i];
-  const float more = log2f(s.y), logit = bad ? 0.f : picked[i];  // (of the same products: the largest logit less itself is zero)
-  float2 of = {(s.x + more) * LN2, (fmaf(-logit, LOG2E, s.x) + more) * LN2};
-  if (s.x == INFINITY) of = float2{s.y, s.y - logit};
-  if (bad) of = float2{NAN, NAN};
+  const float more = logf(s.y), logit = bad ? 0.f : picked[i];  // (of the same products: the largest logit less itself is zero)
+  const float2 of = bad ? float2{NAN, NAN} : float2{s.x + more, (s.x - logit) + more};
   each[r] = of;
   if (loss) loss[r] = of.y;
 }

@@ -6,7 +6,7 @@ import pytest
 import torch
 
 import top_ref as ref
-from test_top_emulation import FAR_ROUTES, LOSSES, ROUTES, routed
+from test_top_emulation import FAR_ROUTES, LARGE, LOSSES, ROUTES, large_logits, large_logits64, routed
 
 pytestmark = pytest.mark.gpu
 F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
@@ -285,6 +285,26 @@ def test_gradients_of_nearly_sure_rows(tt, dim, dtype):
         check(got, want[name], name)
         off = (got.double().cpu() - want[name][0]).norm() / want[name][0].norm()
         assert off < 3 * torch.finfo(dtype).eps + 4 * (dim + 2) * ref.U * 14 + 8 * ref.U / (1 - p), (name, float(off))
+
+
+@pytest.mark.parametrize("size", LARGE)
+@pytest.mark.parametrize("dim,dtype", [(64, F32), (64, BF16), (50, F16), (100, BF16), (128, F32), (136, BF16), (200, F32)])
+@pytest.mark.parametrize("biased", [False, True])
+def test_cross_entropy_of_large_logits(tt, size, dim, dtype, biased):
+    """Finite logits of any size, far apart: losses to fp32's precision and never below zero, gradients of zeros and ones."""
+    if dtype == F16:
+        size = min(size, 2.0 ** 24 if not biased else 2.0 ** 14)
+    x, w, b, labels = large_logits(size, dim, dtype, biased)
+    grad = torch.tensor([1.0, -2.0, 0.5, 1.0, 2.0, 1.0, 0.25])
+    want = large_logits64(x, w, b, labels, grad)
+    leaves = [put(t).requires_grad_() for t in (x, w, b) if t is not None]
+    loss = tt.tt_cross_entropy(leaves[0], leaves[1], labels.cuda(), leaves[2] if biased else None, reduction="none")
+    assert bool((loss >= 0).all())
+    check(loss, want["loss"], "loss")
+    beyond = 2.0 ** 16 if dtype == F16 else math.inf  # (what rounds to fp16's infinity)
+    for got, name in zip(torch.autograd.grad(loss, leaves, grad.cuda()), ("dx", "dw", "dbias")):
+        ref.check(got.cpu().float().clamp(-beyond, beyond), want[name][0] if name != "dbias" else want[name][0][:, 0],
+                  want[name][1] if name != "dbias" else want[name][1][:, 0], name)
 
 
 def test_no_rows(tt):

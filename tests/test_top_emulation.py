@@ -578,6 +578,104 @@ def test_cross_entropy_of_large_operands(lib, dim, dtype, reduction):
             ref.check(got, want[name][0], want[name][1] + small, name)
 
 
+LARGE = [2.0 ** 12, 2.0 ** 20, 2.0 ** 24, 2.0 ** 27, 2.0 ** 32, 1e19, 2.0 ** 100, 1e38]
+
+
+def large_logits(size, dim, dtype, biased):
+    """x, w, bias and labels of rows whose largest logits are `size` and 1.5 times that (rounded to the type), nothing near them: every probability is 0 or 1."""
+    classes, scale = 40, 2.0 ** 10  # (a logit is one product)
+    z = torch.zeros(7, classes)
+    z[0, 5], z[0, 9] = size, 1.5 * size
+    z[1, 5], z[1, 9] = size, 1.5 * size
+    z[2], z[2, 30] = -1.5 * size, -size
+    z[3], z[3, 30] = -1.5 * size, -size
+    z[4, 17] = size
+    z[5, 17] = -size
+    z[5, 18] = size
+    z[6, 39], z[6, 0] = 1.25 * size, -size
+    labels = torch.tensor([5, 9, 0, 30, 3, 17, 39])
+    x, w, b = torch.zeros(7, dim), torch.zeros(classes, dim), None
+    w[torch.arange(classes), torch.arange(classes)] = scale
+    x[:, :classes] = z / scale
+    if biased:  # the same logits, less what the bias has
+        b = torch.zeros(classes)
+        b[9], b[30] = size / 4, size / 4
+    return x.to(dtype), w.to(dtype), None if b is None else b.to(dtype), labels
+
+
+def large_logits64(x, w, b, labels, grad):
+    """loss, dx, dw and dbias in 64 bits with their tolerances: one product and one sum make a logit, and G is exact, so that fp32 rounds a logit twice, the loss twice more, and
+    sums over rows by 2 (rows + 2) u of their terms."""
+    dtype, x, w = x.dtype, x.double(), w.double()
+    bias = torch.zeros(w.shape[0], dtype=torch.float64) if b is None else b.double()
+    z = x @ w.t() + bias
+    lse, zl = torch.logsumexp(z, 1), z.gather(1, labels[:, None])[:, 0]
+    G = (torch.exp(z - lse[:, None]) - torch.zeros_like(z).scatter_(1, labels[:, None], 1.0)) * grad.double()[:, None]
+    assert bool(((G == 0) | (G.abs() == grad.double().abs()[:, None])).all())
+    result = dict(loss=(lse - zl, 2 * ref.U * (2 * (lse - zl).abs() + lse.abs() * (b is not None) + zl.abs() * (b is not None))))
+    for name, a, c in (("dx", G, w), ("dw", G.t(), x), ("dbias", G.t(), torch.ones(x.shape[0], 1, dtype=torch.float64))):
+        v, size = a @ c, a.abs() @ c.abs()
+        result[name] = (v, 2 * (x.shape[0] + 2) * ref.U * size + ref.rounding(v, dtype))
+    return result
+
+
+@pytest.mark.parametrize("size", LARGE)
+@pytest.mark.parametrize("dim,dtype", [(64, F32), (64, BF16), (50, F16), (100, BF16), (128, F32), (136, BF16), (200, F32)])
+@pytest.mark.parametrize("biased,reduction", [(False, "none"), (True, "none"), (True, "sum")])
+def test_cross_entropy_of_large_logits(lib, size, dim, dtype, biased, reduction):
+    """Finite logits of any size, far apart: losses to fp32's precision and never below zero, gradients of zeros and ones."""
+    from paper_2507_14668_amd import binding
+    if dtype == F16:
+        size = min(size, 2.0 ** 24 if not biased else 2.0 ** 14)
+    x, w, b, labels = large_logits(size, dim, dtype, biased)
+    grad = torch.tensor([1.0, -2.0, 0.5, 1.0, 3.0, 1.0, 0.25]) if reduction == "none" else torch.ones(7)
+    want = large_logits64(x, w, b, labels, grad)
+    gx, gw, gb, gl, gg = place(x), place(w), place(None if b is None else b[None]), place(labels[None]), place(grad[None, :7 if reduction == "none" else 1])
+    op = binding.CLoss(DT[dtype], binding.REDUCTIONS[reduction], 7, dim, 40, -100)
+    ws = Guarded((1, max(lib.tt_cross_entropy_workspace_bytes(ctypes.byref(op), i) for i in (0, 1))), torch.uint8)
+    loss, stats = Guarded((1, 7), F32), Guarded((7, 2), F32)
+    dx, dw, db = Guarded((7, dim), dtype), Guarded((40, dim), dtype), Guarded((1, 40), dtype)
+    call = (ctypes.byref(op), gx.ptr, gw.ptr, ptr(gb), gl.ptr)
+    assert lib.tt_cross_entropy_forward(*call, loss.ptr, stats.ptr, ws.ptr, ws.cols, None) == 0
+    assert lib.tt_cross_entropy_backward(*call, stats.ptr, gg.ptr, dx.ptr, dw.ptr, db.ptr, ws.ptr, ws.cols, None) == 0
+    assert bool((stats.t[:, 1] >= 0).all())
+    ref.check(stats.t[:, 1], *want["loss"], "loss")
+    beyond = 2.0 ** 16 if dtype == F16 else math.inf  # (what rounds to fp16's infinity: 3 times 2^24 / 2^10 and more)
+    for got, name in ((dx.t, "dx"), (dw.t, "dw"), (db.t.t(), "dbias")):
+        ref.check(got.float().clamp(-beyond, beyond), *want[name], name)
+    intact(gx, gw, gb, gl, gg, ws, stats, dx, dw, db)
+
+
+@pytest.mark.parametrize("std", [20.0, 60.0])
+@pytest.mark.parametrize("dim", [64, 128])
+def test_cross_entropy_gradients_of_rows_and_classes_are_as_good(lib, dim, std):
+    """fp32, short rows, an lse of some ten to hundred: dx, dW and dbias come of the same softmax.  A probability is off by the error of a logit (twice dim + 2 units of the sum of its terms'
+    sizes, 6 for the parts' dropped terms), of lse (its own rounding, and a row's error of the same kind) and of exp2's argument; G's errors go into the sums in the 2-norm
+    no more than G's size times that; the sums add rows + 2 and classes + 2 units.  Chains that started at -lse lost ulp(lse) at every step: 2e-5 and 6e-5."""
+    from paper_2507_14668_amd import binding
+    gen = torch.Generator().manual_seed(dim)
+    rows, classes = 48, 700
+    x, w, labels = randn(gen, rows, dim), randn(gen, classes, dim, std=std * dim ** -0.5), torch.randint(0, classes, (rows,), generator=gen)
+    z = x.double() @ w.double().t()
+    lse, grad = torch.logsumexp(z, 1), torch.ones(1)
+    G = torch.softmax(z, 1)
+    G[torch.arange(rows), labels] = -(1 - G[torch.arange(rows), labels])
+    op = binding.CLoss(0, binding.REDUCTIONS["sum"], rows, dim, classes, -100)
+    ws = Guarded((1, max(lib.tt_cross_entropy_workspace_bytes(ctypes.byref(op), i) for i in (0, 1))), torch.uint8)
+    loss, stats, dx, dw, db = torch.empty(1), torch.empty(rows, 2), torch.empty_like(x), torch.empty_like(w), torch.empty(classes)
+    call = (ctypes.byref(op), x.data_ptr(), w.data_ptr(), None, labels.data_ptr())
+    assert lib.tt_cross_entropy_forward(*call, loss.data_ptr(), stats.data_ptr(), ws.ptr, ws.cols, None) == 0
+    assert lib.tt_cross_entropy_backward(*call, stats.data_ptr(), grad.data_ptr(), dx.data_ptr(), dw.data_ptr(), db.data_ptr(), ws.ptr, ws.cols, None) == 0
+    # random roundings of a chain of dim / 8 additions of partial sums up to |z| (the instruction adds eight products at a time): sqrt of their number, three deviations
+    logit = 3 * ref.U * math.sqrt(dim / 8 * 6) * float(z.abs().max())
+    most = 2 * logit + 2 * ref.U * float(lse.max()) + 32 * ref.U
+    off = {}
+    for got, want, name in ((dx, G @ w.double(), "dx"), (dw, G.t() @ x.double(), "dw"), (db, G.sum(0), "dbias")):
+        off[name] = float((got.double() - want).norm() / want.norm())
+        assert off[name] <= most, (name, off, most)
+    assert max(off.values()) <= 8 * off["dx"] + 8 * ref.U, off
+
+
 def test_cross_entropy_refusals(lib):
     from paper_2507_14668_amd import binding
     x, w, b, lab, loss, lse = torch.zeros(4, 8), torch.zeros(10, 8), torch.zeros(10), torch.zeros(4, dtype=torch.int64), torch.zeros(4), torch.zeros(4, 2)

@@ -649,8 +649,8 @@ tt_status tt_expert_combine_backward(const tt_deal *op, const void *y, const int
  * without the fp32 instruction where parts cannot do (numbers below 2^-100 have fewer bits, numbers that bf16 cannot hold give NaN).  Losses
  * and lse are float whatever the dtype: lse is rounded by up to 2^-24 of itself, and G's probabilities are off by that, relative to their size.
  *   labels DEVICE int64[rows];  stats DEVICE float[rows][2]: the log of the sum and the loss of each row, 0 in rows that do not
- *   count; written by the forward (not NULL), read by the backward (which forms the label's softmax - 1 from the loss: its
- *   relative precision lasts where a row is nearly sure)
+ *   count; written by the forward (not NULL), read by the backward (which forms the label's softmax - 1 from the loss; the
+ *   loss is of the other classes' share beside the label, so the relative precision of both lasts however sure a row is, and no loss is below zero)
  *   workspace DEVICE, 256-byte aligned, tt_cross_entropy_workspace_bytes(op, backward) (0 on invalid arguments)
  */
 typedef enum { TT_REDUCE_NONE = 0, TT_REDUCE_SUM = 1, TT_REDUCE_MEAN = 2 } tt_reduce;

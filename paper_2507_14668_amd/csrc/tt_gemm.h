@@ -17,7 +17,7 @@
 // are the softmax loss's (tt_loss.hip), each for the layouts that it needs: rows of z by K-contiguous operands, ACC with a
 // row-contiguous B, SCALED with both row-contiguous.
 #define TT_GEMM_PLAIN 0
-#define TT_GEMM_STATS 1    // nothing is stored but, of each row's columns in the tile, the largest z and the sum of exp(z - it), and the label's z
+#define TT_GEMM_STATS 1    // nothing is stored but, of each row's columns in the tile, the largest z and the sum of exp(z - it), the label's z apart
 #define TT_GEMM_SOFTMAX 2  // out = (n is the label ? hot[m] : exp(z - lse[m])) * row_grad[m], zeros in columns N .. n_padded - 1
 #define TT_GEMM_ACC 3      // acc[m][n] = z, plus what is there if acc_add, in fp32
 #define TT_GEMM_SCALED 4   // out and rowsum times *scale

@@ -420,7 +420,7 @@ __device__ __forceinline__ void finish_acc(const TTGemm &g, int z, int m, int n,
   store_n<float, 8>(to, valid, t);
 }
 // Of each row of a wavefront's results (as in finish_tile, in its registers still) the largest z and the sum of exp(z - it), over its columns,
-// to `stats` (LDS, a pair for each of the wavefront's rows); the label's z to picked.  A lane has 4 FY columns of FX rows, four lanes a row.
+// to `stats` (LDS, a pair for each of the wavefront's rows); the label's z to picked, and not into these.  A lane has 4 FY columns of FX rows, four lanes a row.
 // Columns of -infinity count as nothing; a NaN is in the sum.
 template <class T, int FX, int FY> __device__ __forceinline__ void tile_stats(const TTGemm &g, int z, int m0, int end, int n0, const f32x4 (&acc)[FX][FY], float2 *stats) {
   const int lane = threadIdx.x & 63, q = lane >> 4, j = lane & 15;
@@ -443,7 +443,10 @@ template <class T, int FX, int FY> __device__ __forceinline__ void tile_stats(co
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         v[y][i] = fmaf(g.alpha, acc[x][y][i], bias[y][i]);
-        if (label == 16 * y + i && n0 + 16 * y + 4 * q + i < g.N) g.picked[m] = v[y][i];
+        if (label == 16 * y + i && n0 + 16 * y + 4 * q + i < g.N) {
+          g.picked[m] = v[y][i];
+          v[y][i] = -INFINITY;
+        }
         top = fmaxf(top, v[y][i]);
       }
     top = fmaxf(top, __shfl(top, lane ^ 16, 64));

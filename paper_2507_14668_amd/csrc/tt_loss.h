@@ -32,6 +32,19 @@ struct TTNarrow {
   float *starts;            // [classes], and up to whole steps of TT_LOSS_STEP
 };
 
+// A row's lse and loss from the label's logit and the statistics of the other classes: m, a logit among them that the largest exceeds by little (-infinity: there is none), and s, the
+// sum of exp(logit - m).  Where the label's is above, the loss is log1p of what the others have beside it, and keeps its relative precision down to the smallest numbers; else both
+// terms are of one sign.  So it is never below zero.
+__device__ __forceinline__ float2 row_of_loss(float2 others, float label) {
+  if (!(label < INFINITY)) return float2{NAN, NAN};
+  if (label > others.x) {
+    const float loss = log1pf(others.y * expf(others.x - label));
+    return float2{label + loss, loss};
+  }
+  const float more = logf(others.y + expf(label - others.x));
+  return float2{others.x + more, (others.x - label) + more};
+}
+
 bool ttk_narrow_serves(int dim);
 int ttk_narrow_padded(int dim);
 size_t ttk_narrow_stats_bytes(const TTNarrow &n);  // (sizes alone are looked at)

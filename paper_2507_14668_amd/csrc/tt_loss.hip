@@ -130,7 +130,10 @@ __global__ void __launch_bounds__(TT_BLOCK) k_loss_pairs(const float *__restrict
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         v[k][e] = c + e < n ? a[e] : -INFINITY;
-        if (c + e == label && c + e < n) picked[i] = a[e];
+        if (c + e == label && c + e < n) {  // (in no sum: row_of_loss)
+          picked[i] = a[e];
+          v[k][e] = -INFINITY;
+        }
         top = fmaxf(top, v[k][e]);
       }
     }
@@ -188,11 +191,8 @@ __global__ void __launch_bounds__(TT_BLOCK) k_loss_fold(const float2 *__restrict
     run[i] = s;
     return;
   }
-  const bool bad = w.label[i] < 0;
   const int r = w.of[i];
-  // (the difference of the logits first: near a loss of zero lse less the label's logit would be lse's rounding)
-  const float more = logf(s.y);
-  each[r] = bad ? float2{NAN, NAN} : float2{s.x + more, (s.x - picked[i]) + more};
+  each[r] = w.label[i] < 0 ? float2{NAN, NAN} : row_of_loss(s, picked[i]);
   if (loss) loss[r] = each[r].y;
 }
 // One workgroup: the sum or the mean, in 64 bits.

@@ -9,7 +9,7 @@ using namespace ttg;
 
 // Three kernels of one build.  A wavefront holds 64 vectors (`held`) in its registers as one operand of the products, and a workgroup of four
 // streams the others through LDS, 32 at a time, as the other:
-//   STATS    held rows, streamed classes: running largest logit and sum of exponentials of each row
+//   STATS    held rows, streamed classes: running largest logit and sum of exponentials of each row, its label's apart
 //   ROWS     held rows, streamed classes: dx^T += W^T P
 //   CLASSES  held classes, streamed rows: dW^T += x^T P (and its sums: dbias)
 // The first product's result S (streamed x held) leaves a lane four neighbouring streamed vectors of one held one, and the second product sums
@@ -143,7 +143,7 @@ template <int KP, Mode MODE, bool SHARES, int PARTS> struct Fetcher {
 // which else has every read wait for the loads.)
 // hit: a label of the rows is among the classes here, which few steps have; one branch, since what is on its two sides is not
 // interleaved.  `label`: of the held rows, less the step's first class; CLASSES lane l's is row l's, less the first held class.
-// STATS gives the label's logit out there.  The others have the label's softmax less one, which the loss says to its last bits (`hot`, of the held rows or, CLASSES,
+// STATS gives the label's logit out there, and leaves it out of its sums (row_of_loss).  The others have the label's softmax less one, which the loss says to its last bits (`hot`, of the held rows or, CLASSES,
 // of the step's): where a row is nearly sure of its label, exp(z - lse) - 1 would be the rounding of lse.
 template <class T, int KP, Mode MODE, bool SHARES, int PARTS, int H, int DO>
 __device__ __forceinline__ void step_of(const char *__restrict__ now, char *__restrict__ next, const Fetcher<KP, MODE, SHARES, PARTS> &fetcher, long long ahead,
@@ -178,7 +178,10 @@ __device__ __forceinline__ void step_of(const char *__restrict__ now, char *__re
         for (int x = 0; x < H; ++x)
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            if (label[x] == 16 * half + 4 * q + i) picked[16 * x + j] = S[half][x][i];
+            if (label[x] == 16 * half + 4 * q + i) {
+              picked[16 * x + j] = S[half][x][i];
+              S[half][x][i] = -INFINITY;
+            }
       }
 #pragma unroll
       for (int x = 0; x < H; ++x) {
@@ -425,10 +428,8 @@ __global__ void __launch_bounds__(TT_BLOCK) k_narrow_fold(TTNarrow n, const floa
 #pragma unroll
   for (int o = 1; o < 64; o *= 2) s = join_runs(s, float2{__shfl(s.x, lane ^ o, 64), __shfl(s.y, lane ^ o, 64)});
   if (lane != 0) return;
-  const bool bad = n.r.label[i] < 0;
   const int r = n.r.of[i];
-  const float more = logf(s.y), logit = bad ? 0.f : picked[i];  // (of the same products: the largest logit less itself is zero)
-  const float2 of = bad ? float2{NAN, NAN} : float2{s.x + more, (s.x - logit) + more};
+  const float2 of = n.r.label[i] < 0 ? float2{NAN, NAN} : row_of_loss(s, picked[i]);
   each[r] = of;
   if (loss) loss[r] = of.y;
 }

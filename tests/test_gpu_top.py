@@ -6,7 +6,7 @@ import pytest
 import torch
 
 import top_ref as ref
-from test_top_emulation import FAR_ROUTES, LARGE, LOSSES, ROUTES, large_logits, large_logits64, routed
+from test_top_emulation import FAR_ROUTES, LARGE, LOSSES, ROUTES, large_logits, large_logits64, routed, sure_rows, sure_rows64
 
 pytestmark = pytest.mark.gpu
 F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
@@ -305,6 +305,21 @@ def test_cross_entropy_of_large_logits(tt, size, dim, dtype, biased):
     for got, name in zip(torch.autograd.grad(loss, leaves, grad.cuda()), ("dx", "dw", "dbias")):
         ref.check(got.cpu().float().clamp(-beyond, beyond), want[name][0] if name != "dbias" else want[name][0][:, 0],
                   want[name][1] if name != "dbias" else want[name][1][:, 0], name)
+
+
+@pytest.mark.parametrize("dim,dtype", [(64, F32), (64, BF16), (80, F16), (128, F32), (128, BF16), (136, F32), (136, BF16), (200, F16)])
+def test_cross_entropy_of_sure_rows(tt, dim, dtype):
+    """Row by row: the losses and gradients of rows that are nearly sure of their label keep their relative precision, however small they are."""
+    x, w, labels = sure_rows(dim, dtype, 50)
+    loss64, eloss, G, eG = sure_rows64(x, w, labels)
+    if dtype != F32:
+        eG = eG + 2.01 * torch.finfo(dtype).eps / 2 * G.abs() + (2.0 ** -37 if dtype == F16 else 2.0 ** -133)
+    leaf = put(x).requires_grad_()
+    loss = tt.tt_cross_entropy(leaf, put(w), labels.cuda(), reduction="none")
+    check(loss, (loss64, eloss), "loss")
+    (dx,) = torch.autograd.grad(loss, leaf, torch.ones_like(loss))
+    check(dx[:, :64], (G, eG + ref.rounding(G, dtype)), "dx")
+    assert not dx[:, 64:].any()
 
 
 def test_no_rows(tt):

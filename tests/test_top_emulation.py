@@ -676,6 +676,71 @@ def test_cross_entropy_gradients_of_rows_and_classes_are_as_good(lib, dim, std):
     assert max(off.values()) <= 8 * off["dx"] + 8 * ref.U, off
 
 
+# a row's label's logit and the others' (all classes, then the first ones): sure of its label by 3 to 60, near zero and near 1000
+SURE = [(3.0, 0.0, []), (8.0, 0.0, [-1.0, 0.5]), (10.5, 0.0, [1.0]), (11.0, 0.0, []), (11.5, 0.0, [0.25, -3.0]), (17.0, -2.0, [1.0]), (24.0, 0.0, []), (40.0, -1.0, [2.0]), (60.0, 0.0, []),
+        (1000.0, 992.0, []), (1000.0, 960.0, [988.0]), (-8.0, -20.0, [-16.0]), (0.0, 0.0, []), (-5.0, 1.0, [7.0, 7.0])]
+
+
+def sure_rows(dim, dtype, label):
+    """x, w and labels with exactly the logits above: a logit is one product with 1."""
+    classes = 64
+    x, w = torch.zeros(len(SURE), dim), torch.zeros(classes, dim)
+    w[torch.arange(classes), torch.arange(classes)] = 1.0
+    for r, (own, rest, more) in enumerate(SURE):
+        x[r, :classes] = rest
+        x[r, :len(more)] = torch.tensor(more)
+        x[r, label] = own
+    return x.to(dtype), w.to(dtype), torch.full((len(SURE),), label)
+
+
+def sure_rows64(x, w, labels):
+    """Losses and G in 64 bits, and their errors relative to their size: the exponent of what the others have beside the label is off by u of itself for the difference, as much for its scaling and as
+    much for m, the sum has 64 terms and three joins, exp, log1p and expm1 add a few units (in all 2 |difference| + 80 u); an lse is rounded by u of itself, and so are differences to it."""
+    z = x.double() @ w.double().t()
+    at = torch.arange(x.shape[0])
+    own = z[at, labels]
+    d = z - own[:, None]
+    d[at, labels] = -math.inf
+    loss = torch.log1p(torch.exp(d).sum(1))
+    G = torch.exp(z - (own + loss)[:, None])
+    G[at, labels] = torch.expm1(-loss)
+    far = d.amax(1).abs()
+    rel = ref.U * (2 * far + 80)
+    each = ref.U * (2 * (own + loss).abs()[:, None] + 2 * (z - (own + loss)[:, None]).abs() + 16)
+    each[at, labels] = rel
+    return loss, rel * loss, G, each * G.abs()
+
+
+@pytest.mark.parametrize("dim,dtype", [(64, F32), (64, BF16), (80, F16), (128, F32), (128, BF16), (136, F32), (136, BF16), (200, F16)])
+@pytest.mark.parametrize("label", [50, 3])
+def test_cross_entropy_of_sure_rows(loss_lib, dim, dtype, label):
+    """Row by row: losses and gradients of rows that are nearly sure of their label keep their relative precision, however small they are, in a late step of the classes too."""
+    from paper_2507_14668_amd import binding
+    x, w, labels = sure_rows(dim, dtype, label)
+    rows, classes = x.shape[0], w.shape[0]
+    loss64, eloss, G, eG = sure_rows64(x, w, labels)
+    eps = torch.finfo(dtype).eps / 2
+    if dtype != F32:  # G to 16 bits (fp16: smallest steps of 2^-37), and the result
+        eG = eG + 2.01 * eps * G.abs() + (2.0 ** -37 if dtype == F16 else 2.0 ** -133)
+    loss, stats, dx, dw, db = torch.empty(rows), torch.empty(rows, 2), torch.empty_like(x), torch.empty_like(w), torch.empty(classes, dtype=dtype)
+    grad = torch.ones(rows)
+    for r in [None, 4, 8]:  # all of them; one row alone, whose gradient dbias then is
+        if r is not None:
+            labels = torch.full_like(labels, -100)
+            labels[r] = label
+        op = binding.CLoss(DT[dtype], 0, rows, dim, classes, -100)
+        ws = Guarded((1, max(loss_lib.tt_cross_entropy_workspace_bytes(ctypes.byref(op), i) for i in (0, 1))), torch.uint8)
+        call = (ctypes.byref(op), x.data_ptr(), w.data_ptr(), None, labels.data_ptr())
+        assert loss_lib.tt_cross_entropy_forward(*call, loss.data_ptr(), stats.data_ptr(), ws.ptr, ws.cols, None) == 0
+        assert loss_lib.tt_cross_entropy_backward(*call, stats.data_ptr(), grad.data_ptr(), dx.data_ptr(), dw.data_ptr(), db.data_ptr(), ws.ptr, ws.cols, None) == 0
+        if r is None:
+            ref.check(loss, loss64, eloss, "loss")
+            want = torch.cat([G, torch.zeros(rows, dim - classes)], 1)  # (W is the unit matrix)
+            ref.check(dx, want, torch.cat([eG, torch.zeros(rows, dim - classes)], 1) + ref.rounding(want, dtype), "dx")
+        else:
+            ref.check(db, G[r], eG[r] + ref.rounding(G[r], dtype), "dbias")
+
+
 def test_cross_entropy_refusals(lib):
     from paper_2507_14668_amd import binding
     x, w, b, lab, loss, lse = torch.zeros(4, 8), torch.zeros(10, 8), torch.zeros(10), torch.zeros(4, dtype=torch.int64), torch.zeros(4), torch.zeros(4, 2)

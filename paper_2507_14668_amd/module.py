@@ -263,13 +263,14 @@ class Routes(NamedTuple):
 
 
 class _RouteFunction(torch.autograd.Function):
-    """The weights that the library has formed, with the logits' gradient behind them."""
+    """The weights that the library has formed, with the logits' gradient behind them.  (They come in a tuple: as an argument of their own they
+    could only be given back as a view, which nobody may change in place.)"""
 
     @staticmethod
-    def forward(ctx, logits, weights, experts, how):
+    def forward(ctx, logits, formed, experts, how):
         ctx.how = how
         ctx.save_for_backward(logits, experts)
-        return weights.view_as(weights)
+        return formed[0]
 
     @staticmethod
     @_once
@@ -285,7 +286,7 @@ def tt_route(logits, k: int, bias=None, scores: str = "softmax", groups: int = 1
     bias = None if bias is None else _packed(bias.detach())
     weights, *rest = binding.tt_route_order(logits, k, bias, scores, groups, top_groups, renormalize, scale)
     if _trained(logits) or _dual():
-        weights = _RouteFunction.apply(logits, weights, rest[0], (scores, renormalize, scale))
+        weights = _RouteFunction.apply(logits, (weights,), rest[0], (scores, renormalize, scale))
     return Routes(weights, *rest)
 
 

@@ -149,6 +149,18 @@ def test_strided_inputs_expanded_gradients_and_second_derivatives(tt, name):
         g.sum().backward()
 
 
+@pytest.mark.parametrize("name", ["norm", "route", "rows", "combine", "loss"])
+def test_outputs_can_be_changed_in_place(tt, name):
+    f, x = calls(tt)[name], torch.randn(3, 6)
+    want, leaf = 2 * f(x), x.clone().requires_grad_()
+    got = f(x).mul_(2)
+    assert torch.equal(got, want)
+    got = f(leaf).mul_(2)
+    assert torch.equal(got, want)
+    (a,), (b,) = torch.autograd.grad(got.sum(), leaf), torch.autograd.grad(f(leaf).sum() * 2, leaf)
+    assert torch.allclose(a, b)
+
+
 def test_route_gives_its_bias_no_gradient(tt):
     z, bias = torch.randn(5, 6, requires_grad=True), torch.zeros(6, requires_grad=True)
     r = tt.tt_route(z, 2, bias=bias)

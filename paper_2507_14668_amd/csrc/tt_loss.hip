@@ -81,7 +81,7 @@ __global__ void __launch_bounds__(SCAN) k_loss_rows(const int64_t *labels, long 
     back = __uint_as_float((unsigned)(e - 13) << 23);
   }
   const float raised = half ? TT_LOSS_RAISE : 1.f;  // (a bf16 G has the range, and its sums need theirs: of rows near 1e38 they would overflow)
-  if (apart && !own) back = all / raised;
+  if (apart && !own) back = places > 0 ? all / raised : 0.f;
   if (threadIdx.x == 0) w.back[0] = back;
 #pragma unroll 4
   for (int i = threadIdx.x; i < places; i += SCAN) {
@@ -227,9 +227,9 @@ template <class T> __global__ void __launch_bounds__(TT_BLOCK) k_loss_dx(const f
 #pragma unroll
         for (int i = 0; i < 4; ++i) v[i] += t[i];
       }
-    }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] *= back;
+      for (int i = 0; i < 4; ++i) v[i] *= back;  // (which may be infinite: not times the zeros of the others)
+    }
     store4(dx + r * ld + c, dim - c, v);
   }
 }

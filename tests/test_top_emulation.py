@@ -741,6 +741,31 @@ def test_cross_entropy_of_sure_rows(loss_lib, dim, dtype, label):
             ref.check(db, G[r], eG[r] + ref.rounding(G[r], dtype), "dbias")
 
 
+@pytest.mark.parametrize("dim", [64, 128, 136, 200])
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("reduction", ["none", "sum", "mean"])
+@pytest.mark.parametrize("share", [math.inf, -math.inf, math.nan])
+def test_cross_entropy_of_rows_that_do_not_count_under_any_gradient(lib, dim, dtype, reduction, share):
+    """A loss scaler's overflow: rows that do not count have gradients of zero all the same, and so have the classes if no row counts."""
+    from paper_2507_14668_amd import binding
+    gen = torch.Generator().manual_seed(dim)
+    x, w = randn(gen, 9, dim, dtype=dtype), randn(gen, 70, dim, std=dim ** -0.5, dtype=dtype)
+    for some in (True, False):
+        labels = torch.randint(0, 70, (9,), generator=gen)
+        labels[[1, 4, 8]] = -100
+        if not some:
+            labels[:] = -100
+        op = binding.CLoss(DT[dtype], binding.REDUCTIONS[reduction], 9, dim, 70, -100)
+        ws = Guarded((1, max(lib.tt_cross_entropy_workspace_bytes(ctypes.byref(op), i) for i in (0, 1))), torch.uint8)
+        loss, stats, dx, dw, db = torch.empty(9), torch.empty(9, 2), torch.empty_like(x), torch.empty_like(w), torch.empty(70, dtype=dtype)
+        grad = torch.full((9,), share)
+        call = (ctypes.byref(op), x.data_ptr(), w.data_ptr(), None, labels.data_ptr())
+        assert lib.tt_cross_entropy_forward(*call, loss.data_ptr(), stats.data_ptr(), ws.ptr, ws.cols, None) == 0
+        assert lib.tt_cross_entropy_backward(*call, stats.data_ptr(), grad.data_ptr(), dx.data_ptr(), dw.data_ptr(), db.data_ptr(), ws.ptr, ws.cols, None) == 0
+        assert not dx[labels == -100].any() and (not some or not dx[labels != -100].isfinite().any())
+        assert some or not dw.any() and not db.any()
+
+
 def test_cross_entropy_refusals(lib):
     from paper_2507_14668_amd import binding
     x, w, b, lab, loss, lse = torch.zeros(4, 8), torch.zeros(10, 8), torch.zeros(10), torch.zeros(4, dtype=torch.int64), torch.zeros(4), torch.zeros(4, 2)

@@ -534,7 +534,8 @@ tt_status tt_core_ortho_update(const tt_table *table, const float *const dcore[3
  * weight and bias [dim] may be NULL (one and zero).  Backward, with h = grad weight and x^ = (x - mean) rstd:
  *   dx = rstd (h - mean(h) - x^ mean(h x^)),  dweight = sum over rows of grad x^,  dbias = sum of grad
  * A row of equal values gives the bias if eps > 0 (without eps it has no answer: NaN or the bias); infinities and
- * NaN stay in their row of out and dx.
+ * NaN stay in their row of out and dx.  Any finite numbers will do: a row whose sum or squares leave the range of fp32 is taken
+ * times a power of two.  What has to be a float is rstd (below 2^-126, of deviations beyond 2^126, it has fewer bits in the gradients).
  *   stats      DEVICE float[rows][2]: mean and rstd, written by the forward (may be NULL), read by the backward
  *   workspace  DEVICE, 256-byte aligned, tt_layer_norm_workspace_bytes(op) bytes; only for dweight and dbias
  */

@@ -72,6 +72,23 @@ template <int LANES> __device__ __forceinline__ void row_sum(float &a, float &b,
     }
   }
 }
+// The largest of v over them; NaN does not count.
+template <int LANES> __device__ __forceinline__ float row_largest(float v, float *room, int &turn) {
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int o = (LANES < 64 ? LANES : 64) / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl(v, lane ^ o, 64));
+  if constexpr (LANES > 64) {
+    float *half = room + turn * 16;
+    turn ^= 1;
+    if (lane == 0) half[threadIdx.x >> 6] = v;
+    __syncthreads();
+    const int first = (int)(threadIdx.x / LANES) * (LANES / 64);
+    v = half[first];
+#pragma unroll
+    for (int w = 1; w < LANES / 64; ++w) v = fmaxf(v, half[first + w]);
+  }
+  return v;
+}
 template <int LANES> constexpr int threads_of() { return LANES > 256 ? LANES : 256; }
 
 // The mean of a row's sum is off by the rounding of that sum, in the size of its elements, which may be far above their spread: it is mended by the mean `off` of
@@ -80,6 +97,28 @@ __device__ __forceinline__ float variance_of(float squares, float off) {
   const float v = fmaf(-off, off, squares);
   return v < 0.f ? 0.f : v;
 }
+// Whether a row's sums have left fp32's range, or its squares are so small that they lose bits that eps does not cover: the row is then taken again, times the power of two
+// that makes its largest number (or the root of eps) about one.
+__device__ __forceinline__ bool out_of_range(float variance, float eps) { return !(variance < 0x1p100f) || variance + eps < 0x1p-100f; }
+__device__ __forceinline__ float scale_for(float largest, float eps) {
+  const int e = (int)(__float_as_uint(fmaxf(largest, sqrtf(eps))) >> 23);  // of 1 127
+  return __uint_as_float((unsigned)(254 - (e < 1 ? 1 : e > 253 ? 253 : e)) << 23);
+}
+// Large numbers that lie close together: the row as it is, whose deviations may be what eps is.
+__device__ __forceinline__ void rescale(float &mean, float &rstd, float &scale, float variance, float eps) {
+  if (!(scale < 1.f)) return;
+  const float whole = variance / scale / scale + eps;
+  if (!(whole < 0x1p100f)) return;
+  mean /= scale;
+  rstd = 1.f / sqrtf(whole);
+  scale = 1.f;
+}
+// Of a row with deviations near the largest numbers, (x - mean) rstd with both halved twice: the difference may be twice as large as those.
+struct Center {
+  float q, mean, rstd;
+  __device__ __forceinline__ Center(float m, float r) : q(r < 0x1p-100f ? 0.25f : 1.f), mean(q * m), rstd(r / q) {}
+  __device__ __forceinline__ float of(float x) const { return fmaf(x, q, -mean) * rstd; }
+};
 // A row stays in the registers of LANES threads, NV pieces each: it is read once, and the variance is the mean of the squares of
 // what is left after the mean.  weight and bias stay in registers over a workgroup's rows.  Bound by memory: 106496 rows of 128 in fp32 18.2 us
 // (6.0 TB/s), 16384 of 4096 in bf16 50 (5.4), a large copy 5.1.
@@ -101,41 +140,55 @@ template <class T, int LANES, int NV> __global__ void __launch_bounds__(threads_
   for (long long r0 = (long long)blockIdx.x * GROUPS; r0 < p.rows; r0 += (long long)gridDim.x * GROUPS) {
     const bool live = r0 + group < p.rows;
     const long long r = live ? r0 + group : p.rows - 1;
-    float sum = 0.f, squares = 0.f, none = 0.f;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = (i * LANES + lane) * C;
       x[i].load((const T *)p.x + r * p.ld_x + c, p.n - c);
     }
+    float scale = 1.f, mean, rstd, variance;  // of the row times scale
+    for (int pass = 0;; ++pass) {
+      float sum = 0.f, squares = 0.f, none = 0.f, off = 0.f;
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
+      for (int i = 0; i < NV; ++i)
 #pragma unroll
-      for (int e = 0; e < C; ++e) sum += x[i].at(e);
-    row_sum<LANES>(sum, none, room, turn);
-    const float about = sum * inv;
-    float off = 0.f;
+        for (int e = 0; e < C; ++e) sum = fmaf(x[i].at(e), scale, sum);
+      row_sum<LANES>(sum, none, room, turn);
+      const float about = sum * inv;
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
+      for (int i = 0; i < NV; ++i)
 #pragma unroll
-      for (int e = 0; e < C; ++e) {
-        const float d = (i * LANES + lane) * C + e < p.n ? x[i].at(e) - about : 0.f;
-        squares = fmaf(d, d, squares);
-        off += d;
-      }
-    row_sum<LANES>(squares, off, room, turn);
-    off *= inv;
-    const float mean = about + off, rstd = 1.f / sqrtf(variance_of(squares * inv, off) + p.eps);
+        for (int e = 0; e < C; ++e) {
+          const float d = (i * LANES + lane) * C + e < p.n ? fmaf(x[i].at(e), scale, -about) : 0.f;
+          squares = fmaf(d, d, squares);
+          off += d;
+        }
+      row_sum<LANES>(squares, off, room, turn);
+      off *= inv;
+      variance = variance_of(squares * inv, off);
+      mean = about + off;
+      rstd = 1.f / sqrtf(variance + p.eps * scale * scale);
+      const bool again = pass == 0 && out_of_range(variance, p.eps);
+      if (!__ballot(again)) break;  // (the wavefront's other rows do the same once more)
+      float largest = 0.f;
+#pragma unroll
+      for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int e = 0; e < C; ++e) largest = fmaxf(largest, fabsf(x[i].at(e)));
+      largest = row_largest<LANES>(largest, room, turn);
+      if (again) scale = scale_for(largest, p.eps);
+    }
+    rescale(mean, rstd, scale, variance, p.eps);
     if (!live) continue;
     if (p.stats && lane == 0) {
-      p.stats[2 * r] = mean;
-      p.stats[2 * r + 1] = rstd;
+      p.stats[2 * r] = mean / scale;
+      p.stats[2 * r + 1] = rstd * scale;
     }
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = (i * LANES + lane) * C;
       float y[C];
 #pragma unroll
-      for (int e = 0; e < C; ++e) y[e] = fmaf((x[i].at(e) - mean) * rstd, w[i].at(e), b[i].at(e));
+      for (int e = 0; e < C; ++e) y[e] = fmaf(fmaf(x[i].at(e), scale, -mean) * rstd, w[i].at(e), b[i].at(e));
       if (c < p.n) store_n<T, C>((T *)p.out + r * p.ld_out + c, p.n - c, y);
     }
   }
@@ -161,7 +214,8 @@ template <class T, int LANES, int NV> __global__ void __launch_bounds__(threads_
   for (long long r0 = (long long)blockIdx.x * GROUPS; r0 < p.rows; r0 += (long long)gridDim.x * GROUPS) {
     const bool live = r0 + group < p.rows;
     const long long r = live ? r0 + group : p.rows - 1;
-    const float mean = p.stats[2 * r], rstd = p.stats[2 * r + 1];
+    const float rstd = p.stats[2 * r + 1];
+    const Center center(p.stats[2 * r], rstd);
     float s = 0.f, sx = 0.f;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
@@ -174,7 +228,7 @@ template <class T, int LANES, int NV> __global__ void __launch_bounds__(threads_
 #pragma unroll
       for (int e = 0; e < C; ++e) {
         const bool in = live && (i * LANES + lane) * C + e < p.n;
-        const float ge = g[i].at(e), xh = (x[i].at(e) - mean) * rstd, h = ge * w[i].at(e);
+        const float ge = g[i].at(e), xh = center.of(x[i].at(e)), h = ge * w[i].at(e);
         s += in ? h : 0.f;
         sx += in ? h * xh : 0.f;
         dw[i][e] += in ? ge * xh : 0.f;
@@ -190,7 +244,7 @@ template <class T, int LANES, int NV> __global__ void __launch_bounds__(threads_
       const int c = (i * LANES + lane) * C;
       float d[C];
 #pragma unroll
-      for (int e = 0; e < C; ++e) d[e] = rstd * (g[i].at(e) * w[i].at(e) - s - (x[i].at(e) - mean) * rstd * sx);
+      for (int e = 0; e < C; ++e) d[e] = rstd * (g[i].at(e) * w[i].at(e) - s - center.of(x[i].at(e)) * sx);
       if (c < p.n) store_n<T, C>((T *)p.out + r * p.ld_out + c, p.n - c, d);
     }
   }
@@ -229,32 +283,42 @@ template <class T> __global__ void __launch_bounds__(WIDE) k_norm_forward_wide(N
   const float inv = 1.f / (float)p.n;
   for (long long r = blockIdx.x; r < p.rows; r += gridDim.x) {
     const T *x = (const T *)p.x + r * p.ld_x;
-    float sum = 0.f, squares = 0.f, none = 0.f;
-    for (int c = threadIdx.x * C; c < p.n; c += WIDE * C) {
-      float v[C];
-      load_n<T, C>(x + c, p.n - c, v);
+    float scale = 1.f, mean, rstd, variance;  // as above
+    for (int pass = 0;; ++pass) {
+      float sum = 0.f, squares = 0.f, none = 0.f, off = 0.f, largest = 0.f;
+      for (int c = threadIdx.x * C; c < p.n; c += WIDE * C) {
+        float v[C];
+        load_n<T, C>(x + c, p.n - c, v);
 #pragma unroll
-      for (int e = 0; e < C; ++e) sum += v[e];
-    }
-    row_sum<WIDE>(sum, none, room, turn);
-    const float about = sum * inv;
-    float off = 0.f;
-    for (int c = threadIdx.x * C; c < p.n; c += WIDE * C) {
-      float v[C];
-      load_n<T, C>(x + c, p.n - c, v);
-#pragma unroll
-      for (int e = 0; e < C; ++e) {
-        const float d = c + e < p.n ? v[e] - about : 0.f;
-        squares = fmaf(d, d, squares);
-        off += d;
+        for (int e = 0; e < C; ++e) {
+          sum = fmaf(v[e], scale, sum);
+          largest = fmaxf(largest, fabsf(v[e]));
+        }
       }
+      row_sum<WIDE>(sum, none, room, turn);
+      const float about = sum * inv;
+      for (int c = threadIdx.x * C; c < p.n; c += WIDE * C) {
+        float v[C];
+        load_n<T, C>(x + c, p.n - c, v);
+#pragma unroll
+        for (int e = 0; e < C; ++e) {
+          const float d = c + e < p.n ? fmaf(v[e], scale, -about) : 0.f;
+          squares = fmaf(d, d, squares);
+          off += d;
+        }
+      }
+      row_sum<WIDE>(squares, off, room, turn);
+      off *= inv;
+      variance = variance_of(squares * inv, off);
+      mean = about + off;
+      rstd = 1.f / sqrtf(variance + p.eps * scale * scale);
+      if (pass != 0 || !out_of_range(variance, p.eps)) break;
+      scale = scale_for(row_largest<WIDE>(largest, room, turn), p.eps);
     }
-    row_sum<WIDE>(squares, off, room, turn);
-    off *= inv;
-    const float mean = about + off, rstd = 1.f / sqrtf(variance_of(squares * inv, off) + p.eps);
+    rescale(mean, rstd, scale, variance, p.eps);
     if (p.stats && threadIdx.x == 0) {
-      p.stats[2 * r] = mean;
-      p.stats[2 * r + 1] = rstd;
+      p.stats[2 * r] = mean / scale;
+      p.stats[2 * r + 1] = rstd * scale;
     }
     for (int c = threadIdx.x * C; c < p.n; c += WIDE * C) {
       float v[C], w[C], b[C];
@@ -262,7 +326,7 @@ template <class T> __global__ void __launch_bounds__(WIDE) k_norm_forward_wide(N
       if (p.weight) load_n<T, C>((const T *)p.weight + c, p.n - c, w);
       if (p.bias) load_n<T, C>((const T *)p.bias + c, p.n - c, b);
 #pragma unroll
-      for (int e = 0; e < C; ++e) v[e] = fmaf((v[e] - mean) * rstd, p.weight ? w[e] : 1.f, p.bias ? b[e] : 0.f);
+      for (int e = 0; e < C; ++e) v[e] = fmaf(fmaf(v[e], scale, -mean) * rstd, p.weight ? w[e] : 1.f, p.bias ? b[e] : 0.f);
       store_n<T, C>((T *)p.out + r * p.ld_out + c, p.n - c, v);
     }
   }
@@ -274,7 +338,8 @@ template <class T> __global__ void __launch_bounds__(WIDE) k_norm_backward_wide(
   const float inv = 1.f / (float)p.n;
   for (long long r = blockIdx.x; r < p.rows; r += gridDim.x) {
     const T *x = (const T *)p.x + r * p.ld_x, *g = (const T *)p.grad + r * p.ld_grad;
-    const float mean = p.stats[2 * r], rstd = p.stats[2 * r + 1];
+    const float rstd = p.stats[2 * r + 1];
+    const Center center(p.stats[2 * r], rstd);
     float s = 0.f, sx = 0.f;
     for (int pass = 0; pass < 2; ++pass) {
       for (int c = threadIdx.x * C; c < p.n; c += WIDE * C) {
@@ -284,7 +349,7 @@ template <class T> __global__ void __launch_bounds__(WIDE) k_norm_backward_wide(
         if (p.weight) load_n<T, C>((const T *)p.weight + c, p.n - c, w);
 #pragma unroll
         for (int e = 0; e < C; ++e) {
-          v[e] = (v[e] - mean) * rstd;
+          v[e] = center.of(v[e]);
           h[e] *= p.weight ? w[e] : 1.f;
           if (pass == 0) {
             s += c + e < p.n ? h[e] : 0.f;
@@ -310,13 +375,13 @@ template <class T> __global__ void __launch_bounds__(TT_BLOCK) k_norm_columns_wi
   if (c >= p.n) return;
   float dw[C] = {}, db[C] = {};
   for (long long r = blockIdx.y; r < p.rows; r += gridDim.y) {
-    const float mean = p.stats[2 * r], rstd = p.stats[2 * r + 1];
+    const Center center(p.stats[2 * r], p.stats[2 * r + 1]);
     float v[C], g[C];
     load_n<T, C>((const T *)p.x + r * p.ld_x + c, p.n - c, v);
     load_n<T, C>((const T *)p.grad + r * p.ld_grad + c, p.n - c, g);
 #pragma unroll
     for (int e = 0; e < C; ++e) {
-      dw[e] += g[e] * ((v[e] - mean) * rstd);
+      dw[e] += g[e] * center.of(v[e]);
       db[e] += g[e];
     }
   }

@@ -6,7 +6,7 @@ import pytest
 import torch
 
 import top_ref as ref
-from test_top_emulation import FAR_ROUTES, LARGE, LOSSES, ROUTES, large_logits, large_logits64, routed, sure_rows, sure_rows64
+from test_top_emulation import FAR_ROUTES, LARGE, LOSSES, ROUTES, far_rows, large_logits, large_logits64, routed, stats_loss, sure_rows, sure_rows64
 
 pytestmark = pytest.mark.gpu
 F32, BF16, F16 = torch.float32, torch.bfloat16, torch.float16
@@ -62,6 +62,34 @@ def test_layer_norm(tt, rows, n, dtype, pad, shift):
     assert torch.equal(out[:, :n], y) and bool((out[:, n:] == 7).all())
     again = torch.autograd.grad(tt.tt_layer_norm(dx, dw, db), [dx, dw, db], put(g, pad, shift))
     assert all(torch.equal(p, q) for p, q in zip(grads, again))
+
+
+@pytest.mark.parametrize("n,dtype", [(2, F32), (8, F32), (100, F32), (40, BF16), (200, BF16), (300, F32), (1000, F32), (3000, F32), (5000, BF16), (6000, F32), (9000, F32), (17000, BF16)])
+def test_layer_norm_of_any_size(tt, n, dtype):
+    """The norm and its gradients of rows near either end of the range, each between ordinary rows, which have the bits that they have alone."""
+    gen = torch.Generator().manual_seed(n)
+    w, b, grad, plain = randn(gen, n, dtype=dtype), randn(gen, n, dtype=dtype), randn(gen, 3, n, dtype=dtype), randn(gen, 2, n, dtype=dtype)
+
+    def run(x, grad, eps):
+        leaves = [put(t).requires_grad_() for t in (x, w, b)]
+        y = tt.tt_layer_norm(*leaves, eps=eps)
+        return [t.detach().cpu() for t in (y, *torch.autograd.grad(y, leaves, put(grad)))]
+    for name, row, eps in far_rows(n, gen):
+        eps = float(torch.tensor(eps, dtype=F32))
+        x = torch.stack([plain[0], row.to(dtype), plain[1]])
+        out, dx, dw, _ = run(x, grad, eps)
+        want = ref.norm64(x, w, b, eps, grad)
+        ref.check(out, *want["out"], name + " out")
+        d = x.double() - x.double().mean(1, keepdim=True)
+        rstd = 1 / ((d * d).mean(1, keepdim=True) + eps).sqrt()
+        ref.check(dx, want["dx"][0], want["dx"][1] + stats_loss(want["dx"][0], rstd), name + " dx")
+        ref.check(dw, want["dweight"][0], want["dweight"][1] + stats_loss((grad.double() * d * rstd).abs().sum(0), rstd.min()), name + " dweight")
+        alone = run(x[:1], grad[:1], eps)
+        assert torch.equal(out[0], alone[0][0]) and torch.equal(dx[0], alone[1][0]), name
+    for value in (1e38, -3.3e38, 1e20, 1e-30):
+        for eps in (1e-5, 1e-20, 1e-38):
+            out, _, dw, _ = run(torch.full((2, n), value).to(dtype), grad[:2], eps)
+            assert torch.equal(out, b.expand(2, n)) and not dw.any(), (value, eps)
 
 
 def test_layer_norm_many_rows(tt):

@@ -122,6 +122,61 @@ def test_layer_norm_special_rows(lib):
     assert out[3].isnan().all() and out[2].isnan().any()
 
 
+def far_rows(n, gen):
+    """(name, row of n, eps): rows whose sums, squares or differences leave what fp32 holds, at either end."""
+    f = lambda size: torch.randn(n, generator=gen) * size
+    sign = torch.where(torch.arange(n) % 2 == 0, 1.0, -1.0)
+    one = torch.full((n,), -3e38)
+    one[0] = 3e38
+    return [("sum", 1e38 + f(1e36), 1e-5), ("squares", 1e20 * sign, 1e-5), ("ends", 3.3e38 * sign, 1e-5), ("one", one, 1e-5), ("random", f(1e30), 1e-5), ("large", f(3e37), 0.0),
+            ("small", 1e-25 * sign, 0.0), ("smaller", f(1e-30), 0.0), ("beside eps", f(1e-19), 1e-38), ("mixed", f(1.0) * 10.0 ** (60 * torch.rand(n, generator=gen) - 25), 1e-5),
+            ("near", 1e30 + f(1e24), 1e30), ("ordinary", f(1.0), 0.0)]
+
+
+def stats_loss(want, rstd):
+    """An rstd below 2^-126 has fewer bits in the statistics: off by up to 2^-150."""
+    return want.abs() * (2.0 ** -150 / rstd)
+
+
+@pytest.mark.parametrize("n,dtype", [(2, F32), (8, F32), (100, F32), (40, BF16), (200, BF16), (300, F32), (1000, F32), (3000, F32), (5000, BF16), (6000, F32), (9000, F32), (17000, BF16)])
+def test_layer_norm_of_any_size(lib, n, dtype):
+    """The norm and its gradients of rows near either end of the range, each between ordinary rows, which have the bits that they have alone."""
+    from paper_2507_14668_amd import binding
+    gen = torch.Generator().manual_seed(n)
+    w, b, grad, plain = randn(gen, n, dtype=dtype), randn(gen, n, dtype=dtype), randn(gen, 3, n, dtype=dtype), randn(gen, 2, n, dtype=dtype)
+
+    def run(x, grad, eps):
+        rows = x.shape[0]
+        out, dx, dw, db, stats = torch.empty_like(x), torch.empty_like(x), torch.empty_like(w), torch.empty_like(w), torch.empty(rows, 2)
+        op = binding.CNorm(DT[dtype], n, rows, eps=eps)
+        ws = Guarded((1, lib.tt_layer_norm_workspace_bytes(ctypes.byref(op))), torch.uint8)
+        assert lib.tt_layer_norm_forward(ctypes.byref(op), x.data_ptr(), w.data_ptr(), b.data_ptr(), out.data_ptr(), stats.data_ptr(), None) == 0
+        assert lib.tt_layer_norm_backward(ctypes.byref(op), x.data_ptr(), w.data_ptr(), stats.data_ptr(), grad.data_ptr(), dx.data_ptr(), dw.data_ptr(), db.data_ptr(), ws.ptr,
+                                          ws.cols, None) == 0
+        return out, dx, dw, stats
+    for name, row, eps in far_rows(n, gen):
+        eps = ctypes.c_float(eps).value
+        x = torch.stack([plain[0], row.to(dtype), plain[1]])
+        out, dx, dw, stats = run(x, grad, eps)
+        want = ref.norm64(x, w, b, eps, grad)
+        ref.check(out, *want["out"], name + " out")
+        d = x.double() - x.double().mean(1, keepdim=True)
+        rstd = 1 / ((d * d).mean(1, keepdim=True) + eps).sqrt()
+        ref.check(dx, want["dx"][0], want["dx"][1] + stats_loss(want["dx"][0], rstd), name + " dx")
+        ref.check(dw, want["dweight"][0], want["dweight"][1] + stats_loss((grad.double() * d * rstd).abs().sum(0), rstd.min()), name + " dweight")
+        alone = run(x[:1], grad[:1], eps)
+        assert torch.equal(out[0], alone[0][0]) and torch.equal(dx[0], alone[1][0]) and torch.equal(stats[0], alone[3][0]), name
+    for value in (1e38, -3.3e38, 1e20, 1e-30, 2.0 ** -149 if dtype == F32 else 2.0 ** -133):  # equal values: the bias, whatever eps
+        for eps in (1e-5, 1e-20, 1e-38):
+            x = torch.full((2, n), value).to(dtype)
+            out, dx, dw, _ = run(x, grad[:2], eps)
+            assert torch.equal(out, b.expand(2, n)) and not dw.any(), (value, eps)
+            h = grad[:2].double() * w.double()
+            want = (h - h.mean(1, keepdim=True)) * ctypes.c_float(eps).value ** -0.5
+            size = (h.abs() + h.abs().mean(1, keepdim=True)) * ctypes.c_float(eps).value ** -0.5
+            ref.check(dx, want, (64 + n // 256 + 12) * ref.U * size + ref.rounding(want, dtype), "dx %g" % value)
+
+
 def test_layer_norm_refusals(lib):
     from paper_2507_14668_amd import binding
     x, out, st, ws = torch.zeros(4, 8), torch.zeros(4, 8), torch.zeros(4, 2), torch.zeros(1 << 16, dtype=torch.uint8)

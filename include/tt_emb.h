@@ -534,7 +534,7 @@ tt_status tt_core_ortho_update(const tt_table *table, const float *const dcore[3
  * weight and bias [dim] may be NULL (one and zero).  Backward, with h = grad weight and x^ = (x - mean) rstd:
  *   dx = rstd (h - mean(h) - x^ mean(h x^)),  dweight = sum over rows of grad x^,  dbias = sum of grad
  * A row of equal values gives the bias if eps > 0 (without eps it has no answer: NaN or the bias); infinities and
- * NaN stay in their row of out and dx.  Any finite numbers will do: a row whose sum or squares leave the range of fp32 is taken
+ * NaN stay in their row of out and dx.  Any finite x will do: a row whose sum or squares leave the range of fp32 is taken
  * times a power of two.  What has to be a float is rstd (below 2^-126, of deviations beyond 2^126, it has fewer bits in the gradients).
  *   stats      DEVICE float[rows][2]: mean and rstd, written by the forward (may be NULL), read by the backward
  *   workspace  DEVICE, 256-byte aligned, tt_layer_norm_workspace_bytes(op) bytes; only for dweight and dbias
@@ -652,7 +652,10 @@ tt_status tt_expert_combine_backward(const tt_deal *op, const void *y, const int
  *   labels DEVICE int64[rows];  stats DEVICE float[rows][2]: the log of the sum and the loss of each row, 0 in rows that do not
  *   count; written by the forward (not NULL), read by the backward (which forms the label's softmax - 1 from the loss; the
  *   loss is of the other classes' share beside the label, so the relative precision of both lasts however sure a row is, and no loss is below zero)
- *   workspace DEVICE, 256-byte aligned, tt_cross_entropy_workspace_bytes(op, backward) (0 on invalid arguments)
+ *   workspace DEVICE, 256-byte aligned, tt_cross_entropy_workspace_bytes(op, backward) (0 on invalid arguments).  For rows of up
+ *   to 128 elements it grows with the classes: W's rows over again, padded to 64 or 128 elements of 2 bytes (fp32: 6), forward and backward
+ *   (500001 x 128 in fp32 384 MB; 16-bit rows of just these lengths are read where they are).  For longer ones: a piece of G, 128 MB or 256 classes of
+ *   all rows, x and its gradient's sums.
  */
 typedef enum { TT_REDUCE_NONE = 0, TT_REDUCE_SUM = 1, TT_REDUCE_MEAN = 2 } tt_reduce;
 #define TT_LOSS_MAX_CLASSES (1 << 30)

@@ -1163,7 +1163,8 @@ def _loss_op(x, w, labels, bias, ignore_index, reduction):
 
 
 def tt_cross_entropy_workspace_bytes(x, w, labels, bias=None, ignore_index=-100, reduction="mean", backward=False) -> int:
-    """Bytes of workspace the calls below take for these operands (they allocate it if none is given)."""
+    """Bytes of workspace the calls below take for these operands (they allocate it if none is given).  For rows of up to 128 elements it grows
+    with the classes: a copy of w whose rows are padded to 64 or 128 elements of 2 bytes (float32: 6)."""
     op = _loss_op(x, w, labels, bias, ignore_index, reduction)[0]
     return int(load_library().tt_cross_entropy_workspace_bytes(ctypes.byref(op), int(backward)))
 

@@ -22,8 +22,8 @@ using namespace ttg;
 // fp32 operands come in PARTS = 3 planes of bf16 (tt_split_bf16), P is split as it is formed, and six of the nine products count, as in the other fp32
 // products; what they redo with the fp32 instruction (numbers below 2^-100 in size, or near the range's end) has fewer bits here, or is NaN.
 // 512 registers of a SIMD's lane are two wavefronts of 256: 48 of the held operand (three tiles of 16), 96 of the sums, 24 of S.
-// Measured, 4096 rows (3686 count) of 128 in bf16 against 500001 classes: STATS 574 us, ROWS 797, CLASSES 835; with G stored in pieces and multiplied
-// from there the training pass took 7129, now 2257.  The matrix cores are busy 36, 50 and 49 % of it, as much again goes to the exponentials and what is around
+// Measured, 4096 rows (3686 count) of 128 in bf16 against 500001 classes: STATS 600 us, ROWS 803, CLASSES 844; with G stored in pieces and multiplied
+// from there the training pass took 7129, now 2300.  The matrix cores are busy 34, 50 and 47 % of it, as much again goes to the exponentials and what is around
 // them, and two wavefronts a SIMD do not hide the one behind the other; the clock falls to 2.2 GHz.  Four held tiles spill, a step of the
 // other half prefetched into registers does too, and loads through registers instead of straight into LDS took 742, 964 and 1052.
 constexpr int WAVES = 4, THREADS = 64 * WAVES, STEP = TT_LOSS_STEP;
@@ -91,7 +91,8 @@ __device__ __forceinline__ void wait_loads() {
 }
 
 // 16-byte pieces of an LDS row are spread so that sixteen neighbouring rows at one piece, and eight at two neighbouring pieces (the transposing
-// read), meet every bank once.
+// read), lie in banks of their own.  The hardware takes the lanes in another grouping: 44 % of the LDS cycles of STATS, which reads `frag` alone, and 31 % of those of the
+// other two are conflicts still.
 template <int KP> __device__ __forceinline__ int spread(int r) {
   if constexpr (KP == 128) return (r & 7) << 1 | (r >> 3 & 1);
   else return (r >> 1 & 3) << 1 | (r >> 3 & 1);  // (two rows of 128 bytes share the banks)

@@ -120,8 +120,8 @@ struct Center {
   __device__ __forceinline__ float of(float x) const { return fmaf(x, q, -mean) * rstd; }
 };
 // A row stays in the registers of LANES threads, NV pieces each: it is read once, and the variance is the mean of the squares of
-// what is left after the mean.  weight and bias stay in registers over a workgroup's rows.  Bound by memory: 106496 rows of 128 in fp32 18.2 us
-// (6.0 TB/s), 16384 of 4096 in bf16 50 (5.4), a large copy 5.1.
+// what is left after the mean.  weight and bias stay in registers over a workgroup's rows.  Bound by memory: 106496 rows of 128 in fp32 18.3 us
+// (6.0 TB/s), 16384 of 4096 in bf16 52 (5.2), a large copy 5.1.
 template <class T, int LANES, int NV> __global__ void __launch_bounds__(threads_of<LANES>()) k_norm_forward(Norm p) {
   constexpr int C = Piece<T>::C, GROUPS = threads_of<LANES>() / LANES;
   __shared__ float room[32];
@@ -195,7 +195,7 @@ template <class T, int LANES, int NV> __global__ void __launch_bounds__(threads_
 }
 
 // dx in one pass, and beside it the workgroup's share of dweight and dbias, summed over its rows in registers and written to
-// partial[workgroup][2][n].  512 workgroups: 27.6 us (5.9 TB/s) and 88 us (4.6) for the rows above, and 4 for the joining of their shares.
+// partial[workgroup][2][n].  512 workgroups: 27.9 us (5.9 TB/s) and 90 us (4.5) for the rows above, and 4 for the joining of their shares.
 template <class T, int LANES, int NV> __global__ void __launch_bounds__(threads_of<LANES>()) k_norm_backward(Norm p) {
   constexpr int C = Piece<T>::C, THREADS = threads_of<LANES>(), GROUPS = THREADS / LANES;
   __shared__ float room[32];

@@ -400,7 +400,8 @@ class _LossFunction(torch.autograd.Function):
 def tt_cross_entropy(x, w, labels, bias=None, ignore_index: int = -100, reduction: str = "mean"):
     """Softmax cross entropy of rows x [rows, dim] against the classes of w [classes, dim]: `logsumexp(x w^T + bias)` less the
     label's logit, float32, differentiable in x, w and bias.  The logits are not kept: the gradients form them again, a piece of
-    the classes at a time.  reduction "none" gives [rows], "sum" and "mean" one number (the mean over rows whose label is
+    the classes at a time.  (Each call takes workspace; for rows of up to 128 elements that holds w over again, padded to 64 or 128 elements a row,
+    float32 in 6 bytes each: `tt_cross_entropy_workspace_bytes`.)  reduction "none" gives [rows], "sum" and "mean" one number (the mean over rows whose label is
     not ignore_index, 0 if there are none)."""
     x, w, bias, labels = _row_major(x), _packed(w), _packed(bias), _packed(labels)
     if not _trained(x, w, bias) and not _dual():

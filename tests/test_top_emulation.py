@@ -154,7 +154,8 @@ def test_layer_norm_of_any_size(lib, n, dtype):
         assert lib.tt_layer_norm_backward(ctypes.byref(op), x.data_ptr(), w.data_ptr(), stats.data_ptr(), grad.data_ptr(), dx.data_ptr(), dw.data_ptr(), db.data_ptr(), ws.ptr,
                                           ws.cols, None) == 0
         return out, dx, dw, stats
-    for name, row, eps in far_rows(n, gen):
+    long = n > 4000  # (seconds a row here: some of them)
+    for name, row, eps in far_rows(n, gen)[::4 if long else 1]:
         eps = ctypes.c_float(eps).value
         x = torch.stack([plain[0], row.to(dtype), plain[1]])
         out, dx, dw, stats = run(x, grad, eps)
@@ -166,8 +167,8 @@ def test_layer_norm_of_any_size(lib, n, dtype):
         ref.check(dw, want["dweight"][0], want["dweight"][1] + stats_loss((grad.double() * d * rstd).abs().sum(0), rstd.min()), name + " dweight")
         alone = run(x[:1], grad[:1], eps)
         assert torch.equal(out[0], alone[0][0]) and torch.equal(dx[0], alone[1][0]) and torch.equal(stats[0], alone[3][0]), name
-    for value in (1e38, -3.3e38, 1e20, 1e-30, 2.0 ** -149 if dtype == F32 else 2.0 ** -133):  # equal values: the bias, whatever eps
-        for eps in (1e-5, 1e-20, 1e-38):
+    for value in (1e38, -3.3e38, 1e20, 1e-30, 2.0 ** -149 if dtype == F32 else 2.0 ** -133)[::4 if long else 1]:  # equal values: the bias, whatever eps
+        for eps in (1e-5,) if long else (1e-5, 1e-20, 1e-38):
             x = torch.full((2, n), value).to(dtype)
             out, dx, dw, _ = run(x, grad[:2], eps)
             assert torch.equal(out, b.expand(2, n)) and not dw.any(), (value, eps)

@@ -350,6 +350,37 @@ def test_cross_entropy_of_sure_rows(tt, dim, dtype):
     assert not dx[:, 64:].any()
 
 
+@pytest.mark.parametrize("reduction", ["none", "sum", "mean"])
+@pytest.mark.parametrize("dim,dtype", [(64, F32), (64, BF16), (100, BF16), (128, F32), (136, BF16), (200, F32)])
+def test_cross_entropy_of_large_operands(tt, dim, dtype, reduction):
+    """Rows, then classes, near the type's largest number, and logits of ordinary size: gradients that the type holds are not lost on the way."""
+    size, up, classes = 2.0 ** 125, 2.0 ** -125, 9
+    for first, second in ((size, up), (up, size)):
+        x, w = torch.zeros(3, dim), torch.zeros(classes, dim)
+        x[0, 1], x[1, 1], x[2, 20] = first, -first, first / 2
+        w[2, 1], w[3, 1], w[4, 20] = 2 * second, -second, second / 2
+        labels, grad = torch.tensor([2, 3, 4]), torch.ones(3) if reduction == "none" else torch.tensor(1.0)
+        x, w = x.to(dtype), w.to(dtype)
+        want = ref.loss64(x, w, labels, reduction=reduction, grad=grad)
+        leaves = [put(x).requires_grad_(), put(w).requires_grad_()]
+        loss = tt.tt_cross_entropy(*leaves, labels.cuda(), reduction=reduction)
+        check(loss, want["loss"], "loss")
+        small = 2.0 ** -100 if dtype == F32 else 0.0  # (short fp32 rows: numbers below 2^-100 may have fewer bits)
+        for got, name in zip(torch.autograd.grad(loss, leaves, grad.cuda()), ("dx", "dw")):
+            check(got, (want[name][0], want[name][1] + small), name)
+
+
+def test_routed_weights_changed_in_place(tt):
+    z = torch.randn(50, 8, device="cuda", requires_grad=True)
+    r = tt.tt_route(z, 2)
+    plain, g = r.weights.detach().clone(), torch.randn(50, 2, device="cuda")
+    (want,) = torch.autograd.grad(tt.tt_route(z, 2).weights, z, 2 * g)
+    r.weights.mul_(2)
+    assert torch.equal(r.weights, 2 * plain)
+    (got,) = torch.autograd.grad(r.weights, z, g)
+    assert torch.equal(got, want)
+
+
 def test_no_rows(tt):
     """An empty batch through all of them, with gradients."""
     m = tt.TTExperts(16, 24, 8, 2)
